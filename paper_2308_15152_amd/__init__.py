@@ -23,12 +23,14 @@ __all__ = [
     "sgemm_emu_launch_form", "sgemm_emu_acc_launch_form",
     "sgemm_emu_batched_acc", "sgemm_emu_scan",
     "householder_emu_batched", "householder_emu_batched_ex", "givens_emu_batched",
+    "rotary_emu", "rotary_emu_table", "delta_emu_forward_workspace", "delta_emu_forward",
+    "delta_emu_backward_workspace", "delta_emu_backward", "delta_emu_step",
     "sgemm_emu_split", "mfmae_num_elements", "mfmae_map", "mfmae_foreach", "mfmae_mma_probe",
     "sgemm_emu_strerror", "sgemm_emu_last_hip_error",
     "sgemm_emu_xcd_order", "sgemm_emu_tile_order", "sgemm_emu_block_order",
     "sgemm_emu_stream_probe", "sgemm_emu_mfma_probe",
     "HOUSEHOLDER_RULE", "HOUSEHOLDER_LDS", "SPLIT_SCALAR", "SPLIT_PAIR", "SPLIT_EIGHT",
-    "OP_N", "OP_T", "ROW_MAJOR", "COL_MAJOR",
+    "OP_N", "OP_T", "ROW_MAJOR", "COL_MAJOR", "F32", "BF16", "F16",
     "GIVENS_AUTO", "GIVENS_MAP", "GIVENS_EMBEDDED", "GIVENS_LDS",
     "Policy", "FLOW_AUTO", "FLOW_SPLIT", "FLOW_DIRECT", "FLOW_STAGED", "FLOW_REG",
     "TILE_AUTO", "TILE_64x64", "TILE_128x128", "TILE_256x128", "TILE_128x256",
@@ -48,6 +50,7 @@ OP_N, OP_T = 0, 1
 HOUSEHOLDER_RULE, HOUSEHOLDER_LDS = 0, 1
 SPLIT_SCALAR, SPLIT_PAIR, SPLIT_EIGHT = 0, 1, 2
 ROW_MAJOR, COL_MAJOR = 0, 1
+F32, BF16, F16 = 0, 1, 2
 
 # Every symbol declared in include/sgemm_emu.h.
 EXPORTED_SYMBOLS = (
@@ -55,6 +58,8 @@ EXPORTED_SYMBOLS = (
     "sgemm_emu_launch_form", "sgemm_emu_acc_launch_form",
     "sgemm_emu_batched_acc", "sgemm_emu_scan",
     "householder_emu_batched", "householder_emu_batched_ex", "givens_emu_batched",
+    "rotary_emu", "rotary_emu_table", "delta_emu_forward_workspace", "delta_emu_forward",
+    "delta_emu_backward_workspace", "delta_emu_backward", "delta_emu_step",
     "sgemm_emu_split", "mfmae_num_elements", "mfmae_map", "mfmae_foreach", "mfmae_mma_probe",
     "sgemm_emu_strerror", "sgemm_emu_last_hip_error",
     "sgemm_emu_xcd_order", "sgemm_emu_tile_order", "sgemm_emu_block_order",
@@ -134,6 +139,7 @@ def load():
     lib = ctypes.CDLL(path)
     i32, i64, P = _CheckedInt32, _CheckedInt64, ctypes.c_void_p
     ip = ctypes.POINTER(ctypes.c_int)
+    f64 = ctypes.c_double
     sig = {
         "sgemm_emu_batched": ([i32, i32, i32, P, i32, P, i32, P, i32, i32, Stride, P], i32),
         "sgemm_emu_batched_ex": ([i32, i32, i32, P, i32, P, i32, P, i32, i32, Stride,
@@ -155,6 +161,13 @@ def load():
                                        i32),
         "givens_emu_batched": ([i32, i32, i32, P, P, i64, P, i32, i64, i32, P, i32, i64, i32,
                                 i32, P], i32),
+        "rotary_emu": ([P, P], i32),
+        "rotary_emu_table": ([i32, i32, f64, f64, f64, f64, f64, f64, P, P, P], i32),
+        "delta_emu_forward_workspace": ([P], i64),
+        "delta_emu_forward": ([P, P], i32),
+        "delta_emu_backward_workspace": ([P], i64),
+        "delta_emu_backward": ([P, P], i32),
+        "delta_emu_step": ([P, P], i32),
         "sgemm_emu_split": ([i64, P, P, P, i32, P], i32),
         "mfmae_num_elements": ([i32, i32], i32),
         "mfmae_map": ([i32, i32, i32, i32, ip, ip], i32),
@@ -171,7 +184,7 @@ def load():
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
-        fn.restype = ctypes.c_int if res is i32 else res  # plain int results
+        fn.restype = {i32: ctypes.c_int, i64: ctypes.c_int64}.get(res, res)  # plain int results
     # The entry points called once per launch again, with plain C types: the
     # checked ones convert every argument in Python, 5 us a call.  Their
     # callers below check the ranges themselves.
@@ -700,3 +713,9 @@ def mfmae_mma_probe(shape: int, a_lanes, b_lanes, *, stream=None):
                                     _stream(stream))
     _check(rc, "mfmae_mma_probe")
     return d
+
+
+from .mixing import (  # noqa: E402  (uses the helpers above)
+    delta_emu_backward, delta_emu_backward_workspace, delta_emu_forward,
+    delta_emu_forward_workspace, delta_emu_step, rotary_emu, rotary_emu_table,
+)

@@ -5,6 +5,7 @@
 
 #include <initializer_list>
 
+#include "checks.h"
 #include "internal.h"
 #include "mfmae/frag.hpp"
 #include "sgemm_emu.h"
@@ -12,49 +13,22 @@
 #include "tiling.hpp"
 
 namespace {
-
 thread_local int g_last_hip_error = 0;
+}
 
-int hip_fail(hipError_t e) {
+int sgemm_emu::hip_fail(hipError_t e) {
     g_last_hip_error = (int)e;
     return SGEMM_EMU_ERR_HIP;
 }
 
-struct Extent {
-    uintptr_t lo, hi;  // [lo, hi) in bytes; empty if lo == hi
-    bool ok;           // false: the span runs past the end of the address space
-};
+namespace {
 
-// Bytes spanned by `items` row-major matrices of rows x cols with leading
-// dimension ld and item stride s (elements of `elem` bytes), starting at p.
-// All arguments are non-negative; the span is computed in 128 bits, so no
-// stride or leading dimension can wrap it.
-Extent extent(const void* p, int64_t items, int64_t rows, int64_t cols, int64_t ld, int64_t s,
-              int64_t elem = sizeof(float)) {
-    Extent e{(uintptr_t)p, (uintptr_t)p, true};
-    if (items <= 0 || rows <= 0 || cols <= 0) return e;
-    const __int128 last = (__int128)(items - 1) * s + (__int128)(rows - 1) * ld + cols;
-    const __int128 bytes = last * elem;
-    if (bytes > (__int128)(UINTPTR_MAX - e.lo)) {
-        e.ok = false;
-        return e;
-    }
-    e.hi = e.lo + (uintptr_t)bytes;
-    return e;
-}
-
-bool all_ok(std::initializer_list<Extent> es) {
-    for (const Extent& e : es)
-        if (!e.ok) return false;
-    return true;
-}
-
-bool overlap(Extent a, Extent b) {
-    if (a.lo == a.hi || b.lo == b.hi) return false;
-    return a.lo < b.hi && b.lo < a.hi;
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+using sgemm_emu::aligned16;
+using sgemm_emu::all_ok;
+using sgemm_emu::Extent;
+using sgemm_emu::extent;
+using sgemm_emu::hip_fail;
+using sgemm_emu::overlap;
 
 int pick_tile(int m, int n, int batch) {
     if (m <= 64 && n <= 64) return SGEMM_EMU_TILE_64x64;

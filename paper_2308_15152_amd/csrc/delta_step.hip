@@ -1,0 +1,176 @@
+// The gated delta rule token by token (its recurrent form):
+//   S <- e^g S + k u^T,  u = beta (v - e^g S^T k),  o = scale S^T q.
+//
+// The columns of S are independent, so a block owns kCols columns of one
+// head's state and holds them in registers across the tokens: thread (x, y) has
+// kVec columns from kVec x and the rows y, y + kRows, ... .  With S before the
+// token, S^T k and S^T q are both sums over the rows, taken together: o = scale (e^g
+// S^T q + u (k.q)), so a token costs one reduction over the block.
+//
+// Bound by memory at large batches: the state is read and written once for
+// all tokens of the call (8 bytes an element); q, k and v are small.  At small
+// batches the launch and the state's latency bound it, and narrow column
+// slices spread a head over more CUs.
+#include "mixing.hpp"
+
+namespace sgemm_emu {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxK = 128;
+
+// kVec columns a thread, kX threads along the columns.
+template <class T, int kVec, int kX>
+__global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
+                                                              int64_t first) {
+    constexpr int kCols = kVec * kX;
+    constexpr int kRows = kThreads / kX;       // threads along the rows
+    constexpr int kEach = kMaxK / kRows;       // rows of a thread
+    constexpr int kWaves = kThreads / 64;
+    typedef typename Pack<float, kVec>::type Vec;
+    __shared__ float sums[2][kWaves][2 * kCols + 1];
+    __shared__ float keys[2][2][kMaxK];
+
+    const int x = threadIdx.x % kX, y = threadIdx.x / kX;
+    const int wave = threadIdx.x >> 6;
+    const int slices = (p.v_size + kCols - 1) / kCols;
+    int64_t task = first + blockIdx.x;
+    const int slice = (int)(task % slices);
+    task /= slices;
+    const int h = (int)(task % p.v_heads), n = (int)(task / p.v_heads);
+    const int kh = h / (p.v_heads / p.k_heads);
+    const bool packed = p.cu_seqlens != nullptr;
+    const Span s = span_of(p.cu_seqlens, n, p.tokens);
+    const int col = slice * kCols + kVec * x;
+    const bool in = col < p.v_size;  // kVec divides v_size or is 1
+
+    const T* q = row_of<const T>(p.q, packed, n, s, kh);
+    const T* k = row_of<const T>(p.k, packed, n, s, kh);
+    const T* v = row_of<const T>(p.v, packed, n, s, h);
+    T* o = row_of<T>(p.o, packed, n, s, h);
+    const int slot = p.slots ? p.slots[n] : n;
+    if (slot < 0 || slot >= p.n_slots) {  // the whole block
+        if (in && y == 0)
+            for (int t = 0; t < s.count; ++t)
+                for (int i = 0; i < kVec; ++i) o[t * p.o.token + col + i] = from_f32<T>(0.0f);
+        return;
+    }
+    const int64_t at = slot * p.state_stride + (int64_t)h * p.k_size * p.v_size + col;
+    float S[kEach][kVec];
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) {
+        const int row = y + kRows * r;
+        Vec w{};
+        if (in && row < p.k_size && p.from)
+            w = *reinterpret_cast<const Vec*>(p.from + at + (int64_t)row * p.v_size);
+        __builtin_memcpy(S[r], &w, sizeof(Vec));
+    }
+    const float* g = p.g.p ? row_of<const float>(p.g, packed, n, s, h) : nullptr;
+    const float* beta = p.beta.p ? row_of<const float>(p.beta, packed, n, s, h) : nullptr;
+
+    for (int t = 0; t < s.count; ++t) {
+        const int buf = t & 1;
+        {
+            const int e = threadIdx.x % kMaxK;
+            const T* from = threadIdx.x < kMaxK ? k + t * p.k.token : q + t * p.q.token;
+            keys[buf][threadIdx.x / kMaxK][e] = e < p.k_size ? to_f32(from[e]) : 0.0f;
+        }
+        float vt[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) vt[i] = in ? to_f32(v[t * p.v.token + col + i]) : 0.0f;
+        const float decay = g ? expf(log_decay(g[t * p.g.token])) : 1.0f;
+        const float b = beta ? beta[t * p.beta.token] : 1.0f;
+        __syncthreads();
+        float kr[kEach], qr[kEach], sk[kVec] = {}, sq[kVec] = {}, kq = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kEach; ++r) {
+            kr[r] = keys[buf][0][y + kRows * r];
+            qr[r] = keys[buf][1][y + kRows * r];
+            kq = __builtin_fmaf(kr[r], qr[r], kq);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                sk[i] = __builtin_fmaf(S[r][i], kr[r], sk[i]);
+                sq[i] = __builtin_fmaf(S[r][i], qr[r], sq[i]);
+            }
+        }
+        // over the wave's rows, then over the waves
+#pragma unroll
+        for (int d = kX; d < 64; d *= 2) {
+            kq += __shfl_xor(kq, d, 64);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                sk[i] += __shfl_xor(sk[i], d, 64);
+                sq[i] += __shfl_xor(sq[i], d, 64);
+            }
+        }
+        if ((threadIdx.x & 63) < kX) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                sums[buf][wave][kVec * x + i] = sk[i];
+                sums[buf][wave][kCols + kVec * x + i] = sq[i];
+            }
+            if (x == 0) sums[buf][wave][2 * kCols] = kq;
+        }
+        __syncthreads();
+        float tk[kVec] = {}, tq[kVec] = {}, tkq = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            tkq += sums[buf][w][2 * kCols];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                tk[i] += sums[buf][w][kVec * x + i];
+                tq[i] += sums[buf][w][kCols + kVec * x + i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float u = b * __builtin_fmaf(-decay, tk[i], vt[i]);
+#pragma unroll
+            for (int r = 0; r < kEach; ++r) S[r][i] = __builtin_fmaf(kr[r], u, decay * S[r][i]);
+            tq[i] = p.scale * __builtin_fmaf(u, tkq, decay * tq[i]);
+        }
+        if (in && y == 0)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) o[t * p.o.token + col + i] = from_f32<T>(tq[i]);
+    }
+    if (p.to && in)
+#pragma unroll
+        for (int r = 0; r < kEach; ++r) {
+            const int row = y + kRows * r;
+            if (row < p.k_size) {
+                Vec w;
+                __builtin_memcpy(&w, S[r], sizeof(Vec));
+                *reinterpret_cast<Vec*>(p.to + at + (int64_t)row * p.v_size) = w;
+            }
+        }
+}
+
+template <class T, int kVec, int kX>
+hipError_t launch(const DeltaStep& a, hipStream_t stream) {
+    const int64_t slices = (a.v_size + kVec * kX - 1) / (kVec * kX);
+    const int64_t blocks = slices * a.v_heads * a.batch;
+    for (int64_t first = 0; first < blocks; first += kMostBlocks) {
+        const int64_t count = blocks - first < kMostBlocks ? blocks - first : kMostBlocks;
+        hipLaunchKernelGGL((delta_step_kernel<T, kVec, kX>), dim3((unsigned)count), dim3(kThreads),
+                           0, stream, a, first);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_delta_step(const DeltaStep& a, hipStream_t stream) {
+    if (a.batch == 0 || a.v_size == 0) return hipSuccess;
+    // 16-byte accesses of the state's rows; otherwise one column a thread
+    const bool wide = a.v_size % 4 == 0 && a.state_stride % 4 == 0 &&
+                      (uintptr_t)a.from % 16 == 0 && (uintptr_t)a.to % 16 == 0;
+    return by_dtype(a.dtype, [&](auto t) {
+        using T = decltype(t);
+        if (!wide) return launch<T, 1, 32>(a, stream);
+        return launch<T, 4, 8>(a, stream);
+    });
+}
+
+}  // namespace sgemm_emu

@@ -1,0 +1,139 @@
+"""The recurrent form against the recurrence in 64 bits.
+
+Tolerances.  Inputs are of order one and keys of length one, so states stay
+of the order of the first state and the values.  A token adds a few FP32
+roundings (2^-24 relative to a row sum over at most 128 rows) to a state whose
+errors the rule does not amplify: 2^-24 sqrt(128) (tokens + 2) of the largest
+magnitude covers them with room; outputs are rounded once more to their type."""
+import pytest
+import torch
+
+import paper_2308_15152_amd as emu
+from delta_plain import delta
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def inputs(b, t, hk, hv, ks, vs, dtype, seed=0, decay=1.0):
+    g = torch.Generator().manual_seed(seed)
+
+    def r(*shape):
+        return torch.randn(shape, generator=g)
+
+    q, k = (torch.nn.functional.normalize(r(b, t, hk, ks), dim=-1).to(dtype) for _ in range(2))
+    return (q, k, r(b, t, hv, vs).to(dtype), -decay * r(b, t, hv).abs(),
+            torch.sigmoid(r(b, t, hv)))
+
+
+def close(got, want, tokens, dtype=torch.float32):
+    got, want = got.cpu().double(), want.detach()
+    assert got.shape == want.shape
+    top = max(1.0, float(want.abs().max()) if want.numel() else 1.0)
+    tol = 2.0 ** -24 * 11.4 * (tokens + 2) * top
+    tol = tol + (UNIT[dtype] * want.abs() + 2.0 ** -25 if dtype != torch.float32 else 0.0)
+    bad = (got - want).abs() > tol
+    assert not bad.any(), (int(bad.sum()), float((got - want).abs().max()))
+
+
+def dev(*ts):
+    return [None if t is None else t.to(DEV) for t in ts]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("b,t,hk,hv,ks,vs", [
+    (1, 1, 1, 1, 1, 1), (2, 1, 2, 2, 128, 128), (3, 5, 1, 3, 96, 80), (2, 2, 2, 4, 33, 7),
+    (1, 9, 1, 2, 17, 130), (5, 1, 2, 6, 64, 256), (2, 3, 1, 1, 128, 36)])
+def test_tokens(dtype, b, t, hk, hv, ks, vs):
+    x = inputs(b, t, hk, hv, ks, vs, dtype, seed=b * 100 + ks)
+    first = torch.randn(b, hv, ks, vs)
+    want, last = delta(*x, first)
+    state = first.to(DEV)
+    o = emu.delta_emu_step(*dev(*x), state)
+    close(o, want, t, dtype)
+    close(state, last, t)
+
+
+def test_slots_of_a_pool_and_sequences_left_out():
+    b, t, hv, ks, vs = 5, 2, 3, 32, 24
+    x = inputs(b, t, 1, hv, ks, vs, torch.float32)
+    pool = torch.randn(9, hv, ks, vs)
+    slots = torch.tensor([7, -1, 0, 9, 3], dtype=torch.int32)
+    state = pool.to(DEV)
+    o = emu.delta_emu_step(*dev(*x), state, slots=slots.to(DEV)).cpu()
+    live = [0, 2, 4]
+    want, last = delta(*(y[live] for y in x), pool[slots[live].long()])
+    close(o[live], want, t)
+    assert not o[1].any() and not o[3].any()
+    expect = pool.double().clone()
+    expect[slots[live].long()] = last
+    close(state, expect, t)
+    untouched = [1, 2, 4, 5, 6, 8]
+    assert torch.equal(state.cpu()[untouched], pool[untouched])
+
+
+def test_without_decay_or_strength_and_a_padded_pool():
+    x = inputs(2, 3, 2, 2, 40, 24, torch.bfloat16)
+    first = torch.randn(2, 2, 40, 24)
+    want, last = delta(*x[:3], None, None, first, scale=0.5)
+    padded = torch.zeros(2, 3, 40, 24, device=DEV)
+    state = padded[:, :2]
+    state.copy_(first)
+    o = emu.delta_emu_step(*dev(*x[:3]), None, None, state, scale=0.5)
+    close(o, want, 3, torch.bfloat16)
+    close(state, last, 3)
+    assert not padded[:, 2].any()
+
+
+def test_extreme_decays():
+    """g = -infinity, the lowest value and -1000 empty the state; the token's
+    own write stays."""
+    x = list(inputs(1, 4, 1, 3, 16, 16, torch.float32))
+    x[3][0, 1, 0] = -torch.inf
+    x[3][0, 1, 1] = torch.finfo(torch.float32).min
+    x[3][0, 2, 2] = -1000.0
+    first = torch.randn(1, 3, 16, 16)
+    want, last = delta(*x, first)
+    state = first.to(DEV)
+    o = emu.delta_emu_step(*dev(*x), state)
+    close(o, want, 4)
+    close(state, last, 4)
+
+
+def test_strided_inputs_and_another_stream():
+    x = inputs(3, 2, 2, 4, 32, 32, torch.float16)
+    rows = torch.cat([y.flatten(2) for y in x[:3]], 2).to(DEV)
+    q, k, v = rows.split([64, 64, 128], 2)
+    first = torch.randn(3, 4, 32, 32)
+    want, last = delta(*x, first)
+    gates = torch.stack([x[3], x[4]], -1).to(DEV)
+    state = first.to(DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        o = emu.delta_emu_step(q.unflatten(2, (2, 32)), k.unflatten(2, (2, 32)),
+                               v.unflatten(2, (4, 32)), gates[..., 0], gates[..., 1], state)
+    side.synchronize()
+    close(o, want, 2, torch.float16)
+    close(state, last, 2)
+
+
+def test_graph_replays():
+    x = dev(*inputs(2, 1, 1, 2, 64, 64, torch.bfloat16))
+    first = torch.randn(2, 2, 64, 64, device=DEV)
+    state, out = first.clone(), torch.empty_like(x[2])
+    eager, outs = first.clone(), []
+    for _ in range(4):
+        outs.append(emu.delta_emu_step(*x, eager).clone())
+    emu.delta_emu_step(*x, state.clone(), out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        emu.delta_emu_step(*x, state, out=out)
+    state.copy_(first)
+    for i in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, outs[i]), i
+    assert torch.equal(state, eager)
