@@ -35,7 +35,7 @@ __all__ = [
     "Policy", "FLOW_AUTO", "FLOW_SPLIT", "FLOW_DIRECT", "FLOW_STAGED", "FLOW_REG",
     "TILE_AUTO", "TILE_64x64", "TILE_128x128", "TILE_256x128", "TILE_128x256",
     "SHAPE_16x16x32", "SHAPE_32x32x16", "USE_A", "USE_B", "USE_ACC",
-    "EXPORTED_SYMBOLS",
+    "EXPORTED_SYMBOLS", "MIXING_SYMBOLS",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -58,12 +58,15 @@ EXPORTED_SYMBOLS = (
     "sgemm_emu_launch_form", "sgemm_emu_acc_launch_form",
     "sgemm_emu_batched_acc", "sgemm_emu_scan",
     "householder_emu_batched", "householder_emu_batched_ex", "givens_emu_batched",
-    "rotary_emu", "rotary_emu_table", "delta_emu_forward_workspace", "delta_emu_forward",
-    "delta_emu_backward_workspace", "delta_emu_backward", "delta_emu_step",
     "sgemm_emu_split", "mfmae_num_elements", "mfmae_map", "mfmae_foreach", "mfmae_mma_probe",
     "sgemm_emu_strerror", "sgemm_emu_last_hip_error",
     "sgemm_emu_xcd_order", "sgemm_emu_tile_order", "sgemm_emu_block_order",
     "sgemm_emu_stream_probe", "sgemm_emu_mfma_probe",
+)
+# Every symbol declared in include/mixing_emu.h.
+MIXING_SYMBOLS = (
+    "rotary_emu", "rotary_emu_table", "delta_emu_forward_workspace", "delta_emu_forward",
+    "delta_emu_backward_workspace", "delta_emu_backward", "delta_emu_step",
 )
 
 

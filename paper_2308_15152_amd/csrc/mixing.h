@@ -6,7 +6,7 @@
 
 #include <hip/hip_runtime.h>
 
-#include "sgemm_emu.h"
+#include "mixing_emu.h"
 
 namespace sgemm_emu {
 

@@ -12,7 +12,7 @@ import struct
 
 import paper_2308_15152_amd as _pkg
 
-# The C argument structs of include/sgemm_emu.h.  A view is a pointer and the
+# The C argument structs of include/mixing_emu.h.  A view is a pointer and the
 # element strides of batch, token and head.
 _ROTARY = struct.Struct("=10i16q3q3q2i")
 _FORWARD = struct.Struct("=7if" + "q" + "24q" + "2q" + "2q")
