@@ -1,5 +1,18 @@
-// The gated delta rule over sequences: sizes, workspaces and launches.
+// The gated delta rule over sequences: the chunk form's workspace and launches.
+//
+// Tokens go in chunks of 64.  With G the running sum of g inside a chunk, E_ts =
+// e^{G_t - G_s} for s <= t and S the state before the chunk,
+//   A = diag(beta) strict_lower(E . K K^T),   T = (I + A)^-1,
+//   U = T diag(beta) (V - diag(e^G) K S),
+//   O = scale (diag(e^G) Q S + lower(E . Q K^T) U),
+//   S' = e^{G_64} S + K^T diag(e^{G_64 - G}) U.
+// T and P = scale lower(E . Q K^T) depend on one chunk only: a first kernel
+// makes them for all chunks at once (delta_prep.hip).  A second one walks the
+// chunks of every sequence in order, 16 columns of S to a wave
+// (delta_chain.hip).
 #pragma once
+
+#include <initializer_list>
 
 #include "mixing.h"
 
@@ -10,13 +23,74 @@ constexpr int kDeltaChunk = 64;  // tokens of a chunk
 // Chunks x value heads of one call: one block each, one launch.
 constexpr int64_t kDeltaMostTasks = 1 << 22;
 
-// Chunks that the sequences of a call can have.  Sequence n's chunks are
-// numbered from chunk_base(n); packed sequences leave at most one number
-// between them unused.
+// Chunks that the sequences of a call can have.  Packed sequences: sequence n's
+// are numbered from first row / 64 + n, which leaves at most one number
+// between two sequences unused.
 inline int64_t delta_chunks(int64_t batch, int64_t tokens, bool packed) {
     if (packed) return tokens / kDeltaChunk + batch;
     return batch * ((tokens + kDeltaChunk - 1) / kDeltaChunk);
 }
+
+// What the first kernel leaves for one chunk of one value head, in bytes.
+// Matrices are fp16 operand fragments of v_mfma_f32_16x16x32_f16 (1 KiB: 16
+// bytes a lane) of the six (16-row tile, 32-column step) pairs that a lower (or,
+// transposed, upper) triangular 64 x 64 matrix fills, hi fragments before
+// lo ones; rows are scaled by powers of two.
+struct DeltaRecord {
+    enum Factor {   // rows of 64 floats
+        kKeyScale,  // 2^a: a key row times it has its largest entry in [2^14, 2^15)
+        kQueryScale,
+        kRise,       // e^G / key scale
+        kBeta,       // beta
+        kTail,       // e^{G_64 - G} / key scale
+        kQueryRise,  // scale e^G / query scale
+        kT,          // inverse row scales of T, P, T^T, P^T
+        kP,
+        kTt,
+        kPt,
+        kDecay,  // [0]: e^{G_64}
+        kFactors
+    };
+    static constexpr int kMatrix = 6 * 1024;             // one part of one matrix
+    static constexpr int kFactorBytes = kFactors * 256;  // at the record's start
+    static constexpr int kAtT = kFactorBytes;            // two parts
+    static constexpr int kAtP = kAtT + 2 * kMatrix;      // two parts (one for bfloat16)
+    static constexpr int kForward = kAtP + 2 * kMatrix;
+    static constexpr int kAtTt = kAtP;  // the backward form has no P
+    static constexpr int kAtPt = kAtTt + 2 * kMatrix;
+    static constexpr int kBackward = kAtPt + 2 * kMatrix;
+};
+
+// Arguments of the chunk kernels.
+struct DeltaChunks {
+    int dtype, batch, tokens, k_heads, v_heads, k_size, v_size;
+    float scale;
+    const int* cu_seqlens;
+    sgemm_emu_view_t q, k, v, g, beta, o;
+    const float* initial;
+    float* final_state;
+    char* records;        // of chunk c, value head h: at (c v_heads + h) record_bytes
+    int64_t record_bytes;
+    int chunks;
+    bool backward;        // records of the backward form
+    // what the walk over the chunks keeps for the gradient, per chunk and
+    // value head: S before the chunk (k_size x v_size) and U (64 x v_size)
+    float* states;
+    float* updates;
+    bool wide;            // 16-byte loads of q's and k's rows
+};
+
+// Whether every row of q and k can be loaded 16 bytes at a time.
+template <class A>
+bool delta_wide(const A& a) {
+    const int64_t n = a.dtype == SGEMM_EMU_F32 ? 4 : 8;
+    for (const sgemm_emu_view_t* v : {&a.q, &a.k})
+        if ((uintptr_t)v->p % 16 || v->batch % n || v->token % n || v->head % n) return false;
+    return a.k_size % 8 == 0;
+}
+
+hipError_t launch_delta_prep(const DeltaChunks& a, hipStream_t stream);
+hipError_t launch_delta_chain(const DeltaChunks& a, hipStream_t stream);
 
 int64_t delta_forward_workspace(const delta_emu_forward_t& a);
 hipError_t launch_delta_forward(const delta_emu_forward_t& a, hipStream_t stream);

@@ -1,0 +1,309 @@
+// The gated delta rule, first kernel: for every chunk of 64 tokens of every
+// value head, the two triangular matrices of the chunk form,
+//   T = (I + A)^-1,  A_ts = beta_t e^{G_t - G_s} k_t.k_s (s < t),
+//   P_ts = scale e^{G_t - G_s} q_t.k_s (s <= t),
+// as operand fragments, and the row factors of the walk over the chunks.
+//
+// G is summed in FP64: decays of e^-200 and less (a reset) would leave FP32
+// sums too coarse for the differences after them.  The inverse starts from
+// the four 16 x 16 diagonal blocks (forward substitution, a column to a
+// lane) and joins them with FP32 matrix products, two sizes up:
+//   [A 0; C D]^-1 = [A^-1 0; -D^-1 C A^-1, D^-1].
+#include "delta_chunk.hpp"
+
+namespace sgemm_emu {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPitch = 68;  // floats of a row of the matrices in LDS
+
+// The 8 k-values of a lane as MFMA operand, in the type of the input or, for
+// FP32, split.
+template <class T>
+struct Operand;
+template <>
+struct Operand<bf16_t> {
+    typedef __bf16 vec __attribute__((ext_vector_type(8)));
+    vec v;
+    __device__ void set(const Eight<bf16_t>& x, float) { __builtin_memcpy(&v, &x, 16); }
+};
+template <>
+struct Operand<f16_t> {
+    half8_t v;
+    __device__ void set(const Eight<f16_t>& x, float) { __builtin_memcpy(&v, &x, 16); }
+};
+template <>
+struct Operand<float> {
+    Frag<2> v;
+    __device__ void set(const Eight<float>& x, float up) { v = split<2>(x.x, up); }
+};
+__device__ inline f32x4 product(const Operand<bf16_t>& a, const Operand<bf16_t>& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ inline f32x4 product(const Operand<f16_t>& a, const Operand<f16_t>& b, f32x4 c) {
+    return mfma(a.v, b.v, c);
+}
+__device__ inline f32x4 product(const Operand<float>& a, const Operand<float>& b, f32x4 c) {
+    return multiply(a.v, b.v, c);
+}
+
+// Row r of a 16 x 16 block of X (in LDS) as the A operand of the four
+// FP32 products of a 16 x 16 x 16 one: step i contracts columns 4 g + i.
+__device__ inline f32x4 block_rows(const float* X, int lane) {
+    return *reinterpret_cast<const f32x4*>(X + (lane & 15) * kPitch + 4 * (lane >> 4));
+}
+__device__ inline f32x4 block_columns(const float* X, int lane) {
+    f32x4 b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = X[(4 * (lane >> 4) + i) * kPitch + (lane & 15)];
+    return b;
+}
+__device__ inline f32x4 block_product(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+__device__ inline void block_store(float* X, int lane, f32x4 d) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) X[(4 * (lane >> 4) + i) * kPitch + (lane & 15)] = d[i];
+}
+
+// Fragments of tile `tile`'s rows of the matrix M (or its transpose), with the
+// rows' inverse scales.  Blocks on the empty side of the diagonal are zero
+// whatever M holds there.
+template <bool kTransposed, int kParts>
+__device__ inline void write_fragments(const float* M, int tile, int lane, char* to, float* inverse) {
+    const int row = lane & 15, g = lane >> 4;
+    float x[2][8], m = 0.0f;
+#pragma unroll
+    for (int step = 0; step < 2; ++step)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int other = 2 * step + half;
+            const bool full = kTransposed ? other >= tile : other <= tile;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int a = 16 * tile + row, b = 16 * other + 4 * g + i;
+                const float v = !full ? 0.0f : kTransposed ? M[b * kPitch + a] : M[a * kPitch + b];
+                x[step][4 * half + i] = v;
+                m = fmaxf(m, fabsf(v));
+            }
+        }
+    const Scale s = scale_of(max_groups(m));
+    if (g == 0) inverse[16 * tile + row] = s.down;
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+        if (kTransposed ? step < tile / 2 : step > tile / 2) continue;
+        const int at = kTransposed ? upper_at(tile, step) : lower_at(tile, step);
+        const Frag<kParts> f = split<kParts>(x[step], s.up);
+#pragma unroll
+        for (int p = 0; p < kParts; ++p)
+            *reinterpret_cast<half8_t*>(to + (p * 6 + at) * 1024 + lane * 16) = f.part[p];
+    }
+}
+
+template <class T, int kK, bool kBackward>
+__global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
+    constexpr int kSteps = kK / 32;
+    __shared__ __attribute__((aligned(16))) float A[kC * kPitch];
+    __shared__ __attribute__((aligned(16))) float P[kC * kPitch];
+    __shared__ double G[kC];
+    __shared__ float beta[kC];
+
+    const int h = blockIdx.x % p.v_heads, c = blockIdx.x / p.v_heads;
+    const Place at = place_of(p.cu_seqlens, c, p.batch, p.tokens);
+    if (at.count <= 0) return;  // the whole block
+    const bool packed = p.cu_seqlens != nullptr;
+    const int kh = h / (p.v_heads / p.k_heads);
+    char* record = p.records + ((int64_t)c * p.v_heads + h) * p.record_bytes;
+    float* factors = reinterpret_cast<float*>(record);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = lane & 15, g = lane >> 4;
+
+    if (wave == 0) {  // running sums of the decays, and the strengths
+        const bool in = lane < at.count;
+        const int t = at.first + lane;
+        double sum = 0.0;
+        float b = in ? 1.0f : 0.0f;
+        if (in && p.g.p)
+            sum = log_decay(row_of<const float>(p.g, packed, at.n, at.span, h)[t * p.g.token]);
+        if (in && p.beta.p)
+            b = row_of<const float>(p.beta, packed, at.n, at.span, h)[t * p.beta.token];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const double u = __shfl_up(sum, d, 64);
+            if (lane >= d) sum += u;
+        }
+        G[lane] = sum;
+        beta[lane] = b;
+    }
+
+    // k's four row tiles and this wave's tile of q, in operand order
+    const T* k = row_of<const T>(p.k, packed, at.n, at.span, kh) + (int64_t)at.first * p.k.token;
+    const T* q = row_of<const T>(p.q, packed, at.n, at.span, kh) + (int64_t)at.first * p.q.token;
+    Operand<T> kf[4][kSteps], qf[kSteps];
+    Scale ks[4], qs, mine;
+    auto load_tile = [&](const T* from, int64_t stride, int tile, Operand<T>(&f)[kSteps], Scale& s) {
+        const int t = 16 * tile + row;
+        Eight<T> x[kSteps];
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            x[j] = load_eight(from + t * stride, 32 * j + 8 * g, p.k_size, t < at.count, p.wide);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(to_f32(x[j].x[i])));
+        }
+        s = scale_of(max_groups(m));
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) f[j].set(x[j], s.up);
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i <= wave) load_tile(k, p.k.token, i, kf[i], ks[i]);
+    load_tile(q, p.q.token, wave, qf, qs);
+    Operand<T> kw[kSteps];  // this wave's tile of k
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i == wave) {
+            mine = ks[i];
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) kw[j] = kf[i][j];
+        }
+    __syncthreads();
+
+    // this wave's rows of A and P
+    f32x4 d{};
+    double Gt[4];
+    float bt[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        Gt[r] = G[16 * wave + 4 * g + r];
+        bt[r] = beta[16 * wave + 4 * g + r];
+        // scales of the rows this lane holds of a result
+        d[r] = __shfl(mine.down, 4 * g + r, 64);
+    }
+    f32x4 dq;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) dq[r] = __shfl(qs.down, 4 * g + r, 64);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i > wave) continue;
+        f32x4 kk{}, qk{};
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            kk = product(kw[j], kf[i][j], kk);
+            qk = product(qf[j], kf[i][j], qk);
+        }
+        const int s = 16 * i + row;
+        const double Gs = G[s];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = 16 * wave + 4 * g + r;
+            const float e = s <= t ? expf((float)(Gt[r] - Gs)) : 0.0f;
+            float a = kk[r], b = qk[r];
+            if (sizeof(T) == 4) {  // FP32 rows were scaled
+                a = a * d[r] * ks[i].down;
+                b = b * dq[r] * ks[i].down;
+            }
+            A[t * kPitch + s] = s < t ? bt[r] * e * a : 0.0f;
+            P[t * kPitch + s] = s <= t ? p.scale * e * b : 0.0f;
+        }
+    }
+    // row factors
+    if (g == 0) {
+        const int t = 16 * wave + row;
+        const double last = G[kC - 1];
+        factors[64 * DeltaRecord::kKeyScale + t] = mine.up;
+        factors[64 * DeltaRecord::kQueryScale + t] = qs.up;
+        factors[64 * DeltaRecord::kRise + t] = expf((float)G[t]) * mine.down;
+        factors[64 * DeltaRecord::kBeta + t] = beta[t];
+        factors[64 * DeltaRecord::kTail + t] = expf((float)(last - G[t])) * mine.down;
+        factors[64 * DeltaRecord::kQueryRise + t] = p.scale * expf((float)G[t]) * qs.down;
+        factors[64 * DeltaRecord::kDecay + t] = expf((float)last);
+    }
+
+    // the diagonal block, whose rows and columns are all this wave's: column
+    // `row` of its inverse, in every group of lanes
+    float* D = A + 16 * wave * (kPitch + 1);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float v = i == row ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < i; ++j) v = __builtin_fmaf(-D[i * kPitch + j], x[j], v);
+        x[i] = v;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    if (g == 0)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) D[i * kPitch + row] = x[i];
+    __syncthreads();
+    const auto block = [&](int i, int j) { return A + 16 * (i * kPitch + j); };
+    // 32 x 32: blocks (1, 0) and (3, 2), read and written by one wave each
+    if (wave & 1) {
+        f32x4 y = block_product(block_rows(block(wave, wave - 1), lane),
+                                block_columns(block(wave - 1, wave - 1), lane), f32x4{});
+        y = block_product(-block_rows(block(wave, wave), lane), y, f32x4{});
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        block_store(block(wave, wave - 1), lane, y);
+    }
+    __syncthreads();
+    {  // 64 x 64: wave (i, j) makes block (2 + i, j)
+        const int i = 2 + (wave >> 1), j = wave & 1;
+        f32x4 y[2], z{};
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            y[r] = f32x4{};
+            if (2 + r > i) continue;
+            if (j == 0)
+                y[r] = block_product(block_rows(block(2 + r, 0), lane),
+                                     block_columns(block(0, 0), lane), y[r]);
+            y[r] = block_product(block_rows(block(2 + r, 1), lane),
+                                 block_columns(block(1, j), lane), y[r]);
+            z = block_product(-block_rows(block(i, 2 + r), lane), y[r], z);
+        }
+        __syncthreads();
+        block_store(block(i, j), lane, z);
+    }
+    __syncthreads();
+
+    write_fragments<false, 2>(A, wave, lane, record + DeltaRecord::kAtT,
+                              factors + 64 * DeltaRecord::kT);
+    if (kBackward) {
+        write_fragments<true, 2>(A, wave, lane, record + DeltaRecord::kAtTt,
+                                 factors + 64 * DeltaRecord::kTt);
+        write_fragments<true, 2>(P, wave, lane, record + DeltaRecord::kAtPt,
+                                 factors + 64 * DeltaRecord::kPt);
+    } else {
+        constexpr int kParts = __is_same(T, bf16_t) ? 1 : 2;
+        write_fragments<false, kParts>(P, wave, lane, record + DeltaRecord::kAtP,
+                                       factors + 64 * DeltaRecord::kP);
+    }
+}
+
+template <class T, int kK>
+void launch(const DeltaChunks& a, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.chunks * a.v_heads));
+    if (a.backward)
+        hipLaunchKernelGGL((delta_prep_kernel<T, kK, true>), grid, dim3(kThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((delta_prep_kernel<T, kK, false>), grid, dim3(kThreads), 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_delta_prep(const DeltaChunks& a, hipStream_t stream) {
+    if (a.chunks == 0) return hipSuccess;
+    return by_dtype(a.dtype, [&](auto t) {
+        using T = decltype(t);
+        if (a.k_size <= 64)
+            launch<T, 64>(a, stream);
+        else
+            launch<T, 128>(a, stream);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace sgemm_emu

@@ -130,7 +130,8 @@ int check_shape(const A& a) {
     if (int rc = check_sizes(a)) return rc;
     if (a.cu_seqlens == nullptr && (int64_t)a.batch * a.tokens > INT32_MAX)
         return SGEMM_EMU_ERR_UNSUPPORTED;
-    if (delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr) * a.v_heads > kDeltaMostTasks)
+    if (delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr) > kDeltaMostTasks / a.v_heads ||
+        (int64_t)a.batch * (((int64_t)a.v_size + 63) / 64) > kDeltaMostTasks / a.v_heads)
         return SGEMM_EMU_ERR_UNSUPPORTED;
     return SGEMM_EMU_OK;
 }
