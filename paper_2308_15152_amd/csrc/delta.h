@@ -10,6 +10,13 @@
 // makes them for all chunks at once (delta_prep.hip).  A second one walks the
 // chunks of every sequence in order, 16 columns of S to a wave
 // (delta_chain.hip).
+//
+// The gradient walks forward the same way, keeping S and U, and then back with
+// the gradient D of the state after the chunk,
+//   dU = P^T dO + diag(e^{G_64 - G}) K D,   dY = T^T dU,   dV = diag(beta) dY,
+//   D before = e^{G_64} D + scale (diag(e^G) Q)^T dO - (diag(e^G) K)^T dV,
+// (delta_back.hip), after which every chunk's dQ, dK, dbeta and dg depend on
+// that chunk only (delta_gradient.hip).
 #pragma once
 
 #include <initializer_list>
@@ -78,21 +85,33 @@ struct DeltaChunks {
     float* states;
     float* updates;
     bool wide;            // 16-byte loads of q's and k's rows
+    // gradients: d_o, dfinal and what the walk back keeps per chunk: the
+    // gradients of S after it and of diag(beta) (V - ...), the right side of U
+    sgemm_emu_view_t d_o, dq, dk, dv, dg, dbeta;
+    const float* dfinal;
+    float* dinitial;
+    float* dstates;
+    float* dsides;
+    bool wide_values;     // 16-byte loads of v's and d_o's rows
 };
 
-// Whether every row of q and k can be loaded 16 bytes at a time.
-template <class A>
-bool delta_wide(const A& a) {
-    const int64_t n = a.dtype == SGEMM_EMU_F32 ? 4 : 8;
-    for (const sgemm_emu_view_t* v : {&a.q, &a.k})
-        if ((uintptr_t)v->p % 16 || v->batch % n || v->token % n || v->head % n) return false;
-    return a.k_size % 8 == 0;
+// Whether rows of `size` elements of these views can be loaded 16 bytes at a
+// time.
+inline bool delta_wide(int dtype, int size, std::initializer_list<sgemm_emu_view_t> views) {
+    const int64_t n = dtype == SGEMM_EMU_F32 ? 4 : 8;
+    for (const sgemm_emu_view_t& v : views)
+        if ((uintptr_t)v.p % 16 || v.batch % n || v.token % n || v.head % n) return false;
+    return size % 8 == 0;
 }
 
 hipError_t launch_delta_prep(const DeltaChunks& a, hipStream_t stream);
 hipError_t launch_delta_chain(const DeltaChunks& a, hipStream_t stream);
+hipError_t launch_delta_chain_back(const DeltaChunks& a, hipStream_t stream);
+hipError_t launch_delta_gradient(const DeltaChunks& a, hipStream_t stream);
 
 int64_t delta_forward_workspace(const delta_emu_forward_t& a);
 hipError_t launch_delta_forward(const delta_emu_forward_t& a, hipStream_t stream);
+int64_t delta_backward_workspace(const delta_emu_backward_t& a);
+hipError_t launch_delta_backward(const delta_emu_backward_t& a, hipStream_t stream);
 
 }  // namespace sgemm_emu

@@ -173,4 +173,137 @@ __device__ inline Eight<T> load_eight(const T* row, int e, int size, bool in, bo
     return v;
 }
 
+// The 8 k-values of a lane as MFMA operand, in the type of the input or, for
+// FP32, split.
+template <class T>
+struct Operand;
+template <>
+struct Operand<bf16_t> {
+    typedef __bf16 vec __attribute__((ext_vector_type(8)));
+    vec v;
+    __device__ void set(const Eight<bf16_t>& x, float) { __builtin_memcpy(&v, &x, 16); }
+};
+template <>
+struct Operand<f16_t> {
+    half8_t v;
+    __device__ void set(const Eight<f16_t>& x, float) { __builtin_memcpy(&v, &x, 16); }
+};
+template <>
+struct Operand<float> {
+    Frag<2> v;
+    __device__ void set(const Eight<float>& x, float up) { v = split<2>(x.x, up); }
+};
+__device__ inline f32x4 product(const Operand<bf16_t>& a, const Operand<bf16_t>& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ inline f32x4 product(const Operand<f16_t>& a, const Operand<f16_t>& b, f32x4 c) {
+    return mfma(a.v, b.v, c);
+}
+__device__ inline f32x4 product(const Operand<float>& a, const Operand<float>& b, f32x4 c) {
+    return multiply(a.v, b.v, c);
+}
+
+// Parts of an input element as operand.
+template <class T>
+constexpr int kPartsOf = sizeof(T) == 4 ? 2 : 1;
+
+// Rows of K or Q as fragments.  A thread takes 4 tokens x 8 elements: as rows
+// (A operand of products with S) two 8-byte pieces a token, as columns (A
+// operand of products that contract over tokens) 8 pieces of 4 tokens.  Lanes
+// of a fragment are permuted by its number, which spreads the pieces that
+// a wave writes at once over the banks.
+template <class T, int kK>
+struct Unit {
+    Eight<T> x[4];
+
+    __device__ void load(const T* rows, int64_t stride, int unit, int count, int size, bool wide) {
+        const int e = 8 * (unit % (kK / 8)), t = 4 * (unit / (kK / 8));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = load_eight(rows + (t + i) * stride, e, size, t + i < count, wide);
+    }
+
+    // scale: of the four tokens
+    template <bool kRowsToo, bool kColumns>
+    __device__ void store(char* rows, char* columns, int unit, f32x4 scale) const {
+        constexpr int kParts = kPartsOf<T>, kSteps = kK / 32;
+        const int eight = unit % (kK / 8), four = unit / (kK / 8);
+        half4_t part[kParts][4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = to_f32(x[i].x[e]);
+                const _Float16 hi = (_Float16)(v * scale[i]);
+                part[0][i][e / 4][e % 4] = hi;
+                if (kParts == 2)
+                    part[kParts - 1][i][e / 4][e % 4] =
+                        (_Float16)__builtin_fmaf(v, scale[i], -(float)hi);
+            }
+        if (kRowsToo) {
+            const int step = eight / 4, half = (eight % 4) / 2, g = 2 * (eight % 2);
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                char* to = rows + ((p * 4 + four / 4) * kSteps + step) * 1024 + half * 8;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int lane = (g + b) * 16 + 4 * (four % 4) + i;
+                        *reinterpret_cast<half4_t*>(to + (lane ^ (step & 3)) * 16) = part[p][i][b];
+                    }
+            }
+        }
+        if (kColumns) {
+            const int tile = eight / 2, step = four / 8, half = (four / 4) % 2, g = four % 4;
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                char* to = columns + ((p * (kK / 16) + tile) * 2 + step) * 1024 + half * 8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int lane = g * 16 + 8 * (eight % 2) + e;
+                    half4_t v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = part[p][i][e / 4][e % 4];
+                    *reinterpret_cast<half4_t*>(to + (lane ^ (tile & 7)) * 16) = v;
+                }
+            }
+        }
+    }
+};
+
+template <class T, int kK>
+__device__ inline Frag<kPartsOf<T>> row_fragment(const char* rows, int tile, int step,
+                                                              int lane) {
+    constexpr int kParts = kPartsOf<T>;
+    Frag<kParts> f;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p)
+        f.part[p] = *reinterpret_cast<const half8_t*>(
+            rows + ((p * 4 + tile) * (kK / 32) + step) * 1024 + (lane ^ (step & 3)) * 16);
+    return f;
+}
+
+template <class T, int kK>
+__device__ inline Frag<kPartsOf<T>> column_fragment(const char* columns, int tile,
+                                                                 int step, int lane) {
+    constexpr int kParts = kPartsOf<T>;
+    Frag<kParts> f;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p)
+        f.part[p] = *reinterpret_cast<const half8_t*>(
+            columns + ((p * (kK / 16) + tile) * 2 + step) * 1024 + (lane ^ (tile & 7)) * 16);
+    return f;
+}
+
+template <int N>
+__device__ inline Frag<N> matrix_fragment(const char* matrix, int at, int lane) {
+    Frag<N> f;
+#pragma unroll
+    for (int p = 0; p < N; ++p)
+        f.part[p] =
+            *reinterpret_cast<const half8_t*>(matrix + (p * 6 + at) * 1024 + lane * 16);
+    return f;
+}
+
 }  // namespace sgemm_emu

@@ -1,0 +1,531 @@
+// The gated delta rule's gradient, last kernel: dQ, dK, dbeta and dg of every
+// chunk, from S before it, the gradient D of S after it, U, dY and dO.  With
+//   E1 = dO S^T,  E2 = dY S^T,  E3 = U D^T             (64 x k_size),
+//   M1 = scale e^{G_t - G_s} (dO U^T)_ts, s <= t,  M2 = e^{G_t - G_s} (dY U^T)_ts, s < t,
+//   W = -(diag(e^G) E2 + M2 K),
+//   C = diag(e^{G_64 - G}) E3 + M1^T Q - M2^T diag(beta) K:
+//   dQ = scale diag(e^G) E1 + M1 K,     dK = diag(beta) W + C,
+//   dbeta_t = dY_t.V_t + K_t.W_t,
+//   dg_t = e^{G_64} <D, S> + sum_{i >= t} a_i + sum_{j < t} b_j + sum_{i >= t > j} X_ij,
+//     a_i = e^{G_i} (scale Q_i.E1_i - beta_i K_i.E2_i),   b_j = e^{G_64 - G_j} K_j.E3_j,
+//     X_ij = M1_ij Q_i.K_j - beta_i M2_ij K_i.K_j
+// (every path of a token's decay: state to state, state to output, write to
+// state, write to output or write).  The last sum is the sum over i >= t of row
+// sums less column sums of X, taken in FP64: it cancels.
+//
+// A block takes one chunk of one key head and goes through its value heads, so
+// that dQ and dK are summed in registers in a fixed order.  A wave owns 16 of
+// the key's elements (columns of E, W, C, dQ, dK): S and D are read and split by
+// one wave each, straight into operand registers, while dO, dY and U go through
+// LDS as fragments that all waves use (also as each other's B operands for M1
+// and M2).  Then M1 and M2 take their place there.
+#include <type_traits>
+
+#include "delta_chunk.hpp"
+
+namespace sgemm_emu {
+
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kPitch = 68;
+
+// LDS, in bytes.
+template <class T, int kK>
+struct Layout {
+    static constexpr int kParts = kPartsOf<T>;
+    static constexpr int kSteps = kK / 32, kTiles = kK / 16;
+    static constexpr int kColumns = kParts * 4 * kSteps * 1024;  // K^T or Q^T
+    // columns of V taken at a time, in steps of 32
+    static constexpr int kVSteps = sizeof(T) == 4 ? 2 : 4;
+    static constexpr int kPart = 4 * kVSteps * 1024;  // one part of dO, dY or U
+    static constexpr int kAtKt = 0;
+    static constexpr int kAtQt = kAtKt + kColumns;
+    static constexpr int kShared = kAtQt + kColumns;
+    static constexpr int kAtDo = kShared;  // dO, dY, U ...
+    static constexpr int kAtDy = kAtDo + kParts * kPart;
+    static constexpr int kAtU = kAtDy + 2 * kPart;
+    static constexpr int kEndA = kAtU + 2 * kPart;
+    static constexpr int kAtM = kShared;  // ... or M1, M2 in FP32, and as fragments
+    static constexpr int kMatrix = kC * kPitch * 4;
+    static constexpr int kAtFragments = kAtM + 2 * kMatrix;
+    static constexpr int kEndB = kAtFragments + 4 * 2 * DeltaRecord::kMatrix;
+    static constexpr int kAtSmall = kEndA > kEndB ? kEndA : kEndB;
+    struct Small {
+        double G[kC];
+        float beta[kC], key_down[kC], query_down[kC];
+        union {
+            float down[3][kC];   // inverse row scales of dO, dY, U
+            double rows[2][kC];  // row sums of X, of either term
+        };
+        float m_down[4][kC];     // of M1, M2, M1^T, M2^T
+        float dot[kC];           // dY_t.V_t
+        float part[3][kTiles][kC];  // K.W, a and b per wave
+        float end[kWaves];          // <D, S> per wave
+        double columns[2][4][kC];   // column sums of X, of each row tile
+    };
+    static constexpr int kBytes = kAtSmall + (int)sizeof(Small);
+};
+
+// Sum over the 16 lanes of a group, in every one of them.
+__device__ inline float sum_row(float x) {
+    const auto turned = [](float y, auto by) {
+        return __builtin_bit_cast(
+            float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, y), 0x120 + decltype(by)::value,
+                                            0xf, 0xf, true));
+    };
+    x += turned(x, std::integral_constant<int, 8>{});
+    x += turned(x, std::integral_constant<int, 4>{});
+    x += turned(x, std::integral_constant<int, 2>{});
+    return x + turned(x, std::integral_constant<int, 1>{});
+}
+
+// Rows of tile `tile` of M (or its transpose), columns times `by`, as fragments.
+template <bool kTransposed>
+__device__ inline void write_fragments(const float* M, const float* by, const float* by2, int tile,
+                                       int lane, char* to, float* down) {
+    const int row = lane & 15, g = lane >> 4;
+    float x[2][8], m = 0.0f;
+#pragma unroll
+    for (int step = 0; step < 2; ++step)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int other = 2 * step + half;
+            const bool full = kTransposed ? other >= tile : other <= tile;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int a = 16 * tile + row, b = 16 * other + 4 * g + i;
+                float v = 0.0f;
+                if (full) v = (kTransposed ? M[b * kPitch + a] : M[a * kPitch + b]) * by[b];
+                if (full && by2) v *= by2[b];
+                x[step][4 * half + i] = v;
+                m = fmaxf(m, fabsf(v));
+            }
+        }
+    const Scale s = scale_of(max_groups(m));
+    if (g == 0) down[16 * tile + row] = s.down;
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+        if (kTransposed ? step < tile / 2 : step > tile / 2) continue;
+        const int at = kTransposed ? upper_at(tile, step) : lower_at(tile, step);
+        const Frag<2> f = split<2>(x[step], s.up);
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            *reinterpret_cast<half8_t*>(to + (p * 6 + at) * 1024 + lane * 16) = f.part[p];
+    }
+}
+
+template <class T, int kK>
+__global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks p) {
+    using L = Layout<T, kK>;
+    constexpr int kVSteps = L::kVSteps, kVBlock = 32 * kVSteps;
+    constexpr int kOwn = 4 * L::kTiles / kWaves;  // token tiles of a wave
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    auto& small = *reinterpret_cast<typename L::Small*>(lds + L::kAtSmall);
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = lane & 15, g = lane >> 4;
+    const int kh = blockIdx.x % p.k_heads, c = blockIdx.x / p.k_heads;
+    const Place at = place_of(p.cu_seqlens, c, p.batch, p.tokens);
+    if (at.count <= 0) return;  // the whole block
+    const bool packed = p.cu_seqlens != nullptr;
+    const int group = p.v_heads / p.k_heads;
+    const int tile = wave % L::kTiles, own = wave / L::kTiles * kOwn;
+    const int ke = 16 * tile + row;  // this lane's element of the key
+    const bool kin = ke < p.k_size;
+
+    // K^T and Q^T, and this lane's elements of K and Q
+    const T* k = row_of<const T>(p.k, packed, at.n, at.span, kh) + (int64_t)at.first * p.k.token;
+    const T* q = row_of<const T>(p.q, packed, at.n, at.span, kh) + (int64_t)at.first * p.q.token;
+    {
+        const float* f = reinterpret_cast<const float*>(
+            p.records + ((int64_t)c * p.v_heads + kh * group) * p.record_bytes);
+        constexpr int kUnits = 16 * kK / 8;
+        for (int w = threadIdx.x; w < 2 * kUnits; w += kThreads) {
+            const bool is_q = w >= kUnits;
+            const int unit = is_q ? w - kUnits : w;
+            Unit<T, kK> u;
+            u.load(is_q ? q : k, is_q ? p.q.token : p.k.token, unit, at.count, p.k_size, p.wide);
+            const f32x4 s = reinterpret_cast<const f32x4*>(
+                f + 64 * (is_q ? DeltaRecord::kQueryScale : DeltaRecord::kKeyScale))[unit / (kK / 8)];
+            u.template store<false, true>(nullptr, lds + (is_q ? L::kAtQt : L::kAtKt), unit, s);
+        }
+        if (threadIdx.x < kC) {  // powers of two: exact
+            small.key_down[threadIdx.x] = 1.0f / f[64 * DeltaRecord::kKeyScale + threadIdx.x];
+            small.query_down[threadIdx.x] = 1.0f / f[64 * DeltaRecord::kQueryScale + threadIdx.x];
+        }
+    }
+    f32x4 kd[kOwn], qd[kOwn], dq[kOwn], dk[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = 16 * (own + i) + 4 * g + r;
+            kd[i][r] = kin && t < at.count ? to_f32(k[(int64_t)t * p.k.token + ke]) : 0.0f;
+            qd[i][r] = kin && t < at.count ? to_f32(q[(int64_t)t * p.q.token + ke]) : 0.0f;
+            dq[i][r] = dk[i][r] = 0.0f;
+        }
+
+    // rows wave % 4 of Q K^T (waves 0 to 3) and K K^T, for the decays' gradient
+    f32x4 kk[4] = {};
+    if (p.dg.p) {
+        const int mt = wave % 4;
+        const auto load_tile = [&](const T* from, int64_t stride, int i, Operand<T>(&f)[L::kSteps]) {
+            const int t = 16 * i + row;
+            Eight<T> x[L::kSteps];
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < L::kSteps; ++j) {
+                x[j] = load_eight(from + t * stride, 32 * j + 8 * g, p.k_size, t < at.count, p.wide);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(to_f32(x[j].x[e])));
+            }
+            const Scale s = scale_of(max_groups(m));
+#pragma unroll
+            for (int j = 0; j < L::kSteps; ++j) f[j].set(x[j], s.up);
+            return s.down;
+        };
+        Operand<T> a[L::kSteps], b[L::kSteps];
+        const float ad = wave < 4 ? load_tile(q, p.q.token, mt, a) : load_tile(k, p.k.token, mt, a);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i > mt) continue;
+            const float bd = load_tile(k, p.k.token, i, b);
+#pragma unroll
+            for (int j = 0; j < L::kSteps; ++j) kk[i] = product(a[j], b[j], kk[i]);
+            if (sizeof(T) == 4)  // FP32 rows were scaled
+#pragma unroll
+                for (int r = 0; r < 4; ++r) kk[i][r] *= __shfl(ad, 4 * g + r, 64) * bd;
+        }
+    }
+
+    for (int h = kh * group; h < (kh + 1) * group; ++h) {
+        const int64_t task = (int64_t)c * p.v_heads + h;
+        __syncthreads();  // the last head's values are used
+        if (wave == 0) {
+            const bool in = lane < at.count;
+            const int t = at.first + lane;
+            double sum = 0.0;
+            float b = in ? 1.0f : 0.0f;
+            if (in && p.g.p)
+                sum = log_decay(row_of<const float>(p.g, packed, at.n, at.span, h)[t * p.g.token]);
+            if (in && p.beta.p)
+                b = row_of<const float>(p.beta, packed, at.n, at.span, h)[t * p.beta.token];
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const double u = __shfl_up(sum, d, 64);
+                if (lane >= d) sum += u;
+            }
+            small.G[lane] = sum;
+            small.beta[lane] = b;
+            small.dot[lane] = 0.0f;
+        }
+        const T* v = row_of<const T>(p.v, packed, at.n, at.span, h) + (int64_t)at.first * p.v.token;
+        const T* d_o = row_of<const T>(p.d_o, packed, at.n, at.span, h) + (int64_t)at.first * p.d_o.token;
+        const float* u = p.updates + task * kC * p.v_size;
+        const float* dy = p.dsides + task * kC * p.v_size;
+        const float* S = p.states + task * p.k_size * p.v_size;
+        const float* D = p.dstates + task * p.k_size * p.v_size;
+        const bool wide_f = p.v_size % 8 == 0;
+
+        f32x4 e1[kOwn] = {}, e2[kOwn] = {}, e3[kOwn] = {}, m[4] = {};
+        float sd = 0.0f;
+        for (int v0 = 0; v0 < p.v_size; v0 += kVBlock) {
+            __syncthreads();  // the last block's fragments are used
+            // dO, dY and U: 12 tiles of 16 rows, one wave each
+            for (int job = wave; job < 12; job += kWaves) {
+                const int which = job / 4, i = job % 4, t = 16 * i + row;
+                const auto put = [&](auto parts, const auto (&x)[kVSteps], char* to, float* down) {
+                    constexpr int kN = decltype(parts)::value;
+                    float w[kVSteps][8], top = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < kVSteps; ++j)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            w[j][e] = to_f32(x[j].x[e]);
+                            top = fmaxf(top, fabsf(w[j][e]));
+                        }
+                    const Scale s = scale_of(max_groups(top));
+                    if (g == 0) down[t] = s.down;
+#pragma unroll
+                    for (int j = 0; j < kVSteps; ++j) {
+                        const Frag<kN> f = split<kN>(w[j], s.up);
+#pragma unroll
+                        for (int n = 0; n < kN; ++n)
+                            *reinterpret_cast<half8_t*>(to + n * L::kPart + (i * kVSteps + j) * 1024 +
+                                                        lane * 16) = f.part[n];
+                    }
+                };
+                if (which == 0) {
+                    Eight<T> x[kVSteps];
+#pragma unroll
+                    for (int j = 0; j < kVSteps; ++j)
+                        x[j] = load_eight(d_o + (int64_t)t * p.d_o.token, v0 + 32 * j + 8 * g,
+                                          p.v_size, t < at.count, p.wide_values);
+                    put(std::integral_constant<int, L::kParts>{}, x, lds + L::kAtDo, small.down[0]);
+                } else {
+                    const float* from = which == 1 ? dy : u;
+                    Eight<float> x[kVSteps];
+#pragma unroll
+                    for (int j = 0; j < kVSteps; ++j)
+                        x[j] = load_eight(from + (int64_t)t * p.v_size, v0 + 32 * j + 8 * g,
+                                          p.v_size, true, wide_f);
+                    put(std::integral_constant<int, 2>{}, x, lds + (which == 1 ? L::kAtDy : L::kAtU),
+                        small.down[which]);
+                    if (which == 1) {
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < kVSteps; ++j) {
+                            const Eight<T> y = load_eight(v + (int64_t)t * p.v.token,
+                                                          v0 + 32 * j + 8 * g, p.v_size,
+                                                          t < at.count, p.wide_values);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                sum = __builtin_fmaf(x[j].x[e], to_f32(y.x[e]), sum);
+                        }
+                        sum += __shfl_xor(sum, 16, 64);
+                        sum += __shfl_xor(sum, 32, 64);
+                        if (g == 0) small.dot[t] += sum;
+                    }
+                }
+            }
+            // this wave's rows of S and D as B operands (columns: key elements)
+            Eight<float> sx[kVSteps], dx[kVSteps];
+            float smax = 0.0f, dmax = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kVSteps; ++j) {
+                sx[j] = load_eight(S + (int64_t)ke * p.v_size, v0 + 32 * j + 8 * g, p.v_size, kin, wide_f);
+                dx[j] = load_eight(D + (int64_t)ke * p.v_size, v0 + 32 * j + 8 * g, p.v_size, kin, wide_f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    smax = fmaxf(smax, fabsf(sx[j].x[e]));
+                    dmax = fmaxf(dmax, fabsf(dx[j].x[e]));
+                    if (own == 0) sd = __builtin_fmaf(sx[j].x[e], dx[j].x[e], sd);
+                }
+            }
+            const Scale ss = scale_of(max_groups(smax)), ds = scale_of(max_groups(dmax));
+            __syncthreads();
+            const auto fragment = [&](auto parts, int from, int i, int j) {
+                constexpr int kN = decltype(parts)::value;
+                Frag<kN> f;
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+                    f.part[n] = *reinterpret_cast<const half8_t*>(
+                        lds + from + n * L::kPart + (i * kVSteps + j) * 1024 + lane * 16);
+                return f;
+            };
+            constexpr std::integral_constant<int, L::kParts> one{};
+            constexpr std::integral_constant<int, 2> two{};
+            {
+                f32x4 a1[kOwn] = {}, a2[kOwn] = {}, a3[kOwn] = {};
+#pragma unroll
+                for (int j = 0; j < kVSteps; ++j) {
+                    const Frag<2> sb = split<2>(sx[j].x, ss.up), db = split<2>(dx[j].x, ds.up);
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) {
+                        a1[i] = multiply(fragment(one, L::kAtDo, own + i, j), sb, a1[i]);
+                        a2[i] = multiply(fragment(two, L::kAtDy, own + i, j), sb, a2[i]);
+                        a3[i] = multiply(fragment(two, L::kAtU, own + i, j), db, a3[i]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int t = 16 * (own + i) + 4 * g + r;
+                        e1[i][r] = __builtin_fmaf(a1[i][r], small.down[0][t] * ss.down, e1[i][r]);
+                        e2[i][r] = __builtin_fmaf(a2[i][r], small.down[1][t] * ss.down, e2[i][r]);
+                        e3[i][r] = __builtin_fmaf(a3[i][r], small.down[2][t] * ds.down, e3[i][r]);
+                    }
+            }
+            // rows wave % 4 of dO U^T (waves 0 to 3) and dY U^T
+            const int mt = wave % 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i > mt) continue;
+                f32x4 a{};
+#pragma unroll
+                for (int j = 0; j < kVSteps; ++j) {
+                    const Frag<2> b = fragment(two, L::kAtU, i, j);
+                    if (wave < 4)
+                        a = multiply(fragment(one, L::kAtDo, mt, j), b, a);
+                    else
+                        a = multiply(fragment(two, L::kAtDy, mt, j), b, a);
+                }
+                const float cd = small.down[2][16 * i + row];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    m[i][r] = __builtin_fmaf(a[r], small.down[wave < 4 ? 0 : 1][16 * mt + 4 * g + r] * cd,
+                                             m[i][r]);
+            }
+        }
+        __syncthreads();  // dO, dY and U are used
+        float* M1 = reinterpret_cast<float*>(lds + L::kAtM);
+        float* M2 = M1 + kC * kPitch;
+        {
+            const int mt = wave % 4;
+            float* M = wave < 4 ? M1 : M2;
+            double rows[4] = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = 16 * i + row;
+                double column = 0.0;
+                if (i <= mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int t = 16 * mt + 4 * g + r;
+                        const bool on = wave < 4 ? s <= t : s < t;
+                        const float e = on ? expf((float)(small.G[t] - small.G[s])) : 0.0f;
+                        const float x = on ? (wave < 4 ? p.scale * e : e) * m[i][r] : 0.0f;
+                        M[t * kPitch + s] = x;
+                        // a token and itself have no decay between them
+                        const double y =
+                            s < t ? (double)((wave < 4 ? x : -small.beta[t] * x) * kk[i][r]) : 0.0;
+                        rows[r] += y;
+                        column += y;
+                    }
+                column += __shfl_xor(column, 16, 64);
+                column += __shfl_xor(column, 32, 64);
+                if (g == 0) small.columns[wave / 4][mt][s] = column;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int d = 1; d < 16; d *= 2) rows[r] += __shfl_xor(rows[r], d, 64);
+                if (row == 0) small.rows[wave / 4][16 * mt + 4 * g + r] = rows[r];
+            }
+        }
+        __syncthreads();
+        {
+            const int mt = wave % 4;
+            char* to = lds + L::kAtFragments;
+            constexpr int kBytes = 2 * DeltaRecord::kMatrix;
+            if (wave < 4) {
+                write_fragments<false>(M1, small.key_down, nullptr, mt, lane, to, small.m_down[0]);
+                write_fragments<true>(M1, small.query_down, nullptr, mt, lane, to + 2 * kBytes,
+                                      small.m_down[2]);
+            } else {
+                write_fragments<false>(M2, small.key_down, nullptr, mt, lane, to + kBytes,
+                                       small.m_down[1]);
+                write_fragments<true>(M2, small.key_down, small.beta, mt, lane, to + 3 * kBytes,
+                                      small.m_down[3]);
+            }
+        }
+        __syncthreads();
+        const double last = small.G[kC - 1];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int ti = own + i;
+            f32x4 a[4] = {};
+            const char* from = lds + L::kAtFragments;
+            constexpr int kBytes = 2 * DeltaRecord::kMatrix;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const auto kt = column_fragment<T, kK>(lds + L::kAtKt, tile, j, lane);
+                if (j <= ti / 2) {
+                    a[0] = multiply(matrix_fragment<2>(from, lower_at(ti, j), lane), kt, a[0]);
+                    a[1] = multiply(matrix_fragment<2>(from + kBytes, lower_at(ti, j), lane), kt, a[1]);
+                }
+                if (j >= ti / 2) {
+                    const auto qt = column_fragment<T, kK>(lds + L::kAtQt, tile, j, lane);
+                    a[2] = multiply(matrix_fragment<2>(from + 2 * kBytes, upper_at(ti, j), lane), qt, a[2]);
+                    a[3] = multiply(matrix_fragment<2>(from + 3 * kBytes, upper_at(ti, j), lane), kt, a[3]);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * ti + 4 * g + r;
+                const float rise = expf((float)small.G[t]);
+                const float tail = expf((float)(last - small.G[t]));
+                const float de = p.scale * rise * e1[i][r], we = rise * e2[i][r];
+                const float w = -__builtin_fmaf(small.m_down[1][t], a[1][r], we);
+                const float te = tail * e3[i][r];
+                const float bt = small.beta[t];
+                dq[i][r] += __builtin_fmaf(small.m_down[0][t], a[0][r], de);
+                dk[i][r] += bt * w +
+                            (te + (small.m_down[2][t] * a[2][r] - small.m_down[3][t] * a[3][r]));
+                const float sums[3] = {sum_row(kd[i][r] * w),
+                                       sum_row(__builtin_fmaf(qd[i][r], de, -(bt * kd[i][r] * we))),
+                                       sum_row(kd[i][r] * te)};
+                if (row == 0)
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) small.part[n][tile][t] = sums[n];
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) sd += __shfl_xor(sd, d, 64);
+        if (lane == 0) small.end[wave] = sd;
+        __syncthreads();
+        if (wave == 0) {
+            float db = small.dot[lane], s = 0.0f;
+            double later = 0.0, before = 0.0;  // summed over i >= t and j <= t
+#pragma unroll
+            for (int i = 0; i < L::kTiles; ++i) {
+                db += small.part[0][i][lane];
+                later += small.part[1][i][lane];
+                before += small.part[2][i][lane];
+            }
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) s += small.end[i];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                later += small.rows[n][lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) later -= small.columns[n][i][lane];
+            }
+            const double b = before;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const double x = __shfl_down(later, d, 64), y = __shfl_up(before, d, 64);
+                if (lane + d < 64) later += x;
+                if (lane >= d) before += y;
+            }
+            if (lane < at.count) {
+                const int64_t t = at.first + lane;
+                if (p.dbeta.p)
+                    row_of<float>(p.dbeta, packed, at.n, at.span, h)[t * p.dbeta.token] = db;
+                if (p.dg.p)
+                    row_of<float>(p.dg, packed, at.n, at.span, h)[t * p.dg.token] =
+                        (float)(later + (before - b) + (double)(expf((float)last) * s));
+            }
+        }
+    }
+    T* dqo = row_of<T>(p.dq, packed, at.n, at.span, kh) + (int64_t)at.first * p.dq.token + ke;
+    T* dko = row_of<T>(p.dk, packed, at.n, at.span, kh) + (int64_t)at.first * p.dk.token + ke;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int t = 16 * (own + i) + 4 * g + r;
+            if (kin && t < at.count) {
+                dqo[(int64_t)t * p.dq.token] = from_f32<T>(dq[i][r]);
+                dko[(int64_t)t * p.dk.token] = from_f32<T>(dk[i][r]);
+            }
+        }
+}
+
+template <class T, int kK>
+hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
+    constexpr int kBytes = Layout<T, kK>::kBytes;
+    static_assert(kBytes <= 160 * 1024, "LDS of a CU");
+    const void* kernel = reinterpret_cast<const void*>(delta_gradient_kernel<T, kK>);
+    if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes))
+        return e;
+    hipLaunchKernelGGL((delta_gradient_kernel<T, kK>), dim3((unsigned)(a.chunks * a.k_heads)),
+                       dim3(kThreads), kBytes, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_delta_gradient(const DeltaChunks& a, hipStream_t stream) {
+    if (a.chunks == 0) return hipSuccess;
+    return by_dtype(a.dtype, [&](auto t) {
+        using T = decltype(t);
+        return a.k_size <= 64 ? launch<T, 64>(a, stream) : launch<T, 128>(a, stream);
+    });
+}
+
+}  // namespace sgemm_emu

@@ -18,36 +18,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPitch = 68;  // floats of a row of the matrices in LDS
 
-// The 8 k-values of a lane as MFMA operand, in the type of the input or, for
-// FP32, split.
-template <class T>
-struct Operand;
-template <>
-struct Operand<bf16_t> {
-    typedef __bf16 vec __attribute__((ext_vector_type(8)));
-    vec v;
-    __device__ void set(const Eight<bf16_t>& x, float) { __builtin_memcpy(&v, &x, 16); }
-};
-template <>
-struct Operand<f16_t> {
-    half8_t v;
-    __device__ void set(const Eight<f16_t>& x, float) { __builtin_memcpy(&v, &x, 16); }
-};
-template <>
-struct Operand<float> {
-    Frag<2> v;
-    __device__ void set(const Eight<float>& x, float up) { v = split<2>(x.x, up); }
-};
-__device__ inline f32x4 product(const Operand<bf16_t>& a, const Operand<bf16_t>& b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
-}
-__device__ inline f32x4 product(const Operand<f16_t>& a, const Operand<f16_t>& b, f32x4 c) {
-    return mfma(a.v, b.v, c);
-}
-__device__ inline f32x4 product(const Operand<float>& a, const Operand<float>& b, f32x4 c) {
-    return multiply(a.v, b.v, c);
-}
-
 // Row r of a 16 x 16 block of X (in LDS) as the A operand of the four
 // FP32 products of a 16 x 16 x 16 one: step i contracts columns 4 g + i.
 __device__ inline f32x4 block_rows(const float* X, int lane) {

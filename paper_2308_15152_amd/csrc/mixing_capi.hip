@@ -274,12 +274,42 @@ int delta_emu_forward(const delta_emu_forward_t* args, hipStream_t stream) {
 
 int64_t delta_emu_backward_workspace(const delta_emu_backward_t* a) {
     if (a == nullptr) return SGEMM_EMU_ERR_NULL;
-    return SGEMM_EMU_ERR_UNSUPPORTED;
+    if (int rc = check_shape(*a)) return rc;
+    return delta_backward_workspace(*a);
 }
 
-int delta_emu_backward(const delta_emu_backward_t* a, hipStream_t) {
-    if (a == nullptr) return SGEMM_EMU_ERR_NULL;
-    return SGEMM_EMU_ERR_UNSUPPORTED;
+int delta_emu_backward(const delta_emu_backward_t* args, hipStream_t stream) {
+    if (args == nullptr) return SGEMM_EMU_ERR_NULL;
+    const delta_emu_backward_t& a = *args;
+    if (int rc = check_shape(a)) return rc;
+    if (a.batch == 0) return SGEMM_EMU_OK;
+    const bool packed = a.cu_seqlens != nullptr;
+    const int64_t batch = packed ? 1 : a.batch, e = dtype_bytes(a.dtype);
+    if (a.tokens > 0 && (!a.q.p || !a.k.p || !a.dq.p || !a.dk.p)) return SGEMM_EMU_ERR_NULL;
+    if (a.tokens > 0 && a.v_size > 0 && (!a.v.p || !a.d_o.p || !a.dv.p)) return SGEMM_EMU_ERR_NULL;
+    const Tensor q{a.q, batch, a.tokens, a.k_heads, a.k_size, e};
+    const Tensor k{a.k, batch, a.tokens, a.k_heads, a.k_size, e};
+    const Tensor v{a.v, batch, a.tokens, a.v_heads, a.v_size, e};
+    const Tensor g{a.g, batch, a.tokens, a.v_heads, 1, 4};
+    const Tensor beta{a.beta, batch, a.tokens, a.v_heads, 1, 4};
+    const Tensor d_o{a.d_o, batch, a.tokens, a.v_heads, a.v_size, e};
+    const Tensor dq{a.dq, batch, a.tokens, a.k_heads, a.k_size, e};
+    const Tensor dk{a.dk, batch, a.tokens, a.k_heads, a.k_size, e};
+    const Tensor dv{a.dv, batch, a.tokens, a.v_heads, a.v_size, e};
+    const Tensor dg{a.dg, batch, a.tokens, a.v_heads, 1, 4};
+    const Tensor dbeta{a.dbeta, batch, a.tokens, a.v_heads, 1, 4};
+    const __int128 states = (__int128)a.batch * a.v_heads * a.k_size * a.v_size * 4;
+    const int64_t need = delta_backward_workspace(a);
+    if (need > 0 && a.workspace == nullptr) return SGEMM_EMU_ERR_NULL;
+    if (need > 0 && (a.workspace_bytes < need || (uintptr_t)a.workspace % 256 != 0))
+        return SGEMM_EMU_ERR_DIM;
+    const Extent last = array(a.dfinal == a.dinitial ? nullptr : a.dfinal, states);
+    if (int rc = check_tensors({q, k, v, g, beta, d_o}, {dq, dk, dv, dg, dbeta},
+                               {array(a.initial, states), last,
+                                array(a.cu_seqlens, ((__int128)a.batch + 1) * 4)},
+                               {array(a.dinitial, states), array(a.workspace, need)}))
+        return rc;
+    return done(launch_delta_backward(a, stream));
 }
 
 }  // extern "C"
