@@ -107,9 +107,11 @@ int rotary_emu_table(int rows, int rot, double base, double factor, double origi
  * initial: states before the first tokens, or NULL (zero).
  * workspace: device memory, 256-byte aligned, at least what the _workspace query
  *   for the same arguments returns; its contents need not be kept.
- * Sizes: k_size <= 128, k_heads divides v_heads.  Empty sequences leave
+ * Sizes: k_size <= 128, v_size <= 65536, token strides <= 2^22 (of q, k, v, o
+ * and their gradients), k_heads divides v_heads.  Empty sequences leave
  * final = initial.
- * Errors: _DIM, _UNSUPPORTED (dtype, k_size, head counts, too many chunks for one launch),
+ * Errors: _DIM, _UNSUPPORTED (dtype, sizes and strides above, head counts, more than
+ * 2^22 chunks x value heads),
  * _NULL, _STRIDE, _ALIAS, _HIP.
  */
 typedef struct {

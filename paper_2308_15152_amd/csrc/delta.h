@@ -27,6 +27,8 @@ namespace sgemm_emu {
 
 constexpr int kDeltaMaxK = 128;  // largest key size
 constexpr int kDeltaChunk = 64;  // tokens of a chunk
+constexpr int kDeltaMaxV = 1 << 16;
+constexpr int64_t kDeltaMostStride = 1 << 22;  // of tokens, in elements
 // Chunks x value heads of one call: one block each, one launch.
 constexpr int64_t kDeltaMostTasks = 1 << 22;
 

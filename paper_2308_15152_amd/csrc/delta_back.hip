@@ -16,8 +16,7 @@ struct Layout {
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
     static constexpr int kRows = 4 * kSteps * 1024;
     static constexpr int kAtK = 0;
-    static constexpr int kAtKt = kAtK + kParts * kRows;
-    static constexpr int kAtQt = kAtKt + kParts * kRows;
+    static constexpr int kAtQt = kAtK + kParts * kRows;
     static constexpr int kAtTt = kAtQt + kParts * kRows;
     static constexpr int kAtPt = kAtTt + 2 * DeltaRecord::kMatrix;
     static constexpr int kAtF = kAtPt + 2 * DeltaRecord::kMatrix;
@@ -109,8 +108,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void delta_back_kernel(DeltaChunks 
         for (int i = 0; i < kMine; ++i) {
             const int unit = threadIdx.x + i * kThreads;
             if (kUnits % kThreads != 0 && unit >= kUnits) continue;
-            ku[i].template store<true, true>(to + L::kAtK, to + L::kAtKt, unit, kscale[i]);
-            qu[i].template store<false, true>(nullptr, to + L::kAtQt, unit, qscale[i]);
+            ku[i].store(to + L::kAtK, unit, kscale[i]);
+            qu[i].store(to + L::kAtQt, unit, qscale[i]);
         }
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
@@ -219,7 +218,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void delta_back_kernel(DeltaChunks 
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     a = multiply<true>(column_fragment<T, kK>(at + L::kAtQt, i, j, lane), bo[j], a);
-                    a = multiply<true>(column_fragment<T, kK>(at + L::kAtKt, i, j, lane), by[j], a);
+                    a = multiply<true>(column_fragment<T, kK>(at + L::kAtK, i, j, lane), by[j], a);
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) D[i][r] = __builtin_fmaf(a[r], s.down, decay * D[i][r]);

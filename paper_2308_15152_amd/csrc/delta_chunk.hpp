@@ -207,92 +207,159 @@ __device__ inline f32x4 product(const Operand<float>& a, const Operand<float>& b
 template <class T>
 constexpr int kPartsOf = sizeof(T) == 4 ? 2 : 1;
 
-// Rows of K or Q as fragments.  A thread takes 4 tokens x 8 elements: as rows
-// (A operand of products with S) two 8-byte pieces a token, as columns (A
-// operand of products that contract over tokens) 8 pieces of 4 tokens.  Lanes
-// of a fragment are permuted by its number, which spreads the pieces that
-// a wave writes at once over the banks.
+// LDS is shared by the block's waves: orders this wave's accesses to it around
+// the barrier, and leaves loads from memory in flight.
+__device__ inline void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Buffer descriptor of everything from p on: offsets below 2^31 are inside
+// what the caller may read or write, and kPastEnd is not: loads there return
+// zero, stores are dropped.
+constexpr uint32_t kPastEnd = 0x80000000;
+
+__device__ inline __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000);
+}
+template <int kBytes>
+struct Word;
+template <>
+struct Word<2> {
+    typedef uint16_t type;
+    __device__ static type load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+    }
+    __device__ static void store(type v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
+        __builtin_amdgcn_raw_buffer_store_b16(v, r, at, 0, 0);
+    }
+};
+template <>
+struct Word<4> {
+    typedef uint32_t type;
+    __device__ static type load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+    }
+    __device__ static void store(type v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
+        __builtin_amdgcn_raw_buffer_store_b32(v, r, at, 0, 0);
+    }
+};
+template <class T>
+__device__ inline T load_word(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    return __builtin_bit_cast(T, Word<sizeof(T)>::load(r, at));
+}
+template <class T>
+__device__ inline void store_word(T v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
+    Word<sizeof(T)>::store(__builtin_bit_cast(typename Word<sizeof(T)>::type, v), r, at);
+}
+
+// Place of lane l's 16 bytes in the fragment of step `step` of K's or Q's rows.
+// The permutation spreads over the banks what a wave writes at once (pieces of
+// 8 bytes, Unit below) and what it reads at once as columns.
+__device__ inline int slot(int lane, int step) {
+    return (lane ^ (step & 3) ^ ((lane >> 4) << 2)) * 16;
+}
+
+// Rows of K or Q as fragments in LDS.  A thread takes 4 tokens x 8 elements, in
+// two 8-byte pieces a token.
 template <class T, int kK>
 struct Unit {
+    static constexpr int kUnits = 16 * kK / 8;  // of a chunk
     Eight<T> x[4];
 
+    // rows: of the chunk's first token
     __device__ void load(const T* rows, int64_t stride, int unit, int count, int size, bool wide) {
         const int e = 8 * (unit % (kK / 8)), t = 4 * (unit / (kK / 8));
+        const __amdgpu_buffer_rsrc_t r = buffer_at(rows);
+        const uint32_t step = (uint32_t)stride * sizeof(T);
+        const uint32_t at = t * step + e * sizeof(T);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            x[i] = load_eight(rows + (t + i) * stride, e, size, t + i < count, wide);
-    }
-
-    // scale: of the four tokens
-    template <bool kRowsToo, bool kColumns>
-    __device__ void store(char* rows, char* columns, int unit, f32x4 scale) const {
-        constexpr int kParts = kPartsOf<T>, kSteps = kK / 32;
-        const int eight = unit % (kK / 8), four = unit / (kK / 8);
-        half4_t part[kParts][4][2];
+        for (int i = 0; i < 4; ++i) {
+            if (wide) {
+                const uint32_t off = t + i < count && e < size ? at + i * step : kPastEnd;
+                u32x4 w[sizeof(T) / 2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+                for (int n = 0; n < (int)sizeof(T) / 2; ++n)
+                    w[n] = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * n, 0, 0);
+                __builtin_memcpy(&x[i], w, sizeof(w));
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = to_f32(x[i].x[e]);
-                const _Float16 hi = (_Float16)(v * scale[i]);
-                part[0][i][e / 4][e % 4] = hi;
-                if (kParts == 2)
-                    part[kParts - 1][i][e / 4][e % 4] =
-                        (_Float16)__builtin_fmaf(v, scale[i], -(float)hi);
-            }
-        if (kRowsToo) {
-            const int step = eight / 4, half = (eight % 4) / 2, g = 2 * (eight % 2);
-#pragma unroll
-            for (int p = 0; p < kParts; ++p) {
-                char* to = rows + ((p * 4 + four / 4) * kSteps + step) * 1024 + half * 8;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const int lane = (g + b) * 16 + 4 * (four % 4) + i;
-                        *reinterpret_cast<half4_t*>(to + (lane ^ (step & 3)) * 16) = part[p][i][b];
-                    }
+                for (int n = 0; n < 8; ++n)
+                    x[i].x[n] = load_word<T>(r, t + i < count && e + n < size
+                                                    ? at + i * step + n * (uint32_t)sizeof(T)
+                                                    : kPastEnd);
             }
         }
-        if (kColumns) {
-            const int tile = eight / 2, step = four / 8, half = (four / 4) % 2, g = four % 4;
+    }
+
+    // scale: of the four tokens (float16 is taken as it is)
+    __device__ void store(char* rows, int unit, f32x4 scale) const {
+        constexpr int kParts = kPartsOf<T>, kSteps = kK / 32;
+        const int eight = unit % (kK / 8), four = unit / (kK / 8);
+        const int step = eight / 4, half = (eight % 4) / 2, g = 2 * (eight % 2);
+        char* to = rows + ((four / 4) * kSteps + step) * 1024 + half * 8;
 #pragma unroll
-            for (int p = 0; p < kParts; ++p) {
-                char* to = columns + ((p * (kK / 16) + tile) * 2 + step) * 1024 + half * 8;
+        for (int i = 0; i < 4; ++i) {
+            half4_t part[kParts][2];
+            if (__is_same(T, f16_t)) {
+                __builtin_memcpy(part, &x[i], 16);
+            } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int lane = g * 16 + 8 * (eight % 2) + e;
-                    half4_t v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = part[p][i][e / 4][e % 4];
-                    *reinterpret_cast<half4_t*>(to + (lane ^ (tile & 7)) * 16) = v;
+                    const float v = to_f32(x[i].x[e]);
+                    const _Float16 hi = (_Float16)(v * scale[i]);
+                    part[0][e / 4][e % 4] = hi;
+                    if (kParts == 2)
+                        part[kParts - 1][e / 4][e % 4] =
+                            (_Float16)__builtin_fmaf(v, scale[i], -(float)hi);
                 }
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int at = slot((g + b) * 16 + 4 * (four % 4) + i, step);
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+                    *reinterpret_cast<half4_t*>(to + p * 4 * kSteps * 1024 + at) = part[p][b];
             }
         }
     }
 };
 
+// Token tile `tile`, step `step` of those rows as an operand that contracts
+// over elements.
 template <class T, int kK>
-__device__ inline Frag<kPartsOf<T>> row_fragment(const char* rows, int tile, int step,
-                                                              int lane) {
-    constexpr int kParts = kPartsOf<T>;
-    Frag<kParts> f;
+__device__ inline Frag<kPartsOf<T>> row_fragment(const char* rows, int tile, int step, int lane) {
+    Frag<kPartsOf<T>> f;
 #pragma unroll
-    for (int p = 0; p < kParts; ++p)
+    for (int p = 0; p < kPartsOf<T>; ++p)
         f.part[p] = *reinterpret_cast<const half8_t*>(
-            rows + ((p * 4 + tile) * (kK / 32) + step) * 1024 + (lane ^ (step & 3)) * 16);
+            rows + ((p * 4 + tile) * (kK / 32) + step) * 1024 + slot(lane, step));
     return f;
 }
 
+// Elements 16 tile ... + 15, tokens of step `step` as an operand that contracts
+// over tokens: the same rows, read transposed.  Each group of 16 lanes names
+// four tokens' pieces of four elements (lane 4 a + b: token a, piece b) and
+// lane n receives element n of the four tokens.
 template <class T, int kK>
-__device__ inline Frag<kPartsOf<T>> column_fragment(const char* columns, int tile,
-                                                                 int step, int lane) {
-    constexpr int kParts = kPartsOf<T>;
-    Frag<kParts> f;
+__device__ inline Frag<kPartsOf<T>> column_fragment(const char* rows, int tile, int step,
+                                                    int lane) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    const int from = ((lane & 3) << 4) + ((lane >> 4) << 2) + ((lane >> 2) & 3);
+    Frag<kPartsOf<T>> f;
 #pragma unroll
-    for (int p = 0; p < kParts; ++p)
-        f.part[p] = *reinterpret_cast<const half8_t*>(
-            columns + ((p * (kK / 16) + tile) * 2 + step) * 1024 + (lane ^ (tile & 7)) * 16);
+    for (int p = 0; p < kPartsOf<T>; ++p) {
+        s16x4 v[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const char* at = rows + ((p * 4 + 2 * step + half) * (kK / 32) + tile / 2) * 1024 +
+                             slot(from, tile / 2) + 8 * (tile % 2);
+            v[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(s16x4*)at);
+        }
+        __builtin_memcpy(&f.part[p], v, 16);
+    }
     return f;
 }
 
@@ -305,5 +372,27 @@ __device__ inline Frag<N> matrix_fragment(const char* matrix, int at, int lane) 
             *reinterpret_cast<const half8_t*>(matrix + (p * 6 + at) * 1024 + lane * 16);
     return f;
 }
+
+// A piece of a record on its way to LDS, 16 bytes a thread and turn.
+template <int kBytes, int kThreads>
+struct Copy {
+    static constexpr int kPieces = kBytes / 16, kTurns = (kPieces + kThreads - 1) / kThreads;
+    u32x4 x[kTurns];
+    __device__ void load(const char* from, int thread) {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int at = thread + i * kThreads;
+            if (kPieces % kThreads == 0 || at < kPieces)
+                x[i] = reinterpret_cast<const u32x4*>(from)[at];
+        }
+    }
+    __device__ void store(char* to, int thread) const {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int at = thread + i * kThreads;
+            if (kPieces % kThreads == 0 || at < kPieces) reinterpret_cast<u32x4*>(to)[at] = x[i];
+        }
+    }
+};
 
 }  // namespace sgemm_emu

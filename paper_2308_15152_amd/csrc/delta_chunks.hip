@@ -21,6 +21,7 @@ hipError_t launch_delta_forward(const delta_emu_forward_t& a, hipStream_t stream
     c.record_bytes = DeltaRecord::kForward;
     c.chunks = (int)delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr);
     c.wide = delta_wide(a.dtype, a.k_size, {a.q, a.k});
+    c.wide_values = delta_wide(a.dtype, a.v_size, {a.v});
     if (hipError_t e = launch_delta_prep(c, stream)) return e;
     return launch_delta_chain(c, stream);
 }
@@ -40,7 +41,7 @@ BackwardParts backward_parts(const delta_emu_backward_t& a) {
     BackwardParts b;
     b.tasks = delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr) * a.v_heads;
     b.records = b.tasks * DeltaRecord::kBackward;
-    b.states = rounded(b.tasks * a.k_size * a.v_size * 4);
+    b.states = rounded(b.tasks * ((a.k_size + 15) / 16 * 16) * a.v_size * 4);
     b.updates = rounded(b.tasks * kDeltaChunk * a.v_size * 4);
     return b;
 }

@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             u.load(is_q ? q : k, is_q ? p.q.token : p.k.token, unit, at.count, p.k_size, p.wide);
             const f32x4 s = reinterpret_cast<const f32x4*>(
                 f + 64 * (is_q ? DeltaRecord::kQueryScale : DeltaRecord::kKeyScale))[unit / (kK / 8)];
-            u.template store<false, true>(nullptr, lds + (is_q ? L::kAtQt : L::kAtKt), unit, s);
+            u.store(lds + (is_q ? L::kAtQt : L::kAtKt), unit, s);
         }
         if (threadIdx.x < kC) {  // powers of two: exact
             small.key_down[threadIdx.x] = 1.0f / f[64 * DeltaRecord::kKeyScale + threadIdx.x];
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         const T* d_o = row_of<const T>(p.d_o, packed, at.n, at.span, h) + (int64_t)at.first * p.d_o.token;
         const float* u = p.updates + task * kC * p.v_size;
         const float* dy = p.dsides + task * kC * p.v_size;
-        const float* S = p.states + task * p.k_size * p.v_size;
+        const float* S = p.states + task * ((p.k_size + 15) / 16 * 16) * p.v_size;
         const float* D = p.dstates + task * p.k_size * p.v_size;
         const bool wide_f = p.v_size % 8 == 0;
 

@@ -184,6 +184,7 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
     if (g == 0) {
         const int t = 16 * wave + row;
         const double last = G[kC - 1];
+        if (__is_same(T, f16_t)) mine = qs = Scale{1.0f, 1.0f};  // taken as they are
         factors[64 * DeltaRecord::kKeyScale + t] = mine.up;
         factors[64 * DeltaRecord::kQueryScale + t] = qs.up;
         factors[64 * DeltaRecord::kRise + t] = expf((float)G[t]) * mine.down;

@@ -90,6 +90,13 @@ int check_sizes(const A& a) {
     return SGEMM_EMU_OK;
 }
 
+// The chunk kernels address a chunk's 64 rows of a head with 32-bit offsets.
+bool within_reach(std::initializer_list<sgemm_emu_view_t> views, int v_size) {
+    for (const sgemm_emu_view_t& v : views)
+        if (v.token > kDeltaMostStride) return false;
+    return v_size <= kDeltaMaxV;
+}
+
 // Every input present, every output apart, no output over an input.
 int check_tensors(std::initializer_list<Tensor> ins, std::initializer_list<Tensor> outs,
                   std::initializer_list<Extent> arrays_in, std::initializer_list<Extent> arrays_out) {
@@ -250,6 +257,7 @@ int delta_emu_forward(const delta_emu_forward_t* args, hipStream_t stream) {
     if (args == nullptr) return SGEMM_EMU_ERR_NULL;
     const delta_emu_forward_t& a = *args;
     if (int rc = check_shape(a)) return rc;
+    if (!within_reach({a.q, a.k, a.v, a.o}, a.v_size)) return SGEMM_EMU_ERR_UNSUPPORTED;
     if (a.batch == 0 || a.v_size == 0) return SGEMM_EMU_OK;
     const bool packed = a.cu_seqlens != nullptr;
     const int64_t batch = packed ? 1 : a.batch, e = dtype_bytes(a.dtype);
@@ -282,6 +290,8 @@ int delta_emu_backward(const delta_emu_backward_t* args, hipStream_t stream) {
     if (args == nullptr) return SGEMM_EMU_ERR_NULL;
     const delta_emu_backward_t& a = *args;
     if (int rc = check_shape(a)) return rc;
+    if (!within_reach({a.q, a.k, a.v, a.d_o, a.dq, a.dk, a.dv}, a.v_size))
+        return SGEMM_EMU_ERR_UNSUPPORTED;
     if (a.batch == 0) return SGEMM_EMU_OK;
     const bool packed = a.cu_seqlens != nullptr;
     const int64_t batch = packed ? 1 : a.batch, e = dtype_bytes(a.dtype);
