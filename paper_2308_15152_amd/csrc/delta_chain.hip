@@ -9,11 +9,13 @@
 // fast one such wave gets through its instructions, so it is left with those of the
 // chain only.  The block's other waves help: they bring K, Q, T, P and V of the next
 // chunk into LDS as fragments (each is loaded into registers a chunk ahead), and
-// make O from the S and U that the walking waves leave in LDS.  Two barriers a
-// chunk: after the first (A) the chunk's K and T are there, after the second (B)
-// its S and Q are:
-//   walking  A: V to registers, S split and put down.  B: U, put down; next S.
-//   helping  A: O of the last chunk finished; Q down.  B: Q S; next K, T, V, this P down.
+// make O from the S and U that the walking waves leave in LDS.
+//
+// One barrier a chunk (A): behind it the chunk's K, T, V and Q are there, and
+// the last chunk's U.  Inside a chunk a walking wave posts when its S is down and
+// its V is taken; the helpers wait for that before they read S and write the next V.  In
+// FP32, for whose two parts LDS holds Q only once, the post is a second barrier (B),
+// before which the chunk's Q goes down.
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
@@ -22,11 +24,12 @@ namespace {
 
 enum { kOutputs, kStates };  // what the walk writes: O, or S and U per chunk
 
-constexpr int kHelpers = 4;
-
-// LDS, in bytes.
+// LDS, in bytes, and the number of helping waves.
 template <class T, int kK, int kWalkers, int kMode>
 struct Layout {
+    static constexpr bool kPosts = sizeof(T) == 2;
+    // with eight helpers, four bring K, T and V and four Q and P
+    static constexpr int kHelpers = kMode == kOutputs && kPosts ? 8 : 4;
     static constexpr int kParts = kPartsOf<T>;  // of K and Q
     // of P, and of S and U where they make O: rounding them to fp16 alone costs
     // 2^-12 relative, unseen in a bfloat16 result (2^-8) but not in others
@@ -34,29 +37,36 @@ struct Layout {
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
     static constexpr int kRows = kParts * 4 * kSteps * 1024;  // K or Q
     static constexpr int kMatrices = 2 * DeltaRecord::kMatrix;
+    static constexpr int kBytesP = kMode == kOutputs ? kOut * DeltaRecord::kMatrix : 0;
     // two buffers of these
     static constexpr int kAtK = 0;
     static constexpr int kAtT = kAtK + kRows;
     static constexpr int kAtF = kAtT + kMatrices;
     static constexpr int kBuffer = kAtF + DeltaRecord::kFactorBytes;
-    // one of these
-    static constexpr int kAtV = 2 * kBuffer;
-    static constexpr int kEachV = kC * 16 * sizeof(T);
-    static constexpr int kAtQ = kAtV + kWalkers * kEachV;
+    // one or two of Q and P
+    static constexpr int kAtQ = 2 * kBuffer;
     static constexpr int kAtP = kAtQ + (kMode == kOutputs ? kRows : 0);
-    static constexpr int kBytesP = kMode == kOutputs ? kOut * DeltaRecord::kMatrix : 0;
-    static constexpr int kAtS = kAtP + kBytesP;
+    static constexpr int kBufferQ = kAtP + kBytesP - kAtQ;
+    // one of these
+    static constexpr int kAtV = kAtQ + (kPosts ? 2 : 1) * kBufferQ;
+    using V = Values<T, kWalkers, 256>;
+    static constexpr int kAtS = kAtV + kWalkers * V::kEach;
     static constexpr int kEachS = kOut * kSteps * 1024 + 256;  // and its scale
     static constexpr int kAtU = kAtS + (kMode == kOutputs ? kWalkers * kEachS : 0);
     static constexpr int kEachU = kC * 16 * 4;
-    static constexpr int kBytes = kAtU + (kMode == kOutputs ? kWalkers * kEachU : 0);
+    static constexpr int kBufferU = kMode == kOutputs ? kWalkers * kEachU : 0;  // one or two
+    static constexpr int kAtPosts = kAtU + (kPosts ? 2 : 1) * kBufferU;
+    static constexpr int kBytes = kAtPosts + 16 * kWalkers;
 };
 
 template <class T, int kK, int kWalkers, int kMode>
-__global__ __launch_bounds__(64 * (kWalkers + kHelpers), 1) void delta_chain_kernel(DeltaChunks p) {
+__global__ __launch_bounds__(64 * (kWalkers + Layout<T, kK, kWalkers, kMode>::kHelpers), 1)
+void delta_chain_kernel(DeltaChunks p) {
     using L = Layout<T, kK, kWalkers, kMode>;
-    constexpr int kOut = L::kOut;
+    constexpr int kOut = L::kOut, kHelpers = L::kHelpers;
+    constexpr bool kPosts = L::kPosts;
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);  // one each 4 ints: chunks posted
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -73,6 +83,7 @@ __global__ __launch_bounds__(64 * (kWalkers + kHelpers), 1) void delta_chain_ker
     const int col0 = slice * kWalkers * 16;
     const char* records = p.records + ((int64_t)first_chunk * p.v_heads + h) * p.record_bytes;
     const int64_t record_step = (int64_t)p.v_heads * p.record_bytes;
+    if (kPosts && threadIdx.x < kWalkers) posts[4 * threadIdx.x] = 0;
 
     if (wave < kWalkers) {
         const int col = col0 + 16 * wave + (lane & 15);
@@ -87,7 +98,7 @@ __global__ __launch_bounds__(64 * (kWalkers + kHelpers), 1) void delta_chain_ker
                 S[i][r] = p.initial && in && row < p.k_size
                               ? p.initial[state + (int64_t)row * p.v_size] : 0.0f;
             }
-        const char* v_at = lds + L::kAtV + wave * L::kEachV + lane * 4 * (int)sizeof(T);
+        const char* v_at = lds + L::kAtV + wave * L::V::kEach + lane * 4 * (int)sizeof(T);
         char* s_at = lds + L::kAtS + wave * L::kEachS;
         char* u_at = lds + L::kAtU + wave * L::kEachU + lane * 16;
 
@@ -129,7 +140,13 @@ __global__ __launch_bounds__(64 * (kWalkers + kHelpers), 1) void delta_chain_ker
             }
             if (kMode == kOutputs)
                 reinterpret_cast<float*>(s_at + kOut * L::kSteps * 1024)[lane] = ss.down;
-            lds_barrier();  // B
+            if (kPosts) {
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+                __hip_atomic_store(posts + 4 * wave, c + 1, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_WORKGROUP);
+            } else {
+                lds_barrier();  // B
+            }
             // beta (V - e^G K S)
             f32x4 x[4] = {};
 #pragma unroll
@@ -157,7 +174,9 @@ __global__ __launch_bounds__(64 * (kWalkers + kHelpers), 1) void delta_chain_ker
                         u[i] = multiply(matrix_fragment<2>(at + L::kAtT, lower_at(i, j), lane), b[j],
                                         u[i]);
                     u[i] *= factor(DeltaRecord::kT, i) * xs.down;
-                    if (kMode == kOutputs) *reinterpret_cast<f32x4*>(u_at + i * 1024) = u[i];
+                    if (kMode == kOutputs)
+                        *reinterpret_cast<f32x4*>(u_at + (kPosts ? (c & 1) * L::kBufferU : 0) +
+                                                  i * 1024) = u[i];
                 }
             }
             if (kMode == kStates) {
@@ -202,156 +221,123 @@ __global__ __launch_bounds__(64 * (kWalkers + kHelpers), 1) void delta_chain_ker
     }
 
     // ---- the helping waves
-    constexpr int kThreads = 64 * kHelpers;
-    constexpr int kMine = (Unit<T, kK>::kUnits + kThreads - 1) / kThreads;
-    const int id = threadIdx.x - 64 * kWalkers;
+    const int helper = wave - kWalkers;
+    const bool brings_k = helper < 4, brings_q = kMode == kOutputs && helper >= kHelpers - 4;
+    const int id = (threadIdx.x - 64 * kWalkers) & 255;
     const T* k = row_of<const T>(p.k, packed, n, span, kh);
     const T* q = row_of<const T>(p.q, packed, n, span, kh);
-    const T* v = row_of<const T>(p.v, packed, n, span, h);
-    // V goes down as the walking waves hold it: a thread takes 4 tokens x 4 columns
-    constexpr int kVUnits = 16 * 4 * kWalkers;
-    const int v_four = id / (4 * kWalkers), v_cols = id % (4 * kWalkers) * 4;
-
-    Unit<T, kK> ku[kMine], qu[kMine];
-    f32x4 kscale[kMine], qscale[kMine];
-    Copy<L::kMatrices, kThreads> tcopy;
-    Copy<DeltaRecord::kFactorBytes, kThreads> fcopy;
-    Copy<L::kBytesP == 0 ? 16 : L::kBytesP, kThreads> pcopy;
-    T vu[4][4];
+    const T* v = row_of<const T>(p.v, packed, n, span, h) + col0;
+    Rows<T, kK, 256> ku, qu;
+    Copy<L::kMatrices, 256> tcopy;
+    Copy<DeltaRecord::kFactorBytes, 256> fcopy;
+    Copy<L::kBytesP == 0 ? 16 : L::kBytesP, 256> pcopy;
+    typename L::V vu;
     const auto load_k = [&](int c) {
         const int count = min(kC, span.count - c * kC);
         const char* record = records + c * record_step;
-        const float* f = reinterpret_cast<const float*>(record);
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int unit = id + i * kThreads;
-            if (Unit<T, kK>::kUnits % kThreads != 0 && unit >= Unit<T, kK>::kUnits) continue;
-            ku[i].load(k + (int64_t)c * kC * p.k.token, p.k.token, unit, count, p.k_size, p.wide);
-            kscale[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kKeyScale)[unit / (kK / 8)];
-        }
+        ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, count, p.k_size, p.wide,
+                reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
         tcopy.load(record + DeltaRecord::kAtT, id);
         fcopy.load(record, id);
-        if (kVUnits >= kThreads || id < kVUnits) {
-            const __amdgpu_buffer_rsrc_t r = buffer_at(v + (int64_t)c * kC * p.v.token + col0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = 4 * v_four + i;
-                const uint32_t off = (t * (uint32_t)p.v.token + v_cols) * sizeof(T);
-                if (p.wide_values) {
-                    const uint32_t o = t < count && col0 + v_cols < p.v_size ? off : kPastEnd;
-                    if (sizeof(T) == 2) {
-                        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0);
-                        __builtin_memcpy(vu[i], &w, 8);
-                    } else {
-                        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0);
-                        __builtin_memcpy(vu[i], &w, 4 * sizeof(T));
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        vu[i][e] = load_word<T>(r, t < count && col0 + v_cols + e < p.v_size
-                                                       ? off + e * (uint32_t)sizeof(T) : kPastEnd);
-                }
-            }
-        }
+        vu.load(v + (int64_t)c * kC * p.v.token, p.v.token, count, p.v_size - col0, p.wide_values, id);
     };
     const auto store_k = [&](int c) {
         char* to = lds + (c & 1) * L::kBuffer;
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int unit = id + i * kThreads;
-            if (Unit<T, kK>::kUnits % kThreads != 0 && unit >= Unit<T, kK>::kUnits) continue;
-            ku[i].store(to + L::kAtK, unit, kscale[i]);
-        }
+        ku.store(to + L::kAtK, id);
         tcopy.store(to + L::kAtT, id);
         fcopy.store(to + L::kAtF, id);
-        if (kVUnits >= kThreads || id < kVUnits) {
-            char* at = lds + L::kAtV + v_cols / 16 * L::kEachV +
-                       (v_four / 4 * 64 + v_four % 4 * 16 + v_cols % 16) * 4 * sizeof(T);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const T w[4] = {vu[0][e], vu[1][e], vu[2][e], vu[3][e]};
-                __builtin_memcpy(at + e * 4 * sizeof(T), w, 4 * sizeof(T));
-            }
-        }
+        vu.store(lds + L::kAtV, id);
     };
     const auto load_q = [&](int c) {
-        const int count = min(kC, span.count - c * kC);
         const char* record = records + c * record_step;
-        const float* f = reinterpret_cast<const float*>(record);
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int unit = id + i * kThreads;
-            if (Unit<T, kK>::kUnits % kThreads != 0 && unit >= Unit<T, kK>::kUnits) continue;
-            qu[i].load(q + (int64_t)c * kC * p.q.token, p.q.token, unit, count, p.k_size, p.wide);
-            qscale[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryScale)[unit / (kK / 8)];
-        }
-        pcopy.load(record + DeltaRecord::kAtP, id);
+        qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, min(kC, span.count - c * kC), p.k_size,
+                p.wide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
     };
+    const auto load_p = [&](int c) { pcopy.load(records + c * record_step + DeltaRecord::kAtP, id); };
+    const auto buffer_q = [&](int c) { return lds + (kPosts ? (c & 1) * L::kBufferQ : 0); };
 
     // O: 16 columns and kOwn token tiles of a chunk to a wave
-    constexpr int kOwn = 4 * kWalkers / kHelpers;
-    const int helper = wave - kWalkers;
+    constexpr int kOwn = 4 * kWalkers / kHelpers < 1 ? 1 : 4 * kWalkers / kHelpers;
     const int block = helper % kWalkers, own = helper / kWalkers * kOwn;
+    const bool outputs = kMode == kOutputs && own < 4;
     const int col = col0 + 16 * block + (lane & 15);
     const bool in = col < p.v_size;
     T* o = kMode == kOutputs ? row_of<T>(p.o, packed, n, span, h) : nullptr;
-    f32x4 y[kOwn];
+    const uint32_t o_step = (uint32_t)p.o.token * sizeof(T);
+    const uint32_t o_at = in ? (16 * own + 4 * g) * o_step + col * (uint32_t)sizeof(T) : kPastEnd;
+    f32x4 y[kOwn], pf[kOwn];  // scale diag(e^G) Q S, and the scales of P's rows
+    const auto finish = [&](int c) {
+        const char* u_at = lds + L::kAtU + (kPosts ? (c & 1) * L::kBufferU : 0) +
+                           block * L::kEachU + lane * 16;
+        f32x4 u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(u_at + i * 1024);
+        const Scale us = scale_of(max_groups(largest(u)));
+        const Frag<kOut> b[2] = {split<kOut>(u[0], u[1], us.up), split<kOut>(u[2], u[3], us.up)};
+        const int count = min(kC, span.count - c * kC);
+        const __amdgpu_buffer_rsrc_t to = buffer_at(o + (int64_t)c * kC * p.o.token);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int tile = own + i;
+            f32x4 a{};
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (j <= tile / 2)
+                    a = multiply(matrix_fragment<kOut>(buffer_q(c) + L::kAtP, lower_at(tile, j), lane),
+                                 b[j], a);
+            a *= pf[i] * us.down;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * tile + 4 * g + r;
+                const uint32_t off = o_at + (16 * i + r) * o_step;
+                store_word(from_f32<T>(a[r] + y[i][r]), to,
+                           count == kC || t < count ? off : kPastEnd);
+            }
+        }
+    };
 
     if (chunks > 0) {
-        load_k(0);
-        store_k(0);
-        if (chunks > 1) load_k(1);
-        if (kMode == kOutputs) load_q(0);
+        if (brings_k) {
+            load_k(0);
+            store_k(0);
+            if (chunks > 1) load_k(1);
+        }
+        if (brings_q) {
+            load_q(0);
+            load_p(0);
+            if (kPosts) {
+                qu.store(buffer_q(0) + L::kAtQ, id);
+                if (chunks > 1) load_q(1);
+            }
+        }
     }
     for (int c = 0; c < chunks; ++c) {
         lds_barrier();  // A
-        const auto finish = [&](int c) {
-            const float* f = reinterpret_cast<const float*>(lds + (c & 1) * L::kBuffer + L::kAtF);
-            const char* u_at = lds + L::kAtU + block * L::kEachU + lane * 16;
-            f32x4 u[4];
+        if (outputs && c > 0) finish(c - 1);
+        if (kPosts) {
+            // every walking wave is in this chunk and posts on its way
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(u_at + i * 1024);
-            const Scale us = scale_of(max_groups(largest(u)));
-            const Frag<kOut> b[2] = {split<kOut>(u[0], u[1], us.up), split<kOut>(u[2], u[3], us.up)};
-            const int count = min(kC, span.count - c * kC);
-            const __amdgpu_buffer_rsrc_t to = buffer_at(o + (int64_t)c * kC * p.o.token);
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) {
-                const int tile = own + i;
-                f32x4 a{};
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (j <= tile / 2)
-                        a = multiply(matrix_fragment<kOut>(lds + L::kAtP, lower_at(tile, j), lane),
-                                     b[j], a);
-                const f32x4 pf = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kP)[4 * tile + g] * us.down;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int t = 16 * tile + 4 * g + r;
-                    store_word(from_f32<T>(__builtin_fmaf(pf[r], a[r], y[i][r])), to,
-                               in && t < count ? (t * (uint32_t)p.o.token + col) * (uint32_t)sizeof(T)
-                                               : kPastEnd);
+            for (int w = 0; w < kWalkers; ++w)
+                while (__hip_atomic_load(posts + 4 * w, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= c)
+                    __builtin_amdgcn_s_sleep(1);
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        } else {
+            if (brings_q) qu.store(lds + L::kAtQ, id);
+            lds_barrier();  // B
+            if (brings_q) {
+                pcopy.store(lds + L::kAtP, id);
+                if (c + 1 < chunks) {
+                    load_q(c + 1);
+                    load_p(c + 1);
                 }
             }
-        };
-        if (kMode == kOutputs) {
-            if (c > 0) finish(c - 1);
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                const int unit = id + i * kThreads;
-                if (Unit<T, kK>::kUnits % kThreads != 0 && unit >= Unit<T, kK>::kUnits) continue;
-                qu[i].store(lds + L::kAtQ, unit, qscale[i]);
-            }
         }
-        lds_barrier();  // B
-        if (kMode == kOutputs) {
-            pcopy.store(lds + L::kAtP, id);
-            if (c + 1 < chunks) load_q(c + 1);
+        if (brings_k && c + 1 < chunks) {
+            store_k(c + 1);
+            if (c + 2 < chunks) load_k(c + 2);
         }
-        if (c + 1 < chunks) store_k(c + 1);
-        if (c + 2 < chunks) load_k(c + 2);
-        if (kMode == kOutputs) {
+        if (outputs) {
             const float* f = reinterpret_cast<const float*>(lds + (c & 1) * L::kBuffer + L::kAtF);
             const char* s_at = lds + L::kAtS + block * L::kEachS;
             const float down = reinterpret_cast<const float*>(s_at + kOut * L::kSteps * 1024)[lane];
@@ -366,30 +352,45 @@ __global__ __launch_bounds__(64 * (kWalkers + kHelpers), 1) void delta_chain_ker
                         s_at + (r * L::kSteps + j) * 1024 + lane * 16);
 #pragma unroll
                 for (int i = 0; i < kOwn; ++i)
-                    y[i] = multiply(row_fragment<T, kK>(lds + L::kAtQ, own + i, j, lane), b, y[i]);
+                    y[i] = multiply(row_fragment<T, kK>(buffer_q(c) + L::kAtQ, own + i, j, lane), b,
+                                    y[i]);
             }
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i)
-                y[i] *= reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryRise)[4 * (own + i) + g] * down;
-            if (c + 1 == chunks) {
-                lds_barrier();  // the last U
-                finish(c);
+            for (int i = 0; i < kOwn; ++i) {
+                const int at = 4 * (own + i) + g;
+                y[i] *= reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryRise)[at] * down;
+                pf[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kP)[at];
             }
         }
+        if (kPosts && brings_q) {
+            // this chunk's P and the next one's Q: the other buffer's P is in use
+            // until the next barrier
+            pcopy.store(buffer_q(c) + L::kAtP, id);
+            if (c + 1 < chunks) {
+                load_p(c + 1);
+                qu.store(buffer_q(c + 1) + L::kAtQ, id);
+                if (c + 2 < chunks) load_q(c + 2);
+            }
+        }
+    }
+    if (kMode == kOutputs && chunks > 0) {
+        lds_barrier();  // the last U
+        if (outputs) finish(chunks - 1);
     }
 }
 
 template <class T, int kK, int kWalkers, int kMode>
 hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
-    constexpr int kBytes = Layout<T, kK, kWalkers, kMode>::kBytes;
-    static_assert(kBytes <= 160 * 1024, "LDS of a CU");
+    using L = Layout<T, kK, kWalkers, kMode>;
+    static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
     const int64_t slices = (a.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
     const void* kernel = reinterpret_cast<const void*>(delta_chain_kernel<T, kK, kWalkers, kMode>);
-    if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes))
+    if (hipError_t e =
+            hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
     hipLaunchKernelGGL((delta_chain_kernel<T, kK, kWalkers, kMode>),
                        dim3((unsigned)(slices * a.v_heads * a.batch)),
-                       dim3(64 * (kWalkers + kHelpers)), kBytes, stream, a);
+                       dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
 }
 

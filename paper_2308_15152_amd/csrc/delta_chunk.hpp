@@ -273,22 +273,29 @@ struct Unit {
         const int e = 8 * (unit % (kK / 8)), t = 4 * (unit / (kK / 8));
         const __amdgpu_buffer_rsrc_t r = buffer_at(rows);
         const uint32_t step = (uint32_t)stride * sizeof(T);
-        const uint32_t at = t * step + e * sizeof(T);
+        if (wide) {
+            uint32_t at = e < size ? t * step + e * (uint32_t)sizeof(T) : kPastEnd;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (wide) {
-                const uint32_t off = t + i < count && e < size ? at + i * step : kPastEnd;
+            for (int i = 0; i < 4; ++i, at += step) {  // past the end stays past it
+                const uint32_t off = count == kC || t + i < count ? at : kPastEnd;
                 u32x4 w[sizeof(T) / 2];
 #pragma unroll
                 for (int n = 0; n < (int)sizeof(T) / 2; ++n)
                     w[n] = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * n, 0, 0);
                 __builtin_memcpy(&x[i], w, sizeof(w));
-            } else {
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                Eight<T> y;
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
-                    x[i].x[n] = load_word<T>(r, t + i < count && e + n < size
-                                                    ? at + i * step + n * (uint32_t)sizeof(T)
-                                                    : kPastEnd);
+                    y.x[n] = load_word<T>(r, t + i < count && e + n < size
+                                                 ? (t + i) * step + (e + n) * (uint32_t)sizeof(T)
+                                                 : kPastEnd);
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    if (n == i) x[n] = y;
             }
         }
     }
@@ -391,6 +398,89 @@ struct Copy {
         for (int i = 0; i < kTurns; ++i) {
             const int at = thread + i * kThreads;
             if (kPieces % kThreads == 0 || at < kPieces) reinterpret_cast<u32x4*>(to)[at] = x[i];
+        }
+    }
+};
+
+// A chunk's rows of K or Q on their way to LDS, with their scales.
+template <class T, int kK, int kThreads>
+struct Rows {
+    using U = Unit<T, kK>;
+    static constexpr int kMine = (U::kUnits + kThreads - 1) / kThreads;
+    U u[kMine];
+    f32x4 scale[kMine];
+    __device__ void load(const T* rows, int64_t stride, int count, int size, bool wide,
+                         const float* scales, int thread) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int unit = thread + i * kThreads;
+            if (U::kUnits % kThreads != 0 && unit >= U::kUnits) continue;
+            u[i].load(rows, stride, unit, count, size, wide);
+            if (!__is_same(T, f16_t))
+                scale[i] = reinterpret_cast<const f32x4*>(scales)[unit / (kK / 8)];
+        }
+    }
+    __device__ void store(char* to, int thread) const {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int unit = thread + i * kThreads;
+            if (U::kUnits % kThreads != 0 && unit >= U::kUnits) continue;
+            u[i].store(to, unit, scale[i]);
+        }
+    }
+};
+
+// Columns of V or dO on their way to LDS, where they lie as the waves that own
+// 16 columns hold them: 4 tokens of a column together.  A thread takes 4
+// tokens x 4 columns of 16 kBlocks ones.
+template <class T, int kBlocks, int kThreads>
+struct Values {
+    static constexpr int kUnits = 16 * 4 * kBlocks;
+    static constexpr int kEach = kC * 16 * sizeof(T);  // bytes of a block of 16 columns
+    static constexpr int kMine = (kUnits + kThreads - 1) / kThreads;
+    T x[kMine][4][4];
+    // rows: of the chunk's first token and first column; size: columns there are
+    __device__ void load(const T* rows, int64_t stride, int count, int size, bool wide, int thread) {
+        const __amdgpu_buffer_rsrc_t r = buffer_at(rows);
+        const uint32_t step = (uint32_t)stride * sizeof(T);
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) {
+            const int unit = thread + m * kThreads;
+            if (kUnits % kThreads != 0 && unit >= kUnits) continue;
+            const int t = unit / (4 * kBlocks) * 4, c = unit % (4 * kBlocks) * 4;
+            uint32_t at = c < size ? t * step + c * (uint32_t)sizeof(T) : kPastEnd;
+#pragma unroll
+            for (int i = 0; i < 4; ++i, at += step) {
+                if (wide) {
+                    const uint32_t off = count == kC || t + i < count ? at : kPastEnd;
+                    if (sizeof(T) == 2) {
+                        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+                        __builtin_memcpy(x[m][i], &w, 8);
+                    } else {
+                        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+                        __builtin_memcpy(x[m][i], &w, 4 * sizeof(T));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[m][i][e] = load_word<T>(r, t + i < count && c + e < size
+                                                         ? at + e * (uint32_t)sizeof(T) : kPastEnd);
+                }
+            }
+        }
+    }
+    __device__ void store(char* to, int thread) const {
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) {
+            const int unit = thread + m * kThreads;
+            if (kUnits % kThreads != 0 && unit >= kUnits) continue;
+            const int four = unit / (4 * kBlocks), c = unit % (4 * kBlocks) * 4;
+            char* at = to + c / 16 * kEach + (four / 4 * 64 + four % 4 * 16 + c % 16) * 4 * sizeof(T);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const T w[4] = {x[m][0][e], x[m][1][e], x[m][2][e], x[m][3][e]};
+                __builtin_memcpy(at + e * 4 * sizeof(T), w, 4 * sizeof(T));
+            }
         }
     }
 };
