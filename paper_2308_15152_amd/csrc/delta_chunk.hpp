@@ -149,26 +149,69 @@ __device__ inline Place place_of(const int* cu, int c, int batch, int tokens) {
     return p;
 }
 
-// Eight consecutive elements of a row, from element e on; zero at `size` and
-// after, and everywhere if !in.
+// Buffer descriptor of everything from p on: offsets below 2^31 are inside
+// what the caller may read or write, and kPastEnd is not: loads there return
+// zero, stores are dropped.
+constexpr uint32_t kPastEnd = 0x80000000;
+
+__device__ inline __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000);
+}
+template <int kBytes>
+struct Word;
+template <>
+struct Word<2> {
+    typedef uint16_t type;
+    __device__ static type load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+    }
+    __device__ static void store(type v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
+        __builtin_amdgcn_raw_buffer_store_b16(v, r, at, 0, 0);
+    }
+};
+template <>
+struct Word<4> {
+    typedef uint32_t type;
+    __device__ static type load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+        return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+    }
+    __device__ static void store(type v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
+        __builtin_amdgcn_raw_buffer_store_b32(v, r, at, 0, 0);
+    }
+};
+template <class T>
+__device__ inline T load_word(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    return __builtin_bit_cast(T, Word<sizeof(T)>::load(r, at));
+}
+template <class T>
+__device__ inline void store_word(T v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
+    Word<sizeof(T)>::store(__builtin_bit_cast(typename Word<sizeof(T)>::type, v), r, at);
+}
+
+// Eight consecutive elements of a row.
 template <class T>
 struct Eight {
     T x[8];
 };
 
+// Elements e ... e + 7 of the row that starts at byte `row` of r; zero at `size`
+// and after, and everywhere if !in.
 template <class T>
-__device__ inline Eight<T> load_eight(const T* row, int e, int size, bool in, bool wide) {
+__device__ inline Eight<T> load_eight(__amdgpu_buffer_rsrc_t r, uint32_t row, int e, int size,
+                                      bool in, bool wide) {
     Eight<T> v;
+    const uint32_t at = row + e * (uint32_t)sizeof(T);
     if (wide) {  // size is a multiple of 8, the row 16-byte aligned
-        u32x4 w[sizeof(T) / 2] = {};
-        if (in && e < size)
+        u32x4 w[sizeof(T) / 2];
+        const uint32_t off = in && e < size ? at : kPastEnd;
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-                w[i] = reinterpret_cast<const u32x4*>(row + e)[i];
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            w[i] = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * i, 0, 0);
         __builtin_memcpy(&v, w, sizeof(v));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v.x[i] = in && e + i < size ? row[e + i] : from_f32<T>(0.0f);
+        for (int i = 0; i < 8; ++i)
+            v.x[i] = load_word<T>(r, in && e + i < size ? at + i * (uint32_t)sizeof(T) : kPastEnd);
     }
     return v;
 }
@@ -213,45 +256,6 @@ __device__ inline void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
-// Buffer descriptor of everything from p on: offsets below 2^31 are inside
-// what the caller may read or write, and kPastEnd is not: loads there return
-// zero, stores are dropped.
-constexpr uint32_t kPastEnd = 0x80000000;
-
-__device__ inline __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000);
-}
-template <int kBytes>
-struct Word;
-template <>
-struct Word<2> {
-    typedef uint16_t type;
-    __device__ static type load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-        return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
-    }
-    __device__ static void store(type v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
-        __builtin_amdgcn_raw_buffer_store_b16(v, r, at, 0, 0);
-    }
-};
-template <>
-struct Word<4> {
-    typedef uint32_t type;
-    __device__ static type load(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-        return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
-    }
-    __device__ static void store(type v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
-        __builtin_amdgcn_raw_buffer_store_b32(v, r, at, 0, 0);
-    }
-};
-template <class T>
-__device__ inline T load_word(__amdgpu_buffer_rsrc_t r, uint32_t at) {
-    return __builtin_bit_cast(T, Word<sizeof(T)>::load(r, at));
-}
-template <class T>
-__device__ inline void store_word(T v, __amdgpu_buffer_rsrc_t r, uint32_t at) {
-    Word<sizeof(T)>::store(__builtin_bit_cast(typename Word<sizeof(T)>::type, v), r, at);
 }
 
 // Place of lane l's 16 bytes in the fragment of step `step` of K's or Q's rows.

@@ -53,7 +53,7 @@ struct Layout {
     static constexpr int kEndB = kAtFragments + 4 * 2 * DeltaRecord::kMatrix;
     static constexpr int kAtSmall = kEndA > kEndB ? kEndA : kEndB;
     struct Small {
-        double G[kC];
+        double G[kC];  // (the arrays stay 16-byte aligned)
         float beta[kC], key_down[kC], query_down[kC];
         union {
             float down[3][kC];   // inverse row scales of dO, dY, U
@@ -157,28 +157,20 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             small.query_down[threadIdx.x] = 1.0f / f[64 * DeltaRecord::kQueryScale + threadIdx.x];
         }
     }
-    f32x4 kd[kOwn], qd[kOwn], dq[kOwn], dk[kOwn];
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = 16 * (own + i) + 4 * g + r;
-            kd[i][r] = kin && t < at.count ? to_f32(k[(int64_t)t * p.k.token + ke]) : 0.0f;
-            qd[i][r] = kin && t < at.count ? to_f32(q[(int64_t)t * p.q.token + ke]) : 0.0f;
-            dq[i][r] = dk[i][r] = 0.0f;
-        }
-
+    f32x4 dq[kOwn] = {}, dk[kOwn] = {};
     // rows wave % 4 of Q K^T (waves 0 to 3) and K K^T, for the decays' gradient
     f32x4 kk[4] = {};
     if (p.dg.p) {
         const int mt = wave % 4;
         const auto load_tile = [&](const T* from, int64_t stride, int i, Operand<T>(&f)[L::kSteps]) {
             const int t = 16 * i + row;
+            const __amdgpu_buffer_rsrc_t r = buffer_at(from);
             Eight<T> x[L::kSteps];
             float m = 0.0f;
 #pragma unroll
             for (int j = 0; j < L::kSteps; ++j) {
-                x[j] = load_eight(from + t * stride, 32 * j + 8 * g, p.k_size, t < at.count, p.wide);
+                x[j] = load_eight<T>(r, t * (uint32_t)stride * (uint32_t)sizeof(T), 32 * j + 8 * g,
+                                     p.k_size, t < at.count, p.wide);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(to_f32(x[j].x[e])));
             }
@@ -202,6 +194,11 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
     }
 
     for (int h = kh * group; h < (kh + 1) * group; ++h) {
+        // Everything that depends on the lane is formed again for every head:
+        // kept from one to the next, some 250 LDS addresses would be in scratch.
+        int lane = threadIdx.x & 63;
+        __asm__ volatile("" : "+v"(lane));
+        const int row = lane & 15, g = lane >> 4;
         const int64_t task = (int64_t)c * p.v_heads + h;
         __syncthreads();  // the last head's values are used
         if (wave == 0) {
@@ -233,6 +230,8 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         f32x4 e1[kOwn] = {}, e2[kOwn] = {}, e3[kOwn] = {}, m[4] = {};
         float sd = 0.0f;
         for (int v0 = 0; v0 < p.v_size; v0 += kVBlock) {
+            __asm__ volatile("" : "+v"(lane));
+            const int row = lane & 15, g = lane >> 4;
             __syncthreads();  // the last block's fragments are used
             // dO, dY and U: 12 tiles of 16 rows, one wave each
             for (int job = wave; job < 12; job += kWaves) {
@@ -262,25 +261,26 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
                     Eight<T> x[kVSteps];
 #pragma unroll
                     for (int j = 0; j < kVSteps; ++j)
-                        x[j] = load_eight(d_o + (int64_t)t * p.d_o.token, v0 + 32 * j + 8 * g,
-                                          p.v_size, t < at.count, p.wide_values);
+                        x[j] = load_eight<T>(buffer_at(d_o), t * (uint32_t)p.d_o.token * (uint32_t)sizeof(T),
+                                             v0 + 32 * j + 8 * g, p.v_size, t < at.count,
+                                             p.wide_values);
                     put(std::integral_constant<int, L::kParts>{}, x, lds + L::kAtDo, small.down[0]);
                 } else {
                     const float* from = which == 1 ? dy : u;
                     Eight<float> x[kVSteps];
 #pragma unroll
                     for (int j = 0; j < kVSteps; ++j)
-                        x[j] = load_eight(from + (int64_t)t * p.v_size, v0 + 32 * j + 8 * g,
-                                          p.v_size, true, wide_f);
+                        x[j] = load_eight<float>(buffer_at(from), 4u * t * p.v_size,
+                                                 v0 + 32 * j + 8 * g, p.v_size, true, wide_f);
                     put(std::integral_constant<int, 2>{}, x, lds + (which == 1 ? L::kAtDy : L::kAtU),
                         small.down[which]);
                     if (which == 1) {
                         float sum = 0.0f;
 #pragma unroll
                         for (int j = 0; j < kVSteps; ++j) {
-                            const Eight<T> y = load_eight(v + (int64_t)t * p.v.token,
-                                                          v0 + 32 * j + 8 * g, p.v_size,
-                                                          t < at.count, p.wide_values);
+                            const Eight<T> y = load_eight<T>(
+                                buffer_at(v), t * (uint32_t)p.v.token * (uint32_t)sizeof(T),
+                                v0 + 32 * j + 8 * g, p.v_size, t < at.count, p.wide_values);
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
                                 sum = __builtin_fmaf(x[j].x[e], to_f32(y.x[e]), sum);
@@ -296,8 +296,10 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             float smax = 0.0f, dmax = 0.0f;
 #pragma unroll
             for (int j = 0; j < kVSteps; ++j) {
-                sx[j] = load_eight(S + (int64_t)ke * p.v_size, v0 + 32 * j + 8 * g, p.v_size, kin, wide_f);
-                dx[j] = load_eight(D + (int64_t)ke * p.v_size, v0 + 32 * j + 8 * g, p.v_size, kin, wide_f);
+                sx[j] = load_eight<float>(buffer_at(S), 4u * ke * p.v_size, v0 + 32 * j + 8 * g,
+                                          p.v_size, kin, wide_f);
+                dx[j] = load_eight<float>(buffer_at(D), 4u * ke * p.v_size, v0 + 32 * j + 8 * g,
+                                          p.v_size, kin, wide_f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     smax = fmaxf(smax, fabsf(sx[j].x[e]));
@@ -306,6 +308,9 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
                 }
             }
             const Scale ss = scale_of(max_groups(smax)), ds = scale_of(max_groups(dmax));
+            Frag<2> sb[kVSteps];
+#pragma unroll
+            for (int j = 0; j < kVSteps; ++j) sb[j] = split<2>(sx[j].x, ss.up);
             __syncthreads();
             const auto fragment = [&](auto parts, int from, int i, int j) {
                 constexpr int kN = decltype(parts)::value;
@@ -318,27 +323,31 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             };
             constexpr std::integral_constant<int, L::kParts> one{};
             constexpr std::integral_constant<int, 2> two{};
-            {
-                f32x4 a1[kOwn] = {}, a2[kOwn] = {}, a3[kOwn] = {};
+            // (the barriers to the scheduler keep few values alive at a time)
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                f32x4 a1{}, a2{};
 #pragma unroll
                 for (int j = 0; j < kVSteps; ++j) {
-                    const Frag<2> sb = split<2>(sx[j].x, ss.up), db = split<2>(dx[j].x, ds.up);
-#pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        a1[i] = multiply(fragment(one, L::kAtDo, own + i, j), sb, a1[i]);
-                        a2[i] = multiply(fragment(two, L::kAtDy, own + i, j), sb, a2[i]);
-                        a3[i] = multiply(fragment(two, L::kAtU, own + i, j), db, a3[i]);
-                    }
+                    a1 = multiply(fragment(one, L::kAtDo, own + i, j), sb[j], a1);
+                    a2 = multiply(fragment(two, L::kAtDy, own + i, j), sb[j], a2);
                 }
+                const int t = 16 * (own + i) + 4 * g;
+                e1[i] += a1 * *reinterpret_cast<const f32x4*>(small.down[0] + t) * ss.down;
+                e2[i] += a2 * *reinterpret_cast<const f32x4*>(small.down[1] + t) * ss.down;
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
-                for (int i = 0; i < kOwn; ++i)
+            for (int j = 0; j < kVSteps; ++j) sb[j] = split<2>(dx[j].x, ds.up);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int t = 16 * (own + i) + 4 * g + r;
-                        e1[i][r] = __builtin_fmaf(a1[i][r], small.down[0][t] * ss.down, e1[i][r]);
-                        e2[i][r] = __builtin_fmaf(a2[i][r], small.down[1][t] * ss.down, e2[i][r]);
-                        e3[i][r] = __builtin_fmaf(a3[i][r], small.down[2][t] * ds.down, e3[i][r]);
-                    }
+            for (int i = 0; i < kOwn; ++i) {
+                f32x4 a3{};
+#pragma unroll
+                for (int j = 0; j < kVSteps; ++j)
+                    a3 = multiply(fragment(two, L::kAtU, own + i, j), sb[j], a3);
+                const int t = 16 * (own + i) + 4 * g;
+                e3[i] += a3 * *reinterpret_cast<const f32x4*>(small.down[2] + t) * ds.down;
+                __builtin_amdgcn_sched_barrier(0);
             }
             // rows wave % 4 of dO U^T (waves 0 to 3) and dY U^T
             const int mt = wave % 4;
@@ -359,6 +368,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
                 for (int r = 0; r < 4; ++r)
                     m[i][r] = __builtin_fmaf(a[r], small.down[wave < 4 ? 0 : 1][16 * mt + 4 * g + r] * cd,
                                              m[i][r]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         __syncthreads();  // dO, dY and U are used
@@ -415,6 +425,16 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         }
         __syncthreads();
         const double last = small.G[kC - 1];
+            // this lane's element of K or Q at row 16 i + 4 g + r, from the fragments
+            const auto element = [&](const char* rows, const float* down, int i, int r) {
+                const char* from = rows + (i * L::kSteps + tile / 2) * 1024 +
+                                   slot(((row >> 2) << 4) + 4 * g + r, tile / 2) + 8 * (tile % 2) +
+                                   2 * (row & 3);
+                float x = (float)*reinterpret_cast<const _Float16*>(from);
+                if (L::kParts == 2)
+                    x += (float)*reinterpret_cast<const _Float16*>(from + 4 * L::kSteps * 1024);
+                return x * down[16 * i + 4 * g + r];
+            };
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
             const int ti = own + i;
@@ -437,6 +457,8 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int t = 16 * ti + 4 * g + r;
+                const float kd = element(lds + L::kAtKt, small.key_down, ti, r);
+                const float qd = element(lds + L::kAtQt, small.query_down, ti, r);
                 const float rise = expf((float)small.G[t]);
                 const float tail = expf((float)(last - small.G[t]));
                 const float de = p.scale * rise * e1[i][r], we = rise * e2[i][r];
@@ -446,13 +468,14 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
                 dq[i][r] += __builtin_fmaf(small.m_down[0][t], a[0][r], de);
                 dk[i][r] += bt * w +
                             (te + (small.m_down[2][t] * a[2][r] - small.m_down[3][t] * a[3][r]));
-                const float sums[3] = {sum_row(kd[i][r] * w),
-                                       sum_row(__builtin_fmaf(qd[i][r], de, -(bt * kd[i][r] * we))),
-                                       sum_row(kd[i][r] * te)};
+                const float sums[3] = {sum_row(kd * w),
+                                       sum_row(__builtin_fmaf(qd, de, -(bt * kd * we))),
+                                       sum_row(kd * te)};
                 if (row == 0)
 #pragma unroll
                     for (int n = 0; n < 3; ++n) small.part[n][tile][t] = sums[n];
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) sd += __shfl_xor(sd, d, 64);

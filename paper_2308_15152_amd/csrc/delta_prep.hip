@@ -116,11 +116,13 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
     Scale ks[4], qs, mine;
     auto load_tile = [&](const T* from, int64_t stride, int tile, Operand<T>(&f)[kSteps], Scale& s) {
         const int t = 16 * tile + row;
+        const __amdgpu_buffer_rsrc_t r = buffer_at(from);
         Eight<T> x[kSteps];
         float m = 0.0f;
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-            x[j] = load_eight(from + t * stride, 32 * j + 8 * g, p.k_size, t < at.count, p.wide);
+            x[j] = load_eight<T>(r, t * (uint32_t)stride * (uint32_t)sizeof(T), 32 * j + 8 * g, p.k_size,
+                                 t < at.count, p.wide);
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(to_f32(x[j].x[i])));
         }

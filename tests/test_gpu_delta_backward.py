@@ -8,7 +8,9 @@ tokens terms q.dq and k.dk that largely cancel, so its error goes with those:
 the same factor of its own norm plus 8 (= sqrt 64) times theirs.  dinitial is a
 sum over tokens of scale q do^T and -k dv^T (as it leaves a chunk), whose
 rounding goes with the norm of the terms where they cancel to a few values:
-that norm is added to its own."""
+that norm is added to its own; likewise for dbeta, a difference of sums of
+dY v and K (S dY) over the value's elements, the norm of the terms dY v (dY = dv /
+beta)."""
 import math
 
 import pytest
@@ -22,6 +24,11 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 NAMES = ("dq", "dk", "dv", "dg", "dbeta", "dinitial")
+
+
+@pytest.fixture(autouse=True)
+def seeded():
+    torch.manual_seed(11)
 
 
 def check(got, want, x, do, tokens, dtype):
@@ -42,6 +49,9 @@ def check(got, want, x, do, tokens, dtype):
             size = x[0].shape[-1] ** -0.5
             tol += c * math.hypot(size * float(do.double().norm() * q.norm(dim=-1).max()),
                                   float(want[2].norm() * k.norm(dim=-1).max()))
+        if name == "dbeta" and tokens > 0:
+            dy = want[2] / x[4].double().clamp_min(1e-3)[..., None]
+            tol += c * float((dy * x[2].double()).norm())
         if rounded and dtype == torch.float16:
             tol += 2.0 ** -25 * math.sqrt(b.numel())
         off = float((a - b).norm())

@@ -20,6 +20,11 @@ DEV = "cuda:0"
 UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 
 
+@pytest.fixture(autouse=True)
+def seeded():
+    torch.manual_seed(11)
+
+
 def near(got, want, tokens, dtype=torch.float32):
     got, want = got.cpu().double(), want.detach()
     assert got.shape == want.shape

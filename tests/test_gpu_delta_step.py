@@ -16,6 +16,11 @@ DEV = "cuda:0"
 UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 
 
+@pytest.fixture(autouse=True)
+def seeded():
+    torch.manual_seed(11)
+
+
 def inputs(b, t, hk, hv, ks, vs, dtype, seed=0, decay=1.0):
     g = torch.Generator().manual_seed(seed)
 
