@@ -2,43 +2,65 @@
 // the gradient D of the state after the chunk:
 //   dU = P^T dO + diag(e^{G_64 - G}) K D,   dY = T^T dU,   dV = diag(beta) dY,
 //   D before = e^{G_64} D + scale (diag(e^G) Q)^T dO - (diag(e^G) K)^T dV.
-// Columns are independent here too: laid out, staged and bound like the walk
-// forward (delta_chain.hip).  Leaves D after and dY of every chunk.
+// Columns are independent here too, and the work is shared out as on the way
+// forward (delta_chain.hip): walking waves carry 16 columns of D each and
+// do what waits for D; helping waves bring K and T^T of the next chunk, and make
+// what does not wait, P^T dO and the product with Q, a chunk ahead from Q, P^T and dO,
+// which they bring two chunks ahead.  Leaves D after and dY of every chunk.
+//
+// One barrier a chunk (A).  Inside a chunk a walking wave posts when it has taken
+// its two products; then the helpers put down the next ones.  In FP32, for whose
+// two parts LDS holds Q only once, the post is a second barrier (B), before which
+// the helpers have read the Q that they overwrite after it.
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
 
 namespace {
 
-template <class T, int kK>
+// LDS, in bytes, and the number of helping waves.
+template <class T, int kK, int kWalkers>
 struct Layout {
+    static constexpr bool kPosts = sizeof(T) == 2;
+    // with eight helpers, four bring K and T^T and four Q, P^T and dO
+    static constexpr int kHelpers = kPosts ? 8 : 4;
     static constexpr int kParts = kPartsOf<T>;
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
-    static constexpr int kRows = 4 * kSteps * 1024;
+    static constexpr int kRows = kParts * 4 * kSteps * 1024;
+    static constexpr int kMatrix = 2 * DeltaRecord::kMatrix;
+    // two buffers of these
     static constexpr int kAtK = 0;
-    static constexpr int kAtQt = kAtK + kParts * kRows;
-    static constexpr int kAtTt = kAtQt + kParts * kRows;
-    static constexpr int kAtPt = kAtTt + 2 * DeltaRecord::kMatrix;
-    static constexpr int kAtF = kAtPt + 2 * DeltaRecord::kMatrix;
-    static constexpr int kBytes = kAtF + DeltaRecord::kFactorBytes;
-    static constexpr int kBuffers = 2 * kBytes <= 160 * 1024 ? 2 : 1;
+    static constexpr int kAtTt = kAtK + kRows;
+    static constexpr int kAtF = kAtTt + kMatrix;
+    static constexpr int kBuffer = kAtF + DeltaRecord::kFactorBytes;
+    // one or two of these
+    static constexpr int kAtQ = 0;
+    static constexpr int kAtPt = kAtQ + kRows;
+    static constexpr int kAtFq = kAtPt + kMatrix;
+    static constexpr int kAtDo = kAtFq + DeltaRecord::kFactorBytes;
+    using V = Values<T, kWalkers, 256>;
+    static constexpr int kBufferQ = kAtDo + kWalkers * V::kEach;
+    static constexpr int kAtQs = 2 * kBuffer;
+    // the products, as the walking waves hold them: 4 tiles and kTiles tiles
+    static constexpr int kAtProducts = kAtQs + (kPosts ? 2 : 1) * kBufferQ;
+    static constexpr int kEach = (4 + kTiles) * 1024;
+    static constexpr int kAtPosts = kAtProducts + kWalkers * kEach;
+    static constexpr int kBytes = kAtPosts + 16 * kWalkers;
 };
 
-template <class T, int kK, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 1) void delta_back_kernel(DeltaChunks p) {
-    using L = Layout<T, kK>;
-    constexpr int kThreads = 64 * kWaves;
-    constexpr int kUnits = 16 * kK / 8;
-    constexpr int kMine = (kUnits + kThreads - 1) / kThreads;
-    constexpr int kCopy = (L::kAtF - L::kAtTt) / 16;  // 16-byte pieces of T^T and P^T
-    constexpr int kCopies = (kCopy + kThreads - 1) / kThreads;
-    constexpr int kFactors = DeltaRecord::kFactorBytes / 16;
-    constexpr int kFactorCopies = (kFactors + kThreads - 1) / kThreads;
+template <class T, int kK, int kWalkers>
+__global__ __launch_bounds__(64 * (kWalkers + Layout<T, kK, kWalkers>::kHelpers), 1)
+void delta_back_kernel(DeltaChunks p) {
+    using L = Layout<T, kK, kWalkers>;
+    constexpr bool kPosts = L::kPosts;
+    constexpr int kHelpers = L::kHelpers;
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);  // one each 4 ints: steps posted
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4;
-    const int slices = (p.v_size + 16 * kWaves - 1) / (16 * kWaves);
+    const int slices = (p.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
     const int slice = blockIdx.x % slices;
     const int h = (blockIdx.x / slices) % p.v_heads, n = blockIdx.x / slices / p.v_heads;
     const int kh = h / (p.v_heads / p.k_heads);
@@ -47,209 +69,300 @@ __global__ __launch_bounds__(64 * kWaves, 1) void delta_back_kernel(DeltaChunks 
     const int chunks = (span.count + kC - 1) / kC;
     const int first_chunk = packed ? chunk_base(p.cu_seqlens, n, p.tokens)
                                    : n * ((p.tokens + kC - 1) / kC);
-    const int col = (slice * kWaves + wave) * 16 + (lane & 15);
-    const bool in = col < p.v_size;
+    const int col0 = slice * kWalkers * 16;
+    const char* records = p.records + ((int64_t)first_chunk * p.v_heads + h) * p.record_bytes;
+    const int64_t record_step = (int64_t)p.v_heads * p.record_bytes;
+    if (kPosts && threadIdx.x < kWalkers) posts[4 * threadIdx.x] = 0;
 
-    const T* k = row_of<const T>(p.k, packed, n, span, kh);
-    const T* q = row_of<const T>(p.q, packed, n, span, kh);
-    const T* d_o = row_of<const T>(p.d_o, packed, n, span, h) + col;
-    T* dv = row_of<T>(p.dv, packed, n, span, h) + col;
-
-    f32x4 D[L::kTiles];
-    const int64_t state = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size + col;
-#pragma unroll
-    for (int i = 0; i < L::kTiles; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = 16 * i + 4 * g + r;
-            D[i][r] = p.dfinal && in && row < p.k_size ? p.dfinal[state + (int64_t)row * p.v_size]
-                                                       : 0.0f;
-        }
-
-    Unit<T, kK> ku[kMine], qu[kMine];
-    f32x4 kscale[kMine], qscale[kMine];
-    u32x4 copy[kCopies], fcopy[kFactorCopies];
-    T dt[4][4];
-    const auto load_next = [&](int c) {
-        const int count = min(kC, span.count - c * kC);
-        const char* record =
-            p.records + ((int64_t)(first_chunk + c) * p.v_heads + h) * p.record_bytes;
-        const float* f = reinterpret_cast<const float*>(record);
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int unit = threadIdx.x + i * kThreads;
-            if (kUnits % kThreads != 0 && unit >= kUnits) continue;
-            ku[i].load(k + (int64_t)c * kC * p.k.token, p.k.token, unit, count, p.k_size, p.wide);
-            qu[i].load(q + (int64_t)c * kC * p.q.token, p.q.token, unit, count, p.k_size, p.wide);
-            kscale[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kKeyScale)[unit / (kK / 8)];
-            qscale[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryScale)[unit / (kK / 8)];
-        }
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            const int at = threadIdx.x + i * kThreads;
-            if (at < kCopy) copy[i] = reinterpret_cast<const u32x4*>(record + DeltaRecord::kAtTt)[at];
-        }
-#pragma unroll
-        for (int i = 0; i < kFactorCopies; ++i) {
-            const int at = threadIdx.x + i * kThreads;
-            if (at < kFactors) fcopy[i] = reinterpret_cast<const u32x4*>(record)[at];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = 16 * i + 4 * g + r;
-                dt[i][r] = in && t < count ? d_o[(int64_t)(c * kC + t) * p.d_o.token]
-                                           : from_f32<T>(0.0f);
-            }
-    };
-    const auto store_next = [&](char* to) {
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int unit = threadIdx.x + i * kThreads;
-            if (kUnits % kThreads != 0 && unit >= kUnits) continue;
-            ku[i].store(to + L::kAtK, unit, kscale[i]);
-            qu[i].store(to + L::kAtQt, unit, qscale[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            const int at = threadIdx.x + i * kThreads;
-            if (at < kCopy) reinterpret_cast<u32x4*>(to + L::kAtTt)[at] = copy[i];
-        }
-#pragma unroll
-        for (int i = 0; i < kFactorCopies; ++i) {
-            const int at = threadIdx.x + i * kThreads;
-            if (at < kFactors) reinterpret_cast<u32x4*>(to + L::kAtF)[at] = fcopy[i];
-        }
-    };
-
-    if (chunks > 0) {
-        load_next(chunks - 1);
-        store_next(lds + (L::kBuffers == 2 ? ((chunks - 1) & 1) * L::kBytes : 0));
-    }
-    for (int c = chunks - 1; c >= 0; --c) {
-        const char* at = lds + (L::kBuffers == 2 ? (c & 1) * L::kBytes : 0);
-        const float* f = reinterpret_cast<const float*>(at + L::kAtF);
-        const auto factor = [&](int which, int tile) {
-            return reinterpret_cast<const f32x4*>(f + 64 * which)[4 * tile + g];
-        };
-        const int count = min(kC, span.count - c * kC);
-        const int64_t task = (int64_t)(first_chunk + c) * p.v_heads + h;
-        f32x4 o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) o[i][r] = to_f32(dt[i][r]);
-        __syncthreads();  // the chunk is in LDS
-        if (c > 0) load_next(c - 1);
-
-        float* to = p.dstates + task * p.k_size * p.v_size + col;
+    // Steps s = 0, 1, ... are chunks from the last to the first.
+    if (wave < kWalkers) {
+        const int col = col0 + 16 * wave + (lane & 15);
+        const bool in = col < p.v_size;
+        f32x4 D[L::kTiles];  // rows 16 i + 4 g + r
+        const int64_t state = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size + col;
 #pragma unroll
         for (int i = 0; i < L::kTiles; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * i + 4 * g + r;
-                if (in && row < p.k_size) to[(int64_t)row * p.v_size] = D[i][r];
+                D[i][r] = p.dfinal && in && row < p.k_size
+                              ? p.dfinal[state + (int64_t)row * p.v_size] : 0.0f;
             }
-
-        // dU
-        f32x4 u[4] = {};
-        {
-            const Scale s = scale_of(max_groups(largest(D)));
-#pragma unroll
-            for (int j = 0; j < L::kSteps; ++j) {
-                const Frag<2> b = split<2>(D[2 * j], D[2 * j + 1], s.up);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    u[i] = multiply(row_fragment<T, kK>(at + L::kAtK, i, j, lane), b, u[i]);
-            }
-            const Scale os = scale_of(max_groups(largest(o)));
-            const Frag<L::kParts> b[2] = {split<L::kParts>(o[0], o[1], os.up),
-                                          split<L::kParts>(o[2], o[3], os.up)};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f32x4 a{};
-#pragma unroll
-                for (int j = i / 2; j < 2; ++j)
-                    a = multiply(matrix_fragment<2>(at + L::kAtPt, upper_at(i, j), lane), b[j], a);
-                const f32x4 tail = factor(DeltaRecord::kTail, i), pf = factor(DeltaRecord::kPt, i);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    u[i][r] = __builtin_fmaf(tail[r] * s.down, u[i][r], pf[r] * os.down * a[r]);
-            }
+        const char* products = lds + L::kAtProducts + wave * L::kEach + lane * 16;
+        T* dv = row_of<T>(p.dv, packed, n, span, h);
+        const uint32_t v_step = (uint32_t)p.dv.token * sizeof(T);
+        const uint32_t v_at = in ? 4 * g * v_step + col * (uint32_t)sizeof(T) : kPastEnd;
+        const uint32_t f_at = in ? 4u * (4 * g * p.v_size + col) : kPastEnd;
+        if (chunks > 0) {
+            lds_barrier();
+            lds_barrier();
         }
-        // dY, and dV
-        f32x4 y[4] = {};
-        {
-            const Scale s = scale_of(max_groups(largest(u)));
-            const Frag<2> b[2] = {split<2>(u[0], u[1], s.up), split<2>(u[2], u[3], s.up)};
-            float* dy = p.dsides + task * kC * p.v_size + col;
+        for (int s = 0; s < chunks; ++s) {
+            const int c = chunks - 1 - s;
+            const char* at = lds + (s & 1) * L::kBuffer;
+            const float* f = reinterpret_cast<const float*>(at + L::kAtF);
+            const auto factor = [&](int which, int tile) {
+                return reinterpret_cast<const f32x4*>(f + 64 * which)[4 * tile + g];
+            };
+            const int count = min(kC, span.count - c * kC);
+            const int64_t task = (int64_t)(first_chunk + c) * p.v_heads + h;
+            lds_barrier();  // A
+            f32x4 u[4], add[L::kTiles];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(products + i * 1024);
 #pragma unroll
-                for (int j = i / 2; j < 2; ++j)
-                    y[i] = multiply(matrix_fragment<2>(at + L::kAtTt, upper_at(i, j), lane), b[j], y[i]);
-                const f32x4 tf = factor(DeltaRecord::kTt, i), beta = factor(DeltaRecord::kBeta, i);
+            for (int i = 0; i < L::kTiles; ++i)
+                add[i] = *reinterpret_cast<const f32x4*>(products + (4 + i) * 1024);
+            if (kPosts) {
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+                __hip_atomic_store(posts + 4 * wave, s + 1, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_WORKGROUP);
+            } else {
+                lds_barrier();  // B
+            }
+            {
+                const __amdgpu_buffer_rsrc_t to =
+                    buffer_at(p.dstates + task * ((p.k_size + 15) / 16 * 16) * p.v_size);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int t = 16 * i + 4 * g + r;
-                    y[i][r] *= tf[r] * s.down;
-                    if (in) dy[(int64_t)t * p.v_size] = y[i][r];
-                    y[i][r] *= beta[r];
-                    if (in && t < count)
-                        dv[(int64_t)(c * kC + t) * p.dv.token] = from_f32<T>(y[i][r]);
+                for (int i = 0; i < L::kTiles; ++i)
+                    if (16 * i < p.k_size)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            __builtin_amdgcn_raw_buffer_store_b32(
+                                __builtin_bit_cast(uint32_t, (float)D[i][r]), to, f_at,
+                                4 * (16 * i + r) * p.v_size, 0);
+            }
+            // dU
+            {
+                const Scale ds = scale_of(max_groups(largest(D)));
+                f32x4 a[4] = {};
+#pragma unroll
+                for (int j = 0; j < L::kSteps; ++j) {
+                    const Frag<2> b = split<2>(D[2 * j], D[2 * j + 1], ds.up);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        a[i] = multiply(row_fragment<T, kK>(at + L::kAtK, i, j, lane), b, a[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 tail = factor(DeltaRecord::kTail, i) * ds.down;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) u[i][r] = __builtin_fmaf(tail[r], a[i][r], u[i][r]);
                 }
             }
-        }
-        // D: both products in one accumulator, under one scale
-        {
+            // dY, and dV
+            f32x4 y[4] = {};
+            {
+                const Scale us = scale_of(max_groups(largest(u)));
+                const Frag<2> b[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
+                const __amdgpu_buffer_rsrc_t dy = buffer_at(p.dsides + task * kC * p.v_size);
+                const __amdgpu_buffer_rsrc_t to = buffer_at(dv + (int64_t)c * kC * p.dv.token);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                o[i] *= factor(DeltaRecord::kQueryRise, i);
-                y[i] *= -factor(DeltaRecord::kRise, i);
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int j = i / 2; j < 2; ++j)
+                        y[i] = multiply(matrix_fragment<2>(at + L::kAtTt, upper_at(i, j), lane), b[j],
+                                        y[i]);
+                    y[i] *= factor(DeltaRecord::kTt, i) * us.down;
+                    const f32x4 beta = factor(DeltaRecord::kBeta, i);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        __builtin_amdgcn_raw_buffer_store_b32(
+                            __builtin_bit_cast(uint32_t, (float)y[i][r]), dy, f_at,
+                            4 * (16 * i + r) * p.v_size, 0);
+                        y[i][r] *= beta[r];
+                        store_word(from_f32<T>(y[i][r]), to,
+                                   count == kC || 16 * i + 4 * g + r < count
+                                       ? v_at + (16 * i + r) * v_step : kPastEnd);
+                    }
+                    y[i] *= -factor(DeltaRecord::kRise, i);
+                }
             }
-            const Scale s = scale_of(max_groups(fmaxf(largest(o), largest(y))));
-            const Frag<2> bo[2] = {split<2>(o[0], o[1], s.up), split<2>(o[2], o[3], s.up)};
-            const Frag<2> by[2] = {split<2>(y[0], y[1], s.up), split<2>(y[2], y[3], s.up)};
+            // D
+            const Scale ys = scale_of(max_groups(largest(y)));
+            const Frag<2> b[2] = {split<2>(y[0], y[1], ys.up), split<2>(y[2], y[3], ys.up)};
             const float decay = f[64 * DeltaRecord::kDecay];
 #pragma unroll
             for (int i = 0; i < L::kTiles; ++i) {
                 f32x4 a{};
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    a = multiply<true>(column_fragment<T, kK>(at + L::kAtQt, i, j, lane), bo[j], a);
-                    a = multiply<true>(column_fragment<T, kK>(at + L::kAtK, i, j, lane), by[j], a);
-                }
+                for (int j = 0; j < 2; ++j)  // lo.lo too: as for S
+                    a = multiply<true>(column_fragment<T, kK>(at + L::kAtK, i, j, lane), b[j], a);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) D[i][r] = __builtin_fmaf(a[r], s.down, decay * D[i][r]);
+                for (int r = 0; r < 4; ++r)
+                    D[i][r] = __builtin_fmaf(a[r], ys.down,
+                                             __builtin_fmaf(decay, D[i][r], add[i][r]));
             }
         }
-        if (c > 0) {
-            if (L::kBuffers == 1) __syncthreads();
-            store_next(lds + (L::kBuffers == 2 ? ((c - 1) & 1) * L::kBytes : 0));
+        if (p.dinitial && in)
+#pragma unroll
+            for (int i = 0; i < L::kTiles; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * i + 4 * g + r;
+                    if (row < p.k_size) p.dinitial[state + (int64_t)row * p.v_size] = D[i][r];
+                }
+        return;
+    }
+
+    // ---- the helping waves
+    if (chunks == 0) return;
+    const int helper = wave - kWalkers;
+    const bool brings_k = helper < 4, brings_q = helper >= kHelpers - 4;
+    const int id = (threadIdx.x - 64 * kWalkers) & 255;
+    const T* k = row_of<const T>(p.k, packed, n, span, kh);
+    const T* q = row_of<const T>(p.q, packed, n, span, kh);
+    const T* d_o = row_of<const T>(p.d_o, packed, n, span, h) + col0;
+    Rows<T, kK, 256> ku, qu;
+    Copy<L::kMatrix, 256> tcopy, pcopy;
+    Copy<DeltaRecord::kFactorBytes, 256> fcopy, fqcopy;
+    typename L::V vu;
+    const auto load_k = [&](int s) {
+        const int c = chunks - 1 - s;
+        const char* record = records + c * record_step;
+        ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, min(kC, span.count - c * kC), p.k_size,
+                p.wide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
+        tcopy.load(record + DeltaRecord::kAtTt, id);
+        fcopy.load(record, id);
+    };
+    const auto store_k = [&](int s) {
+        char* to = lds + (s & 1) * L::kBuffer;
+        ku.store(to + L::kAtK, id);
+        tcopy.store(to + L::kAtTt, id);
+        fcopy.store(to + L::kAtF, id);
+    };
+    const auto load_q = [&](int s) {
+        const int c = chunks - 1 - s, count = min(kC, span.count - c * kC);
+        const char* record = records + c * record_step;
+        qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, count, p.k_size, p.wide,
+                reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
+        pcopy.load(record + DeltaRecord::kAtPt, id);
+        fqcopy.load(record, id);
+        vu.load(d_o + (int64_t)c * kC * p.d_o.token, p.d_o.token, count, p.v_size - col0,
+                p.wide_values, id);
+    };
+    const auto buffer_q = [&](int s) { return lds + L::kAtQs + (kPosts ? (s & 1) * L::kBufferQ : 0); };
+    const auto store_q = [&](int s) {
+        char* to = buffer_q(s);
+        qu.store(to + L::kAtQ, id);
+        pcopy.store(to + L::kAtPt, id);
+        fqcopy.store(to + L::kAtFq, id);
+        vu.store(to + L::kAtDo, id);
+    };
+
+    // P^T dO and the product with Q: 16 columns to a wave, kOwn of the 4 token
+    // tiles and kOwnK of the kTiles element tiles
+    constexpr int kOwn = 4 * kWalkers / kHelpers, kOwnK = L::kTiles * kWalkers / kHelpers;
+    static_assert(kOwn >= 1 && kOwnK >= 1, "every wave has a part");
+    const int block = helper % kWalkers, part = helper / kWalkers;
+    f32x4 pd[kOwn], qd[kOwnK];
+    const auto make = [&](int s) {
+        const char* at = buffer_q(s);
+        const float* f = reinterpret_cast<const float*>(at + L::kAtFq);
+        const char* v_at = at + L::kAtDo + block * L::V::kEach + lane * 4 * (int)sizeof(T);
+        f32x4 o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            T x[4];
+            __builtin_memcpy(x, v_at + i * 64 * 4 * sizeof(T), 4 * sizeof(T));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[i][r] = to_f32(x[r]);
+        }
+        const Scale os = scale_of(max_groups(largest(o)));
+        {
+            const Frag<L::kParts> b[2] = {split<L::kParts>(o[0], o[1], os.up),
+                                          split<L::kParts>(o[2], o[3], os.up)};
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                const int tile = part * kOwn + i;
+                f32x4 a{};
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (j >= tile / 2)
+                        a = multiply(matrix_fragment<2>(at + L::kAtPt, upper_at(tile, j), lane), b[j], a);
+                pd[i] = a * reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kPt)[4 * tile + g] * os.down;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[i] *= reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryRise)[4 * i + g];
+        const Scale qs = scale_of(max_groups(largest(o)));
+        const Frag<2> b[2] = {split<2>(o[0], o[1], qs.up), split<2>(o[2], o[3], qs.up)};
+#pragma unroll
+        for (int i = 0; i < kOwnK; ++i) {
+            f32x4 a{};
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                a = multiply<true>(column_fragment<T, kK>(at + L::kAtQ, part * kOwnK + i, j, lane), b[j], a);
+            qd[i] = a * qs.down;
+        }
+    };
+    const auto put = [&]() {
+        char* to = lds + L::kAtProducts + block * L::kEach + lane * 16;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+            *reinterpret_cast<f32x4*>(to + (part * kOwn + i) * 1024) = pd[i];
+#pragma unroll
+        for (int i = 0; i < kOwnK; ++i)
+            *reinterpret_cast<f32x4*>(to + (4 + part * kOwnK + i) * 1024) = qd[i];
+    };
+
+    if (brings_k) {
+        load_k(0);
+        store_k(0);
+        if (chunks > 1) load_k(1);
+    }
+    if (brings_q) {
+        load_q(0);
+        store_q(0);
+        if (chunks > 1) load_q(1);
+    }
+    lds_barrier();
+    make(0);
+    lds_barrier();
+    put();
+    if (brings_q && chunks > 1) {
+        store_q(1);
+        if (chunks > 2) load_q(2);
+    }
+    for (int s = 0; s < chunks; ++s) {
+        lds_barrier();  // A
+        if (s + 1 < chunks) make(s + 1);
+        if (kPosts) {
+            // every walking wave is in this step and posts on its way
+#pragma unroll
+            for (int w = 0; w < kWalkers; ++w)
+                while (__hip_atomic_load(posts + 4 * w, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= s)
+                    __builtin_amdgcn_s_sleep(1);
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        } else {
+            lds_barrier();  // B
+        }
+        if (s + 1 < chunks) put();
+        if (brings_k && s + 1 < chunks) {
+            store_k(s + 1);
+            if (s + 2 < chunks) load_k(s + 2);
+        }
+        if (brings_q && s + 2 < chunks) {
+            store_q(s + 2);
+            if (s + 3 < chunks) load_q(s + 3);
         }
     }
-    if (p.dinitial && in)
-#pragma unroll
-        for (int i = 0; i < L::kTiles; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * i + 4 * g + r;
-                if (row < p.k_size) p.dinitial[state + (int64_t)row * p.v_size] = D[i][r];
-            }
 }
 
-template <class T, int kK, int kWaves>
+template <class T, int kK, int kWalkers>
 hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
-    using L = Layout<T, kK>;
-    constexpr int kBytes = L::kBuffers * L::kBytes;
-    const int64_t slices = (a.v_size + 16 * kWaves - 1) / (16 * kWaves);
-    const void* kernel = reinterpret_cast<const void*>(delta_back_kernel<T, kK, kWaves>);
-    if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes))
+    using L = Layout<T, kK, kWalkers>;
+    static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
+    const int64_t slices = (a.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
+    const void* kernel = reinterpret_cast<const void*>(delta_back_kernel<T, kK, kWalkers>);
+    if (hipError_t e =
+            hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
-    hipLaunchKernelGGL((delta_back_kernel<T, kK, kWaves>),
-                       dim3((unsigned)(slices * a.v_heads * a.batch)), dim3(64 * kWaves), kBytes,
-                       stream, a);
+    hipLaunchKernelGGL((delta_back_kernel<T, kK, kWalkers>),
+                       dim3((unsigned)(slices * a.v_heads * a.batch)),
+                       dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
 }
 
@@ -258,7 +371,8 @@ hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
 hipError_t launch_delta_chain_back(const DeltaChunks& a, hipStream_t stream) {
     return by_dtype(a.dtype, [&](auto t) {
         using T = decltype(t);
-        return a.k_size <= 64 ? launch<T, 64, 4>(a, stream) : launch<T, 128, 4>(a, stream);
+        return a.k_size <= 64 ? launch<T, 64, 2>(a, stream)
+                              : launch<T, 128, sizeof(T) == 4 ? 1 : 2>(a, stream);
     });
 }
 

@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         const float* u = p.updates + task * kC * p.v_size;
         const float* dy = p.dsides + task * kC * p.v_size;
         const float* S = p.states + task * ((p.k_size + 15) / 16 * 16) * p.v_size;
-        const float* D = p.dstates + task * p.k_size * p.v_size;
+        const float* D = p.dstates + task * ((p.k_size + 15) / 16 * 16) * p.v_size;
         const bool wide_f = p.v_size % 8 == 0;
 
         f32x4 e1[kOwn] = {}, e2[kOwn] = {}, e3[kOwn] = {}, m[4] = {};
