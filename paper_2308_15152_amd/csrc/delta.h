@@ -62,7 +62,8 @@ struct DeltaRecord {
     };
     static constexpr int kMatrix = 6 * 1024;             // one part of one matrix
     static constexpr int kFactorBytes = kFactors * 256;  // at the record's start
-    static constexpr int kAtT = kFactorBytes;            // two parts
+    static constexpr int kAtSums = kFactorBytes;         // G, 64 doubles
+    static constexpr int kAtT = kAtSums + 512;           // two parts
     static constexpr int kAtP = kAtT + 2 * kMatrix;      // two parts (one for bfloat16)
     static constexpr int kForward = kAtP + 2 * kMatrix;
     static constexpr int kAtTt = kAtP;  // the backward form has no P
@@ -95,7 +96,22 @@ struct DeltaChunks {
     float* dstates;
     float* dsides;
     bool wide_values;     // 16-byte loads of v's and d_o's rows
+    // Long sequences of few heads are cut into parts of `part_chunks` chunks (0:
+    // not cut), which are walked at the same time: a part takes the state S to
+    // M S + N.  Per part and value head: N, then the state before the part
+    // (k_size x v_size), and M (rows x rows, rows = k_size up to a multiple of 16).
+    int part_chunks, parts;
+    float* part_states;
+    float* part_steps;
+    float* part_dstates;  // the same of the walk back
 };
+
+// Parts that the sequences of a call can have; numbered as chunks are.
+inline int64_t delta_parts(int64_t batch, int64_t tokens, bool packed, int64_t part_chunks) {
+    const int64_t chunks = delta_chunks(batch, tokens, packed);
+    if (packed) return chunks / part_chunks + batch;
+    return batch == 0 ? 0 : batch * ((chunks / batch + part_chunks - 1) / part_chunks);
+}
 
 // Whether rows of `size` elements of these views can be loaded 16 bytes at a
 // time.
@@ -107,8 +123,14 @@ inline bool delta_wide(int dtype, int size, std::initializer_list<sgemm_emu_view
 }
 
 hipError_t launch_delta_prep(const DeltaChunks& a, hipStream_t stream);
-hipError_t launch_delta_chain(const DeltaChunks& a, hipStream_t stream);
-hipError_t launch_delta_chain_back(const DeltaChunks& a, hipStream_t stream);
+// What a walk writes: the outputs; the state and U of every chunk (or, back,
+// the state's gradient and dY); or nothing but N and M of every part.
+enum DeltaWalk { kDeltaOutputs, kDeltaStates, kDeltaParts };
+hipError_t launch_delta_chain(const DeltaChunks& a, DeltaWalk walk, hipStream_t stream);
+hipError_t launch_delta_chain_back(const DeltaChunks& a, DeltaWalk walk, hipStream_t stream);
+// The states before every part from the first one's: part_states (back: the
+// gradients after every part from the last one's, with M^T: part_dstates).
+hipError_t launch_delta_join(const DeltaChunks& a, bool back, hipStream_t stream);
 hipError_t launch_delta_gradient(const DeltaChunks& a, hipStream_t stream);
 
 int64_t delta_forward_workspace(const delta_emu_forward_t& a);

@@ -6,7 +6,9 @@
 // forward (delta_chain.hip): walking waves carry 16 columns of D each and
 // do what waits for D; helping waves bring K and T^T of the next chunk, and make
 // what does not wait, P^T dO and the product with Q, a chunk ahead from Q, P^T and dO,
-// which they bring two chunks ahead.  Leaves D after and dY of every chunk.
+// which they bring two chunks ahead.  Leaves D after and dY of every chunk.  A
+// sequence cut into parts is walked twice, as on the way forward: every part
+// but the first from D = 0, then all from their own (M^T takes D across a part).
 //
 // One barrier a chunk (A).  Inside a chunk a walking wave posts when it has taken
 // its two products; then the helpers put down the next ones.  In FP32, for whose
@@ -48,7 +50,8 @@ struct Layout {
     static constexpr int kBytes = kAtPosts + 16 * kWalkers;
 };
 
-template <class T, int kK, int kWalkers>
+// kCarry: only D before every part, from zero after it.
+template <class T, int kK, int kWalkers, bool kCarry>
 __global__ __launch_bounds__(64 * (kWalkers + Layout<T, kK, kWalkers>::kHelpers), 1)
 void delta_back_kernel(DeltaChunks p) {
     using L = Layout<T, kK, kWalkers>;
@@ -61,17 +64,22 @@ void delta_back_kernel(DeltaChunks p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4;
     const int slices = (p.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
-    const int slice = blockIdx.x % slices;
-    const int h = (blockIdx.x / slices) % p.v_heads, n = blockIdx.x / slices / p.v_heads;
+    // slices of a head on one XCD: they read the same K, Q, T and P
+    const int walk_task = xcd_task(blockIdx.x, gridDim.x);
+    const int slice = walk_task % slices;
+    const int h = (walk_task / slices) % p.v_heads, index = walk_task / slices / p.v_heads;
     const int kh = h / (p.v_heads / p.k_heads);
     const bool packed = p.cu_seqlens != nullptr;
-    const Span span = span_of(p.cu_seqlens, n, p.tokens);
-    const int chunks = (span.count + kC - 1) / kC;
-    const int first_chunk = packed ? chunk_base(p.cu_seqlens, n, p.tokens)
-                                   : n * ((p.tokens + kC - 1) / kC);
+    const Walk walk = walk_of(p, index);
+    const int chunks = walk.count;
+    if (chunks < 0 || (kCarry && walk.part == 0)) return;  // the whole block
+    const int n = walk.n;
+    const Span span = {walk.span.first, walk.span.count - walk.first * kC};  // from the part on
+    const int first_chunk = walk.base + walk.first;
     const int col0 = slice * kWalkers * 16;
     const char* records = p.records + ((int64_t)first_chunk * p.v_heads + h) * p.record_bytes;
     const int64_t record_step = (int64_t)p.v_heads * p.record_bytes;
+    const int64_t skip = (int64_t)walk.first * kC;  // tokens of the parts before
     if (kPosts && threadIdx.x < kWalkers) posts[4 * threadIdx.x] = 0;
 
     // Steps s = 0, 1, ... are chunks from the last to the first.
@@ -79,17 +87,21 @@ void delta_back_kernel(DeltaChunks p) {
         const int col = col0 + 16 * wave + (lane & 15);
         const bool in = col < p.v_size;
         f32x4 D[L::kTiles];  // rows 16 i + 4 g + r
-        const int64_t state = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size + col;
+        const int64_t sequence = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size;
+        const int64_t part = ((int64_t)index * p.v_heads + h) * p.k_size * p.v_size;
+        const float* from = kCarry              ? nullptr
+                            : p.part_chunks > 0 ? p.part_dstates + part
+                            : p.dfinal          ? p.dfinal + sequence
+                                                : nullptr;
 #pragma unroll
         for (int i = 0; i < L::kTiles; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * i + 4 * g + r;
-                D[i][r] = p.dfinal && in && row < p.k_size
-                              ? p.dfinal[state + (int64_t)row * p.v_size] : 0.0f;
+                D[i][r] = from && in && row < p.k_size ? from[(int64_t)row * p.v_size + col] : 0.0f;
             }
         const char* products = lds + L::kAtProducts + wave * L::kEach + lane * 16;
-        T* dv = row_of<T>(p.dv, packed, n, span, h);
+        T* dv = row_of<T>(p.dv, packed, n, span, h) + skip * p.dv.token;
         const uint32_t v_step = (uint32_t)p.dv.token * sizeof(T);
         const uint32_t v_at = in ? 4 * g * v_step + col * (uint32_t)sizeof(T) : kPastEnd;
         const uint32_t f_at = in ? 4u * (4 * g * p.v_size + col) : kPastEnd;
@@ -101,7 +113,7 @@ void delta_back_kernel(DeltaChunks p) {
             const int c = chunks - 1 - s;
             const char* at = lds + (s & 1) * L::kBuffer;
             const float* f = reinterpret_cast<const float*>(at + L::kAtF);
-            const auto factor = [&](int which, int tile) {
+            const auto factor = [&](int which, int tile) __attribute__((always_inline)) {
                 return reinterpret_cast<const f32x4*>(f + 64 * which)[4 * tile + g];
             };
             const int count = min(kC, span.count - c * kC);
@@ -120,7 +132,7 @@ void delta_back_kernel(DeltaChunks p) {
             } else {
                 lds_barrier();  // B
             }
-            {
+            if (!kCarry) {
                 const __amdgpu_buffer_rsrc_t to =
                     buffer_at(p.dstates + task * ((p.k_size + 15) / 16 * 16) * p.v_size);
 #pragma unroll
@@ -167,10 +179,12 @@ void delta_back_kernel(DeltaChunks p) {
                     const f32x4 beta = factor(DeltaRecord::kBeta, i);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        __builtin_amdgcn_raw_buffer_store_b32(
-                            __builtin_bit_cast(uint32_t, (float)y[i][r]), dy, f_at,
-                            4 * (16 * i + r) * p.v_size, 0);
+                        if (!kCarry)
+                            __builtin_amdgcn_raw_buffer_store_b32(
+                                __builtin_bit_cast(uint32_t, (float)y[i][r]), dy, f_at,
+                                4 * (16 * i + r) * p.v_size, 0);
                         y[i][r] *= beta[r];
+                        if (kCarry) continue;
                         store_word(from_f32<T>(y[i][r]), to,
                                    count == kC || 16 * i + 4 * g + r < count
                                        ? v_at + (16 * i + r) * v_step : kPastEnd);
@@ -194,13 +208,16 @@ void delta_back_kernel(DeltaChunks p) {
                                              __builtin_fmaf(decay, D[i][r], add[i][r]));
             }
         }
-        if (p.dinitial && in)
+        float* to = kCarry                            ? p.part_dstates + part
+                    : p.dinitial && walk.part == 0 ? p.dinitial + sequence
+                                                   : nullptr;
+        if (to && in)
 #pragma unroll
             for (int i = 0; i < L::kTiles; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = 16 * i + 4 * g + r;
-                    if (row < p.k_size) p.dinitial[state + (int64_t)row * p.v_size] = D[i][r];
+                    if (row < p.k_size) to[(int64_t)row * p.v_size + col] = D[i][r];
                 }
         return;
     }
@@ -210,14 +227,14 @@ void delta_back_kernel(DeltaChunks p) {
     const int helper = wave - kWalkers;
     const bool brings_k = helper < 4, brings_q = helper >= kHelpers - 4;
     const int id = (threadIdx.x - 64 * kWalkers) & 255;
-    const T* k = row_of<const T>(p.k, packed, n, span, kh);
-    const T* q = row_of<const T>(p.q, packed, n, span, kh);
-    const T* d_o = row_of<const T>(p.d_o, packed, n, span, h) + col0;
+    const T* k = row_of<const T>(p.k, packed, n, span, kh) + skip * p.k.token;
+    const T* q = row_of<const T>(p.q, packed, n, span, kh) + skip * p.q.token;
+    const T* d_o = row_of<const T>(p.d_o, packed, n, span, h) + skip * p.d_o.token + col0;
     Rows<T, kK, 256> ku, qu;
     Copy<L::kMatrix, 256> tcopy, pcopy;
     Copy<DeltaRecord::kFactorBytes, 256> fcopy, fqcopy;
     typename L::V vu;
-    const auto load_k = [&](int s) {
+    const auto load_k = [&](int s) __attribute__((always_inline)) {
         const int c = chunks - 1 - s;
         const char* record = records + c * record_step;
         ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, min(kC, span.count - c * kC), p.k_size,
@@ -225,13 +242,13 @@ void delta_back_kernel(DeltaChunks p) {
         tcopy.load(record + DeltaRecord::kAtTt, id);
         fcopy.load(record, id);
     };
-    const auto store_k = [&](int s) {
+    const auto store_k = [&](int s) __attribute__((always_inline)) {
         char* to = lds + (s & 1) * L::kBuffer;
         ku.store(to + L::kAtK, id);
         tcopy.store(to + L::kAtTt, id);
         fcopy.store(to + L::kAtF, id);
     };
-    const auto load_q = [&](int s) {
+    const auto load_q = [&](int s) __attribute__((always_inline)) {
         const int c = chunks - 1 - s, count = min(kC, span.count - c * kC);
         const char* record = records + c * record_step;
         qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, count, p.k_size, p.wide,
@@ -241,8 +258,8 @@ void delta_back_kernel(DeltaChunks p) {
         vu.load(d_o + (int64_t)c * kC * p.d_o.token, p.d_o.token, count, p.v_size - col0,
                 p.wide_values, id);
     };
-    const auto buffer_q = [&](int s) { return lds + L::kAtQs + (kPosts ? (s & 1) * L::kBufferQ : 0); };
-    const auto store_q = [&](int s) {
+    const auto buffer_q = [&](int s) __attribute__((always_inline)) { return lds + L::kAtQs + (kPosts ? (s & 1) * L::kBufferQ : 0); };
+    const auto store_q = [&](int s) __attribute__((always_inline)) {
         char* to = buffer_q(s);
         qu.store(to + L::kAtQ, id);
         pcopy.store(to + L::kAtPt, id);
@@ -256,7 +273,7 @@ void delta_back_kernel(DeltaChunks p) {
     static_assert(kOwn >= 1 && kOwnK >= 1, "every wave has a part");
     const int block = helper % kWalkers, part = helper / kWalkers;
     f32x4 pd[kOwn], qd[kOwnK];
-    const auto make = [&](int s) {
+    const auto make = [&](int s) __attribute__((always_inline)) {
         const char* at = buffer_q(s);
         const float* f = reinterpret_cast<const float*>(at + L::kAtFq);
         const char* v_at = at + L::kAtDo + block * L::V::kEach + lane * 4 * (int)sizeof(T);
@@ -297,7 +314,7 @@ void delta_back_kernel(DeltaChunks p) {
             qd[i] = a * qs.down;
         }
     };
-    const auto put = [&]() {
+    const auto put = [&]() __attribute__((always_inline)) {
         char* to = lds + L::kAtProducts + block * L::kEach + lane * 16;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i)
@@ -351,28 +368,33 @@ void delta_back_kernel(DeltaChunks p) {
     }
 }
 
-template <class T, int kK, int kWalkers>
+template <class T, int kK, int kWalkers, bool kCarry>
 hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
     using L = Layout<T, kK, kWalkers>;
     static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
     const int64_t slices = (a.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
-    const void* kernel = reinterpret_cast<const void*>(delta_back_kernel<T, kK, kWalkers>);
+    const int64_t walks = a.part_chunks > 0 ? a.parts : a.batch;
+    const void* kernel = reinterpret_cast<const void*>(delta_back_kernel<T, kK, kWalkers, kCarry>);
     if (hipError_t e =
             hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
-    hipLaunchKernelGGL((delta_back_kernel<T, kK, kWalkers>),
-                       dim3((unsigned)(slices * a.v_heads * a.batch)),
+    hipLaunchKernelGGL((delta_back_kernel<T, kK, kWalkers, kCarry>),
+                       dim3((unsigned)(slices * a.v_heads * walks)),
                        dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_delta_chain_back(const DeltaChunks& a, hipStream_t stream) {
+hipError_t launch_delta_chain_back(const DeltaChunks& a, DeltaWalk walk, hipStream_t stream) {
     return by_dtype(a.dtype, [&](auto t) {
         using T = decltype(t);
-        return a.k_size <= 64 ? launch<T, 64, 2>(a, stream)
-                              : launch<T, 128, sizeof(T) == 4 ? 1 : 2>(a, stream);
+        constexpr int kWide = sizeof(T) == 4 ? 1 : 2;
+        if (walk == kDeltaParts)
+            return a.k_size <= 64 ? launch<T, 64, 2, true>(a, stream)
+                                  : launch<T, 128, kWide, true>(a, stream);
+        return a.k_size <= 64 ? launch<T, 64, 2, false>(a, stream)
+                              : launch<T, 128, kWide, false>(a, stream);
     });
 }
 

@@ -16,13 +16,19 @@
 // its V is taken; the helpers wait for that before they read S and write the next V.  In
 // FP32, for whose two parts LDS holds Q only once, the post is a second barrier (B),
 // before which the chunk's Q goes down.
+//
+// A long sequence of few heads leaves most CUs idle.  It is cut into parts, and
+// walked three times less deep: first every part but the last from S = 0, and, as
+// further columns with V = 0, from the columns of the identity, which gives N and M of
+// S -> M S + N; then the states before the parts follow one from another
+// (delta_join.hip); then all parts are walked for their outputs.
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
 
 namespace {
 
-enum { kOutputs, kStates };  // what the walk writes: O, or S and U per chunk
+constexpr int kOutputs = kDeltaOutputs, kStates = kDeltaStates, kPartSteps = kDeltaParts;
 
 // LDS, in bytes, and the number of helping waves.
 template <class T, int kK, int kWalkers, int kMode>
@@ -71,32 +77,49 @@ void delta_chain_kernel(DeltaChunks p) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4;
-    const int slices = (p.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
-    const int slice = blockIdx.x % slices;
-    const int h = (blockIdx.x / slices) % p.v_heads, n = blockIdx.x / slices / p.v_heads;
+    const int v_slices = (p.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
+    const int slices =
+        v_slices + (kMode == kPartSteps ? (p.k_size + 16 * kWalkers - 1) / (16 * kWalkers) : 0);
+    // slices of a head on one XCD: they read the same K, Q, T and P
+    const int task = xcd_task(blockIdx.x, gridDim.x);
+    int slice = task % slices;
+    const int h = (task / slices) % p.v_heads, index = task / slices / p.v_heads;
     const int kh = h / (p.v_heads / p.k_heads);
     const bool packed = p.cu_seqlens != nullptr;
-    const Span span = span_of(p.cu_seqlens, n, p.tokens);
-    const int chunks = (span.count + kC - 1) / kC;
-    const int first_chunk = packed ? chunk_base(p.cu_seqlens, n, p.tokens)
-                                   : n * ((p.tokens + kC - 1) / kC);
+    const Walk walk = walk_of(p, index);
+    const int chunks = walk.count;
+    // (the whole block)
+    if (chunks < 0 || (kMode == kPartSteps && !p.backward && walk.part + 1 == walk.parts)) return;
+    const int n = walk.n;
+    const Span span = {walk.span.first, walk.span.count - walk.first * kC};  // from the part on
+    // columns of S, or (kPartSteps, later slices) of M, which has no V
+    const bool of_m = kMode == kPartSteps && slice >= v_slices;
+    if (of_m) slice -= v_slices;
+    const int columns = of_m ? p.k_size : p.v_size;
     const int col0 = slice * kWalkers * 16;
+    const int first_chunk = walk.base + walk.first;
     const char* records = p.records + ((int64_t)first_chunk * p.v_heads + h) * p.record_bytes;
     const int64_t record_step = (int64_t)p.v_heads * p.record_bytes;
+    const int64_t skip = (int64_t)walk.first * kC;  // tokens of the parts before
     if (kPosts && threadIdx.x < kWalkers) posts[4 * threadIdx.x] = 0;
 
     if (wave < kWalkers) {
         const int col = col0 + 16 * wave + (lane & 15);
-        const bool in = col < p.v_size;
+        const bool in = col < columns;
         f32x4 S[L::kTiles];  // rows 16 i + 4 g + r
-        const int64_t state = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size + col;
+        const int64_t sequence = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size;
+        const int64_t part = ((int64_t)index * p.v_heads + h) * p.k_size * p.v_size;
+        const float* from = kMode == kPartSteps    ? nullptr
+                            : p.part_chunks > 0 ? p.part_states + part
+                            : p.initial         ? p.initial + sequence
+                                                : nullptr;
 #pragma unroll
         for (int i = 0; i < L::kTiles; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 16 * i + 4 * g + r;
-                S[i][r] = p.initial && in && row < p.k_size
-                              ? p.initial[state + (int64_t)row * p.v_size] : 0.0f;
+                S[i][r] = from && in && row < p.k_size ? from[(int64_t)row * p.v_size + col] : 0.0f;
+                if (of_m && row == col) S[i][r] = 1.0f;
             }
         const char* v_at = lds + L::kAtV + wave * L::V::kEach + lane * 4 * (int)sizeof(T);
         char* s_at = lds + L::kAtS + wave * L::kEachS;
@@ -105,7 +128,7 @@ void delta_chain_kernel(DeltaChunks p) {
         for (int c = 0; c < chunks; ++c) {
             const char* at = lds + (c & 1) * L::kBuffer;
             const float* f = reinterpret_cast<const float*>(at + L::kAtF);
-            const auto factor = [&](int which, int tile) {
+            const auto factor = [&](int which, int tile) __attribute__((always_inline)) {
                 return reinterpret_cast<const f32x4*>(f + 64 * which)[4 * tile + g];
             };
             lds_barrier();  // A
@@ -209,13 +232,20 @@ void delta_chain_kernel(DeltaChunks p) {
             }
         }
         if (kMode == kOutputs && chunks > 0) lds_barrier();  // the last U
-        if (p.final_state && in)
+        const int rows = (p.k_size + 15) / 16 * 16;
+        float* to = kMode == kPartSteps
+                        ? (of_m ? p.part_steps + ((int64_t)index * p.v_heads + h) * rows * rows
+                                : p.part_states + part)
+                    : p.final_state && walk.part + 1 == walk.parts ? p.final_state + sequence
+                                                                   : nullptr;
+        const int stride = of_m ? rows : p.v_size;
+        if (to && (in || (of_m && col < rows)))
 #pragma unroll
             for (int i = 0; i < L::kTiles; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = 16 * i + 4 * g + r;
-                    if (row < p.k_size) p.final_state[state + (int64_t)row * p.v_size] = S[i][r];
+                    if (row < (of_m ? rows : p.k_size)) to[(int64_t)row * stride + col] = S[i][r];
                 }
         return;
     }
@@ -224,37 +254,38 @@ void delta_chain_kernel(DeltaChunks p) {
     const int helper = wave - kWalkers;
     const bool brings_k = helper < 4, brings_q = kMode == kOutputs && helper >= kHelpers - 4;
     const int id = (threadIdx.x - 64 * kWalkers) & 255;
-    const T* k = row_of<const T>(p.k, packed, n, span, kh);
-    const T* q = row_of<const T>(p.q, packed, n, span, kh);
-    const T* v = row_of<const T>(p.v, packed, n, span, h) + col0;
+    const T* k = row_of<const T>(p.k, packed, n, span, kh) + skip * p.k.token;
+    const T* q = row_of<const T>(p.q, packed, n, span, kh) + skip * p.q.token;
+    const T* v = row_of<const T>(p.v, packed, n, span, h) + skip * p.v.token + col0;
     Rows<T, kK, 256> ku, qu;
     Copy<L::kMatrices, 256> tcopy;
     Copy<DeltaRecord::kFactorBytes, 256> fcopy;
     Copy<L::kBytesP == 0 ? 16 : L::kBytesP, 256> pcopy;
     typename L::V vu;
-    const auto load_k = [&](int c) {
+    const auto load_k = [&](int c) __attribute__((always_inline)) {
         const int count = min(kC, span.count - c * kC);
         const char* record = records + c * record_step;
         ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, count, p.k_size, p.wide,
                 reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
         tcopy.load(record + DeltaRecord::kAtT, id);
         fcopy.load(record, id);
-        vu.load(v + (int64_t)c * kC * p.v.token, p.v.token, count, p.v_size - col0, p.wide_values, id);
+        vu.load(v + (int64_t)c * kC * p.v.token, p.v.token, count, of_m ? 0 : p.v_size - col0,
+                p.wide_values, id);
     };
-    const auto store_k = [&](int c) {
+    const auto store_k = [&](int c) __attribute__((always_inline)) {
         char* to = lds + (c & 1) * L::kBuffer;
         ku.store(to + L::kAtK, id);
         tcopy.store(to + L::kAtT, id);
         fcopy.store(to + L::kAtF, id);
         vu.store(lds + L::kAtV, id);
     };
-    const auto load_q = [&](int c) {
+    const auto load_q = [&](int c) __attribute__((always_inline)) {
         const char* record = records + c * record_step;
         qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, min(kC, span.count - c * kC), p.k_size,
                 p.wide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
     };
-    const auto load_p = [&](int c) { pcopy.load(records + c * record_step + DeltaRecord::kAtP, id); };
-    const auto buffer_q = [&](int c) { return lds + (kPosts ? (c & 1) * L::kBufferQ : 0); };
+    const auto load_p = [&](int c) __attribute__((always_inline)) { pcopy.load(records + c * record_step + DeltaRecord::kAtP, id); };
+    const auto buffer_q = [&](int c) __attribute__((always_inline)) { return lds + (kPosts ? (c & 1) * L::kBufferQ : 0); };
 
     // O: 16 columns and kOwn token tiles of a chunk to a wave
     constexpr int kOwn = 4 * kWalkers / kHelpers < 1 ? 1 : 4 * kWalkers / kHelpers;
@@ -262,11 +293,11 @@ void delta_chain_kernel(DeltaChunks p) {
     const bool outputs = kMode == kOutputs && own < 4;
     const int col = col0 + 16 * block + (lane & 15);
     const bool in = col < p.v_size;
-    T* o = kMode == kOutputs ? row_of<T>(p.o, packed, n, span, h) : nullptr;
+    T* o = kMode == kOutputs ? row_of<T>(p.o, packed, n, span, h) + skip * p.o.token : nullptr;
     const uint32_t o_step = (uint32_t)p.o.token * sizeof(T);
     const uint32_t o_at = in ? (16 * own + 4 * g) * o_step + col * (uint32_t)sizeof(T) : kPastEnd;
     f32x4 y[kOwn], pf[kOwn];  // scale diag(e^G) Q S, and the scales of P's rows
-    const auto finish = [&](int c) {
+    const auto finish = [&](int c) __attribute__((always_inline)) {
         const char* u_at = lds + L::kAtU + (kPosts ? (c & 1) * L::kBufferU : 0) +
                            block * L::kEachU + lane * 16;
         f32x4 u[4];
@@ -383,28 +414,38 @@ template <class T, int kK, int kWalkers, int kMode>
 hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
     using L = Layout<T, kK, kWalkers, kMode>;
     static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
-    const int64_t slices = (a.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
+    constexpr int kColumns = 16 * kWalkers;
+    int64_t slices = (a.v_size + kColumns - 1) / kColumns;
+    if (kMode == kPartSteps) slices += (a.k_size + kColumns - 1) / kColumns;
+    const int64_t walks = a.part_chunks > 0 ? a.parts : a.batch;
     const void* kernel = reinterpret_cast<const void*>(delta_chain_kernel<T, kK, kWalkers, kMode>);
     if (hipError_t e =
             hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
     hipLaunchKernelGGL((delta_chain_kernel<T, kK, kWalkers, kMode>),
-                       dim3((unsigned)(slices * a.v_heads * a.batch)),
+                       dim3((unsigned)(slices * a.v_heads * walks)),
                        dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_delta_chain(const DeltaChunks& a, hipStream_t stream) {
+hipError_t launch_delta_chain(const DeltaChunks& a, DeltaWalk walk, hipStream_t stream) {
     return by_dtype(a.dtype, [&](auto t) {
         using T = decltype(t);
         constexpr bool kF32 = sizeof(T) == 4;
-        if (a.backward)
-            return a.k_size <= 64 ? launch<T, 64, 2, kStates>(a, stream)
-                                  : launch<T, 128, 2, kStates>(a, stream);
-        return a.k_size <= 64 ? launch<T, 64, 2, kOutputs>(a, stream)
-                              : launch<T, 128, kF32 ? 1 : 2, kOutputs>(a, stream);
+        const bool small = a.k_size <= 64;
+        switch (walk) {
+            case kDeltaStates:
+                return small ? launch<T, 64, 2, kStates>(a, stream)
+                             : launch<T, 128, 2, kStates>(a, stream);
+            case kDeltaParts:
+                return small ? launch<T, 64, 4, kPartSteps>(a, stream)
+                             : launch<T, 128, kF32 ? 2 : 4, kPartSteps>(a, stream);
+            default:
+                return small ? launch<T, 64, 2, kOutputs>(a, stream)
+                             : launch<T, 128, kF32 ? 1 : 2, kOutputs>(a, stream);
+        }
     });
 }
 

@@ -20,6 +20,7 @@
 #include "delta.h"
 #include "mfmae/frag.hpp"
 #include "mixing.hpp"
+#include "tiling.hpp"
 
 namespace sgemm_emu {
 
@@ -111,6 +112,59 @@ __device__ inline float largest(const f32x4 (&x)[N]) {
 __device__ constexpr int lower_at(int tile, int step) { return tile < 2 ? tile : 2 * tile - 2 + step; }
 __device__ constexpr int upper_at(int tile, int step) { return tile < 2 ? 2 * tile + step : tile + 2; }
 
+__device__ inline int chunk_base(const int* cu, int n, int tokens) {
+    return min(max(cu[n], 0), tokens) / kC + n;
+}
+
+// A walk over one sequence or one of its parts: chunks [first, first + count)
+// of sequence n, numbered from base in the call; parts: all of the sequence's.
+struct Walk {
+    int n;
+    Span span;
+    int base, first, count, part, parts;
+};
+
+__device__ inline int part_base(const DeltaChunks& p, int n) {
+    return chunk_base(p.cu_seqlens, n, p.tokens) / p.part_chunks + n;
+}
+
+// Walk `index`: a sequence, or a part; count <= 0 if there is no such part.
+__device__ inline Walk walk_of(const DeltaChunks& p, int index) {
+    Walk w{};
+    const int each = (p.tokens + kC - 1) / kC;
+    if (p.part_chunks == 0) {
+        w.n = index;
+        w.parts = 1;
+    } else if (p.cu_seqlens == nullptr) {
+        w.parts = (each + p.part_chunks - 1) / p.part_chunks;
+        w.n = index / w.parts;
+        w.part = index - w.n * w.parts;
+    } else {  // the last sequence whose parts start at index or before
+        int lo = 0, len = p.batch;
+        while (len > 1) {
+            const int step = (len + 63) / 64;
+            const int i = lo + (int)(threadIdx.x & 63) * step;
+            const bool at = i < lo + len && part_base(p, i) <= index;
+            const int k = max(__popcll(__ballot(at)) - 1, 0);
+            len = min(step, len - k * step);
+            lo += k * step;
+        }
+        w.n = __builtin_amdgcn_readfirstlane(lo);
+        w.part = index - part_base(p, w.n);
+    }
+    w.span = span_of(p.cu_seqlens, w.n, p.tokens);
+    w.base = p.cu_seqlens ? chunk_base(p.cu_seqlens, w.n, p.tokens) : w.n * each;
+    const int chunks = (w.span.count + kC - 1) / kC;
+    w.count = chunks;
+    if (p.part_chunks != 0) {
+        // a sequence without tokens has one part, without chunks
+        w.parts = max((chunks + p.part_chunks - 1) / p.part_chunks, 1);
+        w.first = w.part * p.part_chunks;
+        w.count = w.part < 0 || w.part >= w.parts ? -1 : min(p.part_chunks, chunks - w.first);
+    }
+    return w;
+}
+
 // Chunk c of a call: its sequence, the chunk's number in it, first row and
 // rows of the chunk; count <= 0 if there is no such chunk.
 struct Place {
@@ -118,10 +172,6 @@ struct Place {
     Span span;
     int first, count;
 };
-
-__device__ inline int chunk_base(const int* cu, int n, int tokens) {
-    return min(max(cu[n], 0), tokens) / kC + n;
-}
 
 __device__ inline Place place_of(const int* cu, int c, int batch, int tokens) {
     Place p;

@@ -1,84 +1,135 @@
-// The gated delta rule over whole sequences: the chunk form's kernels and
-// workspace.
+// The gated delta rule over whole sequences: workspaces and the order of the
+// chunk form's kernels.
+#include <cstdlib>
+
 #include "delta.h"
 
 namespace sgemm_emu {
-
-int64_t delta_forward_workspace(const delta_emu_forward_t& a) {
-    return delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr) * a.v_heads *
-           DeltaRecord::kForward;
-}
-
-hipError_t launch_delta_forward(const delta_emu_forward_t& a, hipStream_t stream) {
-    DeltaChunks c{};
-    c.dtype = a.dtype, c.batch = a.batch, c.tokens = a.tokens;
-    c.k_heads = a.k_heads, c.v_heads = a.v_heads, c.k_size = a.k_size, c.v_size = a.v_size;
-    c.scale = a.scale;
-    c.cu_seqlens = a.cu_seqlens;
-    c.q = a.q, c.k = a.k, c.v = a.v, c.g = a.g, c.beta = a.beta, c.o = a.o;
-    c.initial = a.initial, c.final_state = a.final_state;
-    c.records = static_cast<char*>(a.workspace);
-    c.record_bytes = DeltaRecord::kForward;
-    c.chunks = (int)delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr);
-    c.wide = delta_wide(a.dtype, a.k_size, {a.q, a.k});
-    c.wide_values = delta_wide(a.dtype, a.v_size, {a.v});
-    if (hipError_t e = launch_delta_prep(c, stream)) return e;
-    return launch_delta_chain(c, stream);
-}
 
 namespace {
 
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// What the gradient keeps per chunk and value head, in bytes: the record, S and
-// its gradient, U and the gradient of its right side.
-struct BackwardParts {
-    int64_t tasks, records, states, updates;
-    int64_t total() const { return records + 2 * states + 2 * updates; }
+// Chunks of a part that the sequences are cut into, 0 if they are not.
+template <class A>
+int part_chunks_of(const A& a, bool backward) {
+    if (a.batch == 0 || a.tokens == 0 || a.v_size == 0) return 0;
+    if (const char* e = getenv("DELTA_PART")) return atoi(e);
+    return 0;
+}
+
+// Byte offsets in the workspace.
+struct Plan {
+    bool packed;
+    int chunks, part_chunks, parts;
+    int64_t record_bytes, states, dstates, updates, dsides, part_states, part_dstates, part_steps,
+        total;
 };
 
-BackwardParts backward_parts(const delta_emu_backward_t& a) {
-    BackwardParts b;
-    b.tasks = delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr) * a.v_heads;
-    b.records = b.tasks * DeltaRecord::kBackward;
-    b.states = rounded(b.tasks * ((a.k_size + 15) / 16 * 16) * a.v_size * 4);
-    b.updates = rounded(b.tasks * kDeltaChunk * a.v_size * 4);
-    return b;
+template <class A>
+Plan plan_of(const A& a, bool backward) {
+    Plan p{};
+    p.packed = a.cu_seqlens != nullptr;
+    p.chunks = (int)delta_chunks(a.batch, a.tokens, p.packed);
+    p.part_chunks = part_chunks_of(a, backward);
+    if (p.part_chunks > 0)
+        p.parts = (int)delta_parts(a.batch, a.tokens, p.packed, p.part_chunks);
+    p.record_bytes = backward ? DeltaRecord::kBackward : DeltaRecord::kForward;
+    const int64_t tasks = (int64_t)p.chunks * a.v_heads, walks = (int64_t)p.parts * a.v_heads;
+    const int64_t rows = (a.k_size + 15) / 16 * 16;
+    const auto take = [&](int64_t bytes) {
+        const int64_t at = p.total;
+        p.total += rounded(bytes);
+        return at;
+    };
+    take(tasks * p.record_bytes);
+    if (backward) {
+        p.states = take(tasks * rows * a.v_size * 4);
+        p.dstates = take(tasks * rows * a.v_size * 4);
+        p.updates = take(tasks * kDeltaChunk * a.v_size * 4);
+        p.dsides = take(tasks * kDeltaChunk * a.v_size * 4);
+    }
+    if (p.parts > 0) {
+        p.part_states = take(walks * a.k_size * a.v_size * 4);
+        p.part_steps = take(walks * rows * rows * 4);
+        if (backward) p.part_dstates = take(walks * a.k_size * a.v_size * 4);
+    }
+    return p;
 }
 
-}  // namespace
-
-int64_t delta_backward_workspace(const delta_emu_backward_t& a) {
-    return backward_parts(a).total();
-}
-
-hipError_t launch_delta_backward(const delta_emu_backward_t& a, hipStream_t stream) {
-    const BackwardParts b = backward_parts(a);
+template <class A>
+DeltaChunks arguments(const A& a, const Plan& p) {
     char* at = static_cast<char*>(a.workspace);
     DeltaChunks c{};
     c.dtype = a.dtype, c.batch = a.batch, c.tokens = a.tokens;
     c.k_heads = a.k_heads, c.v_heads = a.v_heads, c.k_size = a.k_size, c.v_size = a.v_size;
     c.scale = a.scale;
     c.cu_seqlens = a.cu_seqlens;
-    c.q = a.q, c.k = a.k, c.v = a.v, c.g = a.g, c.beta = a.beta, c.d_o = a.d_o;
-    c.dq = a.dq, c.dk = a.dk, c.dv = a.dv, c.dg = a.dg, c.dbeta = a.dbeta;
-    c.initial = a.initial, c.dfinal = a.dfinal, c.dinitial = a.dinitial;
+    c.q = a.q, c.k = a.k, c.v = a.v, c.g = a.g, c.beta = a.beta;
+    c.initial = a.initial;
     c.records = at;
-    c.record_bytes = DeltaRecord::kBackward;
-    c.states = reinterpret_cast<float*>(at + b.records);
-    c.dstates = reinterpret_cast<float*>(at + b.records + b.states);
-    c.updates = reinterpret_cast<float*>(at + b.records + 2 * b.states);
-    c.dsides = reinterpret_cast<float*>(at + b.records + 2 * b.states + b.updates);
-    c.chunks = (int)(b.tasks / a.v_heads);
-    c.backward = true;
+    c.record_bytes = p.record_bytes;
+    c.chunks = p.chunks;
+    c.part_chunks = p.part_chunks, c.parts = p.parts;
+    c.part_states = reinterpret_cast<float*>(at + p.part_states);
+    c.part_steps = reinterpret_cast<float*>(at + p.part_steps);
     c.wide = delta_wide(a.dtype, a.k_size, {a.q, a.k});
-    c.wide_values = delta_wide(a.dtype, a.v_size, {a.v, a.d_o});
-    if (hipError_t e = launch_delta_prep(c, stream)) return e;
-    if (c.v_size > 0) {
-        if (hipError_t e = launch_delta_chain(c, stream)) return e;
-        if (hipError_t e = launch_delta_chain_back(c, stream)) return e;
+    return c;
+}
+
+}  // namespace
+
+int64_t delta_forward_workspace(const delta_emu_forward_t& a) { return plan_of(a, false).total; }
+
+int64_t delta_backward_workspace(const delta_emu_backward_t& a) { return plan_of(a, true).total; }
+
+hipError_t launch_delta_forward(const delta_emu_forward_t& a, hipStream_t stream) {
+    const Plan p = plan_of(a, false);
+    DeltaChunks c = arguments(a, p);
+    c.o = a.o;
+    c.final_state = a.final_state;
+    c.wide_values = delta_wide(a.dtype, a.v_size, {a.v});
+    hipError_t e = launch_delta_prep(c, stream);
+    if (e == hipSuccess && p.parts > 0) {
+        e = launch_delta_chain(c, kDeltaParts, stream);
+        if (e == hipSuccess) e = launch_delta_join(c, false, stream);
     }
-    return launch_delta_gradient(c, stream);
+    if (e == hipSuccess) e = launch_delta_chain(c, kDeltaOutputs, stream);
+    return e;
+}
+
+hipError_t launch_delta_backward(const delta_emu_backward_t& a, hipStream_t stream) {
+    const Plan p = plan_of(a, true);
+    char* at = static_cast<char*>(a.workspace);
+    DeltaChunks c = arguments(a, p);
+    c.d_o = a.d_o;
+    c.dq = a.dq, c.dk = a.dk, c.dv = a.dv, c.dg = a.dg, c.dbeta = a.dbeta;
+    c.dfinal = a.dfinal, c.dinitial = a.dinitial;
+    c.states = reinterpret_cast<float*>(at + p.states);
+    c.dstates = reinterpret_cast<float*>(at + p.dstates);
+    c.updates = reinterpret_cast<float*>(at + p.updates);
+    c.dsides = reinterpret_cast<float*>(at + p.dsides);
+    c.part_dstates = reinterpret_cast<float*>(at + p.part_dstates);
+    c.backward = true;
+    c.wide_values = delta_wide(a.dtype, a.v_size, {a.v, a.d_o});
+    hipError_t e = launch_delta_prep(c, stream);
+    const auto then = [&](auto&& launch) {
+        if (e == hipSuccess) e = launch();
+    };
+    if (a.v_size > 0) {
+        if (p.parts > 0) {
+            then([&] { return launch_delta_chain(c, kDeltaParts, stream); });
+            then([&] { return launch_delta_join(c, false, stream); });
+        }
+        then([&] { return launch_delta_chain(c, kDeltaStates, stream); });
+        if (p.parts > 0) {
+            then([&] { return launch_delta_chain_back(c, kDeltaParts, stream); });
+            then([&] { return launch_delta_join(c, true, stream); });
+        }
+        then([&] { return launch_delta_chain_back(c, kDeltaStates, stream); });
+    }
+    then([&] { return launch_delta_gradient(c, stream); });
+    return e;
 }
 
 }  // namespace sgemm_emu

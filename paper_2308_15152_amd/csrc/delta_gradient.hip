@@ -81,6 +81,20 @@ __device__ inline float sum_row(float x) {
     return x + turned(x, std::integral_constant<int, 1>{});
 }
 
+__device__ inline double sum_row(double x) {
+    const auto turned = [](double y, auto by) {
+        uint64_t u = __builtin_bit_cast(uint64_t, y);
+        const uint32_t lo = __builtin_amdgcn_mov_dpp((int)u, 0x120 + decltype(by)::value, 0xf, 0xf, true);
+        const uint32_t hi =
+            __builtin_amdgcn_mov_dpp((int)(u >> 32), 0x120 + decltype(by)::value, 0xf, 0xf, true);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    };
+    x += turned(x, std::integral_constant<int, 8>{});
+    x += turned(x, std::integral_constant<int, 4>{});
+    x += turned(x, std::integral_constant<int, 2>{});
+    return x + turned(x, std::integral_constant<int, 1>{});
+}
+
 // Rows of tile `tile` of M (or its transpose), columns times `by`, as fragments.
 template <bool kTransposed>
 __device__ inline void write_fragments(const float* M, const float* by, const float* by2, int tile,
@@ -116,7 +130,8 @@ __device__ inline void write_fragments(const float* M, const float* by, const fl
     }
 }
 
-template <class T, int kK>
+// kWide: all rows of q, k, v, d_o and of the workspace in 16-byte loads.
+template <class T, int kK, bool kWide>
 __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks p) {
     using L = Layout<T, kK>;
     constexpr int kVSteps = L::kVSteps, kVBlock = 32 * kVSteps;
@@ -142,16 +157,13 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
     {
         const float* f = reinterpret_cast<const float*>(
             p.records + ((int64_t)c * p.v_heads + kh * group) * p.record_bytes);
-        constexpr int kUnits = 16 * kK / 8;
-        for (int w = threadIdx.x; w < 2 * kUnits; w += kThreads) {
-            const bool is_q = w >= kUnits;
-            const int unit = is_q ? w - kUnits : w;
-            Unit<T, kK> u;
-            u.load(is_q ? q : k, is_q ? p.q.token : p.k.token, unit, at.count, p.k_size, p.wide);
-            const f32x4 s = reinterpret_cast<const f32x4*>(
-                f + 64 * (is_q ? DeltaRecord::kQueryScale : DeltaRecord::kKeyScale))[unit / (kK / 8)];
-            u.store(lds + (is_q ? L::kAtQt : L::kAtKt), unit, s);
-        }
+        // half of the waves each
+        const bool is_q = wave >= kWaves / 2;
+        const int id = threadIdx.x & (kThreads / 2 - 1);
+        Rows<T, kK, kThreads / 2> u;
+        u.load(is_q ? q : k, is_q ? p.q.token : p.k.token, at.count, p.k_size, kWide,
+               f + 64 * (is_q ? DeltaRecord::kQueryScale : DeltaRecord::kKeyScale), id);
+        u.store(lds + (is_q ? L::kAtQt : L::kAtKt), id);
         if (threadIdx.x < kC) {  // powers of two: exact
             small.key_down[threadIdx.x] = 1.0f / f[64 * DeltaRecord::kKeyScale + threadIdx.x];
             small.query_down[threadIdx.x] = 1.0f / f[64 * DeltaRecord::kQueryScale + threadIdx.x];
@@ -162,34 +174,18 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
     f32x4 kk[4] = {};
     if (p.dg.p) {
         const int mt = wave % 4;
-        const auto load_tile = [&](const T* from, int64_t stride, int i, Operand<T>(&f)[L::kSteps]) {
-            const int t = 16 * i + row;
-            const __amdgpu_buffer_rsrc_t r = buffer_at(from);
-            Eight<T> x[L::kSteps];
-            float m = 0.0f;
-#pragma unroll
-            for (int j = 0; j < L::kSteps; ++j) {
-                x[j] = load_eight<T>(r, t * (uint32_t)stride * (uint32_t)sizeof(T), 32 * j + 8 * g,
-                                     p.k_size, t < at.count, p.wide);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(to_f32(x[j].x[e])));
-            }
-            const Scale s = scale_of(max_groups(m));
-#pragma unroll
-            for (int j = 0; j < L::kSteps; ++j) f[j].set(x[j], s.up);
-            return s.down;
-        };
-        Operand<T> a[L::kSteps], b[L::kSteps];
-        const float ad = wave < 4 ? load_tile(q, p.q.token, mt, a) : load_tile(k, p.k.token, mt, a);
+        __syncthreads();
+        const char* from = lds + (wave < 4 ? L::kAtQt : L::kAtKt);
+        const f32x4 ad = reinterpret_cast<const f32x4*>(wave < 4 ? small.query_down
+                                                                 : small.key_down)[4 * mt + g];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (i > mt) continue;
-            const float bd = load_tile(k, p.k.token, i, b);
 #pragma unroll
-            for (int j = 0; j < L::kSteps; ++j) kk[i] = product(a[j], b[j], kk[i]);
-            if (sizeof(T) == 4)  // FP32 rows were scaled
-#pragma unroll
-                for (int r = 0; r < 4; ++r) kk[i][r] *= __shfl(ad, 4 * g + r, 64) * bd;
+            for (int j = 0; j < L::kSteps; ++j)
+                kk[i] = multiply(row_fragment<T, kK>(from, mt, j, lane),
+                                 row_fragment<T, kK>(lds + L::kAtKt, i, j, lane), kk[i]);
+            kk[i] *= ad * small.key_down[16 * i + row];
         }
     }
 
@@ -202,21 +198,9 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         const int64_t task = (int64_t)c * p.v_heads + h;
         __syncthreads();  // the last head's values are used
         if (wave == 0) {
-            const bool in = lane < at.count;
-            const int t = at.first + lane;
-            double sum = 0.0;
-            float b = in ? 1.0f : 0.0f;
-            if (in && p.g.p)
-                sum = log_decay(row_of<const float>(p.g, packed, at.n, at.span, h)[t * p.g.token]);
-            if (in && p.beta.p)
-                b = row_of<const float>(p.beta, packed, at.n, at.span, h)[t * p.beta.token];
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const double u = __shfl_up(sum, d, 64);
-                if (lane >= d) sum += u;
-            }
-            small.G[lane] = sum;
-            small.beta[lane] = b;
+            const char* record = p.records + task * p.record_bytes;
+            small.G[lane] = reinterpret_cast<const double*>(record + DeltaRecord::kAtSums)[lane];
+            small.beta[lane] = reinterpret_cast<const float*>(record)[64 * DeltaRecord::kBeta + lane];
             small.dot[lane] = 0.0f;
         }
         const T* v = row_of<const T>(p.v, packed, at.n, at.span, h) + (int64_t)at.first * p.v.token;
@@ -225,7 +209,6 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         const float* dy = p.dsides + task * kC * p.v_size;
         const float* S = p.states + task * ((p.k_size + 15) / 16 * 16) * p.v_size;
         const float* D = p.dstates + task * ((p.k_size + 15) / 16 * 16) * p.v_size;
-        const bool wide_f = p.v_size % 8 == 0;
 
         f32x4 e1[kOwn] = {}, e2[kOwn] = {}, e3[kOwn] = {}, m[4] = {};
         float sd = 0.0f;
@@ -233,86 +216,82 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             __asm__ volatile("" : "+v"(lane));
             const int row = lane & 15, g = lane >> 4;
             __syncthreads();  // the last block's fragments are used
-            // dO, dY and U: 12 tiles of 16 rows, one wave each
-            for (int job = wave; job < 12; job += kWaves) {
-                const int which = job / 4, i = job % 4, t = 16 * i + row;
-                const auto put = [&](auto parts, const auto (&x)[kVSteps], char* to, float* down) {
-                    constexpr int kN = decltype(parts)::value;
-                    float w[kVSteps][8], top = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < kVSteps; ++j)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            w[j][e] = to_f32(x[j].x[e]);
-                            top = fmaxf(top, fabsf(w[j][e]));
-                        }
-                    const Scale s = scale_of(max_groups(top));
-                    if (g == 0) down[t] = s.down;
-#pragma unroll
-                    for (int j = 0; j < kVSteps; ++j) {
-                        const Frag<kN> f = split<kN>(w[j], s.up);
-#pragma unroll
-                        for (int n = 0; n < kN; ++n)
-                            *reinterpret_cast<half8_t*>(to + n * L::kPart + (i * kVSteps + j) * 1024 +
-                                                        lane * 16) = f.part[n];
-                    }
-                };
-                if (which == 0) {
-                    Eight<T> x[kVSteps];
-#pragma unroll
-                    for (int j = 0; j < kVSteps; ++j)
-                        x[j] = load_eight<T>(buffer_at(d_o), t * (uint32_t)p.d_o.token * (uint32_t)sizeof(T),
-                                             v0 + 32 * j + 8 * g, p.v_size, t < at.count,
-                                             p.wide_values);
-                    put(std::integral_constant<int, L::kParts>{}, x, lds + L::kAtDo, small.down[0]);
-                } else {
-                    const float* from = which == 1 ? dy : u;
-                    Eight<float> x[kVSteps];
-#pragma unroll
-                    for (int j = 0; j < kVSteps; ++j)
-                        x[j] = load_eight<float>(buffer_at(from), 4u * t * p.v_size,
-                                                 v0 + 32 * j + 8 * g, p.v_size, true, wide_f);
-                    put(std::integral_constant<int, 2>{}, x, lds + (which == 1 ? L::kAtDy : L::kAtU),
-                        small.down[which]);
-                    if (which == 1) {
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int j = 0; j < kVSteps; ++j) {
-                            const Eight<T> y = load_eight<T>(
-                                buffer_at(v), t * (uint32_t)p.v.token * (uint32_t)sizeof(T),
-                                v0 + 32 * j + 8 * g, p.v_size, t < at.count, p.wide_values);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                sum = __builtin_fmaf(x[j].x[e], to_f32(y.x[e]), sum);
-                        }
-                        sum += __shfl_xor(sum, 16, 64);
-                        sum += __shfl_xor(sum, 32, 64);
-                        if (g == 0) small.dot[t] += sum;
-                    }
-                }
-            }
-            // this wave's rows of S and D as B operands (columns: key elements)
+            // this wave's rows of S and D, to be B operands (columns: key elements)
             Eight<float> sx[kVSteps], dx[kVSteps];
-            float smax = 0.0f, dmax = 0.0f;
 #pragma unroll
             for (int j = 0; j < kVSteps; ++j) {
-                sx[j] = load_eight<float>(buffer_at(S), 4u * ke * p.v_size, v0 + 32 * j + 8 * g,
-                                          p.v_size, kin, wide_f);
-                dx[j] = load_eight<float>(buffer_at(D), 4u * ke * p.v_size, v0 + 32 * j + 8 * g,
-                                          p.v_size, kin, wide_f);
+                const int e = v0 + 32 * j + 8 * g;
+                sx[j] = load_eight<float>(buffer_at(S), 4u * ke * p.v_size, e, p.v_size, kin, kWide);
+                dx[j] = load_eight<float>(buffer_at(D), 4u * ke * p.v_size, e, p.v_size, kin, kWide);
+            }
+            // 16 rows of dO and U (waves 0 to 3) or of dY and V (4 to 7)
+            const int t = 16 * (wave % 4) + row;
+            Eight<T> tx[kVSteps];
+            Eight<float> fx[kVSteps];
+            {
+                const T* from = wave < 4 ? d_o : v;
+                const uint32_t at_t = t * (uint32_t)(wave < 4 ? p.d_o.token : p.v.token) *
+                                      (uint32_t)sizeof(T);
+                const __amdgpu_buffer_rsrc_t rt = buffer_at(from), rf = buffer_at(wave < 4 ? u : dy);
+#pragma unroll
+                for (int j = 0; j < kVSteps; ++j) {
+                    const int e = v0 + 32 * j + 8 * g;
+                    tx[j] = load_eight<T>(rt, at_t, e, p.v_size, t < at.count, kWide);
+                    fx[j] = load_eight<float>(rf, 4u * t * p.v_size, e, p.v_size, true, kWide);
+                }
+            }
+            const auto put = [&](auto parts, const auto (&x)[kVSteps], char* to, float* down) __attribute__((always_inline)) {
+                constexpr int kN = decltype(parts)::value;
+                float top = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kVSteps; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(to_f32(x[j].x[e])));
+                const Scale s = scale_of(max_groups(top));
+                if (g == 0) down[t] = s.down;
+#pragma unroll
+                for (int j = 0; j < kVSteps; ++j) {
+                    float w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = to_f32(x[j].x[e]);
+                    const Frag<kN> f = split<kN>(w, s.up);
+#pragma unroll
+                    for (int n = 0; n < kN; ++n)
+                        *reinterpret_cast<half8_t*>(to + n * L::kPart +
+                                                    ((wave % 4) * kVSteps + j) * 1024 + lane * 16) =
+                            f.part[n];
+                }
+            };
+            if (wave < 4) {
+                put(std::integral_constant<int, L::kParts>{}, tx, lds + L::kAtDo, small.down[0]);
+            } else {
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < kVSteps; ++j)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        sum = __builtin_fmaf(fx[j].x[e], to_f32(tx[j].x[e]), sum);
+                sum += __shfl_xor(sum, 16, 64);
+                sum += __shfl_xor(sum, 32, 64);
+                if (g == 0) small.dot[t] += sum;
+            }
+            put(std::integral_constant<int, 2>{}, fx, lds + (wave < 4 ? L::kAtU : L::kAtDy),
+                small.down[wave < 4 ? 2 : 1]);
+            float smax = 0.0f, dmax = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kVSteps; ++j)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     smax = fmaxf(smax, fabsf(sx[j].x[e]));
                     dmax = fmaxf(dmax, fabsf(dx[j].x[e]));
                     if (own == 0) sd = __builtin_fmaf(sx[j].x[e], dx[j].x[e], sd);
                 }
-            }
             const Scale ss = scale_of(max_groups(smax)), ds = scale_of(max_groups(dmax));
             Frag<2> sb[kVSteps];
 #pragma unroll
             for (int j = 0; j < kVSteps; ++j) sb[j] = split<2>(sx[j].x, ss.up);
             __syncthreads();
-            const auto fragment = [&](auto parts, int from, int i, int j) {
+            const auto fragment = [&](auto parts, int from, int i, int j) __attribute__((always_inline)) {
                 constexpr int kN = decltype(parts)::value;
                 Frag<kN> f;
 #pragma unroll
@@ -402,8 +381,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-#pragma unroll
-                for (int d = 1; d < 16; d *= 2) rows[r] += __shfl_xor(rows[r], d, 64);
+                rows[r] = sum_row(rows[r]);
                 if (row == 0) small.rows[wave / 4][16 * mt + 4 * g + r] = rows[r];
             }
         }
@@ -426,7 +404,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         __syncthreads();
         const double last = small.G[kC - 1];
             // this lane's element of K or Q at row 16 i + 4 g + r, from the fragments
-            const auto element = [&](const char* rows, const float* down, int i, int r) {
+            const auto element = [&](const char* rows, const float* down, int i, int r) __attribute__((always_inline)) {
                 const char* from = rows + (i * L::kSteps + tile / 2) * 1024 +
                                    slot(((row >> 2) << 4) + 4 * g + r, tile / 2) + 8 * (tile % 2) +
                                    2 * (row & 3);
@@ -529,14 +507,14 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         }
 }
 
-template <class T, int kK>
+template <class T, int kK, bool kWide>
 hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
     constexpr int kBytes = Layout<T, kK>::kBytes;
     static_assert(kBytes <= 160 * 1024, "LDS of a CU");
-    const void* kernel = reinterpret_cast<const void*>(delta_gradient_kernel<T, kK>);
+    const void* kernel = reinterpret_cast<const void*>(delta_gradient_kernel<T, kK, kWide>);
     if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes))
         return e;
-    hipLaunchKernelGGL((delta_gradient_kernel<T, kK>), dim3((unsigned)(a.chunks * a.k_heads)),
+    hipLaunchKernelGGL((delta_gradient_kernel<T, kK, kWide>), dim3((unsigned)(a.chunks * a.k_heads)),
                        dim3(kThreads), kBytes, stream, a);
     return hipGetLastError();
 }
@@ -547,7 +525,12 @@ hipError_t launch_delta_gradient(const DeltaChunks& a, hipStream_t stream) {
     if (a.chunks == 0) return hipSuccess;
     return by_dtype(a.dtype, [&](auto t) {
         using T = decltype(t);
-        return a.k_size <= 64 ? launch<T, 64>(a, stream) : launch<T, 128>(a, stream);
+        // single-element loads are a kernel of their own: in one with the wide
+        // ones they would double its code, which does not fit the instruction
+        // cache as it is
+        if (a.wide && a.wide_values)
+            return a.k_size <= 64 ? launch<T, 64, true>(a, stream) : launch<T, 128, true>(a, stream);
+        return a.k_size <= 64 ? launch<T, 64, false>(a, stream) : launch<T, 128, false>(a, stream);
     });
 }
 

@@ -106,6 +106,7 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
             if (lane >= d) sum += u;
         }
         G[lane] = sum;
+        if (kBackward) reinterpret_cast<double*>(record + DeltaRecord::kAtSums)[lane] = sum;
         beta[lane] = b;
     }
 
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
     const T* q = row_of<const T>(p.q, packed, at.n, at.span, kh) + (int64_t)at.first * p.q.token;
     Operand<T> kf[4][kSteps], qf[kSteps];
     Scale ks[4], qs, mine;
-    auto load_tile = [&](const T* from, int64_t stride, int tile, Operand<T>(&f)[kSteps], Scale& s) {
+    auto load_tile = [&](const T* from, int64_t stride, int tile, Operand<T>(&f)[kSteps], Scale& s) __attribute__((always_inline)) {
         const int t = 16 * tile + row;
         const __amdgpu_buffer_rsrc_t r = buffer_at(from);
         Eight<T> x[kSteps];
@@ -213,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) D[i * kPitch + row] = x[i];
     __syncthreads();
-    const auto block = [&](int i, int j) { return A + 16 * (i * kPitch + j); };
+    const auto block = [&](int i, int j) __attribute__((always_inline)) { return A + 16 * (i * kPitch + j); };
     // 32 x 32: blocks (1, 0) and (3, 2), read and written by one wave each
     if (wave & 1) {
         f32x4 y = block_product(block_rows(block(wave, wave - 1), lane),
