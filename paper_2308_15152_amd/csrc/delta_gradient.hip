@@ -61,7 +61,7 @@ struct Layout {
         };
         float m_down[4][kC];     // of M1, M2, M1^T, M2^T
         float dot[kC];           // dY_t.V_t
-        float part[3][kTiles][kC];  // K.W, a and b per wave
+        float rise[kC], tail[kC];  // e^G, e^{G_64 - G}
         float end[kWaves];          // <D, S> per wave
         double columns[2][4][kC];   // column sums of X, of each row tile
     };
@@ -131,7 +131,8 @@ __device__ inline void write_fragments(const float* M, const float* by, const fl
 }
 
 // kWide: all rows of q, k, v, d_o and of the workspace in 16-byte loads.
-template <class T, int kK, bool kWide>
+// kShared: key heads with more than one value head.
+template <class T, int kK, bool kWide, bool kShared>
 __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks p) {
     using L = Layout<T, kK>;
     constexpr int kVSteps = L::kVSteps, kVBlock = 32 * kVSteps;
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = lane & 15, g = lane >> 4;
+    const int row = lane & 15;
     const int kh = blockIdx.x % p.k_heads, c = blockIdx.x / p.k_heads;
     const Place at = place_of(p.cu_seqlens, c, p.batch, p.tokens);
     if (at.count <= 0) return;  // the whole block
@@ -169,26 +170,23 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             small.query_down[threadIdx.x] = 1.0f / f[64 * DeltaRecord::kQueryScale + threadIdx.x];
         }
     }
-    f32x4 dq[kOwn] = {}, dk[kOwn] = {};
-    // rows wave % 4 of Q K^T (waves 0 to 3) and K K^T, for the decays' gradient
-    f32x4 kk[4] = {};
-    if (p.dg.p) {
-        const int mt = wave % 4;
-        __syncthreads();
-        const char* from = lds + (wave < 4 ? L::kAtQt : L::kAtKt);
-        const f32x4 ad = reinterpret_cast<const f32x4*>(wave < 4 ? small.query_down
-                                                                 : small.key_down)[4 * mt + g];
+    f32x4 dq[kOwn] = {}, dk[kOwn] = {};  // sums over the heads (kShared)
+    T* dqo = row_of<T>(p.dq, packed, at.n, at.span, kh) + (int64_t)at.first * p.dq.token;
+    T* dko = row_of<T>(p.dk, packed, at.n, at.span, kh) + (int64_t)at.first * p.dk.token;
+    const auto put_rows = [&](int i, f32x4 x, f32x4 y) __attribute__((always_inline)) {
+        const int lane = threadIdx.x & 63;
+        const int e = 16 * tile + (lane & 15);
+        const __amdgpu_buffer_rsrc_t to_q = buffer_at(dqo), to_k = buffer_at(dko);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i > mt) continue;
-#pragma unroll
-            for (int j = 0; j < L::kSteps; ++j)
-                kk[i] = multiply(row_fragment<T, kK>(from, mt, j, lane),
-                                 row_fragment<T, kK>(lds + L::kAtKt, i, j, lane), kk[i]);
-            kk[i] *= ad * small.key_down[16 * i + row];
+        for (int r = 0; r < 4; ++r) {
+            const int t = 16 * i + 4 * (lane >> 4) + r;
+            const bool in = e < p.k_size && t < at.count;
+            store_word(from_f32<T>(x[r]), to_q,
+                       in ? (t * (uint32_t)p.dq.token + e) * (uint32_t)sizeof(T) : kPastEnd);
+            store_word(from_f32<T>(y[r]), to_k,
+                       in ? (t * (uint32_t)p.dk.token + e) * (uint32_t)sizeof(T) : kPastEnd);
         }
-    }
-
+    };
     for (int h = kh * group; h < (kh + 1) * group; ++h) {
         // Everything that depends on the lane is formed again for every head:
         // kept from one to the next, some 250 LDS addresses would be in scratch.
@@ -199,7 +197,10 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         __syncthreads();  // the last head's values are used
         if (wave == 0) {
             const char* record = p.records + task * p.record_bytes;
-            small.G[lane] = reinterpret_cast<const double*>(record + DeltaRecord::kAtSums)[lane];
+            const double G = reinterpret_cast<const double*>(record + DeltaRecord::kAtSums)[lane];
+            small.G[lane] = G;
+            small.rise[lane] = expf((float)G);
+            small.tail[lane] = expf((float)(__shfl(G, 63, 64) - G));
             small.beta[lane] = reinterpret_cast<const float*>(record)[64 * DeltaRecord::kBeta + lane];
             small.dot[lane] = 0.0f;
         }
@@ -357,24 +358,41 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             const int mt = wave % 4;
             float* M = wave < 4 ? M1 : M2;
             double rows[4] = {};
+            const char* kk_rows = lds + (wave < 4 ? L::kAtQt : L::kAtKt);
+            const int at_t = 4 * mt + g;
+            const f32x4 beta = reinterpret_cast<const f32x4*>(small.beta)[at_t];
+            f32x4 by = reinterpret_cast<const f32x4*>(wave < 4 ? small.query_down
+                                                               : small.key_down)[at_t];
+            if (wave >= 4) by *= -beta;
+            double Gt[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) Gt[r] = small.G[16 * mt + 4 * g + r];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int s = 16 * i + row;
                 double column = 0.0;
-                if (i <= mt)
+                if (i <= mt) {
+                    // Q K^T or -diag(beta) K K^T
+                    f32x4 kk{};
+#pragma unroll
+                    for (int j = 0; j < L::kSteps; ++j)
+                        kk = multiply(row_fragment<T, kK>(kk_rows, mt, j, lane),
+                                      row_fragment<T, kK>(lds + L::kAtKt, i, j, lane), kk);
+                    kk *= by * small.key_down[s];
+                    const double Gs = small.G[s];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int t = 16 * mt + 4 * g + r;
                         const bool on = wave < 4 ? s <= t : s < t;
-                        const float e = on ? expf((float)(small.G[t] - small.G[s])) : 0.0f;
+                        const float e = on ? expf((float)(Gt[r] - Gs)) : 0.0f;
                         const float x = on ? (wave < 4 ? p.scale * e : e) * m[i][r] : 0.0f;
                         M[t * kPitch + s] = x;
                         // a token and itself have no decay between them
-                        const double y =
-                            s < t ? (double)((wave < 4 ? x : -small.beta[t] * x) * kk[i][r]) : 0.0;
+                        const double y = s < t ? (double)(x * kk[r]) : 0.0;
                         rows[r] += y;
                         column += y;
                     }
+                }
                 column += __shfl_xor(column, 16, 64);
                 column += __shfl_xor(column, 32, 64);
                 if (g == 0) small.columns[wave / 4][mt][s] = column;
@@ -403,15 +421,17 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
         }
         __syncthreads();
         const double last = small.G[kC - 1];
-            // this lane's element of K or Q at row 16 i + 4 g + r, from the fragments
-            const auto element = [&](const char* rows, const float* down, int i, int r) __attribute__((always_inline)) {
+        // K.W, a and b of every tile of elements, where M1 was
+        auto& part = *reinterpret_cast<float(*)[3][L::kTiles][kC]>(lds + L::kAtM);
+            // this lane's element of K or Q at row 16 i + 4 g + r, scaled as the fragments
+            const auto element = [&](const char* rows, int i, int r) __attribute__((always_inline)) {
                 const char* from = rows + (i * L::kSteps + tile / 2) * 1024 +
                                    slot(((row >> 2) << 4) + 4 * g + r, tile / 2) + 8 * (tile % 2) +
                                    2 * (row & 3);
                 float x = (float)*reinterpret_cast<const _Float16*>(from);
                 if (L::kParts == 2)
                     x += (float)*reinterpret_cast<const _Float16*>(from + 4 * L::kSteps * 1024);
-                return x * down[16 * i + 4 * g + r];
+                return x;
             };
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
@@ -432,26 +452,34 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
                     a[3] = multiply(matrix_fragment<2>(from + 3 * kBytes, upper_at(ti, j), lane), kt, a[3]);
                 }
             }
+            const auto of_rows = [&](const float* x) __attribute__((always_inline)) {
+                return reinterpret_cast<const f32x4*>(x)[4 * ti + g];
+            };
+            const f32x4 beta = of_rows(small.beta), rise = of_rows(small.rise);
+            const f32x4 de = e1[i] * rise * p.scale, we = e2[i] * rise;
+            const f32x4 te = e3[i] * of_rows(small.tail);
+            const f32x4 w = -(we + a[1] * of_rows(small.m_down[1]));
+            const f32x4 dqt = de + a[0] * of_rows(small.m_down[0]);
+            const f32x4 dkt = beta * w + (te + (a[2] * of_rows(small.m_down[2]) -
+                                                a[3] * of_rows(small.m_down[3])));
+            const f32x4 kdown = of_rows(small.key_down), qdown = of_rows(small.query_down);
+            if (kShared) {
+                dq[i] += dqt;
+                dk[i] += dkt;
+            } else {
+                put_rows(ti, dqt, dkt);
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int t = 16 * ti + 4 * g + r;
-                const float kd = element(lds + L::kAtKt, small.key_down, ti, r);
-                const float qd = element(lds + L::kAtQt, small.query_down, ti, r);
-                const float rise = expf((float)small.G[t]);
-                const float tail = expf((float)(last - small.G[t]));
-                const float de = p.scale * rise * e1[i][r], we = rise * e2[i][r];
-                const float w = -__builtin_fmaf(small.m_down[1][t], a[1][r], we);
-                const float te = tail * e3[i][r];
-                const float bt = small.beta[t];
-                dq[i][r] += __builtin_fmaf(small.m_down[0][t], a[0][r], de);
-                dk[i][r] += bt * w +
-                            (te + (small.m_down[2][t] * a[2][r] - small.m_down[3][t] * a[3][r]));
-                const float sums[3] = {sum_row(kd * w),
-                                       sum_row(__builtin_fmaf(qd, de, -(bt * kd * we))),
-                                       sum_row(kd * te)};
+                const float kd = element(lds + L::kAtKt, ti, r) * kdown[r];
+                const float qd = element(lds + L::kAtQt, ti, r) * qdown[r];
+                const float sums[3] = {sum_row(kd * w[r]),
+                                       sum_row(__builtin_fmaf(qd, de[r], -(beta[r] * kd * we[r]))),
+                                       sum_row(kd * te[r])};
                 if (row == 0)
 #pragma unroll
-                    for (int n = 0; n < 3; ++n) small.part[n][tile][t] = sums[n];
+                    for (int n = 0; n < 3; ++n) part[n][tile][t] = sums[n];
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -464,9 +492,9 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             double later = 0.0, before = 0.0;  // summed over i >= t and j <= t
 #pragma unroll
             for (int i = 0; i < L::kTiles; ++i) {
-                db += small.part[0][i][lane];
-                later += small.part[1][i][lane];
-                before += small.part[2][i][lane];
+                db += part[0][i][lane];
+                later += part[1][i][lane];
+                before += part[2][i][lane];
             }
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) s += small.end[i];
@@ -493,28 +521,19 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             }
         }
     }
-    T* dqo = row_of<T>(p.dq, packed, at.n, at.span, kh) + (int64_t)at.first * p.dq.token + ke;
-    T* dko = row_of<T>(p.dk, packed, at.n, at.span, kh) + (int64_t)at.first * p.dk.token + ke;
+    if (kShared)
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = 16 * (own + i) + 4 * g + r;
-            if (kin && t < at.count) {
-                dqo[(int64_t)t * p.dq.token] = from_f32<T>(dq[i][r]);
-                dko[(int64_t)t * p.dk.token] = from_f32<T>(dk[i][r]);
-            }
-        }
+        for (int i = 0; i < kOwn; ++i) put_rows(own + i, dq[i], dk[i]);
 }
 
-template <class T, int kK, bool kWide>
+template <class T, int kK, bool kWide, bool kShared>
 hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
     constexpr int kBytes = Layout<T, kK>::kBytes;
     static_assert(kBytes <= 160 * 1024, "LDS of a CU");
-    const void* kernel = reinterpret_cast<const void*>(delta_gradient_kernel<T, kK, kWide>);
+    const void* kernel = reinterpret_cast<const void*>(delta_gradient_kernel<T, kK, kWide, kShared>);
     if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kBytes))
         return e;
-    hipLaunchKernelGGL((delta_gradient_kernel<T, kK, kWide>), dim3((unsigned)(a.chunks * a.k_heads)),
+    hipLaunchKernelGGL((delta_gradient_kernel<T, kK, kWide, kShared>), dim3((unsigned)(a.chunks * a.k_heads)),
                        dim3(kThreads), kBytes, stream, a);
     return hipGetLastError();
 }
@@ -528,9 +547,15 @@ hipError_t launch_delta_gradient(const DeltaChunks& a, hipStream_t stream) {
         // single-element loads are a kernel of their own: in one with the wide
         // ones they would double its code, which does not fit the instruction
         // cache as it is
-        if (a.wide && a.wide_values)
-            return a.k_size <= 64 ? launch<T, 64, true>(a, stream) : launch<T, 128, true>(a, stream);
-        return a.k_size <= 64 ? launch<T, 64, false>(a, stream) : launch<T, 128, false>(a, stream);
+        const bool small = a.k_size <= 64;
+        if (!a.wide || !a.wide_values)
+            return small ? launch<T, 64, false, true>(a, stream)
+                         : launch<T, 128, false, true>(a, stream);
+        if (a.v_heads > a.k_heads)
+            return small ? launch<T, 64, true, true>(a, stream)
+                         : launch<T, 128, true, true>(a, stream);
+        return small ? launch<T, 64, true, false>(a, stream)
+                     : launch<T, 128, true, false>(a, stream);
     });
 }
 
