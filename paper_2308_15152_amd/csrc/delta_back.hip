@@ -64,10 +64,10 @@ void delta_back_kernel(DeltaChunks p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = lane >> 4;
     const int slices = (p.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
-    // slices of a head on one XCD: they read the same K, Q, T and P
-    const int walk_task = xcd_task(blockIdx.x, gridDim.x);
-    const int slice = walk_task % slices;
-    const int h = (walk_task / slices) % p.v_heads, index = walk_task / slices / p.v_heads;
+    const WalkTask w = walk_task(slices);
+    const int slice = w.slice;
+    const int h = w.task % p.v_heads, index = w.task / p.v_heads;
+    if (index >= (p.part_chunks > 0 ? p.parts : p.batch)) return;  // the whole block
     const int kh = h / (p.v_heads / p.k_heads);
     const bool packed = p.cu_seqlens != nullptr;
     const Walk walk = walk_of(p, index);
@@ -379,7 +379,7 @@ hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
             hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
     hipLaunchKernelGGL((delta_back_kernel<T, kK, kWalkers, kCarry>),
-                       dim3((unsigned)(slices * a.v_heads * walks)),
+                       dim3((unsigned)walk_blocks(walks * a.v_heads, slices)),
                        dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
 }

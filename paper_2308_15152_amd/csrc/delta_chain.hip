@@ -80,10 +80,10 @@ void delta_chain_kernel(DeltaChunks p) {
     const int v_slices = (p.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
     const int slices =
         v_slices + (kMode == kPartSteps ? (p.k_size + 16 * kWalkers - 1) / (16 * kWalkers) : 0);
-    // slices of a head on one XCD: they read the same K, Q, T and P
-    const int task = xcd_task(blockIdx.x, gridDim.x);
-    int slice = task % slices;
-    const int h = (task / slices) % p.v_heads, index = task / slices / p.v_heads;
+    const WalkTask w = walk_task(slices);
+    int slice = w.slice;
+    const int h = w.task % p.v_heads, index = w.task / p.v_heads;
+    if (index >= (p.part_chunks > 0 ? p.parts : p.batch)) return;  // the whole block
     const int kh = h / (p.v_heads / p.k_heads);
     const bool packed = p.cu_seqlens != nullptr;
     const Walk walk = walk_of(p, index);
@@ -423,7 +423,7 @@ hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
             hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
     hipLaunchKernelGGL((delta_chain_kernel<T, kK, kWalkers, kMode>),
-                       dim3((unsigned)(slices * a.v_heads * walks)),
+                       dim3((unsigned)walk_blocks(walks * a.v_heads, slices)),
                        dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
 }

@@ -20,7 +20,6 @@
 #include "delta.h"
 #include "mfmae/frag.hpp"
 #include "mixing.hpp"
-#include "tiling.hpp"
 
 namespace sgemm_emu {
 
@@ -164,6 +163,20 @@ __device__ inline Walk walk_of(const DeltaChunks& p, int index) {
     }
     return w;
 }
+
+// Block -> (walk and value head, slice of columns).  The slices of a head read
+// the same K, Q, T and P: they go to one XCD (blocks are dealt out to the 8 in
+// turn), and consecutive heads to different ones, so that sequences of different
+// lengths spread over all.  The grid is walk_blocks(); task >= tasks: nothing to do.
+struct WalkTask {
+    int task, slice;
+};
+
+__device__ inline WalkTask walk_task(int slices) {
+    const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
+    return {i / slices * 8 + xcd, i % slices};
+}
+inline int64_t walk_blocks(int64_t tasks, int64_t slices) { return (tasks + 7) / 8 * 8 * slices; }
 
 // Chunk c of a call: its sequence, the chunk's number in it, first row and
 // rows of the chunk; count <= 0 if there is no such chunk.

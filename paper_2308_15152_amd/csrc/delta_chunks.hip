@@ -1,7 +1,5 @@
 // The gated delta rule over whole sequences: workspaces and the order of the
 // chunk form's kernels.
-#include <cstdlib>
-
 #include "delta.h"
 
 namespace sgemm_emu {
@@ -10,12 +8,61 @@ namespace {
 
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Chunks of a part that the sequences are cut into, 0 if they are not.
+// Columns of the state that a block of a walk takes (delta_chain.hip,
+// delta_back.hip).
+struct Columns {
+    int outputs, states, steps, back;
+};
+
+Columns columns_of(int dtype, int k_size) {
+    const bool large_f32 = dtype == SGEMM_EMU_F32 && k_size > 64;
+    return {large_f32 ? 16 : 32, 32, large_f32 ? 32 : 64, large_f32 ? 16 : 32};
+}
+
+// Chunks of a part that the sequences are cut into, 0 if they are not.  A walk
+// takes a time per chunk whatever the number of its blocks up to one per CU, and the parts
+// cost a walk more, over k_size more columns, and the join.  The estimate below uses
+// measured times (us, 128 x 128 states in bfloat16; other sizes keep their ratios): a chunk
+// takes 2.3 to 2.9 in the walk for outputs, 2.5 for states, 2.6 for N and M, 4.1 back;
+// a part 7.5 in the join.  32768 tokens on 8 heads: 8 parts 405 us, not cut 1160; 4096
+// tokens on 64 heads: 2 parts 250, not cut 183.
 template <class A>
 int part_chunks_of(const A& a, bool backward) {
     if (a.batch == 0 || a.tokens == 0 || a.v_size == 0) return 0;
-    if (const char* e = getenv("DELTA_PART")) return atoi(e);
-    return 0;
+    constexpr double kCus = 256, kOutputs = 2.8, kStates = 2.5, kSteps = 2.6, kBack = 4.1,
+                     kJoin = 7.5, kJoinStart = 10;
+    const Columns c = columns_of(a.dtype, a.k_size);
+    const auto blocks = [&](int64_t columns, int each) {  // of all sequences and heads
+        return (double)((columns + each - 1) / each) * a.v_heads * a.batch;
+    };
+    const auto rounds = [&](double n) { return n <= kCus ? 1.0 : (double)((int64_t)((n + kCus - 1) / kCus)); };
+    // chunks of a sequence; of packed ones, whose lengths are not known here, the mean
+    const int64_t chunks = a.cu_seqlens ? (a.tokens / kDeltaChunk + a.batch) / a.batch
+                                        : (a.tokens + kDeltaChunk - 1) / kDeltaChunk;
+    const double steps = blocks(a.v_size, c.steps) + blocks(a.k_size, c.steps);
+    double best = 0;
+    int64_t chosen = 0;
+    for (int64_t parts = 1; parts <= 64 && parts <= chunks; ++parts) {
+        const int64_t m = (chunks + parts - 1) / parts;
+        const double p = (double)((chunks + m - 1) / m);
+        double walk = backward ? rounds(p * blocks(a.v_size, c.states)) * kStates +
+                                     rounds(p * blocks(a.v_size, c.back)) * kBack
+                               : rounds(p * blocks(a.v_size, c.outputs)) * kOutputs;
+        double time = 0;
+        if (parts > 1) {
+            walk += rounds((backward ? p : p - 1) * steps) * kSteps;
+            if (backward) walk += rounds((p - 1) * blocks(a.v_size, c.back)) * kBack;
+            time = (backward ? 2 : 1) * (kJoinStart + kJoin * p);
+        }
+        time += walk * m;
+        if (parts == 1) {
+            best = 0.9 * time;  // worth the trouble
+        } else if (time < best) {
+            best = time;
+            chosen = m;
+        }
+    }
+    return (int)chosen;
 }
 
 // Byte offsets in the workspace.
