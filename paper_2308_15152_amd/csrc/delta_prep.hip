@@ -74,12 +74,14 @@ __device__ inline void write_fragments(const float* M, int tile, int lane, char*
 }
 
 template <class T, int kK, bool kBackward>
-__global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_kernel(DeltaChunks p) {
     constexpr int kSteps = kK / 32;
-    __shared__ __attribute__((aligned(16))) float A[kC * kPitch];
-    __shared__ __attribute__((aligned(16))) float P[kC * kPitch];
+    // A and P; before them, in the same place, k's rows as operands
+    __shared__ __attribute__((aligned(16))) float lds[2 * kC * kPitch];
+    float *A = lds, *P = lds + kC * kPitch;
+    static_assert(sizeof(Operand<T>) * 64 * 4 * kSteps <= sizeof(lds), "k's rows");
     __shared__ double G[kC];
-    __shared__ float beta[kC];
+    __shared__ float beta[kC], key_down[kC];
 
     const int h = blockIdx.x % p.v_heads, c = blockIdx.x / p.v_heads;
     const Place at = place_of(p.cu_seqlens, c, p.batch, p.tokens);
@@ -88,18 +90,49 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
     const int kh = h / (p.v_heads / p.k_heads);
     char* record = p.records + ((int64_t)c * p.v_heads + h) * p.record_bytes;
     float* factors = reinterpret_cast<float*>(record);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 15, g = lane >> 4;
 
-    if (wave == 0) {  // running sums of the decays, and the strengths
-        const bool in = lane < at.count;
+    // This wave's 16 rows of k and q, in operand order, on their way (after the
+    // decays, which are waited for first).
+    double sum = 0.0;
+    float strength = lane < at.count ? 1.0f : 0.0f;
+    if (wave == 0 && lane < at.count) {
         const int t = at.first + lane;
-        double sum = 0.0;
-        float b = in ? 1.0f : 0.0f;
-        if (in && p.g.p)
+        if (p.g.p)
             sum = log_decay(row_of<const float>(p.g, packed, at.n, at.span, h)[t * p.g.token]);
-        if (in && p.beta.p)
-            b = row_of<const float>(p.beta, packed, at.n, at.span, h)[t * p.beta.token];
+        if (p.beta.p)
+            strength = row_of<const float>(p.beta, packed, at.n, at.span, h)[t * p.beta.token];
+    }
+    const T* k = row_of<const T>(p.k, packed, at.n, at.span, kh) + (int64_t)at.first * p.k.token;
+    const T* q = row_of<const T>(p.q, packed, at.n, at.span, kh) + (int64_t)at.first * p.q.token;
+    const auto load_tile = [&](const T* from, int64_t stride, int tile, Eight<T>(&x)[kSteps])
+                               __attribute__((always_inline)) {
+        const int t = 16 * tile + row;
+        const __amdgpu_buffer_rsrc_t r = buffer_at(from);
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+            x[j] = load_eight<T>(r, t * (uint32_t)stride * (uint32_t)sizeof(T), 32 * j + 8 * g, p.k_size,
+                                 t < at.count, p.wide);
+    };
+    const auto take_tile = [&](const Eight<T>(&x)[kSteps], Operand<T>(&f)[kSteps])
+                               __attribute__((always_inline)) {
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(to_f32(x[j].x[i])));
+        const Scale s = scale_of(max_groups(m));
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) f[j].set(x[j], s.up);
+        return s;
+    };
+    Eight<T> kx[kSteps], qx[kSteps];
+    load_tile(k, p.k.token, wave, kx);
+    load_tile(q, p.q.token, wave, qx);
+
+    if (wave == 0) {  // running sums of the decays, and the strengths
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const double u = __shfl_up(sum, d, 64);
@@ -107,42 +140,14 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
         }
         G[lane] = sum;
         if (kBackward) reinterpret_cast<double*>(record + DeltaRecord::kAtSums)[lane] = sum;
-        beta[lane] = b;
+        beta[lane] = strength;
     }
-
-    // k's four row tiles and this wave's tile of q, in operand order
-    const T* k = row_of<const T>(p.k, packed, at.n, at.span, kh) + (int64_t)at.first * p.k.token;
-    const T* q = row_of<const T>(p.q, packed, at.n, at.span, kh) + (int64_t)at.first * p.q.token;
-    Operand<T> kf[4][kSteps], qf[kSteps];
-    Scale ks[4], qs, mine;
-    auto load_tile = [&](const T* from, int64_t stride, int tile, Operand<T>(&f)[kSteps], Scale& s) __attribute__((always_inline)) {
-        const int t = 16 * tile + row;
-        const __amdgpu_buffer_rsrc_t r = buffer_at(from);
-        Eight<T> x[kSteps];
-        float m = 0.0f;
+    Operand<T> kw[kSteps], qf[kSteps];
+    Scale mine = take_tile(kx, kw), qs = take_tile(qx, qf);
+    Operand<T>* rows = reinterpret_cast<Operand<T>*>(lds);
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j) {
-            x[j] = load_eight<T>(r, t * (uint32_t)stride * (uint32_t)sizeof(T), 32 * j + 8 * g, p.k_size,
-                                 t < at.count, p.wide);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(to_f32(x[j].x[i])));
-        }
-        s = scale_of(max_groups(m));
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j) f[j].set(x[j], s.up);
-    };
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i <= wave) load_tile(k, p.k.token, i, kf[i], ks[i]);
-    load_tile(q, p.q.token, wave, qf, qs);
-    Operand<T> kw[kSteps];  // this wave's tile of k
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i == wave) {
-            mine = ks[i];
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j) kw[j] = kf[i][j];
-        }
+    for (int j = 0; j < kSteps; ++j) rows[(wave * kSteps + j) * 64 + lane] = kw[j];
+    if (g == 0) key_down[16 * wave + row] = mine.down;
     __syncthreads();
 
     // this wave's rows of A and P
@@ -159,25 +164,32 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaChunks p) {
     f32x4 dq;
 #pragma unroll
     for (int r = 0; r < 4; ++r) dq[r] = __shfl(qs.down, 4 * g + r, 64);
+    f32x4 kk[4] = {}, qk[4] = {};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (i > wave) continue;
-        f32x4 kk{}, qk{};
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-            kk = product(kw[j], kf[i][j], kk);
-            qk = product(qf[j], kf[i][j], qk);
+            const Operand<T> kf = rows[(i * kSteps + j) * 64 + lane];
+            kk[i] = product(kw[j], kf, kk[i]);
+            qk[i] = product(qf[j], kf, qk[i]);
         }
+    }
+    __syncthreads();  // k's rows are used
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i > wave) continue;
+        const float down = key_down[16 * i + row];
         const int s = 16 * i + row;
         const double Gs = G[s];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int t = 16 * wave + 4 * g + r;
             const float e = s <= t ? expf((float)(Gt[r] - Gs)) : 0.0f;
-            float a = kk[r], b = qk[r];
+            float a = kk[i][r], b = qk[i][r];
             if (sizeof(T) == 4) {  // FP32 rows were scaled
-                a = a * d[r] * ks[i].down;
-                b = b * dq[r] * ks[i].down;
+                a = a * d[r] * down;
+                b = b * dq[r] * down;
             }
             A[t * kPitch + s] = s < t ? bt[r] * e * a : 0.0f;
             P[t * kPitch + s] = s <= t ? p.scale * e * b : 0.0f;
