@@ -39,7 +39,7 @@ __device__ inline void store(T* p, Vec<T, N> v) {
 
 // A piece is N pairs: in interleaved order 2N consecutive elements, in half
 // order N elements and their N partners; or 2N elements that are copied.
-template <class T, int N, bool kInterleaved>
+template <class T, int N, bool kInterleaved, int kHeads>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs p, int64_t first_block) {
     const rotary_emu_t& a = p.a;
     const int items = p.units * p.parts;
@@ -69,40 +69,48 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs p, int64_t 
             }
         }
         const int first = part * p.per, last = min(first + p.per, a.heads[0] + a.heads[1]);
-        for (int h = first; h < last; ++h) {
+        const auto row_at = [&](const sgemm_emu_view_t(&views)[2], int h) __attribute__((always_inline)) {
             const int which = h < a.heads[0] ? 0 : 1;
-            const sgemm_emu_view_t& vx = a.x[which];
-            const sgemm_emu_view_t& vy = a.y[which];
-            const int head = which ? h - a.heads[0] : h;
-            const T* x = static_cast<const T*>(vx.p) + b * vx.batch + t * vx.token + head * vx.head;
-            T* y = static_cast<T*>(vy.p) + b * vy.batch + t * vy.token + head * vy.head;
-            if (!turn) {
-                const int e = a.rot + (unit - p.turned) * 2 * N;
-                if (x == y) continue;
-                if (e + 2 * N <= a.size) {
-                    const Vec<T, N> u = load<T, N>(x + e), v = load<T, N>(x + e + N);
-                    store<T, N>(y + e, u);
-                    store<T, N>(y + e + N, v);
-                } else {
-                    for (int i = e; i < a.size; ++i) y[i] = x[i];
-                }
-                continue;
-            }
-            const int ea = kInterleaved ? unit * 2 * N : unit * N;
-            const int eb = kInterleaved ? ea + N : ea + half;
-            Vec<T, N> u = load<T, N>(x + ea), v = load<T, N>(x + eb);
-            T in[2 * N], out[2 * N];
-            *reinterpret_cast<Vec<T, N>*>(in) = u;
-            *reinterpret_cast<Vec<T, N>*>(in + N) = v;
+            const sgemm_emu_view_t& v = views[which];
+            return static_cast<T*>(v.p) + b * v.batch + t * v.token +
+                   (which ? h - a.heads[0] : h) * v.head;
+        };
+        if (turn || a.rot + (unit - p.turned + 1) * 2 * N <= a.size) {
+            // two vectors of each head: all loads first, so that they are in flight together
+            const int c0 = a.rot + (unit - p.turned) * 2 * N;
+            const int ea = !turn ? c0 : kInterleaved ? unit * 2 * N : unit * N;
+            const int eb = !turn || kInterleaved ? ea + N : ea + half;
+            T in[kHeads][2 * N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int ia = kInterleaved ? 2 * i : i, ib = kInterleaved ? 2 * i + 1 : N + i;
-                const float xa = to_f32(in[ia]), xb = to_f32(in[ib]);
-                out[ia] = from_f32<T>(__builtin_fmaf(xa, c[i], -(xb * s[i])));
-                out[ib] = from_f32<T>(__builtin_fmaf(xa, s[i], xb * c[i]));
+            for (int j = 0; j < kHeads; ++j)
+                if (first + j < last) {
+                    const T* x = row_at(a.x, first + j);
+                    *reinterpret_cast<Vec<T, N>*>(in[j]) = load<T, N>(x + ea);
+                    *reinterpret_cast<Vec<T, N>*>(in[j] + N) = load<T, N>(x + eb);
+                }
+#pragma unroll
+            for (int j = 0; j < kHeads; ++j) {
+                if (first + j >= last) continue;
+                T* y = row_at(a.y, first + j);
+                if (!turn && y == row_at(a.x, first + j)) continue;
+                T out[2 * N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int ia = kInterleaved ? 2 * i : i, ib = kInterleaved ? 2 * i + 1 : N + i;
+                    const float xa = to_f32(in[j][ia]), xb = to_f32(in[j][ib]);
+                    out[ia] = turn ? from_f32<T>(__builtin_fmaf(xa, c[i], -(xb * s[i]))) : in[j][ia];
+                    out[ib] = turn ? from_f32<T>(__builtin_fmaf(xa, s[i], xb * c[i])) : in[j][ib];
+                }
+                store<T, N>(y + ea, *reinterpret_cast<Vec<T, N>*>(out));
+                store<T, N>(y + eb, *reinterpret_cast<Vec<T, N>*>(out + N));
             }
-            store<T, N>(y + ea, *reinterpret_cast<Vec<T, N>*>(out));
-            store<T, N>(y + eb, *reinterpret_cast<Vec<T, N>*>(out + N));
+        } else {  // the end of a row that is copied
+            for (int h = first; h < last; ++h) {
+                const T* x = row_at(a.x, h);
+                T* y = row_at(a.y, h);
+                if (x != y)
+                    for (int e = a.rot + (unit - p.turned) * 2 * N; e < a.size; ++e) y[e] = x[e];
+            }
         }
     }
 }
@@ -113,16 +121,11 @@ bool rows_aligned(const sgemm_emu_view_t& v, int elem, int bytes) {
     return (uintptr_t)v.p % bytes == 0 && v.batch % n == 0 && v.token % n == 0 && v.head % n == 0;
 }
 
-template <class T, int N>
-hipError_t launch(RotaryArgs p, hipStream_t stream) {
+template <class T, int N, int kHeads>
+hipError_t launch_heads(RotaryArgs p, hipStream_t stream) {
     const rotary_emu_t& a = p.a;
     const int heads = a.heads[0] + a.heads[1];
-    p.turned = a.rot / (2 * N);
-    p.units = p.turned + (a.size - a.rot + 2 * N - 1) / (2 * N);
-    // Heads that share a thread's angles: four, where that still leaves
-    // every CU its eight blocks, else one
-    const int64_t work = p.total * p.units * heads;
-    p.per = work / (4 * kThreads) >= 8 * 256 ? 4 : 1;
+    p.per = kHeads;
     p.parts = (heads + p.per - 1) / p.per;
     const int64_t items = (int64_t)p.units * p.parts;
     p.rows = items >= kThreads ? 1 : (int)(kThreads / items);
@@ -130,14 +133,26 @@ hipError_t launch(RotaryArgs p, hipStream_t stream) {
     for (int64_t first = 0; first < blocks; first += kMostBlocks) {
         const dim3 grid((unsigned)(blocks - first < kMostBlocks ? blocks - first : kMostBlocks));
         if (a.interleaved)
-            hipLaunchKernelGGL((rotary_kernel<T, N, true>), grid, dim3(kThreads), 0, stream, p,
+            hipLaunchKernelGGL((rotary_kernel<T, N, true, kHeads>), grid, dim3(kThreads), 0, stream, p,
                                first);
         else
-            hipLaunchKernelGGL((rotary_kernel<T, N, false>), grid, dim3(kThreads), 0, stream, p,
+            hipLaunchKernelGGL((rotary_kernel<T, N, false, kHeads>), grid, dim3(kThreads), 0, stream, p,
                                first);
         if (hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
+}
+
+template <class T, int N>
+hipError_t launch(RotaryArgs p, hipStream_t stream) {
+    const rotary_emu_t& a = p.a;
+    p.turned = a.rot / (2 * N);
+    p.units = p.turned + (a.size - a.rot + 2 * N - 1) / (2 * N);
+    // Heads that share a thread's angles, whose loads are in flight together:
+    // four, where that still leaves every CU its eight blocks, else one
+    const int64_t work = p.total * p.units * (a.heads[0] + a.heads[1]);
+    return work / (4 * kThreads) >= 8 * 256 ? launch_heads<T, N, 4>(p, stream)
+                                            : launch_heads<T, N, 1>(p, stream);
 }
 
 __global__ __launch_bounds__(kThreads) void rotary_table_kernel(int rows, int half, double base,
