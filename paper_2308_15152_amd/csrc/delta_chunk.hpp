@@ -313,14 +313,6 @@ __device__ inline f32x4 product(const Operand<float>& a, const Operand<float>& b
 template <class T>
 constexpr int kPartsOf = sizeof(T) == 4 ? 2 : 1;
 
-// LDS is shared by the block's waves: orders this wave's accesses to it around
-// the barrier, and leaves loads from memory in flight.
-__device__ inline void lds_barrier() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 // Place of lane l's 16 bytes in the fragment of step `step` of K's or Q's rows.
 // The permutation spreads over the banks what a wave writes at once (pieces of
 // 8 bytes, Unit below) and what it reads at once as columns.

@@ -20,6 +20,24 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxK = 128;
 
+// Sum over the lanes of a wave that agree in l % kX, in every one of them.
+template <int kX>
+__device__ inline float sum_rows(float x) {
+    if (kX <= 8)
+        x += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x128,
+                                                                0xf, 0xf, true));  // 8 lanes on
+    if (kX <= 16) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, x);
+        const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        const uint32_t a0 = a[0], a1 = a[1];
+        x = __builtin_bit_cast(float, a0) + __builtin_bit_cast(float, a1);
+    }
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t a0 = a[0], a1 = a[1];
+    return __builtin_bit_cast(float, a0) + __builtin_bit_cast(float, a1);
+}
+
 // kVec columns a thread, kX threads along the columns.
 template <class T, int kVec, int kX>
 __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
@@ -29,7 +47,8 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
     constexpr int kEach = kMaxK / kRows;       // rows of a thread
     constexpr int kWaves = kThreads / 64;
     typedef typename Pack<float, kVec>::type Vec;
-    __shared__ float sums[2][kWaves][2 * kCols + 1];
+    static_assert(kX >= 8 && kX <= 32, "lanes of a row");
+    __shared__ __attribute__((aligned(16))) float sums[2][kWaves][2 * kCols + 4];
     __shared__ float keys[2][2][kMaxK];
 
     const int x = threadIdx.x % kX, y = threadIdx.x / kX;
@@ -69,19 +88,31 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
     const float* g = p.g.p ? row_of<const float>(p.g, packed, n, s, h) : nullptr;
     const float* beta = p.beta.p ? row_of<const float>(p.beta, packed, n, s, h) : nullptr;
 
+    // the next token's values, on their way while one is computed
+    const int e = threadIdx.x % kMaxK;
+    const bool is_key = threadIdx.x < kMaxK, has_key = e < p.k_size;
+    const T* key_row = is_key ? k + e : q + e;
+    const int64_t key_step = is_key ? p.k.token : p.q.token;
+    T key{}, value[kVec]{};
+    float gate = 0.0f, strength = 1.0f;
+    const auto load_token = [&](int t) __attribute__((always_inline)) {
+        if (has_key) key = key_row[t * key_step];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (in) value[i] = v[t * p.v.token + col + i];
+        if (g) gate = g[t * p.g.token];
+        if (beta) strength = beta[t * p.beta.token];
+    };
+    if (s.count > 0) load_token(0);
     for (int t = 0; t < s.count; ++t) {
         const int buf = t & 1;
-        {
-            const int e = threadIdx.x % kMaxK;
-            const T* from = threadIdx.x < kMaxK ? k + t * p.k.token : q + t * p.q.token;
-            keys[buf][threadIdx.x / kMaxK][e] = e < p.k_size ? to_f32(from[e]) : 0.0f;
-        }
+        keys[buf][threadIdx.x / kMaxK][e] = has_key ? to_f32(key) : 0.0f;
         float vt[kVec];
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) vt[i] = in ? to_f32(v[t * p.v.token + col + i]) : 0.0f;
-        const float decay = g ? expf(log_decay(g[t * p.g.token])) : 1.0f;
-        const float b = beta ? beta[t * p.beta.token] : 1.0f;
-        __syncthreads();
+        for (int i = 0; i < kVec; ++i) vt[i] = in ? to_f32(value[i]) : 0.0f;
+        const float decay = g ? expf(log_decay(gate)) : 1.0f, b = strength;
+        if (t + 1 < s.count) load_token(t + 1);
+        lds_barrier();
         float kr[kEach], qr[kEach], sk[kVec] = {}, sq[kVec] = {}, kq = 0.0f;
 #pragma unroll
         for (int r = 0; r < kEach; ++r) {
@@ -95,32 +126,34 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
             }
         }
         // over the wave's rows, then over the waves
+        kq = sum_rows<kX>(kq);
 #pragma unroll
-        for (int d = kX; d < 64; d *= 2) {
-            kq += __shfl_xor(kq, d, 64);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                sk[i] += __shfl_xor(sk[i], d, 64);
-                sq[i] += __shfl_xor(sq[i], d, 64);
-            }
+        for (int i = 0; i < kVec; ++i) {
+            sk[i] = sum_rows<kX>(sk[i]);
+            sq[i] = sum_rows<kX>(sq[i]);
         }
+        Vec out_k, out_q;
+        __builtin_memcpy(&out_k, sk, sizeof(Vec));
+        __builtin_memcpy(&out_q, sq, sizeof(Vec));
         if ((threadIdx.x & 63) < kX) {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                sums[buf][wave][kVec * x + i] = sk[i];
-                sums[buf][wave][kCols + kVec * x + i] = sq[i];
-            }
-            if (x == 0) sums[buf][wave][2 * kCols] = kq;
+            float* to = sums[buf][wave];
+            *reinterpret_cast<Vec*>(to + kVec * x) = out_k;
+            *reinterpret_cast<Vec*>(to + kCols + kVec * x) = out_q;
+            if (x == 0) to[2 * kCols] = kq;
         }
-        __syncthreads();
+        lds_barrier();
         float tk[kVec] = {}, tq[kVec] = {}, tkq = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            tkq += sums[buf][w][2 * kCols];
+            const float* from = sums[buf][w];
+            tkq += from[2 * kCols];
+            float a[kVec], c[kVec];
+            __builtin_memcpy(a, from + kVec * x, sizeof(a));
+            __builtin_memcpy(c, from + kCols + kVec * x, sizeof(c));
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                tk[i] += sums[buf][w][kVec * x + i];
-                tq[i] += sums[buf][w][kCols + kVec * x + i];
+                tk[i] += a[i];
+                tq[i] += c[i];
             }
         }
 #pragma unroll

@@ -62,6 +62,14 @@ __device__ inline float log_decay(float g) { return fmaxf(g, kLeastDecay); }
 // Blocks of 256 threads of one launch, which stays below 2^31 threads.
 constexpr int64_t kMostBlocks = 1 << 22;
 
+// LDS is shared by the block's waves: orders this wave's accesses to it around
+// the barrier, and leaves loads from memory in flight.
+__device__ inline void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Calls f(T{}) with the element type of a dtype that has been checked.
 template <class F>
 inline hipError_t by_dtype(int dtype, F&& f) {

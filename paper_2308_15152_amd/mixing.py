@@ -46,6 +46,15 @@ def _launch(name, dev, stream, args):
         raise _pkg.SgemmEmuError(rc, name)
 
 
+def _device(*ts):
+    """Index of the one device that every tensor given (None skipped) is on."""
+    dev = ts[0].get_device()
+    for t in ts:
+        if t is not None and t.get_device() != dev or dev < 0:
+            return _pkg._device_index(*ts)  # says what is wrong
+    return dev
+
+
 def _view(t, name, shape, dtype):
     """(pointer, batch, token and head stride) of a tensor of that shape and
     type whose last dimension is contiguous."""
@@ -54,11 +63,11 @@ def _view(t, name, shape, dtype):
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     st = t.stride()
-    if len(st) == 3:  # per token and head: no inner dimension
+    if len(st) == 4:  # (three: per token and head, no inner dimension)
+        if st[3] != 1 and shape[3] > 1:
+            raise ValueError(f"{name} must be contiguous along its last dimension")
         return (t.data_ptr(), st[0], st[1], st[2])
-    if st[3] != 1 and shape[3] > 1:
-        raise ValueError(f"{name} must be contiguous along its last dimension")
-    return (t.data_ptr(), st[0], st[1], st[2])
+    return (t.data_ptr(), *st)
 
 
 def _sizes(q, k, v):
@@ -139,7 +148,7 @@ def rotary_emu(q, k, cos, sin, *, positions=None, offset: int = 0, interleaved: 
         if k.dim() != 4:
             raise ValueError("k must be (batch, tokens, heads, size)")
         hk = k.shape[2]
-        shape = torch.Size((b, t, hk, size))
+        shape = (b, t, hk, size)
         if ok is None:
             raise ValueError("out must hold a tensor for k")
         xk, yk = _view(k, "k", shape, dtype), _view(ok, "out", shape, dtype)
@@ -168,7 +177,7 @@ def rotary_emu(q, k, cos, sin, *, positions=None, offset: int = 0, interleaved: 
                         1 if inverse else 0, cos.shape[0], hq, hk, *xq, *xk, *yq, *yk,
                         cos.data_ptr(), sin.data_ptr(), at, at_batch, at_token, int(offset),
                         at_bytes, 0)
-    _launch("rotary_emu", _pkg._device_index(q, k, cos, sin, positions, oq, ok), stream, args)
+    _launch("rotary_emu", _device(q, k, cos, sin, positions, oq, ok), stream, args)
     return oq, ok
 
 
@@ -199,7 +208,7 @@ def _forward_args(q, k, v, g, beta, o, initial, final, scale, cu, n, ws, ws_byte
     torch = _pkg._torch
     b, t, hk, hv, ks, vs = _sizes(q, k, v)
     dtype, f32 = q.dtype, torch.float32
-    values, gates = torch.Size((b, t, hv, vs)), torch.Size((b, t, hv))
+    values, gates = (b, t, hv, vs), (b, t, hv)
     states = (n, hv, ks, vs)
     return _FORWARD.pack(
         _dtypes[dtype], n, t, hk, hv, ks, vs, ks ** -0.5 if scale is None else scale, cu,
@@ -248,8 +257,7 @@ def delta_emu_forward(q, k, v, g=None, beta=None, initial_state=None, *, scale=N
         out = torch.empty((b, t, hv, vs), dtype=q.dtype, device=q.device)
     if final_state is None:
         final_state = torch.empty((n, hv, ks, vs), dtype=torch.float32, device=q.device)
-    dev = _pkg._device_index(q, k, v, g, beta, initial_state, cu_seqlens, out, final_state,
-                             workspace)
+    dev = _device(q, k, v, g, beta, initial_state, cu_seqlens, out, final_state, workspace)
     args = _forward_args(q, k, v, g, beta, out, initial_state, final_state, scale, cu, n, 0, 0)
     need = _calls["delta_emu_forward_workspace"](args)
     if need < 0:
@@ -265,7 +273,7 @@ def _backward_args(q, k, v, g, beta, do, grads, initial, dfinal, dinitial, scale
     torch = _pkg._torch
     b, t, hk, hv, ks, vs = _sizes(q, k, v)
     dtype, f32 = q.dtype, torch.float32
-    values, gates = torch.Size((b, t, hv, vs)), torch.Size((b, t, hv))
+    values, gates = (b, t, hv, vs), (b, t, hv)
     states = (n, hv, ks, vs)
     if grads is None:
         out = _NO_VIEW * 5
@@ -317,8 +325,7 @@ def delta_emu_backward(q, k, v, g, beta, do, initial_state=None, dfinal=None, *,
                for x in (q, k, v, g, beta)]
         out.append(torch.empty((n, hv, ks, vs), dtype=torch.float32, device=q.device))
     *grads, dinitial = out
-    dev = _pkg._device_index(q, k, v, g, beta, do, initial_state, dfinal, cu_seqlens, workspace,
-                             *out)
+    dev = _device(q, k, v, g, beta, do, initial_state, dfinal, cu_seqlens, workspace, *out)
     args = _backward_args(q, k, v, g, beta, do, grads, initial_state, dfinal, dinitial, scale, cu,
                           n)
     need = _calls["delta_emu_backward_workspace"](args)
@@ -342,7 +349,7 @@ def delta_emu_step(q, k, v, g, beta, state, *, slots=None, scale=None, out=None,
     torch = _pkg._torch
     b, t, hk, hv, ks, vs = _sizes(q, k, v)
     dtype, f32 = q.dtype, torch.float32
-    values, gates = torch.Size((b, t, hv, vs)), torch.Size((b, t, hv))
+    values, gates = (b, t, hv, vs), (b, t, hv)
     if out is None:
         out = torch.empty(values, dtype=dtype, device=q.device)
     if state.dtype is not f32 or state.dim() != 4 or state.shape[1:] != (hv, ks, vs):
@@ -364,6 +371,6 @@ def delta_emu_step(q, k, v, g, beta, state, *, slots=None, scale=None, out=None,
         *(_NO_VIEW if beta is None else _view(beta, "beta", gates, f32)),
         *_view(out, "out", values, dtype),
         state.data_ptr(), stride[0] if n_slots > 1 else hv * ks * vs, at, n_slots, 0)
-    _launch("delta_emu_step", _pkg._device_index(q, k, v, g, beta, state, slots, out), stream,
+    _launch("delta_emu_step", _device(q, k, v, g, beta, state, slots, out), stream,
             args)
     return out
