@@ -53,7 +53,8 @@ typedef struct {
  *   x[1].p == NULL or heads[1] == 0: one tensor only.
  *   y[i] may be x[i] itself (same pointer and strides: in place).
  * Errors: _DIM (also a negative offset), _UNSUPPORTED (rot odd, < 0 or > size;
- * dtype or position_bytes unknown; more than 2^31 - 1 tokens in all),
+ * dtype or position_bytes unknown; more than 2^31 - 1 tokens in all, or elements
+ * of a token),
  * _NULL, _STRIDE, _ALIAS, _HIP.
  */
 typedef struct {
@@ -108,7 +109,7 @@ int rotary_emu_table(int rows, int rot, double base, double factor, double origi
  * workspace: device memory, 256-byte aligned, at least what the _workspace query
  *   for the same arguments returns; its contents need not be kept.
  * Sizes: k_size <= 128, v_size <= 65536, token strides <= 2^22 (of q, k, v, o
- * and their gradients), k_heads divides v_heads.  Empty sequences leave
+ * and their gradients; the recurrent form takes any), k_heads divides v_heads.  Empty sequences leave
  * final = initial.
  * Errors: _DIM, _UNSUPPORTED (dtype, sizes and strides above, head counts, more than
  * 2^22 chunks x value heads),

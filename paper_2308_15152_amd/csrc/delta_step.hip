@@ -59,19 +59,18 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
     task /= slices;
     const int h = (int)(task % p.v_heads), n = (int)(task / p.v_heads);
     const int kh = h / (p.v_heads / p.k_heads);
-    const bool packed = p.cu_seqlens != nullptr;
-    const Span s = span_of(p.cu_seqlens, n, p.tokens);
+    const Span s = span_of(nullptr, n, p.tokens);
     const int col = slice * kCols + kVec * x;
     const bool in = col < p.v_size;  // kVec divides v_size or is 1
 
-    const T* q = row_of<const T>(p.q, packed, n, s, kh);
-    const T* k = row_of<const T>(p.k, packed, n, s, kh);
-    const T* v = row_of<const T>(p.v, packed, n, s, h);
-    T* o = row_of<T>(p.o, packed, n, s, h);
+    const T* q = row_of<const T>(p.q, false, n, s, kh);
+    const T* k = row_of<const T>(p.k, false, n, s, kh);
+    const T* v = row_of<const T>(p.v, false, n, s, h);
+    T* o = row_of<T>(p.o, false, n, s, h);
     const int slot = p.slots ? p.slots[n] : n;
     if (slot < 0 || slot >= p.n_slots) {  // the whole block
         if (in && y == 0)
-            for (int t = 0; t < s.count; ++t)
+            for (int t = 0; t < p.tokens; ++t)
                 for (int i = 0; i < kVec; ++i) o[t * p.o.token + col + i] = from_f32<T>(0.0f);
         return;
     }
@@ -85,8 +84,8 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
             w = *reinterpret_cast<const Vec*>(p.from + at + (int64_t)row * p.v_size);
         __builtin_memcpy(S[r], &w, sizeof(Vec));
     }
-    const float* g = p.g.p ? row_of<const float>(p.g, packed, n, s, h) : nullptr;
-    const float* beta = p.beta.p ? row_of<const float>(p.beta, packed, n, s, h) : nullptr;
+    const float* g = p.g.p ? row_of<const float>(p.g, false, n, s, h) : nullptr;
+    const float* beta = p.beta.p ? row_of<const float>(p.beta, false, n, s, h) : nullptr;
 
     // the next token's values, on their way while one is computed
     const int e = threadIdx.x % kMaxK;
@@ -103,15 +102,15 @@ __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStep p,
         if (g) gate = g[t * p.g.token];
         if (beta) strength = beta[t * p.beta.token];
     };
-    if (s.count > 0) load_token(0);
-    for (int t = 0; t < s.count; ++t) {
+    if (p.tokens > 0) load_token(0);
+    for (int t = 0; t < p.tokens; ++t) {
         const int buf = t & 1;
         keys[buf][threadIdx.x / kMaxK][e] = has_key ? to_f32(key) : 0.0f;
         float vt[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) vt[i] = in ? to_f32(value[i]) : 0.0f;
         const float decay = g ? expf(log_decay(gate)) : 1.0f, b = strength;
-        if (t + 1 < s.count) load_token(t + 1);
+        if (t + 1 < p.tokens) load_token(t + 1);
         lds_barrier();
         float kr[kEach], qr[kEach], sk[kVec] = {}, sq[kVec] = {}, kq = 0.0f;
 #pragma unroll

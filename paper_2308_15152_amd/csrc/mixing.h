@@ -20,7 +20,6 @@ hipError_t launch_rotary_table(int rows, int rot, double base, double factor, do
 struct DeltaStep {
     int dtype, batch, tokens, k_heads, v_heads, k_size, v_size;
     float scale;
-    const int* cu_seqlens;  // packed sequences, or null
     sgemm_emu_view_t q, k, v, g, beta, o;
     const float* from;  // states before, or null (zero)
     float* to;          // states after, or null

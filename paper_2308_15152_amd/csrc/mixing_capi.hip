@@ -85,16 +85,16 @@ int check_sizes(const A& a) {
         a.v_size < 0)
         return SGEMM_EMU_ERR_DIM;
     if (a.k_size < 1 || a.k_size > kDeltaMaxK || a.k_heads < 1 || a.v_heads < 1 ||
-        a.v_heads % a.k_heads != 0)
+        a.v_heads % a.k_heads != 0 || a.v_size > kDeltaMaxV)
         return SGEMM_EMU_ERR_UNSUPPORTED;
     return SGEMM_EMU_OK;
 }
 
 // The chunk kernels address a chunk's 64 rows of a head with 32-bit offsets.
-bool within_reach(std::initializer_list<sgemm_emu_view_t> views, int v_size) {
+bool within_reach(std::initializer_list<sgemm_emu_view_t> views) {
     for (const sgemm_emu_view_t& v : views)
         if (v.token > kDeltaMostStride) return false;
-    return v_size <= kDeltaMaxV;
+    return true;
 }
 
 // Every input present, every output apart, no output over an input.
@@ -160,7 +160,7 @@ int rotary_emu(const rotary_emu_t* args, hipStream_t stream) {
     if (a.positions != nullptr && a.position_bytes != 4 && a.position_bytes != 8)
         return SGEMM_EMU_ERR_UNSUPPORTED;
     if ((int64_t)a.batch * a.tokens > INT32_MAX ||
-        (int64_t)a.heads[0] + a.heads[1] > INT32_MAX / 2)
+        ((int64_t)a.heads[0] + a.heads[1]) * a.size > INT32_MAX)
         return SGEMM_EMU_ERR_UNSUPPORTED;
     if (a.batch == 0 || a.tokens == 0 || a.size == 0) return SGEMM_EMU_OK;
     const int64_t elem = dtype_bytes(a.dtype);
@@ -257,7 +257,7 @@ int delta_emu_forward(const delta_emu_forward_t* args, hipStream_t stream) {
     if (args == nullptr) return SGEMM_EMU_ERR_NULL;
     const delta_emu_forward_t& a = *args;
     if (int rc = check_shape(a)) return rc;
-    if (!within_reach({a.q, a.k, a.v, a.o}, a.v_size)) return SGEMM_EMU_ERR_UNSUPPORTED;
+    if (!within_reach({a.q, a.k, a.v, a.o})) return SGEMM_EMU_ERR_UNSUPPORTED;
     if (a.batch == 0 || a.v_size == 0) return SGEMM_EMU_OK;
     const bool packed = a.cu_seqlens != nullptr;
     const int64_t batch = packed ? 1 : a.batch, e = dtype_bytes(a.dtype);
@@ -290,7 +290,7 @@ int delta_emu_backward(const delta_emu_backward_t* args, hipStream_t stream) {
     if (args == nullptr) return SGEMM_EMU_ERR_NULL;
     const delta_emu_backward_t& a = *args;
     if (int rc = check_shape(a)) return rc;
-    if (!within_reach({a.q, a.k, a.v, a.d_o, a.dq, a.dk, a.dv}, a.v_size))
+    if (!within_reach({a.q, a.k, a.v, a.d_o, a.dq, a.dk, a.dv}))
         return SGEMM_EMU_ERR_UNSUPPORTED;
     if (a.batch == 0) return SGEMM_EMU_OK;
     const bool packed = a.cu_seqlens != nullptr;
