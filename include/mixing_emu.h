@@ -107,10 +107,13 @@ int rotary_emu_table(int rows, int rot, double base, double factor, double origi
  *     [0, tokens]; others are clamped to that).  Rows of no sequence are not written.
  * initial: states before the first tokens, or NULL (zero).
  * workspace: device memory, 256-byte aligned, at least what the _workspace query
- *   for the same arguments returns; its contents need not be kept.
+ *   for the same arguments returns (0 for up to 16 tokens that are not packed, which
+ *   go token by token); its contents need not be kept.
  * Sizes: k_size <= 128, v_size <= 65536, token strides <= 2^22 (of q, k, v, o
- * and their gradients; the recurrent form takes any), k_heads divides v_heads.  Empty sequences leave
- * final = initial.
+ * and their gradients; the recurrent form takes any), k_heads divides v_heads.
+ * Empty sequences leave final = initial.  A value that is not finite reaches what the
+ * recurrence takes it to: no earlier token, other sequence, head or, if it is in
+ * v or a state, column.
  * Errors: _DIM, _UNSUPPORTED (dtype, sizes and strides above, head counts, more than
  * 2^22 chunks x value heads),
  * _NULL, _STRIDE, _ALIAS, _HIP.

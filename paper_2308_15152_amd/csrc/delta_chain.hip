@@ -59,7 +59,7 @@ struct Layout {
     static constexpr int kAtS = kAtV + kWalkers * V::kEach;
     static constexpr int kEachS = kOut * kSteps * 1024 + 256;  // and its scale
     static constexpr int kAtU = kAtS + (kMode == kOutputs ? kWalkers * kEachS : 0);
-    static constexpr int kEachU = kC * 16 * 4;
+    static constexpr int kEachU = kC * 16 * 4 + 256;  // and the rows that count (cut_column)
     static constexpr int kBufferU = kMode == kOutputs ? kWalkers * kEachU : 0;  // one or two
     static constexpr int kAtPosts = kAtU + (kPosts ? 2 : 1) * kBufferU;
     static constexpr int kBytes = kAtPosts + 16 * kWalkers;
@@ -187,8 +187,12 @@ void delta_chain_kernel(DeltaChunks p) {
             }
             // U
             f32x4 u[4] = {};
+            int cut = kC;
             {
-                const Scale xs = scale_of(max_groups(largest(x)));
+                float top = column_largest(x);
+                const bool cuts = __any(!finite(top));
+                if (cuts) cut = cut_column(x, top);
+                const Scale xs = scale_of(top);
                 const Frag<2> b[2] = {split<2>(x[0], x[1], xs.up), split<2>(x[2], x[3], xs.up)};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -197,10 +201,17 @@ void delta_chain_kernel(DeltaChunks p) {
                         u[i] = multiply(matrix_fragment<2>(at + L::kAtT, lower_at(i, j), lane), b[j],
                                         u[i]);
                     u[i] *= factor(DeltaRecord::kT, i) * xs.down;
+                    if (kMode == kStates && cuts)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (16 * i + 4 * g + r >= cut) u[i][r] = __builtin_nanf("");
                     if (kMode == kOutputs)
                         *reinterpret_cast<f32x4*>(u_at + (kPosts ? (c & 1) * L::kBufferU : 0) +
                                                   i * 1024) = u[i];
                 }
+                if (kMode == kOutputs)
+                    *reinterpret_cast<int*>(u_at + (kPosts ? (c & 1) * L::kBufferU : 0) -
+                                            lane * 12 + kC * 16 * 4) = cut;
             }
             if (kMode == kStates) {
                 const int64_t task = (int64_t)(first_chunk + c) * p.v_heads + h;
@@ -220,6 +231,7 @@ void delta_chain_kernel(DeltaChunks p) {
             const Scale us = scale_of(max_groups(largest(u)));
             const Frag<2> b[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
             const float decay = f[64 * DeltaRecord::kDecay];
+            const float down = cut == kC ? us.down : __builtin_nanf("");
 #pragma unroll
             for (int i = 0; i < L::kTiles; ++i) {
                 f32x4 a{};
@@ -228,7 +240,7 @@ void delta_chain_kernel(DeltaChunks p) {
                     a = multiply<true>(column_fragment<T, kK>(at + L::kAtK, i, j, lane), b[j], a);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    S[i][r] = __builtin_fmaf(a[r], us.down, decay * S[i][r]);
+                    S[i][r] = __builtin_fmaf(a[r], down, decay * S[i][r]);
             }
         }
         if (kMode == kOutputs && chunks > 0) lds_barrier();  // the last U
@@ -303,6 +315,7 @@ void delta_chain_kernel(DeltaChunks p) {
         f32x4 u[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(u_at + i * 1024);
+        const int cut = *reinterpret_cast<const int*>(u_at - lane * 12 + kC * 16 * 4);
         const Scale us = scale_of(max_groups(largest(u)));
         const Frag<kOut> b[2] = {split<kOut>(u[0], u[1], us.up), split<kOut>(u[2], u[3], us.up)};
         const int count = min(kC, span.count - c * kC);
@@ -321,7 +334,7 @@ void delta_chain_kernel(DeltaChunks p) {
             for (int r = 0; r < 4; ++r) {
                 const int t = 16 * tile + 4 * g + r;
                 const uint32_t off = o_at + (16 * i + r) * o_step;
-                store_word(from_f32<T>(a[r] + y[i][r]), to,
+                store_word(from_f32<T>(t < cut ? a[r] + y[i][r] : __builtin_nanf("")), to,
                            count == kC || t < count ? off : kPastEnd);
             }
         }

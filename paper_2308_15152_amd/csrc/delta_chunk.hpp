@@ -106,6 +106,51 @@ __device__ inline float largest(const f32x4 (&x)[N]) {
     return m;
 }
 
+// A value that is not finite may reach later tokens of its chunk but no earlier
+// ones, and a product with a triangular matrix would take it to all (0 NaN).
+// So such a product's operand is looked at first: the rows of a column
+// from the first such value on are left out and give NaN afterwards.  The
+// check is the maximum that the scale needs anyway, taken so that NaN stays.
+__device__ inline float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+__device__ inline float column_largest(const f32x4 (&x)[4]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = max_nan(m, fabsf(x[i][r]));
+    uint32_t u = __builtin_bit_cast(uint32_t, m);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t a0 = a[0], a1 = a[1];
+    u = __builtin_bit_cast(uint32_t, max_nan(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t b0 = b[0], b1 = b[1];
+    return max_nan(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+
+__device__ inline bool finite(float x) { return fabsf(x) < __builtin_inff(); }
+
+// The first row of this lane's column (kC if none) with a value that is not
+// finite; it and the rows after it become zero, m the largest of those left.
+__device__ inline int cut_column(f32x4 (&x)[4], float& m) {
+    const int g = (threadIdx.x & 63) >> 4;
+    int first = kC;
+#pragma unroll
+    for (int i = 3; i >= 0; --i)
+#pragma unroll
+        for (int r = 3; r >= 0; --r)
+            if (!finite(x[i][r])) first = 16 * i + 4 * g + r;
+    first = min(first, __shfl_xor(first, 16, 64));
+    first = min(first, __shfl_xor(first, 32, 64));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (16 * i + 4 * g + r >= first) x[i][r] = 0.0f;
+    m = column_largest(x);
+    return first;
+}
+
 // Number of a triangular matrix's fragment: lower ones fill steps 0 .. i / 2 of
 // tile i, upper ones steps i / 2 .. 1.
 __device__ constexpr int lower_at(int tile, int step) { return tile < 2 ? tile : 2 * tile - 2 + step; }

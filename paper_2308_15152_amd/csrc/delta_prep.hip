@@ -191,7 +191,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
                 a = a * d[r] * down;
                 b = b * dq[r] * down;
             }
-            A[t * kPitch + s] = s < t ? bt[r] * e * a : 0.0f;
+            a *= bt[r] * e;
+            // a value that is not finite must not reach rows before it
+            if (s < t && !finite(a)) {
+                beta[t] = __builtin_nanf("");
+                a = 0.0f;
+            }
+            A[t * kPitch + s] = s < t ? a : 0.0f;
             P[t * kPitch + s] = s <= t ? p.scale * e * b : 0.0f;
         }
     }

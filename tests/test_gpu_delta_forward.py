@@ -242,3 +242,25 @@ def test_graph_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager) and torch.equal(state, last)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("which", ["q", "k", "v", "g", "beta"])
+@pytest.mark.parametrize("t,at", [(10, 4), (150, 0), (150, 21), (150, 63), (150, 64), (150, 149)])
+def test_what_is_not_finite_reaches_no_earlier_token(dtype, which, t, at):
+    """Nor another column, sequence or head than the recurrence takes it to."""
+    x = list(inputs(2, t, 1, 2, 64, 48, dtype, seed=at, decay=0.2))
+    i = ("q", "k", "v", "g", "beta").index(which)
+    first = torch.randn(2, 2, 64, 48)
+    for value in (torch.nan, torch.inf):
+        if which == "g" and value == torch.inf:
+            continue
+        y = list(x)
+        y[i] = x[i].clone()
+        y[i][(1, at, -1, 7)[:y[i].dim()]] = value
+        want, last = delta(*y, first)
+        o, state = run(y, first)
+        for a, b, kind in ((o, want, dtype), (state, last, torch.float32)):
+            a, keep = a.cpu(), b.isfinite()
+            assert torch.equal(a.isfinite(), keep), value
+            near(a[keep], b[keep], t, kind)
