@@ -49,11 +49,11 @@ struct DeltaRecord {
     enum Factor {   // rows of 64 floats
         kKeyScale,  // 2^a: a key row times it has its largest entry in [2^14, 2^15)
         kQueryScale,
-        kRise,       // e^G / key scale
+        kRise,       // e^G / key scale, NaN where beta is not finite
         kBeta,       // beta
         kTail,       // e^{G_64 - G} / key scale
         kQueryRise,  // scale e^G / query scale
-        kT,          // inverse row scales of T, P, T^T, P^T
+        kT,          // inverse row scales of T diag(beta), P, T^T, P^T
         kP,
         kTt,
         kPt,

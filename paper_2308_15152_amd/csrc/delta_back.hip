@@ -276,7 +276,8 @@ void delta_back_kernel(DeltaChunks p) {
     const auto make = [&](int s) __attribute__((always_inline)) {
         const char* at = buffer_q(s);
         const float* f = reinterpret_cast<const float*>(at + L::kAtFq);
-        const char* v_at = at + L::kAtDo + block * L::V::kEach + lane * 4 * (int)sizeof(T);
+        const char* v_at = at + L::kAtDo + block * L::V::kEach +
+                           value_slot(lane, block) * 4 * (int)sizeof(T);
         f32x4 o[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

@@ -55,11 +55,11 @@ struct Layout {
     static constexpr int kBufferQ = kAtP + kBytesP - kAtQ;
     // one of these
     static constexpr int kAtV = kAtQ + (kPosts ? 2 : 1) * kBufferQ;
-    using V = Values<T, kWalkers, 256>;
+    using V = Values<T, kWalkers, 256, float>;
     static constexpr int kAtS = kAtV + kWalkers * V::kEach;
     static constexpr int kEachS = kOut * kSteps * 1024 + 256;  // and its scale
     static constexpr int kAtU = kAtS + (kMode == kOutputs ? kWalkers * kEachS : 0);
-    static constexpr int kEachU = kC * 16 * 4 + 256;  // and the rows that count (cut_column)
+    static constexpr int kEachU = kC * 16 * 4 + 128;  // and each column's rows that count, and scale
     static constexpr int kBufferU = kMode == kOutputs ? kWalkers * kEachU : 0;  // one or two
     static constexpr int kAtPosts = kAtU + (kPosts ? 2 : 1) * kBufferU;
     static constexpr int kBytes = kAtPosts + 16 * kWalkers;
@@ -121,7 +121,7 @@ void delta_chain_kernel(DeltaChunks p) {
                 S[i][r] = from && in && row < p.k_size ? from[(int64_t)row * p.v_size + col] : 0.0f;
                 if (of_m && row == col) S[i][r] = 1.0f;
             }
-        const char* v_at = lds + L::kAtV + wave * L::V::kEach + lane * 4 * (int)sizeof(T);
+        const char* v_at = lds + L::kAtV + wave * L::V::kEach + value_slot(lane, wave) * 16;
         char* s_at = lds + L::kAtS + wave * L::kEachS;
         char* u_at = lds + L::kAtU + wave * L::kEachU + lane * 16;
 
@@ -132,10 +132,9 @@ void delta_chain_kernel(DeltaChunks p) {
                 return reinterpret_cast<const f32x4*>(f + 64 * which)[4 * tile + g];
             };
             lds_barrier();  // A
-            T vt[4][4];
+            f32x4 vt[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                __builtin_memcpy(vt[i], v_at + i * 64 * 4 * sizeof(T), 4 * sizeof(T));
+            for (int i = 0; i < 4; ++i) vt[i] = *reinterpret_cast<const f32x4*>(v_at + i * 1024);
             if (kMode == kStates) {
                 const int64_t task = (int64_t)(first_chunk + c) * p.v_heads + h;
                 const __amdgpu_buffer_rsrc_t to =
@@ -170,7 +169,7 @@ void delta_chain_kernel(DeltaChunks p) {
             } else {
                 lds_barrier();  // B
             }
-            // beta (V - e^G K S)
+            // V - e^G K S
             f32x4 x[4] = {};
 #pragma unroll
             for (int j = 0; j < L::kSteps; ++j)
@@ -180,14 +179,13 @@ void delta_chain_kernel(DeltaChunks p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x4 rise = factor(DeltaRecord::kRise, i) * ss.down;
-                const f32x4 beta = factor(DeltaRecord::kBeta, i);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    x[i][r] = beta[r] * __builtin_fmaf(-rise[r], x[i][r], to_f32(vt[i][r]));
+                for (int r = 0; r < 4; ++r) x[i][r] = __builtin_fmaf(-rise[r], x[i][r], vt[i][r]);
             }
             // U
             f32x4 u[4] = {};
             int cut = kC;
+            float u_down;  // U: u times it
             {
                 float top = column_largest(x);
                 const bool cuts = __any(!finite(top));
@@ -200,7 +198,8 @@ void delta_chain_kernel(DeltaChunks p) {
                     for (int j = 0; j <= i / 2; ++j)
                         u[i] = multiply(matrix_fragment<2>(at + L::kAtT, lower_at(i, j), lane), b[j],
                                         u[i]);
-                    u[i] *= factor(DeltaRecord::kT, i) * xs.down;
+                    u[i] *= kMode == kStates ? factor(DeltaRecord::kT, i) * xs.down
+                                             : factor(DeltaRecord::kT, i);
                     if (kMode == kStates && cuts)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
@@ -209,9 +208,12 @@ void delta_chain_kernel(DeltaChunks p) {
                         *reinterpret_cast<f32x4*>(u_at + (kPosts ? (c & 1) * L::kBufferU : 0) +
                                                   i * 1024) = u[i];
                 }
-                if (kMode == kOutputs)
-                    *reinterpret_cast<int*>(u_at + (kPosts ? (c & 1) * L::kBufferU : 0) -
-                                            lane * 12 + kC * 16 * 4) = cut;
+                u_down = kMode == kStates ? 1.0f : xs.down;
+                if (kMode == kOutputs) {
+                    char* to = u_at + (kPosts ? (c & 1) * L::kBufferU : 0) - lane * 16 + kC * 16 * 4;
+                    reinterpret_cast<int*>(to)[lane & 15] = cut;
+                    reinterpret_cast<float*>(to)[16 + (lane & 15)] = u_down;
+                }
             }
             if (kMode == kStates) {
                 const int64_t task = (int64_t)(first_chunk + c) * p.v_heads + h;
@@ -231,7 +233,8 @@ void delta_chain_kernel(DeltaChunks p) {
             const Scale us = scale_of(max_groups(largest(u)));
             const Frag<2> b[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
             const float decay = f[64 * DeltaRecord::kDecay];
-            const float down = cut == kC ? us.down : __builtin_nanf("");
+            float down = cut == kC ? us.down * u_down : __builtin_nanf("");
+            asm("" : "+v"(down));  // one select, not one for every product with it
 #pragma unroll
             for (int i = 0; i < L::kTiles; ++i) {
                 f32x4 a{};
@@ -289,8 +292,8 @@ void delta_chain_kernel(DeltaChunks p) {
         ku.store(to + L::kAtK, id);
         tcopy.store(to + L::kAtT, id);
         fcopy.store(to + L::kAtF, id);
-        vu.store(lds + L::kAtV, id);
     };
+    const auto store_v = [&]() __attribute__((always_inline)) { vu.store(lds + L::kAtV, id); };
     const auto load_q = [&](int c) __attribute__((always_inline)) {
         const char* record = records + c * record_step;
         qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, min(kC, span.count - c * kC), p.k_size,
@@ -315,7 +318,9 @@ void delta_chain_kernel(DeltaChunks p) {
         f32x4 u[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(u_at + i * 1024);
-        const int cut = *reinterpret_cast<const int*>(u_at - lane * 12 + kC * 16 * 4);
+        const char* column = u_at - lane * 16 + kC * 16 * 4 + (lane & 15) * 4;
+        const int cut = *reinterpret_cast<const int*>(column);
+        const float u_down = *reinterpret_cast<const float*>(column + 64);
         const Scale us = scale_of(max_groups(largest(u)));
         const Frag<kOut> b[2] = {split<kOut>(u[0], u[1], us.up), split<kOut>(u[2], u[3], us.up)};
         const int count = min(kC, span.count - c * kC);
@@ -329,7 +334,7 @@ void delta_chain_kernel(DeltaChunks p) {
                 if (j <= tile / 2)
                     a = multiply(matrix_fragment<kOut>(buffer_q(c) + L::kAtP, lower_at(tile, j), lane),
                                  b[j], a);
-            a *= pf[i] * us.down;
+            a *= pf[i] * (us.down * u_down);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int t = 16 * tile + 4 * g + r;
@@ -344,6 +349,7 @@ void delta_chain_kernel(DeltaChunks p) {
         if (brings_k) {
             load_k(0);
             store_k(0);
+            store_v();
             if (chunks > 1) load_k(1);
         }
         if (brings_q) {
@@ -357,6 +363,13 @@ void delta_chain_kernel(DeltaChunks p) {
     }
     for (int c = 0; c < chunks; ++c) {
         lds_barrier();  // A
+        // what the last chunk was the last to read; now, while the walking waves need
+        // little of the LDS (their K S does)
+        if (brings_k && c + 1 < chunks) store_k(c + 1);
+        if (kPosts && brings_q) {
+            pcopy.store(buffer_q(c) + L::kAtP, id);
+            if (c + 1 < chunks) qu.store(buffer_q(c + 1) + L::kAtQ, id);
+        }
         if (outputs && c > 0) finish(c - 1);
         if (kPosts) {
             // every walking wave is in this chunk and posts on its way
@@ -378,7 +391,7 @@ void delta_chain_kernel(DeltaChunks p) {
             }
         }
         if (brings_k && c + 1 < chunks) {
-            store_k(c + 1);
+            store_v();
             if (c + 2 < chunks) load_k(c + 2);
         }
         if (outputs) {
@@ -407,12 +420,8 @@ void delta_chain_kernel(DeltaChunks p) {
             }
         }
         if (kPosts && brings_q) {
-            // this chunk's P and the next one's Q: the other buffer's P is in use
-            // until the next barrier
-            pcopy.store(buffer_q(c) + L::kAtP, id);
             if (c + 1 < chunks) {
                 load_p(c + 1);
-                qu.store(buffer_q(c + 1) + L::kAtQ, id);
                 if (c + 2 < chunks) load_q(c + 2);
             }
         }

@@ -81,9 +81,14 @@ template <int N>
 __device__ inline Frag<N> split(const float (&x)[8], float up) {
     Frag<N> f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        f.part[0][i] = (_Float16)(x[i] * up);
-        if (N == 2)
+    for (int i = 0; i < 8; ++i) f.part[0][i] = (_Float16)(x[i] * up);
+    if (N == 2) {
+        // hi as it is packed (the compiler would make every one a second time)
+        u32x4 hi = __builtin_bit_cast(u32x4, f.part[0]);
+        asm("" : "+v"(hi));
+        f.part[0] = __builtin_bit_cast(half8_t, hi);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
             f.part[N - 1][i] = (_Float16)__builtin_fmaf(x[i], up, -(float)f.part[0][i]);
     }
     return f;
@@ -360,9 +365,13 @@ constexpr int kPartsOf = sizeof(T) == 4 ? 2 : 1;
 
 // Place of lane l's 16 bytes in the fragment of step `step` of K's or Q's rows.
 // The permutation spreads over the banks what a wave writes at once (pieces of
-// 8 bytes, Unit below) and what it reads at once as columns.
+// 8 bytes, Unit below) and keeps its reads of 16 bytes a lane apart: the LDS takes
+// those 16 lanes at a time, 0-3 with 12-15 and 20-27 and so on, so the lanes of
+// group 1 may move by 0 or 12, and of group 3 from group 2's place by 0 or 12.
+// (Counted: no conflicts in either; reads as columns use half of the banks, since a
+// tile is one of the two pieces of every slot.)
 __device__ inline int slot(int lane, int step) {
-    return (lane ^ (step & 3) ^ ((lane >> 4) << 2)) * 16;
+    return (lane ^ (step & 3) ^ ((lane >> 4 & 1) * 12) ^ ((lane >> 5) * 4)) * 16;
 }
 
 // Rows of K or Q as fragments in LDS.  A thread takes 4 tokens x 8 elements, in
@@ -534,13 +543,17 @@ struct Rows {
     }
 };
 
+// Place of lane l's four tokens among the 64 of a tile of a block of 16
+// columns: spread over the banks for those who write them, four columns each.
+__device__ inline int value_slot(int lane, int block) { return lane ^ (((lane >> 4) ^ block) & 3); }
+
 // Columns of V or dO on their way to LDS, where they lie as the waves that own
-// 16 columns hold them: 4 tokens of a column together.  A thread takes 4
+// 16 columns hold them: 4 tokens of a column together, as To.  A thread takes 4
 // tokens x 4 columns of 16 kBlocks ones.
-template <class T, int kBlocks, int kThreads>
+template <class T, int kBlocks, int kThreads, class To = T>
 struct Values {
     static constexpr int kUnits = 16 * 4 * kBlocks;
-    static constexpr int kEach = kC * 16 * sizeof(T);  // bytes of a block of 16 columns
+    static constexpr int kEach = kC * 16 * sizeof(To);  // bytes of a block of 16 columns
     static constexpr int kMine = (kUnits + kThreads - 1) / kThreads;
     T x[kMine][4][4];
     // rows: of the chunk's first token and first column; size: columns there are
@@ -579,11 +592,19 @@ struct Values {
             const int unit = thread + m * kThreads;
             if (kUnits % kThreads != 0 && unit >= kUnits) continue;
             const int four = unit / (4 * kBlocks), c = unit % (4 * kBlocks) * 4;
-            char* at = to + c / 16 * kEach + (four / 4 * 64 + four % 4 * 16 + c % 16) * 4 * sizeof(T);
+            char* at = to + c / 16 * kEach + four / 4 * 64 * 4 * sizeof(To);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const T w[4] = {x[m][0][e], x[m][1][e], x[m][2][e], x[m][3][e]};
-                __builtin_memcpy(at + e * 4 * sizeof(T), w, 4 * sizeof(T));
+                To w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (__is_same(T, To))
+                        w[i] = x[m][i][e];
+                    else
+                        w[i] = to_f32(x[m][i][e]);
+                }
+                __builtin_memcpy(at + value_slot(four % 4 * 16 + c % 16 + e, c / 16) * 4 * sizeof(To),
+                                 w, 4 * sizeof(To));
             }
         }
     }

@@ -9,6 +9,7 @@
 // the four 16 x 16 diagonal blocks (forward substitution, a column to a
 // lane) and joins them with FP32 matrix products, two sizes up:
 //   [A 0; C D]^-1 = [A^-1 0; -D^-1 C A^-1, D^-1].
+// The walk forward takes T diag(beta), the one back T^T.
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
@@ -40,10 +41,11 @@ __device__ inline void block_store(float* X, int lane, f32x4 d) {
 }
 
 // Fragments of tile `tile`'s rows of the matrix M (or its transpose), with the
-// rows' inverse scales.  Blocks on the empty side of the diagonal are zero
-// whatever M holds there.
+// rows' inverse scales; its columns times `columns`, if given.  Blocks on the
+// empty side of the diagonal are zero whatever M holds there.
 template <bool kTransposed, int kParts>
-__device__ inline void write_fragments(const float* M, int tile, int lane, char* to, float* inverse) {
+__device__ inline void write_fragments(const float* M, int tile, int lane, char* to, float* inverse,
+                                       const float* columns = nullptr) {
     const int row = lane & 15, g = lane >> 4;
     float x[2][8], m = 0.0f;
 #pragma unroll
@@ -55,7 +57,8 @@ __device__ inline void write_fragments(const float* M, int tile, int lane, char*
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int a = 16 * tile + row, b = 16 * other + 4 * g + i;
-                const float v = !full ? 0.0f : kTransposed ? M[b * kPitch + a] : M[a * kPitch + b];
+                float v = !full ? 0.0f : kTransposed ? M[b * kPitch + a] : M[a * kPitch + b];
+                if (columns) v *= columns[b];
                 x[step][4 * half + i] = v;
                 m = fmaxf(m, fabsf(v));
             }
@@ -176,6 +179,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
         }
     }
     __syncthreads();  // k's rows are used
+    int bad = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (i > wave) continue;
@@ -193,14 +197,17 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
             }
             a *= bt[r] * e;
             // a value that is not finite must not reach rows before it
-            if (s < t && !finite(a)) {
-                beta[t] = __builtin_nanf("");
-                a = 0.0f;
-            }
-            A[t * kPitch + s] = s < t ? a : 0.0f;
+            const bool spoilt = s < t && !finite(a);
+            bad |= spoilt ? 1 << r : 0;
+            A[t * kPitch + s] = s < t && !spoilt ? a : 0.0f;
             P[t * kPitch + s] = s <= t ? p.scale * e * b : 0.0f;
         }
     }
+    if (bad != 0)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (bad >> r & 1) beta[16 * wave + 4 * g + r] = __builtin_nanf("");
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     // row factors
     if (g == 0) {
         const int t = 16 * wave + row;
@@ -208,8 +215,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
         if (__is_same(T, f16_t)) mine = qs = Scale{1.0f, 1.0f};  // taken as they are
         factors[64 * DeltaRecord::kKeyScale + t] = mine.up;
         factors[64 * DeltaRecord::kQueryScale + t] = qs.up;
-        factors[64 * DeltaRecord::kRise + t] = expf((float)G[t]) * mine.down;
+        // (where beta is not finite, what a walk makes of the row is not either)
+        const bool in = finite(beta[t]);
+        factors[64 * DeltaRecord::kRise + t] =
+            in ? expf((float)G[t]) * mine.down : __builtin_nanf("");
         factors[64 * DeltaRecord::kBeta + t] = beta[t];
+        if (!in) beta[t] = 0.0f;
         factors[64 * DeltaRecord::kTail + t] = expf((float)(last - G[t])) * mine.down;
         factors[64 * DeltaRecord::kQueryRise + t] = p.scale * expf((float)G[t]) * qs.down;
         factors[64 * DeltaRecord::kDecay + t] = expf((float)last);
@@ -262,7 +273,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
     __syncthreads();
 
     write_fragments<false, 2>(A, wave, lane, record + DeltaRecord::kAtT,
-                              factors + 64 * DeltaRecord::kT);
+                              factors + 64 * DeltaRecord::kT, beta);
     if (kBackward) {
         write_fragments<true, 2>(A, wave, lane, record + DeltaRecord::kAtTt,
                                  factors + 64 * DeltaRecord::kTt);
