@@ -47,19 +47,23 @@ inline int64_t delta_chunks(int64_t batch, int64_t tokens, bool packed) {
 // lo ones; rows are scaled by powers of two.
 struct DeltaRecord {
     enum Factor {   // rows of 64 floats
+        kPt,         // inverse row scale of P^T
+        kQueryRise,  // scale e^G / query scale
+        kT,          // inverse row scales of T diag(beta), P
+        kP,
+        kRise,   // e^G / key scale, NaN where beta is not finite
+        kTail,   // e^{G_64 - G} / key scale
+        kDecay,  // [0]: e^{G_64}
+        kBeta,   // beta
+        kTt,     // inverse row scale of T^T
         kKeyScale,  // 2^a: a key row times it has its largest entry in [2^14, 2^15)
         kQueryScale,
-        kRise,       // e^G / key scale, NaN where beta is not finite
-        kBeta,       // beta
-        kTail,       // e^{G_64 - G} / key scale
-        kQueryRise,  // scale e^G / query scale
-        kT,          // inverse row scales of T diag(beta), P, T^T, P^T
-        kP,
-        kTt,
-        kPt,
-        kDecay,  // [0]: e^{G_64}
         kFactors
     };
+    // what the walks take of them: forward, back, and back's products ahead
+    static constexpr int kFirstChain = kQueryRise, kChain = kDecay + 1 - kQueryRise;
+    static constexpr int kFirstBack = kRise, kBack = kTt + 1 - kRise;
+    static constexpr int kFirstAhead = kPt, kAhead = kQueryRise + 1 - kPt;
     static constexpr int kMatrix = 6 * 1024;             // one part of one matrix
     static constexpr int kFactorBytes = kFactors * 256;  // at the record's start
     static constexpr int kAtSums = kFactorBytes;         // G, 64 doubles

@@ -34,12 +34,14 @@ struct Layout {
     static constexpr int kAtK = 0;
     static constexpr int kAtTt = kAtK + kRows;
     static constexpr int kAtF = kAtTt + kMatrix;
-    static constexpr int kBuffer = kAtF + DeltaRecord::kFactorBytes;
+    static constexpr int kFactorBytes = 256 * DeltaRecord::kBack;
+    static constexpr int kBuffer = kAtF + kFactorBytes;
     // one or two of these
     static constexpr int kAtQ = 0;
     static constexpr int kAtPt = kAtQ + kRows;
     static constexpr int kAtFq = kAtPt + kMatrix;
-    static constexpr int kAtDo = kAtFq + DeltaRecord::kFactorBytes;
+    static constexpr int kAheadBytes = 256 * DeltaRecord::kAhead;
+    static constexpr int kAtDo = kAtFq + kAheadBytes;
     using V = Values<T, kWalkers, 256>;
     static constexpr int kBufferQ = kAtDo + kWalkers * V::kEach;
     static constexpr int kAtQs = 2 * kBuffer;
@@ -50,8 +52,8 @@ struct Layout {
     static constexpr int kBytes = kAtPosts + 16 * kWalkers;
 };
 
-// kCarry: only D before every part, from zero after it.
-template <class T, int kK, int kWalkers, bool kCarry>
+// kCarry: only D before every part, from zero after it; kWide: as in delta_chain.hip.
+template <class T, int kK, int kWalkers, bool kCarry, bool kWide>
 __global__ __launch_bounds__(64 * (kWalkers + Layout<T, kK, kWalkers>::kHelpers), 1)
 void delta_back_kernel(DeltaChunks p) {
     using L = Layout<T, kK, kWalkers>;
@@ -112,7 +114,8 @@ void delta_back_kernel(DeltaChunks p) {
         for (int s = 0; s < chunks; ++s) {
             const int c = chunks - 1 - s;
             const char* at = lds + (s & 1) * L::kBuffer;
-            const float* f = reinterpret_cast<const float*>(at + L::kAtF);
+            const float* f =
+                reinterpret_cast<const float*>(at + L::kAtF) - 64 * DeltaRecord::kFirstBack;
             const auto factor = [&](int which, int tile) __attribute__((always_inline)) {
                 return reinterpret_cast<const f32x4*>(f + 64 * which)[4 * tile + g];
             };
@@ -232,15 +235,16 @@ void delta_back_kernel(DeltaChunks p) {
     const T* d_o = row_of<const T>(p.d_o, packed, n, span, h) + skip * p.d_o.token + col0;
     Rows<T, kK, 256> ku, qu;
     Copy<L::kMatrix, 256> tcopy, pcopy;
-    Copy<DeltaRecord::kFactorBytes, 256> fcopy, fqcopy;
+    Copy<L::kFactorBytes, 256> fcopy;
+    Copy<L::kAheadBytes, 256> fqcopy;
     typename L::V vu;
     const auto load_k = [&](int s) __attribute__((always_inline)) {
         const int c = chunks - 1 - s;
         const char* record = records + c * record_step;
         ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, min(kC, span.count - c * kC), p.k_size,
-                p.wide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
+                kWide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
         tcopy.load(record + DeltaRecord::kAtTt, id);
-        fcopy.load(record, id);
+        fcopy.load(record + 256 * DeltaRecord::kFirstBack, id);
     };
     const auto store_k = [&](int s) __attribute__((always_inline)) {
         char* to = lds + (s & 1) * L::kBuffer;
@@ -251,12 +255,12 @@ void delta_back_kernel(DeltaChunks p) {
     const auto load_q = [&](int s) __attribute__((always_inline)) {
         const int c = chunks - 1 - s, count = min(kC, span.count - c * kC);
         const char* record = records + c * record_step;
-        qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, count, p.k_size, p.wide,
+        qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, count, p.k_size, kWide,
                 reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
         pcopy.load(record + DeltaRecord::kAtPt, id);
-        fqcopy.load(record, id);
+        fqcopy.load(record + 256 * DeltaRecord::kFirstAhead, id);
         vu.load(d_o + (int64_t)c * kC * p.d_o.token, p.d_o.token, count, p.v_size - col0,
-                p.wide_values, id);
+                kWide, id);
     };
     const auto buffer_q = [&](int s) __attribute__((always_inline)) { return lds + L::kAtQs + (kPosts ? (s & 1) * L::kBufferQ : 0); };
     const auto store_q = [&](int s) __attribute__((always_inline)) {
@@ -275,7 +279,8 @@ void delta_back_kernel(DeltaChunks p) {
     f32x4 pd[kOwn], qd[kOwnK];
     const auto make = [&](int s) __attribute__((always_inline)) {
         const char* at = buffer_q(s);
-        const float* f = reinterpret_cast<const float*>(at + L::kAtFq);
+        const float* f =
+            reinterpret_cast<const float*>(at + L::kAtFq) - 64 * DeltaRecord::kFirstAhead;
         const char* v_at = at + L::kAtDo + block * L::V::kEach +
                            value_slot(lane, block) * 4 * (int)sizeof(T);
         f32x4 o[4];
@@ -369,20 +374,27 @@ void delta_back_kernel(DeltaChunks p) {
     }
 }
 
-template <class T, int kK, int kWalkers, bool kCarry>
-hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
+template <class T, int kK, int kWalkers, bool kCarry, bool kWide>
+hipError_t launch_rows(const DeltaChunks& a, hipStream_t stream) {
     using L = Layout<T, kK, kWalkers>;
     static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
     const int64_t slices = (a.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
     const int64_t walks = a.part_chunks > 0 ? a.parts : a.batch;
-    const void* kernel = reinterpret_cast<const void*>(delta_back_kernel<T, kK, kWalkers, kCarry>);
+    const void* kernel =
+        reinterpret_cast<const void*>(delta_back_kernel<T, kK, kWalkers, kCarry, kWide>);
     if (hipError_t e =
             hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
-    hipLaunchKernelGGL((delta_back_kernel<T, kK, kWalkers, kCarry>),
+    hipLaunchKernelGGL((delta_back_kernel<T, kK, kWalkers, kCarry, kWide>),
                        dim3((unsigned)walk_blocks(walks * a.v_heads, slices)),
                        dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
+}
+
+template <class T, int kK, int kWalkers, bool kCarry>
+hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
+    return a.wide && a.wide_values ? launch_rows<T, kK, kWalkers, kCarry, true>(a, stream)
+                                   : launch_rows<T, kK, kWalkers, kCarry, false>(a, stream);
 }
 
 }  // namespace
@@ -390,12 +402,12 @@ hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
 hipError_t launch_delta_chain_back(const DeltaChunks& a, DeltaWalk walk, hipStream_t stream) {
     return by_dtype(a.dtype, [&](auto t) {
         using T = decltype(t);
-        constexpr int kWide = sizeof(T) == 4 ? 1 : 2;
+        constexpr int kLarge = sizeof(T) == 4 ? 1 : 2;  // walking waves, keys above 64
         if (walk == kDeltaParts)
             return a.k_size <= 64 ? launch<T, 64, 2, true>(a, stream)
-                                  : launch<T, 128, kWide, true>(a, stream);
+                                  : launch<T, 128, kLarge, true>(a, stream);
         return a.k_size <= 64 ? launch<T, 64, 2, false>(a, stream)
-                              : launch<T, 128, kWide, false>(a, stream);
+                              : launch<T, 128, kLarge, false>(a, stream);
     });
 }
 

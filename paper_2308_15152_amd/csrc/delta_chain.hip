@@ -22,6 +22,8 @@
 // further columns with V = 0, from the columns of the identity, which gives N and M of
 // S -> M S + N; then the states before the parts follow one from another
 // (delta_join.hip); then all parts are walked for their outputs.
+#include <type_traits>
+
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
@@ -31,6 +33,7 @@ namespace {
 constexpr int kOutputs = kDeltaOutputs, kStates = kDeltaStates, kPartSteps = kDeltaParts;
 
 // LDS, in bytes, and the number of helping waves.
+// kWalkers: groups of 16 columns, a pair of walking waves each.
 template <class T, int kK, int kWalkers, int kMode>
 struct Layout {
     static constexpr bool kPosts = sizeof(T) == 2;
@@ -41,6 +44,7 @@ struct Layout {
     // 2^-12 relative, unseen in a bfloat16 result (2^-8) but not in others
     static constexpr int kOut = __is_same(T, bf16_t) ? 1 : 2;
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
+    static constexpr int kHalf = kTiles / 2;                  // row tiles of a wave of a pair
     static constexpr int kRows = kParts * 4 * kSteps * 1024;  // K or Q
     static constexpr int kMatrices = 2 * DeltaRecord::kMatrix;
     static constexpr int kBytesP = kMode == kOutputs ? kOut * DeltaRecord::kMatrix : 0;
@@ -48,31 +52,59 @@ struct Layout {
     static constexpr int kAtK = 0;
     static constexpr int kAtT = kAtK + kRows;
     static constexpr int kAtF = kAtT + kMatrices;
-    static constexpr int kBuffer = kAtF + DeltaRecord::kFactorBytes;
+    static constexpr int kFactorBytes = 256 * DeltaRecord::kChain;
+    static constexpr int kBuffer = kAtF + kFactorBytes;
     // one or two of Q and P
     static constexpr int kAtQ = 2 * kBuffer;
     static constexpr int kAtP = kAtQ + (kMode == kOutputs ? kRows : 0);
     static constexpr int kBufferQ = kAtP + kBytesP - kAtQ;
     // one of these
     static constexpr int kAtV = kAtQ + (kPosts ? 2 : 1) * kBufferQ;
-    using V = Values<T, kWalkers, 256, float>;
+    // V as FP32 but for float16, where the LDS is full
+    using VType = typename std::conditional<__is_same(T, f16_t), f16_t, float>::type;
+    using V = Values<T, kWalkers, 256, VType>;
     static constexpr int kAtS = kAtV + kWalkers * V::kEach;
-    static constexpr int kEachS = kOut * kSteps * 1024 + 256;  // and its scale
+    static constexpr int kEachS = kOut * kSteps * 1024 + 128;  // and the scales of its halves
     static constexpr int kAtU = kAtS + (kMode == kOutputs ? kWalkers * kEachS : 0);
     static constexpr int kEachU = kC * 16 * 4 + 128;  // and each column's rows that count, and scale
     static constexpr int kBufferU = kMode == kOutputs ? kWalkers * kEachU : 0;  // one or two
-    static constexpr int kAtPosts = kAtU + (kPosts ? 2 : 1) * kBufferU;
+    // what the waves of a pair give each other
+    static constexpr int kAtX = kAtU + (kPosts ? 2 : 1) * kBufferU;
+    static constexpr int kEachX = 4 * 1024 + 64;
+    // chunks done: [wave] S is down, V taken; [2 kWalkers + wave] given to the other
+    static constexpr int kAtPosts = kAtX + kWalkers * kEachX;
     static constexpr int kBytes = kAtPosts + 16 * kWalkers;
 };
 
-template <class T, int kK, int kWalkers, int kMode>
-__global__ __launch_bounds__(64 * (kWalkers + Layout<T, kK, kWalkers, kMode>::kHelpers), 1)
+// Gives what was written to LDS before, by flag, to the other wave of a pair.  A wave's
+// LDS accesses are carried out in order, so neither side has to wait for its own.
+__device__ inline void give(int* flag, int n) {
+    asm volatile("" ::: "memory");
+    __hip_atomic_store(flag, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+// Reads behind a flag, until they came after its n-th rise.
+template <class F>
+__device__ inline void take(const int* flag, int n, F&& read) {
+    int given;
+    do {
+        given = __hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        asm volatile("" ::: "memory");
+        read();
+        asm volatile("" ::: "memory");
+    } while (__builtin_amdgcn_readfirstlane(given) < n);
+}
+
+// kWide: all rows can be loaded 16 bytes at a time (8 of V's).  (Decided here, not where
+// they are loaded: loads of two kinds into the same registers would be waited for
+// as if both were under way.)
+template <class T, int kK, int kWalkers, int kMode, bool kWide>
+__global__ __launch_bounds__(64 * (2 * kWalkers + Layout<T, kK, kWalkers, kMode>::kHelpers), 1)
 void delta_chain_kernel(DeltaChunks p) {
     using L = Layout<T, kK, kWalkers, kMode>;
     constexpr int kOut = L::kOut, kHelpers = L::kHelpers;
     constexpr bool kPosts = L::kPosts;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);  // one each 4 ints: chunks posted
+    int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -101,12 +133,15 @@ void delta_chain_kernel(DeltaChunks p) {
     const char* records = p.records + ((int64_t)first_chunk * p.v_heads + h) * p.record_bytes;
     const int64_t record_step = (int64_t)p.v_heads * p.record_bytes;
     const int64_t skip = (int64_t)walk.first * kC;  // tokens of the parts before
-    if (kPosts && threadIdx.x < kWalkers) posts[4 * threadIdx.x] = 0;
+    if (threadIdx.x < 4 * kWalkers) posts[threadIdx.x] = 0;
 
-    if (wave < kWalkers) {
-        const int col = col0 + 16 * wave + (lane & 15);
+    if (wave < 2 * kWalkers) {
+        const int group = wave >> 1, half = wave & 1;
+        const bool leads = half == 0;
+        const int row0 = half * 16 * L::kHalf;
+        const int col = col0 + 16 * group + (lane & 15);
         const bool in = col < columns;
-        f32x4 S[L::kTiles];  // rows 16 i + 4 g + r
+        f32x4 S[L::kHalf];  // rows row0 + 16 i + 4 g + r
         const int64_t sequence = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size;
         const int64_t part = ((int64_t)index * p.v_heads + h) * p.k_size * p.v_size;
         const float* from = kMode == kPartSteps    ? nullptr
@@ -114,35 +149,44 @@ void delta_chain_kernel(DeltaChunks p) {
                             : p.initial         ? p.initial + sequence
                                                 : nullptr;
 #pragma unroll
-        for (int i = 0; i < L::kTiles; ++i)
+        for (int i = 0; i < L::kHalf; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int row = 16 * i + 4 * g + r;
+                const int row = row0 + 16 * i + 4 * g + r;
                 S[i][r] = from && in && row < p.k_size ? from[(int64_t)row * p.v_size + col] : 0.0f;
                 if (of_m && row == col) S[i][r] = 1.0f;
             }
-        const char* v_at = lds + L::kAtV + wave * L::V::kEach + value_slot(lane, wave) * 16;
-        char* s_at = lds + L::kAtS + wave * L::kEachS;
-        char* u_at = lds + L::kAtU + wave * L::kEachU + lane * 16;
+        const char* v_at = lds + L::kAtV + group * L::V::kEach + 
+                           value_slot(lane, group) * 4 * (int)sizeof(typename L::VType);
+        char* s_at = lds + L::kAtS + group * L::kEachS;
+        char* u_at = lds + L::kAtU + group * L::kEachU + lane * 16;
+        char* x_at = lds + L::kAtX + group * L::kEachX;
+        int* given = posts + 2 * kWalkers;
 
         for (int c = 0; c < chunks; ++c) {
             const char* at = lds + (c & 1) * L::kBuffer;
-            const float* f = reinterpret_cast<const float*>(at + L::kAtF);
+            const float* f =
+                reinterpret_cast<const float*>(at + L::kAtF) - 64 * DeltaRecord::kFirstChain;
             const auto factor = [&](int which, int tile) __attribute__((always_inline)) {
                 return reinterpret_cast<const f32x4*>(f + 64 * which)[4 * tile + g];
             };
             lds_barrier();  // A
             f32x4 vt[4];
+            if (leads)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) vt[i] = *reinterpret_cast<const f32x4*>(v_at + i * 1024);
+                for (int i = 0; i < 4; ++i) {
+                    typename L::VType w[4];
+                    __builtin_memcpy(w, v_at + i * 64 * sizeof(w), sizeof(w));
+                    vt[i] = f32x4{to_f32(w[0]), to_f32(w[1]), to_f32(w[2]), to_f32(w[3])};
+                }
             if (kMode == kStates) {
                 const int64_t task = (int64_t)(first_chunk + c) * p.v_heads + h;
                 const __amdgpu_buffer_rsrc_t to =
                     buffer_at(p.states + task * ((p.k_size + 15) / 16 * 16) * p.v_size);
-                const uint32_t off = in ? 4u * (4 * g * p.v_size + col) : kPastEnd;
+                const uint32_t off = in ? 4u * ((row0 + 4 * g) * p.v_size + col) : kPastEnd;
 #pragma unroll
-                for (int i = 0; i < L::kTiles; ++i)
-                    if (16 * i < p.k_size)
+                for (int i = 0; i < L::kHalf; ++i)
+                    if (row0 + 16 * i < p.k_size)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             __builtin_amdgcn_raw_buffer_store_b32(
@@ -150,21 +194,23 @@ void delta_chain_kernel(DeltaChunks p) {
                                 4 * (16 * i + r) * p.v_size, 0);
             }
             const Scale ss = scale_of(max_groups(largest(S)));
-            Frag<2> sb[L::kSteps];
+            Frag<2> sb[L::kSteps / 2];
 #pragma unroll
-            for (int j = 0; j < L::kSteps; ++j) {
+            for (int j = 0; j < L::kSteps / 2; ++j) {
                 sb[j] = split<2>(S[2 * j], S[2 * j + 1], ss.up);
                 if (kMode == kOutputs)
 #pragma unroll
                     for (int q = 0; q < kOut; ++q)
-                        *reinterpret_cast<half8_t*>(s_at + (q * L::kSteps + j) * 1024 + lane * 16) =
+                        *reinterpret_cast<half8_t*>(
+                            s_at + (q * L::kSteps + half * (L::kSteps / 2) + j) * 1024 + lane * 16) =
                             sb[j].part[q];
             }
             if (kMode == kOutputs)
-                reinterpret_cast<float*>(s_at + kOut * L::kSteps * 1024)[lane] = ss.down;
+                reinterpret_cast<float*>(s_at + kOut * L::kSteps * 1024)[16 * half + (lane & 15)] =
+                    ss.down;
             if (kPosts) {
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-                __hip_atomic_store(posts + 4 * wave, c + 1, __ATOMIC_RELAXED,
+                __hip_atomic_store(posts + wave, c + 1, __ATOMIC_RELAXED,
                                    __HIP_MEMORY_SCOPE_WORKGROUP);
             } else {
                 lds_barrier();  // B
@@ -172,15 +218,44 @@ void delta_chain_kernel(DeltaChunks p) {
             // V - e^G K S
             f32x4 x[4] = {};
 #pragma unroll
-            for (int j = 0; j < L::kSteps; ++j)
+            for (int j = 0; j < L::kSteps / 2; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    x[i] = multiply(row_fragment<T, kK>(at + L::kAtK, i, j, lane), sb[j], x[i]);
+                    x[i] = multiply(row_fragment<T, kK>(at + L::kAtK, i, half * (L::kSteps / 2) + j,
+                                                        lane), sb[j], x[i]);
+            Frag<2> b[2];
+            float down;
+            if (!leads) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(x_at + i * 1024 + lane * 16) = x[i] * ss.down;
+                give(given + wave, c + 1);
+                while (__hip_atomic_load(given + wave - 1, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= c)
+                    __builtin_amdgcn_s_sleep(1);
+                take(given + wave - 1, c + 1, [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            b[j].part[q] = *reinterpret_cast<const half8_t*>(
+                                x_at + (2 * j + q) * 1024 + lane * 16);
+                    down = reinterpret_cast<const float*>(x_at + 4096)[lane & 15];
+                });
+            } else {
+            f32x4 other[4];
+            take(given + wave + 1, c + 1, [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    other[i] = *reinterpret_cast<const f32x4*>(x_at + i * 1024 + lane * 16);
+            });
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f32x4 rise = factor(DeltaRecord::kRise, i) * ss.down;
+                const f32x4 rise = factor(DeltaRecord::kRise, i);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[i][r] = __builtin_fmaf(-rise[r], x[i][r], vt[i][r]);
+                for (int r = 0; r < 4; ++r)
+                    x[i][r] = __builtin_fmaf(
+                        -rise[r], __builtin_fmaf(x[i][r], ss.down, other[i][r]), vt[i][r]);
             }
             // U
             f32x4 u[4] = {};
@@ -191,12 +266,12 @@ void delta_chain_kernel(DeltaChunks p) {
                 const bool cuts = __any(!finite(top));
                 if (cuts) cut = cut_column(x, top);
                 const Scale xs = scale_of(top);
-                const Frag<2> b[2] = {split<2>(x[0], x[1], xs.up), split<2>(x[2], x[3], xs.up)};
+                const Frag<2> xb[2] = {split<2>(x[0], x[1], xs.up), split<2>(x[2], x[3], xs.up)};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
 #pragma unroll
                     for (int j = 0; j <= i / 2; ++j)
-                        u[i] = multiply(matrix_fragment<2>(at + L::kAtT, lower_at(i, j), lane), b[j],
+                        u[i] = multiply(matrix_fragment<2>(at + L::kAtT, lower_at(i, j), lane), xb[j],
                                         u[i]);
                     u[i] *= kMode == kStates ? factor(DeltaRecord::kT, i) * xs.down
                                              : factor(DeltaRecord::kT, i);
@@ -231,16 +306,26 @@ void delta_chain_kernel(DeltaChunks p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) u[i] *= factor(DeltaRecord::kTail, i);
             const Scale us = scale_of(max_groups(largest(u)));
-            const Frag<2> b[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
-            const float decay = f[64 * DeltaRecord::kDecay];
-            float down = cut == kC ? us.down * u_down : __builtin_nanf("");
+            b[0] = split<2>(u[0], u[1], us.up);
+            b[1] = split<2>(u[2], u[3], us.up);
+            down = cut == kC ? us.down * u_down : __builtin_nanf("");
             asm("" : "+v"(down));  // one select, not one for every product with it
 #pragma unroll
-            for (int i = 0; i < L::kTiles; ++i) {
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    *reinterpret_cast<half8_t*>(x_at + (2 * j + q) * 1024 + lane * 16) = b[j].part[q];
+            reinterpret_cast<float*>(x_at + 4096)[lane & 15] = down;
+            give(given + wave, c + 1);
+            }
+            const float decay = f[64 * DeltaRecord::kDecay];
+#pragma unroll
+            for (int i = 0; i < L::kHalf; ++i) {
                 f32x4 a{};
 #pragma unroll
                 for (int j = 0; j < 2; ++j)  // lo.lo too: updates of like keys cancel
-                    a = multiply<true>(column_fragment<T, kK>(at + L::kAtK, i, j, lane), b[j], a);
+                    a = multiply<true>(
+                        column_fragment<T, kK>(at + L::kAtK, half * L::kHalf + i, j, lane), b[j], a);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     S[i][r] = __builtin_fmaf(a[r], down, decay * S[i][r]);
@@ -256,36 +341,36 @@ void delta_chain_kernel(DeltaChunks p) {
         const int stride = of_m ? rows : p.v_size;
         if (to && (in || (of_m && col < rows)))
 #pragma unroll
-            for (int i = 0; i < L::kTiles; ++i)
+            for (int i = 0; i < L::kHalf; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * i + 4 * g + r;
+                    const int row = row0 + 16 * i + 4 * g + r;
                     if (row < (of_m ? rows : p.k_size)) to[(int64_t)row * stride + col] = S[i][r];
                 }
         return;
     }
 
     // ---- the helping waves
-    const int helper = wave - kWalkers;
+    const int helper = wave - 2 * kWalkers;
     const bool brings_k = helper < 4, brings_q = kMode == kOutputs && helper >= kHelpers - 4;
-    const int id = (threadIdx.x - 64 * kWalkers) & 255;
+    const int id = (threadIdx.x - 128 * kWalkers) & 255;
     const T* k = row_of<const T>(p.k, packed, n, span, kh) + skip * p.k.token;
     const T* q = row_of<const T>(p.q, packed, n, span, kh) + skip * p.q.token;
     const T* v = row_of<const T>(p.v, packed, n, span, h) + skip * p.v.token + col0;
     Rows<T, kK, 256> ku, qu;
     Copy<L::kMatrices, 256> tcopy;
-    Copy<DeltaRecord::kFactorBytes, 256> fcopy;
+    Copy<L::kFactorBytes, 256> fcopy;
     Copy<L::kBytesP == 0 ? 16 : L::kBytesP, 256> pcopy;
     typename L::V vu;
     const auto load_k = [&](int c) __attribute__((always_inline)) {
         const int count = min(kC, span.count - c * kC);
         const char* record = records + c * record_step;
-        ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, count, p.k_size, p.wide,
+        ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, count, p.k_size, kWide,
                 reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
         tcopy.load(record + DeltaRecord::kAtT, id);
-        fcopy.load(record, id);
+        fcopy.load(record + 256 * DeltaRecord::kFirstChain, id);
         vu.load(v + (int64_t)c * kC * p.v.token, p.v.token, count, of_m ? 0 : p.v_size - col0,
-                p.wide_values, id);
+                kWide, id);
     };
     const auto store_k = [&](int c) __attribute__((always_inline)) {
         char* to = lds + (c & 1) * L::kBuffer;
@@ -297,7 +382,7 @@ void delta_chain_kernel(DeltaChunks p) {
     const auto load_q = [&](int c) __attribute__((always_inline)) {
         const char* record = records + c * record_step;
         qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, min(kC, span.count - c * kC), p.k_size,
-                p.wide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
+                kWide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
     };
     const auto load_p = [&](int c) __attribute__((always_inline)) { pcopy.load(records + c * record_step + DeltaRecord::kAtP, id); };
     const auto buffer_q = [&](int c) __attribute__((always_inline)) { return lds + (kPosts ? (c & 1) * L::kBufferQ : 0); };
@@ -374,8 +459,8 @@ void delta_chain_kernel(DeltaChunks p) {
         if (kPosts) {
             // every walking wave is in this chunk and posts on its way
 #pragma unroll
-            for (int w = 0; w < kWalkers; ++w)
-                while (__hip_atomic_load(posts + 4 * w, __ATOMIC_RELAXED,
+            for (int w = 0; w < 2 * kWalkers; ++w)
+                while (__hip_atomic_load(posts + w, __ATOMIC_RELAXED,
                                          __HIP_MEMORY_SCOPE_WORKGROUP) <= c)
                     __builtin_amdgcn_s_sleep(1);
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
@@ -395,13 +480,23 @@ void delta_chain_kernel(DeltaChunks p) {
             if (c + 2 < chunks) load_k(c + 2);
         }
         if (outputs) {
-            const float* f = reinterpret_cast<const float*>(lds + (c & 1) * L::kBuffer + L::kAtF);
+            const float* f = reinterpret_cast<const float*>(lds + (c & 1) * L::kBuffer + L::kAtF) -
+                             64 * DeltaRecord::kFirstChain;
             const char* s_at = lds + L::kAtS + block * L::kEachS;
-            const float down = reinterpret_cast<const float*>(s_at + kOut * L::kSteps * 1024)[lane];
+            const float* downs =
+                reinterpret_cast<const float*>(s_at + kOut * L::kSteps * 1024) + (lane & 15);
+            const float first = downs[0], last = downs[16];  // of S's halves
+            f32x4 z[kOwn];
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) y[i] = f32x4{};
 #pragma unroll
             for (int j = 0; j < L::kSteps; ++j) {
+                if (j == L::kSteps / 2)
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) {
+                        z[i] = y[i] * first;
+                        y[i] = f32x4{};
+                    }
                 Frag<kOut> b;
 #pragma unroll
                 for (int r = 0; r < kOut; ++r)
@@ -415,7 +510,8 @@ void delta_chain_kernel(DeltaChunks p) {
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
                 const int at = 4 * (own + i) + g;
-                y[i] *= reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryRise)[at] * down;
+                y[i] = (y[i] * last + z[i]) *
+                       reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryRise)[at];
                 pf[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kP)[at];
             }
         }
@@ -432,22 +528,29 @@ void delta_chain_kernel(DeltaChunks p) {
     }
 }
 
-template <class T, int kK, int kWalkers, int kMode>
-hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
+template <class T, int kK, int kWalkers, int kMode, bool kWide>
+hipError_t launch_rows(const DeltaChunks& a, hipStream_t stream) {
     using L = Layout<T, kK, kWalkers, kMode>;
     static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
     constexpr int kColumns = 16 * kWalkers;
     int64_t slices = (a.v_size + kColumns - 1) / kColumns;
     if (kMode == kPartSteps) slices += (a.k_size + kColumns - 1) / kColumns;
     const int64_t walks = a.part_chunks > 0 ? a.parts : a.batch;
-    const void* kernel = reinterpret_cast<const void*>(delta_chain_kernel<T, kK, kWalkers, kMode>);
+    const void* kernel =
+        reinterpret_cast<const void*>(delta_chain_kernel<T, kK, kWalkers, kMode, kWide>);
     if (hipError_t e =
             hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes))
         return e;
-    hipLaunchKernelGGL((delta_chain_kernel<T, kK, kWalkers, kMode>),
+    hipLaunchKernelGGL((delta_chain_kernel<T, kK, kWalkers, kMode, kWide>),
                        dim3((unsigned)walk_blocks(walks * a.v_heads, slices)),
-                       dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
+                       dim3(64 * (2 * kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
+}
+
+template <class T, int kK, int kWalkers, int kMode>
+hipError_t launch(const DeltaChunks& a, hipStream_t stream) {
+    return a.wide && a.wide_values ? launch_rows<T, kK, kWalkers, kMode, true>(a, stream)
+                                   : launch_rows<T, kK, kWalkers, kMode, false>(a, stream);
 }
 
 }  // namespace

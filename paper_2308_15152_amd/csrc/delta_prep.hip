@@ -76,7 +76,7 @@ __device__ inline void write_fragments(const float* M, int tile, int lane, char*
     }
 }
 
-template <class T, int kK, bool kBackward>
+template <class T, int kK, bool kBackward, bool kWide>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_kernel(DeltaChunks p) {
     constexpr int kSteps = kK / 32;
     // A and P; before them, in the same place, k's rows as operands
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
 #pragma unroll
         for (int j = 0; j < kSteps; ++j)
             x[j] = load_eight<T>(r, t * (uint32_t)stride * (uint32_t)sizeof(T), 32 * j + 8 * g, p.k_size,
-                                 t < at.count, p.wide);
+                                 t < at.count, kWide);
     };
     const auto take_tile = [&](const Eight<T>(&x)[kSteps], Operand<T>(&f)[kSteps])
                                __attribute__((always_inline)) {
@@ -286,13 +286,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
     }
 }
 
-template <class T, int kK>
-void launch(const DeltaChunks& a, hipStream_t stream) {
+template <class T, int kK, bool kWide>
+void launch_rows(const DeltaChunks& a, hipStream_t stream) {
     const dim3 grid((unsigned)(a.chunks * a.v_heads));
     if (a.backward)
-        hipLaunchKernelGGL((delta_prep_kernel<T, kK, true>), grid, dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL((delta_prep_kernel<T, kK, true, kWide>), grid, dim3(kThreads), 0,
+                           stream, a);
     else
-        hipLaunchKernelGGL((delta_prep_kernel<T, kK, false>), grid, dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL((delta_prep_kernel<T, kK, false, kWide>), grid, dim3(kThreads), 0,
+                           stream, a);
+}
+
+template <class T, int kK>
+void launch(const DeltaChunks& a, hipStream_t stream) {
+    if (a.wide)
+        launch_rows<T, kK, true>(a, stream);
+    else
+        launch_rows<T, kK, false>(a, stream);
 }
 
 }  // namespace
