@@ -36,9 +36,10 @@ constexpr int kOutputs = kDeltaOutputs, kStates = kDeltaStates, kPartSteps = kDe
 // kWalkers: groups of 16 columns, a pair of walking waves each.
 template <class T, int kK, int kWalkers, int kMode>
 struct Layout {
-    static constexpr bool kPosts = sizeof(T) == 2;
-    // with eight helpers, four bring K, T and V and four Q and P
-    static constexpr int kHelpers = kMode == kOutputs && kPosts ? 8 : 4;
+    static constexpr bool kPosts = sizeof(T) == 2 || kMode != kOutputs;
+    // Four bring the operands, four make O.  (Stores of O among a wave's loads
+    // would be waited for with them.)
+    static constexpr int kHelpers = kMode == kOutputs ? 8 : 4;
     static constexpr int kParts = kPartsOf<T>;  // of K and Q
     // of P, and of S and U where they make O: rounding them to fp16 alone costs
     // 2^-12 relative, unseen in a bfloat16 result (2^-8) but not in others
@@ -101,7 +102,7 @@ template <class T, int kK, int kWalkers, int kMode, bool kWide>
 __global__ __launch_bounds__(64 * (2 * kWalkers + Layout<T, kK, kWalkers, kMode>::kHelpers), 1)
 void delta_chain_kernel(DeltaChunks p) {
     using L = Layout<T, kK, kWalkers, kMode>;
-    constexpr int kOut = L::kOut, kHelpers = L::kHelpers;
+    constexpr int kOut = L::kOut;
     constexpr bool kPosts = L::kPosts;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);
@@ -352,48 +353,119 @@ void delta_chain_kernel(DeltaChunks p) {
 
     // ---- the helping waves
     const int helper = wave - 2 * kWalkers;
-    const bool brings_k = helper < 4, brings_q = kMode == kOutputs && helper >= kHelpers - 4;
-    const int id = (threadIdx.x - 128 * kWalkers) & 255;
-    const T* k = row_of<const T>(p.k, packed, n, span, kh) + skip * p.k.token;
-    const T* q = row_of<const T>(p.q, packed, n, span, kh) + skip * p.q.token;
-    const T* v = row_of<const T>(p.v, packed, n, span, h) + skip * p.v.token + col0;
-    Rows<T, kK, 256> ku, qu;
-    Copy<L::kMatrices, 256> tcopy;
-    Copy<L::kFactorBytes, 256> fcopy;
-    Copy<L::kBytesP == 0 ? 16 : L::kBytesP, 256> pcopy;
-    typename L::V vu;
-    const auto load_k = [&](int c) __attribute__((always_inline)) {
-        const int count = min(kC, span.count - c * kC);
-        const char* record = records + c * record_step;
-        ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, count, p.k_size, kWide,
-                reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
-        tcopy.load(record + DeltaRecord::kAtT, id);
-        fcopy.load(record + 256 * DeltaRecord::kFirstChain, id);
-        vu.load(v + (int64_t)c * kC * p.v.token, p.v.token, count, of_m ? 0 : p.v_size - col0,
-                kWide, id);
+    const auto buffer_q = [&](int c) __attribute__((always_inline)) {
+        return lds + (kPosts ? (c & 1) * L::kBufferQ : 0);
     };
-    const auto store_k = [&](int c) __attribute__((always_inline)) {
-        char* to = lds + (c & 1) * L::kBuffer;
-        ku.store(to + L::kAtK, id);
-        tcopy.store(to + L::kAtT, id);
-        fcopy.store(to + L::kAtF, id);
+    // until every walking wave, which is in chunk c and posts on its way, has posted
+    const auto wait_posts = [&](int c) __attribute__((always_inline)) {
+        if (kPosts) {
+#pragma unroll
+            for (int w = 0; w < 2 * kWalkers; ++w)
+                while (__hip_atomic_load(posts + w, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= c)
+                    __builtin_amdgcn_s_sleep(1);
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        } else {
+            lds_barrier();  // B
+        }
     };
-    const auto store_v = [&]() __attribute__((always_inline)) { vu.store(lds + L::kAtV, id); };
-    const auto load_q = [&](int c) __attribute__((always_inline)) {
-        const char* record = records + c * record_step;
-        qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, min(kC, span.count - c * kC), p.k_size,
-                kWide, reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
-    };
-    const auto load_p = [&](int c) __attribute__((always_inline)) { pcopy.load(records + c * record_step + DeltaRecord::kAtP, id); };
-    const auto buffer_q = [&](int c) __attribute__((always_inline)) { return lds + (kPosts ? (c & 1) * L::kBufferQ : 0); };
+
+    if (helper < 4) {  // bring the operands
+        int id = threadIdx.x - 128 * kWalkers;
+        const T* k = row_of<const T>(p.k, packed, n, span, kh) + skip * p.k.token;
+        const T* q = row_of<const T>(p.q, packed, n, span, kh) + skip * p.q.token;
+        const T* v = row_of<const T>(p.v, packed, n, span, h) + skip * p.v.token + col0;
+        Rows<T, kK, 256> ku, qu;
+        Copy<L::kMatrices, 256> tcopy;
+        Copy<L::kFactorBytes, 256> fcopy;
+        Copy<L::kBytesP == 0 ? 16 : L::kBytesP, 256> pcopy;
+        typename L::V vu;
+        const auto load_k = [&](int c) __attribute__((always_inline)) {
+            const int count = min(kC, span.count - c * kC);
+            const char* record = records + c * record_step;
+            ku.load(k + (int64_t)c * kC * p.k.token, p.k.token, count, p.k_size, kWide,
+                    reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kKeyScale, id);
+            tcopy.load(record + DeltaRecord::kAtT, id);
+            fcopy.load(record + 256 * DeltaRecord::kFirstChain, id);
+        };
+        const auto load_v = [&](int c) __attribute__((always_inline)) {
+            vu.load(v + (int64_t)c * kC * p.v.token, p.v.token, min(kC, span.count - c * kC),
+                    of_m ? 0 : p.v_size - col0, kWide, id);
+        };
+        const auto store_k = [&](int c) __attribute__((always_inline)) {
+            char* to = lds + (c & 1) * L::kBuffer;
+            ku.store(to + L::kAtK, id);
+            tcopy.store(to + L::kAtT, id);
+            fcopy.store(to + L::kAtF, id);
+        };
+        const auto store_v = [&]() __attribute__((always_inline)) { vu.store(lds + L::kAtV, id); };
+        const auto load_q = [&](int c) __attribute__((always_inline)) {
+            if (kMode != kOutputs) return;
+            const char* record = records + c * record_step;
+            qu.load(q + (int64_t)c * kC * p.q.token, p.q.token, min(kC, span.count - c * kC),
+                    p.k_size, kWide,
+                    reinterpret_cast<const float*>(record) + 64 * DeltaRecord::kQueryScale, id);
+        };
+        const auto load_p = [&](int c) __attribute__((always_inline)) {
+            if (kMode == kOutputs) pcopy.load(records + c * record_step + DeltaRecord::kAtP, id);
+        };
+        const auto store_q = [&](int c) __attribute__((always_inline)) {
+            if (kMode == kOutputs) qu.store(buffer_q(c) + L::kAtQ, id);
+        };
+        const auto store_p = [&](int c) __attribute__((always_inline)) {
+            if (kMode == kOutputs) pcopy.store(buffer_q(c) + L::kAtP, id);
+        };
+        // A chunk's operands are loaded as soon as the registers are free, a chunk before
+        // they go down; Q goes down a chunk ahead like K, or (FP32) in its own chunk.
+        // There are no conditions, so that it is known at every wait which loads are
+        // behind the one waited for: after the last chunk it is brought again.
+        constexpr int kAhead = kPosts ? 1 : 0;
+        const int last = chunks - 1;
+        if (chunks > 0) {
+            load_k(0);
+            load_q(0);
+            load_p(0);
+            load_v(0);
+            store_k(0);
+            load_k(min(1, last));
+            if (kAhead > 0) {
+                store_q(0);
+                load_q(min(1, last));
+            }
+            store_v();
+            load_v(min(1, last));
+        }
+        for (int c = 0; c < chunks; ++c) {
+            lds_barrier();  // A
+            if (!kPosts) asm volatile("" : "+v"(id));  // places made anew, not kept
+            // what the last chunk was the last to read; now, while the walking waves
+            // need little of the LDS (their K S does)
+            store_k(c + 1);
+            load_k(min(c + 2, last));
+            if (kPosts) {
+                store_p(c);
+                load_p(min(c + 1, last));
+            }
+            store_q(c + kAhead);
+            load_q(min(c + kAhead + 1, last));
+            wait_posts(c);
+            if (!kPosts) {
+                store_p(c);
+                load_p(min(c + 1, last));
+            }
+            store_v();
+            load_v(min(c + 2, last));
+        }
+        if (kMode == kOutputs && chunks > 0) lds_barrier();  // the last U
+        return;
+    }
 
     // O: 16 columns and kOwn token tiles of a chunk to a wave
-    constexpr int kOwn = 4 * kWalkers / kHelpers < 1 ? 1 : 4 * kWalkers / kHelpers;
-    const int block = helper % kWalkers, own = helper / kWalkers * kOwn;
-    const bool outputs = kMode == kOutputs && own < 4;
+    constexpr int kOwn = kWalkers;
+    const int block = helper % kWalkers, own = (helper - 4) / kWalkers * kOwn;
     const int col = col0 + 16 * block + (lane & 15);
     const bool in = col < p.v_size;
-    T* o = kMode == kOutputs ? row_of<T>(p.o, packed, n, span, h) + skip * p.o.token : nullptr;
+    T* o = row_of<T>(p.o, packed, n, span, h) + skip * p.o.token;
     const uint32_t o_step = (uint32_t)p.o.token * sizeof(T);
     const uint32_t o_at = in ? (16 * own + 4 * g) * o_step + col * (uint32_t)sizeof(T) : kPastEnd;
     f32x4 y[kOwn], pf[kOwn];  // scale diag(e^G) Q S, and the scales of P's rows
@@ -430,101 +502,48 @@ void delta_chain_kernel(DeltaChunks p) {
         }
     };
 
-    if (chunks > 0) {
-        if (brings_k) {
-            load_k(0);
-            store_k(0);
-            store_v();
-            if (chunks > 1) load_k(1);
-        }
-        if (brings_q) {
-            load_q(0);
-            load_p(0);
-            if (kPosts) {
-                qu.store(buffer_q(0) + L::kAtQ, id);
-                if (chunks > 1) load_q(1);
-            }
-        }
-    }
     for (int c = 0; c < chunks; ++c) {
         lds_barrier();  // A
-        // what the last chunk was the last to read; now, while the walking waves need
-        // little of the LDS (their K S does)
-        if (brings_k && c + 1 < chunks) store_k(c + 1);
-        if (kPosts && brings_q) {
-            pcopy.store(buffer_q(c) + L::kAtP, id);
-            if (c + 1 < chunks) qu.store(buffer_q(c + 1) + L::kAtQ, id);
-        }
-        if (outputs && c > 0) finish(c - 1);
-        if (kPosts) {
-            // every walking wave is in this chunk and posts on its way
+        if (c > 0) finish(c - 1);
+        wait_posts(c);
+        const float* f = reinterpret_cast<const float*>(lds + (c & 1) * L::kBuffer + L::kAtF) -
+                         64 * DeltaRecord::kFirstChain;
+        const char* s_at = lds + L::kAtS + block * L::kEachS;
+        const float* downs =
+            reinterpret_cast<const float*>(s_at + kOut * L::kSteps * 1024) + (lane & 15);
+        const float first = downs[0], last = downs[16];  // of S's halves
+        f32x4 z[kOwn];
 #pragma unroll
-            for (int w = 0; w < 2 * kWalkers; ++w)
-                while (__hip_atomic_load(posts + w, __ATOMIC_RELAXED,
-                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= c)
-                    __builtin_amdgcn_s_sleep(1);
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-        } else {
-            if (brings_q) qu.store(lds + L::kAtQ, id);
-            lds_barrier();  // B
-            if (brings_q) {
-                pcopy.store(lds + L::kAtP, id);
-                if (c + 1 < chunks) {
-                    load_q(c + 1);
-                    load_p(c + 1);
+        for (int i = 0; i < kOwn; ++i) y[i] = f32x4{};
+#pragma unroll
+        for (int j = 0; j < L::kSteps; ++j) {
+            if (j == L::kSteps / 2)
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    z[i] = y[i] * first;
+                    y[i] = f32x4{};
                 }
-            }
+            Frag<kOut> b;
+#pragma unroll
+            for (int r = 0; r < kOut; ++r)
+                b.part[r] = *reinterpret_cast<const half8_t*>(
+                    s_at + (r * L::kSteps + j) * 1024 + lane * 16);
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i)
+                y[i] = multiply(row_fragment<T, kK>(buffer_q(c) + L::kAtQ, own + i, j, lane), b,
+                                y[i]);
         }
-        if (brings_k && c + 1 < chunks) {
-            store_v();
-            if (c + 2 < chunks) load_k(c + 2);
-        }
-        if (outputs) {
-            const float* f = reinterpret_cast<const float*>(lds + (c & 1) * L::kBuffer + L::kAtF) -
-                             64 * DeltaRecord::kFirstChain;
-            const char* s_at = lds + L::kAtS + block * L::kEachS;
-            const float* downs =
-                reinterpret_cast<const float*>(s_at + kOut * L::kSteps * 1024) + (lane & 15);
-            const float first = downs[0], last = downs[16];  // of S's halves
-            f32x4 z[kOwn];
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i) y[i] = f32x4{};
-#pragma unroll
-            for (int j = 0; j < L::kSteps; ++j) {
-                if (j == L::kSteps / 2)
-#pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        z[i] = y[i] * first;
-                        y[i] = f32x4{};
-                    }
-                Frag<kOut> b;
-#pragma unroll
-                for (int r = 0; r < kOut; ++r)
-                    b.part[r] = *reinterpret_cast<const half8_t*>(
-                        s_at + (r * L::kSteps + j) * 1024 + lane * 16);
-#pragma unroll
-                for (int i = 0; i < kOwn; ++i)
-                    y[i] = multiply(row_fragment<T, kK>(buffer_q(c) + L::kAtQ, own + i, j, lane), b,
-                                    y[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) {
-                const int at = 4 * (own + i) + g;
-                y[i] = (y[i] * last + z[i]) *
-                       reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryRise)[at];
-                pf[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kP)[at];
-            }
-        }
-        if (kPosts && brings_q) {
-            if (c + 1 < chunks) {
-                load_p(c + 1);
-                if (c + 2 < chunks) load_q(c + 2);
-            }
+        for (int i = 0; i < kOwn; ++i) {
+            const int at = 4 * (own + i) + g;
+            y[i] = (y[i] * last + z[i]) *
+                   reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kQueryRise)[at];
+            pf[i] = reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kP)[at];
         }
     }
-    if (kMode == kOutputs && chunks > 0) {
+    if (chunks > 0) {
         lds_barrier();  // the last U
-        if (outputs) finish(chunks - 1);
+        finish(chunks - 1);
     }
 }
 

@@ -493,18 +493,17 @@ __device__ inline Frag<N> matrix_fragment(const char* matrix, int at, int lane) 
     return f;
 }
 
-// A piece of a record on its way to LDS, 16 bytes a thread and turn.
+// A piece of a record on its way to LDS, 16 bytes a thread and turn.  (Here and below,
+// threads without a part of their own load one all the same: which loads are
+// under way is then the same on every path, and a wait waits for no later ones.)
 template <int kBytes, int kThreads>
 struct Copy {
     static constexpr int kPieces = kBytes / 16, kTurns = (kPieces + kThreads - 1) / kThreads;
     u32x4 x[kTurns];
     __device__ void load(const char* from, int thread) {
 #pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            const int at = thread + i * kThreads;
-            if (kPieces % kThreads == 0 || at < kPieces)
-                x[i] = reinterpret_cast<const u32x4*>(from)[at];
-        }
+        for (int i = 0; i < kTurns; ++i)
+            x[i] = reinterpret_cast<const u32x4*>(from)[(thread + i * kThreads) % kPieces];
     }
     __device__ void store(char* to, int thread) const {
 #pragma unroll
@@ -526,8 +525,7 @@ struct Rows {
                          const float* scales, int thread) {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            const int unit = thread + i * kThreads;
-            if (U::kUnits % kThreads != 0 && unit >= U::kUnits) continue;
+            const int unit = (thread + i * kThreads) % U::kUnits;
             u[i].load(rows, stride, unit, count, size, wide);
             if (!__is_same(T, f16_t))
                 scale[i] = reinterpret_cast<const f32x4*>(scales)[unit / (kK / 8)];
@@ -562,8 +560,7 @@ struct Values {
         const uint32_t step = (uint32_t)stride * sizeof(T);
 #pragma unroll
         for (int m = 0; m < kMine; ++m) {
-            const int unit = thread + m * kThreads;
-            if (kUnits % kThreads != 0 && unit >= kUnits) continue;
+            const int unit = (thread + m * kThreads) % kUnits;
             const int t = unit / (4 * kBlocks) * 4, c = unit % (4 * kBlocks) * 4;
             uint32_t at = c < size ? t * step + c * (uint32_t)sizeof(T) : kPastEnd;
 #pragma unroll
