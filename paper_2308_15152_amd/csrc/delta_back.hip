@@ -14,6 +14,8 @@
 // its two products; then the helpers put down the next ones.  In FP32, for whose
 // two parts LDS holds Q only once, the post is a second barrier (B), before which
 // the helpers have read the Q that they overwrite after it.
+#include <type_traits>
+
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
@@ -21,13 +23,15 @@ namespace sgemm_emu {
 namespace {
 
 // LDS, in bytes, and the number of helping waves.
+// kWalkers: groups of 16 columns, a pair of walking waves each.
 template <class T, int kK, int kWalkers>
 struct Layout {
-    static constexpr bool kPosts = sizeof(T) == 2;
+    static constexpr bool kPosts = sizeof(T) == 2 || kK == 64;  // as LDS allows
     // with eight helpers, four bring K and T^T and four Q, P^T and dO
     static constexpr int kHelpers = kPosts ? 8 : 4;
     static constexpr int kParts = kPartsOf<T>;
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
+    static constexpr int kHalf = kTiles / 2;  // row tiles of a wave of a pair
     static constexpr int kRows = kParts * 4 * kSteps * 1024;
     static constexpr int kMatrix = 2 * DeltaRecord::kMatrix;
     // two buffers of these
@@ -48,19 +52,23 @@ struct Layout {
     // the products, as the walking waves hold them: 4 tiles and kTiles tiles
     static constexpr int kAtProducts = kAtQs + (kPosts ? 2 : 1) * kBufferQ;
     static constexpr int kEach = (4 + kTiles) * 1024;
-    static constexpr int kAtPosts = kAtProducts + kWalkers * kEach;
+    // what the waves of a pair give each other
+    static constexpr int kAtX = kAtProducts + kWalkers * kEach;
+    static constexpr int kEachX = 4 * 1024 + 64;
+    // steps done: [wave] products taken; [2 kWalkers + wave] given to the other
+    static constexpr int kAtPosts = kAtX + kWalkers * kEachX;
     static constexpr int kBytes = kAtPosts + 16 * kWalkers;
 };
 
 // kCarry: only D before every part, from zero after it; kWide: as in delta_chain.hip.
 template <class T, int kK, int kWalkers, bool kCarry, bool kWide>
-__global__ __launch_bounds__(64 * (kWalkers + Layout<T, kK, kWalkers>::kHelpers), 1)
+__global__ __launch_bounds__(64 * (2 * kWalkers + Layout<T, kK, kWalkers>::kHelpers), 1)
 void delta_back_kernel(DeltaChunks p) {
     using L = Layout<T, kK, kWalkers>;
     constexpr bool kPosts = L::kPosts;
     constexpr int kHelpers = L::kHelpers;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);  // one each 4 ints: steps posted
+    int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -82,13 +90,16 @@ void delta_back_kernel(DeltaChunks p) {
     const char* records = p.records + ((int64_t)first_chunk * p.v_heads + h) * p.record_bytes;
     const int64_t record_step = (int64_t)p.v_heads * p.record_bytes;
     const int64_t skip = (int64_t)walk.first * kC;  // tokens of the parts before
-    if (kPosts && threadIdx.x < kWalkers) posts[4 * threadIdx.x] = 0;
+    if (threadIdx.x < 4 * kWalkers) posts[threadIdx.x] = 0;
 
     // Steps s = 0, 1, ... are chunks from the last to the first.
-    if (wave < kWalkers) {
-        const int col = col0 + 16 * wave + (lane & 15);
+    if (wave < 2 * kWalkers) {
+        const int group = wave >> 1, half = wave & 1;
+        const bool leads = half == 0;
+        const int row0 = half * 16 * L::kHalf;
+        const int col = col0 + 16 * group + (lane & 15);
         const bool in = col < p.v_size;
-        f32x4 D[L::kTiles];  // rows 16 i + 4 g + r
+        f32x4 D[L::kHalf];  // rows row0 + 16 i + 4 g + r
         const int64_t sequence = ((int64_t)n * p.v_heads + h) * p.k_size * p.v_size;
         const int64_t part = ((int64_t)index * p.v_heads + h) * p.k_size * p.v_size;
         const float* from = kCarry              ? nullptr
@@ -96,17 +107,20 @@ void delta_back_kernel(DeltaChunks p) {
                             : p.dfinal          ? p.dfinal + sequence
                                                 : nullptr;
 #pragma unroll
-        for (int i = 0; i < L::kTiles; ++i)
+        for (int i = 0; i < L::kHalf; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int row = 16 * i + 4 * g + r;
+                const int row = row0 + 16 * i + 4 * g + r;
                 D[i][r] = from && in && row < p.k_size ? from[(int64_t)row * p.v_size + col] : 0.0f;
             }
-        const char* products = lds + L::kAtProducts + wave * L::kEach + lane * 16;
+        const char* products = lds + L::kAtProducts + group * L::kEach + lane * 16;
+        char* x_at = lds + L::kAtX + group * L::kEachX;
+        int* given = posts + 2 * kWalkers;
         T* dv = row_of<T>(p.dv, packed, n, span, h) + skip * p.dv.token;
         const uint32_t v_step = (uint32_t)p.dv.token * sizeof(T);
         const uint32_t v_at = in ? 4 * g * v_step + col * (uint32_t)sizeof(T) : kPastEnd;
         const uint32_t f_at = in ? 4u * (4 * g * p.v_size + col) : kPastEnd;
+        const uint32_t d_at = in ? 4u * ((row0 + 4 * g) * p.v_size + col) : kPastEnd;
         if (chunks > 0) {
             lds_barrier();
             lds_barrier();
@@ -122,15 +136,17 @@ void delta_back_kernel(DeltaChunks p) {
             const int count = min(kC, span.count - c * kC);
             const int64_t task = (int64_t)(first_chunk + c) * p.v_heads + h;
             lds_barrier();  // A
-            f32x4 u[4], add[L::kTiles];
+            f32x4 u[4], add[L::kHalf];
+            if (leads)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(products + i * 1024);
+                for (int i = 0; i < 4; ++i)
+                    u[i] = *reinterpret_cast<const f32x4*>(products + i * 1024);
 #pragma unroll
-            for (int i = 0; i < L::kTiles; ++i)
-                add[i] = *reinterpret_cast<const f32x4*>(products + (4 + i) * 1024);
+            for (int i = 0; i < L::kHalf; ++i)
+                add[i] = *reinterpret_cast<const f32x4*>(products + (4 + half * L::kHalf + i) * 1024);
             if (kPosts) {
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-                __hip_atomic_store(posts + 4 * wave, s + 1, __ATOMIC_RELAXED,
+                __hip_atomic_store(posts + wave, s + 1, __ATOMIC_RELAXED,
                                    __HIP_MEMORY_SCOPE_WORKGROUP);
             } else {
                 lds_barrier();  // B
@@ -139,75 +155,112 @@ void delta_back_kernel(DeltaChunks p) {
                 const __amdgpu_buffer_rsrc_t to =
                     buffer_at(p.dstates + task * ((p.k_size + 15) / 16 * 16) * p.v_size);
 #pragma unroll
-                for (int i = 0; i < L::kTiles; ++i)
-                    if (16 * i < p.k_size)
+                for (int i = 0; i < L::kHalf; ++i)
+                    if (row0 + 16 * i < p.k_size)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             __builtin_amdgcn_raw_buffer_store_b32(
-                                __builtin_bit_cast(uint32_t, (float)D[i][r]), to, f_at,
+                                __builtin_bit_cast(uint32_t, (float)D[i][r]), to, d_at,
                                 4 * (16 * i + r) * p.v_size, 0);
             }
             // dU
-            {
-                const Scale ds = scale_of(max_groups(largest(D)));
-                f32x4 a[4] = {};
+            Frag<2> b[2];
+            float down;
+            f32x4 a[4] = {};
+            const Scale ds = scale_of(max_groups(largest(D)));
 #pragma unroll
-                for (int j = 0; j < L::kSteps; ++j) {
-                    const Frag<2> b = split<2>(D[2 * j], D[2 * j + 1], ds.up);
+            for (int j = 0; j < L::kSteps / 2; ++j) {
+                const Frag<2> db = split<2>(D[2 * j], D[2 * j + 1], ds.up);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    a[i] = multiply(row_fragment<T, kK>(at + L::kAtK, i, half * (L::kSteps / 2) + j,
+                                                        lane), db, a[i]);
+            }
+            if (!leads) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(x_at + i * 1024 + lane * 16) = a[i] * ds.down;
+                give(given + wave, s + 1);
+                wait_given(given + wave - 1, s + 1);
+                take(given + wave - 1, s + 1, [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            b[j].part[q] = *reinterpret_cast<const half8_t*>(
+                                x_at + (2 * j + q) * 1024 + lane * 16);
+                    down = reinterpret_cast<const float*>(x_at + 4096)[lane & 15];
+                });
+            } else {
+                f32x4 other[4];
+                take(given + wave + 1, s + 1, [&]() __attribute__((always_inline)) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        a[i] = multiply(row_fragment<T, kK>(at + L::kAtK, i, j, lane), b, a[i]);
-                }
+                        other[i] = *reinterpret_cast<const f32x4*>(x_at + i * 1024 + lane * 16);
+                });
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f32x4 tail = factor(DeltaRecord::kTail, i) * ds.down;
+                    const f32x4 tail = factor(DeltaRecord::kTail, i);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) u[i][r] = __builtin_fmaf(tail[r], a[i][r], u[i][r]);
+                    for (int r = 0; r < 4; ++r)
+                        u[i][r] = __builtin_fmaf(
+                            tail[r], __builtin_fmaf(a[i][r], ds.down, other[i][r]), u[i][r]);
                 }
-            }
-            // dY, and dV
-            f32x4 y[4] = {};
-            {
-                const Scale us = scale_of(max_groups(largest(u)));
-                const Frag<2> b[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
-                const __amdgpu_buffer_rsrc_t dy = buffer_at(p.dsides + task * kC * p.v_size);
-                const __amdgpu_buffer_rsrc_t to = buffer_at(dv + (int64_t)c * kC * p.dv.token);
+                // dY, and dV
+                f32x4 y[4] = {};
+                {
+                    const Scale us = scale_of(max_groups(largest(u)));
+                    const Frag<2> ub[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
+                    const __amdgpu_buffer_rsrc_t dy = buffer_at(p.dsides + task * kC * p.v_size);
+                    const __amdgpu_buffer_rsrc_t to = buffer_at(dv + (int64_t)c * kC * p.dv.token);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                    for (int j = i / 2; j < 2; ++j)
-                        y[i] = multiply(matrix_fragment<2>(at + L::kAtTt, upper_at(i, j), lane), b[j],
-                                        y[i]);
-                    y[i] *= factor(DeltaRecord::kTt, i) * us.down;
-                    const f32x4 beta = factor(DeltaRecord::kBeta, i);
+                        for (int j = i / 2; j < 2; ++j)
+                            y[i] = multiply(matrix_fragment<2>(at + L::kAtTt, upper_at(i, j), lane), ub[j],
+                                            y[i]);
+                        y[i] *= factor(DeltaRecord::kTt, i) * us.down;
+                        const f32x4 beta = factor(DeltaRecord::kBeta, i);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (!kCarry)
-                            __builtin_amdgcn_raw_buffer_store_b32(
-                                __builtin_bit_cast(uint32_t, (float)y[i][r]), dy, f_at,
-                                4 * (16 * i + r) * p.v_size, 0);
-                        y[i][r] *= beta[r];
-                        if (kCarry) continue;
-                        store_word(from_f32<T>(y[i][r]), to,
-                                   count == kC || 16 * i + 4 * g + r < count
-                                       ? v_at + (16 * i + r) * v_step : kPastEnd);
+                        for (int r = 0; r < 4; ++r) {
+                            if (!kCarry)
+                                __builtin_amdgcn_raw_buffer_store_b32(
+                                    __builtin_bit_cast(uint32_t, (float)y[i][r]), dy, f_at,
+                                    4 * (16 * i + r) * p.v_size, 0);
+                            y[i][r] *= beta[r];
+                            if (kCarry) continue;
+                            store_word(from_f32<T>(y[i][r]), to,
+                                       count == kC || 16 * i + 4 * g + r < count
+                                           ? v_at + (16 * i + r) * v_step : kPastEnd);
+                        }
+                        y[i] *= -factor(DeltaRecord::kRise, i);
                     }
-                    y[i] *= -factor(DeltaRecord::kRise, i);
                 }
+                const Scale ys = scale_of(max_groups(largest(y)));
+                b[0] = split<2>(y[0], y[1], ys.up);
+                b[1] = split<2>(y[2], y[3], ys.up);
+                down = ys.down;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        *reinterpret_cast<half8_t*>(x_at + (2 * j + q) * 1024 + lane * 16) =
+                            b[j].part[q];
+                reinterpret_cast<float*>(x_at + 4096)[lane & 15] = down;
+                give(given + wave, s + 1);
             }
             // D
-            const Scale ys = scale_of(max_groups(largest(y)));
-            const Frag<2> b[2] = {split<2>(y[0], y[1], ys.up), split<2>(y[2], y[3], ys.up)};
             const float decay = f[64 * DeltaRecord::kDecay];
 #pragma unroll
-            for (int i = 0; i < L::kTiles; ++i) {
+            for (int i = 0; i < L::kHalf; ++i) {
                 f32x4 a{};
 #pragma unroll
                 for (int j = 0; j < 2; ++j)  // lo.lo too: as for S
-                    a = multiply<true>(column_fragment<T, kK>(at + L::kAtK, i, j, lane), b[j], a);
+                    a = multiply<true>(
+                        column_fragment<T, kK>(at + L::kAtK, half * L::kHalf + i, j, lane), b[j], a);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    D[i][r] = __builtin_fmaf(a[r], ys.down,
+                    D[i][r] = __builtin_fmaf(a[r], down,
                                              __builtin_fmaf(decay, D[i][r], add[i][r]));
             }
         }
@@ -216,10 +269,10 @@ void delta_back_kernel(DeltaChunks p) {
                                                    : nullptr;
         if (to && in)
 #pragma unroll
-            for (int i = 0; i < L::kTiles; ++i)
+            for (int i = 0; i < L::kHalf; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * i + 4 * g + r;
+                    const int row = row0 + 16 * i + 4 * g + r;
                     if (row < p.k_size) to[(int64_t)row * p.v_size + col] = D[i][r];
                 }
         return;
@@ -227,9 +280,8 @@ void delta_back_kernel(DeltaChunks p) {
 
     // ---- the helping waves
     if (chunks == 0) return;
-    const int helper = wave - kWalkers;
-    const bool brings_k = helper < 4, brings_q = helper >= kHelpers - 4;
-    const int id = (threadIdx.x - 64 * kWalkers) & 255;
+    const int helper = wave - 2 * kWalkers, last = chunks - 1;
+    const int id = (threadIdx.x - 128 * kWalkers) & 255;
     const T* k = row_of<const T>(p.k, packed, n, span, kh) + skip * p.k.token;
     const T* q = row_of<const T>(p.q, packed, n, span, kh) + skip * p.q.token;
     const T* d_o = row_of<const T>(p.d_o, packed, n, span, h) + skip * p.d_o.token + col0;
@@ -330,48 +382,58 @@ void delta_back_kernel(DeltaChunks p) {
             *reinterpret_cast<f32x4*>(to + (4 + part * kOwnK + i) * 1024) = qd[i];
     };
 
-    if (brings_k) {
-        load_k(0);
-        store_k(0);
-        if (chunks > 1) load_k(1);
-    }
-    if (brings_q) {
-        load_q(0);
-        store_q(0);
-        if (chunks > 1) load_q(1);
-    }
-    lds_barrier();
-    make(0);
-    lds_barrier();
-    put();
-    if (brings_q && chunks > 1) {
-        store_q(1);
-        if (chunks > 2) load_q(2);
-    }
-    for (int s = 0; s < chunks; ++s) {
-        lds_barrier();  // A
-        if (s + 1 < chunks) make(s + 1);
-        if (kPosts) {
-            // every walking wave is in this step and posts on its way
+    // Loads are a step ahead of the stores and without conditions, as in delta_chain.hip.
+    const auto run = [&](auto brings_k, auto brings_q) __attribute__((always_inline)) {
+        if (brings_k) {
+            load_k(0);
+            store_k(0);
+            load_k(min(1, last));
+        }
+        if (brings_q) {
+            load_q(0);
+            store_q(0);
+            load_q(min(1, last));
+        }
+        lds_barrier();
+        make(0);
+        lds_barrier();
+        put();
+        if (brings_q) {
+            store_q(1);
+            load_q(min(2, last));
+        }
+        for (int s = 0; s < chunks; ++s) {
+            lds_barrier();  // A
+            if (brings_k) {
+                store_k(s + 1);
+                load_k(min(s + 2, last));
+            }
+            if (kPosts && brings_q) {
+                store_q(s + 2);
+                load_q(min(s + 3, last));
+            }
+            make(s + 1);
+            if (kPosts) {
+                // every walking wave is in this step and posts on its way
 #pragma unroll
-            for (int w = 0; w < kWalkers; ++w)
-                while (__hip_atomic_load(posts + 4 * w, __ATOMIC_RELAXED,
-                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= s)
-                    __builtin_amdgcn_s_sleep(1);
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-        } else {
-            lds_barrier();  // B
+                for (int w = 0; w < 2 * kWalkers; ++w) wait_given(posts + w, s + 1);
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+            } else {
+                lds_barrier();  // B
+            }
+            put();
+            if (!kPosts && brings_q) {
+                store_q(s + 2);
+                load_q(min(s + 3, last));
+            }
         }
-        if (s + 1 < chunks) put();
-        if (brings_k && s + 1 < chunks) {
-            store_k(s + 1);
-            if (s + 2 < chunks) load_k(s + 2);
-        }
-        if (brings_q && s + 2 < chunks) {
-            store_q(s + 2);
-            if (s + 3 < chunks) load_q(s + 3);
-        }
-    }
+    };
+    if constexpr (kHelpers == 4)
+        run(std::true_type{}, std::true_type{});
+    else if (helper < 4)
+        run(std::true_type{}, std::false_type{});
+    else
+        run(std::false_type{}, std::true_type{});
 }
 
 template <class T, int kK, int kWalkers, bool kCarry, bool kWide>
@@ -387,7 +449,7 @@ hipError_t launch_rows(const DeltaChunks& a, hipStream_t stream) {
         return e;
     hipLaunchKernelGGL((delta_back_kernel<T, kK, kWalkers, kCarry, kWide>),
                        dim3((unsigned)walk_blocks(walks * a.v_heads, slices)),
-                       dim3(64 * (kWalkers + L::kHelpers)), L::kBytes, stream, a);
+                       dim3(64 * (2 * kWalkers + L::kHelpers)), L::kBytes, stream, a);
     return hipGetLastError();
 }
 

@@ -77,24 +77,6 @@ struct Layout {
     static constexpr int kBytes = kAtPosts + 16 * kWalkers;
 };
 
-// Gives what was written to LDS before, by flag, to the other wave of a pair.  A wave's
-// LDS accesses are carried out in order, so neither side has to wait for its own.
-__device__ inline void give(int* flag, int n) {
-    asm volatile("" ::: "memory");
-    __hip_atomic_store(flag, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-}
-// Reads behind a flag, until they came after its n-th rise.
-template <class F>
-__device__ inline void take(const int* flag, int n, F&& read) {
-    int given;
-    do {
-        given = __hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        asm volatile("" ::: "memory");
-        read();
-        asm volatile("" ::: "memory");
-    } while (__builtin_amdgcn_readfirstlane(given) < n);
-}
-
 // kWide: all rows can be loaded 16 bytes at a time (8 of V's).  (Decided here, not where
 // they are loaded: loads of two kinds into the same registers would be waited for
 // as if both were under way.)
@@ -231,9 +213,7 @@ void delta_chain_kernel(DeltaChunks p) {
                 for (int i = 0; i < 4; ++i)
                     *reinterpret_cast<f32x4*>(x_at + i * 1024 + lane * 16) = x[i] * ss.down;
                 give(given + wave, c + 1);
-                while (__hip_atomic_load(given + wave - 1, __ATOMIC_RELAXED,
-                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= c)
-                    __builtin_amdgcn_s_sleep(1);
+                wait_given(given + wave - 1, c + 1);
                 take(given + wave - 1, c + 1, [&]() __attribute__((always_inline)) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
@@ -360,10 +340,7 @@ void delta_chain_kernel(DeltaChunks p) {
     const auto wait_posts = [&](int c) __attribute__((always_inline)) {
         if (kPosts) {
 #pragma unroll
-            for (int w = 0; w < 2 * kWalkers; ++w)
-                while (__hip_atomic_load(posts + w, __ATOMIC_RELAXED,
-                                         __HIP_MEMORY_SCOPE_WORKGROUP) <= c)
-                    __builtin_amdgcn_s_sleep(1);
+            for (int w = 0; w < 2 * kWalkers; ++w) wait_given(posts + w, c + 1);
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
         } else {
             lds_barrier();  // B

@@ -493,6 +493,30 @@ __device__ inline Frag<N> matrix_fragment(const char* matrix, int at, int lane) 
     return f;
 }
 
+// Gives what was written to LDS before, by flag, to the other wave of a pair.  A wave's
+// LDS accesses are carried out in order, so neither side has to wait for its own.
+__device__ inline void give(int* flag, int n) {
+    asm volatile("" ::: "memory");
+    __hip_atomic_store(flag, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+// Reads behind a flag, until they came after its n-th rise.
+template <class F>
+__device__ inline void take(const int* flag, int n, F&& read) {
+    int given;
+    do {
+        given = __hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        asm volatile("" ::: "memory");
+        read();
+        asm volatile("" ::: "memory");
+    } while (__builtin_amdgcn_readfirstlane(given) < n);
+}
+
+// Until a flag is at n.
+__device__ inline void wait_given(const int* flag, int n) {
+    while (__hip_atomic_load(flag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < n)
+        __builtin_amdgcn_s_sleep(1);
+}
+
 // A piece of a record on its way to LDS, 16 bytes a thread and turn.  (Here and below,
 // threads without a part of their own load one all the same: which loads are
 // under way is then the same on every path, and a wait waits for no later ones.)
