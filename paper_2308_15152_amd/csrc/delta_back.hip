@@ -28,7 +28,7 @@ template <class T, int kK, int kWalkers>
 struct Layout {
     static constexpr bool kPosts = sizeof(T) == 2 || kK == 64;  // as LDS allows
     // with eight helpers, four bring K and T^T and four Q, P^T and dO
-    static constexpr int kHelpers = kPosts ? 8 : 4;
+    static constexpr int kHelpers = kPosts && kWalkers > 1 ? 8 : 4;
     static constexpr int kParts = kPartsOf<T>;
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
     static constexpr int kHalf = kTiles / 2;  // row tiles of a wave of a pair
@@ -465,6 +465,13 @@ hipError_t launch_delta_chain_back(const DeltaChunks& a, DeltaWalk walk, hipStre
     return by_dtype(a.dtype, [&](auto t) {
         using T = decltype(t);
         constexpr int kLarge = sizeof(T) == 4 ? 1 : 2;  // walking waves, keys above 64
+        if (narrow(a)) {
+            if (walk == kDeltaParts)
+                return a.k_size <= 64 ? launch<T, 64, 1, true>(a, stream)
+                                      : launch<T, 128, 1, true>(a, stream);
+            return a.k_size <= 64 ? launch<T, 64, 1, false>(a, stream)
+                                  : launch<T, 128, 1, false>(a, stream);
+        }
         if (walk == kDeltaParts)
             return a.k_size <= 64 ? launch<T, 64, 2, true>(a, stream)
                                   : launch<T, 128, kLarge, true>(a, stream);

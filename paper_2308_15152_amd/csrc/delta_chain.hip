@@ -558,12 +558,18 @@ hipError_t launch_delta_chain(const DeltaChunks& a, DeltaWalk walk, hipStream_t 
         const bool small = a.k_size <= 64;
         switch (walk) {
             case kDeltaStates:
+                if (narrow(a))
+                    return small ? launch<T, 64, 1, kStates>(a, stream)
+                                 : launch<T, 128, 1, kStates>(a, stream);
                 return small ? launch<T, 64, 2, kStates>(a, stream)
                              : launch<T, 128, 2, kStates>(a, stream);
             case kDeltaParts:
                 return small ? launch<T, 64, 4, kPartSteps>(a, stream)
                              : launch<T, 128, kF32 ? 2 : 4, kPartSteps>(a, stream);
             default:
+                if (narrow(a))
+                    return small ? launch<T, 64, 1, kOutputs>(a, stream)
+                                 : launch<T, 128, 1, kOutputs>(a, stream);
                 return small ? launch<T, 64, 2, kOutputs>(a, stream)
                              : launch<T, 128, kF32 ? 1 : 2, kOutputs>(a, stream);
         }

@@ -226,6 +226,13 @@ __device__ inline WalkTask walk_task(int slices) {
     const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
     return {i / slices * 8 + xcd, i % slices};
 }
+// Whether a walk takes 16 columns a block rather than 32: where those leave half of
+// the CUs idle (the walk back of 32 heads of 128 x 128: 128 blocks 226 us, 256
+// blocks 207; with more heads than that K and Q would be brought twice as often for nothing).
+inline bool narrow(const DeltaChunks& a) {
+    const int64_t walks = a.part_chunks > 0 ? a.parts : a.batch;
+    return walks * a.v_heads * ((a.v_size + 31) / 32) <= 128;
+}
 inline int64_t walk_blocks(int64_t tasks, int64_t slices) { return (tasks + 7) / 8 * 8 * slices; }
 
 // Chunk c of a call: its sequence, the chunk's number in it, first row and
