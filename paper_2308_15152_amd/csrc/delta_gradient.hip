@@ -174,7 +174,9 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
     T* dqo = row_of<T>(p.dq, packed, at.n, at.span, kh) + (int64_t)at.first * p.dq.token;
     T* dko = row_of<T>(p.dk, packed, at.n, at.span, kh) + (int64_t)at.first * p.dk.token;
     const auto put_rows = [&](int i, f32x4 x, f32x4 y) __attribute__((always_inline)) {
-        const int lane = threadIdx.x & 63;
+        // (Addresses made here: from scratch, each would wait for the store before it.)
+        int lane = threadIdx.x & 63;
+        __asm__ volatile("" : "+v"(lane));
         const int e = 16 * tile + (lane & 15);
         const __amdgpu_buffer_rsrc_t to_q = buffer_at(dqo), to_k = buffer_at(dko);
 #pragma unroll
