@@ -38,7 +38,7 @@ struct Layout {
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
     static constexpr int kColumns = kParts * 4 * kSteps * 1024;  // K^T or Q^T
     // columns of V taken at a time, in steps of 32
-    static constexpr int kVSteps = sizeof(T) == 4 ? 2 : 4;
+    static constexpr int kVSteps = 2;
     static constexpr int kPart = 4 * kVSteps * 1024;  // one part of dO, dY or U
     static constexpr int kAtKt = 0;
     static constexpr int kAtQt = kAtKt + kColumns;
