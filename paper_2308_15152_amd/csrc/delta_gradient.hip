@@ -37,7 +37,8 @@ struct Layout {
     static constexpr int kParts = kPartsOf<T>;
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
     static constexpr int kColumns = kParts * 4 * kSteps * 1024;  // K^T or Q^T
-    // columns of V taken at a time, in steps of 32
+    // columns of V taken at a time, in steps of 32 (with four steps the registers do
+    // not hold them, at 128 x 128: 307 us against 268 for 2 x 4096 tokens of 16 heads)
     static constexpr int kVSteps = 2;
     static constexpr int kPart = 4 * kVSteps * 1024;  // one part of dO, dY or U
     static constexpr int kAtKt = 0;
@@ -142,15 +143,12 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = lane & 15;
     const int kh = blockIdx.x % p.k_heads, c = blockIdx.x / p.k_heads;
     const Place at = place_of(p.cu_seqlens, c, p.batch, p.tokens);
     if (at.count <= 0) return;  // the whole block
     const bool packed = p.cu_seqlens != nullptr;
     const int group = p.v_heads / p.k_heads;
     const int tile = wave % L::kTiles, own = wave / L::kTiles * kOwn;
-    const int ke = 16 * tile + row;  // this lane's element of the key
-    const bool kin = ke < p.k_size;
 
     // K^T and Q^T, and this lane's elements of K and Q
     const T* k = row_of<const T>(p.k, packed, at.n, at.span, kh) + (int64_t)at.first * p.k.token;
@@ -215,34 +213,47 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
 
         f32x4 e1[kOwn] = {}, e2[kOwn] = {}, e3[kOwn] = {}, m[4] = {};
         float sd = 0.0f;
+        // A block's rows: this wave's of S and D, to be B operands (columns: key
+        // elements), and 16 of dO and U (waves 0 to 3) or of dY and V (4 to 7).  With keys
+        // of up to 64 they are loaded while the block before is multiplied (3 x 1001
+        // tokens of 6 heads, 64 x 96, in float32: 71 us without, 67 with); with 128 there
+        // are no registers for that (2 x 4096 tokens: 268 us without, 333 with).
+        constexpr bool kAhead = kK == 64;
+        Eight<float> sx[kVSteps], dx[kVSteps], fx[kVSteps];
+        Eight<T> tx[kVSteps];
+        const auto load_state = [&](const float* from, Eight<float>(&x)[kVSteps], int v0, int lane)
+                                    __attribute__((always_inline)) {
+            const int ke = 16 * tile + (lane & 15);
+#pragma unroll
+            for (int j = 0; j < kVSteps; ++j)
+                x[j] = load_eight<float>(buffer_at(from), 4u * ke * p.v_size,
+                                         v0 + 32 * j + 8 * (lane >> 4), p.v_size, ke < p.k_size, kWide);
+        };
+        const auto load_rows = [&](int v0, int lane) __attribute__((always_inline)) {
+            const int t = 16 * (wave % 4) + (lane & 15);
+            const uint32_t at_t = t * (uint32_t)(wave < 4 ? p.d_o.token : p.v.token) *
+                                  (uint32_t)sizeof(T);
+            const __amdgpu_buffer_rsrc_t rt = buffer_at(wave < 4 ? d_o : v),
+                                         rf = buffer_at(wave < 4 ? u : dy);
+#pragma unroll
+            for (int j = 0; j < kVSteps; ++j) {
+                const int e = v0 + 32 * j + 8 * (lane >> 4);
+                tx[j] = load_eight<T>(rt, at_t, e, p.v_size, t < at.count, kWide);
+                fx[j] = load_eight<float>(rf, 4u * t * p.v_size, e, p.v_size, true, kWide);
+            }
+        };
+        const auto load_all = [&](int v0, int lane) __attribute__((always_inline)) {
+            load_state(S, sx, v0, lane);
+            load_rows(v0, lane);
+            load_state(D, dx, v0, lane);
+        };
+        if (kAhead) load_all(0, lane);
         for (int v0 = 0; v0 < p.v_size; v0 += kVBlock) {
             __asm__ volatile("" : "+v"(lane));
             const int row = lane & 15, g = lane >> 4;
-            __syncthreads();  // the last block's fragments are used
-            // this wave's rows of S and D, to be B operands (columns: key elements)
-            Eight<float> sx[kVSteps], dx[kVSteps];
-#pragma unroll
-            for (int j = 0; j < kVSteps; ++j) {
-                const int e = v0 + 32 * j + 8 * g;
-                sx[j] = load_eight<float>(buffer_at(S), 4u * ke * p.v_size, e, p.v_size, kin, kWide);
-                dx[j] = load_eight<float>(buffer_at(D), 4u * ke * p.v_size, e, p.v_size, kin, kWide);
-            }
-            // 16 rows of dO and U (waves 0 to 3) or of dY and V (4 to 7)
+            lds_barrier();  // the last block's fragments are used
+            if (!kAhead) load_all(v0, lane);
             const int t = 16 * (wave % 4) + row;
-            Eight<T> tx[kVSteps];
-            Eight<float> fx[kVSteps];
-            {
-                const T* from = wave < 4 ? d_o : v;
-                const uint32_t at_t = t * (uint32_t)(wave < 4 ? p.d_o.token : p.v.token) *
-                                      (uint32_t)sizeof(T);
-                const __amdgpu_buffer_rsrc_t rt = buffer_at(from), rf = buffer_at(wave < 4 ? u : dy);
-#pragma unroll
-                for (int j = 0; j < kVSteps; ++j) {
-                    const int e = v0 + 32 * j + 8 * g;
-                    tx[j] = load_eight<T>(rt, at_t, e, p.v_size, t < at.count, kWide);
-                    fx[j] = load_eight<float>(rf, 4u * t * p.v_size, e, p.v_size, true, kWide);
-                }
-            }
             const auto put = [&](auto parts, const auto (&x)[kVSteps], char* to, float* down) __attribute__((always_inline)) {
                 constexpr int kN = decltype(parts)::value;
                 float top = 0.0f;
@@ -293,7 +304,11 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             Frag<2> sb[kVSteps];
 #pragma unroll
             for (int j = 0; j < kVSteps; ++j) sb[j] = split<2>(sx[j].x, ss.up);
-            __syncthreads();
+            lds_barrier();
+            if (kAhead) {  // (zero, and not loaded, after the last block)
+                load_state(S, sx, v0 + kVBlock, lane);
+                load_rows(v0 + kVBlock, lane);
+            }
             const auto fragment = [&](auto parts, int from, int i, int j) __attribute__((always_inline)) {
                 constexpr int kN = decltype(parts)::value;
                 Frag<kN> f;
@@ -321,6 +336,7 @@ __global__ __launch_bounds__(kThreads, 1) void delta_gradient_kernel(DeltaChunks
             }
 #pragma unroll
             for (int j = 0; j < kVSteps; ++j) sb[j] = split<2>(dx[j].x, ds.up);
+            if (kAhead) load_state(D, dx, v0 + kVBlock, lane);
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
                 f32x4 a3{};
