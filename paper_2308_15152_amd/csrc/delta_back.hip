@@ -3,12 +3,14 @@
 //   dU = P^T dO + diag(e^{G_64 - G}) K D,   dY = T^T dU,   dV = diag(beta) dY,
 //   D before = e^{G_64} D + scale (diag(e^G) Q)^T dO - (diag(e^G) K)^T dV.
 // Columns are independent here too, and the work is shared out as on the way
-// forward (delta_chain.hip): walking waves carry 16 columns of D each and
+// forward (delta_chain.hip): pairs of walking waves carry 16 columns of D and
 // do what waits for D; helping waves bring K and T^T of the next chunk, and make
 // what does not wait, P^T dO and the product with Q, a chunk ahead from Q, P^T and dO,
 // which they bring two chunks ahead.  Leaves D after and dY of every chunk.  A
 // sequence cut into parts is walked twice, as on the way forward: every part
 // but the first from D = 0, then all from their own (M^T takes D across a part).
+// Measured: 2 x 4096 tokens of 16 heads (bfloat16, 128 x 128) 207 us, 3.2 us a chunk,
+// bound by the chain like the walk forward.
 //
 // One barrier a chunk (A).  Inside a chunk a walking wave posts when it has taken
 // its two products; then the helpers put down the next ones.  In FP32, for whose
@@ -314,7 +316,9 @@ void delta_back_kernel(DeltaChunks p) {
         vu.load(d_o + (int64_t)c * kC * p.d_o.token, p.d_o.token, count, p.v_size - col0,
                 kWide, id);
     };
-    const auto buffer_q = [&](int s) __attribute__((always_inline)) { return lds + L::kAtQs + (kPosts ? (s & 1) * L::kBufferQ : 0); };
+    const auto buffer_q = [&](int s) __attribute__((always_inline)) {
+        return lds + L::kAtQs + (kPosts ? (s & 1) * L::kBufferQ : 0);
+    };
     const auto store_q = [&](int s) __attribute__((always_inline)) {
         char* to = buffer_q(s);
         qu.store(to + L::kAtQ, id);

@@ -5,8 +5,8 @@
 // A block takes 32 columns of one head of one sequence, a wave 16 of them, which
 // stay in its registers from part to part.  M is split once per block into
 // fragments in LDS; the next part's M and N are loaded meanwhile.  Bound by that
-// loop's latency: a part's M is 64 KiB, and the parts follow one another.  (With 128
-// columns to a block, a fourth of the CUs, a part takes 15 us for 8 heads.)
+// loop's latency: a part's M is 64 KiB, and the parts follow one another: 6.3 us a part
+// for 8 heads.  (With 128 columns to a block, a fourth of the CUs, a part takes 15 us.)
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
@@ -34,8 +34,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void delta_join_kernel(DeltaChunks 
     const int rows = (p.k_size + 15) / 16 * 16;
     const int col = (slice * kWaves + wave) * 16 + row;
     const bool in = col < p.v_size;
-    const auto part_at = [&](int j) __attribute__((always_inline)) { return ((int64_t)(first + j) * p.v_heads + h); };
-    const auto of = [&](int step) __attribute__((always_inline)) { return kBack ? parts - 1 - step : step; };  // part of a step
+    const auto part_at = [&](int j) __attribute__((always_inline)) {
+        return ((int64_t)(first + j) * p.v_heads + h);
+    };
+    const auto of = [&](int step) __attribute__((always_inline)) {  // part of a step
+        return kBack ? parts - 1 - step : step;
+    };
 
     // this wave's rows of M, in operand order: kOwn tiles of 16 rows
     constexpr int kOwn = kTiles / kWaves;
@@ -66,7 +70,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void delta_join_kernel(DeltaChunks 
         const int e = 16 * i + 4 * g + r;
         return in && (16 * i + 16 <= p.k_size || e < p.k_size) ? 4u * (e * p.v_size + col) : kPastEnd;
     };
-    const auto load_state = [&](const float* from, f32x4(&to)[kTiles]) __attribute__((always_inline)) {
+    const auto load_state = [&](const float* from, f32x4(&to)[kTiles])
+        __attribute__((always_inline)) {
         const __amdgpu_buffer_rsrc_t r = buffer_at(from);
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
@@ -83,7 +88,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void delta_join_kernel(DeltaChunks 
         for (int i = 0; i < kTiles; ++i) S[i] = f32x4{};
     float* states = kBack ? p.part_dstates : p.part_states;
     f32x4 next[kTiles];  // N of the step
-    const auto load_n = [&](int j) __attribute__((always_inline)) { load_state(states + part_at(j) * state, next); };
+    const auto load_n = [&](int j) __attribute__((always_inline)) {
+        load_state(states + part_at(j) * state, next);
+    };
     if (parts > 1) {
         load(of(0));
         load_n(of(0));

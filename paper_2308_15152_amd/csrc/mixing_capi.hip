@@ -234,7 +234,9 @@ int delta_emu_step(const delta_emu_step_t* args, hipStream_t stream) {
     const Tensor g{a.g, a.batch, a.tokens, a.v_heads, 1, 4};
     const Tensor beta{a.beta, a.batch, a.tokens, a.v_heads, 1, 4};
     const Tensor o{a.o, a.batch, a.tokens, a.v_heads, a.v_size, e};
-    const Extent state = array(a.state, a.n_slots == 0 ? 0 : ((__int128)(a.n_slots - 1) * a.state_stride + each) * 4);
+    const __int128 pool =
+        a.n_slots == 0 ? 0 : ((__int128)(a.n_slots - 1) * a.state_stride + each) * 4;
+    const Extent state = array(a.state, pool);
     const Extent slots = array(a.slots, (__int128)a.batch * 4);
     if (int rc = check_tensors({q, k, v, g, beta}, {o}, {slots}, {state})) return rc;
     DeltaStep s{};
@@ -274,7 +276,8 @@ int delta_emu_forward(const delta_emu_forward_t* args, hipStream_t stream) {
     if (need > 0 && (a.workspace_bytes < need || (uintptr_t)a.workspace % 256 != 0))
         return SGEMM_EMU_ERR_DIM;
     const Extent first = array(a.initial == a.final_state ? nullptr : a.initial, states);
-    if (int rc = check_tensors({q, k, v, g, beta}, {o}, {first, array(a.cu_seqlens, ((__int128)a.batch + 1) * 4)},
+    if (int rc = check_tensors({q, k, v, g, beta}, {o},
+                               {first, array(a.cu_seqlens, ((__int128)a.batch + 1) * 4)},
                                {array(a.final_state, states), array(a.workspace, need)}))
         return rc;
     return done(launch_delta_forward(a, stream));

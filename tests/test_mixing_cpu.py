@@ -143,7 +143,8 @@ def forward(query=False, cu=0, initial=8 * MB, final=9 * MB, ws=1 << 30, ws_byte
 
 SIZES = [
     (dict(dtype=7), UNSUPPORTED), (dict(batch=-1), DIM), (dict(tokens=-1), DIM),
-    (dict(v_size=-1), DIM), (dict(v_size=65537), UNSUPPORTED), (dict(k_size=0), UNSUPPORTED), (dict(k_size=129), UNSUPPORTED),
+    (dict(v_size=-1), DIM), (dict(v_size=65537), UNSUPPORTED), (dict(k_size=0), UNSUPPORTED),
+    (dict(k_size=129), UNSUPPORTED),
     (dict(k_heads=0), UNSUPPORTED), (dict(k_heads=3), UNSUPPORTED),
     (dict(batch=1 << 20, tokens=65), UNSUPPORTED),  # more than 2^22 (chunk, head) pairs
 ]
