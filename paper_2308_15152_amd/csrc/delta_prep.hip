@@ -59,13 +59,20 @@ __device__ inline void write_fragments(const float* M, int tile, int lane, char*
         for (int half = 0; half < 2; ++half) {
             const int other = 2 * step + half;
             const bool full = kTransposed ? other >= tile : other <= tile;
+            const int a = 16 * tile + row, b = 16 * other + 4 * g;
+            f32x4 v{};
+            if (full) {
+                if (kTransposed)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = M[(b + i) * kPitch + a];
+                else
+                    v = *reinterpret_cast<const f32x4*>(M + a * kPitch + b);
+                if (columns) v *= *reinterpret_cast<const f32x4*>(columns + b);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int a = 16 * tile + row, b = 16 * other + 4 * g + i;
-                float v = !full ? 0.0f : kTransposed ? M[b * kPitch + a] : M[a * kPitch + b];
-                if (columns) v *= columns[b];
-                x[step][4 * half + i] = v;
-                m = fmaxf(m, fabsf(v));
+                x[step][4 * half + i] = v[i];
+                m = fmaxf(m, fabsf(v[i]));
             }
         }
     const Scale s = scale_of(max_groups(m));
@@ -89,7 +96,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
     float *A = lds, *P = lds + kC * kPitch;
     static_assert(sizeof(Operand<T>) * 64 * 4 * kSteps <= sizeof(lds), "k's rows");
     __shared__ double G[kC];
-    __shared__ float beta[kC], key_down[kC];
+    __shared__ __attribute__((aligned(16))) float beta[kC], key_down[kC];
 
     const int h = blockIdx.x % p.v_heads, c = blockIdx.x / p.v_heads;
     const Place at = place_of(p.cu_seqlens, c, p.batch, p.tokens);

@@ -70,6 +70,14 @@ def _view(t, name, shape, dtype):
     return (t.data_ptr(), *st)
 
 
+def _like(t):
+    """A new contiguous tensor like t."""
+    torch = _pkg._torch
+    if t.is_contiguous():
+        return torch.empty_like(t)
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _sizes(q, k, v):
     """(batch, tokens, key heads, value heads, key size, value size)."""
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
@@ -138,8 +146,7 @@ def rotary_emu(q, k, cos, sin, *, positions=None, offset: int = 0, interleaved: 
     b, t, hq, size = q.shape
     dtype = q.dtype
     if out is None:
-        oq = torch.empty(q.shape, dtype=dtype, device=q.device)
-        ok = None if k is None else torch.empty(k.shape, dtype=dtype, device=q.device)
+        oq, ok = _like(q), None if k is None else _like(k)
     else:
         oq, ok = out
     xq, yq = _view(q, "q", q.shape, dtype), _view(oq, "out", q.shape, dtype)
