@@ -29,8 +29,9 @@ constexpr int kDeltaMaxK = 128;  // largest key size
 constexpr int kDeltaChunk = 64;  // tokens of a chunk
 constexpr int kDeltaMaxV = 1 << 16;
 constexpr int64_t kDeltaMostStride = 1 << 22;  // of tokens, in elements
-// Chunks x value heads of one call: one block each, one launch.
-constexpr int64_t kDeltaMostTasks = 1 << 22;
+// Chunks x value heads of one call: one block each, one launch.  (A walk's blocks, up to two
+// a chunk and head, have 768 threads, and a launch has less than 2^32.)
+constexpr int64_t kDeltaMostTasks = 1 << 21;
 
 // Chunks that the sequences of a call can have.  Packed sequences: sequence n's
 // are numbered from first row / 64 + n, which leaves at most one number

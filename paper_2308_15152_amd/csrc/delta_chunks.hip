@@ -24,14 +24,14 @@ Columns columns_of(int dtype, int k_size) {
 // and the parts cost a walk more, over k_size more columns, and the join.  The estimate
 // below uses measured times (us, 128 x 128 states in bfloat16; other sizes keep their
 // ratios): a chunk takes 2.2 (few blocks) to 2.9 (on all CUs) in the walk for outputs, 2.3
-// to 2.6 for states, 2.8 for N and M, 3.3 to 4.4 back; a part 6 to 8 in the join.  Walks
-// and joins: 32768 tokens of 8 heads 402 in 8 parts, 1120 not cut; 4096 tokens of 64 heads
-// 310 in two, 190 not cut; their gradient with 32 heads 447 in two, 358 not cut.
+// to 2.6 for states, 2.8 for N and M, 3.3 to 4.4 back; a part 3 in the join.  Walks
+// and joins: 32768 tokens of 8 heads 377 in 8 parts, 1120 not cut; 4096 tokens of 64 heads
+// 300 in two, 190 not cut; their gradient with 32 heads 430 in two, 358 not cut.
 template <class A>
 int part_chunks_of(const A& a, bool backward) {
     if (a.batch == 0 || a.tokens == 0 || a.v_size == 0) return 0;
     constexpr double kCus = 256, kOutputs = 2.6, kStates = 2.4, kSteps = 2.8, kBack = 3.8,
-                     kJoin = 7.0, kJoinStart = 5;
+                     kJoin = 3.0, kJoinStart = 3;
     const Columns c = columns_of(a.dtype, a.k_size);
     const auto blocks = [&](int64_t columns, int each) {  // of all sequences and heads
         return (double)((columns + each - 1) / each) * a.v_heads * a.batch;

@@ -146,7 +146,7 @@ SIZES = [
     (dict(v_size=-1), DIM), (dict(v_size=65537), UNSUPPORTED), (dict(k_size=0), UNSUPPORTED),
     (dict(k_size=129), UNSUPPORTED),
     (dict(k_heads=0), UNSUPPORTED), (dict(k_heads=3), UNSUPPORTED),
-    (dict(batch=1 << 20, tokens=65), UNSUPPORTED),  # more than 2^22 (chunk, head) pairs
+    (dict(batch=1 << 20, tokens=65), UNSUPPORTED),  # more than 2^21 (chunk, head) pairs
 ]
 
 
