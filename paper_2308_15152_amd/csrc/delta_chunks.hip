@@ -24,14 +24,15 @@ Columns columns_of(int dtype, int k_size) {
 // and the parts cost a walk more, over k_size more columns, and the join.  The estimate
 // below uses measured times (us, 128 x 128 states in bfloat16; other sizes keep their
 // ratios): a chunk takes 2.2 (few blocks) to 2.9 (on all CUs) in the walk for outputs, 2.3
-// to 2.6 for states, 2.8 for N and M, 3.3 to 4.4 back; a part 3 in the join.  Walks
-// and joins: 32768 tokens of 8 heads 377 in 8 parts, 1120 not cut; 4096 tokens of 64 heads
-// 300 in two, 190 not cut; their gradient with 32 heads 430 in two, 358 not cut.
+// to 2.6 for states, 2.8 for N and M, 3.3 to 4.4 back; a part 3 in the join, and each of
+// these launches 5.  Walks and joins: 32768 tokens of 8 heads 377 in 8 parts, 1120 not cut; 4096 tokens of 64 heads
+// 300 in two, 190 not cut; their gradient with 32 heads 430 in two, 358 not cut; 1001
+// tokens of 18 heads of 64 x 96 in float32 98 in three, 88 not cut.
 template <class A>
 int part_chunks_of(const A& a, bool backward) {
     if (a.batch == 0 || a.tokens == 0 || a.v_size == 0) return 0;
     constexpr double kCus = 256, kOutputs = 2.6, kStates = 2.4, kSteps = 2.8, kBack = 3.8,
-                     kJoin = 3.0, kJoinStart = 3;
+                     kJoin = 3.0, kStart = 5.0;
     const Columns c = columns_of(a.dtype, a.k_size);
     const auto blocks = [&](int64_t columns, int each) {  // of all sequences and heads
         return (double)((columns + each - 1) / each) * a.v_heads * a.batch;
@@ -48,6 +49,7 @@ int part_chunks_of(const A& a, bool backward) {
     for (int64_t parts = 1; parts <= 64 && parts <= chunks; ++parts) {
         const int64_t m = (chunks + parts - 1) / parts;
         const double p = (double)((chunks + m - 1) / m);
+        double launches = backward ? 2 : 1;  // of walks and joins
         double walk = backward ? rounds(p * blocks(a.v_size, c.states)) * kStates +
                                      rounds(p * blocks(a.v_size, c.back)) * kBack
                                : rounds(p * blocks(a.v_size, c.outputs)) * kOutputs;
@@ -55,9 +57,10 @@ int part_chunks_of(const A& a, bool backward) {
         if (parts > 1) {
             walk += rounds((backward ? p : p - 1) * steps) * kSteps;
             if (backward) walk += rounds((p - 1) * blocks(a.v_size, c.back)) * kBack;
-            time = (backward ? 2 : 1) * (kJoinStart + kJoin * p);
+            time = (backward ? 2 : 1) * kJoin * p;
+            launches *= 3;
         }
-        time += walk * m;
+        time += walk * m + kStart * launches;
         if (parts == 1) {
             best = 0.9 * time;  // worth the trouble
         } else if (time < best) {
