@@ -69,7 +69,7 @@ struct DeltaRecord {
     static constexpr int kFactorBytes = kFactors * 256;  // at the record's start
     static constexpr int kAtSums = kFactorBytes;         // G, 64 doubles
     static constexpr int kAtT = kAtSums + 512;           // two parts
-    static constexpr int kAtP = kAtT + 2 * kMatrix;      // two parts (one for bfloat16)
+    static constexpr int kAtP = kAtT + 2 * kMatrix;      // two parts
     static constexpr int kForward = kAtP + 2 * kMatrix;
     static constexpr int kAtTt = kAtP;  // the backward form has no P
     static constexpr int kAtPt = kAtTt + 2 * kMatrix;

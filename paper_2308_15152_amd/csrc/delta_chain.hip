@@ -19,7 +19,7 @@
 // FP32, for whose two parts LDS holds Q only once, the post is a second barrier (B),
 // before which the chunk's Q goes down.
 //
-// Measured (bfloat16, 128 x 128): 4 x 4096 tokens of 16 heads 190 us, 2.9 us a
+// Measured (bfloat16, 128 x 128): 4 x 4096 tokens of 16 heads 212 us, 3.3 us a
 // chunk on all CUs (the four that bring and the pair take about as long); 32768 tokens of 8
 // heads, not cut, 2.2 us a chunk.  One wave to 16 columns, alone on its CU: 2.4.
 //
@@ -47,14 +47,11 @@ struct Layout {
     // would be waited for with them.)
     static constexpr int kHelpers = kMode == kOutputs ? 8 : 4;
     static constexpr int kParts = kPartsOf<T>;  // of K and Q
-    // of P, and of S and U where they make O: rounding them to fp16 alone costs
-    // 2^-12 relative, unseen in a bfloat16 result (2^-8) but not in others
-    static constexpr int kOut = __is_same(T, bf16_t) ? 1 : 2;
     static constexpr int kSteps = kK / 32, kTiles = kK / 16;
     static constexpr int kHalf = kTiles / 2;                  // row tiles of a wave of a pair
     static constexpr int kRows = kParts * 4 * kSteps * 1024;  // K or Q
     static constexpr int kMatrices = 2 * DeltaRecord::kMatrix;
-    static constexpr int kBytesP = kMode == kOutputs ? kOut * DeltaRecord::kMatrix : 0;
+    static constexpr int kBytesP = kMode == kOutputs ? kMatrices : 0;
     // two buffers of these
     static constexpr int kAtK = 0;
     static constexpr int kAtT = kAtK + kRows;
@@ -67,11 +64,9 @@ struct Layout {
     static constexpr int kBufferQ = kAtP + kBytesP - kAtQ;
     // one of these
     static constexpr int kAtV = kAtQ + (kPosts ? 2 : 1) * kBufferQ;
-    // V as FP32 but for float16, where the LDS is full
-    using VType = typename std::conditional<__is_same(T, f16_t), f16_t, float>::type;
-    using V = Values<T, kWalkers, 256, VType>;
+    using V = Values<T, kWalkers, 256>;
     static constexpr int kAtS = kAtV + kWalkers * V::kEach;
-    static constexpr int kEachS = kOut * kSteps * 1024 + 128;  // and the scales of its halves
+    static constexpr int kEachS = 2 * kSteps * 1024 + 128;  // and the scales of its halves
     static constexpr int kAtU = kAtS + (kMode == kOutputs ? kWalkers * kEachS : 0);
     static constexpr int kEachU = kC * 16 * 4 + 128;  // and each column's rows that count, and scale
     static constexpr int kBufferU = kMode == kOutputs ? kWalkers * kEachU : 0;  // one or two
@@ -90,7 +85,6 @@ template <class T, int kK, int kWalkers, int kMode, bool kWide>
 __global__ __launch_bounds__(64 * (2 * kWalkers + Layout<T, kK, kWalkers, kMode>::kHelpers), 1)
 void delta_chain_kernel(DeltaChunks p) {
     using L = Layout<T, kK, kWalkers, kMode>;
-    constexpr int kOut = L::kOut;
     constexpr bool kPosts = L::kPosts;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     int* posts = reinterpret_cast<int*>(lds + L::kAtPosts);
@@ -146,7 +140,7 @@ void delta_chain_kernel(DeltaChunks p) {
                 if (of_m && row == col) S[i][r] = 1.0f;
             }
         const char* v_at = lds + L::kAtV + group * L::V::kEach + 
-                           value_slot(lane, group) * 4 * (int)sizeof(typename L::VType);
+                           value_slot(lane, group) * 4 * (int)sizeof(T);
         char* s_at = lds + L::kAtS + group * L::kEachS;
         char* u_at = lds + L::kAtU + group * L::kEachU + lane * 16;
         char* x_at = lds + L::kAtX + group * L::kEachX;
@@ -164,7 +158,7 @@ void delta_chain_kernel(DeltaChunks p) {
             if (leads)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    typename L::VType w[4];
+                    T w[4];
                     __builtin_memcpy(w, v_at + i * 64 * sizeof(w), sizeof(w));
                     vt[i] = f32x4{to_f32(w[0]), to_f32(w[1]), to_f32(w[2]), to_f32(w[3])};
                 }
@@ -189,13 +183,13 @@ void delta_chain_kernel(DeltaChunks p) {
                 sb[j] = split<2>(S[2 * j], S[2 * j + 1], ss.up);
                 if (kMode == kOutputs)
 #pragma unroll
-                    for (int q = 0; q < kOut; ++q)
+                    for (int q = 0; q < 2; ++q)
                         *reinterpret_cast<half8_t*>(
                             s_at + (q * L::kSteps + half * (L::kSteps / 2) + j) * 1024 + lane * 16) =
                             sb[j].part[q];
             }
             if (kMode == kOutputs)
-                reinterpret_cast<float*>(s_at + kOut * L::kSteps * 1024)[16 * half + (lane & 15)] =
+                reinterpret_cast<float*>(s_at + 2 * L::kSteps * 1024)[16 * half + (lane & 15)] =
                     ss.down;
             if (kPosts) {
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -462,7 +456,7 @@ void delta_chain_kernel(DeltaChunks p) {
         const int cut = *reinterpret_cast<const int*>(column);
         const float u_down = *reinterpret_cast<const float*>(column + 64);
         const Scale us = scale_of(max_groups(largest(u)));
-        const Frag<kOut> b[2] = {split<kOut>(u[0], u[1], us.up), split<kOut>(u[2], u[3], us.up)};
+        const Frag<2> b[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
         const int count = min(kC, span.count - c * kC);
         const __amdgpu_buffer_rsrc_t to = buffer_at(o + (int64_t)c * kC * p.o.token);
 #pragma unroll
@@ -472,7 +466,7 @@ void delta_chain_kernel(DeltaChunks p) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
                 if (j <= tile / 2)
-                    a = multiply(matrix_fragment<kOut>(buffer_q(c) + L::kAtP, lower_at(tile, j), lane),
+                    a = multiply(matrix_fragment<2>(buffer_q(c) + L::kAtP, lower_at(tile, j), lane),
                                  b[j], a);
             a *= pf[i] * (us.down * u_down);
 #pragma unroll
@@ -493,7 +487,7 @@ void delta_chain_kernel(DeltaChunks p) {
                          64 * DeltaRecord::kFirstChain;
         const char* s_at = lds + L::kAtS + block * L::kEachS;
         const float* downs =
-            reinterpret_cast<const float*>(s_at + kOut * L::kSteps * 1024) + (lane & 15);
+            reinterpret_cast<const float*>(s_at + 2 * L::kSteps * 1024) + (lane & 15);
         const float first = downs[0], last = downs[16];  // of S's halves
         f32x4 z[kOwn];
 #pragma unroll
@@ -506,9 +500,9 @@ void delta_chain_kernel(DeltaChunks p) {
                     z[i] = y[i] * first;
                     y[i] = f32x4{};
                 }
-            Frag<kOut> b;
+            Frag<2> b;
 #pragma unroll
-            for (int r = 0; r < kOut; ++r)
+            for (int r = 0; r < 2; ++r)
                 b.part[r] = *reinterpret_cast<const half8_t*>(
                     s_at + (r * L::kSteps + j) * 1024 + lane * 16);
 #pragma unroll

@@ -577,12 +577,12 @@ struct Rows {
 __device__ inline int value_slot(int lane, int block) { return lane ^ (((lane >> 4) ^ block) & 3); }
 
 // Columns of V or dO on their way to LDS, where they lie as the waves that own
-// 16 columns hold them: 4 tokens of a column together, as To.  A thread takes 4
+// 16 columns hold them: 4 tokens of a column together.  A thread takes 4
 // tokens x 4 columns of 16 kBlocks ones.
-template <class T, int kBlocks, int kThreads, class To = T>
+template <class T, int kBlocks, int kThreads>
 struct Values {
     static constexpr int kUnits = 16 * 4 * kBlocks;
-    static constexpr int kEach = kC * 16 * sizeof(To);  // bytes of a block of 16 columns
+    static constexpr int kEach = kC * 16 * sizeof(T);  // bytes of a block of 16 columns
     static constexpr int kMine = (kUnits + kThreads - 1) / kThreads;
     T x[kMine][4][4];
     // rows: of the chunk's first token and first column; size: columns there are
@@ -620,19 +620,14 @@ struct Values {
             const int unit = thread + m * kThreads;
             if (kUnits % kThreads != 0 && unit >= kUnits) continue;
             const int four = unit / (4 * kBlocks), c = unit % (4 * kBlocks) * 4;
-            char* at = to + c / 16 * kEach + four / 4 * 64 * 4 * sizeof(To);
+            char* at = to + c / 16 * kEach + four / 4 * 64 * 4 * sizeof(T);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                To w[4];
+                T w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (__is_same(T, To))
-                        w[i] = x[m][i][e];
-                    else
-                        w[i] = to_f32(x[m][i][e]);
-                }
-                __builtin_memcpy(at + value_slot(four % 4 * 16 + c % 16 + e, c / 16) * 4 * sizeof(To),
-                                 w, 4 * sizeof(To));
+                for (int i = 0; i < 4; ++i) w[i] = x[m][i][e];
+                __builtin_memcpy(at + value_slot(four % 4 * 16 + c % 16 + e, c / 16) * 4 * sizeof(T),
+                                 w, 4 * sizeof(T));
             }
         }
     }

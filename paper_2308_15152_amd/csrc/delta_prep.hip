@@ -48,7 +48,7 @@ __device__ inline void block_store(float* X, int lane, f32x4 d) {
 // Fragments of tile `tile`'s rows of the matrix M (or its transpose), with the
 // rows' inverse scales; its columns times `columns`, if given.  Blocks on the
 // empty side of the diagonal are zero whatever M holds there.
-template <bool kTransposed, int kParts>
+template <bool kTransposed>
 __device__ inline void write_fragments(const float* M, int tile, int lane, char* to, float* inverse,
                                        const float* columns = nullptr) {
     const int row = lane & 15, g = lane >> 4;
@@ -81,9 +81,9 @@ __device__ inline void write_fragments(const float* M, int tile, int lane, char*
     for (int step = 0; step < 2; ++step) {
         if (kTransposed ? step < tile / 2 : step > tile / 2) continue;
         const int at = kTransposed ? upper_at(tile, step) : lower_at(tile, step);
-        const Frag<kParts> f = split<kParts>(x[step], s.up);
+        const Frag<2> f = split<2>(x[step], s.up);
 #pragma unroll
-        for (int p = 0; p < kParts; ++p)
+        for (int p = 0; p < 2; ++p)
             *reinterpret_cast<half8_t*>(to + (p * 6 + at) * 1024 + lane * 16) = f.part[p];
     }
 }
@@ -286,17 +286,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4) void delta_prep_k
     }
     __syncthreads();
 
-    write_fragments<false, 2>(A, wave, lane, record + DeltaRecord::kAtT,
+    write_fragments<false>(A, wave, lane, record + DeltaRecord::kAtT,
                               factors + 64 * DeltaRecord::kT, beta);
     if (kBackward) {
-        write_fragments<true, 2>(A, wave, lane, record + DeltaRecord::kAtTt,
+        write_fragments<true>(A, wave, lane, record + DeltaRecord::kAtTt,
                                  factors + 64 * DeltaRecord::kTt);
-        write_fragments<true, 2>(P, wave, lane, record + DeltaRecord::kAtPt,
+        write_fragments<true>(P, wave, lane, record + DeltaRecord::kAtPt,
                                  factors + 64 * DeltaRecord::kPt);
     } else {
-        constexpr int kParts = __is_same(T, bf16_t) ? 1 : 2;
-        write_fragments<false, kParts>(P, wave, lane, record + DeltaRecord::kAtP,
-                                       factors + 64 * DeltaRecord::kP);
+        write_fragments<false>(P, wave, lane, record + DeltaRecord::kAtP,
+                               factors + 64 * DeltaRecord::kP);
     }
 }
 
