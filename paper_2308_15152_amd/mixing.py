@@ -5,6 +5,11 @@ the arithmetic runs in the HIP kernels.
 Tensors are (batch, tokens, heads, size); all but the last dimension may have
 any strides.  q, k, v, o and their gradients share one type (float32, bfloat16
 or float16); decays, strengths, states and tables are float32.
+
+A call runs on the current torch stream or on ``stream`` (a hipStream_t handle).
+What it allocates (outputs and a workspace that are not given) is allocated, and
+filled where it is, on the stream it runs on; the outputs are kept from reuse
+until the stream that is current in the call is through with them, too.
 """
 from __future__ import annotations
 
@@ -46,6 +51,34 @@ def _launch(name, dev, stream, args):
         raise _pkg.SgemmEmuError(rc, name)
 
 
+def _side(stream, device):
+    """The torch stream of a handle, None if it is the current one's."""
+    torch = _pkg._torch
+    if device.type != "cuda":
+        return None
+    index = torch.cuda.current_device() if device.index is None else device.index
+    if int(stream) == torch._C._cuda_getCurrentRawStream(index):
+        return None
+    return torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def _new(stream, shape, dtype, device, zero=False):
+    """A new tensor, made and filled on the stream that the call runs on: memory that
+    the current stream is still to read or write is not given out, and the fill comes before
+    the kernels.  The caller has it on the current stream, so its memory waits for
+    that one too."""
+    torch = _pkg._torch
+    make = torch.zeros if zero else torch.empty
+    side = None if stream is None else _side(stream, device)
+    if side is None:
+        return make(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(side):
+        t = make(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
 def _device(*ts):
     """Index of the one device that every tensor given (None skipped) is on."""
     dev = ts[0].get_device()
@@ -70,12 +103,11 @@ def _view(t, name, shape, dtype):
     return (t.data_ptr(), *st)
 
 
-def _like(t):
+def _like(t, stream):
     """A new contiguous tensor like t."""
-    torch = _pkg._torch
-    if t.is_contiguous():
-        return torch.empty_like(t)
-    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    if stream is None and t.is_contiguous():
+        return _pkg._torch.empty_like(t)
+    return _new(stream, t.shape, t.dtype, t.device)
 
 
 def _sizes(q, k, v):
@@ -111,15 +143,13 @@ def _packed(cu_seqlens, batch):
     return cu_seqlens.data_ptr(), cu_seqlens.shape[0] - 1
 
 
-def _workspace(need, given, dev, stream):
+def _workspace(need, given, device, stream):
     """(tensor, pointer, bytes) of a call's workspace."""
     torch = _pkg._torch
     if given is None:
         if need == 0:
             return None, 0, 0
-        given = torch.empty(need, dtype=torch.uint8, device=dev)
-        if stream is not None:  # the allocator may not reuse it before that stream is through
-            given.record_stream(torch.cuda.ExternalStream(int(stream), device=dev))
+        given = _new(stream, need, torch.uint8, device)
     elif not given.is_contiguous():
         raise ValueError("workspace must be contiguous")
     return given, given.data_ptr(), given.numel() * given.element_size()
@@ -146,7 +176,7 @@ def rotary_emu(q, k, cos, sin, *, positions=None, offset: int = 0, interleaved: 
     b, t, hq, size = q.shape
     dtype = q.dtype
     if out is None:
-        oq, ok = _like(q), None if k is None else _like(k)
+        oq, ok = _like(q, stream), None if k is None else _like(k, stream)
     else:
         oq, ok = out
     xq, yq = _view(q, "q", q.shape, dtype), _view(oq, "out", q.shape, dtype)
@@ -202,8 +232,8 @@ def rotary_emu_table(rows: int, rot: int, *, base: float = 10000.0, factor: floa
     low, high = (0.0, 0.0) if ramp is None else ramp
     rows, rot = int(rows), int(rot)
     device = torch.device("cuda" if device is None else device)
-    c = torch.empty((max(rows, 0), max(rot, 0) // 2), dtype=torch.float32, device=device)
-    s = torch.empty_like(c)
+    c, s = (_new(stream, (max(rows, 0), max(rot, 0) // 2), torch.float32, device)
+            for _ in range(2))
     with _pkg._on_device(c, s):
         rc = _pkg.load().rotary_emu_table(rows, rot, base, factor, original, low, high, amplitude,
                                           c.data_ptr(), s.data_ptr(), _pkg._stream(stream))
@@ -260,17 +290,18 @@ def delta_emu_forward(q, k, v, g=None, beta=None, initial_state=None, *, scale=N
     torch = _pkg._torch
     b, t, hk, hv, ks, vs = _sizes(q, k, v)
     cu, n = _packed(cu_seqlens, b)
+    device = q.device
     if out is None:
-        out = torch.empty((b, t, hv, vs), dtype=q.dtype, device=q.device)
+        out = _new(stream, (b, t, hv, vs), q.dtype, device)
     if final_state is None:
-        final_state = torch.empty((n, hv, ks, vs), dtype=torch.float32, device=q.device)
+        final_state = _new(stream, (n, hv, ks, vs), torch.float32, device)
     dev = _device(q, k, v, g, beta, initial_state, cu_seqlens, out, final_state, workspace)
     args = _forward_args(q, k, v, g, beta, out, initial_state, final_state, scale, cu, n, 0, 0)
     need = _calls["delta_emu_forward_workspace"](args)
     if need < 0:
         raise _pkg.SgemmEmuError(need, "delta_emu_forward")
     if need > 0 or workspace is not None:
-        workspace, at, size = _workspace(need, workspace, q.device, stream)
+        workspace, at, size = _workspace(need, workspace, device, stream)
         args = args[:-16] + struct.pack("=2q", at, size)
     _launch("delta_emu_forward", dev, stream, args)
     return out, final_state
@@ -327,10 +358,10 @@ def delta_emu_backward(q, k, v, g, beta, do, initial_state=None, dfinal=None, *,
     b, t, hk, hv, ks, vs = _sizes(q, k, v)
     cu, n = _packed(cu_seqlens, b)
     if out is None:
-        make = torch.empty if cu_seqlens is None else torch.zeros
-        out = [make(x.shape, dtype=x.dtype, device=q.device) if x is not None else None
+        out = [None if x is None else _new(stream, x.shape, x.dtype, q.device,
+                                           zero=cu_seqlens is not None)
                for x in (q, k, v, g, beta)]
-        out.append(torch.empty((n, hv, ks, vs), dtype=torch.float32, device=q.device))
+        out.append(_new(stream, (n, hv, ks, vs), torch.float32, q.device))
     *grads, dinitial = out
     dev = _device(q, k, v, g, beta, do, initial_state, dfinal, cu_seqlens, workspace, *out)
     args = _backward_args(q, k, v, g, beta, do, grads, initial_state, dfinal, dinitial, scale, cu,
@@ -358,7 +389,7 @@ def delta_emu_step(q, k, v, g, beta, state, *, slots=None, scale=None, out=None,
     dtype, f32 = q.dtype, torch.float32
     values, gates = (b, t, hv, vs), (b, t, hv)
     if out is None:
-        out = torch.empty(values, dtype=dtype, device=q.device)
+        out = _new(stream, values, dtype, q.device)
     if state.dtype is not f32 or state.dim() != 4 or state.shape[1:] != (hv, ks, vs):
         raise ValueError(f"state must be a float32 tensor (slots, {hv}, {ks}, {vs})")
     n_slots, stride = state.shape[0], state.stride()
