@@ -30,12 +30,14 @@ _dtypes = {}
 
 
 def _start():
+    global _calls
     lib = _pkg.load()
     torch = _pkg._load_torch()
     _dtypes.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-    for name in ("rotary_emu", "delta_emu_forward", "delta_emu_backward", "delta_emu_step",
-                 "delta_emu_forward_workspace", "delta_emu_backward_workspace"):
-        _calls[name] = getattr(lib, name)
+    # whole, and last: other threads take a filled _calls for all of this
+    _calls = {name: getattr(lib, name) for name in (
+        "rotary_emu", "delta_emu_forward", "delta_emu_backward", "delta_emu_step",
+        "delta_emu_forward_workspace", "delta_emu_backward_workspace")}
 
 
 def _launch(name, dev, stream, args):
