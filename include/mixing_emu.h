@@ -115,7 +115,8 @@ int rotary_emu_table(int rows, int rot, double base, double factor, double origi
  * recurrence takes it to: no earlier token, other sequence, head or, if it is in
  * v or a state, column.
  * Errors: _DIM, _UNSUPPORTED (dtype, sizes and strides above, head counts, more than
- * 2^21 chunks x value heads),
+ * 2^21 chunks x value heads, or sequences x value heads x groups of 64 value columns; of 32
+ * where float32 outputs of more than 16 tokens have keys above 64),
  * _NULL, _STRIDE, _ALIAS, _HIP.
  */
 typedef struct {

@@ -29,9 +29,32 @@ constexpr int kDeltaMaxK = 128;  // largest key size
 constexpr int kDeltaChunk = 64;  // tokens of a chunk
 constexpr int kDeltaMaxV = 1 << 16;
 constexpr int64_t kDeltaMostStride = 1 << 22;  // of tokens, in elements
-// Chunks x value heads of one call: one block each, one launch.  (A walk's blocks, up to two
-// a chunk and head, have 768 threads, and a launch has less than 2^32.)
+// Chunks x value heads of one call (one block each, one launch), and sequences x value
+// heads x groups of columns: two blocks of a walk take a group, and a launch has less than
+// 2^32 threads.
 constexpr int64_t kDeltaMostTasks = 1 << 21;
+constexpr int kDeltaMostThreads = 768;  // of a walk's block
+static_assert(2 * kDeltaMostTasks * kDeltaMostThreads < int64_t{1} << 32, "one launch");
+
+// Columns of the state that a block of a walk takes, at least but for short calls
+// (delta_chain.hip, delta_back.hip).
+struct DeltaColumns {
+    int outputs, states, steps, back;
+};
+
+inline DeltaColumns delta_columns(int dtype, int k_size) {
+    const bool large_f32 = dtype == SGEMM_EMU_F32 && k_size > 64;
+    return {large_f32 ? 16 : 32, 32, large_f32 ? 32 : 64, large_f32 ? 16 : 32};
+}
+
+// Sequences of up to this many tokens go token by token (delta_step.hip): 16
+// tokens of 16 heads of 128 x 128 take 17.5 us either way, of 1024 heads 94
+// against 158; 24 tokens 25 against 17, and 135 against 158.
+constexpr int kDeltaFewTokens = 16;
+
+inline bool delta_few_tokens(const delta_emu_forward_t& a) {
+    return a.cu_seqlens == nullptr && a.tokens <= kDeltaFewTokens;
+}
 
 // Chunks that the sequences of a call can have.  Packed sequences: sequence n's
 // are numbered from first row / 64 + n, which leaves at most one number

@@ -444,6 +444,8 @@ template <class T, int kK, int kWalkers, bool kCarry, bool kWide>
 hipError_t launch_rows(const DeltaChunks& a, hipStream_t stream) {
     using L = Layout<T, kK, kWalkers>;
     static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
+    static_assert(64 * (2 * kWalkers + L::kHelpers) * 2 <= kDeltaMostThreads * kWalkers,
+                  "32 columns: one launch");
     const int64_t slices = (a.v_size + 16 * kWalkers - 1) / (16 * kWalkers);
     const int64_t walks = a.part_chunks > 0 ? a.parts : a.batch;
     const void* kernel =

@@ -528,6 +528,7 @@ template <class T, int kK, int kWalkers, int kMode, bool kWide>
 hipError_t launch_rows(const DeltaChunks& a, hipStream_t stream) {
     using L = Layout<T, kK, kWalkers, kMode>;
     static_assert(L::kBytes <= 160 * 1024, "LDS of a CU");
+    static_assert(64 * (2 * kWalkers + L::kHelpers) <= kDeltaMostThreads, "one launch");
     constexpr int kColumns = 16 * kWalkers;
     int64_t slices = (a.v_size + kColumns - 1) / kColumns;
     if (kMode == kPartSteps) slices += (a.k_size + kColumns - 1) / kColumns;

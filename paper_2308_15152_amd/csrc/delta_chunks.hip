@@ -8,17 +8,6 @@ namespace {
 
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Columns of the state that a block of a walk takes (delta_chain.hip,
-// delta_back.hip).
-struct Columns {
-    int outputs, states, steps, back;
-};
-
-Columns columns_of(int dtype, int k_size) {
-    const bool large_f32 = dtype == SGEMM_EMU_F32 && k_size > 64;
-    return {large_f32 ? 16 : 32, 32, large_f32 ? 32 : 64, large_f32 ? 16 : 32};
-}
-
 // Chunks of a part that the sequences are cut into, 0 if they are not.  A walk
 // takes about the same time per chunk whatever the number of its blocks up to one per CU,
 // and the parts cost a walk more, over k_size more columns, and the join.  The estimate
@@ -33,7 +22,7 @@ int part_chunks_of(const A& a, bool backward) {
     if (a.batch == 0 || a.tokens == 0 || a.v_size == 0) return 0;
     constexpr double kCus = 256, kOutputs = 2.6, kStates = 2.4, kSteps = 2.8, kBack = 3.8,
                      kJoin = 3.0, kStart = 5.0;
-    const Columns c = columns_of(a.dtype, a.k_size);
+    const DeltaColumns c = delta_columns(a.dtype, a.k_size);
     const auto blocks = [&](int64_t columns, int each) {  // of all sequences and heads
         return (double)((columns + each - 1) / each) * a.v_heads * a.batch;
     };
@@ -110,15 +99,6 @@ Plan plan_of(const A& a, bool backward) {
     return p;
 }
 
-// Sequences of up to this many tokens go token by token (delta_step.hip): 16
-// tokens of 16 heads of 128 x 128 take 17.5 us either way, of 1024 heads 94
-// against 158; 24 tokens 25 against 17, and 135 against 158.
-constexpr int kFewTokens = 16;
-
-bool few_tokens(const delta_emu_forward_t& a) {
-    return a.cu_seqlens == nullptr && a.tokens <= kFewTokens;
-}
-
 template <class A>
 DeltaChunks arguments(const A& a, const Plan& p) {
     char* at = static_cast<char*>(a.workspace);
@@ -142,13 +122,13 @@ DeltaChunks arguments(const A& a, const Plan& p) {
 }  // namespace
 
 int64_t delta_forward_workspace(const delta_emu_forward_t& a) {
-    return few_tokens(a) ? 0 : plan_of(a, false).total;
+    return delta_few_tokens(a) ? 0 : plan_of(a, false).total;
 }
 
 int64_t delta_backward_workspace(const delta_emu_backward_t& a) { return plan_of(a, true).total; }
 
 hipError_t launch_delta_forward(const delta_emu_forward_t& a, hipStream_t stream) {
-    if (few_tokens(a)) {
+    if (delta_few_tokens(a)) {
         DeltaStep s{};
         s.dtype = a.dtype, s.batch = a.batch, s.tokens = a.tokens;
         s.k_heads = a.k_heads, s.v_heads = a.v_heads, s.k_size = a.k_size, s.v_size = a.v_size;

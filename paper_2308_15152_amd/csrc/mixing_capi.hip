@@ -131,16 +131,26 @@ int check_tensors(std::initializer_list<Tensor> ins, std::initializer_list<Tenso
 }
 
 // Checks that do not look behind pointers, for the workspace queries and the
-// calls alike.
+// calls alike.  columns: that a block of the call's walks takes, 0 without a walk.
 template <class A>
-int check_shape(const A& a) {
+int check_shape(const A& a, int columns) {
     if (int rc = check_sizes(a)) return rc;
     if (a.cu_seqlens == nullptr && (int64_t)a.batch * a.tokens > INT32_MAX)
         return SGEMM_EMU_ERR_UNSUPPORTED;
-    if (delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr) > kDeltaMostTasks / a.v_heads ||
-        (int64_t)a.batch * (((int64_t)a.v_size + 63) / 64) > kDeltaMostTasks / a.v_heads)
+    if (delta_chunks(a.batch, a.tokens, a.cu_seqlens != nullptr) > kDeltaMostTasks / a.v_heads)
+        return SGEMM_EMU_ERR_UNSUPPORTED;
+    const int64_t group = columns > 0 ? 2 * columns : 64;
+    if ((int64_t)a.batch * ((a.v_size + group - 1) / group) > kDeltaMostTasks / a.v_heads)
         return SGEMM_EMU_ERR_UNSUPPORTED;
     return SGEMM_EMU_OK;
+}
+
+int check_shape(const delta_emu_forward_t& a) {
+    return check_shape(a, delta_few_tokens(a) ? 0 : delta_columns(a.dtype, a.k_size).outputs);
+}
+int check_shape(const delta_emu_backward_t& a) {
+    // (a block of the walk back that takes 16 columns has half of the threads)
+    return check_shape(a, delta_columns(a.dtype, a.k_size).states);
 }
 
 int done(hipError_t e) { return e == hipSuccess ? SGEMM_EMU_OK : hip_fail(e); }
