@@ -27,7 +27,9 @@ extern "C" {
  * Tensors are (batch, token, head, element) views with element strides for
  * the first three; the last dimension is contiguous.  Input strides may be
  * zero (broadcast); an output's elements must be apart (ERR_STRIDE).  Spans
- * of outputs must not overlap spans of inputs (ERR_ALIAS) except where noted.
+ * of outputs must not overlap spans of inputs (ERR_ALIAS) except where noted, and
+ * two outputs must not share elements (ERR_ALIAS); their spans may overlap where they lie
+ * between each other with the same strides (slices of one buffer).
  * Any alignment is accepted; with 16-byte aligned rows the loads are vectors. */
 #define SGEMM_EMU_F32 0
 #define SGEMM_EMU_BF16 1

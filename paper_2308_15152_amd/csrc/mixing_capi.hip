@@ -3,11 +3,11 @@
 #include <stdint.h>
 
 #include <cmath>
-#include <utility>
 
 #include "checks.h"
 #include "delta.h"
 #include "mixing.h"
+#include "views.h"
 
 namespace {
 
@@ -15,55 +15,6 @@ using namespace sgemm_emu;
 
 bool known_dtype(int d) { return d >= SGEMM_EMU_F32 && d <= SGEMM_EMU_F16; }
 int64_t dtype_bytes(int d) { return d == SGEMM_EMU_F32 ? 4 : 2; }
-
-// A tensor argument: its view, sizes and element bytes.
-struct Tensor {
-    const sgemm_emu_view_t& v;
-    int64_t batch, tokens, heads, size, elem;
-    bool empty() const { return batch == 0 || tokens == 0 || heads == 0 || size == 0; }
-};
-
-bool negative(const sgemm_emu_view_t& v) { return v.batch < 0 || v.token < 0 || v.head < 0; }
-
-// Bytes the tensor spans (strides not negative).
-Extent span(const Tensor& t) {
-    Extent e{(uintptr_t)t.v.p, (uintptr_t)t.v.p, true};
-    if (t.empty()) return e;
-    const __int128 last = (__int128)(t.batch - 1) * t.v.batch + (__int128)(t.tokens - 1) * t.v.token +
-                          (__int128)(t.heads - 1) * t.v.head + t.size;
-    const __int128 bytes = last * t.elem;
-    if (bytes > (__int128)(UINTPTR_MAX - e.lo)) {
-        e.ok = false;
-        return e;
-    }
-    e.hi = e.lo + (uintptr_t)bytes;
-    return e;
-}
-
-// Whether the elements of an output are apart: with the dimensions of more
-// than one entry ordered by stride, each stride steps over all that the
-// smaller ones reach.
-bool apart(const Tensor& t) {
-    if (t.empty()) return true;
-    int64_t n[3] = {t.batch, t.tokens, t.heads}, s[3] = {t.v.batch, t.v.token, t.v.head};
-    for (int i = 0; i < 2; ++i)
-        for (int j = i + 1; j < 3; ++j)
-            if (s[j] < s[i]) {
-                std::swap(s[i], s[j]);
-                std::swap(n[i], n[j]);
-            }
-    __int128 reach = t.size;
-    for (int i = 0; i < 3; ++i) {
-        if (n[i] <= 1) continue;
-        if (s[i] < reach) return false;
-        reach += (__int128)(n[i] - 1) * s[i];
-    }
-    return true;
-}
-
-bool same(const sgemm_emu_view_t& a, const sgemm_emu_view_t& b) {
-    return a.p == b.p && a.batch == b.batch && a.token == b.token && a.head == b.head;
-}
 
 // A contiguous array of `bytes` bytes.
 Extent array(const void* p, __int128 bytes) {
@@ -97,7 +48,7 @@ bool within_reach(std::initializer_list<sgemm_emu_view_t> views) {
     return true;
 }
 
-// Every input present, every output apart, no output over an input.
+// Strides not negative, every output apart, no output over an input or another one.
 int check_tensors(std::initializer_list<Tensor> ins, std::initializer_list<Tensor> outs,
                   std::initializer_list<Extent> arrays_in, std::initializer_list<Extent> arrays_out) {
     for (const auto* list : {&ins, &outs})
@@ -120,6 +71,8 @@ int check_tensors(std::initializer_list<Tensor> ins, std::initializer_list<Tenso
         if (!clear(span(o))) return SGEMM_EMU_ERR_ALIAS;
         for (const Extent& e : arrays_out)
             if (overlap(span(o), e)) return SGEMM_EMU_ERR_ALIAS;
+        for (const Tensor* other = outs.begin(); other != &o; ++other)
+            if (other->v.p != nullptr && meet(*other, o)) return SGEMM_EMU_ERR_ALIAS;
     }
     const Extent* prev = arrays_out.begin();
     for (const Extent* e = prev; e != arrays_out.end(); ++e) {
@@ -186,8 +139,7 @@ int rotary_emu(const rotary_emu_t* args, hipStream_t stream) {
     const sgemm_emu_view_t at{const_cast<void*>(a.positions), a.position_batch, a.position_token, 0};
     const Tensor places{at, a.batch, a.tokens, 1, 1, a.positions ? a.position_bytes : 1};
     const Extent tables[2] = {array(a.cos_table, table), array(a.sin_table, table)};
-    // the two tensors' outputs may only meet their own inputs, and those
-    // only in place
+    // an output may only meet its own input, in place, and not the other output
     for (int i = 0; i < 2; ++i) {
         if (heads[i] == 0) continue;
         const Tensor y{a.y[i], a.batch, a.tokens, heads[i], a.size, elem};
@@ -206,6 +158,7 @@ int rotary_emu(const rotary_emu_t* args, hipStream_t stream) {
                 return SGEMM_EMU_ERR_STRIDE;
             if (overlap(span(y), span(other))) return SGEMM_EMU_ERR_ALIAS;
         }
+        if (i == 1 && heads[0] > 0 && meet(others, y)) return SGEMM_EMU_ERR_ALIAS;
     }
     return done(launch_rotary(a, stream));
 }
