@@ -140,7 +140,10 @@ int delta_emu_forward(const delta_emu_forward_t* a, hipStream_t stream);
 /* The gradient: from d_o (like o) and dfinal (gradient of the final states, or
  * NULL) to dq, dk, dv (the inputs' type), dg, dbeta (FP32; p NULL: not
  * wanted) and dinitial (or NULL).  Sums over the value heads of a key head and over
- * tokens are in FP32 in a fixed order.  dinitial may be dfinal. */
+ * tokens are in FP32 in a fixed order.  dinitial may be dfinal.  A value of d_o or dfinal
+ * that is not finite reaches no later token (nor other sequence, head or, in dv and
+ * dinitial, column); where q, k, v, g, beta or a state is not, any gradient of that sequence's
+ * key head may not be. */
 typedef struct {
     int32_t dtype, batch, tokens, k_heads, v_heads, k_size, v_size;
     float scale;

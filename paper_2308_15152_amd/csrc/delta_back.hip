@@ -210,8 +210,12 @@ void delta_back_kernel(DeltaChunks p) {
                 }
                 // dY, and dV
                 f32x4 y[4] = {};
+                int cut = 0;
                 {
-                    const Scale us = scale_of(max_groups(largest(u)));
+                    float top = column_largest(u);
+                    const bool cuts = __any(!finite(top));
+                    if (cuts) cut = cut_column_back(u, top);
+                    const Scale us = scale_of(top);
                     const Frag<2> ub[2] = {split<2>(u[0], u[1], us.up), split<2>(u[2], u[3], us.up)};
                     const __amdgpu_buffer_rsrc_t dy = buffer_at(p.dsides + task * kC * p.v_size);
                     const __amdgpu_buffer_rsrc_t to = buffer_at(dv + (int64_t)c * kC * p.dv.token);
@@ -237,11 +241,20 @@ void delta_back_kernel(DeltaChunks p) {
                         }
                         y[i] *= -factor(DeltaRecord::kRise, i);
                     }
+                    if (cuts && !kCarry)  // over what was stored
+#pragma unroll 1
+                        for (int t = fresh(4 * g); t < cut; t += t % 4 == 3 ? 13 : 1) {
+                            store_word(__builtin_nanf(""), dy,
+                                       in ? 4u * (t * p.v_size + col) : kPastEnd);
+                            store_word(from_f32<T>(__builtin_nanf("")), to,
+                                       in && t < count
+                                           ? t * v_step + col * (uint32_t)sizeof(T) : kPastEnd);
+                        }
                 }
                 const Scale ys = scale_of(max_groups(largest(y)));
                 b[0] = split<2>(y[0], y[1], ys.up);
                 b[1] = split<2>(y[2], y[3], ys.up);
-                down = ys.down;
+                down = cut == 0 ? ys.down : __builtin_nanf("");
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -347,7 +360,11 @@ void delta_back_kernel(DeltaChunks p) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) o[i][r] = to_f32(x[r]);
         }
-        const Scale os = scale_of(max_groups(largest(o)));
+        float top = column_largest(o);
+        const bool cuts = __any(!finite(top));
+        int cut = 0;
+        if (cuts) cut = cut_column_back(o, top);
+        const Scale os = scale_of(top);
         {
             const Frag<L::kParts> b[2] = {split<L::kParts>(o[0], o[1], os.up),
                                           split<L::kParts>(o[2], o[3], os.up)};
@@ -361,6 +378,14 @@ void delta_back_kernel(DeltaChunks p) {
                         a = multiply(matrix_fragment<2>(at + L::kAtPt, upper_at(tile, j), lane), b[j], a);
                 pd[i] = a * reinterpret_cast<const f32x4*>(f + 64 * DeltaRecord::kPt)[4 * tile + g] * os.down;
             }
+            if (cuts) {
+                const int first = fresh(cut - 16 * part * kOwn - 4 * g);
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * i + r < first) pd[i][r] = __builtin_nanf("");
+            }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -373,7 +398,7 @@ void delta_back_kernel(DeltaChunks p) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
                 a = multiply<true>(column_fragment<T, kK>(at + L::kAtQ, part * kOwnK + i, j, lane), b[j], a);
-            qd[i] = a * qs.down;
+            qd[i] = a * (cut == 0 ? qs.down : __builtin_nanf(""));
         }
     };
     const auto put = [&]() __attribute__((always_inline)) {

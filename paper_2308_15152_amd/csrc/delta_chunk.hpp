@@ -135,6 +135,13 @@ __device__ inline float column_largest(const f32x4 (&x)[4]) {
 
 __device__ inline bool finite(float x) { return fabsf(x) < __builtin_inff(); }
 
+// x, of which the compiler keeps nothing ready: in code that hardly ever runs, row numbers
+// made before a loop would take registers from all that does.
+__device__ inline int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // The first row of this lane's column (kC if none) with a value that is not
 // finite; it and the rows after it become zero, m the largest of those left.
 __device__ inline int cut_column(f32x4 (&x)[4], float& m) {
@@ -152,6 +159,27 @@ __device__ inline int cut_column(f32x4 (&x)[4], float& m) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             if (16 * i + 4 * g + r >= first) x[i][r] = 0.0f;
+    m = column_largest(x);
+    return first;
+}
+
+// The same where values reach earlier tokens and no later ones (the way back): the rows up
+// to the last such value become zero.  The first row after them (0 if there is none).
+__device__ inline int cut_column_back(f32x4 (&x)[4], float& m) {
+    const int g = fresh((threadIdx.x & 63) >> 4);
+    int first = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (!finite(x[i][r])) first = 16 * i + 4 * g + r + 1;
+    first = max(first, __shfl_xor(first, 16, 64));
+    first = max(first, __shfl_xor(first, 32, 64));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (16 * i + 4 * g + r < first) x[i][r] = 0.0f;
     m = column_largest(x);
     return first;
 }
