@@ -122,6 +122,11 @@ def _sizes(q, k, v):
     return b, t, hk, v.shape[2], ks, v.shape[3]
 
 
+def _scale(scale, k_size):
+    """The outputs' scale (a key size of 0 is the library's to refuse)."""
+    return max(k_size, 1) ** -0.5 if scale is None else scale
+
+
 def _states(t, name, shape):
     """Pointer of a contiguous float32 tensor of that shape, or 0."""
     if t is None:
@@ -250,7 +255,7 @@ def _forward_args(q, k, v, g, beta, o, initial, final, scale, cu, n, ws, ws_byte
     values, gates = (b, t, hv, vs), (b, t, hv)
     states = (n, hv, ks, vs)
     return _FORWARD.pack(
-        _dtypes[dtype], n, t, hk, hv, ks, vs, ks ** -0.5 if scale is None else scale, cu,
+        _dtypes[dtype], n, t, hk, hv, ks, vs, _scale(scale, ks), cu,
         *_view(q, "q", q.shape, dtype), *_view(k, "k", q.shape, dtype),
         *_view(v, "v", values, dtype),
         *(_NO_VIEW if g is None else _view(g, "g", gates, f32)),
@@ -324,7 +329,7 @@ def _backward_args(q, k, v, g, beta, do, grads, initial, dfinal, dinitial, scale
                *(_NO_VIEW if dg is None else _view(dg, "dg", gates, f32)),
                *(_NO_VIEW if dbeta is None else _view(dbeta, "dbeta", gates, f32)))
     return _BACKWARD.pack(
-        _dtypes[dtype], n, t, hk, hv, ks, vs, ks ** -0.5 if scale is None else scale, cu,
+        _dtypes[dtype], n, t, hk, hv, ks, vs, _scale(scale, ks), cu,
         *_view(q, "q", q.shape, dtype), *_view(k, "k", q.shape, dtype),
         *_view(v, "v", values, dtype),
         *(_NO_VIEW if g is None else _view(g, "g", gates, f32)),
@@ -404,7 +409,7 @@ def delta_emu_step(q, k, v, g, beta, state, *, slots=None, scale=None, out=None,
             raise ValueError("slots must be a contiguous int32 vector of the batch")
         at = slots.data_ptr()
     args = _STEP.pack(
-        _dtypes[dtype], b, t, hk, hv, ks, vs, ks ** -0.5 if scale is None else scale,
+        _dtypes[dtype], b, t, hk, hv, ks, vs, _scale(scale, ks),
         *_view(q, "q", q.shape, dtype), *_view(k, "k", q.shape, dtype),
         *_view(v, "v", values, dtype),
         *(_NO_VIEW if g is None else _view(g, "g", gates, f32)),
