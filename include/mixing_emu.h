@@ -30,7 +30,7 @@ extern "C" {
  * of outputs must not overlap spans of inputs (ERR_ALIAS) except where noted, and
  * two outputs must not share elements (ERR_ALIAS); their spans may overlap where they lie
  * between each other with the same strides (slices of one buffer).
- * Any alignment is accepted; with 16-byte aligned rows the loads are vectors. */
+ * Elements are aligned to their size; with 16-byte aligned rows the loads are vectors. */
 #define SGEMM_EMU_F32 0
 #define SGEMM_EMU_BF16 1
 #define SGEMM_EMU_F16 2
@@ -105,8 +105,9 @@ int rotary_emu_table(int rows, int rot, double base, double factor, double origi
  *   cu_seqlens NULL: `batch` sequences of `tokens` tokens.
  *   else: packed sequences; the views' batch stride is not used, `tokens` is the
  *     number of rows in all, and sequence n is rows cu_seqlens[n] to
- *     cu_seqlens[n+1] - 1 (device, int32, batch + 1 values, not decreasing, within
- *     [0, tokens]; others are clamped to that).  Rows of no sequence are not written.
+ *     cu_seqlens[n+1] - 1 (device, int32, batch + 1 values, not decreasing; values outside
+ *     [0, tokens] are clamped to it; where they decrease, results are unspecified, and
+ *     nothing outside the tensors is touched).  Rows of no sequence are not written.
  * initial: states before the first tokens, or NULL (zero).
  * workspace: device memory, 256-byte aligned, at least what the _workspace query
  *   for the same arguments returns (0 for up to 16 tokens that are not packed, which

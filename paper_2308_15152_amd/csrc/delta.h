@@ -47,9 +47,9 @@ inline DeltaColumns delta_columns(int dtype, int k_size) {
     return {large_f32 ? 16 : 32, 32, large_f32 ? 32 : 64, large_f32 ? 16 : 32};
 }
 
-// Sequences of up to this many tokens go token by token (delta_step.hip): 16
-// tokens of 16 heads of 128 x 128 take 17.5 us either way, of 1024 heads 94
-// against 158; 24 tokens 25 against 17, and 135 against 158.
+// Sequences of up to this many tokens go token by token (delta_step.hip).  Kernel times, 128 x
+// 128 in bfloat16: 16 tokens of 16 heads 17.8 us against 16.7 in chunks, which are a launch
+// more, and of 1024 heads 97 against 126; 24 tokens 25 against 17, and 143 against 127.
 constexpr int kDeltaFewTokens = 16;
 
 inline bool delta_few_tokens(const delta_emu_forward_t& a) {

@@ -21,7 +21,7 @@
 //
 // Measured (bfloat16, 128 x 128): 4 x 4096 tokens of 16 heads 212 us, 3.3 us a
 // chunk on all CUs (the four that bring and the pair take about as long); 32768 tokens of 8
-// heads, not cut, 2.2 us a chunk.  One wave to 16 columns, alone on its CU: 2.4.
+// heads, not cut, 2.3 us a chunk.
 //
 // A long sequence of few heads leaves most CUs idle.  It is cut into parts, and
 // walked three times less deep: first every part but the last from S = 0, and, as

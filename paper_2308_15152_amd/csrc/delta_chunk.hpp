@@ -7,7 +7,8 @@
 // down to 2^-15 of the largest keep 22 bits and smaller ones an absolute 2^-39
 // of it, and inputs of any FP32 magnitude are represented.  The powers are
 // taken out of the FP32 result, whose rows and columns are A's rows and B's
-// columns.  bfloat16 and float16 inputs are exact with hi alone.
+// columns.  Inputs of 16 bits have hi alone: float16 ones are exact, bfloat16 ones down to
+// 2^-32 of their row's largest (below, to an absolute 2^-39 of it).
 //
 // Where the result of one product is the B operand of the next, it stays in
 // registers: lane l of the accumulator holds rows 4 (l / 16) + 0..3 of column
@@ -255,8 +256,8 @@ __device__ inline WalkTask walk_task(int slices) {
     return {i / slices * 8 + xcd, i % slices};
 }
 // Whether a walk takes 16 columns a block rather than 32: where those leave half of
-// the CUs idle (the walk back of 32 heads of 128 x 128: 128 blocks 226 us, 256
-// blocks 207; with more heads than that K and Q would be brought twice as often for nothing).
+// the CUs idle (the walk back of 32 heads of 128 x 128: 128 blocks 227 us, 256
+// blocks 213; with more heads than that K and Q would be brought twice as often for nothing).
 inline bool narrow(const DeltaChunks& a) {
     const int64_t walks = a.part_chunks > 0 ? a.parts : a.batch;
     return walks * a.v_heads * ((a.v_size + 31) / 32) <= 128;

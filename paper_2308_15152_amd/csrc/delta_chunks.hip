@@ -11,16 +11,17 @@ int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // Chunks of a part that the sequences are cut into, 0 if they are not.  A walk
 // takes about the same time per chunk whatever the number of its blocks up to one per CU,
 // and the parts cost a walk more, over k_size more columns, and the join.  The estimate
-// below uses measured times (us, 128 x 128 states in bfloat16; other sizes keep their
-// ratios): a chunk takes 2.2 (few blocks) to 2.9 (on all CUs) in the walk for outputs, 2.3
-// to 2.6 for states, 2.8 for N and M, 3.3 to 4.4 back; a part 3 in the join, and each of
-// these launches 5.  Walks and joins: 32768 tokens of 8 heads 377 in 8 parts, 1120 not cut; 4096 tokens of 64 heads
-// 300 in two, 190 not cut; their gradient with 32 heads 430 in two, 358 not cut; 1001
-// tokens of 18 heads of 64 x 96 in float32 98 in three, 88 not cut.
+// below uses measured times (us, 128 x 128 states in bfloat16; for other types and sizes
+// it takes them as they are, which was checked at the last case below only): a chunk takes
+// 2.3 (few blocks) to 3.3 (on all CUs) in the walk for outputs, 2.3 to 2.6 for states, 2.8
+// for N and M, 3.3 to 4.4 back; a part 3 in the join, and each of these launches 5.  Walks and
+// joins: 32768 tokens of 8 heads 403 in 8 parts, 1163 not cut; 4096 tokens of 64 heads 329 in
+// two, 204 not cut; their gradient with 32 heads 438 in two, 361 not cut; that of 1001
+// tokens of 18 heads of 64 x 96 in float32 111 in three, 88 not cut.
 template <class A>
 int part_chunks_of(const A& a, bool backward) {
     if (a.batch == 0 || a.tokens == 0 || a.v_size == 0) return 0;
-    constexpr double kCus = 256, kOutputs = 2.6, kStates = 2.4, kSteps = 2.8, kBack = 3.8,
+    constexpr double kCus = 256, kOutputs = 2.7, kStates = 2.4, kSteps = 2.8, kBack = 3.8,
                      kJoin = 3.0, kStart = 5.0;
     const DeltaColumns c = delta_columns(a.dtype, a.k_size);
     const auto blocks = [&](int64_t columns, int each) {  // of all sequences and heads

@@ -12,8 +12,8 @@
 // The walk forward takes T diag(beta), the one back T^T.
 //
 // A block makes one chunk of one head, a wave 16 rows of it.  Bound by the records that it
-// writes (20 KB a chunk, or 40 for the gradient) and, in part, by the latency of the
-// triangular inverse: 4 x 4096 tokens of 16 heads of 128 in bfloat16 take 54 us,
+// writes (27 KB a chunk, or 39 for the gradient) and, in part, by the latency of the
+// triangular inverse: 4 x 4096 tokens of 16 heads of 128 in bfloat16 take 60 us,
 // 4.1 TB/s of K, Q and records.
 #include "delta_chunk.hpp"
 

@@ -187,7 +187,7 @@ hipError_t launch_rotary(const rotary_emu_t& a, hipStream_t stream) {
     if (p.total == 0 || a.size == 0 || p.a.heads[0] + p.a.heads[1] == 0) return hipSuccess;
     return by_dtype(a.dtype, [&](auto t) {
         using T = decltype(t);
-        // 16 bytes, then 8, then 4 at a time as rows, halves and the part
+        // 16 bytes, then 8, then an element at a time as rows, halves and the part
         // that is copied allow
         const auto fits = [&](int n) {
             const int bytes = n * (int)sizeof(T);

@@ -9,7 +9,9 @@ or float16); decays, strengths, states and tables are float32.
 A call runs on the current torch stream or on ``stream`` (a hipStream_t handle).
 What it allocates (outputs and a workspace that are not given) is allocated, and
 filled where it is, on the stream it runs on; the outputs are kept from reuse
-until the stream that is current in the call is through with them, too.
+until the stream that is current in the call is through with them, too.  No autograd
+graph is recorded, as by the package's other functions: the gradients have
+entries of their own.
 """
 from __future__ import annotations
 
@@ -290,7 +292,8 @@ def delta_emu_forward(q, k, v, g=None, beta=None, initial_state=None, *, scale=N
     None (no decay, beta = 1); states: (batch, value heads, key size, value
     size) float32, contiguous.  scale: key size ** -0.5 by default.
     cu_seqlens: int32 bounds of packed sequences (then batch is 1 and the states
-    are per sequence).  out, final_state (may be initial_state) and workspace
+    are per sequence; rows of no sequence are not written, and hold anything in an
+    out made here).  out, final_state (may be initial_state) and workspace
     (uint8, ``delta_emu_forward_workspace`` bytes) are allocated if None."""
     if not _calls:
         _start()
