@@ -36,8 +36,8 @@ constexpr int64_t kDeltaMostTasks = 1 << 21;
 constexpr int kDeltaMostThreads = 768;  // of a walk's block
 static_assert(2 * kDeltaMostTasks * kDeltaMostThreads < int64_t{1} << 32, "one launch");
 
-// Columns of the state that a block of a walk takes, at least but for short calls
-// (delta_chain.hip, delta_back.hip).
+// Columns of the state that a block of a walk takes (delta_chain.hip, delta_back.hip), where
+// there are enough blocks for all CUs; with fewer, it may take 16.
 struct DeltaColumns {
     int outputs, states, steps, back;
 };

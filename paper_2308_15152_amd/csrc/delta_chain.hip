@@ -28,8 +28,6 @@
 // further columns with V = 0, from the columns of the identity, which gives N and M of
 // S -> M S + N; then the states before the parts follow one from another
 // (delta_join.hip); then all parts are walked for their outputs.
-#include <type_traits>
-
 #include "delta_chunk.hpp"
 
 namespace sgemm_emu {
