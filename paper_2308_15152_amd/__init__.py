@@ -25,6 +25,8 @@ __all__ = [
     "householder_emu_batched", "householder_emu_batched_ex", "givens_emu_batched",
     "rotary_emu", "rotary_emu_table", "delta_emu_forward_workspace", "delta_emu_forward",
     "delta_emu_backward_workspace", "delta_emu_backward", "delta_emu_step",
+    "attention_emu_forward", "attention_emu_backward_workspace", "attention_emu_backward",
+    "attention_emu_step_workspace", "attention_emu_step",
     "sgemm_emu_split", "mfmae_num_elements", "mfmae_map", "mfmae_foreach", "mfmae_mma_probe",
     "sgemm_emu_strerror", "sgemm_emu_last_hip_error",
     "sgemm_emu_xcd_order", "sgemm_emu_tile_order", "sgemm_emu_block_order",
@@ -35,7 +37,7 @@ __all__ = [
     "Policy", "FLOW_AUTO", "FLOW_SPLIT", "FLOW_DIRECT", "FLOW_STAGED", "FLOW_REG",
     "TILE_AUTO", "TILE_64x64", "TILE_128x128", "TILE_256x128", "TILE_128x256",
     "SHAPE_16x16x32", "SHAPE_32x32x16", "USE_A", "USE_B", "USE_ACC",
-    "EXPORTED_SYMBOLS", "MIXING_SYMBOLS",
+    "EXPORTED_SYMBOLS", "MIXING_SYMBOLS", "ATTENTION_SYMBOLS",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -67,6 +69,11 @@ EXPORTED_SYMBOLS = (
 MIXING_SYMBOLS = (
     "rotary_emu", "rotary_emu_table", "delta_emu_forward_workspace", "delta_emu_forward",
     "delta_emu_backward_workspace", "delta_emu_backward", "delta_emu_step",
+)
+# Every symbol declared in include/attention_emu.h.
+ATTENTION_SYMBOLS = (
+    "attention_emu_forward", "attention_emu_backward_workspace", "attention_emu_backward",
+    "attention_emu_step_workspace", "attention_emu_step",
 )
 
 
@@ -171,6 +178,11 @@ def load():
         "delta_emu_backward_workspace": ([P], i64),
         "delta_emu_backward": ([P, P], i32),
         "delta_emu_step": ([P, P], i32),
+        "attention_emu_forward": ([P, P], i32),
+        "attention_emu_backward_workspace": ([P], i64),
+        "attention_emu_backward": ([P, P], i32),
+        "attention_emu_step_workspace": ([P], i64),
+        "attention_emu_step": ([P, P], i32),
         "sgemm_emu_split": ([i64, P, P, P, i32, P], i32),
         "mfmae_num_elements": ([i32, i32], i32),
         "mfmae_map": ([i32, i32, i32, i32, ip, ip], i32),
@@ -718,6 +730,10 @@ def mfmae_mma_probe(shape: int, a_lanes, b_lanes, *, stream=None):
     return d
 
 
+from .attention import (  # noqa: E402
+    attention_emu_backward, attention_emu_backward_workspace, attention_emu_forward,
+    attention_emu_step, attention_emu_step_workspace,
+)
 from .mixing import (  # noqa: E402  (uses the helpers above)
     delta_emu_backward, delta_emu_backward_workspace, delta_emu_forward,
     delta_emu_forward_workspace, delta_emu_step, rotary_emu, rotary_emu_table,

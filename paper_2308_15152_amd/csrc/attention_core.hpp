@@ -1,0 +1,230 @@
+// One pass of softmax attention over a range of keys, for a block's query rows.
+//
+// Per row, with scores s_j = q k_j (unscaled) and c = scale log2 e > 0, the pass keeps a
+// reference z (in units of c s), l = sum_j 2^(c s_j - z) and O = sum_j 2^(c s_j - z) v_j,
+// all in FP32.  z only moves, and O and l with it, where a row's largest score is more
+// than 2^kSlack above it: the weights then stay below 2^(kSlack + kBias) and the
+// result does not depend on z.
+//
+// The products are S^T = K Q^T and O^T = V^T P^T in 32 x 32 tiles: a lane holds
+// one query row, so that its reference, sum and rescaling are scalars of the lane, and
+// the weights of S^T's accumulator are the second product's operand in place.  Weights
+// are rounded to the inputs' type (11 or 8 bits, relative to each weight) for the matrix
+// instructions; l sums them before that.
+#pragma once
+
+#include "attention_tile.hpp"
+
+namespace sgemm_emu {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// kRowGroups waves with 32 rows each share the block's tiles of kKeys keys; or
+// (kRowGroups == 1) kKeyGroups waves with the same 32 rows take every
+// kKeyGroups-th tile, each in its own part of LDS, and are joined at the end.
+template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
+struct Attend {
+    static_assert(kRowGroups == 1 || kKeyGroups == 1, "");
+    static constexpr bool kShared = kRowGroups > 1;
+    static constexpr int kThreads = 64 * kRowGroups * kKeyGroups;
+    static constexpr int kRows = 32 * kRowGroups;
+    static constexpr int kTileBytes = kKeys * D * (int)sizeof(T);
+    static constexpr int kBuffers = kShared ? 2 : 1;
+    static constexpr int kTiles = kKeyGroups * kBuffers * 2 * kTileBytes;
+    static constexpr int kJoinRow = D + 4;  // floats
+    static constexpr int kJoin = kShared ? 0 : kKeyGroups * 32 * (kJoinRow + 2) * 4;
+    static constexpr int kLds = (kTiles > kJoin ? kTiles : kJoin) + 16;
+    static constexpr int kTileThreads = kShared ? kThreads : 64;
+    // FP16 weights keep 11 bits down to 2^-14: 2^-21 of a row's largest
+    static constexpr float kBias = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 7.0f : 0.0f;
+    static constexpr float kSlack = 8.0f;
+
+    // rows: query rows there are; the block takes row0 to row0 + kRows - 1.
+    // q_row(r): its elements; limit(r): how many keys it sees (not decreasing in r).
+    // k, v: row 0 of the keys and values; the pass goes over keys first to end - 1.
+    // out.begin(r, l, z), out.four(r, d, ...): results of a row.
+    template <class QRow, class Limit, class Out>
+    static __device__ __attribute__((always_inline)) void run(
+        char* lds, int rows, int row0, QRow q_row, Limit limit, const T* k, int64_t k_token,
+        const T* v, int64_t v_token, int first, int end, int size, float c, bool negative, Out out) {
+        using KV = Tile<T, D>;
+        constexpr int kBlocks = D / kBlock<T>;
+        constexpr int kParts = 32 / kBlock<T>;  // operand blocks of 32 keys
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int group = kShared ? 0 : wave;
+        const int wave_row = row0 + (kShared ? 32 * wave : 0);
+        const int tile_thread = kShared ? (int)threadIdx.x : lane;
+        char* tiles = lds + group * kBuffers * 2 * kTileBytes;
+        int* bad = reinterpret_cast<int*>(lds + kLds - 16);
+
+        const int row = wave_row + (lane & 31), last_row = rows - 1;
+        Frag<T> Q[kBlocks];
+        {
+            const T* p = q_row(min(row, last_row));
+#pragma unroll
+            for (int kb = 0; kb < kBlocks; ++kb) {
+                Q[kb] = load_chunk<T, kVec>(p, 2 * kb + half, size, row < rows);
+                if (negative)
+#pragma unroll
+                    for (int j = 0; j < kPer<T>; ++j) Q[kb][j] = -Q[kb][j];
+            }
+        }
+        // keys seen by the lane's row, by the wave's first and last one, by the block's
+        const auto seen = [&](int r) { return min(max(limit(min(r, last_row)), first), end); };
+        const int lim = seen(row), lim_min = seen(wave_row), lim_max = seen(wave_row + 31);
+        const int block_min = seen(row0), block_max = seen(row0 + kRows - 1);
+        const int count = (block_max - first + kKeys - 1) / kKeys;
+        // from this tile on, some row of the block does not see all of the keys
+        const int cleared = (block_min - first) / kKeys;
+
+        f32x16 O[D / 32];
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) O[dt] = f32x16{};
+        float l = 0.0f, z = -1e30f;
+        bool found = false;
+        if (threadIdx.x == 0) *bad = 0;
+        lds_barrier();
+
+        Staged<T, D, kKeys, kTileThreads, kVec> sk, sv;
+        const int step = kShared ? 1 : kKeyGroups;
+        const auto load = [&](int t) {
+            sk.load(k, k_token, first + t * kKeys, end, size, tile_thread);
+            sv.load(v, v_token, first + t * kKeys, end, size, tile_thread);
+        };
+        if (group < count) load(group);
+        for (int t = group; t < count; t += step) {
+            char* kt = tiles + (kShared ? (t & 1) * 2 * kTileBytes : 0);
+            char* vt = kt + kTileBytes;
+            sk.store(kt, tile_thread);
+            // values that are not finite reach only rows that see them: where some row
+            // does not, they are left out here and added at the end
+            if (t >= cleared) found |= sv.clear_not_finite();
+            sv.store(vt, tile_thread);
+            if (t + step < count) load(t + step);
+            if (kShared) lds_barrier();
+            const int key0 = first + t * kKeys;
+            if (key0 >= lim_max) continue;
+
+            f32x16 S[kKeys / 32];
+#pragma unroll
+            for (int s = 0; s < kKeys / 32; ++s) {
+                S[s] = f32x16{};
+#pragma unroll
+                for (int kb = 0; kb < kBlocks; ++kb)
+                    S[s] = mma(KV::along(kt, 32 * s, kb, lane), Q[kb], S[s]);
+            }
+            if (key0 + kKeys > lim_min) {
+#pragma unroll
+                for (int s = 0; s < kKeys / 32; ++s)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (key0 + 32 * s + acc_row(i, half) >= lim) S[s][i] = -__builtin_inff();
+            }
+            float top = S[0][0];
+#pragma unroll
+            for (int s = 0; s < kKeys / 32; ++s)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, S[s][i]);
+            const float want = max_halves(top) * c - kBias;
+            if (__any(want > z + kSlack)) {
+                const float to = want > z + kSlack ? want : z;
+                const float f = __builtin_amdgcn_exp2f(z - to);
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) O[dt][i] *= f;
+                l *= f;
+                z = to;
+            }
+#pragma unroll
+            for (int s = 0; s < kKeys / 32; ++s) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    S[s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s][i], c, -z));
+                    l += S[s][i];
+                }
+#pragma unroll
+                for (int kb = 0; kb < kParts; ++kb) {
+                    const Frag<T> P = operand<T>(S[s], kb);
+#pragma unroll
+                    for (int dt = 0; dt < D / 32; ++dt)
+                        O[dt] = mma(KV::across(vt, s * kParts + kb, 32 * dt, lane), P, O[dt]);
+                }
+            }
+        }
+        l = sum_halves(l);
+        if (found) *bad = 1;
+        __syncthreads();
+        const bool repair = *bad != 0;
+
+        if constexpr (kShared) {
+            if (row < rows) {
+                if (repair)
+                    for (int j = first + cleared * kKeys; j < lim; ++j)
+#pragma unroll
+                        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                O[dt][i] += not_finite(v + j * v_token, 32 * dt + acc_row(i, half), size);
+                const float f = l == 0.0f ? 0.0f : 1.0f / l;
+                if (half == 0) out.begin(row, l, z);
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        out.four(row, 32 * dt + acc_row(i, half), O[dt][i] * f, O[dt][i + 1] * f,
+                                 O[dt][i + 2] * f, O[dt][i + 3] * f);
+            }
+        } else {
+            float* join = reinterpret_cast<float*>(lds);
+            float* state = join + kKeyGroups * 32 * kJoinRow;
+            const int n = lane & 31;
+            float* mine = join + (wave * 32 + n) * kJoinRow;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<Pack<float, 4>::type*>(mine + 32 * dt + acc_row(i, half)) =
+                        Pack<float, 4>::type{O[dt][i], O[dt][i + 1], O[dt][i + 2], O[dt][i + 3]};
+            if (half == 0) state[2 * (wave * 32 + n)] = l, state[2 * (wave * 32 + n) + 1] = z;
+            __syncthreads();
+            for (int w = threadIdx.x; w < 32 * (D / 4); w += kThreads) {
+                const int r = w / (D / 4), d = w % (D / 4) * 4;
+                if (row0 + r >= rows) break;
+                float zs = -1e30f, ls = 0.0f;
+#pragma unroll
+                for (int g = 0; g < kKeyGroups; ++g) zs = fmaxf(zs, state[2 * (g * 32 + r) + 1]);
+                Pack<float, 4>::type x{};
+#pragma unroll
+                for (int g = 0; g < kKeyGroups; ++g) {
+                    const float f = __builtin_amdgcn_exp2f(state[2 * (g * 32 + r) + 1] - zs);
+                    ls += f * state[2 * (g * 32 + r)];
+                    const auto y = *reinterpret_cast<const Pack<float, 4>::type*>(
+                        join + (g * 32 + r) * kJoinRow + d);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+                }
+                const float f = ls == 0.0f ? 0.0f : 1.0f / ls;
+                if (repair) {
+                    const int to = seen(row0 + r);
+                    for (int j = first + cleared * kKeys; j < to; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] += not_finite(v + j * v_token, d + e, size);
+                }
+                if (d == 0) out.begin(row0 + r, ls, zs);
+                out.four(row0 + r, d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+            }
+        }
+    }
+
+    // Element d of a row of values if it is not finite, else 0.  A positive weight of infinity
+    // or NaN is the same.
+    static __device__ inline float not_finite(const T* p, int d, int size) {
+        const float x = d < size ? to_f32(p[d]) : 0.0f;
+        return __builtin_fabsf(x) < __builtin_inff() ? 0.0f : x;
+    }
+};
+
+}  // namespace sgemm_emu

@@ -13,21 +13,6 @@ namespace {
 
 using namespace sgemm_emu;
 
-bool known_dtype(int d) { return d >= SGEMM_EMU_F32 && d <= SGEMM_EMU_F16; }
-int64_t dtype_bytes(int d) { return d == SGEMM_EMU_F32 ? 4 : 2; }
-
-// A contiguous array of `bytes` bytes.
-Extent array(const void* p, __int128 bytes) {
-    Extent e{(uintptr_t)p, (uintptr_t)p, true};
-    if (p == nullptr || bytes <= 0) return e;
-    if (bytes > (__int128)(UINTPTR_MAX - e.lo)) {
-        e.ok = false;
-        return e;
-    }
-    e.hi = e.lo + (uintptr_t)bytes;
-    return e;
-}
-
 // Sizes that the delta entries share.
 template <class A>
 int check_sizes(const A& a) {
@@ -46,41 +31,6 @@ bool within_reach(std::initializer_list<sgemm_emu_view_t> views) {
     for (const sgemm_emu_view_t& v : views)
         if (v.token > kDeltaMostStride) return false;
     return true;
-}
-
-// Strides not negative, every output apart, no output over an input or another one.
-int check_tensors(std::initializer_list<Tensor> ins, std::initializer_list<Tensor> outs,
-                  std::initializer_list<Extent> arrays_in, std::initializer_list<Extent> arrays_out) {
-    for (const auto* list : {&ins, &outs})
-        for (const Tensor& t : *list) {
-            if (negative(t.v)) return SGEMM_EMU_ERR_STRIDE;
-            if (t.v.p != nullptr && !span(t).ok) return SGEMM_EMU_ERR_STRIDE;
-        }
-    if (!all_ok(arrays_in) || !all_ok(arrays_out)) return SGEMM_EMU_ERR_DIM;
-    for (const Tensor& o : outs)
-        if (o.v.p != nullptr && !apart(o)) return SGEMM_EMU_ERR_STRIDE;
-    const auto clear = [&](const Extent& o) {
-        for (const Tensor& t : ins)
-            if (t.v.p != nullptr && overlap(o, span(t))) return false;
-        for (const Extent& e : arrays_in)
-            if (overlap(o, e)) return false;
-        return true;
-    };
-    for (const Tensor& o : outs) {
-        if (o.v.p == nullptr) continue;
-        if (!clear(span(o))) return SGEMM_EMU_ERR_ALIAS;
-        for (const Extent& e : arrays_out)
-            if (overlap(span(o), e)) return SGEMM_EMU_ERR_ALIAS;
-        for (const Tensor* other = outs.begin(); other != &o; ++other)
-            if (other->v.p != nullptr && meet(*other, o)) return SGEMM_EMU_ERR_ALIAS;
-    }
-    const Extent* prev = arrays_out.begin();
-    for (const Extent* e = prev; e != arrays_out.end(); ++e) {
-        for (const Extent* f = prev; f != e; ++f)
-            if (overlap(*e, *f)) return SGEMM_EMU_ERR_ALIAS;
-        if (!clear(*e)) return SGEMM_EMU_ERR_ALIAS;
-    }
-    return SGEMM_EMU_OK;
 }
 
 // Checks that do not look behind pointers, for the workspace queries and the

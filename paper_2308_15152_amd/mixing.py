@@ -43,8 +43,12 @@ def _start():
 
 
 def _launch(name, dev, stream, args):
+    _launch_on(_calls[name], name, dev, stream, args)
+
+
+def _launch_on(fn, name, dev, stream, args):
+    """Calls an entry point of that name with device dev as the current one."""
     torch = _pkg._torch
-    fn = _calls[name]
     if dev == torch._C._cuda_getDevice():
         rc = fn(args, torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream))
     else:
