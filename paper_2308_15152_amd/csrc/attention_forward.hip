@@ -24,7 +24,7 @@ struct ForwardOut {
 };
 
 template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
-__global__ __launch_bounds__(64 * kRowGroups * kKeyGroups) void attention_forward_kernel(
+__global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_forward_kernel(
     attention_emu_forward_t a, int64_t first_block) {
     using Pass = Attend<T, D, kRowGroups, kKeyGroups, kKeys, kVec>;
     __shared__ __attribute__((aligned(16))) char lds[Pass::kLds];
