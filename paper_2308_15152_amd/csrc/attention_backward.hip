@@ -62,7 +62,7 @@ constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
 
 template <class T, int D, bool kVec>
-__global__ __launch_bounds__(64 * kDqWaves) void attention_dq_kernel(attention_emu_backward_t a,
+__global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attention_emu_backward_t a,
                                                                      int64_t first_block) {
     using KV = Tile<T, D>;
     constexpr int kThreads = 64 * kDqWaves, kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;
@@ -193,7 +193,7 @@ constexpr int kDkvKeys = 32 * kDkvWaves;
 constexpr int kDkvRows = 32;
 
 template <class T, int D, bool kVec>
-__global__ __launch_bounds__(64 * kDkvWaves) void attention_dkv_kernel(attention_emu_backward_t a,
+__global__ __launch_bounds__(64 * kDkvWaves, 2) void attention_dkv_kernel(attention_emu_backward_t a,
                                                                        int64_t first_block) {
     using QD = Tile<T, D>;
     constexpr int kThreads = 64 * kDkvWaves, kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;

@@ -21,17 +21,19 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // kRowGroups waves with 32 rows each share the block's tiles of kKeys keys; or
-// (kRowGroups == 1) kKeyGroups waves with the same 32 rows take every
-// kKeyGroups-th tile, each in its own part of LDS, and are joined at the end.
+// (kRowGroups == 1) kKeyGroups waves with the same 32 rows take every kKeyGroups-th tile for
+// themselves, keys straight from memory as operands and values through a part of LDS of their
+// own, and are joined at the end.
 template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
 struct Attend {
     static_assert(kRowGroups == 1 || kKeyGroups == 1, "");
     static constexpr bool kShared = kRowGroups > 1;
+    static_assert(kShared || kKeys == 32, "");
     static constexpr int kThreads = 64 * kRowGroups * kKeyGroups;
     static constexpr int kRows = 32 * kRowGroups;
-    static constexpr int kTileBytes = kKeys * D * (int)sizeof(T);
-    static constexpr int kBuffers = kShared ? 2 : 1;
-    static constexpr int kTiles = kKeyGroups * kBuffers * 2 * kTileBytes;
+    static constexpr int kTileBytes = kKeys * Tile<T, D>::kRowBytes;
+    static constexpr int kPlace = (kShared ? 2 : 1) * kTileBytes;  // of a tile's keys and values
+    static constexpr int kTiles = kKeyGroups * 2 * kPlace;
     static constexpr int kJoinRow = D + 4;  // floats
     static constexpr int kJoin = kShared ? 0 : kKeyGroups * 32 * (kJoinRow + 2) * 4;
     static constexpr int kLds = (kTiles > kJoin ? kTiles : kJoin) + 16;
@@ -43,7 +45,7 @@ struct Attend {
     // rows: query rows there are; the block takes row0 to row0 + kRows - 1.
     // q_row(r): its elements; limit(r): how many keys it sees (not decreasing in r).
     // k, v: row 0 of the keys and values; the pass goes over keys first to end - 1.
-    // out.begin(r, l, z), out.four(r, d, ...): results of a row.
+    // out(r): where a row's results go; of that, sums(l, z) and four(d, ...).
     template <class QRow, class Limit, class Out>
     static __device__ __attribute__((always_inline)) void run(
         char* lds, int rows, int row0, QRow q_row, Limit limit, const T* k, int64_t k_token,
@@ -56,7 +58,7 @@ struct Attend {
         const int group = kShared ? 0 : wave;
         const int wave_row = row0 + (kShared ? 32 * wave : 0);
         const int tile_thread = kShared ? (int)threadIdx.x : lane;
-        char* tiles = lds + group * kBuffers * 2 * kTileBytes;
+        char* tiles = lds + group * 2 * kPlace;
         int* bad = reinterpret_cast<int*>(lds + kLds - 16);
 
         const int row = wave_row + (lane & 31), last_row = rows - 1;
@@ -85,35 +87,66 @@ struct Attend {
         float l = 0.0f, z = -1e30f;
         bool found = false;
         if (threadIdx.x == 0) *bad = 0;
+        if (kVec && size < Tile<T, D>::kRowBytes / (int)sizeof(T))
+            clear_lds(lds, kTiles, threadIdx.x, kThreads);
         lds_barrier();
 
-        Staged<T, D, kKeys, kTileThreads, kVec> sk, sv;
+        using Load = Flow<T, D, kKeys, kTileThreads, kVec>;
+        Load fk, fv;
+        Frag<T> K[kShared ? 1 : kBlocks];
         const int step = kShared ? 1 : kKeyGroups;
+        const uint32_t k_row = (uint32_t)k_token * sizeof(T), v_row = (uint32_t)v_token * sizeof(T);
+        const auto place = [&](int t) {
+            return tiles + ((kShared ? t : t / kKeyGroups) & 1) * kPlace;
+        };
+        if (kShared) fk.rows([&](int r) { return r * k_row; }, tile_thread);
+        fv.rows([&](int r) { return r * v_row; }, tile_thread);
         const auto load = [&](int t) {
-            sk.load(k, k_token, first + t * kKeys, end, size, tile_thread);
-            sv.load(v, v_token, first + t * kKeys, end, size, tile_thread);
+            const int key = first + t * kKeys, most = end - 1 - key;
+            if (most < kKeys - 1) {  // (rows behind the last one hold it again: they are masked)
+                if (kShared) fk.rows([&](int r) { return min(r, most) * k_row; }, tile_thread);
+                fv.rows([&](int r) { return min(r, most) * v_row; }, tile_thread);
+            }
+            if constexpr (kShared) {
+                fk.start(place(t), k + key * k_token, size, tile_thread);
+            } else {
+                const T* p = k + (key + min(lane & 31, most)) * k_token;
+#pragma unroll
+                for (int kb = 0; kb < kBlocks; ++kb)
+                    K[kb] = load_chunk<T, kVec>(p, 2 * kb + half, size, true);
+            }
+            fv.start(place(t) + kPlace - kTileBytes, v + key * v_token, size, tile_thread);
         };
         if (group < count) load(group);
         for (int t = group; t < count; t += step) {
-            char* kt = tiles + (kShared ? (t & 1) * 2 * kTileBytes : 0);
-            char* vt = kt + kTileBytes;
-            sk.store(kt, tile_thread);
+            char* kt = place(t);
+            char* vt = kt + kPlace - kTileBytes;
+            if (kShared) fk.finish(kt, tile_thread);
+            fv.finish(vt, tile_thread);
             // values that are not finite reach only rows that see them: where some row
             // does not, they are left out here and added at the end
-            if (t >= cleared) found |= sv.clear_not_finite();
-            sv.store(vt, tile_thread);
-            if (t + step < count) load(t + step);
-            if (kShared) lds_barrier();
+            if (t >= cleared) found |= Load::clear_not_finite(vt, tile_thread);
+            f32x16 S[kKeys / 32];
+            if constexpr (kShared) {
+                lds_barrier();
+                if (t + step < count) load(t + step);
+            } else {
+                S[0] = f32x16{};
+#pragma unroll
+                for (int kb = 0; kb < kBlocks; ++kb) S[0] = mma(K[kb], Q[kb], S[0]);
+                if (t + step < count) load(t + step);
+            }
             const int key0 = first + t * kKeys;
             if (key0 >= lim_max) continue;
 
-            f32x16 S[kKeys / 32];
+            if constexpr (kShared) {
 #pragma unroll
-            for (int s = 0; s < kKeys / 32; ++s) {
-                S[s] = f32x16{};
+                for (int s = 0; s < kKeys / 32; ++s) {
+                    S[s] = f32x16{};
 #pragma unroll
-                for (int kb = 0; kb < kBlocks; ++kb)
-                    S[s] = mma(KV::along(kt, 32 * s, kb, lane), Q[kb], S[s]);
+                    for (int kb = 0; kb < kBlocks; ++kb)
+                        S[s] = mma(KV::along(kt, 32 * s, kb, lane), Q[kb], S[s]);
+                }
             }
             if (key0 + kKeys > lim_min) {
 #pragma unroll
@@ -169,13 +202,14 @@ struct Attend {
                             for (int i = 0; i < 16; ++i)
                                 O[dt][i] += not_finite(v + j * v_token, 32 * dt + acc_row(i, half), size);
                 const float f = l == 0.0f ? 0.0f : 1.0f / l;
-                if (half == 0) out.begin(row, l, z);
+                const auto to = out(row);
+                if (half == 0) to.sums(l, z);
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4)
-                        out.four(row, 32 * dt + acc_row(i, half), O[dt][i] * f, O[dt][i + 1] * f,
-                                 O[dt][i + 2] * f, O[dt][i + 3] * f);
+                        to.four(32 * dt + acc_row(i, half), O[dt][i] * f, O[dt][i + 1] * f,
+                                O[dt][i + 2] * f, O[dt][i + 3] * f);
             }
         } else {
             float* join = reinterpret_cast<float*>(lds);
@@ -213,8 +247,9 @@ struct Attend {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] += not_finite(v + j * v_token, d + e, size);
                 }
-                if (d == 0) out.begin(row0 + r, ls, zs);
-                out.four(row0 + r, d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+                const auto to = out(row0 + r);
+                if (d == 0) to.sums(ls, zs);
+                to.four(d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
             }
         }
     }

@@ -8,43 +8,41 @@ namespace sgemm_emu {
 namespace {
 
 template <class T, bool kVec>
-struct ForwardOut {
-    const attention_emu_forward_t& a;
-    T* o;        // of the sequence's first token, key head's first query head
+struct ForwardRow {
+    T* o;
     float* lse;  // or null
-    int group;
-    __device__ inline void begin(int r, float l, float z) const {
+    int size;
+    __device__ inline void sums(float l, float z) const {
         if (lse != nullptr)
-            lse[r / group * a.lse.token + r % group * a.lse.head] =
-                l == 0.0f ? -__builtin_inff() : (z + __builtin_amdgcn_logf(l)) * kLn2;
+            *lse = l == 0.0f ? -__builtin_inff() : (z + __builtin_amdgcn_logf(l)) * kLn2;
     }
-    __device__ inline void four(int r, int d, float x, float y, float z, float w) const {
-        store_four<T, kVec>(o + r / group * a.o.token + r % group * a.o.head, d, a.size, x, y, z, w);
+    __device__ inline void four(int d, float x, float y, float z, float w) const {
+        store_four<T, kVec>(o, d, size, x, y, z, w);
     }
 };
 
 template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
 __global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_forward_kernel(
-    attention_emu_forward_t a, int64_t first_block) {
+    attention_emu_forward_t a, int first_block) {
     using Pass = Attend<T, D, kRowGroups, kKeyGroups, kKeys, kVec>;
     __shared__ __attribute__((aligned(16))) char lds[Pass::kLds];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
-    const int64_t block = first_block + blockIdx.x;
+    const int block = first_block + (int)blockIdx.x;
     int n, head, tile;
     if (packed) {
-        head = (int)(block % a.k_heads);
+        head = block % a.k_heads;
         const Place p = find_part(a.cu_seqlens, a.batch, a.tokens, group, Pass::kRows,
-                                  (int)(block / a.k_heads));
+                                  block / a.k_heads);
         if (!p.found) return;
         n = p.n, tile = p.tile;
     } else {
         // the last rows of all sequences first: with a causal mask they take longest
         const int pairs = a.batch * a.k_heads;
         const int tiles = (a.tokens * group + Pass::kRows - 1) / Pass::kRows;
-        const int pair = (int)(block % pairs);
+        const int pair = block % pairs;
         n = pair / a.k_heads, head = pair % a.k_heads;
-        tile = tiles - 1 - (int)(block / pairs);
+        tile = tiles - 1 - block / pairs;
     }
     const Span sq = span_of(a.cu_seqlens, n, a.tokens);
     const Span sk = span_of(a.cu_keys, n, a.keys);
@@ -53,7 +51,12 @@ __global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_for
     const T* k = row_of<T>(a.k, packed, n, sk, head);
     const T* v = row_of<T>(a.v, packed, n, sk, head);
     float* lse = a.lse.p == nullptr ? nullptr : row_of<float>(a.lse, packed, n, sq, head * group);
-    const ForwardOut<T, kVec> out{a, row_of<T>(a.o, packed, n, sq, head * group), lse, group};
+    T* o = row_of<T>(a.o, packed, n, sq, head * group);
+    const auto out = [&](int r) {
+        const int token = r / group, h = r % group;
+        return ForwardRow<T, kVec>{o + token * a.o.token + h * a.o.head,
+                                   lse ? lse + token * a.lse.token + h * a.lse.head : nullptr, a.size};
+    };
     const int shift = sk.count - sq.count + 1;
     Pass::run(
         lds, rows, tile * Pass::kRows,
@@ -68,7 +71,7 @@ hipError_t launch(const attention_emu_forward_t& a, hipStream_t stream) {
     const int64_t parts = most_parts(a.batch, (int64_t)a.tokens * group, 32 * kRowGroups,
                                      a.cu_seqlens != nullptr);
     return launch_blocks(attention_forward_kernel<T, D, kRowGroups, kKeyGroups, kKeys, kVec>,
-                         parts * a.k_heads, 64 * kRowGroups * kKeyGroups, 0, stream, a);
+                         parts * a.k_heads, 64 * kRowGroups * kKeyGroups, stream, a);
 }
 
 }  // namespace
@@ -81,7 +84,9 @@ hipError_t launch_attention_forward(const attention_emu_forward_t& args, hipStre
                      rows_aligned16(a.v, e) && rows_aligned16(a.o, e);
     return by_form(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
         using T = decltype(t);
-        return launch<T, decltype(d)::value, 4, 1, 64, decltype(vec)::value != 0>(a, stream);
+        constexpr int D = decltype(d)::value;
+        constexpr int kKeys = sizeof(T) == 2 || D <= 64 ? 64 : 32;
+        return launch<T, D, 4, 1, kKeys, decltype(vec)::value != 0>(a, stream);
     });
 }
 

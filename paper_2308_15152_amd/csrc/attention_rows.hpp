@@ -54,14 +54,15 @@ inline bool rows_aligned16(const sgemm_emu_view_t& v, int elem) {
     return (uintptr_t)v.p % 16 == 0 && v.batch % n == 0 && v.token % n == 0 && v.head % n == 0;
 }
 
-// Launches `blocks` blocks of a kernel that takes the number of its first block last.
+// Launches `blocks` blocks (below 2^31) of a kernel that takes the number of its first block
+// last.
 template <class Kernel, class... Args>
-inline hipError_t launch_blocks(Kernel kernel, int64_t blocks, int threads, int lds,
-                                hipStream_t stream, const Args&... args) {
+inline hipError_t launch_blocks(Kernel kernel, int64_t blocks, int threads, hipStream_t stream,
+                                const Args&... args) {
     constexpr int64_t kMost = 1 << 21;  // below 2^31 threads
     for (int64_t first = 0; first < blocks; first += kMost) {
         const unsigned n = (unsigned)(blocks - first < kMost ? blocks - first : kMost);
-        hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), lds, stream, args..., first);
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), 0, stream, args..., (int)first);
         if (hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
@@ -79,7 +80,7 @@ inline hipError_t by_form(int dtype, int size, bool vec, F&& f) {
         const auto with = [&](auto d) {
             return vec ? f(t, d, Number<1>{}) : f(t, d, Number<0>{});
         };
-        return size <= 64 ? with(Number<64>{}) : with(Number<128>{});
+        return size <= 64 ? with(Number<64>{}) : size <= 96 ? with(Number<96>{}) : with(Number<128>{});
     });
 }
 

@@ -17,63 +17,64 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPrefixRows = 128;
 
+// Elements from one row of a part to the next.
+template <int D>
+constexpr int kStride = D <= 64 ? 64 : 128;
+
 struct StepArgs {
     attention_emu_step_t a;
     int prefix_parts, prefix_tiles, prefix_keys;  // parts, row tiles, keys of a part
     int own_parts;
-    float* parts;  // [part][row][D], or null: one part, written to o
+    float* parts;  // [part][row][kStride], or null: one part, written to o
     float* logs;   // [part][row], base 2
     int64_t rows;  // batch x tokens x q_heads
 };
 
-template <class T, int D, bool kVec>
-struct StepOut {
-    const StepArgs& s;
-    int part, first, head;  // row r is token first + r / group, query head head + r % group
-    int group;
-    __device__ inline int64_t row(int r) const {
-        return (int64_t)(first + r / group) * s.a.q_heads + head + r % group;
+template <class T, bool kVec>
+struct StepRow {
+    T* o;         // or, of a part,
+    float* part;  // its row
+    float* log;
+    int size;
+    __device__ inline void sums(float l, float z) const {
+        if (part != nullptr) *log = l == 0.0f ? -__builtin_inff() : z + __builtin_amdgcn_logf(l);
     }
-    __device__ inline void begin(int r, float l, float z) const {
-        if (s.parts != nullptr)
-            s.logs[part * s.rows + row(r)] =
-                l == 0.0f ? -__builtin_inff() : z + __builtin_amdgcn_logf(l);
-    }
-    __device__ inline void four(int r, int d, float x, float y, float z, float w) const {
-        if (s.parts != nullptr) {
-            if (d < s.a.size)
-                *reinterpret_cast<Pack<float, 4>::type*>(s.parts + (part * s.rows + row(r)) * D + d) =
-                    Pack<float, 4>::type{x, y, z, w};
-        } else {
-            const int t = first + r / group, h = head + r % group;
-            T* o = static_cast<T*>(s.a.o.p) + t / s.a.tokens * s.a.o.batch +
-                   t % s.a.tokens * s.a.o.token + h * s.a.o.head;
-            store_four<T, kVec>(o, d, s.a.size, x, y, z, w);
-        }
+    __device__ inline void four(int d, float x, float y, float z, float w) const {
+        if (part == nullptr)
+            store_four<T, kVec>(o, d, size, x, y, z, w);
+        else if (d < size)
+            *reinterpret_cast<Pack<float, 4>::type*>(part + d) = Pack<float, 4>::type{x, y, z, w};
     }
 };
 
 template <class T, int D, bool kVec>
-__global__ __launch_bounds__(kThreads) void attention_step_kernel(StepArgs s, int64_t first_block) {
-    using Prefix = Attend<T, D, 4, 1, sizeof(T) == 2 ? 64 : 32, kVec>;
+__global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s, int first_block) {
+    using Prefix = Attend<T, D, 4, 1, sizeof(T) == 2 || D <= 64 ? 64 : 32, kVec>;
     using Own = Attend<T, D, 1, 4, 32, kVec>;
     constexpr int kLds = Prefix::kLds > Own::kLds ? Prefix::kLds : Own::kLds;
     __shared__ __attribute__((aligned(16))) char lds[kLds];
     const attention_emu_step_t& a = s.a;
     const int group = a.q_heads / a.k_heads;
     const float c = __builtin_fabsf(a.scale) * kLog2e;
-    int64_t block = first_block + blockIdx.x;
-    const int64_t prefix_blocks = (int64_t)s.prefix_parts * s.prefix_tiles * a.k_heads;
+    int block = first_block + (int)blockIdx.x;
+    const int prefix_blocks = s.prefix_parts * s.prefix_tiles * a.k_heads;
+    // results of part p for query head h of token t of all
+    const auto out_of = [&](int p, int t, int h) {
+        const int64_t row = (int64_t)t * a.q_heads + h;
+        T* o = static_cast<T*>(a.o.p) + t / a.tokens * a.o.batch + t % a.tokens * a.o.token +
+               h * a.o.head;
+        return StepRow<T, kVec>{o, s.parts ? s.parts + (p * s.rows + row) * kStride<D> : nullptr,
+                                s.logs + p * s.rows + row, a.size};
+    };
     const auto q_row = [&](int t, int h) {
         return static_cast<const T*>(a.q.p) + t / a.tokens * a.q.batch + t % a.tokens * a.q.token +
                h * a.q.head;
     };
     if (block < prefix_blocks) {
-        const int head = (int)(block % a.k_heads);
-        const int64_t rest = block / a.k_heads;
-        const int part = (int)(rest % s.prefix_parts), tile = (int)(rest / s.prefix_parts);
+        const int head = block % a.k_heads, rest = block / a.k_heads;
+        const int part = rest % s.prefix_parts, tile = rest / s.prefix_parts;
         const int first = part * s.prefix_keys, end = min(first + s.prefix_keys, a.prefix);
-        const StepOut<T, D, kVec> out{s, part, 0, head * group, group};
+        const auto out = [&](int r) { return out_of(part, r / group, head * group + r % group); };
         Prefix::run(
             lds, a.batch * a.tokens * group, tile * kPrefixRows,
             [&](int r) { return q_row(r / group, head * group + r % group); },
@@ -85,18 +86,18 @@ __global__ __launch_bounds__(kThreads) void attention_step_kernel(StepArgs s, in
     }
     block -= prefix_blocks;
     const int row_tiles = (a.tokens * group + 31) / 32;
-    const int head = (int)(block % a.k_heads);
-    int64_t rest = block / a.k_heads;
-    const int tile = (int)(rest % row_tiles);
-    rest /= row_tiles;
-    const int part = (int)(rest % s.own_parts), n = (int)(rest / s.own_parts);
+    const int head = block % a.k_heads, rest = block / a.k_heads;
+    const int tile = rest % row_tiles, part = rest / row_tiles % s.own_parts;
+    const int n = rest / row_tiles / s.own_parts;
     const int slot = a.slots == nullptr ? n : a.slots[n];
     const bool in = slot >= 0 && slot < a.n_slots;
     const int keys = in ? min(max(a.lengths[n], 0), a.capacity) : 0;
     const int shift = keys - a.tokens + 1;
     const int each = ((keys + s.own_parts - 1) / s.own_parts + 31) / 32 * 32;
     const int first = min(part * each, keys), end = min(first + each, keys);
-    const StepOut<T, D, kVec> out{s, s.prefix_parts + part, n * a.tokens, head * group, group};
+    const auto out = [&](int r) {
+        return out_of(s.prefix_parts + part, n * a.tokens + r / group, head * group + r % group);
+    };
     const int64_t at = in ? slot : 0;
     Own::run(
         lds, a.tokens * group, tile * 32,
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void attention_step_kernel(StepArgs s, in
 // o = sum_p 2^(log_p - z) part_p / sum_p 2^(log_p - z), z the largest.
 template <class T, int D, bool kVec>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(StepArgs s, int parts,
-                                                                  int64_t first_block) {
+                                                                  int first_block) {
     const attention_emu_step_t& a = s.a;
     const int64_t w = (first_block + blockIdx.x) * kThreads + threadIdx.x;
     const int64_t row = w / (D / 4);
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(StepArgs s, in
             const float f = __builtin_amdgcn_exp2f(log - z);
             l += f;
             const auto y = *reinterpret_cast<const Pack<float, 4>::type*>(
-                s.parts + (p * s.rows + row) * D + d);
+                s.parts + (p * s.rows + row) * kStride<D> + d);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] += f * y[j];
         }
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(StepArgs s, in
     store_four<T, kVec>(o, d, a.size, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
 }
 
-int padded(int size) { return size <= 64 ? 64 : 128; }
+int padded(int size) { return size <= 64 ? 64 : 128; }  // kStride
 
 // How the keys are cut.
 StepArgs cut(const attention_emu_step_t& a) {
@@ -196,12 +197,13 @@ hipError_t launch_attention_step(const attention_emu_step_t& a, hipStream_t stre
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
-        if (hipError_t e = launch_blocks(attention_step_kernel<T, D, kVec>, blocks, kThreads, 0,
-                                         stream, s))
+        if (hipError_t e = launch_blocks(attention_step_kernel<T, D, kVec>, blocks, kThreads, stream,
+                                         s))
             return e;
         if (parts == 1) return hipSuccess;
-        const int64_t joins = (s.rows * (D / 4) + kThreads - 1) / kThreads;
-        return launch_blocks(attention_join_kernel<T, D, kVec>, joins, kThreads, 0, stream, s, parts);
+        constexpr int kRows = kThreads / (kStride<D> / 4);
+        return launch_blocks(attention_join_kernel<T, D, kVec>, (s.rows + kRows - 1) / kRows, kThreads,
+                             stream, s, parts);
     });
 }
 

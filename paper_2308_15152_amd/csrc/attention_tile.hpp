@@ -62,12 +62,12 @@ __device__ inline float sum_halves(float x) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-// Rows of D elements in LDS.  The 16-byte chunks of a row are permuted by
-// swizzle(row): eight rows read at one chunk, and four rows read at two
+// Rows of up to D elements in LDS, 64 or 128 apart.  The 16-byte chunks of a row are
+// permuted by swizzle(row): eight rows read at one chunk, and four rows read at two
 // neighbouring ones, are on different banks.
 template <class T, int D>
 struct Tile {
-    static constexpr int kRowBytes = D * (int)sizeof(T);
+    static constexpr int kRowBytes = (D <= 64 ? 64 : 128) * (int)sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
 
     static __device__ inline int swizzle(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
@@ -136,46 +136,98 @@ __device__ inline Frag<T> load_chunk(const T* row, int c, int size, bool inside)
     return f;
 }
 
-// kRows rows of a head on their way to LDS through registers of kThreads threads:
-// loaded a tile ahead, written when the tile's place is free.
-template <class T, int D, int kRows, int kThreads, bool kVec>
-struct Staged {
-    static constexpr int kChunks = Tile<T, D>::kChunks;
-    static constexpr int kEach = kRows * kChunks / kThreads;
-    static_assert(kEach * kThreads == kRows * kChunks && kThreads % kChunks == 0, "");
-    Frag<T> f[kEach];
+// Address of LDS as the instructions take it.
+__device__ inline uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
 
-    // Rows first to first + kRows - 1 of p; zeros from row `end` on.
-    __device__ inline void load(const T* p, int64_t token, int first, int end, int size, int thread) {
-        const int c = thread % kChunks, r0 = thread / kChunks;
-        const T* base = p + (int64_t)first * token;
+// kRows rows of a head on their way from memory to a tile, moved by kThreads threads.
+//   rows(f): f(r) is the distance in bytes of row r from the first address
+//   start(tile, first): the loads; `first` is the same for all lanes
+//   finish(tile): the rows are there, for this thread's part; a barrier makes it all of them
+// kVec: straight from memory to LDS, 16 bytes a lane; what a tile holds behind `size`
+// elements is not written and has to be zero before.  Else through registers, an element at
+// a time.
+template <class T, int D, int kRows, int kThreads, bool kVec>
+struct Flow {
+    using To = Tile<T, D>;
+    static constexpr int kChunks = To::kChunks;
+    static constexpr int kEach = kRows * kChunks / kThreads;
+    static constexpr int kRowsApart = kThreads / kChunks;
+    static_assert(kEach * kThreads == kRows * kChunks && kRowsApart * kChunks == kThreads, "");
+    Frag<T> f[kVec ? 1 : kEach];
+    uint32_t off[kEach];
+
+    // Row of the thread's first chunk; number of a chunk in its row.
+    static __device__ inline int row(int thread) { return thread / kChunks; }
+    static __device__ inline int chunk(int thread, int i) {
+        return (thread % kChunks) ^ To::swizzle(row(thread) + i * kRowsApart);
+    }
+
+    template <class Distance>
+    __device__ inline void rows(Distance distance, int thread) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            off[i] = distance(row(thread) + i * kRowsApart) + (kVec ? 16 * chunk(thread, i) : 0);
+    }
+
+    __device__ inline void start(char* tile, const T* first, int size, int thread) {
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(tile) + thread / 64 * 1024);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int r = r0 + i * (kThreads / kChunks);
-            f[i] = load_chunk<T, kVec>(base + (int)(r * (int)token), c, size, first + r < end);
+            const int c = chunk(thread, i);
+            if constexpr (kVec) {
+                // (the instruction adds 16 times the lane's number to m0; the builtin would
+                // make every later LDS read wait for it, whatever it reads)
+                if (c * kPer<T> < size)
+                    asm volatile(
+                        "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[i]),
+                        "s"(first), "s"(at + i * kThreads * 16)
+                        : "memory");
+            } else {
+                f[i] = load_chunk<T, false>(
+                    reinterpret_cast<const T*>(reinterpret_cast<const char*>(first) + off[i]), c, size,
+                    true);
+            }
         }
     }
-    __device__ inline void store(char* tile, int thread) const {
-        const int c = thread % kChunks, r0 = thread / kChunks;
+    __device__ inline void finish(char* tile, int thread) {
+        if constexpr (kVec) {
+            // (and this wave is through with what it read before from the places that are written next)
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            *reinterpret_cast<Frag<T>*>(tile + Tile<T, D>::at(r0 + i * (kThreads / kChunks), c)) = f[i];
+            for (int i = 0; i < kEach; ++i)
+                *reinterpret_cast<Frag<T>*>(tile + (thread + i * kThreads) * 16) = f[i];
+        }
     }
-    // Puts zeros in the place of values that are not finite; whether there were any.
-    __device__ inline bool clear_not_finite() {
+    // Puts zeros in the place of values that are not finite in the thread's part of a tile;
+    // whether there were any.
+    static __device__ inline bool clear_not_finite(char* tile, int thread) {
         bool any = false;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
+        for (int i = 0; i < kEach; ++i) {
+            Frag<T>* at = reinterpret_cast<Frag<T>*>(tile + (thread + i * kThreads) * 16);
+            Frag<T> x = *at;
+            bool here = false;
 #pragma unroll
             for (int j = 0; j < kPer<T>; ++j) {
-                const float x = to_f32(f[i][j]);
-                const bool bad = !(__builtin_fabsf(x) < __builtin_inff());
-                any |= bad;
-                if (bad) f[i][j] = from_f32<T>(0.0f);
+                const bool bad = !(__builtin_fabsf(to_f32(x[j])) < __builtin_inff());
+                here |= bad;
+                if (bad) x[j] = from_f32<T>(0.0f);
             }
+            if (here) *at = x;
+            any |= here;
+        }
         return any;
     }
 };
+
+// Zeros in `bytes` of LDS (a multiple of 16).
+__device__ inline void clear_lds(char* p, int bytes, int thread, int threads) {
+    for (int at = thread * 16; at < bytes; at += threads * 16)
+        *reinterpret_cast<Pack<float, 4>::type*>(p + at) = Pack<float, 4>::type{};
+}
 
 // Four neighbouring elements of an output row; kVec: rows are aligned to four
 // elements and size a multiple of four.
