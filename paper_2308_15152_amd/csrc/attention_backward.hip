@@ -63,27 +63,27 @@ constexpr int kDqKeys = 32;
 
 template <class T, int D, bool kVec>
 __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attention_emu_backward_t a,
-                                                                     int64_t first_block) {
+                                                                     int first_block) {
     using KV = Tile<T, D>;
     constexpr int kThreads = 64 * kDqWaves, kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;
-    constexpr int kTileBytes = kDqKeys * D * (int)sizeof(T);
+    constexpr int kTileBytes = kDqKeys * KV::kRowBytes;
     __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
-    const int64_t block = first_block + blockIdx.x;
+    const int block = first_block + (int)blockIdx.x;
     int n, head, tile;
     if (packed) {
-        head = (int)(block % a.k_heads);
+        head = block % a.k_heads;
         const Place p = find_part(a.cu_seqlens, a.batch, a.tokens, group, kDqRows,
-                                  (int)(block / a.k_heads));
+                                  block / a.k_heads);
         if (!p.found) return;
         n = p.n, tile = p.tile;
     } else {
         const int pairs = a.batch * a.k_heads;
         const int tiles = (a.tokens * group + kDqRows - 1) / kDqRows;
-        const int pair = (int)(block % pairs);
+        const int pair = block % pairs;
         n = pair / a.k_heads, head = pair % a.k_heads;
-        tile = tiles - 1 - (int)(block / pairs);
+        tile = tiles - 1 - block / pairs;
     }
     const Span sq = span_of(a.cu_seqlens, n, a.tokens);
     const Span sk = span_of(a.cu_keys, n, a.keys);
@@ -134,19 +134,32 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dQ[dt] = f32x16{};
     Fit fit;
-    Staged<T, D, kDqKeys, kThreads, kVec> st_k, st_v;
+    if (kVec && a.size < KV::kRowBytes / (int)sizeof(T)) {
+        clear_lds(lds, 4 * kTileBytes, threadIdx.x, kThreads);
+        lds_barrier();
+    }
+    Flow<T, D, kDqKeys, kThreads, kVec> fk, fv;
+    const uint32_t k_row = (uint32_t)a.k.token * sizeof(T), v_row = (uint32_t)a.v.token * sizeof(T);
+    const auto from = [&](int most) {  // (rows behind the last one hold it again: they are masked)
+        fk.rows([&](int r) { return min(r, most) * k_row; }, threadIdx.x);
+        fv.rows([&](int r) { return min(r, most) * v_row; }, threadIdx.x);
+    };
+    from(kDqKeys - 1);
     const auto load = [&](int t) {
-        st_k.load(k, a.k.token, t * kDqKeys, sk.count, a.size, threadIdx.x);
-        st_v.load(v, a.v.token, t * kDqKeys, sk.count, a.size, threadIdx.x);
+        const int key = t * kDqKeys, most = sk.count - 1 - key;
+        if (most < kDqKeys - 1) from(most);
+        char* to = lds + (t & 1) * 2 * kTileBytes;
+        fk.start(to, k + key * a.k.token, a.size, threadIdx.x);
+        fv.start(to + kTileBytes, v + key * a.v.token, a.size, threadIdx.x);
     };
     if (count > 0) load(0);
     for (int t = 0; t < count; ++t) {
         char* kt = lds + (t & 1) * 2 * kTileBytes;
         char* vt = kt + kTileBytes;
-        st_k.store(kt, threadIdx.x);
-        st_v.store(vt, threadIdx.x);
-        if (t + 1 < count) load(t + 1);
+        fk.finish(kt, threadIdx.x);
+        fv.finish(vt, threadIdx.x);
         lds_barrier();
+        if (t + 1 < count) load(t + 1);
         const int key0 = t * kDqKeys;
         if (key0 >= lim_max) continue;
         f32x16 S{}, dP;
@@ -188,48 +201,69 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
                                 dQ[dt][i + 1] * f, dQ[dt][i + 2] * f, dQ[dt][i + 3] * f);
 }
 
-constexpr int kDkvWaves = 4;
-constexpr int kDkvKeys = 32 * kDkvWaves;
-constexpr int kDkvRows = 32;
+// A block's waves: kKeyGroups times 32 keys, each shared by kRowGroups waves that take
+// 32 query rows of a tile each and are joined at the end.  As many waves as two for each SIMD,
+// where registers (FP32 of more than 96 elements) and LDS hold them.
+template <class T, int D>
+struct DkvShape {
+    static constexpr int kWide = sizeof(T) == 4 && D > 64;
+    static constexpr int kKeyGroups = kWide && D <= 96 ? 4 : 2;
+    static constexpr int kRowGroups = kWide ? 2 : 4;
+    static constexpr int kWaves = kKeyGroups * kRowGroups, kThreads = 64 * kWaves;
+    static constexpr int kKeys = 32 * kKeyGroups, kRows = 32 * kRowGroups;
+};
 
-template <class T, int D, bool kVec>
-__global__ __launch_bounds__(64 * kDkvWaves, 2) void attention_dkv_kernel(attention_emu_backward_t a,
-                                                                       int64_t first_block) {
+// The query rows of a key head in tiles: `tokens` tokens with `heads` of their `group` query
+// heads each, `parts` tiles for all of those.  One head to a tile where heads are so far
+// apart that distances within a token pass 32 bits.
+struct RowTiles {
+    int tokens, heads, parts;
+    __device__ inline RowTiles(int group, int rows, bool far)
+        : tokens(far ? rows : max(rows / group, 1)),
+          heads(far ? 1 : min(group, rows)),
+          parts((group + heads - 1) / heads) {}
+};
+
+template <class T, int D, bool kVec, class Shape = DkvShape<T, D>>
+__global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_dkv_kernel(
+    attention_emu_backward_t a, int first_block) {
     using QD = Tile<T, D>;
-    constexpr int kThreads = 64 * kDkvWaves, kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;
-    constexpr int kTileBytes = kDkvRows * D * (int)sizeof(T);
-    constexpr int kChunks = QD::kChunks, kEach = kDkvRows * kChunks / kThreads;
+    constexpr int kThreads = Shape::kThreads, kRows = Shape::kRows, kRowGroups = Shape::kRowGroups;
+    constexpr int kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;
+    constexpr int kTileBytes = kRows * QD::kRowBytes;
     // (the weights' shift; FP16 only)
     constexpr float kShift = kNarrow<T> ? 14.0f : 0.0f, kBack = kNarrow<T> ? 0x1p-14f : 1.0f;
     struct Row {
-        float z[kDkvRows], delta[kDkvRows];
-        int seen[kDkvRows];
+        float z[kRows], delta[kRows];
+        int seen[kRows];
     };
-    __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
+    constexpr int kJoin = (kRowGroups - 1) * Shape::kKeyGroups * D / 32 * 4096;
+    constexpr int kLds = 4 * kTileBytes > kJoin ? 4 * kTileBytes : kJoin;
+    __shared__ __attribute__((aligned(16))) char lds[kLds];
     __shared__ __attribute__((aligned(16))) Row of_rows[2];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
-    const int64_t block = first_block + blockIdx.x;
+    const int block = first_block + (int)blockIdx.x;
     int n, head, tile;
     if (packed) {
-        head = (int)(block % a.k_heads);
-        const Place p =
-            find_part(a.cu_keys, a.batch, a.keys, 1, kDkvKeys, (int)(block / a.k_heads));
+        head = block % a.k_heads;
+        const Place p = find_part(a.cu_keys, a.batch, a.keys, 1, Shape::kKeys, block / a.k_heads);
         if (!p.found) return;
         n = p.n, tile = p.tile;
     } else {
         // the first keys of all sequences first: with a causal mask they take longest
         const int pairs = a.batch * a.k_heads;
-        const int pair = (int)(block % pairs);
+        const int pair = block % pairs;
         n = pair / a.k_heads, head = pair % a.k_heads;
-        tile = (int)(block / pairs);
+        tile = block / pairs;
     }
     const Span sq = span_of(a.cu_seqlens, n, a.tokens);
     const Span sk = span_of(a.cu_keys, n, a.keys);
-    const int rows = sq.count * group;
-    const int lane = threadIdx.x & 63, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block_key = tile * kDkvKeys, wave_key = block_key + 32 * wave;
+    const int tokens = sq.count;
+    const int thread = threadIdx.x, lane = thread & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    const int row_group = wave % kRowGroups, key_group = wave / kRowGroups;
+    const int block_key = tile * Shape::kKeys, wave_key = block_key + 32 * key_group;
     const int key = wave_key + (lane & 31);
     const bool valid = key < sk.count;
     const int key_in = min(key, sk.count - 1);
@@ -243,86 +277,115 @@ __global__ __launch_bounds__(64 * kDkvWaves, 2) void attention_dkv_kernel(attent
             V[kb] = load_chunk<T, kVec>(v, 2 * kb + half, a.size, valid);
         }
     }
-    const int shift = sk.count - sq.count + 1;
-    // the first row that sees the block's first key, the wave's first and last one
-    const auto first_row = [&](int key) {
-        return a.causal ? min(max(key - shift + 1, 0), sq.count) * group : 0;
-    };
-    const int t0 = first_row(block_key) / kDkvRows;
-    const int count = (rows + kDkvRows - 1) / kDkvRows;
-    const int wave_from = first_row(wave_key), wave_all = first_row(wave_key + 31);
+    const int shift = sk.count - tokens + 1;  // token i sees keys below i + shift
+    const bool far = (int64_t)(group - 1) * max(a.q.head, a.d_o.head) > (1 << 28);
+    const RowTiles tiles(group, kRows, far);
+    const int count = (tokens + tiles.tokens - 1) / tiles.tokens * tiles.parts;
+    const int from = a.causal ? min(max(block_key - shift + 1, 0), tokens) : 0;
+    const int t0 = from / tiles.tokens * tiles.parts;
+    // tokens of the wave's rows, in a tile
+    const int wave_first = 32 * row_group / tiles.heads, wave_last = (32 * row_group + 31) / tiles.heads;
 
     f32x16 dK[D / 32], dV[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dK[dt] = f32x16{}, dV[dt] = f32x16{};
     Fit fit;
+    if (kVec && a.size < QD::kRowBytes / (int)sizeof(T)) {
+        clear_lds(lds, 4 * kTileBytes, thread, kThreads);
+        lds_barrier();
+    }
 
-    const int my_chunk = threadIdx.x % kChunks, my_row = threadIdx.x / kChunks;
     const T* q0 = row_of<T>(a.q, packed, n, sq, head * group);
     const T* d0 = row_of<T>(a.d_o, packed, n, sq, head * group);
     const float* lse0 = row_of<float>(a.lse, packed, n, sq, head * group);
     const float* delta0 = static_cast<const float*>(a.workspace) +
                           (packed ? sq.first : (int64_t)n * a.tokens) * a.q_heads + head * group;
-    Frag<T> st_q[kEach], st_d[kEach];
+    Flow<T, D, kRows, kThreads, kVec> fq, fd;
+    const auto distances = [&](int most_token, int most_head) {
+        const auto of = [&](const sgemm_emu_view_t& v) {
+            return [=](int r) {
+                return (uint32_t)(min(r / tiles.heads, most_token) * (int)v.token +
+                                  min(r % tiles.heads, most_head) * (int)v.head) *
+                       (uint32_t)sizeof(T);
+            };
+        };
+        fq.rows(of(a.q), thread);
+        fd.rows(of(a.d_o), thread);
+    };
+    distances(tiles.tokens - 1, tiles.heads - 1);
     float st_z = 0.0f, st_delta = 0.0f;
     int st_seen = 0;
     const auto load = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int row = t * kDkvRows + my_row + i * (kThreads / kChunks);
-            const int r = min(row, rows - 1), token = r / group, h = r % group;
-            st_q[i] = load_chunk<T, kVec>(q0 + token * a.q.token + h * a.q.head, my_chunk, a.size,
-                                          row < rows);
-            st_d[i] = load_chunk<T, kVec>(d0 + token * a.d_o.token + h * a.d_o.head, my_chunk,
-                                          a.size, row < rows);
-        }
-        if (threadIdx.x < kDkvRows) {
-            const int row = t * kDkvRows + threadIdx.x;
-            const int r = min(row, rows - 1), token = r / group, h = r % group;
-            const float lse = lse0[token * a.lse.token + h * a.lse.head];
-            const bool sees = row < rows && lse != -__builtin_inff();
-            st_z = sees ? lse * kLog2e - kShift : __builtin_inff();
-            st_delta = row < rows ? delta0[(int64_t)token * a.q_heads + h] : 0.0f;
-            st_seen = a.causal ? token + shift : sk.count;
+        const int token0 = t / tiles.parts * tiles.tokens, head0 = t % tiles.parts * tiles.heads;
+        const int tokens_in = min(tiles.tokens, tokens - token0);
+        const int heads_in = min(tiles.heads, group - head0);
+        if (tokens_in < tiles.tokens || tiles.parts > 1) distances(tokens_in - 1, heads_in - 1);
+        char* to = lds + (t & 1) * 2 * kTileBytes;
+        fq.start(to, q0 + token0 * a.q.token + head0 * a.q.head, a.size, thread);
+        fd.start(to + kTileBytes, d0 + token0 * a.d_o.token + head0 * a.d_o.head, a.size, thread);
+        if (thread < kRows) {
+            const int token = thread / tiles.heads, h = thread % tiles.heads;
+            st_z = __builtin_inff(), st_delta = 0.0f, st_seen = 0;
+            if (token < tokens_in && h < heads_in) {
+                const int64_t i = token0 + token;
+                const float lse = lse0[i * a.lse.token + (head0 + h) * a.lse.head];
+                // (rows that see nothing have lse -infinity)
+                if (lse != -__builtin_inff()) st_z = lse * kLog2e - kShift;
+                st_delta = -delta0[i * a.q_heads + head0 + h];
+                st_seen = a.causal ? token0 + token + shift : sk.count;
+            }
         }
     };
     if (t0 < count) load(t0);
     const float c = a.scale * kLog2e;
     for (int t = t0; t < count; ++t) {
         char* qt = lds + (t & 1) * 2 * kTileBytes;
-        char* dt_ = qt + kTileBytes;
+        char* ot = qt + kTileBytes;
         Row& rw = of_rows[t & 1];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int at = QD::at(my_row + i * (kThreads / kChunks), my_chunk);
-            *reinterpret_cast<Frag<T>*>(qt + at) = st_q[i];
-            *reinterpret_cast<Frag<T>*>(dt_ + at) = st_d[i];
-        }
-        if (threadIdx.x < kDkvRows) {
-            rw.z[threadIdx.x] = st_z;
-            rw.delta[threadIdx.x] = st_delta;
-            rw.seen[threadIdx.x] = st_seen;
-        }
-        if (t + 1 < count) load(t + 1);
+        fq.finish(qt, thread);
+        fd.finish(ot, thread);
+        if (thread < kRows) rw.z[thread] = st_z, rw.delta[thread] = st_delta, rw.seen[thread] = st_seen;
         lds_barrier();
-        if ((t + 1) * kDkvRows <= wave_from) continue;
-        f32x16 S{}, dP;
+        if (t + 1 < count) load(t + 1);
+        const int token0 = t / tiles.parts * tiles.tokens;
+        if (a.causal && token0 + wave_last + shift <= wave_key) continue;
+
+        const int row0 = 32 * row_group;
+        const auto per_row = [&](const float* x, int i) {  // rows of registers i to i + 3
+            return *reinterpret_cast<const Pack<float, 4>::type*>(x + row0 + 8 * (i / 4) + 4 * half);
+        };
+        f32x16 P{}, dP;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) dP[i] = -rw.delta[acc_row(i, half)];
+        for (int kb = 0; kb < kBlocks; ++kb) P = mma(QD::along(qt, row0, kb, lane), K[kb], P);
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) {
-            S = mma(QD::along(qt, 0, kb, lane), K[kb], S);
-            dP = mma(QD::along(dt_, 0, kb, lane), V[kb], dP);
+        for (int i = 0; i < 16; i += 4) {
+            const auto x = per_row(rw.delta, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) dP[i + j] = x[j];
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            S[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i], c, -rw.z[acc_row(i, half)]));
-            dP[i] *= S[i];
+        for (int kb = 0; kb < kBlocks; ++kb) dP = mma(QD::along(ot, row0, kb, lane), V[kb], dP);
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const auto x = per_row(rw.z, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                P[i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(P[i + j], c, -x[j]));
         }
-        if (t * kDkvRows < wave_all) {
+        const bool masked = a.causal && token0 + wave_first + shift <= wave_key + 31;
+        if (masked) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (key >= rw.seen[acc_row(i, half)]) S[i] = 0.0f, dP[i] = 0.0f;
+                if (key >= rw.seen[row0 + acc_row(i, half)]) P[i] = 0.0f, dP[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dP[i] *= P[i];
+#pragma unroll
+        for (int kb = 0; kb < kParts; ++kb) {
+            const Frag<T> x = operand<T>(P, kb);
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+                dV[dt] = mma(QD::across(ot + row0 * QD::kRowBytes, kb, 32 * dt, lane), x, dV[dt]);
         }
         if constexpr (kNarrow<T>) {
             fit.fit(dP, dK);
@@ -330,28 +393,46 @@ __global__ __launch_bounds__(64 * kDkvWaves, 2) void attention_dkv_kernel(attent
         }
 #pragma unroll
         for (int kb = 0; kb < kParts; ++kb) {
-            const Frag<T> p = operand<T>(S, kb), x = operand<T>(dP, kb);
+            const Frag<T> x = operand<T>(dP, kb);
 #pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt) {
-                dV[dt] = mma(QD::across(dt_, kb, 32 * dt, lane), p, dV[dt]);
-                dK[dt] = mma(QD::across(qt, kb, 32 * dt, lane), x, dK[dt]);
-            }
+            for (int dt = 0; dt < D / 32; ++dt)
+                dK[dt] = mma(QD::across(qt + row0 * QD::kRowBytes, kb, 32 * dt, lane), x, dK[dt]);
         }
     }
-    if (!valid) return;
-    const float fk = kNarrow<T> ? a.scale * kBack / fit.f : a.scale;
-    T* dk = row_of<T>(a.dk, packed, n, sk, head) + key * a.dk.token;
-    T* dv = row_of<T>(a.dv, packed, n, sk, head) + key * a.dv.token;
+
+    // the sums of the waves with the same keys, in the order of their rows
+    const auto join = [&](f32x16(&sum)[D / 32], float f, T* to) __attribute__((always_inline)) {
+        typedef Pack<float, 4>::type Four;
+        lds_barrier();
+        Four* const mine = reinterpret_cast<Four*>(lds) +
+                           ((row_group - 1) * Shape::kKeyGroups + key_group) * (D / 8) * 64 + lane;
+        if (row_group > 0) {
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
+            for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int d = 32 * dt + acc_row(i, half);
-            store_four<T, kVec>(dk, d, a.size, dK[dt][i] * fk, dK[dt][i + 1] * fk,
-                                dK[dt][i + 2] * fk, dK[dt][i + 3] * fk);
-            store_four<T, kVec>(dv, d, a.size, dV[dt][i] * kBack, dV[dt][i + 1] * kBack,
-                                dV[dt][i + 2] * kBack, dV[dt][i + 3] * kBack);
+                for (int i = 0; i < 4; ++i)
+                    mine[(dt * 4 + i) * 64] = Four{sum[dt][4 * i] * f, sum[dt][4 * i + 1] * f,
+                                                   sum[dt][4 * i + 2] * f, sum[dt][4 * i + 3] * f};
         }
+        lds_barrier();
+        if (row_group > 0 || !valid) return;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                Four x{sum[dt][4 * i] * f, sum[dt][4 * i + 1] * f, sum[dt][4 * i + 2] * f,
+                       sum[dt][4 * i + 3] * f};
+#pragma unroll
+                for (int g = 1; g < kRowGroups; ++g)
+                    x += reinterpret_cast<const Four*>(lds)[((g - 1) * Shape::kKeyGroups + key_group) *
+                                                                (D / 8) * 64 +
+                                                            (dt * 4 + i) * 64 + lane];
+                store_four<T, kVec>(to, 32 * dt + acc_row(4 * i, half), a.size, x[0], x[1], x[2], x[3]);
+            }
+    };
+    join(dV, kBack, row_of<T>(a.dv, packed, n, sk, head) + key_in * a.dv.token);
+    join(dK, kNarrow<T> ? a.scale * kBack / fit.f : a.scale,
+         row_of<T>(a.dk, packed, n, sk, head) + key_in * a.dk.token);
 }
 
 }  // namespace
@@ -371,16 +452,17 @@ hipError_t launch_attention_backward(const attention_emu_backward_t& args, hipSt
     const bool packed = a.cu_seqlens != nullptr;
     const int64_t group = a.q_heads / a.k_heads;
     const int64_t q_parts = most_parts(a.batch, a.tokens * group, kDqRows, packed) * a.k_heads;
-    const int64_t k_parts = most_parts(a.batch, a.keys, kDkvKeys, packed) * a.k_heads;
     return by_form(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
         if (a.tokens > 0)
             if (hipError_t e = launch_blocks(attention_dq_kernel<T, D, kVec>, q_parts, 64 * kDqWaves,
-                                             0, stream, a))
+                                             stream, a))
                 return e;
-        return launch_blocks(attention_dkv_kernel<T, D, kVec>, k_parts, 64 * kDkvWaves, 0, stream, a);
+        using Shape = DkvShape<T, D>;
+        const int64_t k_parts = most_parts(a.batch, a.keys, Shape::kKeys, packed) * a.k_heads;
+        return launch_blocks(attention_dkv_kernel<T, D, kVec>, k_parts, Shape::kThreads, stream, a);
     });
 }
 
