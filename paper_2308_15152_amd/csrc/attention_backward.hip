@@ -134,24 +134,21 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dQ[dt] = f32x16{};
     Fit fit;
-    if (kVec && a.size < KV::kRowBytes / (int)sizeof(T)) {
-        clear_lds(lds, 4 * kTileBytes, threadIdx.x, kThreads);
-        lds_barrier();
-    }
+    // (what is not loaded multiplies zeros and has to be finite)
+    clear_lds(lds, 4 * kTileBytes, threadIdx.x, kThreads);
+    lds_barrier();
     Flow<T, D, kDqKeys, kThreads, kVec> fk, fv;
     const uint32_t k_row = (uint32_t)a.k.token * sizeof(T), v_row = (uint32_t)a.v.token * sizeof(T);
-    const auto from = [&](int most) {  // (rows behind the last one hold it again: they are masked)
-        fk.rows([&](int r) { return min(r, most) * k_row; }, threadIdx.x);
-        fv.rows([&](int r) { return min(r, most) * v_row; }, threadIdx.x);
-    };
-    from(kDqKeys - 1);
+    fk.rows([&](int r) { return r * k_row; }, threadIdx.x);
+    fv.rows([&](int r) { return r * v_row; }, threadIdx.x);
     const auto load = [&](int t) {
         const int key = t * kDqKeys, most = sk.count - 1 - key;
-        if (most < kDqKeys - 1) from(most);
         char* to = lds + (t & 1) * 2 * kTileBytes;
-        fk.start(to, k + key * a.k.token, a.size, threadIdx.x);
-        fv.start(to + kTileBytes, v + key * a.v.token, a.size, threadIdx.x);
+        const auto there = [&](int, int r) { return r <= most; };
+        fk.start(to, k + key * a.k.token, a.size, threadIdx.x, there);
+        fv.start(to + kTileBytes, v + key * a.v.token, a.size, threadIdx.x, there);
     };
+    const int from_along = KV::from_along(lane), from_across = KV::from_across(lane);
     if (count > 0) load(0);
     for (int t = 0; t < count; ++t) {
         char* kt = lds + (t & 1) * 2 * kTileBytes;
@@ -162,13 +159,15 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
         if (t + 1 < count) load(t + 1);
         const int key0 = t * kDqKeys;
         if (key0 >= lim_max) continue;
+        const uint32_t k_along = KV::base(kt, from_along), v_along = KV::base(vt, from_along);
+        const uint32_t k_across = KV::base(kt, from_across);
         f32x16 S{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] = -delta;
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
-            S = mma(KV::along(kt, 0, kb, lane), Q[kb], S);
-            dP = mma(KV::along(vt, 0, kb, lane), DO[kb], dP);
+            S = mma(KV::along(k_along, 0, kb), Q[kb], S);
+            dP = mma(KV::along(v_along, 0, kb), DO[kb], dP);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
             const Frag<T> x = operand<T>(dP, kb);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
-                dQ[dt] = mma(KV::across(kt, kb, 32 * dt, lane), x, dQ[dt]);
+                dQ[dt] = mma(KV::across(k_across, kb, 32 * dt), x, dQ[dt]);
         }
     }
     if (!valid) return;
@@ -211,6 +210,13 @@ struct DkvShape {
     static constexpr int kRowGroups = kWide ? 2 : 4;
     static constexpr int kWaves = kKeyGroups * kRowGroups, kThreads = 64 * kWaves;
     static constexpr int kKeys = 32 * kKeyGroups, kRows = 32 * kRowGroups;
+    // How much of the keys' and values' operands is in registers; the rest, which
+    // does not fit, is read from LDS for every tile
+    static constexpr int kBlocks = D / kBlock<T>;
+    static constexpr bool kFull = sizeof(T) == 2 && D > 96;
+    static constexpr int kKeyBlocks = kFull ? kBlocks / 2 : kBlocks;
+    static constexpr int kValueBlocks = kFull ? 0 : kBlocks;
+    static constexpr int kLdsBlocks = 2 * kBlocks - kKeyBlocks - kValueBlocks;
 };
 
 // The query rows of a key head in tiles: `tokens` tokens with `heads` of their `group` query
@@ -241,6 +247,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     constexpr int kLds = 4 * kTileBytes > kJoin ? 4 * kTileBytes : kJoin;
     __shared__ __attribute__((aligned(16))) char lds[kLds];
     __shared__ __attribute__((aligned(16))) Row of_rows[2];
+    // [key group][block][lane]
+    __shared__ Frag<T> operands[Shape::kLdsBlocks > 0 ? Shape::kKeyGroups * Shape::kLdsBlocks * 64 : 1];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
     const int block = first_block + (int)blockIdx.x;
@@ -267,16 +275,33 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     const int key = wave_key + (lane & 31);
     const bool valid = key < sk.count;
     const int key_in = min(key, sk.count - 1);
-    Frag<T> K[kBlocks], V[kBlocks];
+    constexpr int kKeyBlocks = Shape::kKeyBlocks, kValueBlocks = Shape::kValueBlocks;
+    Frag<T> K[kKeyBlocks], V[kValueBlocks > 0 ? kValueBlocks : 1];
+    Frag<T>* const more = operands + key_group * Shape::kLdsBlocks * 64 + lane;
     {
         const T* k = row_of<T>(a.k, packed, n, sk, head) + key_in * a.k.token;
         const T* v = row_of<T>(a.v, packed, n, sk, head) + key_in * a.v.token;
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
-            K[kb] = load_chunk<T, kVec>(k, 2 * kb + half, a.size, valid);
-            V[kb] = load_chunk<T, kVec>(v, 2 * kb + half, a.size, valid);
+            const Frag<T> x = load_chunk<T, kVec>(k, 2 * kb + half, a.size, valid);
+            const Frag<T> y = load_chunk<T, kVec>(v, 2 * kb + half, a.size, valid);
+            if (kb < kKeyBlocks)
+                K[kb] = x;
+            else if (row_group == 0)
+                more[(kb - kKeyBlocks) * 64] = x;
+            if (kb < kValueBlocks)
+                V[kb] = y;
+            else if (row_group == 0)
+                more[(kBlocks - kKeyBlocks + kb - kValueBlocks) * 64] = y;
         }
     }
+    const auto key_block = [&](int kb) __attribute__((always_inline)) {
+        return kb < kKeyBlocks ? K[kb < kKeyBlocks ? kb : 0] : more[(kb - kKeyBlocks) * 64];
+    };
+    const auto value_block = [&](int kb) __attribute__((always_inline)) {
+        return kb < kValueBlocks ? V[kb < kValueBlocks ? kb : 0]
+                                 : more[(kBlocks - kKeyBlocks + kb - kValueBlocks) * 64];
+    };
     const int shift = sk.count - tokens + 1;  // token i sees keys below i + shift
     const bool far = (int64_t)(group - 1) * max(a.q.head, a.d_o.head) > (1 << 28);
     const RowTiles tiles(group, kRows, far);
@@ -290,10 +315,9 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dK[dt] = f32x16{}, dV[dt] = f32x16{};
     Fit fit;
-    if (kVec && a.size < QD::kRowBytes / (int)sizeof(T)) {
-        clear_lds(lds, 4 * kTileBytes, thread, kThreads);
-        lds_barrier();
-    }
+    // (what is not loaded multiplies zeros and has to be finite)
+    clear_lds(lds, 4 * kTileBytes, thread, kThreads);
+    lds_barrier();
 
     const T* q0 = row_of<T>(a.q, packed, n, sq, head * group);
     const T* d0 = row_of<T>(a.d_o, packed, n, sq, head * group);
@@ -301,62 +325,85 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     const float* delta0 = static_cast<const float*>(a.workspace) +
                           (packed ? sq.first : (int64_t)n * a.tokens) * a.q_heads + head * group;
     Flow<T, D, kRows, kThreads, kVec> fq, fd;
-    const auto distances = [&](int most_token, int most_head) {
-        const auto of = [&](const sgemm_emu_view_t& v) {
-            return [=](int r) {
-                return (uint32_t)(min(r / tiles.heads, most_token) * (int)v.token +
-                                  min(r % tiles.heads, most_head) * (int)v.head) *
-                       (uint32_t)sizeof(T);
-            };
+    // of the thread's chunks: their rows' tokens and heads in the tile, a byte each
+    uint32_t chunk_tokens[(fq.kEach + 3) / 4] = {}, chunk_heads[(fq.kEach + 3) / 4] = {};
+#pragma unroll
+    for (int i = 0; i < fq.kEach; ++i) {
+        const int r = fq.row(thread) + i * fq.kRowsApart;
+        chunk_tokens[i / 4] |= min(r / tiles.heads, 255) << i % 4 * 8;
+        chunk_heads[i / 4] |= r % tiles.heads << i % 4 * 8;
+    }
+    const auto distance = [&](const sgemm_emu_view_t& v) {
+        return [&](int r) {
+            return (uint32_t)(r / tiles.heads * (int)v.token + r % tiles.heads * (int)v.head) *
+                   (uint32_t)sizeof(T);
         };
-        fq.rows(of(a.q), thread);
-        fd.rows(of(a.d_o), thread);
     };
-    distances(tiles.tokens - 1, tiles.heads - 1);
-    float st_z = 0.0f, st_delta = 0.0f;
+    fq.rows(distance(a.q), thread);
+    fd.rows(distance(a.d_o), thread);
+    float st_lse = 0.0f, st_delta = 0.0f;
     int st_seen = 0;
+    int from_along = QD::from_along(lane), from_across = QD::from_across(lane);
     const auto load = [&](int t) {
         const int token0 = t / tiles.parts * tiles.tokens, head0 = t % tiles.parts * tiles.heads;
         const int tokens_in = min(tiles.tokens, tokens - token0);
         const int heads_in = min(tiles.heads, group - head0);
-        if (tokens_in < tiles.tokens || tiles.parts > 1) distances(tokens_in - 1, heads_in - 1);
         char* to = lds + (t & 1) * 2 * kTileBytes;
-        fq.start(to, q0 + token0 * a.q.token + head0 * a.q.head, a.size, thread);
-        fd.start(to + kTileBytes, d0 + token0 * a.d_o.token + head0 * a.d_o.head, a.size, thread);
+        const auto there = [&](int i, int) {
+            return (int)(chunk_tokens[i / 4] >> i % 4 * 8 & 255) < tokens_in &&
+                   (int)(chunk_heads[i / 4] >> i % 4 * 8 & 255) < heads_in;
+        };
         if (thread < kRows) {
-            const int token = thread / tiles.heads, h = thread % tiles.heads;
-            st_z = __builtin_inff(), st_delta = 0.0f, st_seen = 0;
+            int row = thread;
+            asm volatile("" : "+v"(row));
+            const int token = row / tiles.heads, h = row % tiles.heads;
+            st_lse = -__builtin_inff(), st_delta = 0.0f;
+            st_seen = a.causal ? token0 + token + shift : sk.count;
             if (token < tokens_in && h < heads_in) {
                 const int64_t i = token0 + token;
-                const float lse = lse0[i * a.lse.token + (head0 + h) * a.lse.head];
-                // (rows that see nothing have lse -infinity)
-                if (lse != -__builtin_inff()) st_z = lse * kLog2e - kShift;
-                st_delta = -delta0[i * a.q_heads + head0 + h];
-                st_seen = a.causal ? token0 + token + shift : sk.count;
+                st_lse = lse0[i * a.lse.token + (head0 + h) * a.lse.head];
+                st_delta = delta0[i * a.q_heads + head0 + h];
             }
         }
+        fq.start(to, q0 + token0 * a.q.token + head0 * a.q.head, a.size, thread, there);
+        fd.start(to + kTileBytes, d0 + token0 * a.d_o.token + head0 * a.d_o.head, a.size, thread,
+                 there);
     };
-    if (t0 < count) load(t0);
+    if (t0 < count) load(count - 1);
     const float c = a.scale * kLog2e;
-    for (int t = t0; t < count; ++t) {
+    // from the last rows, which all blocks of a head have, so that those that run beside each
+    // other find them in the caches
+    for (int t = count - 1; t >= t0; --t) {
         char* qt = lds + (t & 1) * 2 * kTileBytes;
         char* ot = qt + kTileBytes;
         Row& rw = of_rows[t & 1];
         fq.finish(qt, thread);
         fd.finish(ot, thread);
-        if (thread < kRows) rw.z[thread] = st_z, rw.delta[thread] = st_delta, rw.seen[thread] = st_seen;
+        if (thread < kRows) {
+            // (rows that see nothing, and those that are none, have lse -infinity)
+            rw.z[thread] = st_lse == -__builtin_inff() ? __builtin_inff() : st_lse * kLog2e - kShift;
+            rw.delta[thread] = -st_delta;
+            rw.seen[thread] = st_seen;
+        }
         lds_barrier();
-        if (t + 1 < count) load(t + 1);
+        if (t > t0) load(t - 1);
         const int token0 = t / tiles.parts * tiles.tokens;
         if (a.causal && token0 + wave_last + shift <= wave_key) continue;
 
+        // (addresses are formed for every tile: kept, they would take registers that the
+        // sums need)
+        asm volatile("" : "+v"(from_along), "+v"(from_across));
         const int row0 = 32 * row_group;
+        const uint32_t q_along = QD::base(qt + row0 * QD::kRowBytes, from_along);
+        const uint32_t o_along = QD::base(ot + row0 * QD::kRowBytes, from_along);
+        const uint32_t q_across = QD::base(qt + row0 * QD::kRowBytes, from_across);
+        const uint32_t o_across = QD::base(ot + row0 * QD::kRowBytes, from_across);
         const auto per_row = [&](const float* x, int i) {  // rows of registers i to i + 3
             return *reinterpret_cast<const Pack<float, 4>::type*>(x + row0 + 8 * (i / 4) + 4 * half);
         };
         f32x16 P{}, dP;
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) P = mma(QD::along(qt, row0, kb, lane), K[kb], P);
+        for (int kb = 0; kb < kBlocks; ++kb) P = mma(QD::along(q_along, 0, kb), key_block(kb), P);
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const auto x = per_row(rw.delta, i);
@@ -364,7 +411,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             for (int j = 0; j < 4; ++j) dP[i + j] = x[j];
         }
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) dP = mma(QD::along(ot, row0, kb, lane), V[kb], dP);
+        for (int kb = 0; kb < kBlocks; ++kb) dP = mma(QD::along(o_along, 0, kb), value_block(kb), dP);
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const auto x = per_row(rw.z, i);
@@ -385,7 +432,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             const Frag<T> x = operand<T>(P, kb);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
-                dV[dt] = mma(QD::across(ot + row0 * QD::kRowBytes, kb, 32 * dt, lane), x, dV[dt]);
+                dV[dt] = mma(QD::across(o_across, kb, 32 * dt), x, dV[dt]);
         }
         if constexpr (kNarrow<T>) {
             fit.fit(dP, dK);
@@ -396,7 +443,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             const Frag<T> x = operand<T>(dP, kb);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
-                dK[dt] = mma(QD::across(qt + row0 * QD::kRowBytes, kb, 32 * dt, lane), x, dK[dt]);
+                dK[dt] = mma(QD::across(q_across, kb, 32 * dt), x, dK[dt]);
         }
     }
 

@@ -81,6 +81,8 @@ struct Attend {
         // from this tile on, some row of the block does not see all of the keys
         const int cleared = (block_min - first) / kKeys;
 
+        const int from_along = KV::from_along(lane), from_across = KV::from_across(lane);
+
         f32x16 O[D / 32];
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) O[dt] = f32x16{};
@@ -103,19 +105,17 @@ struct Attend {
         fv.rows([&](int r) { return r * v_row; }, tile_thread);
         const auto load = [&](int t) {
             const int key = first + t * kKeys, most = end - 1 - key;
-            if (most < kKeys - 1) {  // (rows behind the last one hold it again: they are masked)
-                if (kShared) fk.rows([&](int r) { return min(r, most) * k_row; }, tile_thread);
-                fv.rows([&](int r) { return min(r, most) * v_row; }, tile_thread);
-            }
+            // (keys behind the last one are masked, and values there cleared if need be)
+            const auto there = [&](int, int r) { return r <= most; };
             if constexpr (kShared) {
-                fk.start(place(t), k + key * k_token, size, tile_thread);
+                fk.start(place(t), k + key * k_token, size, tile_thread, there);
             } else {
                 const T* p = k + (key + min(lane & 31, most)) * k_token;
 #pragma unroll
                 for (int kb = 0; kb < kBlocks; ++kb)
                     K[kb] = load_chunk<T, kVec>(p, 2 * kb + half, size, true);
             }
-            fv.start(place(t) + kPlace - kTileBytes, v + key * v_token, size, tile_thread);
+            fv.start(place(t) + kPlace - kTileBytes, v + key * v_token, size, tile_thread, there);
         };
         if (group < count) load(group);
         for (int t = group; t < count; t += step) {
@@ -145,7 +145,7 @@ struct Attend {
                     S[s] = f32x16{};
 #pragma unroll
                     for (int kb = 0; kb < kBlocks; ++kb)
-                        S[s] = mma(KV::along(kt, 32 * s, kb, lane), Q[kb], S[s]);
+                        S[s] = mma(KV::along(KV::base(kt, from_along), 32 * s, kb), Q[kb], S[s]);
                 }
             }
             if (key0 + kKeys > lim_min) {
@@ -183,7 +183,7 @@ struct Attend {
                     const Frag<T> P = operand<T>(S[s], kb);
 #pragma unroll
                     for (int dt = 0; dt < D / 32; ++dt)
-                        O[dt] = mma(KV::across(vt, s * kParts + kb, 32 * dt, lane), P, O[dt]);
+                        O[dt] = mma(KV::across(KV::base(vt, from_across), s * kParts + kb, 32 * dt), P, O[dt]);
                 }
             }
         }

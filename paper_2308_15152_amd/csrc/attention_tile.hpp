@@ -62,57 +62,76 @@ __device__ inline float sum_halves(float x) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// Address of LDS as the instructions take it.
+__device__ inline uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
 // Rows of up to D elements in LDS, 64 or 128 apart.  The 16-byte chunks of a row are
-// permuted by swizzle(row): eight rows read at one chunk, and four rows read at two
-// neighbouring ones, are on different banks.
+// permuted by swizzle(row), so that what the 64 banks serve at a time is on all of them: 16
+// rows at one chunk, or 4 rows at four neighbouring ones.
 template <class T, int D>
 struct Tile {
     static constexpr int kRowBytes = (D <= 64 ? 64 : 128) * (int)sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
+    static constexpr int kMask = kChunks == 8 ? 7 : 15;  // chunk bits that are permuted
+    static constexpr int kPlain = kChunks == 8 ? 3 : 4;  // how many
 
-    static __device__ inline int swizzle(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+    static __device__ inline int swizzle(int row) {
+        if (kChunks == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        return (row & 3) << 2 | (row >> 2 & 3);
+    }
     static __device__ inline int at(int row, int chunk) {
         return row * kRowBytes + ((chunk ^ swizzle(row)) << 4);
     }
 
-    // Block kb of the elements of rows row0 + lane % 32 (row0 a multiple of 8).
-    static __device__ inline Frag<T> along(const char* tile, int row0, int kb, int lane) {
-        const int half = lane >> 5, row = lane & 31;
-        // (chunk bits above the swizzle's three stay an immediate offset)
-        const int chunk = 2 * kb + half;
-        const int low = ((chunk & 7) ^ swizzle(row)) << 4;
-        return *reinterpret_cast<const Frag<T>*>(tile + row * kRowBytes + low + row0 * kRowBytes +
-                                                 ((chunk >> 3) << 7));
+    // What a lane's reads have in common: along(base(tile, from_along(lane)), ...).  The
+    // chunk's bits are added without carry, so that the permutation goes through.
+    static __device__ inline int from_along(int lane) { return at(lane & 31, lane >> 5); }
+    static __device__ inline int from_across(int lane) {
+        const int half = lane >> 5, i = lane & 15;
+        if (sizeof(T) == 2)
+            return at(4 * half + (i >> 2), 2 * (lane >> 4 & 1) + (i >> 1 & 1)) + 8 * (i & 1);
+        return at(4 * half, (lane & 31) >> 2) + 4 * (lane & 3);
+    }
+    static __device__ inline uint32_t base(const char* tile, int from) {
+        return lds_address(tile) + from;
+    }
+    // A chunk further on in a row (where it adds to bits that are zero so far).
+    static __device__ inline uint32_t chunk_on(uint32_t at, int chunk) {
+        return (at ^ ((chunk & kMask) << 4)) + (chunk >> kPlain << (kPlain + 4));
+    }
+
+    // Block kb of the elements of rows row0 + lane % 32 (row0 a multiple of 32).
+    static __device__ inline Frag<T> along(uint32_t base, int row0, int kb) {
+        typedef __attribute__((address_space(3))) const Frag<T> Lds;
+        return *(Lds*)(uintptr_t)(chunk_on(base, 2 * kb) + row0 * kRowBytes);
     }
 
     // Element d0 + lane % 32 of the rows of block kb (d0 a multiple of 32).
-    static __device__ inline Frag<T> across(const char* tile, int kb, int d0, int lane) {
-        const int half = lane >> 5;
+    static __device__ inline Frag<T> across(uint32_t base, int kb, int d0) {
         if constexpr (sizeof(T) == 2) {
             // a transposing read: 16 lanes bring 4 rows of 16 elements, 8 bytes each, and
             // every lane gets the 4 values of its column
             typedef short Short4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) Short4 LdsShort4;
-            const int i = lane & 15, row = 4 * half + (i >> 2);
-            const int chunk = d0 / 8 + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
-            const char* p = tile + row * kRowBytes + (((chunk & 7) ^ swizzle(row)) << 4) +
-                            8 * (i & 1) + ((chunk >> 3) << 7) + kb * 16 * kRowBytes;
+            typedef __attribute__((address_space(3))) Short4 Lds;
+            const uint32_t p = chunk_on(base, d0 / 8) + kb * 16 * kRowBytes;
             union {
                 Short4 part[2];
                 Frag<T> all;
             } u;
-            u.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)p);
-            u.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4*)(p + 8 * kRowBytes));
+            u.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(uintptr_t)p);
+            u.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (Lds*)(uintptr_t)((p ^ swizzle(8) << 4) + 8 * kRowBytes));
             return u.all;
         } else {
-            const int d = d0 + (lane & 31), chunk = d / 4;
+            typedef __attribute__((address_space(3))) const float Lds;
+            const uint32_t p = chunk_on(base, d0 / 4) + (kb >> 1) * 16 * kRowBytes;
             Frag<T> f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int row = 4 * half + j;
-                f[j] = *reinterpret_cast<const float*>(
-                    tile + kb * 8 * kRowBytes + row * kRowBytes +
-                    (((chunk & 7) ^ swizzle(row)) << 4) + ((chunk >> 3) << 7) + 4 * (d & 3));
+                const int row = (kb & 1) * 8 + j;
+                f[j] = *(Lds*)(uintptr_t)((p ^ swizzle(row) << 4) + row * kRowBytes);
             }
             return f;
         }
@@ -136,18 +155,14 @@ __device__ inline Frag<T> load_chunk(const T* row, int c, int size, bool inside)
     return f;
 }
 
-// Address of LDS as the instructions take it.
-__device__ inline uint32_t lds_address(const void* p) {
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
-}
-
 // kRows rows of a head on their way from memory to a tile, moved by kThreads threads.
 //   rows(f): f(r) is the distance in bytes of row r from the first address
-//   start(tile, first): the loads; `first` is the same for all lanes
+//   start(tile, first, there): the loads of those rows, by their number, that there(i, r) says
+//     are there; `first` is the same for all lanes, i the thread's chunk, r its row
 //   finish(tile): the rows are there, for this thread's part; a barrier makes it all of them
-// kVec: straight from memory to LDS, 16 bytes a lane; what a tile holds behind `size`
-// elements is not written and has to be zero before.  Else through registers, an element at
-// a time.
+// kVec: straight from memory to LDS, 16 bytes a lane; rows that are not there, and what a
+// tile holds behind `size` elements, are left as they were.  Else through registers, an
+// element at a time, with zeros in their place.
 template <class T, int D, int kRows, int kThreads, bool kVec>
 struct Flow {
     using To = Tile<T, D>;
@@ -171,15 +186,17 @@ struct Flow {
             off[i] = distance(row(thread) + i * kRowsApart) + (kVec ? 16 * chunk(thread, i) : 0);
     }
 
-    __device__ inline void start(char* tile, const T* first, int size, int thread) {
+    template <class There>
+    __device__ inline void start(char* tile, const T* first, int size, int thread, There there) {
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(tile) + thread / 64 * 1024);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int c = chunk(thread, i);
+            const bool in = there(i, row(thread) + i * kRowsApart);
             if constexpr (kVec) {
                 // (the instruction adds 16 times the lane's number to m0; the builtin would
                 // make every later LDS read wait for it, whatever it reads)
-                if (c * kPer<T> < size)
+                if (in && c * kPer<T> < size)
                     asm volatile(
                         "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[i]),
                         "s"(first), "s"(at + i * kThreads * 16)
@@ -187,7 +204,7 @@ struct Flow {
             } else {
                 f[i] = load_chunk<T, false>(
                     reinterpret_cast<const T*>(reinterpret_cast<const char*>(first) + off[i]), c, size,
-                    true);
+                    in);
             }
         }
     }
