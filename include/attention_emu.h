@@ -34,8 +34,12 @@ extern "C" {
  * A key or value that is not finite reaches only tokens that see it.
  * Scores, statistics and sums are FP32, FP32 products take FP32 operands; with 16-bit types the
  * weights e^{s_j - m} are rounded to the type before they multiply v, the results once.
+ * workspace: device memory, 256-byte aligned, at least what the _workspace query
+ *   for the same arguments returns (0 bytes where the query rows alone fill the device; else
+ *   the keys are cut into parts); its contents need not be kept.
  * Sizes: size <= 128, q_heads a multiple of k_heads, token strides <= 2^22, scale
- * finite and not zero, tokens x q_heads and keys below 2^31 for a sequence.
+ * finite and not zero, tokens x q_heads and keys below 2^31 for a sequence, and blocks of 32
+ * rows or keys below 2^30 in all.
  * Errors: _DIM (also keys != tokens without cu_keys), _UNSUPPORTED (dtype, sizes, scale,
  * strides and head counts above), _NULL, _STRIDE, _ALIAS, _HIP.
  */
@@ -46,8 +50,13 @@ typedef struct {
     const int32_t* cu_seqlens;
     const int32_t* cu_keys;
     sgemm_emu_view_t q, k, v, o, lse;
+    void* workspace;
+    int64_t workspace_bytes;
 } attention_emu_forward_t;
 
+/* Bytes of workspace, or a negative error; pointers are not looked at except for being
+ * NULL. */
+int64_t attention_emu_forward_workspace(const attention_emu_forward_t* a);
 int attention_emu_forward(const attention_emu_forward_t* a, hipStream_t stream);
 
 /* Its gradient: from o and lse of the forward pass and d_o (like o) to dq, dk, dv
@@ -59,8 +68,7 @@ int attention_emu_forward(const attention_emu_forward_t* a, hipStream_t stream);
  * tokens that see no key and of keys that no token sees are zero.  Where q, k, v, o or d_o is
  * not finite, any gradient of its sequence's key head may not be; other sequences and
  * heads are not reached.
- * workspace: device memory, 256-byte aligned, at least what the _workspace query
- *   for the same arguments returns; its contents need not be kept. */
+ * workspace: as above. */
 typedef struct {
     int32_t dtype, batch, tokens, keys, q_heads, k_heads, size, causal;
     float scale;
@@ -72,7 +80,6 @@ typedef struct {
     int64_t workspace_bytes;
 } attention_emu_backward_t;
 
-/* Bytes of workspace, or a negative error; pointers are not looked at. */
 int64_t attention_emu_backward_workspace(const attention_emu_backward_t* a);
 int attention_emu_backward(const attention_emu_backward_t* a, hipStream_t stream);
 

@@ -25,7 +25,8 @@ __all__ = [
     "householder_emu_batched", "householder_emu_batched_ex", "givens_emu_batched",
     "rotary_emu", "rotary_emu_table", "delta_emu_forward_workspace", "delta_emu_forward",
     "delta_emu_backward_workspace", "delta_emu_backward", "delta_emu_step",
-    "attention_emu_forward", "attention_emu_backward_workspace", "attention_emu_backward",
+    "attention_emu_forward_workspace", "attention_emu_forward",
+    "attention_emu_backward_workspace", "attention_emu_backward",
     "attention_emu_step_workspace", "attention_emu_step",
     "sgemm_emu_split", "mfmae_num_elements", "mfmae_map", "mfmae_foreach", "mfmae_mma_probe",
     "sgemm_emu_strerror", "sgemm_emu_last_hip_error",
@@ -72,7 +73,8 @@ MIXING_SYMBOLS = (
 )
 # Every symbol declared in include/attention_emu.h.
 ATTENTION_SYMBOLS = (
-    "attention_emu_forward", "attention_emu_backward_workspace", "attention_emu_backward",
+    "attention_emu_forward_workspace", "attention_emu_forward",
+    "attention_emu_backward_workspace", "attention_emu_backward",
     "attention_emu_step_workspace", "attention_emu_step",
 )
 
@@ -178,6 +180,7 @@ def load():
         "delta_emu_backward_workspace": ([P], i64),
         "delta_emu_backward": ([P, P], i32),
         "delta_emu_step": ([P, P], i32),
+        "attention_emu_forward_workspace": ([P], i64),
         "attention_emu_forward": ([P, P], i32),
         "attention_emu_backward_workspace": ([P], i64),
         "attention_emu_backward": ([P, P], i32),
@@ -732,7 +735,7 @@ def mfmae_mma_probe(shape: int, a_lanes, b_lanes, *, stream=None):
 
 from .attention import (  # noqa: E402
     attention_emu_backward, attention_emu_backward_workspace, attention_emu_forward,
-    attention_emu_step, attention_emu_step_workspace,
+    attention_emu_forward_workspace, attention_emu_step, attention_emu_step_workspace,
 )
 from .mixing import (  # noqa: E402  (uses the helpers above)
     delta_emu_backward, delta_emu_backward_workspace, delta_emu_forward,

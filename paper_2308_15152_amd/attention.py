@@ -16,7 +16,7 @@ from paper_2308_15152_amd.mixing import (
     _NO_VIEW, _device, _launch_on, _new, _packed, _scale, _view, _workspace)
 
 # The C argument structs of include/attention_emu.h.
-_FORWARD = struct.Struct("=8ifi2q20q")
+_FORWARD = struct.Struct("=8ifi2q20q2q")
 _BACKWARD = struct.Struct("=8ifi2q36q2q")
 _STEP = struct.Struct("=9if24q2q2q")
 
@@ -60,8 +60,34 @@ def _bounds(cu_seqlens, cu_keys, batch):
     return at, keys_at, n
 
 
+def _forward_args(q, k, v, out, lse, causal, scale, cu, cu_k, n):
+    b, t, n_keys, hq, hk, size = _sizes(q, k)
+    dtype, keys = q.dtype, (b, n_keys, hk, size)
+    results = _NO_VIEW * 2 if out is None else (
+        *_view(out, "out", q.shape, dtype),
+        *_view(lse, "lse", (b, t, hq), _pkg._torch.float32))
+    return _FORWARD.pack(
+        _dtypes[dtype], n, t, n_keys, hq, hk, size, 1 if causal else 0, _scale(scale, size), 0, cu,
+        cu_k, *_view(q, "q", q.shape, dtype), *_view(k, "k", keys, dtype),
+        *_view(v, "v", keys, dtype), *results, 0, 0)
+
+
+def attention_emu_forward_workspace(q, k, v, *, causal: bool = True, cu_seqlens=None,
+                                    cu_seqlens_k=None) -> int:
+    """Bytes of workspace that ``attention_emu_forward`` needs for these tensors (a
+    host-side query)."""
+    if not _calls:
+        _start()
+    cu, cu_k, n = _bounds(cu_seqlens, cu_seqlens_k, q.shape[0])
+    need = _calls["attention_emu_forward_workspace"](
+        _forward_args(q, k, v, None, None, causal, None, cu, cu_k, n))
+    if need < 0:
+        raise _pkg.SgemmEmuError(need, "attention_emu_forward_workspace")
+    return need
+
+
 def attention_emu_forward(q, k, v, *, causal: bool = True, scale=None, cu_seqlens=None,
-                          cu_seqlens_k=None, out=None, lse=None, stream=None):
+                          cu_seqlens_k=None, out=None, lse=None, workspace=None, stream=None):
     """(o, lse) of softmax attention over whole sequences: for token i
         s_j = scale q_i k_j,  lse_i = log sum_j e^s_j,  o_i = sum_j e^(s_j - lse_i) v_j
     over the keys that it sees.
@@ -72,25 +98,25 @@ def attention_emu_forward(q, k, v, *, causal: bool = True, scale=None, cu_seqlen
     every token sees all; a token that sees none has zeros and -infinity.  scale: size ** -0.5
     by default.  cu_seqlens: int32 bounds of packed sequences (then batch is 1; rows of no
     sequence are not written, and hold anything in tensors made here); cu_seqlens_k: those of
-    the keys, if they are others."""
+    the keys, if they are others.  out, lse and workspace (uint8,
+    ``attention_emu_forward_workspace`` bytes) are allocated if None."""
     if not _calls:
         _start()
-    torch = _pkg._torch
-    b, t, n_keys, hq, hk, size = _sizes(q, k)
-    cu, cu_k, n = _bounds(cu_seqlens, cu_seqlens_k, b)
-    dtype, device = q.dtype, q.device
+    cu, cu_k, n = _bounds(cu_seqlens, cu_seqlens_k, q.shape[0])
+    device = q.device
     if out is None:
-        out = _new(stream, q.shape, dtype, device)
+        out = _new(stream, q.shape, q.dtype, device)
     if lse is None:
-        lse = _new(stream, (b, t, hq), torch.float32, device)
-    keys = (b, n_keys, hk, size)
-    args = _FORWARD.pack(
-        _dtypes[dtype], n, t, n_keys, hq, hk, size, 1 if causal else 0, _scale(scale, size), 0, cu,
-        cu_k, *_view(q, "q", q.shape, dtype), *_view(k, "k", keys, dtype),
-        *_view(v, "v", keys, dtype), *_view(out, "out", q.shape, dtype),
-        *_view(lse, "lse", (b, t, hq), torch.float32))
-    _launch("attention_emu_forward", _device(q, k, v, cu_seqlens, cu_seqlens_k, out, lse), stream,
-            args)
+        lse = _new(stream, q.shape[:3], _pkg._torch.float32, device)
+    args = _forward_args(q, k, v, out, lse, causal, scale, cu, cu_k, n)
+    dev = _device(q, k, v, cu_seqlens, cu_seqlens_k, out, lse, workspace)
+    need = _calls["attention_emu_forward_workspace"](args)
+    if need < 0:
+        raise _pkg.SgemmEmuError(need, "attention_emu_forward")
+    if need > 0 or workspace is not None:
+        workspace, at, size = _workspace(need, workspace, device, stream)
+        args = args[:-16] + struct.pack("=2q", at, size)
+    _launch("attention_emu_forward", dev, stream, args)
     return out, lse
 
 

@@ -14,6 +14,7 @@ constexpr int kAttentionMostSize = 128;
 constexpr int64_t kAttentionMostStride = 1 << 22;
 
 // Bytes of workspace; arguments are validated before these are called.
+int64_t attention_forward_workspace(const attention_emu_forward_t& a);
 int64_t attention_backward_workspace(const attention_emu_backward_t& a);
 int64_t attention_step_workspace(const attention_emu_step_t& a);
 

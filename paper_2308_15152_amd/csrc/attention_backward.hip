@@ -12,8 +12,7 @@
 // either: p is taken times 2^14, and ds times a power of two for each column of the
 // accumulator (a query row, or a key), which is lowered, with what is summed so far, when a
 // larger value comes.
-#include "attention_core.hpp"
-#include "attention_rows.hpp"
+#include "attention_parts.hpp"
 
 namespace sgemm_emu {
 
@@ -23,6 +22,17 @@ template <class T>
 constexpr bool kNarrow = false;
 template <>
 constexpr bool kNarrow<f16_t> = true;
+
+// For the scheduler: kinds of instructions, and f of 0 .. n - 1 as constants.
+constexpr int kMatrix = 0x8, kLdsRead = 0x100;
+
+template <int n, int i = 0, class F>
+__device__ inline __attribute__((always_inline)) void schedule_steps(F f) {
+    if constexpr (i < n) {
+        f(Number<i>{});
+        schedule_steps<n, i + 1>(f);
+    }
+}
 
 // A column's power of two.
 struct Fit {
@@ -237,6 +247,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     constexpr int kThreads = Shape::kThreads, kRows = Shape::kRows, kRowGroups = Shape::kRowGroups;
     constexpr int kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;
     constexpr int kTileBytes = kRows * QD::kRowBytes;
+    constexpr int kPerFragment = sizeof(T) == 2 ? 1 : 4;  // matrix instructions
     // (the weights' shift; FP16 only)
     constexpr float kShift = kNarrow<T> ? 14.0f : 0.0f, kBack = kNarrow<T> ? 0x1p-14f : 1.0f;
     struct Row {
@@ -403,15 +414,25 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         };
         f32x16 P{}, dP;
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) P = mma(QD::along(q_along, 0, kb), key_block(kb), P);
-#pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const auto x = per_row(rw.delta, i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) dP[i + j] = x[j];
         }
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) dP = mma(QD::along(o_along, 0, kb), value_block(kb), dP);
+        for (int kb = 0; kb < kBlocks; ++kb) {
+            P = mma(QD::along(q_along, 0, kb), key_block(kb), P);
+            dP = mma(QD::along(o_along, 0, kb), value_block(kb), dP);
+        }
+        // reads two steps ahead of the products that take them
+        constexpr auto reads = [](int kb) {
+            return kb >= kBlocks ? 0 : 2 + (kb >= kKeyBlocks) + (kb >= kValueBlocks);
+        };
+        __builtin_amdgcn_sched_group_barrier(kLdsRead, 4 + reads(0) + reads(1), 0);
+        schedule_steps<kBlocks>([&](auto step) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 2 * kPerFragment, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsRead, reads(decltype(step)::value + 2), 0);
+        });
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const auto x = per_row(rw.z, i);

@@ -37,9 +37,12 @@ int check_sequences(const A& a) {
     if (a.cu_seqlens == nullptr && a.cu_keys != nullptr) return SGEMM_EMU_ERR_NULL;
     if (a.cu_seqlens != nullptr && a.cu_keys == nullptr && a.keys != a.tokens)
         return SGEMM_EMU_ERR_DIM;
-    // rows and tiles of rows are counted in 32 bits
+    // rows and blocks of at least 32 rows or keys are counted in 32 bits
+    const int64_t sequences = a.cu_seqlens != nullptr ? 1 : a.batch;
     if ((int64_t)a.tokens * a.q_heads > INT32_MAX - 4096 || a.keys > INT32_MAX - 4096 ||
-        (int64_t)a.batch * a.k_heads > INT32_MAX)
+        (__int128)a.tokens * a.q_heads / 32 * sequences + (int64_t)a.batch * a.k_heads >
+            INT32_MAX / 2 ||
+        ((int64_t)a.keys / 32 * sequences + a.batch) * (__int128)a.k_heads > INT32_MAX / 2)
         return SGEMM_EMU_ERR_UNSUPPORTED;
     return SGEMM_EMU_OK;
 }
@@ -50,8 +53,8 @@ int check_step(const attention_emu_step_t& a) {
         (a.slots == nullptr && a.batch > a.n_slots))
         return SGEMM_EMU_ERR_DIM;
     if (int rc = check_heads(a.q_heads, a.k_heads, a.size, a.scale)) return rc;
-    if ((__int128)a.batch * a.tokens * a.q_heads > INT32_MAX - 4096 ||
-        a.prefix > INT32_MAX - 4096 || a.capacity > INT32_MAX - 4096)
+    if ((__int128)a.batch * a.tokens * a.q_heads > INT32_MAX / 2 || a.prefix > INT32_MAX - 4096 ||
+        a.capacity > INT32_MAX - 4096)
         return SGEMM_EMU_ERR_UNSUPPORTED;
     return SGEMM_EMU_OK;
 }
@@ -65,6 +68,12 @@ int check_workspace(int64_t need, const void* p, int64_t bytes) {
 }  // namespace
 
 extern "C" {
+
+int64_t attention_emu_forward_workspace(const attention_emu_forward_t* a) {
+    if (a == nullptr) return SGEMM_EMU_ERR_NULL;
+    if (int rc = check_sequences(*a)) return rc;
+    return attention_forward_workspace(*a);
+}
 
 int attention_emu_forward(const attention_emu_forward_t* args, hipStream_t stream) {
     if (args == nullptr) return SGEMM_EMU_ERR_NULL;
@@ -80,9 +89,12 @@ int attention_emu_forward(const attention_emu_forward_t* args, hipStream_t strea
     const Tensor v{a.v, batch, a.keys, a.k_heads, a.size, e};
     const Tensor o{a.o, batch, a.tokens, a.q_heads, a.size, e};
     const Tensor lse{a.lse, batch, a.tokens, a.q_heads, 1, 4};
+    const int64_t need = attention_forward_workspace(a);
+    if (int rc = check_workspace(need, a.workspace, a.workspace_bytes)) return rc;
     const __int128 bounds = ((__int128)a.batch + 1) * 4;
     if (int rc = check_tensors({q, k, v}, {o, lse},
-                               {array(a.cu_seqlens, bounds), array(a.cu_keys, bounds)}, {}))
+                               {array(a.cu_seqlens, bounds), array(a.cu_keys, bounds)},
+                               {array(a.workspace, need)}))
         return rc;
     return done(launch_attention_forward(a, stream));
 }

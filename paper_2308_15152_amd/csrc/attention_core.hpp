@@ -13,12 +13,9 @@
 // instructions; l sums them before that.
 #pragma once
 
-#include "attention_tile.hpp"
+#include "attention_parts.hpp"
 
 namespace sgemm_emu {
-
-constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kLn2 = 0.69314718055994530942f;
 
 // kRowGroups waves with 32 rows each share the block's tiles of kKeys keys; or
 // (kRowGroups == 1) kKeyGroups waves with the same 32 rows take every kKeyGroups-th tile for
@@ -45,7 +42,7 @@ struct Attend {
     // rows: query rows there are; the block takes row0 to row0 + kRows - 1.
     // q_row(r): its elements; limit(r): how many keys it sees (not decreasing in r).
     // k, v: row 0 of the keys and values; the pass goes over keys first to end - 1.
-    // out(r): where a row's results go; of that, sums(l, z) and four(d, ...).
+    // out(r): where a row's results go; of that, sums(l, z, here) and four(d, ...).
     template <class QRow, class Limit, class Out>
     static __device__ __attribute__((always_inline)) void run(
         char* lds, int rows, int row0, QRow q_row, Limit limit, const T* k, int64_t k_token,
@@ -202,8 +199,8 @@ struct Attend {
                             for (int i = 0; i < 16; ++i)
                                 O[dt][i] += not_finite(v + j * v_token, 32 * dt + acc_row(i, half), size);
                 const float f = l == 0.0f ? 0.0f : 1.0f / l;
-                const auto to = out(row);
-                if (half == 0) to.sums(l, z);
+                auto to = out(row);
+                to.sums(l, z, half == 0);
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -247,8 +244,8 @@ struct Attend {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] += not_finite(v + j * v_token, d + e, size);
                 }
-                const auto to = out(row0 + r);
-                if (d == 0) to.sums(ls, zs);
+                auto to = out(row0 + r);
+                to.sums(ls, zs, d == 0);
                 to.four(d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
             }
         }

@@ -1,34 +1,29 @@
 // Attention over whole sequences: one block per 32 kRowGroups query rows of a
 // key head (a token's query heads that share it are neighbouring rows).
+#include <algorithm>
+
 #include "attention_core.hpp"
-#include "attention_rows.hpp"
 
 namespace sgemm_emu {
 
 namespace {
 
-template <class T, bool kVec>
-struct ForwardRow {
-    T* o;
-    float* lse;  // or null
-    int size;
-    __device__ inline void sums(float l, float z) const {
-        if (lse != nullptr)
-            *lse = l == 0.0f ? -__builtin_inff() : (z + __builtin_amdgcn_logf(l)) * kLn2;
-    }
-    __device__ inline void four(int d, float x, float y, float z, float w) const {
-        store_four<T, kVec>(o, d, size, x, y, z, w);
-    }
+struct ForwardArgs {
+    attention_emu_forward_t a;
+    int count;  // parts that a block's keys are cut into
+    Parts parts;
 };
 
 template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
 __global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_forward_kernel(
-    attention_emu_forward_t a, int first_block) {
+    ForwardArgs args, int first_block) {
+    const attention_emu_forward_t& a = args.a;
     using Pass = Attend<T, D, kRowGroups, kKeyGroups, kKeys, kVec>;
     __shared__ __attribute__((aligned(16))) char lds[Pass::kLds];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
-    const int block = first_block + (int)blockIdx.x;
+    const int part = (first_block + (int)blockIdx.x) % args.count;
+    const int block = (first_block + (int)blockIdx.x) / args.count;
     int n, head, tile;
     if (packed) {
         head = block % a.k_heads;
@@ -52,32 +47,57 @@ __global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_for
     const T* v = row_of<T>(a.v, packed, n, sk, head);
     float* lse = a.lse.p == nullptr ? nullptr : row_of<float>(a.lse, packed, n, sq, head * group);
     T* o = row_of<T>(a.o, packed, n, sq, head * group);
+    const int64_t first_token = packed ? sq.first : (int64_t)n * a.tokens;
     const auto out = [&](int r) {
         const int token = r / group, h = r % group;
-        return ForwardRow<T, kVec>{o + token * a.o.token + h * a.o.head,
-                                   lse ? lse + token * a.lse.token + h * a.lse.head : nullptr, a.size};
+        return row_out<T, D, kVec>(args.parts, part,
+                                   (first_token + token) * a.q_heads + head * group + h,
+                                   o + token * a.o.token + h * a.o.head,
+                                   lse ? lse + token * a.lse.token + h * a.lse.head : nullptr, a.size);
     };
     const int shift = sk.count - sq.count + 1;
+    const auto limit = [&](int r) { return a.causal ? r / group + shift : sk.count; };
+    // the part's share of the keys that the block's rows see
+    const int seen = min(max(limit(min((tile + 1) * Pass::kRows, rows) - 1), 0), sk.count);
+    const int each = (seen + args.count * kKeys - 1) / (args.count * kKeys) * kKeys;
+    const int first = min(part * each, seen), end = min(first + each, seen);
     Pass::run(
         lds, rows, tile * Pass::kRows,
-        [&](int r) { return q + r / group * a.q.token + r % group * a.q.head; },
-        [&](int r) { return a.causal ? r / group + shift : sk.count; }, k, a.k.token, v, a.v.token, 0,
-        sk.count, a.size, __builtin_fabsf(a.scale) * kLog2e, a.scale < 0.0f, out);
+        [&](int r) { return q + r / group * a.q.token + r % group * a.q.head; }, limit, k, a.k.token, v,
+        a.v.token, first, end, a.size, __builtin_fabsf(a.scale) * kLog2e, a.scale < 0.0f, out);
 }
 
-template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
-hipError_t launch(const attention_emu_forward_t& a, hipStream_t stream) {
-    const int group = a.q_heads / a.k_heads;
-    const int64_t parts = most_parts(a.batch, (int64_t)a.tokens * group, 32 * kRowGroups,
-                                     a.cu_seqlens != nullptr);
-    return launch_blocks(attention_forward_kernel<T, D, kRowGroups, kKeyGroups, kKeys, kVec>,
-                         parts * a.k_heads, 64 * kRowGroups * kKeyGroups, stream, a);
+// Blocks of `rows` query rows.
+int64_t blocks_of(const attention_emu_forward_t& a, int rows) {
+    const int64_t group = a.q_heads / a.k_heads;
+    return most_parts(a.batch, a.tokens * group, rows, a.cu_seqlens != nullptr) * a.k_heads;
+}
+
+constexpr int kRowGroups = 4;
+
+// Parts of the keys: where the blocks are fewer than two for each CU, as many as fill
+// those, of at least 256 keys each.
+int parts_of(const attention_emu_forward_t& a) {
+    const int64_t blocks = blocks_of(a, 32 * kRowGroups), most = (a.keys + 255) / 256;
+    if (blocks == 0 || most <= 1 || a.cu_seqlens != nullptr) return 1;
+    return (int)std::max<int64_t>(1, std::min(most, 512 / blocks));
+}
+
+int64_t rows_of(const attention_emu_forward_t& a) {
+    return (a.cu_seqlens != nullptr ? 1 : (int64_t)a.batch) * a.tokens * a.q_heads;
 }
 
 }  // namespace
 
-hipError_t launch_attention_forward(const attention_emu_forward_t& args, hipStream_t stream) {
-    attention_emu_forward_t a = args;
+int64_t attention_forward_workspace(const attention_emu_forward_t& a) {
+    const int parts = parts_of(a);
+    return parts == 1 ? 0 : parts_bytes(parts, rows_of(a), a.size);
+}
+
+hipError_t launch_attention_forward(const attention_emu_forward_t& given, hipStream_t stream) {
+    const int parts = parts_of(given);
+    ForwardArgs args{given, parts, parts_in(given.workspace, parts, rows_of(given), given.size)};
+    attention_emu_forward_t& a = args.a;
     if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) a.cu_keys = a.cu_seqlens;
     const int e = a.dtype == SGEMM_EMU_F32 ? 4 : 2;
     const bool vec = a.size * e % 16 == 0 && rows_aligned16(a.q, e) && rows_aligned16(a.k, e) &&
@@ -85,8 +105,15 @@ hipError_t launch_attention_forward(const attention_emu_forward_t& args, hipStre
     return by_form(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
+        constexpr bool kVec = decltype(vec)::value != 0;
         constexpr int kKeys = sizeof(T) == 2 || D <= 64 ? 64 : 32;
-        return launch<T, D, 4, 1, kKeys, decltype(vec)::value != 0>(a, stream);
+        if (hipError_t e = launch_blocks(attention_forward_kernel<T, D, kRowGroups, 1, kKeys, kVec>,
+                                         blocks_of(a, 32 * kRowGroups) * parts, 64 * kRowGroups,
+                                         stream, args))
+            return e;
+        if (parts == 1) return hipSuccess;
+        return launch_join<T, D, kVec>(
+            JoinArgs{args.parts, a.o, a.lse, parts, a.tokens, a.q_heads, a.size, nullptr, 0}, stream);
     });
 }
 

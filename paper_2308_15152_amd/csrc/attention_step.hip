@@ -2,13 +2,11 @@
 //
 // The prefix is read once for the batch: its blocks take 128 rows of a key head, of any
 // sequences, through a part of the prefix's keys.  The caches' blocks take the rows of one
-// sequence through a part of its cache, 32 keys to a wave.  Each leaves its rows' normalized result
-// and log-sum in the workspace, and a second kernel joins the parts of a row; where there
-// is one part, it is the result.
+// sequence through a part of its cache, 32 keys to a wave.  The parts of a row are joined by a
+// second kernel; where there is one, it is the result.
 #include <algorithm>
 
 #include "attention_core.hpp"
-#include "attention_rows.hpp"
 
 namespace sgemm_emu {
 
@@ -17,34 +15,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPrefixRows = 128;
 
-// Elements from one row of a part to the next.
-template <int D>
-constexpr int kStride = D <= 64 ? 64 : 128;
-
 struct StepArgs {
     attention_emu_step_t a;
     int prefix_parts, prefix_tiles, prefix_keys;  // parts, row tiles, keys of a part
     int own_parts;
-    float* parts;  // [part][row][kStride], or null: one part, written to o
-    float* logs;   // [part][row], base 2
-    int64_t rows;  // batch x tokens x q_heads
-};
-
-template <class T, bool kVec>
-struct StepRow {
-    T* o;         // or, of a part,
-    float* part;  // its row
-    float* log;
-    int size;
-    __device__ inline void sums(float l, float z) const {
-        if (part != nullptr) *log = l == 0.0f ? -__builtin_inff() : z + __builtin_amdgcn_logf(l);
-    }
-    __device__ inline void four(int d, float x, float y, float z, float w) const {
-        if (part == nullptr)
-            store_four<T, kVec>(o, d, size, x, y, z, w);
-        else if (d < size)
-            *reinterpret_cast<Pack<float, 4>::type*>(part + d) = Pack<float, 4>::type{x, y, z, w};
-    }
+    Parts parts;
 };
 
 template <class T, int D, bool kVec>
@@ -63,8 +38,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         const int64_t row = (int64_t)t * a.q_heads + h;
         T* o = static_cast<T*>(a.o.p) + t / a.tokens * a.o.batch + t % a.tokens * a.o.token +
                h * a.o.head;
-        return StepRow<T, kVec>{o, s.parts ? s.parts + (p * s.rows + row) * kStride<D> : nullptr,
-                                s.logs + p * s.rows + row, a.size};
+        return row_out<T, D, kVec>(s.parts, p, row, o, nullptr, a.size);
     };
     const auto q_row = [&](int t, int h) {
         return static_cast<const T*>(a.q.p) + t / a.tokens * a.q.batch + t % a.tokens * a.q.token +
@@ -108,47 +82,12 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         a.size, c, a.scale < 0.0f, out);
 }
 
-// o = sum_p 2^(log_p - z) part_p / sum_p 2^(log_p - z), z the largest.
-template <class T, int D, bool kVec>
-__global__ __launch_bounds__(kThreads) void attention_join_kernel(StepArgs s, int parts,
-                                                                  int first_block) {
-    const attention_emu_step_t& a = s.a;
-    const int64_t w = (first_block + blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t row = w / (D / 4);
-    const int d = (int)(w % (D / 4)) * 4;
-    if (row >= s.rows || d >= a.size) return;
-    const int64_t token = row / a.q_heads;
-    const int h = (int)(row - token * a.q_heads), n = (int)(token / a.tokens);
-    float z = -1e30f, l = 0.0f;
-    for (int p = 0; p < parts; ++p) z = fmaxf(z, s.logs[p * s.rows + row]);
-    Pack<float, 4>::type x{};
-    const int slot = a.slots == nullptr ? n : a.slots[n];
-    if (slot >= 0 && slot < a.n_slots) {
-        for (int p = 0; p < parts; ++p) {
-            const float log = s.logs[p * s.rows + row];
-            if (log == -__builtin_inff()) continue;
-            const float f = __builtin_amdgcn_exp2f(log - z);
-            l += f;
-            const auto y = *reinterpret_cast<const Pack<float, 4>::type*>(
-                s.parts + (p * s.rows + row) * kStride<D> + d);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] += f * y[j];
-        }
-    }
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;
-    T* o = static_cast<T*>(a.o.p) + n * a.o.batch + (token - (int64_t)n * a.tokens) * a.o.token +
-           h * a.o.head;
-    store_four<T, kVec>(o, d, a.size, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-}
-
-int padded(int size) { return size <= 64 ? 64 : 128; }  // kStride
-
 // How the keys are cut.
 StepArgs cut(const attention_emu_step_t& a) {
     StepArgs s{};
     s.a = a;
     const int64_t group = a.q_heads / a.k_heads;
-    s.rows = (int64_t)a.batch * a.tokens * a.q_heads;
+    s.parts.rows = (int64_t)a.batch * a.tokens * a.q_heads;
     const int64_t rows = (int64_t)a.batch * a.tokens * group;
     s.prefix_tiles = (int)((rows + kPrefixRows - 1) / kPrefixRows);
     constexpr int64_t kWanted = 512;  // blocks: two for each CU
@@ -165,25 +104,18 @@ StepArgs cut(const attention_emu_step_t& a) {
     return s;
 }
 
-int64_t part_floats(const StepArgs& s) { return s.rows * padded(s.a.size); }
-
 }  // namespace
 
 int64_t attention_step_workspace(const attention_emu_step_t& a) {
     const StepArgs s = cut(a);
     const int64_t parts = s.prefix_parts + s.own_parts;
-    if (parts == 1) return 0;
-    const int64_t bytes = parts * (part_floats(s) + s.rows) * 4;
-    return (bytes + 255) / 256 * 256;
+    return parts == 1 ? 0 : parts_bytes(parts, s.parts.rows, a.size);
 }
 
 hipError_t launch_attention_step(const attention_emu_step_t& a, hipStream_t stream) {
     StepArgs s = cut(a);
     const int parts = s.prefix_parts + s.own_parts;
-    if (parts > 1) {
-        s.parts = static_cast<float*>(a.workspace);
-        s.logs = s.parts + parts * part_floats(s);
-    }
+    s.parts = parts_in(a.workspace, parts, s.parts.rows, a.size);
     const int64_t group = a.q_heads / a.k_heads;
     const int64_t blocks =
         (int64_t)s.prefix_parts * s.prefix_tiles * a.k_heads +
@@ -201,9 +133,8 @@ hipError_t launch_attention_step(const attention_emu_step_t& a, hipStream_t stre
                                          s))
             return e;
         if (parts == 1) return hipSuccess;
-        constexpr int kRows = kThreads / (kStride<D> / 4);
-        return launch_blocks(attention_join_kernel<T, D, kVec>, (s.rows + kRows - 1) / kRows, kThreads,
-                             stream, s, parts);
+        return launch_join<T, D, kVec>(
+            JoinArgs{s.parts, a.o, {}, parts, a.tokens, a.q_heads, a.size, a.slots, a.n_slots}, stream);
     });
 }
 
