@@ -13,15 +13,26 @@
 // accumulator (a query row, or a key), which is lowered, with what is summed so far, when a
 // larger value comes.
 #include "attention_parts.hpp"
+#include "attention_split.h"
 
 namespace sgemm_emu {
 
 namespace {
 
 template <class T>
-constexpr bool kNarrow = false;
-template <>
-constexpr bool kNarrow<f16_t> = true;
+constexpr bool kNarrow = __is_same(Elem<T>, f16_t);
+
+struct BackwardArgs {
+    attention_emu_backward_t a;
+    float* delta;  // [token in all][query head]
+    // the operands, split if they are FP32
+    sgemm_emu_view_t q, k, v, d_o;
+    const float *q_factors, *k_factors, *v_factors, *do_factors;
+};
+
+__device__ inline Pack<float, 4>::type four_floats(const float* p) {
+    return *reinterpret_cast<const Pack<float, 4>::type*>(p);
+}
 
 // For the scheduler: kinds of instructions, and f of 0 .. n - 1 as constants.
 constexpr int kMatrix = 0x8, kLdsRead = 0x100;
@@ -71,13 +82,18 @@ constexpr int kDqWaves = 4;
 constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
 
+// (FP32 operands of more than 96 elements take the registers of two waves)
 template <class T, int D, bool kVec>
-__global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attention_emu_backward_t a,
-                                                                     int first_block) {
-    using KV = Tile<T, D>;
-    constexpr int kThreads = 64 * kDqWaves, kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;
-    constexpr int kTileBytes = kDqKeys * KV::kRowBytes;
+__global__ __launch_bounds__(64 * kDqWaves, kPlanes<T> == 2 && D > 96 ? 1 : 2) void
+attention_dq_kernel(BackwardArgs args, int first_block) {
+    typedef Elem<T> E;
+    using KV = Planes<T, D, kDqKeys>;
+    constexpr bool kSplit = kPlanes<T> == 2;
+    constexpr int kThreads = 64 * kDqWaves, kBlocks = D / kBlock<E>, kParts = 32 / kBlock<E>;
+    constexpr int kTileBytes = KV::kBytes;
     __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
+    __shared__ float of_tiles[kSplit ? 4 * kDqKeys : 1];  // factors of keys and values
+    const attention_emu_backward_t& a = args.a;
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
     const int block = first_block + (int)blockIdx.x;
@@ -98,8 +114,8 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
     const Span sq = span_of(a.cu_seqlens, n, a.tokens);
     const Span sk = span_of(a.cu_keys, n, a.keys);
     const int rows = sq.count * group, last_row = rows - 1;
-    const T* k = row_of<T>(a.k, packed, n, sk, head);
-    const T* v = row_of<T>(a.v, packed, n, sk, head);
+    const E* k = row_of<E>(args.k, packed, n, sk, head);
+    const E* v = row_of<E>(args.v, packed, n, sk, head);
 
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -107,32 +123,43 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
     const int row = wave_row + (lane & 31);
     const int r = min(row, last_row), token = r / group, h = head * group + r % group;
     const bool valid = row < rows;
-    Frag<T> Q[kBlocks], DO[kBlocks];
+    const int64_t in_all = (packed ? sq.first : (int64_t)n * a.tokens) + token;
+    Operand<T> Q[kBlocks], DO[kBlocks];
     float delta = 0.0f;
     {
-        const T* q = row_of<T>(a.q, packed, n, sq, h) + token * a.q.token;
-        const T* o = row_of<T>(a.o, packed, n, sq, h) + token * a.o.token;
-        const T* d = row_of<T>(a.d_o, packed, n, sq, h) + token * a.d_o.token;
+        const E* q = row_of<E>(args.q, packed, n, sq, h) + token * args.q.token;
+        const E* x = row_of<E>(args.d_o, packed, n, sq, h) + token * args.d_o.token;
+        const Out<T>* o = row_of<Out<T>>(a.o, packed, n, sq, h) + token * a.o.token;
+        const Out<T>* d = row_of<Out<T>>(a.d_o, packed, n, sq, h) + token * a.d_o.token;
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
-            Q[kb] = load_chunk<T, kVec>(q, 2 * kb + half, a.size, valid);
-            DO[kb] = load_chunk<T, kVec>(d, 2 * kb + half, a.size, valid);
-            const Frag<T> x = load_chunk<T, kVec>(o, 2 * kb + half, a.size, valid);
+            Q[kb] = load_operand<T, D, kVec>(q, 2 * kb + half, a.size, valid);
+            DO[kb] = load_operand<T, D, kVec>(x, 2 * kb + half, a.size, valid);
+        }
 #pragma unroll
-            for (int j = 0; j < kPer<T>; ++j)
-                delta = __builtin_fmaf(to_f32(DO[kb][j]), to_f32(x[j]), delta);
+        for (int kb = 0; kb < D / kBlock<Out<T>>; ++kb) {
+            const Frag<Out<T>> x = load_chunk<Out<T>, kVec>(o, 2 * kb + half, a.size, valid);
+            const Frag<Out<T>> y = load_chunk<Out<T>, kVec>(d, 2 * kb + half, a.size, valid);
+#pragma unroll
+            for (int j = 0; j < kPer<Out<T>>; ++j)
+                delta = __builtin_fmaf(to_f32(x[j]), to_f32(y[j]), delta);
         }
         delta = sum_halves(delta);
     }
-    const int64_t out_row = (packed ? sq.first : (int64_t)n * a.tokens) + token;
-    if (valid && half == 0) static_cast<float*>(a.workspace)[out_row * a.q_heads + h] = delta;
+    if (valid && half == 0) args.delta[in_all * a.q_heads + h] = delta;
     // (rows that see nothing have lse -infinity)
     float z = __builtin_inff();
     if (valid) {
         const float lse = row_of<float>(a.lse, packed, n, sq, h)[token * a.lse.token];
         if (lse != -__builtin_inff()) z = lse * kLog2e;
     }
-    const float c = a.scale * kLog2e;
+    // what the row's q and do have been divided by
+    float q_factor = 1.0f, do_factor = 1.0f;
+    if constexpr (kSplit) {
+        q_factor = args.q_factors[in_all * a.q_heads + h];
+        do_factor = args.do_factors[in_all * a.q_heads + h];
+    }
+    const float c = a.scale * kLog2e * q_factor;
     const int shift = sk.count - sq.count + 1;
     const auto seen = [&](int r) {
         return a.causal ? min(max(min(r, last_row) / group + shift, 0), sk.count) : sk.count;
@@ -147,37 +174,71 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
     // (what is not loaded multiplies zeros and has to be finite)
     clear_lds(lds, 4 * kTileBytes, threadIdx.x, kThreads);
     lds_barrier();
-    Flow<T, D, kDqKeys, kThreads, kVec> fk, fv;
-    const uint32_t k_row = (uint32_t)a.k.token * sizeof(T), v_row = (uint32_t)a.v.token * sizeof(T);
+    Flow<E, D, kDqKeys, kThreads, kVec || kSplit> fk, fv;
+    const int width = kSplit ? kWidth<D> : a.size;
+    const uint32_t k_row = (uint32_t)args.k.token * sizeof(E);
+    const uint32_t v_row = (uint32_t)args.v.token * sizeof(E);
+    const int64_t first_key = (packed ? sk.first : (int64_t)n * a.keys) * a.k_heads + head;
+    float st_factor = 0.0f;
     fk.rows([&](int r) { return r * k_row; }, threadIdx.x);
     fv.rows([&](int r) { return r * v_row; }, threadIdx.x);
     const auto load = [&](int t) {
         const int key = t * kDqKeys, most = sk.count - 1 - key;
         char* to = lds + (t & 1) * 2 * kTileBytes;
         const auto there = [&](int, int r) { return r <= most; };
-        fk.start(to, k + key * a.k.token, a.size, threadIdx.x, there);
-        fv.start(to + kTileBytes, v + key * a.v.token, a.size, threadIdx.x, there);
+        if constexpr (kSplit) {
+            const int i = threadIdx.x % kDqKeys;
+            if (threadIdx.x < 2 * kDqKeys)
+                st_factor = i > most ? 0.0f
+                                     : (threadIdx.x < kDqKeys ? args.k_factors : args.v_factors)
+                                           [first_key + (int64_t)(key + i) * a.k_heads];
+        }
+#pragma unroll
+        for (int i = 0; i < kPlanes<T>; ++i) {
+            fk.start(to + i * KV::kPlaneBytes, k + key * args.k.token + i * kWidth<D>, width,
+                     threadIdx.x, there);
+            fv.start(to + kTileBytes + i * KV::kPlaneBytes, v + key * args.v.token + i * kWidth<D>,
+                     width, threadIdx.x, there);
+        }
     };
-    const int from_along = KV::from_along(lane), from_across = KV::from_across(lane);
+    const int from_along = KV::One::from_along(lane);
+    const int from_across = KV::One::from_across(lane);
     if (count > 0) load(0);
     for (int t = 0; t < count; ++t) {
         char* kt = lds + (t & 1) * 2 * kTileBytes;
         char* vt = kt + kTileBytes;
         fk.finish(kt, threadIdx.x);
         fv.finish(vt, threadIdx.x);
+        float* const of_tile = of_tiles + (t & 1) * 2 * kDqKeys;
+        if (kSplit && threadIdx.x < 2 * kDqKeys) of_tile[threadIdx.x] = st_factor;
         lds_barrier();
         if (t + 1 < count) load(t + 1);
         const int key0 = t * kDqKeys;
         if (key0 >= lim_max) continue;
-        const uint32_t k_along = KV::base(kt, from_along), v_along = KV::base(vt, from_along);
-        const uint32_t k_across = KV::base(kt, from_across);
+        const uint32_t k_along = KV::One::base(kt, from_along);
+        const uint32_t v_along = KV::One::base(vt, from_along);
+        const uint32_t k_across = KV::One::base(kt, from_across);
         f32x16 S{}, dP;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) dP[i] = -delta;
+        for (int i = 0; i < 16; ++i) dP[i] = kSplit ? 0.0f : -delta;
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
             S = mma(KV::along(k_along, 0, kb), Q[kb], S);
             dP = mma(KV::along(v_along, 0, kb), DO[kb], dP);
+        }
+        f32x16 by;  // the keys' factors
+        if constexpr (kSplit) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const auto x = four_floats(of_tile + 8 * (i / 4) + 4 * half);
+                const auto y = four_floats(of_tile + kDqKeys + 8 * (i / 4) + 4 * half);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    by[i + j] = x[j];
+                    S[i + j] *= x[j];
+                    dP[i + j] = __builtin_fmaf(dP[i + j] * y[j], do_factor, -delta);
+                }
+            }
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -187,13 +248,16 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
             for (int i = 0; i < 16; ++i)
                 if (key0 + acc_row(i, half) >= lim) dP[i] = 0.0f;
         }
+        if constexpr (kSplit)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dP[i] *= by[i];
         if constexpr (kNarrow<T>) {
             fit.fit(dP, dQ);
             dP = times(dP, fit.f);
         }
 #pragma unroll
         for (int kb = 0; kb < kParts; ++kb) {
-            const Frag<T> x = operand<T>(dP, kb);
+            const Operand<T> x = operand<T>(dP, kb);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
                 dQ[dt] = mma(KV::across(k_across, kb, 32 * dt), x, dQ[dt]);
@@ -201,29 +265,29 @@ __global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_kernel(attentio
     }
     if (!valid) return;
     const float f = kNarrow<T> ? a.scale / fit.f : a.scale;
-    T* dq = row_of<T>(a.dq, packed, n, sq, h) + token * a.dq.token;
+    Out<T>* dq = row_of<Out<T>>(a.dq, packed, n, sq, h) + token * a.dq.token;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-            store_four<T, kVec>(dq, 32 * dt + acc_row(i, half), a.size, dQ[dt][i] * f,
+            store_four<Out<T>, kVec>(dq, 32 * dt + acc_row(i, half), a.size, dQ[dt][i] * f,
                                 dQ[dt][i + 1] * f, dQ[dt][i + 2] * f, dQ[dt][i + 3] * f);
 }
 
 // A block's waves: kKeyGroups times 32 keys, each shared by kRowGroups waves that take
 // 32 query rows of a tile each and are joined at the end.  As many waves as two for each SIMD,
-// where registers (FP32 of more than 96 elements) and LDS hold them.
+// where registers and LDS hold them (not with FP32 of more than 64 elements).
 template <class T, int D>
 struct DkvShape {
-    static constexpr int kWide = sizeof(T) == 4 && D > 64;
-    static constexpr int kKeyGroups = kWide && D <= 96 ? 4 : 2;
+    static constexpr bool kWide = kPlanes<T> == 2 && D > 64;
+    static constexpr int kKeyGroups = 2;
     static constexpr int kRowGroups = kWide ? 2 : 4;
     static constexpr int kWaves = kKeyGroups * kRowGroups, kThreads = 64 * kWaves;
     static constexpr int kKeys = 32 * kKeyGroups, kRows = 32 * kRowGroups;
     // How much of the keys' and values' operands is in registers; the rest, which
     // does not fit, is read from LDS for every tile
-    static constexpr int kBlocks = D / kBlock<T>;
-    static constexpr bool kFull = sizeof(T) == 2 && D > 96;
+    static constexpr int kBlocks = D / kBlock<Elem<T>>;
+    static constexpr bool kFull = kPlanes<T> == 1 && D > 96;
     static constexpr int kKeyBlocks = kFull ? kBlocks / 2 : kBlocks;
     static constexpr int kValueBlocks = kFull ? 0 : kBlocks;
     static constexpr int kLdsBlocks = 2 * kBlocks - kKeyBlocks - kValueBlocks;
@@ -242,24 +306,27 @@ struct RowTiles {
 
 template <class T, int D, bool kVec, class Shape = DkvShape<T, D>>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_dkv_kernel(
-    attention_emu_backward_t a, int first_block) {
-    using QD = Tile<T, D>;
+    BackwardArgs args, int first_block) {
+    typedef Elem<T> E;
+    const attention_emu_backward_t& a = args.a;
+    constexpr bool kSplit = kPlanes<T> == 2;
     constexpr int kThreads = Shape::kThreads, kRows = Shape::kRows, kRowGroups = Shape::kRowGroups;
-    constexpr int kBlocks = D / kBlock<T>, kParts = 32 / kBlock<T>;
-    constexpr int kTileBytes = kRows * QD::kRowBytes;
-    constexpr int kPerFragment = sizeof(T) == 2 ? 1 : 4;  // matrix instructions
+    using QD = Planes<T, D, kRows>;
+    constexpr int kBlocks = D / kBlock<E>, kParts = 32 / kBlock<E>;
+    constexpr int kTileBytes = QD::kBytes, kRowBytes = QD::One::kRowBytes;
     // (the weights' shift; FP16 only)
     constexpr float kShift = kNarrow<T> ? 14.0f : 0.0f, kBack = kNarrow<T> ? 0x1p-14f : 1.0f;
     struct Row {
         float z[kRows], delta[kRows];
         int seen[kRows];
+        float q[kSplit ? kRows : 4], d_o[kSplit ? kRows : 4];  // factors
     };
     constexpr int kJoin = (kRowGroups - 1) * Shape::kKeyGroups * D / 32 * 4096;
     constexpr int kLds = 4 * kTileBytes > kJoin ? 4 * kTileBytes : kJoin;
     __shared__ __attribute__((aligned(16))) char lds[kLds];
     __shared__ __attribute__((aligned(16))) Row of_rows[2];
     // [key group][block][lane]
-    __shared__ Frag<T> operands[Shape::kLdsBlocks > 0 ? Shape::kKeyGroups * Shape::kLdsBlocks * 64 : 1];
+    __shared__ Operand<T> operands[Shape::kLdsBlocks > 0 ? Shape::kKeyGroups * Shape::kLdsBlocks * 64 : 1];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
     const int block = first_block + (int)blockIdx.x;
@@ -287,15 +354,15 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     const bool valid = key < sk.count;
     const int key_in = min(key, sk.count - 1);
     constexpr int kKeyBlocks = Shape::kKeyBlocks, kValueBlocks = Shape::kValueBlocks;
-    Frag<T> K[kKeyBlocks], V[kValueBlocks > 0 ? kValueBlocks : 1];
-    Frag<T>* const more = operands + key_group * Shape::kLdsBlocks * 64 + lane;
+    Operand<T> K[kKeyBlocks], V[kValueBlocks > 0 ? kValueBlocks : 1];
+    Operand<T>* const more = operands + key_group * Shape::kLdsBlocks * 64 + lane;
     {
-        const T* k = row_of<T>(a.k, packed, n, sk, head) + key_in * a.k.token;
-        const T* v = row_of<T>(a.v, packed, n, sk, head) + key_in * a.v.token;
+        const E* k = row_of<E>(args.k, packed, n, sk, head) + key_in * args.k.token;
+        const E* v = row_of<E>(args.v, packed, n, sk, head) + key_in * args.v.token;
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
-            const Frag<T> x = load_chunk<T, kVec>(k, 2 * kb + half, a.size, valid);
-            const Frag<T> y = load_chunk<T, kVec>(v, 2 * kb + half, a.size, valid);
+            const Operand<T> x = load_operand<T, D, kVec>(k, 2 * kb + half, a.size, valid);
+            const Operand<T> y = load_operand<T, D, kVec>(v, 2 * kb + half, a.size, valid);
             if (kb < kKeyBlocks)
                 K[kb] = x;
             else if (row_group == 0)
@@ -314,7 +381,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
                                  : more[(kBlocks - kKeyBlocks + kb - kValueBlocks) * 64];
     };
     const int shift = sk.count - tokens + 1;  // token i sees keys below i + shift
-    const bool far = (int64_t)(group - 1) * max(a.q.head, a.d_o.head) > (1 << 28);
+    const bool far = (int64_t)(group - 1) * max(args.q.head, args.d_o.head) > (1 << 28);
     const RowTiles tiles(group, kRows, far);
     const int count = (tokens + tiles.tokens - 1) / tiles.tokens * tiles.parts;
     const int from = a.causal ? min(max(block_key - shift + 1, 0), tokens) : 0;
@@ -325,17 +392,23 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     f32x16 dK[D / 32], dV[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dK[dt] = f32x16{}, dV[dt] = f32x16{};
-    Fit fit;
+    Fit fit, fit_v;
     // (what is not loaded multiplies zeros and has to be finite)
     clear_lds(lds, 4 * kTileBytes, thread, kThreads);
     lds_barrier();
 
-    const T* q0 = row_of<T>(a.q, packed, n, sq, head * group);
-    const T* d0 = row_of<T>(a.d_o, packed, n, sq, head * group);
+    const E* q0 = row_of<E>(args.q, packed, n, sq, head * group);
+    const E* d0 = row_of<E>(args.d_o, packed, n, sq, head * group);
     const float* lse0 = row_of<float>(a.lse, packed, n, sq, head * group);
-    const float* delta0 = static_cast<const float*>(a.workspace) +
-                          (packed ? sq.first : (int64_t)n * a.tokens) * a.q_heads + head * group;
-    Flow<T, D, kRows, kThreads, kVec> fq, fd;
+    const int64_t row_in_all = (packed ? sq.first : (int64_t)n * a.tokens) * a.q_heads + head * group;
+    // what the lane's key and value have been divided by
+    float k_factor = 1.0f, v_factor = 1.0f;
+    if constexpr (kSplit) {
+        const int64_t i = ((packed ? sk.first : (int64_t)n * a.keys) + key_in) * a.k_heads + head;
+        k_factor = args.k_factors[i], v_factor = args.v_factors[i];
+    }
+    Flow<E, D, kRows, kThreads, kVec || kSplit> fq, fd;
+    const int width = kSplit ? kWidth<D> : a.size;
     // of the thread's chunks: their rows' tokens and heads in the tile, a byte each
     uint32_t chunk_tokens[(fq.kEach + 3) / 4] = {}, chunk_heads[(fq.kEach + 3) / 4] = {};
 #pragma unroll
@@ -347,14 +420,14 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     const auto distance = [&](const sgemm_emu_view_t& v) {
         return [&](int r) {
             return (uint32_t)(r / tiles.heads * (int)v.token + r % tiles.heads * (int)v.head) *
-                   (uint32_t)sizeof(T);
+                   (uint32_t)sizeof(E);
         };
     };
-    fq.rows(distance(a.q), thread);
-    fd.rows(distance(a.d_o), thread);
-    float st_lse = 0.0f, st_delta = 0.0f;
+    fq.rows(distance(args.q), thread);
+    fd.rows(distance(args.d_o), thread);
+    float st_lse = 0.0f, st_delta = 0.0f, st_q = 0.0f, st_do = 0.0f;
     int st_seen = 0;
-    int from_along = QD::from_along(lane), from_across = QD::from_across(lane);
+    int from_along = QD::One::from_along(lane), from_across = QD::One::from_across(lane);
     const auto load = [&](int t) {
         const int token0 = t / tiles.parts * tiles.tokens, head0 = t % tiles.parts * tiles.heads;
         const int tokens_in = min(tiles.tokens, tokens - token0);
@@ -368,20 +441,26 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             int row = thread;
             asm volatile("" : "+v"(row));
             const int token = row / tiles.heads, h = row % tiles.heads;
-            st_lse = -__builtin_inff(), st_delta = 0.0f;
+            st_lse = -__builtin_inff(), st_delta = 0.0f, st_q = 0.0f, st_do = 0.0f;
             st_seen = a.causal ? token0 + token + shift : sk.count;
             if (token < tokens_in && h < heads_in) {
                 const int64_t i = token0 + token;
                 st_lse = lse0[i * a.lse.token + (head0 + h) * a.lse.head];
-                st_delta = delta0[i * a.q_heads + head0 + h];
+                const int64_t at = row_in_all + i * a.q_heads + head0 + h;
+                st_delta = args.delta[at];
+                if constexpr (kSplit) st_q = args.q_factors[at], st_do = args.do_factors[at];
             }
         }
-        fq.start(to, q0 + token0 * a.q.token + head0 * a.q.head, a.size, thread, there);
-        fd.start(to + kTileBytes, d0 + token0 * a.d_o.token + head0 * a.d_o.head, a.size, thread,
-                 there);
+        const E* q = q0 + token0 * args.q.token + head0 * args.q.head;
+        const E* o = d0 + token0 * args.d_o.token + head0 * args.d_o.head;
+#pragma unroll
+        for (int i = 0; i < kPlanes<T>; ++i) {
+            fq.start(to + i * QD::kPlaneBytes, q + i * kWidth<D>, width, thread, there);
+            fd.start(to + kTileBytes + i * QD::kPlaneBytes, o + i * kWidth<D>, width, thread, there);
+        }
     };
     if (t0 < count) load(count - 1);
-    const float c = a.scale * kLog2e;
+    const float c = a.scale * kLog2e * k_factor;
     // from the last rows, which all blocks of a head have, so that those that run beside each
     // other find them in the caches
     for (int t = count - 1; t >= t0; --t) {
@@ -395,6 +474,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             rw.z[thread] = st_lse == -__builtin_inff() ? __builtin_inff() : st_lse * kLog2e - kShift;
             rw.delta[thread] = -st_delta;
             rw.seen[thread] = st_seen;
+            if constexpr (kSplit) rw.q[thread] = st_q, rw.d_o[thread] = st_do;
         }
         lds_barrier();
         if (t > t0) load(t - 1);
@@ -405,34 +485,45 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         // sums need)
         asm volatile("" : "+v"(from_along), "+v"(from_across));
         const int row0 = 32 * row_group;
-        const uint32_t q_along = QD::base(qt + row0 * QD::kRowBytes, from_along);
-        const uint32_t o_along = QD::base(ot + row0 * QD::kRowBytes, from_along);
-        const uint32_t q_across = QD::base(qt + row0 * QD::kRowBytes, from_across);
-        const uint32_t o_across = QD::base(ot + row0 * QD::kRowBytes, from_across);
+        const uint32_t q_along = QD::One::base(qt + row0 * kRowBytes, from_along);
+        const uint32_t o_along = QD::One::base(ot + row0 * kRowBytes, from_along);
+        const uint32_t q_across = QD::One::base(qt + row0 * kRowBytes, from_across);
+        const uint32_t o_across = QD::One::base(ot + row0 * kRowBytes, from_across);
         const auto per_row = [&](const float* x, int i) {  // rows of registers i to i + 3
-            return *reinterpret_cast<const Pack<float, 4>::type*>(x + row0 + 8 * (i / 4) + 4 * half);
+            return four_floats(x + row0 + 8 * (i / 4) + 4 * half);
         };
         f32x16 P{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const auto x = per_row(rw.delta, i);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) dP[i + j] = x[j];
+            for (int j = 0; j < 4; ++j) dP[i + j] = kSplit ? 0.0f : x[j];
         }
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
             P = mma(QD::along(q_along, 0, kb), key_block(kb), P);
             dP = mma(QD::along(o_along, 0, kb), value_block(kb), dP);
         }
-        // reads two steps ahead of the products that take them
-        constexpr auto reads = [](int kb) {
-            return kb >= kBlocks ? 0 : 2 + (kb >= kKeyBlocks) + (kb >= kValueBlocks);
-        };
-        __builtin_amdgcn_sched_group_barrier(kLdsRead, 4 + reads(0) + reads(1), 0);
-        schedule_steps<kBlocks>([&](auto step) {
-            __builtin_amdgcn_sched_group_barrier(kMatrix, 2 * kPerFragment, 0);
-            __builtin_amdgcn_sched_group_barrier(kLdsRead, reads(decltype(step)::value + 2), 0);
-        });
+        if constexpr (!kSplit) {  // reads two steps ahead of the products that take them
+            constexpr auto reads = [](int kb) {
+                return kb >= kBlocks ? 0 : 2 + (kb >= kKeyBlocks) + (kb >= kValueBlocks);
+            };
+            __builtin_amdgcn_sched_group_barrier(kLdsRead, 4 + reads(0) + reads(1), 0);
+            schedule_steps<kBlocks>([&](auto step) {
+                __builtin_amdgcn_sched_group_barrier(kMatrix, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsRead, reads(decltype(step)::value + 2), 0);
+            });
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const auto x = per_row(rw.q, i), y = per_row(rw.d_o, i), z = per_row(rw.delta, i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    P[i + j] *= x[j];
+                    dP[i + j] = __builtin_fmaf(dP[i + j] * y[j], v_factor, z[j]);
+                }
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const auto x = per_row(rw.z, i);
@@ -448,9 +539,19 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] *= P[i];
+        if constexpr (kSplit) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const auto x = per_row(rw.q, i), y = per_row(rw.d_o, i);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) P[i + j] *= y[j], dP[i + j] *= x[j];
+            }
+            fit_v.fit(P, dV);
+            P = times(P, fit_v.f);
+        }
 #pragma unroll
         for (int kb = 0; kb < kParts; ++kb) {
-            const Frag<T> x = operand<T>(P, kb);
+            const Operand<T> x = operand<T>(P, kb);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
                 dV[dt] = mma(QD::across(o_across, kb, 32 * dt), x, dV[dt]);
@@ -461,7 +562,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         }
 #pragma unroll
         for (int kb = 0; kb < kParts; ++kb) {
-            const Frag<T> x = operand<T>(dP, kb);
+            const Operand<T> x = operand<T>(dP, kb);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
                 dK[dt] = mma(QD::across(q_across, kb, 32 * dt), x, dK[dt]);
@@ -469,7 +570,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     }
 
     // the sums of the waves with the same keys, in the order of their rows
-    const auto join = [&](f32x16(&sum)[D / 32], float f, T* to) __attribute__((always_inline)) {
+    const auto join = [&](f32x16(&sum)[D / 32], float f, Out<T>* to) __attribute__((always_inline)) {
         typedef Pack<float, 4>::type Four;
         lds_barrier();
         Four* const mine = reinterpret_cast<Four*>(lds) +
@@ -495,42 +596,66 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
                     x += reinterpret_cast<const Four*>(lds)[((g - 1) * Shape::kKeyGroups + key_group) *
                                                                 (D / 8) * 64 +
                                                             (dt * 4 + i) * 64 + lane];
-                store_four<T, kVec>(to, 32 * dt + acc_row(4 * i, half), a.size, x[0], x[1], x[2], x[3]);
+                store_four<Out<T>, kVec>(to, 32 * dt + acc_row(4 * i, half), a.size, x[0], x[1], x[2], x[3]);
             }
     };
-    join(dV, kBack, row_of<T>(a.dv, packed, n, sk, head) + key_in * a.dv.token);
+    join(dV, kSplit ? kBack / fit_v.f : kBack, row_of<Out<T>>(a.dv, packed, n, sk, head) + key_in * a.dv.token);
     join(dK, kNarrow<T> ? a.scale * kBack / fit.f : a.scale,
-         row_of<T>(a.dk, packed, n, sk, head) + key_in * a.dk.token);
+         row_of<Out<T>>(a.dk, packed, n, sk, head) + key_in * a.dk.token);
+}
+
+int64_t delta_bytes(const attention_emu_backward_t& a) {
+    const int64_t rows = a.cu_seqlens != nullptr ? a.tokens : (int64_t)a.batch * a.tokens;
+    return (rows * a.q_heads * 4 + 255) / 256 * 256;
 }
 
 }  // namespace
 
 int64_t attention_backward_workspace(const attention_emu_backward_t& a) {
-    const int64_t rows = a.cu_seqlens != nullptr ? a.tokens : (int64_t)a.batch * a.tokens;
-    return (rows * a.q_heads * 4 + 255) / 256 * 256;
+    const int64_t batch = a.cu_seqlens != nullptr ? 1 : a.batch;
+    int64_t bytes = delta_bytes(a);
+    if (a.dtype == SGEMM_EMU_F32)
+        bytes += 2 * split_bytes(batch * a.tokens, a.q_heads, a.size) +
+                 2 * split_bytes(batch * a.keys, a.k_heads, a.size);
+    return bytes;
 }
 
-hipError_t launch_attention_backward(const attention_emu_backward_t& args, hipStream_t stream) {
-    attention_emu_backward_t a = args;
-    if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) a.cu_keys = a.cu_seqlens;
+hipError_t launch_attention_backward(const attention_emu_backward_t& a, hipStream_t stream) {
+    BackwardArgs args{a, static_cast<float*>(a.workspace), a.q, a.k, a.v, a.d_o, nullptr, nullptr,
+                      nullptr, nullptr};
+    if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) args.a.cu_keys = a.cu_seqlens;
+    const bool packed = a.cu_seqlens != nullptr;
     const int e = a.dtype == SGEMM_EMU_F32 ? 4 : 2;
     bool vec = a.size * e % 16 == 0;
-    for (const sgemm_emu_view_t* x : {&a.q, &a.k, &a.v, &a.o, &a.d_o, &a.dq, &a.dk, &a.dv})
+    for (const sgemm_emu_view_t* x : {&a.o, &a.d_o, &a.dq, &a.dk, &a.dv})
         vec = vec && rows_aligned16(*x, e);
-    const bool packed = a.cu_seqlens != nullptr;
+    if (a.dtype == SGEMM_EMU_F32) {
+        Splitter split(a.size, static_cast<char*>(a.workspace) + delta_bytes(a));
+        const int batch = packed ? 1 : a.batch;
+        const SplitTensor q = split.add(a.q, batch, a.tokens, a.q_heads);
+        const SplitTensor k = split.add(a.k, batch, a.keys, a.k_heads);
+        const SplitTensor v = split.add(a.v, batch, a.keys, a.k_heads);
+        const SplitTensor d_o = split.add(a.d_o, batch, a.tokens, a.q_heads);
+        args.q = q.planes, args.k = k.planes, args.v = v.planes, args.d_o = d_o.planes;
+        args.q_factors = q.factors, args.k_factors = k.factors, args.v_factors = v.factors;
+        args.do_factors = d_o.factors;
+        if (hipError_t e = split.launch(stream)) return e;
+    } else {
+        for (const sgemm_emu_view_t* x : {&a.q, &a.k, &a.v}) vec = vec && rows_aligned16(*x, e);
+    }
     const int64_t group = a.q_heads / a.k_heads;
     const int64_t q_parts = most_parts(a.batch, a.tokens * group, kDqRows, packed) * a.k_heads;
-    return by_form(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
+    return by_form<split_t>(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
         if (a.tokens > 0)
             if (hipError_t e = launch_blocks(attention_dq_kernel<T, D, kVec>, q_parts, 64 * kDqWaves,
-                                             stream, a))
+                                             stream, args))
                 return e;
         using Shape = DkvShape<T, D>;
         const int64_t k_parts = most_parts(a.batch, a.keys, Shape::kKeys, packed) * a.k_heads;
-        return launch_blocks(attention_dkv_kernel<T, D, kVec>, k_parts, Shape::kThreads, stream, a);
+        return launch_blocks(attention_dkv_kernel<T, D, kVec>, k_parts, Shape::kThreads, stream, args);
     });
 }
 

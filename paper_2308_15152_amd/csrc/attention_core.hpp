@@ -28,28 +28,36 @@ struct Attend {
     static_assert(kShared || kKeys == 32, "");
     static constexpr int kThreads = 64 * kRowGroups * kKeyGroups;
     static constexpr int kRows = 32 * kRowGroups;
-    static constexpr int kTileBytes = kKeys * Tile<T, D>::kRowBytes;
+    typedef Elem<T> E;
+    static constexpr bool kSplit = kPlanes<T> == 2;
+    static_assert(kShared || !kSplit, "");
+    using KV = Planes<T, D, kKeys>;
+    static constexpr int kTileBytes = KV::kBytes;
     static constexpr int kPlace = (kShared ? 2 : 1) * kTileBytes;  // of a tile's keys and values
     static constexpr int kTiles = kKeyGroups * 2 * kPlace;
     static constexpr int kJoinRow = D + 4;  // floats
     static constexpr int kJoin = kShared ? 0 : kKeyGroups * 32 * (kJoinRow + 2) * 4;
-    static constexpr int kLds = (kTiles > kJoin ? kTiles : kJoin) + 16;
+    static constexpr int kFactors = kSplit ? 2 * kKeys : 0;  // of a tile's keys and values
+    static constexpr int kLds = (kTiles > kJoin ? kTiles : kJoin) + 2 * kFactors * 4 + 16;
     static constexpr int kTileThreads = kShared ? kThreads : 64;
     // FP16 weights keep 11 bits down to 2^-14: 2^-21 of a row's largest
-    static constexpr float kBias = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 7.0f : 0.0f;
+    static constexpr float kBias = __is_same(E, f16_t) ? 7.0f : 0.0f;
     static constexpr float kSlack = 8.0f;
 
     // rows: query rows there are; the block takes row0 to row0 + kRows - 1.
     // q_row(r): its elements; limit(r): how many keys it sees (not decreasing in r).
     // k, v: row 0 of the keys and values; the pass goes over keys first to end - 1.
     // out(r): where a row's results go; of that, sums(l, z, here) and four(d, ...).
-    template <class QRow, class Limit, class Out>
+    // factors: what the rows of split tensors have been divided by: q(r), k[], v[] (`step` apart).
+    template <class QRow, class Limit, class Results, class Factors>
     static __device__ __attribute__((always_inline)) void run(
-        char* lds, int rows, int row0, QRow q_row, Limit limit, const T* k, int64_t k_token,
-        const T* v, int64_t v_token, int first, int end, int size, float c, bool negative, Out out) {
-        using KV = Tile<T, D>;
-        constexpr int kBlocks = D / kBlock<T>;
-        constexpr int kParts = 32 / kBlock<T>;  // operand blocks of 32 keys
+        char* lds, int rows, int row0, QRow q_row, Limit limit, const E* k, int64_t k_token,
+        const E* v, int64_t v_token, int first, int end, int size, float c, bool negative,
+        Results out, Factors factors) {
+        constexpr int kBlocks = D / kBlock<E>;
+        constexpr int kParts = 32 / kBlock<E>;  // operand blocks of 32 keys
+        constexpr bool kVecTile = kVec || kSplit;
+        const int width = kSplit ? kWidth<D> : size;
         const int lane = threadIdx.x & 63, half = lane >> 5;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int group = kShared ? 0 : wave;
@@ -59,17 +67,15 @@ struct Attend {
         int* bad = reinterpret_cast<int*>(lds + kLds - 16);
 
         const int row = wave_row + (lane & 31), last_row = rows - 1;
-        Frag<T> Q[kBlocks];
+        Operand<T> Q[kBlocks];
         {
-            const T* p = q_row(min(row, last_row));
+            const E* p = q_row(min(row, last_row));
 #pragma unroll
             for (int kb = 0; kb < kBlocks; ++kb) {
-                Q[kb] = load_chunk<T, kVec>(p, 2 * kb + half, size, row < rows);
-                if (negative)
-#pragma unroll
-                    for (int j = 0; j < kPer<T>; ++j) Q[kb][j] = -Q[kb][j];
+                Q[kb] = load_operand<T, D, kVec>(p, 2 * kb + half, size, row < rows);
             }
         }
+        if constexpr (kSplit) c *= factors.q(min(row, last_row));
         // keys seen by the lane's row, by the wave's first and last one, by the block's
         const auto seen = [&](int r) { return min(max(limit(min(r, last_row)), first), end); };
         const int lim = seen(row), lim_min = seen(wave_row), lim_max = seen(wave_row + 31);
@@ -78,23 +84,26 @@ struct Attend {
         // from this tile on, some row of the block does not see all of the keys
         const int cleared = (block_min - first) / kKeys;
 
-        const int from_along = KV::from_along(lane), from_across = KV::from_across(lane);
+        const int from_along = KV::One::from_along(lane);
+        const int from_across = KV::One::from_across(lane);
 
         f32x16 O[D / 32];
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) O[dt] = f32x16{};
-        float l = 0.0f, z = -1e30f;
+        float l = 0.0f, z = -1e30f, unit = 0x1p-126f;  // O is in units of the largest factor so far
         bool found = false;
-        if (threadIdx.x == 0) *bad = 0;
-        if (kVec && size < Tile<T, D>::kRowBytes / (int)sizeof(T))
+        if (kVecTile && width < kWidth<D>) {
             clear_lds(lds, kTiles, threadIdx.x, kThreads);
-        lds_barrier();
+            lds_barrier();
+        }
 
-        using Load = Flow<T, D, kKeys, kTileThreads, kVec>;
+        using Load = Flow<E, D, kKeys, kTileThreads, kVecTile>;
         Load fk, fv;
-        Frag<T> K[kShared ? 1 : kBlocks];
+        Operand<T> K[kShared ? 1 : kBlocks];
+        float* const of_tiles = reinterpret_cast<float*>(lds + kLds - 16) - 2 * kFactors;
+        float st_factor = 0.0f;
         const int step = kShared ? 1 : kKeyGroups;
-        const uint32_t k_row = (uint32_t)k_token * sizeof(T), v_row = (uint32_t)v_token * sizeof(T);
+        const uint32_t k_row = (uint32_t)k_token * sizeof(E), v_row = (uint32_t)v_token * sizeof(E);
         const auto place = [&](int t) {
             return tiles + ((kShared ? t : t / kKeyGroups) & 1) * kPlace;
         };
@@ -104,17 +113,40 @@ struct Attend {
             const int key = first + t * kKeys, most = end - 1 - key;
             // (keys behind the last one are masked, and values there cleared if need be)
             const auto there = [&](int, int r) { return r <= most; };
+            if constexpr (kSplit) {
+                const int i = tile_thread % kKeys;
+                if (tile_thread < kFactors)
+                    st_factor = i > most ? 0.0f
+                                         : (tile_thread < kKeys ? factors.k
+                                                                : factors.v)[(key + i) * factors.step];
+            }
             if constexpr (kShared) {
-                fk.start(place(t), k + key * k_token, size, tile_thread, there);
+#pragma unroll
+                for (int i = 0; i < kPlanes<T>; ++i)
+                    fk.start(place(t) + i * KV::kPlaneBytes, k + key * k_token + i * kWidth<D>, width,
+                             tile_thread, there);
             } else {
-                const T* p = k + (key + min(lane & 31, most)) * k_token;
+                const E* p = k + (key + min(lane & 31, most)) * k_token;
 #pragma unroll
                 for (int kb = 0; kb < kBlocks; ++kb)
-                    K[kb] = load_chunk<T, kVec>(p, 2 * kb + half, size, true);
+                    K[kb] = load_operand<T, D, kVec>(p, 2 * kb + half, size, true);
             }
-            fv.start(place(t) + kPlace - kTileBytes, v + key * v_token, size, tile_thread, there);
+#pragma unroll
+            for (int i = 0; i < kPlanes<T>; ++i)
+                fv.start(place(t) + kPlace - kTileBytes + i * KV::kPlaneBytes,
+                         v + key * v_token + i * kWidth<D>, width, tile_thread, there);
         };
         if (group < count) load(group);
+        // (after the loads: these wait for the first of them)
+        if (threadIdx.x == 0) *bad = 0;
+        lds_barrier();
+        if (negative)
+#pragma unroll
+            for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < kPlanes<T>; ++i)
+#pragma unroll
+                    for (int j = 0; j < kPer<E>; ++j) Q[kb].p[i][j] = -Q[kb].p[i][j];
         for (int t = group; t < count; t += step) {
             char* kt = place(t);
             char* vt = kt + kPlace - kTileBytes;
@@ -122,7 +154,12 @@ struct Attend {
             fv.finish(vt, tile_thread);
             // values that are not finite reach only rows that see them: where some row
             // does not, they are left out here and added at the end
-            if (t >= cleared) found |= Load::clear_not_finite(vt, tile_thread);
+            if (t >= cleared)
+#pragma unroll
+                for (int i = 0; i < kPlanes<T>; ++i)
+                    found |= Load::clear_not_finite(vt + i * KV::kPlaneBytes, tile_thread);
+            float* const of_tile = of_tiles + (t & 1) * kFactors;
+            if (kSplit && tile_thread < kFactors) of_tile[tile_thread] = st_factor;
             f32x16 S[kKeys / 32];
             if constexpr (kShared) {
                 lds_barrier();
@@ -142,7 +179,32 @@ struct Attend {
                     S[s] = f32x16{};
 #pragma unroll
                     for (int kb = 0; kb < kBlocks; ++kb)
-                        S[s] = mma(KV::along(KV::base(kt, from_along), 32 * s, kb), Q[kb], S[s]);
+                        S[s] = mma(KV::along(KV::One::base(kt, from_along), 32 * s, kb), Q[kb], S[s]);
+                }
+            }
+            // factors of registers i to i + 3
+            const auto four_of = [&](const float* x, int s, int i) {
+                return *reinterpret_cast<const Pack<float, 4>::type*>(x + 32 * s + 8 * (i / 4) +
+                                                                      4 * half);
+            };
+            if constexpr (kSplit) {
+                float most = 0.0f;
+#pragma unroll
+                for (int s = 0; s < kKeys / 32; ++s)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const auto x = four_of(of_tile, s, i), y = four_of(of_tile + kKeys, s, i);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j], most = fmaxf(most, y[j]);
+                    }
+                most = max_halves(most);
+                if (__any(most > unit)) {
+                    const float f = unit * inverse_of_power(most);
+#pragma unroll
+                    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) O[dt][i] *= f;
+                    unit = most;
                 }
             }
             if (key0 + kKeys > lim_min) {
@@ -175,12 +237,22 @@ struct Attend {
                     S[s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s][i], c, -z));
                     l += S[s][i];
                 }
+                if constexpr (kSplit) {
+                    const float by = inverse_of_power(unit);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const auto x = four_of(of_tile + kKeys, s, i);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j] * by;
+                    }
+                }
 #pragma unroll
                 for (int kb = 0; kb < kParts; ++kb) {
-                    const Frag<T> P = operand<T>(S[s], kb);
+                    const Operand<T> P = operand<T>(S[s], kb);
 #pragma unroll
                     for (int dt = 0; dt < D / 32; ++dt)
-                        O[dt] = mma(KV::across(KV::base(vt, from_across), s * kParts + kb, 32 * dt), P, O[dt]);
+                        O[dt] = mma(KV::across(KV::One::base(vt, from_across), s * kParts + kb, 32 * dt),
+                                    P, O[dt]);
                 }
             }
         }
@@ -198,7 +270,7 @@ struct Attend {
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
                                 O[dt][i] += not_finite(v + j * v_token, 32 * dt + acc_row(i, half), size);
-                const float f = l == 0.0f ? 0.0f : 1.0f / l;
+                const float f = l == 0.0f ? 0.0f : (kSplit ? unit : 1.0f) / l;
                 auto to = out(row);
                 to.sums(l, z, half == 0);
 #pragma unroll
@@ -253,7 +325,7 @@ struct Attend {
 
     // Element d of a row of values if it is not finite, else 0.  A positive weight of infinity
     // or NaN is the same.
-    static __device__ inline float not_finite(const T* p, int d, int size) {
+    static __device__ inline float not_finite(const E* p, int d, int size) {
         const float x = d < size ? to_f32(p[d]) : 0.0f;
         return __builtin_fabsf(x) < __builtin_inff() ? 0.0f : x;
     }

@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "attention_core.hpp"
+#include "attention_split.h"
 
 namespace sgemm_emu {
 
@@ -12,6 +13,19 @@ struct ForwardArgs {
     attention_emu_forward_t a;
     int count;  // parts that a block's keys are cut into
     Parts parts;
+    // the operands, split if they are FP32
+    sgemm_emu_view_t q, k, v;
+    const float *q_factors, *k_factors, *v_factors;
+};
+
+struct ForwardFactors {
+    const float* first;  // of the sequence's tokens
+    int q_heads, head, group;
+    const float *k, *v;
+    int64_t step;
+    __device__ inline float q(int r) const {
+        return first[(int64_t)(r / group) * q_heads + head + r % group];
+    }
 };
 
 template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
@@ -42,15 +56,20 @@ __global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_for
     const Span sq = span_of(a.cu_seqlens, n, a.tokens);
     const Span sk = span_of(a.cu_keys, n, a.keys);
     const int rows = sq.count * group;
-    const T* q = row_of<T>(a.q, packed, n, sq, head * group);
-    const T* k = row_of<T>(a.k, packed, n, sk, head);
-    const T* v = row_of<T>(a.v, packed, n, sk, head);
+    typedef Elem<T> E;
+    const E* q = row_of<E>(args.q, packed, n, sq, head * group);
+    const E* k = row_of<E>(args.k, packed, n, sk, head);
+    const E* v = row_of<E>(args.v, packed, n, sk, head);
     float* lse = a.lse.p == nullptr ? nullptr : row_of<float>(a.lse, packed, n, sq, head * group);
-    T* o = row_of<T>(a.o, packed, n, sq, head * group);
+    auto* o = row_of<Out<T>>(a.o, packed, n, sq, head * group);
     const int64_t first_token = packed ? sq.first : (int64_t)n * a.tokens;
+    const int64_t first_key = (packed ? sk.first : (int64_t)n * a.keys) * a.k_heads + head;
+    const ForwardFactors factors{args.q_factors + first_token * a.q_heads, a.q_heads, head * group,
+                                 group, args.k_factors + first_key, args.v_factors + first_key,
+                                 a.k_heads};
     const auto out = [&](int r) {
         const int token = r / group, h = r % group;
-        return row_out<T, D, kVec>(args.parts, part,
+        return row_out<Out<T>, D, kVec>(args.parts, part,
                                    (first_token + token) * a.q_heads + head * group + h,
                                    o + token * a.o.token + h * a.o.head,
                                    lse ? lse + token * a.lse.token + h * a.lse.head : nullptr, a.size);
@@ -63,8 +82,9 @@ __global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_for
     const int first = min(part * each, seen), end = min(first + each, seen);
     Pass::run(
         lds, rows, tile * Pass::kRows,
-        [&](int r) { return q + r / group * a.q.token + r % group * a.q.head; }, limit, k, a.k.token, v,
-        a.v.token, first, end, a.size, __builtin_fabsf(a.scale) * kLog2e, a.scale < 0.0f, out);
+        [&](int r) { return q + r / group * args.q.token + r % group * args.q.head; }, limit, k,
+        args.k.token, v, args.v.token, first, end, a.size, __builtin_fabsf(a.scale) * kLog2e,
+        a.scale < 0.0f, out, factors);
 }
 
 // Blocks of `rows` query rows.
@@ -76,43 +96,68 @@ int64_t blocks_of(const attention_emu_forward_t& a, int rows) {
 constexpr int kRowGroups = 4;
 
 // Parts of the keys: where the blocks are fewer than two for each CU, as many as fill
-// those, of at least 256 keys each.
+// those, of at least 256 keys each, if that saves a block more steps of 64 keys than the join
+// costs (its launch and traffic, about twelve of them).
 int parts_of(const attention_emu_forward_t& a) {
     const int64_t blocks = blocks_of(a, 32 * kRowGroups), most = (a.keys + 255) / 256;
     if (blocks == 0 || most <= 1 || a.cu_seqlens != nullptr) return 1;
-    return (int)std::max<int64_t>(1, std::min(most, 512 / blocks));
+    const int64_t parts = std::max<int64_t>(1, std::min(most, 512 / blocks));
+    const int64_t steps = (a.keys + 63) / 64;
+    return steps - steps / parts > 12 ? (int)parts : 1;
 }
 
-int64_t rows_of(const attention_emu_forward_t& a) {
-    return (a.cu_seqlens != nullptr ? 1 : (int64_t)a.batch) * a.tokens * a.q_heads;
+// Tokens and keys in all.
+int64_t tokens_of(const attention_emu_forward_t& a) {
+    return (a.cu_seqlens != nullptr ? 1 : (int64_t)a.batch) * a.tokens;
+}
+int64_t keys_of(const attention_emu_forward_t& a) {
+    return (a.cu_seqlens != nullptr ? 1 : (int64_t)a.batch) * a.keys;
+}
+
+int64_t bytes_of_parts(const attention_emu_forward_t& a, int parts) {
+    return parts == 1 ? 0 : parts_bytes(parts, tokens_of(a) * a.q_heads, a.size);
 }
 
 }  // namespace
 
 int64_t attention_forward_workspace(const attention_emu_forward_t& a) {
-    const int parts = parts_of(a);
-    return parts == 1 ? 0 : parts_bytes(parts, rows_of(a), a.size);
+    int64_t bytes = bytes_of_parts(a, parts_of(a));
+    if (a.dtype == SGEMM_EMU_F32)
+        bytes += split_bytes(tokens_of(a), a.q_heads, a.size) +
+                 2 * split_bytes(keys_of(a), a.k_heads, a.size);
+    return bytes;
 }
 
-hipError_t launch_attention_forward(const attention_emu_forward_t& given, hipStream_t stream) {
-    const int parts = parts_of(given);
-    ForwardArgs args{given, parts, parts_in(given.workspace, parts, rows_of(given), given.size)};
-    attention_emu_forward_t& a = args.a;
-    if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) a.cu_keys = a.cu_seqlens;
+hipError_t launch_attention_forward(const attention_emu_forward_t& a, hipStream_t stream) {
+    const int parts = parts_of(a);
+    ForwardArgs args{a, parts, parts_in(a.workspace, parts, tokens_of(a) * a.q_heads, a.size), a.q, a.k,
+                     a.v, nullptr, nullptr, nullptr};
+    if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) args.a.cu_keys = a.cu_seqlens;
     const int e = a.dtype == SGEMM_EMU_F32 ? 4 : 2;
-    const bool vec = a.size * e % 16 == 0 && rows_aligned16(a.q, e) && rows_aligned16(a.k, e) &&
-                     rows_aligned16(a.v, e) && rows_aligned16(a.o, e);
-    return by_form(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
+    bool vec = a.size * e % 16 == 0 && rows_aligned16(a.o, e);
+    if (a.dtype == SGEMM_EMU_F32) {
+        Splitter split(a.size, static_cast<char*>(a.workspace) + bytes_of_parts(a, parts));
+        const int batch = a.cu_seqlens != nullptr ? 1 : a.batch;
+        const SplitTensor q = split.add(a.q, batch, a.tokens, a.q_heads);
+        const SplitTensor k = split.add(a.k, batch, a.keys, a.k_heads);
+        const SplitTensor v = split.add(a.v, batch, a.keys, a.k_heads);
+        args.q = q.planes, args.k = k.planes, args.v = v.planes;
+        args.q_factors = q.factors, args.k_factors = k.factors, args.v_factors = v.factors;
+        if (hipError_t e = split.launch(stream)) return e;
+    } else {
+        vec = vec && rows_aligned16(a.q, e) && rows_aligned16(a.k, e) && rows_aligned16(a.v, e);
+    }
+    return by_form<split_t>(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
-        constexpr int kKeys = sizeof(T) == 2 || D <= 64 ? 64 : 32;
+        constexpr int kKeys = kPlanes<T> == 1 || D <= 64 ? 64 : 32;
         if (hipError_t e = launch_blocks(attention_forward_kernel<T, D, kRowGroups, 1, kKeys, kVec>,
                                          blocks_of(a, 32 * kRowGroups) * parts, 64 * kRowGroups,
                                          stream, args))
             return e;
         if (parts == 1) return hipSuccess;
-        return launch_join<T, D, kVec>(
+        return launch_join<Out<T>, D, kVec>(
             JoinArgs{args.parts, a.o, a.lse, parts, a.tokens, a.q_heads, a.size, nullptr, 0}, stream);
     });
 }

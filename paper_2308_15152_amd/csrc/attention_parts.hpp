@@ -32,6 +32,7 @@ inline Parts parts_in(void* workspace, int64_t parts, int64_t rows, int size) {
 }
 
 // Where a pass leaves a row.
+// (T: the results' type)
 template <class T, bool kVec>
 struct RowOut {
     T* o;

@@ -73,15 +73,22 @@ struct Number {
     static constexpr int value = N;
 };
 
-// Calls f(T{}, Number<padded size>, Number<rows move as vectors>).
-template <class F>
+// Calls f(T{}, Number<padded size>, Number<rows move as vectors>), T one of the types or F32 in
+// the place of FP32.
+template <class F32, class F>
 inline hipError_t by_form(int dtype, int size, bool vec, F&& f) {
-    return by_dtype(dtype, [&](auto t) {
-        const auto with = [&](auto d) {
+    const auto with = [&](auto t) {
+        const auto and_with = [&](auto d) {
             return vec ? f(t, d, Number<1>{}) : f(t, d, Number<0>{});
         };
-        return size <= 64 ? with(Number<64>{}) : size <= 96 ? with(Number<96>{}) : with(Number<128>{});
-    });
+        return size <= 64 ? and_with(Number<64>{})
+                          : size <= 96 ? and_with(Number<96>{}) : and_with(Number<128>{});
+    };
+    switch (dtype) {
+        case SGEMM_EMU_BF16: return with(bf16_t{});
+        case SGEMM_EMU_F16: return with(f16_t{});
+        default: return with(F32{});
+    }
 }
 
 }  // namespace sgemm_emu

@@ -31,6 +31,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
     const attention_emu_step_t& a = s.a;
     const int group = a.q_heads / a.k_heads;
     const float c = __builtin_fabsf(a.scale) * kLog2e;
+    const int none = 0;  // (tensors that are not split have no factors)
     int block = first_block + (int)blockIdx.x;
     const int prefix_blocks = s.prefix_parts * s.prefix_tiles * a.k_heads;
     // results of part p for query head h of token t of all
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
             [&](int) { return a.prefix; },
             static_cast<const T*>(a.prefix_k.p) + head * a.prefix_k.head, a.prefix_k.token,
             static_cast<const T*>(a.prefix_v.p) + head * a.prefix_v.head, a.prefix_v.token, first,
-            end, a.size, c, a.scale < 0.0f, out);
+            end, a.size, c, a.scale < 0.0f, out, none);
         return;
     }
     block -= prefix_blocks;
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         [&](int r) { return r / group + shift; },
         static_cast<const T*>(a.k.p) + at * a.k.batch + head * a.k.head, a.k.token,
         static_cast<const T*>(a.v.p) + at * a.v.batch + head * a.v.head, a.v.token, first, end,
-        a.size, c, a.scale < 0.0f, out);
+        a.size, c, a.scale < 0.0f, out, none);
 }
 
 // How the keys are cut.
@@ -125,7 +126,7 @@ hipError_t launch_attention_step(const attention_emu_step_t& a, hipStream_t stre
     const bool vec = a.size * e % 16 == 0 && rows_aligned16(a.q, e) && rows_aligned16(a.k, e) &&
                      rows_aligned16(a.v, e) && rows_aligned16(a.o, e) &&
                      (!prefix || (rows_aligned16(a.prefix_k, e) && rows_aligned16(a.prefix_v, e)));
-    return by_form(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
+    return by_form<float>(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;

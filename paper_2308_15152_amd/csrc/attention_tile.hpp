@@ -38,16 +38,69 @@ __device__ inline f32x16 mma(Frag<float> a, Frag<float> b, f32x16 c) {
     return c;
 }
 
+// FP32 as two FP16 parts, hi = fp16(x s) and lo = fp16(x s - hi), s a power of two for each row
+// that brings its largest element to [2^14, 2^15): 22 bits of an element down to 2^-18 of
+// that.  A product takes three on the matrix instructions, lo lo being below FP32's rounding;
+// in tiles the parts are planes, one behind the other.
+struct split_t {};
+
+template <class T>
+struct FormOf {
+    typedef T Elem;  // of tiles and operands
+    typedef T Out;   // of the caller's tensors
+    static constexpr int kPlanes = 1;
+};
+template <>
+struct FormOf<split_t> {
+    typedef f16_t Elem;
+    typedef float Out;
+    static constexpr int kPlanes = 2;
+};
+template <class T>
+using Elem = typename FormOf<T>::Elem;
+template <class T>
+using Out = typename FormOf<T>::Out;
+template <class T>
+constexpr int kPlanes = FormOf<T>::kPlanes;
+
+// Elements of a row's place in a tile, and of a plane's row in memory.
+template <int D>
+constexpr int kWidth = D <= 64 ? 64 : 128;
+
+template <class T>
+struct Operand {
+    Frag<Elem<T>> p[kPlanes<T>];
+};
+
+template <class T>
+__device__ inline f32x16 mma(const Operand<T>& a, const Operand<T>& b, f32x16 c) {
+    if constexpr (kPlanes<T> == 2) {
+        c = mma(a.p[1], b.p[0], c);
+        c = mma(a.p[0], b.p[1], c);
+    }
+    return mma(a.p[0], b.p[0], c);
+}
+
 // Row of register i of an accumulator in this lane.
 __device__ inline int acc_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
 
 // Block kb of an accumulator's rows as an operand that is summed over them.
 template <class T>
-__device__ inline Frag<T> operand(const f32x16& x, int kb) {
-    Frag<T> f;
+__device__ inline Operand<T> operand(const f32x16& x, int kb) {
+    typedef Elem<T> E;
+    Operand<T> f;
 #pragma unroll
-    for (int j = 0; j < kPer<T>; ++j) f[j] = from_f32<T>(x[kPer<T> * kb + j]);
+    for (int j = 0; j < kPer<E>; ++j) {
+        const float y = x[kPer<E> * kb + j];
+        f.p[0][j] = from_f32<E>(y);
+        if constexpr (kPlanes<T> == 2) f.p[1][j] = from_f32<E>(y - to_f32(f.p[0][j]));
+    }
     return f;
+}
+
+// 1 / x of a power of two x, 2^-126 to 2^126.
+__device__ inline float inverse_of_power(float x) {
+    return __uint_as_float(0x7f000000u - __float_as_uint(x));
 }
 
 // Combines the two lanes that share an accumulator's column (lane and lane ^ 32).
@@ -72,7 +125,7 @@ __device__ inline uint32_t lds_address(const void* p) {
 // rows at one chunk, or 4 rows at four neighbouring ones.
 template <class T, int D>
 struct Tile {
-    static constexpr int kRowBytes = (D <= 64 ? 64 : 128) * (int)sizeof(T);
+    static constexpr int kRowBytes = kWidth<D> * (int)sizeof(T);
     static constexpr int kChunks = kRowBytes / 16;
     static constexpr int kMask = kChunks == 8 ? 7 : 15;  // chunk bits that are permuted
     static constexpr int kPlain = kChunks == 8 ? 3 : 4;  // how many
@@ -138,6 +191,26 @@ struct Tile {
     }
 };
 
+// The planes of a tile of kRows rows.
+template <class T, int D, int kRows>
+struct Planes {
+    using One = Tile<Elem<T>, D>;
+    static constexpr int kPlaneBytes = kRows * One::kRowBytes, kBytes = kPlanes<T> * kPlaneBytes;
+
+    static __device__ inline Operand<T> along(uint32_t base, int row0, int kb) {
+        Operand<T> f;
+#pragma unroll
+        for (int i = 0; i < kPlanes<T>; ++i) f.p[i] = One::along(base + i * kPlaneBytes, row0, kb);
+        return f;
+    }
+    static __device__ inline Operand<T> across(uint32_t base, int kb, int d0) {
+        Operand<T> f;
+#pragma unroll
+        for (int i = 0; i < kPlanes<T>; ++i) f.p[i] = One::across(base + i * kPlaneBytes, kb, d0);
+        return f;
+    }
+};
+
 // `size` elements of a row, from chunk c on, zero behind them.  kVec: rows are
 // 16-byte aligned and size a multiple of kPer.
 template <class T, bool kVec>
@@ -151,6 +224,20 @@ __device__ inline Frag<T> load_chunk(const T* row, int c, int size, bool inside)
 #pragma unroll
         for (int j = 0; j < kPer<T>; ++j)
             if (inside && c * kPer<T> + j < size) f[j] = row[c * kPer<T> + j];
+    }
+    return f;
+}
+
+// Chunk c of a row's planes, which are kWidth apart (and whole: zero behind the size).
+template <class T, int D, bool kVec>
+__device__ inline Operand<T> load_operand(const Elem<T>* row, int c, int size, bool inside) {
+    Operand<T> f;
+    if constexpr (kPlanes<T> == 1) {
+        f.p[0] = load_chunk<T, kVec>(row, c, size, inside);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            f.p[i] = load_chunk<Elem<T>, true>(row + i * kWidth<D>, c, kWidth<D>, inside);
     }
     return f;
 }
