@@ -201,30 +201,28 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
                      width, threadIdx.x, there);
         }
     };
-    const int from_along = KV::One::from_along(lane);
-    const int from_across = KV::One::from_across(lane);
+    const typename KV::Read read(lds, lane);
     if (count > 0) load(0);
-    for (int t = 0; t < count; ++t) {
-        char* kt = lds + (t & 1) * 2 * kTileBytes;
-        char* vt = kt + kTileBytes;
+    // one tile, in the first or the second place
+    const auto step = [&](int t, auto odd) __attribute__((always_inline)) {
+        constexpr int k_at = decltype(odd)::value * 2 * kTileBytes, v_at = k_at + kTileBytes;
+        char* kt = lds + k_at;
+        char* vt = lds + v_at;
         fk.finish(kt, threadIdx.x);
         fv.finish(vt, threadIdx.x);
-        float* const of_tile = of_tiles + (t & 1) * 2 * kDqKeys;
+        float* const of_tile = of_tiles + decltype(odd)::value * 2 * kDqKeys;
         if (kSplit && threadIdx.x < 2 * kDqKeys) of_tile[threadIdx.x] = st_factor;
         lds_barrier();
         if (t + 1 < count) load(t + 1);
         const int key0 = t * kDqKeys;
-        if (key0 >= lim_max) continue;
-        const uint32_t k_along = KV::One::base(kt, from_along);
-        const uint32_t v_along = KV::One::base(vt, from_along);
-        const uint32_t k_across = KV::One::base(kt, from_across);
+        if (key0 >= lim_max) return;
         f32x16 S{}, dP;
 #pragma unroll
         for (int i = 0; i < 16; ++i) dP[i] = kSplit ? 0.0f : -delta;
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
-            S = mma(KV::along(k_along, 0, kb), Q[kb], S);
-            dP = mma(KV::along(v_along, 0, kb), DO[kb], dP);
+            S = mma(KV::along(read, k_at, kb), Q[kb], S);
+            dP = mma(KV::along(read, v_at, kb), DO[kb], dP);
         }
         f32x16 by;  // the keys' factors
         if constexpr (kSplit) {
@@ -260,8 +258,12 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
             const Operand<T> x = operand<T>(dP, kb);
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
-                dQ[dt] = mma(KV::across(k_across, kb, 32 * dt), x, dQ[dt]);
+                dQ[dt] = mma(KV::across(read, k_at, kb, dt), x, dQ[dt]);
         }
+    };
+    for (int t = 0; t < count; t += 2) {
+        step(t, Number<0>{});
+        if (t + 1 < count) step(t + 1, Number<1>{});
     }
     if (!valid) return;
     const float f = kNarrow<T> ? a.scale / fit.f : a.scale;

@@ -84,8 +84,7 @@ struct Attend {
         // from this tile on, some row of the block does not see all of the keys
         const int cleared = (block_min - first) / kKeys;
 
-        const int from_along = KV::One::from_along(lane);
-        const int from_across = KV::One::from_across(lane);
+        const typename KV::Read read(tiles, lane);
 
         f32x16 O[D / 32];
 #pragma unroll
@@ -147,9 +146,11 @@ struct Attend {
                 for (int i = 0; i < kPlanes<T>; ++i)
 #pragma unroll
                     for (int j = 0; j < kPer<E>; ++j) Q[kb].p[i][j] = -Q[kb].p[i][j];
-        for (int t = group; t < count; t += step) {
-            char* kt = place(t);
-            char* vt = kt + kPlace - kTileBytes;
+        // one tile, in the first or the second of the wave's places
+        const auto tile = [&](int t, auto odd) __attribute__((always_inline)) {
+            constexpr int at = decltype(odd)::value * kPlace, v_at = at + kPlace - kTileBytes;
+            char* kt = tiles + at;
+            char* vt = tiles + v_at;
             if (kShared) fk.finish(kt, tile_thread);
             fv.finish(vt, tile_thread);
             // values that are not finite reach only rows that see them: where some row
@@ -158,7 +159,7 @@ struct Attend {
 #pragma unroll
                 for (int i = 0; i < kPlanes<T>; ++i)
                     found |= Load::clear_not_finite(vt + i * KV::kPlaneBytes, tile_thread);
-            float* const of_tile = of_tiles + (t & 1) * kFactors;
+            float* const of_tile = of_tiles + decltype(odd)::value * kFactors;
             if (kSplit && tile_thread < kFactors) of_tile[tile_thread] = st_factor;
             f32x16 S[kKeys / 32];
             if constexpr (kShared) {
@@ -171,7 +172,7 @@ struct Attend {
                 if (t + step < count) load(t + step);
             }
             const int key0 = first + t * kKeys;
-            if (key0 >= lim_max) continue;
+            if (key0 >= lim_max) return;
 
             if constexpr (kShared) {
 #pragma unroll
@@ -179,7 +180,7 @@ struct Attend {
                     S[s] = f32x16{};
 #pragma unroll
                     for (int kb = 0; kb < kBlocks; ++kb)
-                        S[s] = mma(KV::along(KV::One::base(kt, from_along), 32 * s, kb), Q[kb], S[s]);
+                        S[s] = mma(KV::along(read, at + 32 * s * KV::One::kRowBytes, kb), Q[kb], S[s]);
                 }
             }
             // factors of registers i to i + 3
@@ -251,10 +252,13 @@ struct Attend {
                     const Operand<T> P = operand<T>(S[s], kb);
 #pragma unroll
                     for (int dt = 0; dt < D / 32; ++dt)
-                        O[dt] = mma(KV::across(KV::One::base(vt, from_across), s * kParts + kb, 32 * dt),
-                                    P, O[dt]);
+                        O[dt] = mma(KV::across(read, v_at, s * kParts + kb, dt), P, O[dt]);
                 }
             }
+        };
+        for (int t = group; t < count; t += 2 * step) {
+            tile(t, Number<0>{});
+            if (t + step < count) tile(t + step, Number<1>{});
         }
         l = sum_halves(l);
         if (found) *bad = 1;

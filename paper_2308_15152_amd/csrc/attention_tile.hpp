@@ -161,22 +161,25 @@ struct Tile {
         return *(Lds*)(uintptr_t)(chunk_on(base, 2 * kb) + row0 * kRowBytes);
     }
 
+    // Two transposing reads of a 16-bit type: 16 lanes bring 4 rows of 16 elements, 8 bytes
+    // each, and every lane gets the 4 values of its column.
+    static __device__ inline Frag<T> across_at(uint32_t first, uint32_t second) {
+        typedef short Short4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) Short4 Lds;
+        union {
+            Short4 part[2];
+            Frag<T> all;
+        } u;
+        u.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(uintptr_t)first);
+        u.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(uintptr_t)second);
+        return u.all;
+    }
+
     // Element d0 + lane % 32 of the rows of block kb (d0 a multiple of 32).
     static __device__ inline Frag<T> across(uint32_t base, int kb, int d0) {
         if constexpr (sizeof(T) == 2) {
-            // a transposing read: 16 lanes bring 4 rows of 16 elements, 8 bytes each, and
-            // every lane gets the 4 values of its column
-            typedef short Short4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) Short4 Lds;
             const uint32_t p = chunk_on(base, d0 / 8) + kb * 16 * kRowBytes;
-            union {
-                Short4 part[2];
-                Frag<T> all;
-            } u;
-            u.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(uintptr_t)p);
-            u.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (Lds*)(uintptr_t)((p ^ swizzle(8) << 4) + 8 * kRowBytes));
-            return u.all;
+            return across_at(p, (p ^ swizzle(8) << 4) + 8 * kRowBytes);
         } else {
             typedef __attribute__((address_space(3))) const float Lds;
             const uint32_t p = chunk_on(base, d0 / 4) + (kb >> 1) * 16 * kRowBytes;
@@ -188,6 +191,48 @@ struct Tile {
             }
             return f;
         }
+    }
+};
+
+// A lane's addresses for reads of tiles that lie `offset` bytes behind a place in LDS, an
+// immediate of the instructions where it is constant.
+template <class E, int D>
+struct Reader {
+    using One = Tile<E, D>;
+    uint32_t a[D / kBlock<E>], c[D / 32][2];
+    __device__ inline Reader(const char* lds, int lane) {
+        const uint32_t x = One::base(lds, One::from_along(lane));
+        const uint32_t y = One::base(lds, One::from_across(lane));
+#pragma unroll
+        for (int kb = 0; kb < D / kBlock<E>; ++kb) a[kb] = One::chunk_on(x, 2 * kb);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            c[dt][0] = One::chunk_on(y, 4 * dt);
+            c[dt][1] = (c[dt][0] ^ One::swizzle(8) << 4) + 8 * One::kRowBytes;
+        }
+    }
+    // Blocks as Tile's, of rows from the offset on.
+    __device__ inline Frag<E> along(int offset, int kb) const {
+        typedef __attribute__((address_space(3))) const Frag<E> Lds;
+        return *(Lds*)(uintptr_t)(a[kb] + offset);
+    }
+    __device__ inline Frag<E> across(int offset, int kb, int dt) const {
+        return One::across_at(c[dt][0] + offset + kb * 16 * One::kRowBytes,
+                              c[dt][1] + offset + kb * 16 * One::kRowBytes);
+    }
+};
+// (FP32 forms them when it reads: eight for each 32 elements across are too many)
+template <int D>
+struct Reader<float, D> {
+    using One = Tile<float, D>;
+    uint32_t x, y;
+    __device__ inline Reader(const char* lds, int lane)
+        : x(One::base(lds, One::from_along(lane))), y(One::base(lds, One::from_across(lane))) {}
+    __device__ inline Frag<float> along(int offset, int kb) const {
+        return One::along(x + offset, 0, kb);
+    }
+    __device__ inline Frag<float> across(int offset, int kb, int dt) const {
+        return One::across(y + offset, kb, 32 * dt);
     }
 };
 
@@ -207,6 +252,20 @@ struct Planes {
         Operand<T> f;
 #pragma unroll
         for (int i = 0; i < kPlanes<T>; ++i) f.p[i] = One::across(base + i * kPlaneBytes, kb, d0);
+        return f;
+    }
+    // From a tile `offset` bytes behind the reader's place.
+    typedef Reader<Elem<T>, D> Read;
+    static __device__ inline Operand<T> along(const Read& r, int offset, int kb) {
+        Operand<T> f;
+#pragma unroll
+        for (int i = 0; i < kPlanes<T>; ++i) f.p[i] = r.along(offset + i * kPlaneBytes, kb);
+        return f;
+    }
+    static __device__ inline Operand<T> across(const Read& r, int offset, int kb, int dt) {
+        Operand<T> f;
+#pragma unroll
+        for (int i = 0; i < kPlanes<T>; ++i) f.p[i] = r.across(offset + i * kPlaneBytes, kb, dt);
         return f;
     }
 };
