@@ -17,13 +17,11 @@
 
 namespace sgemm_emu {
 
-// kRowGroups waves with 32 rows each share the block's tiles of kKeys keys; or
-// (kRowGroups == 1) kKeyGroups waves with the same 32 rows take every kKeyGroups-th tile for
-// themselves, keys straight from memory as operands and values through a part of LDS of their
-// own, and are joined at the end.
+// A block's waves are kKeyGroups groups that take every kKeyGroups-th tile of kKeys keys and
+// are joined at the end, of kRowGroups waves with 32 rows each.  These share their group's
+// tiles; where they are one (kRowGroups == 1), its keys go straight from memory to operands.
 template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
 struct Attend {
-    static_assert(kRowGroups == 1 || kKeyGroups == 1, "");
     static constexpr bool kShared = kRowGroups > 1;
     static_assert(kShared || kKeys == 32, "");
     static constexpr int kThreads = 64 * kRowGroups * kKeyGroups;
@@ -36,10 +34,14 @@ struct Attend {
     static constexpr int kPlace = (kShared ? 2 : 1) * kTileBytes;  // of a tile's keys and values
     static constexpr int kTiles = kKeyGroups * 2 * kPlace;
     static constexpr int kJoinRow = D + 4;  // floats
-    static constexpr int kJoin = kShared ? 0 : kKeyGroups * 32 * (kJoinRow + 2) * 4;
+    // (shared: [row group][4 registers][lane] of the second group's sums, and l and z)
+    static constexpr int kJoin = kShared ? (kKeyGroups - 1) * kRowGroups * (D / 8 * 1024 + 512)
+                                         : kKeyGroups * 32 * (kJoinRow + 2) * 4;
+    static_assert(!kShared || kKeyGroups <= 2, "");
     static constexpr int kFactors = kSplit ? 2 * kKeys : 0;  // of a tile's keys and values
-    static constexpr int kLds = (kTiles > kJoin ? kTiles : kJoin) + 2 * kFactors * 4 + 16;
-    static constexpr int kTileThreads = kShared ? kThreads : 64;
+    static constexpr int kLds =
+        (kTiles > kJoin ? kTiles : kJoin) + 2 * kKeyGroups * kFactors * 4 + 16;
+    static constexpr int kTileThreads = 64 * kRowGroups;
     // FP16 weights keep 11 bits down to 2^-14: 2^-21 of a row's largest
     static constexpr float kBias = __is_same(E, f16_t) ? 7.0f : 0.0f;
     static constexpr float kSlack = 8.0f;
@@ -60,9 +62,9 @@ struct Attend {
         const int width = kSplit ? kWidth<D> : size;
         const int lane = threadIdx.x & 63, half = lane >> 5;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int group = kShared ? 0 : wave;
-        const int wave_row = row0 + (kShared ? 32 * wave : 0);
-        const int tile_thread = kShared ? (int)threadIdx.x : lane;
+        const int group = wave / kRowGroups, row_group = wave % kRowGroups;
+        const int wave_row = row0 + 32 * row_group;
+        const int tile_thread = (int)threadIdx.x % kTileThreads;
         char* tiles = lds + group * 2 * kPlace;
         int* bad = reinterpret_cast<int*>(lds + kLds - 16);
 
@@ -89,7 +91,8 @@ struct Attend {
         f32x16 O[D / 32];
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) O[dt] = f32x16{};
-        float l = 0.0f, z = -1e30f, unit = 0x1p-126f;  // O is in units of the largest factor so far
+        float l = 0.0f, z = -1e30f;
+        float unit = kSplit ? 0x1p-126f : 1.0f;  // of O: the largest factor of values so far
         bool found = false;
         if (kVecTile && width < kWidth<D>) {
             clear_lds(lds, kTiles, threadIdx.x, kThreads);
@@ -99,12 +102,13 @@ struct Attend {
         using Load = Flow<E, D, kKeys, kTileThreads, kVecTile>;
         Load fk, fv;
         Operand<T> K[kShared ? 1 : kBlocks];
-        float* const of_tiles = reinterpret_cast<float*>(lds + kLds - 16) - 2 * kFactors;
+        float* const of_tiles = reinterpret_cast<float*>(lds + kLds - 16) -
+                                2 * (group + 1) * kFactors;
         float st_factor = 0.0f;
-        const int step = kShared ? 1 : kKeyGroups;
+        constexpr int step = kKeyGroups;
         const uint32_t k_row = (uint32_t)k_token * sizeof(E), v_row = (uint32_t)v_token * sizeof(E);
         const auto place = [&](int t) {
-            return tiles + ((kShared ? t : t / kKeyGroups) & 1) * kPlace;
+            return tiles + (t / kKeyGroups & 1) * kPlace;
         };
         if (kShared) fk.rows([&](int r) { return r * k_row; }, tile_thread);
         fv.rows([&](int r) { return r * v_row; }, tile_thread);
@@ -151,20 +155,28 @@ struct Attend {
             constexpr int at = decltype(odd)::value * kPlace, v_at = at + kPlace - kTileBytes;
             char* kt = tiles + at;
             char* vt = tiles + v_at;
-            if (kShared) fk.finish(kt, tile_thread);
-            fv.finish(vt, tile_thread);
-            // values that are not finite reach only rows that see them: where some row
-            // does not, they are left out here and added at the end
-            if (t >= cleared)
-#pragma unroll
-                for (int i = 0; i < kPlanes<T>; ++i)
-                    found |= Load::clear_not_finite(vt + i * KV::kPlaneBytes, tile_thread);
+            // (a group of several waves may have one tile less than the others, for whose sake
+            // it comes to the barrier)
+            const bool here = kKeyGroups == 1 || !kShared || t < count;
             float* const of_tile = of_tiles + decltype(odd)::value * kFactors;
-            if (kSplit && tile_thread < kFactors) of_tile[tile_thread] = st_factor;
+            if (here) {
+                if (kShared) fk.finish(kt, tile_thread);
+                fv.finish(vt, tile_thread);
+                // values that are not finite reach only rows that see them: where some row
+                // does not, they are left out here and added at the end
+                if (t >= cleared)
+#pragma unroll
+                    for (int i = 0; i < kPlanes<T>; ++i)
+                        found |= Load::clear_not_finite(
+                            vt + i * KV::kPlaneBytes, tile_thread,
+                            [&](int, int r) { return first + t * kKeys + r < end; });
+                if (kSplit && tile_thread < kFactors) of_tile[tile_thread] = st_factor;
+            }
             f32x16 S[kKeys / 32];
             if constexpr (kShared) {
                 lds_barrier();
                 if (t + step < count) load(t + step);
+                if (!here) return;
             } else {
                 S[0] = f32x16{};
 #pragma unroll
@@ -256,15 +268,47 @@ struct Attend {
                 }
             }
         };
-        for (int t = group; t < count; t += 2 * step) {
+        // (waves that meet at barriers go on until the first group is through)
+        const int last = kShared ? count + group : count;
+        for (int t = group; t < last; t += 2 * step) {
             tile(t, Number<0>{});
-            if (t + step < count) tile(t + step, Number<1>{});
+            if (t + step < last) tile(t + step, Number<1>{});
         }
         l = sum_halves(l);
         if (found) *bad = 1;
         __syncthreads();
         const bool repair = *bad != 0;
 
+        if constexpr (kShared && kKeyGroups == 2) {
+            typedef Pack<float, 4>::type Four;
+            Four* const sums = reinterpret_cast<Four*>(lds) + row_group * (D / 8 * 64 + 32) + lane;
+            float* const of_row = reinterpret_cast<float*>(sums + D / 8 * 64 - lane) + lane;
+            if (group == 1) {
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        sums[(4 * dt + i) * 64] = Four{O[dt][4 * i], O[dt][4 * i + 1], O[dt][4 * i + 2],
+                                                       O[dt][4 * i + 3]} * unit;
+                of_row[0] = l, of_row[64] = z;
+            }
+            __syncthreads();
+            if (group == 1) return;
+            const float other_l = of_row[0], other_z = of_row[64], top = fmaxf(z, other_z);
+            const float f = __builtin_amdgcn_exp2f(z - top), g = __builtin_amdgcn_exp2f(other_z - top);
+            l = l * f + other_l * g;
+            z = top;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const Four x = sums[(4 * dt + i) * 64];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        O[dt][4 * i + j] = O[dt][4 * i + j] * (f * unit) + x[j] * g;
+                }
+            unit = 1.0f;
+        }
         if constexpr (kShared) {
             if (row < rows) {
                 if (repair)

@@ -101,9 +101,14 @@ constexpr int kRowGroups = 4;
 int parts_of(const attention_emu_forward_t& a) {
     const int64_t blocks = blocks_of(a, 32 * kRowGroups), most = (a.keys + 255) / 256;
     if (blocks == 0 || most <= 1 || a.cu_seqlens != nullptr) return 1;
-    const int64_t parts = std::max<int64_t>(1, std::min(most, 512 / blocks));
+    const int64_t parts = std::max<int64_t>(1, std::min(most, 256 / blocks));
     const int64_t steps = (a.keys + 63) / 64;
     return steps - steps / parts > 12 ? (int)parts : 1;
+}
+
+// Whether two groups of waves share a block's keys.
+bool paired(const attention_emu_forward_t& a, int64_t blocks) {
+    return blocks <= 256 && a.keys > 128;
 }
 
 // Tokens and keys in all.
@@ -152,10 +157,14 @@ hipError_t launch_attention_forward(const attention_emu_forward_t& a, hipStream_
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
         constexpr int kKeys = kPlanes<T> == 1 || D <= 64 ? 64 : 32;
-        if (hipError_t e = launch_blocks(attention_forward_kernel<T, D, kRowGroups, 1, kKeys, kVec>,
-                                         blocks_of(a, 32 * kRowGroups) * parts, 64 * kRowGroups,
-                                         stream, args))
-            return e;
+        const int64_t blocks = blocks_of(a, 32 * kRowGroups) * parts;
+        const hipError_t e =
+            paired(a, blocks)
+                ? launch_blocks(attention_forward_kernel<T, D, kRowGroups, 2, kKeys, kVec>, blocks,
+                                64 * 2 * kRowGroups, stream, args)
+                : launch_blocks(attention_forward_kernel<T, D, kRowGroups, 1, kKeys, kVec>, blocks,
+                                64 * kRowGroups, stream, args);
+        if (e != hipSuccess) return e;
         if (parts == 1) return hipSuccess;
         return launch_join<Out<T>, D, kVec>(
             JoinArgs{args.parts, a.o, a.lse, parts, a.tokens, a.q_heads, a.size, nullptr, 0}, stream);

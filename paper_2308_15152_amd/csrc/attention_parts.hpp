@@ -77,31 +77,60 @@ struct JoinArgs {
     int n_slots;
 };
 
+// A row's elements are 16 or 32 lanes of four, in `groups` (a power of two up to 8) that take
+// every groups-th part and are joined in LDS: few rows of many parts would otherwise wait for
+// one load after another (256 rows of 32 parts: 20 us with one group, 5 with eight).
 template <class T, int D, bool kVec>
-__global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(JoinArgs a, int first_block) {
+__global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(JoinArgs a, int groups,
+                                                                      int first_block) {
+    typedef Pack<float, 4>::type Four;
     constexpr int kEach = kPartStride<D> / 4;
-    const int64_t row = (int64_t)(first_block + (int)blockIdx.x) * (kJoinThreads / kEach) +
-                        threadIdx.x / kEach;
-    const int d = (int)threadIdx.x % kEach * 4;
-    if (row >= a.parts.rows || d >= a.size) return;
-    const int64_t token = row / a.q_heads;
+    __shared__ Four xs[kJoinThreads];
+    __shared__ float ls[kJoinThreads], zs[kJoinThreads];
+    const int thread = threadIdx.x, rows = kJoinThreads / kEach / groups;
+    const int in_row = thread % kEach, group = thread / kEach % groups;
+    const int64_t row = (int64_t)(first_block + (int)blockIdx.x) * rows + thread / kEach / groups;
+    const int d = in_row * 4;
+    const bool here = row < a.parts.rows && d < a.size;
+    const int64_t token = here ? row / a.q_heads : 0;
     const int h = (int)(row - token * a.q_heads), n = (int)(token / a.tokens);
     float z = -1e30f, l = 0.0f;
-    for (int p = 0; p < a.count; ++p) z = fmaxf(z, a.parts.logs[p * a.parts.rows + row]);
-    Pack<float, 4>::type x{};
+    Four x{};
     const int slot = a.slots == nullptr ? 0 : a.slots[n];
-    if (a.slots == nullptr || (slot >= 0 && slot < a.n_slots)) {
-        for (int p = 0; p < a.count; ++p) {
+    if (here && (a.slots == nullptr || (slot >= 0 && slot < a.n_slots))) {
+#pragma unroll 4
+        for (int p = group; p < a.count; p += groups) {
             const float log = a.parts.logs[p * a.parts.rows + row];
-            if (log == -__builtin_inff()) continue;
-            const float f = __builtin_amdgcn_exp2f(log - z);
-            l += f;
-            const auto y = *reinterpret_cast<const Pack<float, 4>::type*>(
+            Four y = *reinterpret_cast<const Four*>(
                 a.parts.o + (p * a.parts.rows + row) * kPartStride<D> + d);
+            if (log == -__builtin_inff()) y = Four{};  // (not written)
+            const float to = fmaxf(z, log);
+            const float f = __builtin_amdgcn_exp2f(z - to), g = __builtin_amdgcn_exp2f(log - to);
+            l = l * f + g;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] += f * y[j];
+            for (int j = 0; j < 4; ++j) x[j] = x[j] * f + y[j] * g;
+            z = to;
         }
     }
+    if (groups > 1) {
+        xs[thread] = x, ls[thread] = l, zs[thread] = z;
+        __syncthreads();
+        if (group > 0) return;
+        const float mine = z;
+        for (int g = 1; g < groups; ++g) z = fmaxf(z, zs[thread + g * kEach]);
+        const float f = __builtin_amdgcn_exp2f(mine - z);
+        l *= f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] *= f;
+        for (int g = 1; g < groups; ++g) {
+            const float by = __builtin_amdgcn_exp2f(zs[thread + g * kEach] - z);
+            const Four y = xs[thread + g * kEach];
+            l += by * ls[thread + g * kEach];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] += by * y[j];
+        }
+    }
+    if (!here) return;
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
     const int64_t t = token - (int64_t)n * a.tokens;
     T* o = static_cast<T*>(a.o.p) + n * a.o.batch + t * a.o.token + h * a.o.head;
@@ -113,9 +142,11 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(JoinArgs a
 
 template <class T, int D, bool kVec>
 hipError_t launch_join(const JoinArgs& a, hipStream_t stream) {
-    constexpr int kRows = kJoinThreads / (kPartStride<D> / 4);
-    return launch_blocks(attention_join_kernel<T, D, kVec>, (a.parts.rows + kRows - 1) / kRows,
-                         kJoinThreads, stream, a);
+    int groups = 1;
+    while (groups < 8 && groups * 2 <= a.count) groups *= 2;
+    const int rows = kJoinThreads / (kPartStride<D> / 4) / groups;
+    return launch_blocks(attention_join_kernel<T, D, kVec>, (a.parts.rows + rows - 1) / rows,
+                         kJoinThreads, stream, a, groups);
 }
 
 }  // namespace sgemm_emu

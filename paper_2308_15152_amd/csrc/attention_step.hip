@@ -18,6 +18,7 @@ constexpr int kPrefixRows = 128;
 struct StepArgs {
     attention_emu_step_t a;
     int prefix_parts, prefix_tiles, prefix_keys;  // parts, row tiles, keys of a part
+    bool prefix_few;  // rows: 32 to a tile, whose waves share out the keys
     int own_parts;
     Parts parts;
 };
@@ -50,13 +51,17 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         const int part = rest % s.prefix_parts, tile = rest / s.prefix_parts;
         const int first = part * s.prefix_keys, end = min(first + s.prefix_keys, a.prefix);
         const auto out = [&](int r) { return out_of(part, r / group, head * group + r % group); };
-        Prefix::run(
-            lds, a.batch * a.tokens * group, tile * kPrefixRows,
-            [&](int r) { return q_row(r / group, head * group + r % group); },
-            [&](int) { return a.prefix; },
-            static_cast<const T*>(a.prefix_k.p) + head * a.prefix_k.head, a.prefix_k.token,
-            static_cast<const T*>(a.prefix_v.p) + head * a.prefix_v.head, a.prefix_v.token, first,
-            end, a.size, c, a.scale < 0.0f, out, none);
+        const auto row = [&](int r) { return q_row(r / group, head * group + r % group); };
+        const auto all = [&](int) { return a.prefix; };
+        const T* k = static_cast<const T*>(a.prefix_k.p) + head * a.prefix_k.head;
+        const T* v = static_cast<const T*>(a.prefix_v.p) + head * a.prefix_v.head;
+        const int rows = a.batch * a.tokens * group;
+        if (s.prefix_few)
+            Own::run(lds, rows, tile * 32, row, all, k, a.prefix_k.token, v, a.prefix_v.token, first,
+                     end, a.size, c, a.scale < 0.0f, out, none);
+        else
+            Prefix::run(lds, rows, tile * kPrefixRows, row, all, k, a.prefix_k.token, v,
+                        a.prefix_v.token, first, end, a.size, c, a.scale < 0.0f, out, none);
         return;
     }
     block -= prefix_blocks;
@@ -83,25 +88,29 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         a.size, c, a.scale < 0.0f, out, none);
 }
 
-// How the keys are cut.
+// How the keys are cut: into parts of at least 256 keys of the prefix, 512 of a cache, that
+// fill the device.  The prefix's blocks, one for each CU, come first, and those of the caches,
+// which are bound by memory, run beside them.
 StepArgs cut(const attention_emu_step_t& a) {
     StepArgs s{};
     s.a = a;
     const int64_t group = a.q_heads / a.k_heads;
     s.parts.rows = (int64_t)a.batch * a.tokens * a.q_heads;
     const int64_t rows = (int64_t)a.batch * a.tokens * group;
-    s.prefix_tiles = (int)((rows + kPrefixRows - 1) / kPrefixRows);
-    constexpr int64_t kWanted = 512;  // blocks: two for each CU
+    s.prefix_few = rows <= 64;
+    const int64_t tile = s.prefix_few ? 32 : kPrefixRows;
+    s.prefix_tiles = (int)((rows + tile - 1) / tile);
     if (a.prefix > 0) {
         const int64_t blocks = (int64_t)s.prefix_tiles * a.k_heads;
         const int64_t most = (a.prefix + 255) / 256;
-        const int64_t parts = std::max<int64_t>(1, std::min(most, kWanted / blocks));
+        const int64_t parts =
+            std::max<int64_t>(1, std::min(most, 256 / std::max<int64_t>(1, blocks)));
         s.prefix_keys = (int)(((a.prefix + parts - 1) / parts + 63) / 64 * 64);
         s.prefix_parts = (a.prefix + s.prefix_keys - 1) / s.prefix_keys;
     }
     const int64_t blocks = (int64_t)a.batch * a.k_heads * ((a.tokens * group + 31) / 32);
-    const int64_t most = (a.capacity + 255) / 256;
-    s.own_parts = (int)std::max<int64_t>(1, std::min(most, kWanted / std::max<int64_t>(1, blocks)));
+    const int64_t most = (a.capacity + 511) / 512;
+    s.own_parts = (int)std::max<int64_t>(1, std::min(most, 512 / std::max<int64_t>(1, blocks)));
     return s;
 }
 

@@ -365,8 +365,9 @@ struct Flow {
         }
     }
     // Puts zeros in the place of values that are not finite in the thread's part of a tile;
-    // whether there were any.
-    static __device__ inline bool clear_not_finite(char* tile, int thread) {
+    // whether there were any in rows that are there.
+    template <class There>
+    static __device__ inline bool clear_not_finite(char* tile, int thread, There there) {
         bool any = false;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -380,7 +381,7 @@ struct Flow {
                 if (bad) x[j] = from_f32<T>(0.0f);
             }
             if (here) *at = x;
-            any |= here;
+            any |= here && there(i, row(thread) + i * kRowsApart);
         }
         return any;
     }
