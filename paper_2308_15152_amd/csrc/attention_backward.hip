@@ -12,6 +12,8 @@
 // either: p is taken times 2^14, and ds times a power of two for each column of the
 // accumulator (a query row, or a key), which is lowered, with what is summed so far, when a
 // larger value comes.
+#include <algorithm>
+
 #include "attention_parts.hpp"
 #include "attention_split.h"
 
@@ -28,6 +30,11 @@ struct BackwardArgs {
     // the operands, split if they are FP32
     sgemm_emu_view_t q, k, v, d_o;
     const float *q_factors, *k_factors, *v_factors, *do_factors;
+    // parts that the query rows of a block of keys are cut into, and where they leave their sums:
+    // [part][dv, dk][key in all][key head][kPartStride], or null: one part
+    int count;
+    float* parts;
+    int64_t key_rows;
 };
 
 __device__ inline Pack<float, 4>::type four_floats(const float* p) {
@@ -81,18 +88,26 @@ __device__ inline f32x16 times(const f32x16& x, float f) {
 constexpr int kDqWaves = 4;
 constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
+// Below so many blocks (two for each CU) two groups of waves share a block's keys: 384 blocks of
+// 2048 keys take 192 us for 203 in all (16 sequences of up to 2500 tokens 112 for 127), 512 take 3 more.
+constexpr int kDqPaired = 512;
 
 // (FP32 operands of more than 96 elements take the registers of two waves)
-template <class T, int D, bool kVec>
-__global__ __launch_bounds__(64 * kDqWaves, kPlanes<T> == 2 && D > 96 ? 1 : 2) void
+// kGroups groups of waves take every kGroups-th tile of keys and are joined at the end.
+template <class T, int D, bool kVec, int kGroups>
+__global__ __launch_bounds__(64 * kDqWaves * kGroups,
+                             kPlanes<T> == 2 && D > 96 ? kGroups : 2) void
 attention_dq_kernel(BackwardArgs args, int first_block) {
     typedef Elem<T> E;
     using KV = Planes<T, D, kDqKeys>;
     constexpr bool kSplit = kPlanes<T> == 2;
     constexpr int kThreads = 64 * kDqWaves, kBlocks = D / kBlock<E>, kParts = 32 / kBlock<E>;
     constexpr int kTileBytes = KV::kBytes;
-    __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];
-    __shared__ float of_tiles[kSplit ? 4 * kDqKeys : 1];  // factors of keys and values
+    constexpr int kJoin = (kGroups - 1) * kDqWaves * D / 8 * 1024;
+    constexpr int kTiles = kGroups * 4 * kTileBytes;
+    __shared__ __attribute__((aligned(16))) char lds_all[kTiles > kJoin ? kTiles : kJoin];
+    // factors of keys and values
+    __shared__ float of_all[kSplit ? kGroups * 4 * kDqKeys : 1];
     const attention_emu_backward_t& a = args.a;
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
@@ -118,7 +133,11 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
     const E* v = row_of<E>(args.v, packed, n, sk, head);
 
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group_of = all_waves / kDqWaves, wave = all_waves % kDqWaves;
+    const int thread = (int)threadIdx.x % kThreads;  // in the group
+    char* const lds = lds_all + group_of * 4 * kTileBytes;
+    float* const of_tiles = of_all + (kSplit ? group_of * 4 * kDqKeys : 0);
     const int row0 = tile * kDqRows, wave_row = row0 + 32 * wave;
     const int row = wave_row + (lane & 31);
     const int r = min(row, last_row), token = r / group, h = head * group + r % group;
@@ -146,7 +165,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         }
         delta = sum_halves(delta);
     }
-    if (valid && half == 0) args.delta[in_all * a.q_heads + h] = delta;
+    if (valid && half == 0 && group_of == 0) args.delta[in_all * a.q_heads + h] = delta;
     // (rows that see nothing have lse -infinity)
     float z = __builtin_inff();
     if (valid) {
@@ -172,7 +191,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
     for (int dt = 0; dt < D / 32; ++dt) dQ[dt] = f32x16{};
     Fit fit;
     // (what is not loaded multiplies zeros and has to be finite)
-    clear_lds(lds, 4 * kTileBytes, threadIdx.x, kThreads);
+    clear_lds(lds, 4 * kTileBytes, thread, kThreads);
     lds_barrier();
     Flow<E, D, kDqKeys, kThreads, kVec || kSplit> fk, fv;
     const int width = kSplit ? kWidth<D> : a.size;
@@ -180,40 +199,45 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
     const uint32_t v_row = (uint32_t)args.v.token * sizeof(E);
     const int64_t first_key = (packed ? sk.first : (int64_t)n * a.keys) * a.k_heads + head;
     float st_factor = 0.0f;
-    fk.rows([&](int r) { return r * k_row; }, threadIdx.x);
-    fv.rows([&](int r) { return r * v_row; }, threadIdx.x);
+    fk.rows([&](int r) { return r * k_row; }, thread);
+    fv.rows([&](int r) { return r * v_row; }, thread);
     const auto load = [&](int t) {
         const int key = t * kDqKeys, most = sk.count - 1 - key;
-        char* to = lds + (t & 1) * 2 * kTileBytes;
+        char* to = lds + (t / kGroups & 1) * 2 * kTileBytes;
         const auto there = [&](int, int r) { return r <= most; };
         if constexpr (kSplit) {
-            const int i = threadIdx.x % kDqKeys;
-            if (threadIdx.x < 2 * kDqKeys)
+            const int i = thread % kDqKeys;
+            if (thread < 2 * kDqKeys)
                 st_factor = i > most ? 0.0f
-                                     : (threadIdx.x < kDqKeys ? args.k_factors : args.v_factors)
+                                     : (thread < kDqKeys ? args.k_factors : args.v_factors)
                                            [first_key + (int64_t)(key + i) * a.k_heads];
         }
 #pragma unroll
         for (int i = 0; i < kPlanes<T>; ++i) {
             fk.start(to + i * KV::kPlaneBytes, k + key * args.k.token + i * kWidth<D>, width,
-                     threadIdx.x, there);
+                     thread, there);
             fv.start(to + kTileBytes + i * KV::kPlaneBytes, v + key * args.v.token + i * kWidth<D>,
-                     width, threadIdx.x, there);
+                     width, thread, there);
         }
     };
     const typename KV::Read read(lds, lane);
-    if (count > 0) load(0);
+    if (group_of < count) load(group_of);
     // one tile, in the first or the second place
     const auto step = [&](int t, auto odd) __attribute__((always_inline)) {
         constexpr int k_at = decltype(odd)::value * 2 * kTileBytes, v_at = k_at + kTileBytes;
         char* kt = lds + k_at;
         char* vt = lds + v_at;
-        fk.finish(kt, threadIdx.x);
-        fv.finish(vt, threadIdx.x);
+        // (the last group may have one tile less, and comes to the barrier all the same)
+        const bool here = kGroups == 1 || t < count;
         float* const of_tile = of_tiles + decltype(odd)::value * 2 * kDqKeys;
-        if (kSplit && threadIdx.x < 2 * kDqKeys) of_tile[threadIdx.x] = st_factor;
+        if (here) {
+            fk.finish(kt, thread);
+            fv.finish(vt, thread);
+            if (kSplit && thread < 2 * kDqKeys) of_tile[thread] = st_factor;
+        }
         lds_barrier();
-        if (t + 1 < count) load(t + 1);
+        if (t + kGroups < count) load(t + kGroups);
+        if (!here) return;
         const int key0 = t * kDqKeys;
         if (key0 >= lim_max) return;
         f32x16 S{}, dP;
@@ -261,19 +285,43 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
                 dQ[dt] = mma(KV::across(read, k_at, kb, dt), x, dQ[dt]);
         }
     };
-    for (int t = 0; t < count; t += 2) {
+    for (int t = group_of; t < count + group_of; t += 2 * kGroups) {
         step(t, Number<0>{});
-        if (t + 1 < count) step(t + 1, Number<1>{});
+        if (t + kGroups < count + group_of) step(t + kGroups, Number<1>{});
+    }
+    const float f = kNarrow<T> ? a.scale / fit.f : a.scale;
+    if constexpr (kGroups == 2) {
+        typedef Pack<float, 4>::type Four;
+        Four* const sums = reinterpret_cast<Four*>(lds_all) + wave * (D / 8 * 64) + lane;
+        __syncthreads();
+        if (group_of == 1) {
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sums[(4 * dt + i) * 64] = Four{dQ[dt][4 * i], dQ[dt][4 * i + 1],
+                                                   dQ[dt][4 * i + 2], dQ[dt][4 * i + 3]} * f;
+        }
+        __syncthreads();
+        if (group_of == 1 || !valid) return;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const Four x = sums[(4 * dt + i) * 64];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dQ[dt][4 * i + j] = dQ[dt][4 * i + j] * f + x[j];
+            }
     }
     if (!valid) return;
-    const float f = kNarrow<T> ? a.scale / fit.f : a.scale;
+    const float by = kGroups == 2 ? 1.0f : f;
     Out<T>* dq = row_of<Out<T>>(a.dq, packed, n, sq, h) + token * a.dq.token;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-            store_four<Out<T>, kVec>(dq, 32 * dt + acc_row(i, half), a.size, dQ[dt][i] * f,
-                                dQ[dt][i + 1] * f, dQ[dt][i + 2] * f, dQ[dt][i + 3] * f);
+            store_four<Out<T>, kVec>(dq, 32 * dt + acc_row(i, half), a.size, dQ[dt][i] * by,
+                                dQ[dt][i + 1] * by, dQ[dt][i + 2] * by, dQ[dt][i + 3] * by);
 }
 
 // A block's waves: kKeyGroups times 32 keys, each shared by kRowGroups waves that take
@@ -285,7 +333,9 @@ struct DkvShape {
     static constexpr int kKeyGroups = 2;
     static constexpr int kRowGroups = kWide ? 2 : 4;
     static constexpr int kWaves = kKeyGroups * kRowGroups, kThreads = 64 * kWaves;
-    static constexpr int kKeys = 32 * kKeyGroups, kRows = 32 * kRowGroups;
+    // tiles of 32 rows that a wave takes between two barriers: two where they are small
+    static constexpr int kUnits = kPlanes<T> == 1 && D <= 64 ? 2 : 1;
+    static constexpr int kKeys = 32 * kKeyGroups, kRows = 32 * kRowGroups * kUnits;
     // How much of the keys' and values' operands is in registers; the rest, which
     // does not fit, is read from LDS for every tile
     static constexpr int kBlocks = D / kBlock<Elem<T>>;
@@ -331,7 +381,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     __shared__ Operand<T> operands[Shape::kLdsBlocks > 0 ? Shape::kKeyGroups * Shape::kLdsBlocks * 64 : 1];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
-    const int block = first_block + (int)blockIdx.x;
+    const int part = (first_block + (int)blockIdx.x) % args.count;
+    const int block = (first_block + (int)blockIdx.x) / args.count;
     int n, head, tile;
     if (packed) {
         head = block % a.k_heads;
@@ -385,11 +436,20 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     const int shift = sk.count - tokens + 1;  // token i sees keys below i + shift
     const bool far = (int64_t)(group - 1) * max(args.q.head, args.d_o.head) > (1 << 28);
     const RowTiles tiles(group, kRows, far);
-    const int count = (tokens + tiles.tokens - 1) / tiles.tokens * tiles.parts;
+    const int all = (tokens + tiles.tokens - 1) / tiles.tokens * tiles.parts;
     const int from = a.causal ? min(max(block_key - shift + 1, 0), tokens) : 0;
-    const int t0 = from / tiles.tokens * tiles.parts;
-    // tokens of the wave's rows, in a tile
-    const int wave_first = 32 * row_group / tiles.heads, wave_last = (32 * row_group + 31) / tiles.heads;
+    // the tiles of rows that see some of the keys, and the block's part of them
+    const int t_first = from / tiles.tokens * tiles.parts;
+    const int each = (all - t_first + args.count - 1) / args.count;
+    const int t0 = min(t_first + part * each, all), count = min(t0 + each, all);
+
+    // first and last token of the wave's rows in a tile
+    int unit_first[Shape::kUnits], unit_last[Shape::kUnits];
+#pragma unroll
+    for (int unit = 0; unit < Shape::kUnits; ++unit) {
+        unit_first[unit] = 32 * (row_group + unit * kRowGroups) / tiles.heads;
+        unit_last[unit] = (32 * (row_group + unit * kRowGroups) + 31) / tiles.heads;
+    }
 
     f32x16 dK[D / 32], dV[D / 32];
 #pragma unroll
@@ -481,18 +541,20 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         lds_barrier();
         if (t > t0) load(t - 1);
         const int token0 = t / tiles.parts * tiles.tokens;
-        if (a.causal && token0 + wave_last + shift <= wave_key) continue;
-
         // (addresses are formed for every tile: kept, they would take registers that the
         // sums need)
         asm volatile("" : "+v"(from_along), "+v"(from_across));
-        const int row0 = 32 * row_group;
-        const uint32_t q_along = QD::One::base(qt + row0 * kRowBytes, from_along);
-        const uint32_t o_along = QD::One::base(ot + row0 * kRowBytes, from_along);
-        const uint32_t q_across = QD::One::base(qt + row0 * kRowBytes, from_across);
-        const uint32_t o_across = QD::One::base(ot + row0 * kRowBytes, from_across);
-        const auto per_row = [&](const float* x, int i) {  // rows of registers i to i + 3
-            return four_floats(x + row0 + 8 * (i / 4) + 4 * half);
+        const auto rows_of_unit = [&](int unit) __attribute__((always_inline)) {
+            const int row0 = 32 * (row_group + unit * kRowGroups);
+            // tokens of the wave's rows
+            const int wave_first = token0 + unit_first[unit], wave_last = token0 + unit_last[unit];
+            if (a.causal && wave_last + shift <= wave_key) return;
+            const uint32_t q_along = QD::One::base(qt + row0 * kRowBytes, from_along);
+            const uint32_t o_along = QD::One::base(ot + row0 * kRowBytes, from_along);
+            const uint32_t q_across = QD::One::base(qt + row0 * kRowBytes, from_across);
+            const uint32_t o_across = QD::One::base(ot + row0 * kRowBytes, from_across);
+            const auto per_row = [&](const float* x, int i) {  // rows of registers i to i + 3
+                return four_floats(x + row0 + 8 * (i / 4) + 4 * half);
         };
         f32x16 P{}, dP;
 #pragma unroll
@@ -533,7 +595,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             for (int j = 0; j < 4; ++j)
                 P[i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(P[i + j], c, -x[j]));
         }
-        const bool masked = a.causal && token0 + wave_first + shift <= wave_key + 31;
+        const bool masked = a.causal && wave_first + shift <= wave_key + 31;
         if (masked) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -569,10 +631,14 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             for (int dt = 0; dt < D / 32; ++dt)
                 dK[dt] = mma(QD::across(q_across, kb, 32 * dt), x, dK[dt]);
         }
+        };
+        rows_of_unit(0);
+        if (Shape::kUnits == 2) rows_of_unit(1);
     }
 
     // the sums of the waves with the same keys, in the order of their rows
-    const auto join = [&](f32x16(&sum)[D / 32], float f, Out<T>* to) __attribute__((always_inline)) {
+    const auto join = [&](f32x16(&sum)[D / 32], float f, Out<T>* to, float* to_part)
+        __attribute__((always_inline)) {
         typedef Pack<float, 4>::type Four;
         lds_barrier();
         Four* const mine = reinterpret_cast<Four*>(lds) +
@@ -598,42 +664,95 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
                     x += reinterpret_cast<const Four*>(lds)[((g - 1) * Shape::kKeyGroups + key_group) *
                                                                 (D / 8) * 64 +
                                                             (dt * 4 + i) * 64 + lane];
-                store_four<Out<T>, kVec>(to, 32 * dt + acc_row(4 * i, half), a.size, x[0], x[1], x[2], x[3]);
+                const int d = 32 * dt + acc_row(4 * i, half);
+                if (to_part != nullptr)
+                    store_four<float, true>(to_part, d, kPartStride<D>, x[0], x[1], x[2], x[3]);
+                else
+                    store_four<Out<T>, kVec>(to, d, a.size, x[0], x[1], x[2], x[3]);
             }
     };
-    join(dV, kSplit ? kBack / fit_v.f : kBack, row_of<Out<T>>(a.dv, packed, n, sk, head) + key_in * a.dv.token);
+    const int64_t key_row = ((packed ? sk.first : (int64_t)n * a.keys) + key_in) * a.k_heads + head;
+    float* const dv_part = args.parts ? args.parts + (part * 2 * args.key_rows + key_row) * kPartStride<D>
+                                      : nullptr;
+    float* const dk_part = args.parts ? dv_part + args.key_rows * kPartStride<D> : nullptr;
+    join(dV, kSplit ? kBack / fit_v.f : kBack,
+         row_of<Out<T>>(a.dv, packed, n, sk, head) + key_in * a.dv.token, dv_part);
     join(dK, kNarrow<T> ? a.scale * kBack / fit.f : a.scale,
-         row_of<Out<T>>(a.dk, packed, n, sk, head) + key_in * a.dk.token);
+         row_of<Out<T>>(a.dk, packed, n, sk, head) + key_in * a.dk.token, dk_part);
 }
 
+// dv and dk as the sums of their parts, in order.
+template <class T, int D, bool kVec>
+__global__ __launch_bounds__(256) void attention_sum_kernel(BackwardArgs args, int first_block) {
+    typedef Pack<float, 4>::type Four;
+    constexpr int kEach = kPartStride<D> / 4;
+    const attention_emu_backward_t& a = args.a;
+    const int64_t at = (int64_t)(first_block + (int)blockIdx.x) * (256 / kEach) + threadIdx.x / kEach;
+    const int d = threadIdx.x % kEach * 4;
+    if (at >= 2 * args.key_rows || d >= a.size) return;
+    Four x{};
+#pragma unroll 4
+    for (int p = 0; p < args.count; ++p)
+        x += *reinterpret_cast<const Four*>(args.parts + (p * 2 * args.key_rows + at) * kPartStride<D> +
+                                            d);
+    const sgemm_emu_view_t& to = at < args.key_rows ? a.dv : a.dk;
+    const int64_t row = at < args.key_rows ? at : at - args.key_rows;
+    const int64_t key = row / a.k_heads, n = key / a.keys;
+    T* out = static_cast<T*>(to.p) + n * to.batch + (key - n * a.keys) * to.token +
+             (row - key * a.k_heads) * to.head;
+    store_four<T, kVec>(out, d, a.size, x[0], x[1], x[2], x[3]);
+}
+
+int64_t batch_of(const attention_emu_backward_t& a) { return a.cu_seqlens != nullptr ? 1 : a.batch; }
+
 int64_t delta_bytes(const attention_emu_backward_t& a) {
-    const int64_t rows = a.cu_seqlens != nullptr ? a.tokens : (int64_t)a.batch * a.tokens;
-    return (rows * a.q_heads * 4 + 255) / 256 * 256;
+    return (batch_of(a) * a.tokens * a.q_heads * 4 + 255) / 256 * 256;
+}
+
+int64_t planes_bytes(const attention_emu_backward_t& a) {
+    if (a.dtype != SGEMM_EMU_F32) return 0;
+    return 2 * split_bytes(batch_of(a) * a.tokens, a.q_heads, a.size) +
+           2 * split_bytes(batch_of(a) * a.keys, a.k_heads, a.size);
+}
+
+// Parts of the query rows of a block of keys: where the blocks are fewer than the CUs, as many as
+// fill those, of at least 512 rows each.
+int parts_of(const attention_emu_backward_t& a) {
+    const int64_t blocks = most_parts(a.batch, a.keys, 64, a.cu_seqlens != nullptr) * a.k_heads;
+    if (blocks == 0 || a.cu_seqlens != nullptr) return 1;
+    const int64_t most = (int64_t)a.tokens * (a.q_heads / a.k_heads) / 512;
+    return (int)std::max<int64_t>(1, std::min(most, (256 + blocks / 2) / blocks));
+}
+
+int64_t sums_bytes(const attention_emu_backward_t& a, int parts) {
+    if (parts == 1) return 0;
+    return (parts * 2 * batch_of(a) * a.keys * a.k_heads * part_stride(a.size) * 4 + 255) / 256 * 256;
 }
 
 }  // namespace
 
 int64_t attention_backward_workspace(const attention_emu_backward_t& a) {
-    const int64_t batch = a.cu_seqlens != nullptr ? 1 : a.batch;
-    int64_t bytes = delta_bytes(a);
-    if (a.dtype == SGEMM_EMU_F32)
-        bytes += 2 * split_bytes(batch * a.tokens, a.q_heads, a.size) +
-                 2 * split_bytes(batch * a.keys, a.k_heads, a.size);
-    return bytes;
+    return delta_bytes(a) + planes_bytes(a) + sums_bytes(a, parts_of(a));
 }
 
 hipError_t launch_attention_backward(const attention_emu_backward_t& a, hipStream_t stream) {
-    BackwardArgs args{a, static_cast<float*>(a.workspace), a.q, a.k, a.v, a.d_o, nullptr, nullptr,
-                      nullptr, nullptr};
-    if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) args.a.cu_keys = a.cu_seqlens;
+    char* const ws = static_cast<char*>(a.workspace);
     const bool packed = a.cu_seqlens != nullptr;
+    BackwardArgs args{};
+    args.a = a;
+    if (packed && a.cu_keys == nullptr) args.a.cu_keys = a.cu_seqlens;
+    args.delta = reinterpret_cast<float*>(ws);
+    args.q = a.q, args.k = a.k, args.v = a.v, args.d_o = a.d_o;
+    args.count = parts_of(a);
+    args.key_rows = batch_of(a) * a.keys * a.k_heads;
+    if (args.count > 1) args.parts = reinterpret_cast<float*>(ws + delta_bytes(a) + planes_bytes(a));
     const int e = a.dtype == SGEMM_EMU_F32 ? 4 : 2;
     bool vec = a.size * e % 16 == 0;
     for (const sgemm_emu_view_t* x : {&a.o, &a.d_o, &a.dq, &a.dk, &a.dv})
         vec = vec && rows_aligned16(*x, e);
     if (a.dtype == SGEMM_EMU_F32) {
-        Splitter split(a.size, static_cast<char*>(a.workspace) + delta_bytes(a));
-        const int batch = packed ? 1 : a.batch;
+        Splitter split(a.size, ws + delta_bytes(a));
+        const int batch = (int)batch_of(a);
         const SplitTensor q = split.add(a.q, batch, a.tokens, a.q_heads);
         const SplitTensor k = split.add(a.k, batch, a.keys, a.k_heads);
         const SplitTensor v = split.add(a.v, batch, a.keys, a.k_heads);
@@ -646,18 +765,29 @@ hipError_t launch_attention_backward(const attention_emu_backward_t& a, hipStrea
         for (const sgemm_emu_view_t* x : {&a.q, &a.k, &a.v}) vec = vec && rows_aligned16(*x, e);
     }
     const int64_t group = a.q_heads / a.k_heads;
-    const int64_t q_parts = most_parts(a.batch, a.tokens * group, kDqRows, packed) * a.k_heads;
+    const int64_t q_blocks = most_parts(a.batch, a.tokens * group, kDqRows, packed) * a.k_heads;
     return by_form<split_t>(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
-        if (a.tokens > 0)
-            if (hipError_t e = launch_blocks(attention_dq_kernel<T, D, kVec>, q_parts, 64 * kDqWaves,
-                                             stream, args))
-                return e;
+        if (a.tokens > 0) {
+            const hipError_t e =
+                q_blocks < kDqPaired && (kPlanes<T> == 1 || D <= 96)
+                    ? launch_blocks(attention_dq_kernel<T, D, kVec, kPlanes<T> == 1 || D <= 96 ? 2 : 1>, q_blocks, 64 * kDqWaves * 2,
+                                    stream, args)
+                    : launch_blocks(attention_dq_kernel<T, D, kVec, 1>, q_blocks, 64 * kDqWaves, stream,
+                                    args);
+            if (e != hipSuccess) return e;
+        }
         using Shape = DkvShape<T, D>;
-        const int64_t k_parts = most_parts(a.batch, a.keys, Shape::kKeys, packed) * a.k_heads;
-        return launch_blocks(attention_dkv_kernel<T, D, kVec>, k_parts, Shape::kThreads, stream, args);
+        const int64_t blocks = most_parts(a.batch, a.keys, Shape::kKeys, packed) * a.k_heads * args.count;
+        if (hipError_t e = launch_blocks(attention_dkv_kernel<T, D, kVec>, blocks, Shape::kThreads,
+                                         stream, args))
+            return e;
+        if (args.count == 1) return hipSuccess;
+        constexpr int kRows = 256 / (kPartStride<D> / 4);
+        return launch_blocks(attention_sum_kernel<Out<T>, D, kVec>,
+                             (2 * args.key_rows + kRows - 1) / kRows, 256, stream, args);
     });
 }
 

@@ -29,7 +29,8 @@ struct ForwardFactors {
 };
 
 template <class T, int D, int kRowGroups, int kKeyGroups, int kKeys, bool kVec>
-__global__ __launch_bounds__(64 * kRowGroups * kKeyGroups, 2) void attention_forward_kernel(
+__global__ __launch_bounds__(64 * kRowGroups * kKeyGroups,
+                             sizeof(Elem<T>) == 4 && D > 64 ? 1 : 2) void attention_forward_kernel(
     ForwardArgs args, int first_block) {
     const attention_emu_forward_t& a = args.a;
     using Pass = Attend<T, D, kRowGroups, kKeyGroups, kKeys, kVec>;
@@ -95,12 +96,18 @@ int64_t blocks_of(const attention_emu_forward_t& a, int rows) {
 
 constexpr int kRowGroups = 4;
 
+// Whether all is so little that latency counts: blocks of 32 rows whose four waves share out
+// the keys then, up to two tiles each, and FP32 is multiplied as it is.
+bool few(const attention_emu_forward_t& a) {
+    return a.cu_seqlens == nullptr && a.keys <= 256 && blocks_of(a, 32) <= 512;
+}
+
 // Parts of the keys: where the blocks are fewer than two for each CU, as many as fill
 // those, of at least 256 keys each, if that saves a block more steps of 64 keys than the join
 // costs (its launch and traffic, about twelve of them).
 int parts_of(const attention_emu_forward_t& a) {
     const int64_t blocks = blocks_of(a, 32 * kRowGroups), most = (a.keys + 255) / 256;
-    if (blocks == 0 || most <= 1 || a.cu_seqlens != nullptr) return 1;
+    if (few(a) || blocks == 0 || most <= 1 || a.cu_seqlens != nullptr) return 1;
     const int64_t parts = std::max<int64_t>(1, std::min(most, 256 / blocks));
     const int64_t steps = (a.keys + 63) / 64;
     return steps - steps / parts > 12 ? (int)parts : 1;
@@ -127,7 +134,7 @@ int64_t bytes_of_parts(const attention_emu_forward_t& a, int parts) {
 
 int64_t attention_forward_workspace(const attention_emu_forward_t& a) {
     int64_t bytes = bytes_of_parts(a, parts_of(a));
-    if (a.dtype == SGEMM_EMU_F32)
+    if (a.dtype == SGEMM_EMU_F32 && !few(a))
         bytes += split_bytes(tokens_of(a), a.q_heads, a.size) +
                  2 * split_bytes(keys_of(a), a.k_heads, a.size);
     return bytes;
@@ -140,6 +147,14 @@ hipError_t launch_attention_forward(const attention_emu_forward_t& a, hipStream_
     if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) args.a.cu_keys = a.cu_seqlens;
     const int e = a.dtype == SGEMM_EMU_F32 ? 4 : 2;
     bool vec = a.size * e % 16 == 0 && rows_aligned16(a.o, e);
+    if (few(a)) {
+        vec = vec && rows_aligned16(a.q, e) && rows_aligned16(a.k, e) && rows_aligned16(a.v, e);
+        return by_form<float>(a.dtype, a.size, vec, [&](auto t, auto d, auto vec) {
+            return launch_blocks(attention_forward_kernel<decltype(t), decltype(d)::value, 1, 4, 32,
+                                                          decltype(vec)::value != 0>,
+                                 blocks_of(a, 32), 256, stream, args);
+        });
+    }
     if (a.dtype == SGEMM_EMU_F32) {
         Splitter split(a.size, static_cast<char*>(a.workspace) + bytes_of_parts(a, parts));
         const int batch = a.cu_seqlens != nullptr ? 1 : a.batch;
