@@ -13,7 +13,7 @@ import struct
 
 import paper_2308_15152_amd as _pkg
 from paper_2308_15152_amd.mixing import (
-    _NO_VIEW, _device, _launch_on, _new, _packed, _scale, _view, _workspace)
+    _NO_VIEW, _device, _launch_on, _like, _new, _packed, _view, _workspace)
 
 # The C argument structs of include/attention_emu.h.
 _FORWARD = struct.Struct("=8ifi2q20q2q")
@@ -39,12 +39,12 @@ def _launch(name, dev, stream, args):
 
 def _sizes(q, k):
     """(batch, tokens, keys, query heads, key heads, size)."""
-    if q.dim() != 4 or k.dim() != 4:
+    shape, keys = q.shape, k.shape
+    if len(shape) != 4 or len(keys) != 4:
         raise ValueError("q, k and v must be (batch, tokens, heads, size)")
     if q.dtype not in _dtypes:
         raise TypeError(f"q must be float32, bfloat16 or float16, got {q.dtype}")
-    b, t, hq, size = q.shape
-    return b, t, k.shape[1], hq, k.shape[2], size
+    return shape[0], shape[1], keys[1], shape[2], keys[2], shape[3]
 
 
 def _bounds(cu_seqlens, cu_keys, batch):
@@ -60,16 +60,30 @@ def _bounds(cu_seqlens, cu_keys, batch):
     return at, keys_at, n
 
 
+def _alike(x, shape, dtype):
+    """Whether a (batch, tokens, heads, size) tensor needs no closer look: _view says what is
+    wrong with it, at four times the price."""
+    return x.dtype is dtype and x.shape == shape and x.stride(3) == 1
+
+
 def _forward_args(q, k, v, out, lse, causal, scale, cu, cu_k, n):
     b, t, n_keys, hq, hk, size = _sizes(q, k)
-    dtype, keys = q.dtype, (b, n_keys, hk, size)
+    dtype, shape, f32 = q.dtype, q.shape, _pkg._torch.float32
+    keys = (b, n_keys, hk, size)
+    head = (_dtypes[dtype], n, t, n_keys, hq, hk, size, 1 if causal else 0,
+            max(size, 1) ** -0.5 if scale is None else scale, 0, cu, cu_k)
+    if out is not None and _alike(q, shape, dtype) and _alike(k, keys, dtype) \
+            and _alike(v, keys, dtype) and _alike(out, shape, dtype) and lse.dtype is f32 \
+            and lse.shape == (b, t, hq):
+        sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
+        return _FORWARD.pack(
+            *head, q.data_ptr(), sq[0], sq[1], sq[2], k.data_ptr(), sk[0], sk[1], sk[2],
+            v.data_ptr(), sv[0], sv[1], sv[2], out.data_ptr(), so[0], so[1], so[2],
+            lse.data_ptr(), *lse.stride(), 0, 0)
     results = _NO_VIEW * 2 if out is None else (
-        *_view(out, "out", q.shape, dtype),
-        *_view(lse, "lse", (b, t, hq), _pkg._torch.float32))
-    return _FORWARD.pack(
-        _dtypes[dtype], n, t, n_keys, hq, hk, size, 1 if causal else 0, _scale(scale, size), 0, cu,
-        cu_k, *_view(q, "q", q.shape, dtype), *_view(k, "k", keys, dtype),
-        *_view(v, "v", keys, dtype), *results, 0, 0)
+        *_view(out, "out", shape, dtype), *_view(lse, "lse", (b, t, hq), f32))
+    return _FORWARD.pack(*head, *_view(q, "q", shape, dtype), *_view(k, "k", keys, dtype),
+                         *_view(v, "v", keys, dtype), *results, 0, 0)
 
 
 def attention_emu_forward_workspace(q, k, v, *, causal: bool = True, cu_seqlens=None,
@@ -105,7 +119,7 @@ def attention_emu_forward(q, k, v, *, causal: bool = True, scale=None, cu_seqlen
     cu, cu_k, n = _bounds(cu_seqlens, cu_seqlens_k, q.shape[0])
     device = q.device
     if out is None:
-        out = _new(stream, q.shape, q.dtype, device)
+        out = _like(q, stream)
     if lse is None:
         lse = _new(stream, q.shape[:3], _pkg._torch.float32, device)
     args = _forward_args(q, k, v, out, lse, causal, scale, cu, cu_k, n)
@@ -122,15 +136,26 @@ def attention_emu_forward(q, k, v, *, causal: bool = True, scale=None, cu_seqlen
 
 def _backward_args(q, k, v, o, lse, do, grads, causal, scale, cu, cu_k, n):
     b, t, n_keys, hq, hk, size = _sizes(q, k)
-    dtype, keys, f32 = q.dtype, (b, n_keys, hk, size), _pkg._torch.float32
+    dtype, shape, f32 = q.dtype, q.shape, _pkg._torch.float32
+    keys = (b, n_keys, hk, size)
+    head = (_dtypes[dtype], n, t, n_keys, hq, hk, size, 1 if causal else 0,
+            max(size, 1) ** -0.5 if scale is None else scale, 0, cu, cu_k)
+    if grads is not None:
+        dq, dk, dv = grads
+        if all(_alike(x, shape, dtype) for x in (q, o, do, dq)) \
+                and all(_alike(x, keys, dtype) for x in (k, v, dk, dv)) \
+                and lse.dtype is f32 and lse.shape == (b, t, hq):
+            views = []
+            for x in (q, k, v, o, lse, do, dq, dk, dv):
+                views.append(x.data_ptr())
+                views += x.stride()[:3]
+            return _BACKWARD.pack(*head, *views, 0, 0)
     rest = _NO_VIEW * 6 if grads is None else (
-        *_view(o, "o", q.shape, dtype), *_view(lse, "lse", (b, t, hq), f32),
-        *_view(do, "do", q.shape, dtype), *_view(grads[0], "dq", q.shape, dtype),
+        *_view(o, "o", shape, dtype), *_view(lse, "lse", (b, t, hq), f32),
+        *_view(do, "do", shape, dtype), *_view(grads[0], "dq", shape, dtype),
         *_view(grads[1], "dk", keys, dtype), *_view(grads[2], "dv", keys, dtype))
-    return _BACKWARD.pack(
-        _dtypes[dtype], n, t, n_keys, hq, hk, size, 1 if causal else 0, _scale(scale, size), 0, cu,
-        cu_k, *_view(q, "q", q.shape, dtype), *_view(k, "k", keys, dtype),
-        *_view(v, "v", keys, dtype), *rest, 0, 0)
+    return _BACKWARD.pack(*head, *_view(q, "q", shape, dtype), *_view(k, "k", keys, dtype),
+                          *_view(v, "v", keys, dtype), *rest, 0, 0)
 
 
 def attention_emu_backward_workspace(q, k, v, *, causal: bool = True, cu_seqlens=None,
@@ -158,8 +183,8 @@ def attention_emu_backward(q, k, v, o, lse, do, *, causal: bool = True, scale=No
         _start()
     cu, cu_k, n = _bounds(cu_seqlens, cu_seqlens_k, q.shape[0])
     if out is None:
-        out = [_new(stream, x.shape, x.dtype, q.device, zero=cu_seqlens is not None)
-               for x in (q, k, v)]
+        out = [_like(x, stream) if cu_seqlens is None else
+               _new(stream, x.shape, x.dtype, q.device, zero=True) for x in (q, k, v)]
     dev = _device(q, k, v, o, lse, do, cu_seqlens, cu_seqlens_k, workspace, *out)
     args = _backward_args(q, k, v, o, lse, do, out, causal, scale, cu, cu_k, n)
     need = _calls["attention_emu_backward_workspace"](args)
@@ -181,19 +206,30 @@ def _step_args(q, k, v, lengths, prefix_k, prefix_v, slots, scale, out):
             raise ValueError("prefix_k and prefix_v must be (1, prefix, key heads, size)")
         prefix = prefix_k.shape[1]
         shape = (1, prefix, hk, size)
-        views = (*_view(prefix_k, "prefix_k", shape, dtype),
-                 *_view(prefix_v, "prefix_v", shape, dtype))
+        if _alike(prefix_k, shape, dtype) and _alike(prefix_v, shape, dtype):
+            sk, sv = prefix_k.stride(), prefix_v.stride()
+            views = (prefix_k.data_ptr(), sk[0], sk[1], sk[2],
+                     prefix_v.data_ptr(), sv[0], sv[1], sv[2])
+        else:
+            views = (*_view(prefix_k, "prefix_k", shape, dtype),
+                     *_view(prefix_v, "prefix_v", shape, dtype))
     for name, x in (("lengths", lengths), ("slots", slots)):
         if x is not None and (x.dtype is not _pkg._torch.int32 or x.shape != (b,)
                               or not x.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous int32 vector of the batch")
-    return _STEP.pack(
-        _dtypes[dtype], b, t, prefix, capacity, k.shape[0], hq, hk, size, _scale(scale, size),
-        *_view(q, "q", q.shape, dtype), *views, *_view(k, "k", caches, dtype),
-        *_view(v, "v", caches, dtype),
-        *(_NO_VIEW if out is None else _view(out, "out", q.shape, dtype)),
-        0 if lengths is None else lengths.data_ptr(), 0 if slots is None else slots.data_ptr(),
-        0, 0)
+    head = (_dtypes[dtype], b, t, prefix, capacity, k.shape[0], hq, hk, size,
+            max(size, 1) ** -0.5 if scale is None else scale)
+    tail = (0 if lengths is None else lengths.data_ptr(), 0 if slots is None else slots.data_ptr(),
+            0, 0)
+    if out is not None and _alike(q, q.shape, dtype) and _alike(k, caches, dtype) \
+            and _alike(v, caches, dtype) and _alike(out, q.shape, dtype):
+        sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
+        return _STEP.pack(
+            *head, q.data_ptr(), sq[0], sq[1], sq[2], *views, k.data_ptr(), sk[0], sk[1], sk[2],
+            v.data_ptr(), sv[0], sv[1], sv[2], out.data_ptr(), so[0], so[1], so[2], *tail)
+    return _STEP.pack(*head, *_view(q, "q", q.shape, dtype), *views, *_view(k, "k", caches, dtype),
+                      *_view(v, "v", caches, dtype),
+                      *(_NO_VIEW if out is None else _view(out, "out", q.shape, dtype)), *tail)
 
 
 def attention_emu_step_workspace(q, k, v, prefix_k=None, prefix_v=None, *, slots=None) -> int:
@@ -226,7 +262,7 @@ def attention_emu_step(q, k, v, lengths, prefix_k=None, prefix_v=None, *, slots=
     if lengths is None:
         raise ValueError("lengths must be a contiguous int32 vector of the batch")
     if out is None:
-        out = _new(stream, q.shape, q.dtype, q.device)
+        out = _like(q, stream)
     args = _step_args(q, k, v, lengths, prefix_k, prefix_v, slots, scale, out)
     dev = _device(q, k, v, lengths, prefix_k, prefix_v, slots, out, workspace)
     need = _calls["attention_emu_step_workspace"](args)
