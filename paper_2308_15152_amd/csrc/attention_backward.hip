@@ -88,6 +88,9 @@ __device__ inline f32x16 times(const f32x16& x, float f) {
 constexpr int kDqWaves = 4;
 constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
+constexpr int kFewKeys = 128;
+// A row's weights are all there if they sum to one but for FP32's roundings.
+constexpr float kWhole = 0x1p-12f;
 // Below so many blocks (two for each CU) two groups of waves share a block's keys: 384 blocks of
 // 2048 keys take 192 us for 203 in all (16 sequences of up to 2500 tokens 112 for 127), 512 take 3 more.
 constexpr int kDqPaired = 512;
@@ -165,7 +168,6 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         }
         delta = sum_halves(delta);
     }
-    if (valid && half == 0 && group_of == 0) args.delta[in_all * a.q_heads + h] = delta;
     // (rows that see nothing have lse -infinity)
     float z = __builtin_inff();
     if (valid) {
@@ -221,9 +223,9 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         }
     };
     const typename KV::Read read(lds, lane);
-    if (group_of < count) load(group_of);
+    float weight = 0.0f, rest = 0.0f;  // sums of the row's p and ds
     // one tile, in the first or the second place
-    const auto step = [&](int t, auto odd) __attribute__((always_inline)) {
+    const auto step = [&](int t, auto odd, auto only_rest) __attribute__((always_inline)) {
         constexpr int k_at = decltype(odd)::value * 2 * kTileBytes, v_at = k_at + kTileBytes;
         char* kt = lds + k_at;
         char* vt = lds + v_at;
@@ -263,16 +265,23 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
             }
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            dP[i] *= __builtin_amdgcn_exp2f(__builtin_fmaf(S[i], c, -z));
+        for (int i = 0; i < 16; ++i) {
+            S[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i], c, -z));
+            dP[i] *= S[i];
+        }
         if (key0 + kDqKeys > lim_min) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (key0 + acc_row(i, half) >= lim) dP[i] = 0.0f;
+                if (key0 + acc_row(i, half) >= lim) S[i] = dP[i] = 0.0f;
         }
-        if constexpr (kSplit)
+        if constexpr (kSplit) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) dP[i] *= by[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) weight += S[i], rest += dP[i];
+        }
+        if constexpr (decltype(only_rest)::value != 0) return;
         if constexpr (kNarrow<T>) {
             fit.fit(dP, dQ);
             dP = times(dP, fit.f);
@@ -285,10 +294,40 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
                 dQ[dt] = mma(KV::across(read, k_at, kb, dt), x, dQ[dt]);
         }
     };
-    for (int t = group_of; t < count + group_of; t += 2 * kGroups) {
-        step(t, Number<0>{});
-        if (t + kGroups < count + group_of) step(t + kGroups, Number<1>{});
+    const auto pass = [&](auto only_rest) __attribute__((always_inline)) {
+        weight = rest = 0.0f;
+        if (group_of < count) load(group_of);
+        for (int t = group_of; t < count + group_of; t += 2 * kGroups) {
+            step(t, Number<0>{}, only_rest);
+            if (t + kGroups < count + group_of) step(t + kGroups, Number<1>{}, only_rest);
+        }
+        if constexpr (!kSplit) {
+            weight = sum_halves(weight);
+            rest = sum_halves(rest);
+            if constexpr (kGroups == 2) {
+                __shared__ float sums[2][2][kDqRows];
+                const int at = 32 * wave + (lane & 31);
+                if (half == 0) sums[group_of][0][at] = weight, sums[group_of][1][at] = rest;
+                __syncthreads();
+                weight = sums[0][0][at] + sums[1][0][at];
+                rest = sums[0][1][at] + sums[1][1][at];
+            }
+            if (__builtin_fabsf(weight - 1.0f) < kWhole) delta += rest;
+            // (the places are free for the next pass)
+            __syncthreads();
+        }
+    };
+    // Where a row's weights sum to one (o and lse may be of more keys than are given), its ds sum
+    // to zero but for the error of delta, which is that of an o of 8 or 11 bits.  dk is formed
+    // with delta put right by it (FP16, 1000 keys: an error of 2.9e-4 for 3.1e-4; 526 -> 530 us
+    // for 4096 tokens).  In dq it matters where keys are few (bfloat16, 30 keys: 2.3e-3 for
+    // 3.1e-3; 500 keys: 2.35e-3 for 2.5e-3): there it is found beforehand (32 sequences of 64
+    // tokens 38.5 -> 40 us; with 512 keys it would be 251 -> 288).
+    if constexpr (!kSplit) {
+        if (count * kDqKeys <= kFewKeys) pass(Number<1>{});
     }
+    pass(Number<0>{});
+    if (valid && half == 0 && group_of == 0) args.delta[in_all * a.q_heads + h] = delta;
     const float f = kNarrow<T> ? a.scale / fit.f : a.scale;
     if constexpr (kGroups == 2) {
         typedef Pack<float, 4>::type Four;

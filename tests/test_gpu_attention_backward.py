@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2308_15152_amd as emu
-from attention_plain import attention, near
+from attention_plain import attention, near, unit
 from test_gpu_attention_forward import DEV, TYPES, dev, inputs
 
 pytestmark = pytest.mark.gpu
@@ -135,6 +135,24 @@ def test_strides(dtype, size):
     one = do[:, :1, :1].expand(b, t, hq, size)
     check(x, one, emu.attention_emu_backward(q, k, v, o, lse, do[:, :1, :1].to(DEV).expand(
         b, t, hq, size)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cut", [30, 170, 250])
+def test_parts_of_the_keys(dtype, cut):
+    """o and lse of all keys, the gradient over some of them at a time: dq in two parts."""
+    x = inputs(1, 100, 300, 4, 2, 64, dtype, seed=14)
+    do = gradient_of(x)
+    q, k, v = dev(*x)
+    o, lse = emu.attention_emu_forward(q, k, v, causal=False)
+    parts = [emu.attention_emu_backward(q, k[:, y], v[:, y], o, lse, do.to(DEV), causal=False)
+             for y in (slice(0, cut), slice(cut, None))]
+    want = attention(x[0][0], x[1][0], x[2][0], False, None, do[0])
+    halves = [y[0].double().cpu() for y, _, _ in parts]
+    value, bound = want["dq"]  # and each part is rounded
+    near(sum(halves), (value, bound + unit(dtype) * sum(y.abs() for y in halves)), "dq")
+    for i, name in ((1, "dk"), (2, "dv")):
+        near(torch.cat([y[i][0] for y in parts]), want[name], name)
 
 
 def test_against_differences():
