@@ -91,8 +91,9 @@ constexpr int kDqKeys = 32;
 constexpr int kFewKeys = 128;
 // A row's weights are all there if they sum to one but for FP32's roundings.
 constexpr float kWhole = 0x1p-12f;
-// Below so many blocks (two for each CU) two groups of waves share a block's keys: 384 blocks of
-// 2048 keys take 192 us for 203 in all (16 sequences of up to 2500 tokens 112 for 127), 512 take 3 more.
+// Below so many blocks (two for each CU) two groups of waves share a block's keys: the gradient with
+// 384 blocks of 2048 keys takes 192 us for 203, that of 16 packed sequences, 2500 tokens in all, 112
+// for 127; with 512 blocks it would take 3 us more than without.
 constexpr int kDqPaired = 512;
 
 // (FP32 operands of more than 96 elements take the registers of two waves)
@@ -417,7 +418,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     __shared__ __attribute__((aligned(16))) char lds[kLds];
     __shared__ __attribute__((aligned(16))) Row of_rows[2];
     // [key group][block][lane]
-    __shared__ Operand<T> operands[Shape::kLdsBlocks > 0 ? Shape::kKeyGroups * Shape::kLdsBlocks * 64 : 1];
+    __shared__ Operand<T>
+        operands[Shape::kLdsBlocks > 0 ? Shape::kKeyGroups * Shape::kLdsBlocks * 64 : 1];
     const int group = a.q_heads / a.k_heads;
     const bool packed = a.cu_seqlens != nullptr;
     const int part = (first_block + (int)blockIdx.x) % args.count;
@@ -501,7 +503,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     const E* q0 = row_of<E>(args.q, packed, n, sq, head * group);
     const E* d0 = row_of<E>(args.d_o, packed, n, sq, head * group);
     const float* lse0 = row_of<float>(a.lse, packed, n, sq, head * group);
-    const int64_t row_in_all = (packed ? sq.first : (int64_t)n * a.tokens) * a.q_heads + head * group;
+    const int64_t row_in_all =
+        (packed ? sq.first : (int64_t)n * a.tokens) * a.q_heads + head * group;
     // what the lane's key and value have been divided by
     float k_factor = 1.0f, v_factor = 1.0f;
     if constexpr (kSplit) {
@@ -557,7 +560,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
 #pragma unroll
         for (int i = 0; i < kPlanes<T>; ++i) {
             fq.start(to + i * QD::kPlaneBytes, q + i * kWidth<D>, width, thread, there);
-            fd.start(to + kTileBytes + i * QD::kPlaneBytes, o + i * kWidth<D>, width, thread, there);
+            fd.start(to + kTileBytes + i * QD::kPlaneBytes, o + i * kWidth<D>, width, thread,
+                     there);
         }
     };
     if (t0 < count) load(count - 1);
@@ -572,7 +576,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         fd.finish(ot, thread);
         if (thread < kRows) {
             // (rows that see nothing, and those that are none, have lse -infinity)
-            rw.z[thread] = st_lse == -__builtin_inff() ? __builtin_inff() : st_lse * kLog2e - kShift;
+            rw.z[thread] =
+                st_lse == -__builtin_inff() ? __builtin_inff() : st_lse * kLog2e - kShift;
             rw.delta[thread] = -st_delta;
             rw.seen[thread] = st_seen;
             if constexpr (kSplit) rw.q[thread] = st_q, rw.d_o[thread] = st_do;
@@ -711,7 +716,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
             }
     };
     const int64_t key_row = ((packed ? sk.first : (int64_t)n * a.keys) + key_in) * a.k_heads + head;
-    float* const dv_part = args.parts ? args.parts + (part * 2 * args.key_rows + key_row) * kPartStride<D>
+    float* const dv_part = args.parts ? args.parts + (part * 2 * args.key_rows + key_row) *
+                                                         kPartStride<D>
                                       : nullptr;
     float* const dk_part = args.parts ? dv_part + args.key_rows * kPartStride<D> : nullptr;
     join(dV, kSplit ? kBack / fit_v.f : kBack,
@@ -726,7 +732,8 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(BackwardArgs args, i
     typedef Pack<float, 4>::type Four;
     constexpr int kEach = kPartStride<D> / 4;
     const attention_emu_backward_t& a = args.a;
-    const int64_t at = (int64_t)(first_block + (int)blockIdx.x) * (256 / kEach) + threadIdx.x / kEach;
+    const int64_t at =
+        (int64_t)(first_block + (int)blockIdx.x) * (256 / kEach) + threadIdx.x / kEach;
     const int d = threadIdx.x % kEach * 4;
     if (at >= 2 * args.key_rows || d >= a.size) return;
     Four x{};
@@ -742,7 +749,9 @@ __global__ __launch_bounds__(256) void attention_sum_kernel(BackwardArgs args, i
     store_four<T, kVec>(out, d, a.size, x[0], x[1], x[2], x[3]);
 }
 
-int64_t batch_of(const attention_emu_backward_t& a) { return a.cu_seqlens != nullptr ? 1 : a.batch; }
+int64_t batch_of(const attention_emu_backward_t& a) {
+    return a.cu_seqlens != nullptr ? 1 : a.batch;
+}
 
 int64_t delta_bytes(const attention_emu_backward_t& a) {
     return (batch_of(a) * a.tokens * a.q_heads * 4 + 255) / 256 * 256;
@@ -755,7 +764,7 @@ int64_t planes_bytes(const attention_emu_backward_t& a) {
 }
 
 // Parts of the query rows of a block of keys: where the blocks are fewer than the CUs, as many as
-// fill those, of at least 512 rows each.
+// fill those, of at least 512 rows each: 3 x 1001 tokens with 2 key heads in FP32 250 -> 177 us.
 int parts_of(const attention_emu_backward_t& a) {
     const int64_t blocks = most_parts(a.batch, a.keys, 64, a.cu_seqlens != nullptr) * a.k_heads;
     if (blocks == 0 || a.cu_seqlens != nullptr) return 1;
@@ -765,7 +774,8 @@ int parts_of(const attention_emu_backward_t& a) {
 
 int64_t sums_bytes(const attention_emu_backward_t& a, int parts) {
     if (parts == 1) return 0;
-    return (parts * 2 * batch_of(a) * a.keys * a.k_heads * part_stride(a.size) * 4 + 255) / 256 * 256;
+    const int64_t rows = parts * 2 * batch_of(a) * a.keys * a.k_heads;
+    return (rows * part_stride(a.size) * 4 + 255) / 256 * 256;
 }
 
 }  // namespace
@@ -784,7 +794,8 @@ hipError_t launch_attention_backward(const attention_emu_backward_t& a, hipStrea
     args.q = a.q, args.k = a.k, args.v = a.v, args.d_o = a.d_o;
     args.count = parts_of(a);
     args.key_rows = batch_of(a) * a.keys * a.k_heads;
-    if (args.count > 1) args.parts = reinterpret_cast<float*>(ws + delta_bytes(a) + planes_bytes(a));
+    if (args.count > 1)
+        args.parts = reinterpret_cast<float*>(ws + delta_bytes(a) + planes_bytes(a));
     const int e = a.dtype == SGEMM_EMU_F32 ? 4 : 2;
     bool vec = a.size * e % 16 == 0;
     for (const sgemm_emu_view_t* x : {&a.o, &a.d_o, &a.dq, &a.dk, &a.dv})
@@ -810,16 +821,19 @@ hipError_t launch_attention_backward(const attention_emu_backward_t& a, hipStrea
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
         if (a.tokens > 0) {
+            // (split operands of more than 96 elements leave no registers for two groups)
+            constexpr int kGroups = kPlanes<T> == 1 || D <= 96 ? 2 : 1;
             const hipError_t e =
-                q_blocks < kDqPaired && (kPlanes<T> == 1 || D <= 96)
-                    ? launch_blocks(attention_dq_kernel<T, D, kVec, kPlanes<T> == 1 || D <= 96 ? 2 : 1>, q_blocks, 64 * kDqWaves * 2,
-                                    stream, args)
-                    : launch_blocks(attention_dq_kernel<T, D, kVec, 1>, q_blocks, 64 * kDqWaves, stream,
-                                    args);
+                q_blocks < kDqPaired
+                    ? launch_blocks(attention_dq_kernel<T, D, kVec, kGroups>, q_blocks,
+                                    64 * kDqWaves * kGroups, stream, args)
+                    : launch_blocks(attention_dq_kernel<T, D, kVec, 1>, q_blocks, 64 * kDqWaves,
+                                    stream, args);
             if (e != hipSuccess) return e;
         }
         using Shape = DkvShape<T, D>;
-        const int64_t blocks = most_parts(a.batch, a.keys, Shape::kKeys, packed) * a.k_heads * args.count;
+        const int64_t blocks =
+            most_parts(a.batch, a.keys, Shape::kKeys, packed) * a.k_heads * args.count;
         if (hipError_t e = launch_blocks(attention_dkv_kernel<T, D, kVec>, blocks, Shape::kThreads,
                                          stream, args))
             return e;

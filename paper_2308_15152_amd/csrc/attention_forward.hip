@@ -1,5 +1,9 @@
 // Attention over whole sequences: one block per 32 kRowGroups query rows of a
-// key head (a token's query heads that share it are neighbouring rows).
+// key head (a token's query heads that share it are neighbouring rows, so that grouped heads read
+// a key once).  Bound by the matrix instructions and what keeps them from running at once: 4 x
+// 4096 causal tokens, 32 heads of 128 in bfloat16, 593 us (930 TFLOP/s of the 1270 of a large
+// product; 43% of the cycles have matrix instructions in flight, 47% vector ones), one prompt of
+// 16384 2137 us (1030).  On that one, without the softmax's arithmetic 1880, without loads 1814.
 #include <algorithm>
 
 #include "attention_core.hpp"
@@ -97,23 +101,29 @@ int64_t blocks_of(const attention_emu_forward_t& a, int rows) {
 constexpr int kRowGroups = 4;
 
 // Whether all is so little that latency counts: blocks of 32 rows whose four waves share out
-// the keys then, up to two tiles each, and FP32 is multiplied as it is.
+// the keys then, up to two tiles each, and FP32 is multiplied as it is (128 tokens of 32 heads
+// 18.2 -> 12.6 us, 256 in FP32 26.9 -> 23.1; with 512 keys 40.7 -> 49.1 in FP32 and 17.5 -> 17.9 in
+// bfloat16, with 512 blocks 13.5 -> 14.0 and 31.6 -> 35.6 in FP32).
 bool few(const attention_emu_forward_t& a) {
-    return a.cu_seqlens == nullptr && a.keys <= 256 && blocks_of(a, 32) <= 512;
+    return a.cu_seqlens == nullptr && a.keys <= 256 && blocks_of(a, 32) <= 256;
 }
 
-// Parts of the keys: where the blocks are fewer than two for each CU, as many as fill
-// those, of at least 256 keys each, if that saves a block more steps of 64 keys than the join
-// costs (its launch and traffic, about twelve of them).
+// Parts of the keys: where the blocks leave CUs idle, as many as fill those, of at least 256
+// keys each (512: no change), if that saves a block more steps of 64 keys than the join costs
+// (its launch and traffic, about ten of them): 512 tokens, the last of 8192, 144 -> 62 us, 16 of
+// 8192 132 -> 18, 512 of 2048 39 -> 33, 256 of 1024 (12 steps) 23.9 -> 20.4; 1024 tokens (8 steps)
+// 24.2 -> 31.4.
 int parts_of(const attention_emu_forward_t& a) {
     const int64_t blocks = blocks_of(a, 32 * kRowGroups), most = (a.keys + 255) / 256;
     if (few(a) || blocks == 0 || most <= 1 || a.cu_seqlens != nullptr) return 1;
     const int64_t parts = std::max<int64_t>(1, std::min(most, 256 / blocks));
     const int64_t steps = (a.keys + 63) / 64;
-    return steps - steps / parts > 12 ? (int)parts : 1;
+    return steps - steps / parts > 10 ? (int)parts : 1;
 }
 
-// Whether two groups of waves share a block's keys.
+// Whether two groups of waves share a block's keys: 3 x 1001 tokens of 6 heads 26 -> 22 us; where
+// other blocks fill the CUs a block's chain is not what counts (24 packed sequences 67 -> 78 us,
+// 512 blocks 54 -> 64).
 bool paired(const attention_emu_forward_t& a, int64_t blocks) {
     return blocks <= 256 && a.keys > 128;
 }

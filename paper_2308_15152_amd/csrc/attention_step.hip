@@ -4,6 +4,11 @@
 // sequences, through a part of the prefix's keys.  The caches' blocks take the rows of one
 // sequence through a part of its cache, 32 keys to a wave.  The parts of a row are joined by a
 // second kernel; where there is one, it is the result.
+//
+// Bound by memory where the caches are long (128 sequences with caches of 1024 alone: 279 MB in 60
+// us, 4.65 TB/s), the prefix by the matrix instructions (as a prompt of the batch's rows: 54 to 60
+// us), both together 108 to 114 of the 118 us with the join.  Single sequences: latency, 8 to 10 us
+// and 3 of the join.
 #include <algorithm>
 
 #include "attention_core.hpp"
@@ -88,9 +93,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         a.size, c, a.scale < 0.0f, out, none);
 }
 
-// How the keys are cut: into parts of at least 256 keys of the prefix, 512 of a cache, that
-// fill the device.  The prefix's blocks, one for each CU, come first, and those of the caches,
-// which are bound by memory, run beside them.
+// How the keys are cut, into parts that fill the device: of at least 128 keys, a tile for each
+// wave, where a block has all rows that there are (a cache of 4096 keys alone: 14.3 us with parts
+// of 512, 11.7 of 256, 10.1 of 128; 16 rows behind a prefix of 4096 12.2 -> 11.4 from 256 to 128),
+// and of 256 of the prefix where there are more rows, whose parts are more to join (64 rows behind
+// 4096 keys 13.3 us, with 128 16.3).  Up to 64 rows are taken by 32, whose waves share out the
+// keys, instead of 128 (16 rows behind 4096 keys: kernel 8.3 us for 10.8; 256 rows the same).
+// The prefix's blocks, one for each CU, come first, and those of the caches, which are bound
+// by memory, run beside them: 128 sequences behind 16384 keys take 118 us, 144 with the blocks in
+// turn, 141 with the prefix last, 134 with two blocks of the prefix for each CU.
 StepArgs cut(const attention_emu_step_t& a) {
     StepArgs s{};
     s.a = a;
@@ -102,14 +113,14 @@ StepArgs cut(const attention_emu_step_t& a) {
     s.prefix_tiles = (int)((rows + tile - 1) / tile);
     if (a.prefix > 0) {
         const int64_t blocks = (int64_t)s.prefix_tiles * a.k_heads;
-        const int64_t most = (a.prefix + 255) / 256;
+        const int64_t each = rows <= 32 ? 128 : 256, most = (a.prefix + each - 1) / each;
         const int64_t parts =
             std::max<int64_t>(1, std::min(most, 256 / std::max<int64_t>(1, blocks)));
         s.prefix_keys = (int)(((a.prefix + parts - 1) / parts + 63) / 64 * 64);
         s.prefix_parts = (a.prefix + s.prefix_keys - 1) / s.prefix_keys;
     }
     const int64_t blocks = (int64_t)a.batch * a.k_heads * ((a.tokens * group + 31) / 32);
-    const int64_t most = (a.capacity + 511) / 512;
+    const int64_t most = (a.capacity + 127) / 128;
     s.own_parts = (int)std::max<int64_t>(1, std::min(most, 512 / std::max<int64_t>(1, blocks)));
     return s;
 }
