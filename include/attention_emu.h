@@ -31,12 +31,15 @@ extern "C" {
  *     Both are device int32 with batch + 1 values, not decreasing; values
  *     outside the rows are clamped to them; where they decrease, results are unspecified, and
  *     nothing outside the tensors is touched.  Rows of no sequence are not written.
- * A key or value that is not finite reaches only tokens that see it.
- * Scores, statistics and sums are FP32, FP32 products take FP32 operands; with 16-bit types the
- * weights e^{s_j - m} are rounded to the type before they multiply v, the results once.
+ * A key or value that is not finite reaches only tokens that see it (in FP32 it may come as
+ * NaN where the formula says infinity).
+ * Scores, statistics and sums are FP32.  With 16-bit types the weights e^{s_j - m} are
+ * rounded to the type before they multiply v, the results once.  FP32 operands and weights are
+ * taken as two FP16 parts with a power of two for each row (22 bits of an element, down to 2^-39
+ * of its row's largest), or as they are in short calls.
  * workspace: device memory, 256-byte aligned, at least what the _workspace query
- *   for the same arguments returns (0 bytes where the query rows alone fill the device; else
- *   the keys are cut into parts); its contents need not be kept.
+ *   for the same arguments returns (for parts of the keys where the query rows alone do not fill
+ *   the device, and for FP32's parts; 0 bytes where neither is); its contents need not be kept.
  * Sizes: size <= 128, q_heads a multiple of k_heads, token strides <= 2^22, scale
  * finite and not zero, tokens x q_heads and keys below 2^31 for a sequence, and blocks of 32
  * rows or keys below 2^30 in all.
@@ -64,11 +67,13 @@ int attention_emu_forward(const attention_emu_forward_t* a, hipStream_t stream);
  *   p_ij = e^{s_ij - lse_i},  dv_j = sum_i p_ij do_i,
  *   ds_ij = p_ij (do_i v_j - do_i o_i),  dq_i = scale sum_j ds_ij k_j,
  *   dk_j = scale sum_i ds_ij q_i,
- * sums over tokens and over a key head's query heads in FP32 in a fixed order.  Gradients of
+ * sums over tokens and over a key head's query heads in FP32 in a fixed order; with 16-bit
+ * types p and ds are rounded to the type before they multiply.  o and lse may be those of more
+ * keys than are given here (keys in parts: dq is the sum of the parts').  Gradients of
  * tokens that see no key and of keys that no token sees are zero.  Where q, k, v, o or d_o is
  * not finite, any gradient of its sequence's key head may not be; other sequences and
  * heads are not reached.
- * workspace: as above. */
+ * workspace: as above, and for a number for each query row. */
 typedef struct {
     int32_t dtype, batch, tokens, keys, q_heads, k_heads, size, causal;
     float scale;

@@ -176,9 +176,10 @@ def attention_emu_backward(q, k, v, o, lse, do, *, causal: bool = True, scale=No
                            cu_seqlens=None, cu_seqlens_k=None, out=None, workspace=None,
                            stream=None):
     """(dq, dk, dv): the gradients of ``attention_emu_forward`` with these inputs, from its
-    results o and lse and from do (like o).  out: the three tensors to write to; rows of no
-    packed sequence are not written, so tensors made here start as zeros there.  workspace:
-    uint8, ``attention_emu_backward_workspace`` bytes, allocated if None."""
+    results o and lse (which may be of more keys than are given) and from do (like o).  out:
+    the three tensors to write to; rows of no packed sequence are not written, so tensors made
+    here start as zeros there.  workspace: uint8, ``attention_emu_backward_workspace`` bytes,
+    allocated if None."""
     if not _calls:
         _start()
     cu, cu_k, n = _bounds(cu_seqlens, cu_seqlens_k, q.shape[0])

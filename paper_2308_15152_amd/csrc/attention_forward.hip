@@ -3,7 +3,7 @@
 // a key once).  Bound by the matrix instructions and what keeps them from running at once: 4 x
 // 4096 causal tokens, 32 heads of 128 in bfloat16, 593 us (930 TFLOP/s of the 1270 of a large
 // product; 43% of the cycles have matrix instructions in flight, 47% vector ones), one prompt of
-// 16384 2137 us (1030).  On that one, without the softmax's arithmetic 1880, without loads 1814.
+// 32768 with 8 heads 2.12 ms (1040).  On that one, without the softmax's arithmetic 1880, without loads 1814.
 #include <algorithm>
 
 #include "attention_core.hpp"
@@ -77,7 +77,8 @@ __global__ __launch_bounds__(64 * kRowGroups * kKeyGroups,
         return row_out<Out<T>, D, kVec>(args.parts, part,
                                    (first_token + token) * a.q_heads + head * group + h,
                                    o + token * a.o.token + h * a.o.head,
-                                   lse ? lse + token * a.lse.token + h * a.lse.head : nullptr, a.size);
+                                   lse ? lse + token * a.lse.token + h * a.lse.head : nullptr,
+                                   a.size);
     };
     const int shift = sk.count - sq.count + 1;
     const auto limit = [&](int r) { return a.causal ? r / group + shift : sk.count; };
@@ -152,8 +153,8 @@ int64_t attention_forward_workspace(const attention_emu_forward_t& a) {
 
 hipError_t launch_attention_forward(const attention_emu_forward_t& a, hipStream_t stream) {
     const int parts = parts_of(a);
-    ForwardArgs args{a, parts, parts_in(a.workspace, parts, tokens_of(a) * a.q_heads, a.size), a.q, a.k,
-                     a.v, nullptr, nullptr, nullptr};
+    ForwardArgs args{a, parts, parts_in(a.workspace, parts, tokens_of(a) * a.q_heads, a.size),
+                     a.q, a.k, a.v, nullptr, nullptr, nullptr};
     if (a.cu_seqlens != nullptr && a.cu_keys == nullptr) args.a.cu_keys = a.cu_seqlens;
     const int e = a.dtype == SGEMM_EMU_F32 ? 4 : 2;
     bool vec = a.size * e % 16 == 0 && rows_aligned16(a.o, e);
@@ -192,7 +193,8 @@ hipError_t launch_attention_forward(const attention_emu_forward_t& a, hipStream_
         if (e != hipSuccess) return e;
         if (parts == 1) return hipSuccess;
         return launch_join<Out<T>, D, kVec>(
-            JoinArgs{args.parts, a.o, a.lse, parts, a.tokens, a.q_heads, a.size, nullptr, 0}, stream);
+            JoinArgs{args.parts, a.o, a.lse, parts, a.tokens, a.q_heads, a.size, nullptr, 0},
+            stream);
     });
 }
 

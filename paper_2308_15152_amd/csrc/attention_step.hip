@@ -62,8 +62,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         const T* v = static_cast<const T*>(a.prefix_v.p) + head * a.prefix_v.head;
         const int rows = a.batch * a.tokens * group;
         if (s.prefix_few)
-            Own::run(lds, rows, tile * 32, row, all, k, a.prefix_k.token, v, a.prefix_v.token, first,
-                     end, a.size, c, a.scale < 0.0f, out, none);
+            Own::run(lds, rows, tile * 32, row, all, k, a.prefix_k.token, v, a.prefix_v.token,
+                     first, end, a.size, c, a.scale < 0.0f, out, none);
         else
             Prefix::run(lds, rows, tile * kPrefixRows, row, all, k, a.prefix_k.token, v,
                         a.prefix_v.token, first, end, a.size, c, a.scale < 0.0f, out, none);
@@ -93,15 +93,19 @@ __global__ __launch_bounds__(kThreads, 2) void attention_step_kernel(StepArgs s,
         a.size, c, a.scale < 0.0f, out, none);
 }
 
-// How the keys are cut, into parts that fill the device: of at least 128 keys, a tile for each
-// wave, where a block has all rows that there are (a cache of 4096 keys alone: 14.3 us with parts
-// of 512, 11.7 of 256, 10.1 of 128; 16 rows behind a prefix of 4096 12.2 -> 11.4 from 256 to 128),
-// and of 256 of the prefix where there are more rows, whose parts are more to join (64 rows behind
-// 4096 keys 13.3 us, with 128 16.3).  Up to 64 rows are taken by 32, whose waves share out the
-// keys, instead of 128 (16 rows behind 4096 keys: kernel 8.3 us for 10.8; 256 rows the same).
-// The prefix's blocks, one for each CU, come first, and those of the caches, which are bound
-// by memory, run beside them: 128 sequences behind 16384 keys take 118 us, 144 with the blocks in
-// turn, 141 with the prefix last, 134 with two blocks of the prefix for each CU.
+// How the keys are cut.  A cache: into parts of at least 128 keys, a tile for each wave, that
+// fill the CUs (one cache of 4096 keys alone: 14.3 us with parts of 512, 11.7 of 256, 10.1 of
+// 128), or, up to 32, of 384 that fill them twice, where that is more (16 caches of 4096 23.4 us
+// for 25.3, 40 of 1500 25.0 for 29.3; with parts of 128 for that, 33 of 300 take 11.8 us for
+// 10.3, with parts of 512 20 of 2000 22.9 for 20.2; 85 parts of one of 32768 24.0 for 20.1 with
+// 64).  A prefix: into parts that fill the CUs, of at least 128 keys where one block has all
+// rows that there are (16 rows behind 4096 keys 12.2 -> 11.4), else of 256, for more rows are
+// more to join (64 rows behind 4096 keys 13.3 us, with 128 16.3).  Up to 64 rows are taken by
+// 32, whose waves share out the keys, instead of 128 (16 rows behind 4096 keys: kernel 8.3 us
+// for 10.8; 256 rows the same).  The prefix's blocks, one for each CU, come first, and those of
+// the caches, which are bound by memory, run beside them: 128 sequences behind 16384 keys take
+// 118 us, 144 with the blocks in turn, 141 with the prefix last, 134 with two blocks of the
+// prefix for each CU.
 StepArgs cut(const attention_emu_step_t& a) {
     StepArgs s{};
     s.a = a;
@@ -120,8 +124,10 @@ StepArgs cut(const attention_emu_step_t& a) {
         s.prefix_parts = (a.prefix + s.prefix_keys - 1) / s.prefix_keys;
     }
     const int64_t blocks = (int64_t)a.batch * a.k_heads * ((a.tokens * group + 31) / 32);
-    const int64_t most = (a.capacity + 127) / 128;
-    s.own_parts = (int)std::max<int64_t>(1, std::min(most, 512 / std::max<int64_t>(1, blocks)));
+    const auto parts = [&](int64_t keys, int64_t fill) {
+        return std::min((a.capacity + keys - 1) / keys, fill / std::max<int64_t>(1, blocks));
+    };
+    s.own_parts = (int)std::max<int64_t>({1, parts(128, 256), std::min<int64_t>(parts(384, 512), 32)});
     return s;
 }
 
@@ -150,12 +156,13 @@ hipError_t launch_attention_step(const attention_emu_step_t& a, hipStream_t stre
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         constexpr bool kVec = decltype(vec)::value != 0;
-        if (hipError_t e = launch_blocks(attention_step_kernel<T, D, kVec>, blocks, kThreads, stream,
-                                         s))
+        if (hipError_t e =
+                launch_blocks(attention_step_kernel<T, D, kVec>, blocks, kThreads, stream, s))
             return e;
         if (parts == 1) return hipSuccess;
         return launch_join<T, D, kVec>(
-            JoinArgs{s.parts, a.o, {}, parts, a.tokens, a.q_heads, a.size, a.slots, a.n_slots}, stream);
+            JoinArgs{s.parts, a.o, {}, parts, a.tokens, a.q_heads, a.size, a.slots, a.n_slots},
+            stream);
     });
 }
 
