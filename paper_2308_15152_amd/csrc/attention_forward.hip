@@ -2,7 +2,7 @@
 // key head (a token's query heads that share it are neighbouring rows, so that grouped heads read
 // a key once).  Bound by the matrix instructions and what keeps them from running at once: 4 x
 // 4096 causal tokens, 32 heads of 128 in bfloat16, 593 us (930 TFLOP/s of the 1270 of a large
-// product; 43% of the cycles have matrix instructions in flight, 47% vector ones), one prompt of
+// product; 48% of the cycles have matrix instructions in flight, 45% vector ones), one prompt of
 // 32768 with 8 heads 2.12 ms (1040).  On that one, without the softmax's arithmetic 1880, without loads 1814.
 #include <algorithm>
 
