@@ -31,8 +31,8 @@ extern "C" {
  *     Both are device int32 with batch + 1 values, not decreasing; values
  *     outside the rows are clamped to them; where they decrease, results are unspecified, and
  *     nothing outside the tensors is touched.  Rows of no sequence are not written.
- * A key or value that is not finite reaches only tokens that see it (in FP32 it may come as
- * NaN where the formula says infinity).
+ * A key or value that is not finite reaches only tokens that see it (as NaN, it may be, where the
+ * formula says infinity).
  * Scores, statistics and sums are FP32.  With 16-bit types the weights e^{s_j - m} are
  * rounded to the type before they multiply v, the results once.  FP32 operands and weights are
  * taken as two FP16 parts with a power of two for each row (22 bits of an element, down to 2^-39

@@ -94,7 +94,7 @@ struct Attend {
         f32x16 O[D / 32];
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) O[dt] = f32x16{};
-        float l = 0.0f, z = -1e30f;
+        float l = 0.0f, z = kLeast;
         float unit = kSplit ? 0x1p-126f : 1.0f;  // of O: the largest factor of values so far
         bool found = false;
         if (kVecTile && width < kWidth<D>) {
@@ -291,8 +291,9 @@ struct Attend {
                 for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        sums[(4 * dt + i) * 64] = Four{O[dt][4 * i], O[dt][4 * i + 1], O[dt][4 * i + 2],
-                                                       O[dt][4 * i + 3]} * unit;
+                        sums[(4 * dt + i) * 64] =
+                            Four{O[dt][4 * i], O[dt][4 * i + 1], O[dt][4 * i + 2],
+                                 O[dt][4 * i + 3]} * unit;
                 of_row[0] = l, of_row[64] = z;
             }
             __syncthreads();
@@ -347,7 +348,7 @@ struct Attend {
             for (int w = threadIdx.x; w < 32 * (D / 4); w += kThreads) {
                 const int r = w / (D / 4), d = w % (D / 4) * 4;
                 if (row0 + r >= rows) break;
-                float zs = -1e30f, ls = 0.0f;
+                float zs = kLeast, ls = 0.0f;
 #pragma unroll
                 for (int g = 0; g < kKeyGroups; ++g) zs = fmaxf(zs, state[2 * (g * 32 + r) + 1]);
                 Pack<float, 4>::type x{};

@@ -10,6 +10,8 @@ namespace sgemm_emu {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
+// The reference of a row that has seen nothing: below all scores, but 2^(kLeast - kLeast) is one.
+constexpr float kLeast = -3e38f;
 
 // Elements from one row of a part to the next.
 template <int D>
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(JoinArgs a
     const bool here = row < a.parts.rows && d < a.size;
     const int64_t token = here ? row / a.q_heads : 0;
     const int h = (int)(row - token * a.q_heads), n = (int)(token / a.tokens);
-    float z = -1e30f, l = 0.0f;
+    float z = kLeast, l = 0.0f;
     Four x{};
     const int slot = a.slots == nullptr ? 0 : a.slots[n];
     if (here && (a.slots == nullptr || (slot >= 0 && slot < a.n_slots))) {

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2308_15152_amd as emu
-from attention_plain import attention, near
+from attention_plain import attention, near, unit
 from test_gpu_attention_backward import check as check_gradient
 from test_gpu_attention_backward import gradient_of, gradients
 from test_gpu_attention_forward import DEV, TYPES, check, dev, inputs
@@ -181,6 +181,36 @@ def test_offsets_past_32_bits(dtype):
     got = emu.attention_emu_backward(*on[:3], apart, lse, on[3], out=[
         spread(outs, y.shape, i) for i, y in enumerate(x)])
     check_gradient(x, do, got)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("t,n,joined", [(40, 40, False), (400, 400, False), (16, 5000, True)])
+def test_scores_of_any_magnitude(dtype, sign, t, n, joined):
+    """All scores of a row are the same, of magnitude 2^107, so that its weights are equal: o is
+    the mean of what it sees (weights and o are rounded to the type, sums of n terms to n 2^-24).
+    Where parts of the keys are joined by their log-sums, those hold 24 bits, 2^83 and up, and
+    the number of a part's keys is not in them: o is some mean of the values then."""
+    q, k, v = inputs(1, t, n, 2, 1, 64, dtype, seed=n)
+    q[:], k[:] = 0.0, 0.0
+    q[..., 3], k[..., 3] = 2.0 ** 55, sign * 2.0 ** 55
+    o, lse = emu.attention_emu_forward(*dev(q, k, v))
+    assert (lse == sign * 2.0 ** 107).all()  # log n is far below its last bit
+    e = unit(dtype) + n * 2.0 ** -24
+    values = v[0, :, 0].double()
+    if not joined:
+        seen = (torch.arange(n) <= torch.arange(t)[:, None] + n - t).double()
+        seen /= seen.sum(1, keepdim=True)
+        want, size = seen @ values, seen @ values.abs()
+        for h in range(2):
+            assert ((o[0, :, h].double().cpu() - want).abs() <= e * size + e * want.abs()).all()
+    step = emu.attention_emu_step(*dev(q[:, -1:], k, v, torch.tensor([n], dtype=torch.int32)),
+                                  *dev(k, v))
+    for y in (o[0, -1], step[0, 0]):
+        y = y.double().cpu()
+        margin = 2 * e * values.abs().amax(0)
+        assert (y <= values.amax(0) + margin).all() and (y >= values.amin(0) - margin).all()
+        assert (y != 0).any()
 
 
 def test_a_row_of_much_larger_scores():
