@@ -40,8 +40,8 @@ extern "C" {
  * workspace: device memory, 256-byte aligned, at least what the _workspace query
  *   for the same arguments returns (for parts of the keys where the query rows alone do not fill
  *   the device, and for FP32's parts; 0 bytes where neither is); its contents need not be kept.
- * Sizes: size <= 128, q_heads a multiple of k_heads, token strides <= 2^22, scale
- * finite and not zero, tokens x q_heads and keys below 2^31 for a sequence, and blocks of 32
+ * Sizes: size <= 128, q_heads a multiple of k_heads, with FP32 at most 2^14, token strides <=
+ * 2^22, scale finite and not zero, tokens x q_heads and keys below 2^31 for a sequence, and blocks of 32
  * rows or keys below 2^30 in all.
  * Errors: _DIM (also keys != tokens without cu_keys), _UNSUPPORTED (dtype, sizes, scale,
  * strides and head counts above), _NULL, _STRIDE, _ALIAS, _HIP.

@@ -37,6 +37,10 @@ int check_sequences(const A& a) {
     if (a.cu_seqlens == nullptr && a.cu_keys != nullptr) return SGEMM_EMU_ERR_NULL;
     if (a.cu_seqlens != nullptr && a.cu_keys == nullptr && a.keys != a.tokens)
         return SGEMM_EMU_ERR_DIM;
+    // rows of the FP16 planes of FP32 tensors (2 x 64 or 128 elements for each head) are as near
+    // to each other as those of tensors have to be
+    if (a.dtype == SGEMM_EMU_F32 && a.q_heads > kAttentionMostStride / 256)
+        return SGEMM_EMU_ERR_UNSUPPORTED;
     // rows and blocks of at least 32 rows or keys are counted in 32 bits
     const int64_t sequences = a.cu_seqlens != nullptr ? 1 : a.batch;
     if ((int64_t)a.tokens * a.q_heads > INT32_MAX - 4096 || a.keys > INT32_MAX - 4096 ||

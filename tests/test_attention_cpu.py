@@ -92,7 +92,12 @@ SIZES = [
     (dict(batch=BIG, tokens=1), UNSUPPORTED)]
 
 
-@pytest.mark.parametrize("kw,code", SIZES + [
+WIDE = [(dict(dtype=0, q_heads=16386, size=8), UNSUPPORTED),  # planes too far apart
+        (dict(dtype=0, q_heads=16384, size=8, batch=0), OK),
+        (dict(dtype=1, q_heads=16386, size=8, batch=0), OK)]
+
+
+@pytest.mark.parametrize("kw,code", SIZES + WIDE + [
     (dict(batch=0), OK), (dict(tokens=0), OK), (dict(tokens=0, keys=7), OK),
     (dict(views={"q": (0, 1, 1, 1)}), NULL), (dict(views={"k": (0, 1, 1, 1)}), NULL),
     (dict(views={"v": (0, 1, 1, 1)}), NULL), (dict(views={"o": (0, 1, 1, 1)}), NULL),
@@ -140,7 +145,7 @@ def backward(query=False, cu=0, cu_k=0, ws=1 << 32, ws_bytes=1 << 40, views=None
                 (*s.values(), cu, cu_k, *(y for z in x.values() for y in z), ws, ws_bytes), query)
 
 
-@pytest.mark.parametrize("kw,code", SIZES + [(dict(batch=0), OK)] + [
+@pytest.mark.parametrize("kw,code", SIZES + WIDE + [(dict(batch=0), OK)] + [
     (dict(views={name: (0, 1, 1, 1)}), NULL)
     for name in ("q", "k", "v", "o", "lse", "do", "dq", "dk", "dv")] + [
     (dict(ws=0), NULL), (dict(ws_bytes=256), DIM), (dict(ws=(1 << 32) + 128), DIM),
