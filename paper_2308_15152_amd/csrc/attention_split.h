@@ -25,7 +25,6 @@ public:
     // Planes of x, (batch, tokens, heads).
     SplitTensor add(const sgemm_emu_view_t& x, int batch, int tokens, int heads);
     hipError_t launch(hipStream_t stream) const;
-    char* end() const { return at_; }
 
     struct Job {
         sgemm_emu_view_t x;

@@ -195,3 +195,15 @@ def test_the_same_call_gives_the_same_bits():
     first = gradients(x, do)
     for _ in range(3):
         assert all(torch.equal(a, b) for a, b in zip(first, gradients(x, do)))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_broadcast_inputs(dtype):
+    """Keys and values that all sequences, or all key heads, share: a gradient for each."""
+    x = inputs(3, 90, 90, 4, 2, 64, dtype, seed=15)
+    q, k, v = dev(*x)
+    k, v = k[:1].expand(3, -1, -1, -1), v[:, :, :1].expand(-1, -1, 2, -1)
+    do = gradient_of(x)
+    o, lse = emu.attention_emu_forward(q, k, v)
+    got = emu.attention_emu_backward(q, k, v, o, lse, do.to(DEV))
+    check((x[0], x[1][:1].expand(3, -1, -1, -1), x[2][:, :, :1].expand(-1, -1, 2, -1)), do, got)
