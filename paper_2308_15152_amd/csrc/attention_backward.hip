@@ -642,8 +642,12 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         for (int i = 0; i < 16; i += 4) {
             const auto x = per_row(rw.z, i);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                P[i + j] = __builtin_amdgcn_exp2f(__builtin_fmaf(P[i + j], c, -x[j]));
+            for (int j = 0; j < 4; ++j) {
+                float log = __builtin_fmaf(P[i + j], c, -x[j]);
+                // (scores of 2^24 and more have rounding errors that take p past one; NaN stays)
+                if constexpr (kNarrow<T> && !kSplit) log = __builtin_elementwise_minimum(log, kShift);
+                P[i + j] = __builtin_amdgcn_exp2f(log);
+            }
         }
         const bool masked = a.causal && wave_first + shift <= wave_key + 31;
         if (masked) {

@@ -207,3 +207,17 @@ def test_broadcast_inputs(dtype):
     o, lse = emu.attention_emu_forward(q, k, v)
     got = emu.attention_emu_backward(q, k, v, o, lse, do.to(DEV))
     check((x[0], x[1][:1].expand(3, -1, -1, -1), x[2][:, :, :1].expand(-1, -1, 2, -1)), do, got)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_scores_keep_gradients_finite(dtype):
+    """Scores of 2^30, whose last bits are whole numbers: weights are not exact, but dv, a
+    sum of weights up to one times do, is finite and no larger than the sum of |do|."""
+    x = inputs(1, 100, 100, 2, 1, 64, dtype, seed=16)
+    x = x[0] * 2048, x[1] * 8192, x[2]
+    do = gradient_of(x)
+    got = gradients(x, do)
+    assert all(torch.isfinite(y).all() for y in got)
+    if dtype == torch.float16:
+        most = do.double().abs().sum((1, 2))
+        assert (got[2][0, :, 0].double().cpu().abs() <= 1.01 * most).all()
