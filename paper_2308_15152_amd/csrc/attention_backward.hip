@@ -644,7 +644,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float log = __builtin_fmaf(P[i + j], c, -x[j]);
-                // (scores of 2^24 and more have rounding errors that take p past one; NaN stays)
+                // (scores of 2^24 and more have rounding errors that take p past one;
+                // NaN stays)
                 if constexpr (kNarrow<T> && !kSplit) log = __builtin_elementwise_minimum(log, kShift);
                 P[i + j] = __builtin_amdgcn_exp2f(log);
             }
