@@ -34,9 +34,11 @@ extern "C" {
  * A key or value that is not finite reaches only tokens that see it (as NaN, it may be, where the
  * formula says infinity).
  * Scores, statistics and sums are FP32.  With 16-bit types the weights e^{s_j - m} are
- * rounded to the type before they multiply v, the results once.  FP32 operands and weights are
- * taken as two FP16 parts with a power of two for each row (22 bits of an element, down to 2^-39
- * of its row's largest), or as they are in short calls.
+ * rounded to the type before they multiply v, the results once.  FP32 operands are taken as
+ * two FP16 parts with a power of two for each row (22 bits of an element, down to 2^-39 of its
+ * row's largest), and weights, times their value's power of two, in the same way with one for each
+ * token (22 bits, down to 2^-34 of the largest such product that the token has), or both as they are
+ * in short calls.
  * workspace: device memory, 256-byte aligned, at least what the _workspace query
  *   for the same arguments returns (for parts of the keys where the query rows alone do not fill
  *   the device, and for FP32's parts; 0 bytes where neither is); its contents need not be kept.

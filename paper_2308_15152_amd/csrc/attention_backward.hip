@@ -57,39 +57,6 @@ __device__ inline __attribute__((always_inline)) void schedule_steps(F f) {
     }
 }
 
-// A column's power of two.
-struct Fit {
-    float f = 0x1p100f;
-
-    // So that |x| f stays below 2^15; the sums are rescaled where f changes.
-    template <int N>
-    __device__ inline void fit(const f32x16& x, f32x16 (&sum)[N]) {
-        float most = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) most = fmaxf(most, __builtin_fabsf(x[i]));
-        most = max_halves(most);
-        const bool over = most * f > 0x1p15f;
-        if (__any(over)) {
-            // 2^10 <= most f < 2^11
-            const int e = (int)(__float_as_uint(most) >> 23);
-            const float to = over ? __uint_as_float((unsigned)max(min(264 - e, 227), 1) << 23) : f;
-            const float by = to / f;
-#pragma unroll
-            for (int d = 0; d < N; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[d][i] *= by;
-            f = to;
-        }
-    }
-};
-
-__device__ inline f32x16 times(const f32x16& x, float f) {
-    f32x16 y;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = x[i] * f;
-    return y;
-}
-
 constexpr int kDqWaves = 4;
 constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
@@ -197,7 +164,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
     f32x16 dQ[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dQ[dt] = f32x16{};
-    Fit fit;
+    Fit<100> fit;
     // (what is not loaded multiplies zeros and has to be finite)
     clear_lds(lds, 4 * kTileBytes, thread, kThreads);
     lds_barrier();
@@ -289,7 +256,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         }
         if constexpr (decltype(only_rest)::value != 0) return;
         if constexpr (kNarrow<T>) {
-            fit.fit(dP, dQ);
+            fit.fit(largest(dP), dQ);
             dP = times(dP, fit.f);
         }
 #pragma unroll
@@ -501,7 +468,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     f32x16 dK[D / 32], dV[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dK[dt] = f32x16{}, dV[dt] = f32x16{};
-    Fit fit, fit_v;
+    Fit<100> fit, fit_v;
     // (what is not loaded multiplies zeros and has to be finite)
     clear_lds(lds, 4 * kTileBytes, thread, kThreads);
     lds_barrier();
@@ -665,7 +632,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
 #pragma unroll
                 for (int j = 0; j < 4; ++j) P[i + j] *= y[j], dP[i + j] *= x[j];
             }
-            fit_v.fit(P, dV);
+            fit_v.fit(largest(P), dV);
             P = times(P, fit_v.f);
         }
 #pragma unroll
@@ -676,7 +643,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
                 dV[dt] = mma(QD::across(o_across, kb, 32 * dt), x, dV[dt]);
         }
         if constexpr (kNarrow<T>) {
-            fit.fit(dP, dK);
+            fit.fit(largest(dP), dK);
             dP = times(dP, fit.f);
         }
 #pragma unroll

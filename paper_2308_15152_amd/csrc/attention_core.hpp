@@ -95,7 +95,10 @@ struct Attend {
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) O[dt] = f32x16{};
         float l = 0.0f, z = kLeast;
-        float unit = kSplit ? 0x1p-126f : 1.0f;  // of O: the largest factor of values so far
+        // split values: a weight times its value's factor becomes an operand, for which each row
+        // has a power of two by what it weighs itself: by the largest factor of a tile's values,
+        // one that a row does not see, or hardly weighs, took the bits of all others
+        Fit<126> fit;
         bool found = false;
         if (kVecTile && width < kWidth<D>) {
             clear_lds(lds, kTiles, threadIdx.x, kThreads);
@@ -204,24 +207,14 @@ struct Attend {
                                                                       4 * half);
             };
             if constexpr (kSplit) {
-                float most = 0.0f;
 #pragma unroll
                 for (int s = 0; s < kKeys / 32; ++s)
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
-                        const auto x = four_of(of_tile, s, i), y = four_of(of_tile + kKeys, s, i);
+                        const auto x = four_of(of_tile, s, i);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j], most = fmaxf(most, y[j]);
+                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j];
                     }
-                most = max_halves(most);
-                if (__any(most > unit)) {
-                    const float f = unit * inverse_of_power(most);
-#pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) O[dt][i] *= f;
-                    unit = most;
-                }
             }
             if (key0 + kKeys > lim_min) {
 #pragma unroll
@@ -239,10 +232,12 @@ struct Attend {
             if (__any(want > z + kSlack)) {
                 const float to = want > z + kSlack ? want : z;
                 const float f = __builtin_amdgcn_exp2f(z - to);
+                const float of_sum =
+                    kSplit ? __builtin_amdgcn_exp2f(z - to + fit.rise(to - z)) : f;
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) O[dt][i] *= f;
+                    for (int i = 0; i < 16; ++i) O[dt][i] *= of_sum;
                 l *= f;
                 z = to;
             }
@@ -253,15 +248,25 @@ struct Attend {
                     S[s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s][i], c, -z));
                     l += S[s][i];
                 }
-                if constexpr (kSplit) {
-                    const float by = inverse_of_power(unit);
+            }
+            if constexpr (kSplit) {
+                float most = 0.0f;
+#pragma unroll
+                for (int s = 0; s < kKeys / 32; ++s) {
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
                         const auto x = four_of(of_tile + kKeys, s, i);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j] * by;
+                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j];
                     }
+                    most = fmaxf(most, largest(S[s]));
                 }
+                fit.fit(most, O);
+#pragma unroll
+                for (int s = 0; s < kKeys / 32; ++s) S[s] = times(S[s], fit.f);
+            }
+#pragma unroll
+            for (int s = 0; s < kKeys / 32; ++s) {
 #pragma unroll
                 for (int kb = 0; kb < kParts; ++kb) {
                     const Operand<T> P = operand<T>(S[s], kb);
@@ -278,6 +283,7 @@ struct Attend {
             if (t + step < last) tile(t + step, Number<1>{});
         }
         l = sum_halves(l);
+        float unit = kSplit ? inverse_of_power(fit.f) : 1.0f;  // of O
         if (found) *bad = 1;
         __syncthreads();
         const bool repair = *bad != 0;

@@ -115,6 +115,56 @@ __device__ inline float sum_halves(float x) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// The largest magnitude of an accumulator's column (NaN does not count).
+__device__ inline float largest(const f32x16& x) {
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, __builtin_fabsf(x[i]));
+    return max_halves(most);
+}
+
+__device__ inline f32x16 times(const f32x16& x, float f) {
+    f32x16 y;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = x[i] * f;
+    return y;
+}
+
+// A column's power of two, 2^kMost at first, for weights that become FP16 operands.
+template <int kMost>
+struct Fit {
+    static constexpr int kMostBits = 127 + kMost;
+    float f = __builtin_bit_cast(float, (unsigned)kMostBits << 23);
+
+    // So that |x| f stays below 2^15 for the column's x, of magnitudes up to `most`; what is
+    // summed so far is rescaled where f changes.
+    template <int N>
+    __device__ inline void fit(float most, f32x16 (&sum)[N]) {
+        const bool over = most * f > 0x1p15f;
+        if (__any(over)) {
+            // 2^10 <= most f < 2^11
+            const int e = (int)(__float_as_uint(most) >> 23);
+            const float to =
+                over ? __uint_as_float((unsigned)max(min(264 - e, kMostBits), 1) << 23) : f;
+            const float by = to / f;
+#pragma unroll
+            for (int d = 0; d < N; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[d][i] *= by;
+            f = to;
+        }
+    }
+
+    // The x so far have been made smaller by 2^-fall (fall >= 0): f may rise by as much.
+    // Returns log2 of what it rose by.
+    __device__ inline float rise(float fall) {
+        const int room = kMostBits - (int)(__float_as_uint(f) >> 23);
+        const int by = min((int)fminf(fall, 300.0f), room);
+        f = __uint_as_float(__float_as_uint(f) + ((unsigned)by << 23));
+        return (float)by;
+    }
+};
+
 // Address of LDS as the instructions take it.
 __device__ inline uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;

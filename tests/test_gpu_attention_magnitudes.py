@@ -1,0 +1,93 @@
+"""Attention in FP32 on values of very different magnitudes, against the formulas in 64 bits
+(attention_plain.py): what a row does not see, or weighs next to nothing, takes no bits from
+what it does."""
+import pytest
+import torch
+
+import paper_2308_15152_amd as emu
+from test_gpu_attention_backward import check as check_gradient
+from test_gpu_attention_backward import gradient_of, gradients
+from test_gpu_attention_forward import DEV, check, dev, inputs
+
+pytestmark = pytest.mark.gpu
+F32 = torch.float32
+
+
+@pytest.mark.parametrize("size", [64, 128])
+@pytest.mark.parametrize("by", [2.0 ** 20, 2.0 ** 40, 2.0 ** 100])
+@pytest.mark.parametrize("b,t,n,h,at", [
+    (1, 500, 500, 2, 40), (1, 500, 500, 2, 0), (1, 700, 700, 2, 333), (40, 300, 300, 8, 65),
+    (1, 40, 4000, 2, 3990), (1, 200, 3000, 1, 2900)])
+def test_a_large_value(b, t, n, h, at, by, size):
+    """Rows before it give what they give without it, bit for bit."""
+    x = inputs(b, t, n, h, h // 2 or 1, size, F32, seed=t)
+    want, lses = emu.attention_emu_forward(*dev(*x))
+    x[2][0, at] *= by
+    o, lse = emu.attention_emu_forward(*dev(*x))
+    seen = max(at - (n - t), 0)  # the first row that sees it
+    assert torch.equal(o[0, :seen], want[0, :seen]) and torch.equal(o[1:], want[1:])
+    assert torch.equal(lse, lses)
+    check([y[:1] for y in x], (o[:1], lse[:1]))
+
+
+def test_a_large_value_in_packed_sequences():
+    bounds = [0, 300, 301, 420, 600]
+    x = inputs(1, 600, 600, 4, 2, 64, F32, seed=1)
+    for at in (100, 310, 599):
+        x[2][0, at] *= 2.0 ** 30
+    cu = torch.tensor(bounds, dtype=torch.int32, device=DEV)
+    do = gradient_of(x)
+    check(x, emu.attention_emu_forward(*dev(*x), cu_seqlens=cu), True, None, bounds)
+    check_gradient(x, do, gradients(x, do, cu_seqlens=cu), True, None, bounds)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("score,by", [(-20.0, 2.0 ** 20), (-30.0, 2.0 ** 40), (-200.0, 2.0 ** 60)])
+@pytest.mark.parametrize("at", [0, 70, 450])
+def test_a_large_value_of_little_weight(at, score, by, causal):
+    """All rows see it with a weight of about e^score: before the keys that count, among them
+    and behind them."""
+    t = 500
+    x = inputs(1, t, t, 2, 1, 64, F32, seed=at)
+    x[0][..., 0] = 8.0  # the scale is 1 / 8
+    x[1][..., 0] = 0.0
+    x[1][:, at, :, 1:] = 0.0
+    x[1][:, at, :, 0] = score
+    x[2][:, at] *= by
+    do = gradient_of(x)
+    check(x, emu.attention_emu_forward(*dev(*x), causal=causal), causal)
+    check_gradient(x, do, gradients(x, do, causal), causal)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_large_values_before_rising_scores(causal):
+    """Every tile's weights make those before it small, whose values are larger by as much or
+    by less."""
+    t = 600
+    x = inputs(1, t, t, 2, 1, 64, F32, seed=2)
+    ramp = torch.arange(t, dtype=F32) // 32
+    x[0][..., 0] = 8.0
+    for per_tile, fall in ((20.0, 20.0), (40.0, 3.0), (12.0, 24.0)):
+        x[1][..., 0] = per_tile * 0.693147 * ramp[:, None]
+        y = x[0], x[1], x[2] * (2.0 ** (100 - fall * ramp).clamp(min=-100))[:, None, None]
+        check(y, emu.attention_emu_forward(*dev(*y), causal=causal), causal)
+
+
+@pytest.mark.parametrize("first", [-20, 20])
+@pytest.mark.parametrize("seed", range(4))
+def test_rows_of_every_magnitude(first, seed):
+    """Every row of v and do, and of q against a common k, has a magnitude of its own; the first
+    16 of v are the smallest, or the largest."""
+    t = 500
+    q, k, v = inputs(1, t, t, 4, 2, 64, F32, seed=seed)
+    g = torch.Generator().manual_seed(seed)
+
+    def by(low, high):
+        return 2.0 ** torch.randint(low, high, (1, t, 1, 1), generator=g)
+
+    of_v = by(-20, 20)
+    of_v[:, :16] = 2.0 ** first
+    x = q * by(-20, 1), k, v * of_v
+    do = gradient_of(x, seed) * by(-20, 20)
+    check(x, emu.attention_emu_forward(*dev(*x)))
+    check_gradient(x, do, gradients(x, do))
