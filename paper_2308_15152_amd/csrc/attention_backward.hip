@@ -153,7 +153,9 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         q_factor = args.q_factors[in_all * a.q_heads + h];
         do_factor = args.do_factors[in_all * a.q_heads + h];
     }
-    const float c = a.scale * kLog2e * q_factor;
+    // (factors multiply a product at once: one alone may take it past FP32's range)
+    const float c = kSplit ? 1.0f : a.scale * kLog2e;
+    const float of_scores = a.scale * kLog2e * q_factor;
     const int shift = sk.count - sq.count + 1;
     const auto seen = [&](int r) {
         return a.causal ? min(max(min(r, last_row) / group + shift, 0), sk.count) : sk.count;
@@ -164,7 +166,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
     f32x16 dQ[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dQ[dt] = f32x16{};
-    Fit<100> fit;
+    Fit fit;
     // (what is not loaded multiplies zeros and has to be finite)
     clear_lds(lds, 4 * kTileBytes, thread, kThreads);
     lds_barrier();
@@ -232,8 +234,8 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     by[i + j] = x[j];
-                    S[i + j] *= x[j];
-                    dP[i + j] = __builtin_fmaf(dP[i + j] * y[j], do_factor, -delta);
+                    S[i + j] *= x[j] * of_scores;
+                    dP[i + j] = __builtin_fmaf(dP[i + j], y[j] * do_factor, -delta);
                 }
             }
         }
@@ -301,7 +303,9 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
     }
     pass(Number<0>{});
     if (valid && half == 0 && group_of == 0) args.delta[in_all * a.q_heads + h] = delta;
-    const float f = kNarrow<T> ? a.scale / fit.f : a.scale;
+    const float f = kNarrow<T> ? inverse_of_power(fit.f) : 1.0f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) dQ[dt] = times(dQ[dt], a.scale);
     if constexpr (kGroups == 2) {
         typedef Pack<float, 4>::type Four;
         Four* const sums = reinterpret_cast<Four*>(lds_all) + wave * (D / 8 * 64) + lane;
@@ -468,7 +472,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     f32x16 dK[D / 32], dV[D / 32];
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) dK[dt] = f32x16{}, dV[dt] = f32x16{};
-    Fit<100> fit, fit_v;
+    Fit fit, fit_v;
     // (what is not loaded multiplies zeros and has to be finite)
     clear_lds(lds, 4 * kTileBytes, thread, kThreads);
     lds_barrier();
@@ -538,7 +542,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
         }
     };
     if (t0 < count) load(count - 1);
-    const float c = a.scale * kLog2e * k_factor;
+    const float c = kSplit ? 1.0f : a.scale * kLog2e;
+    const float of_scores = a.scale * kLog2e * k_factor;
     // from the last rows, which all blocks of a head have, so that those that run beside each
     // other find them in the caches
     for (int t = count - 1; t >= t0; --t) {
@@ -600,8 +605,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
                 const auto x = per_row(rw.q, i), y = per_row(rw.d_o, i), z = per_row(rw.delta, i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    P[i + j] *= x[j];
-                    dP[i + j] = __builtin_fmaf(dP[i + j] * y[j], v_factor, z[j]);
+                    P[i + j] *= x[j] * of_scores;
+                    dP[i + j] = __builtin_fmaf(dP[i + j], y[j] * v_factor, z[j]);
                 }
             }
         }
@@ -700,7 +705,9 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
     float* const dk_part = args.parts ? dv_part + args.key_rows * kPartStride<D> : nullptr;
     join(dV, kSplit ? kBack / fit_v.f : kBack,
          row_of<Out<T>>(a.dv, packed, n, sk, head) + key_in * a.dv.token, dv_part);
-    join(dK, kNarrow<T> ? a.scale * kBack / fit.f : a.scale,
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) dK[dt] = times(dK[dt], a.scale);
+    join(dK, kNarrow<T> ? kBack / fit.f : 1.0f,
          row_of<Out<T>>(a.dk, packed, n, sk, head) + key_in * a.dk.token, dk_part);
 }
 

@@ -80,7 +80,10 @@ struct Attend {
                 Q[kb] = load_operand<T, D, kVec>(p, 2 * kb + half, size, row < rows);
             }
         }
-        if constexpr (kSplit) c *= factors.q(min(row, last_row));
+        // (split scores come in units of c s: what q and k have been divided by multiplies them at
+        // once, for one alone may take a product past FP32's range)
+        float of_scores = 1.0f;
+        if constexpr (kSplit) of_scores = c * factors.q(min(row, last_row)), c = 1.0f;
         // keys seen by the lane's row, by the wave's first and last one, by the block's
         const auto seen = [&](int r) { return min(max(limit(min(r, last_row)), first), end); };
         const int lim = seen(row), lim_min = seen(wave_row), lim_max = seen(wave_row + 31);
@@ -98,7 +101,7 @@ struct Attend {
         // split values: a weight times its value's factor becomes an operand, for which each row
         // has a power of two by what it weighs itself: by the largest factor of a tile's values,
         // one that a row does not see, or hardly weighs, took the bits of all others
-        Fit<126> fit;
+        Fit fit;
         bool found = false;
         if (kVecTile && width < kWidth<D>) {
             clear_lds(lds, kTiles, threadIdx.x, kThreads);
@@ -213,7 +216,7 @@ struct Attend {
                     for (int i = 0; i < 16; i += 4) {
                         const auto x = four_of(of_tile, s, i);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j];
+                        for (int j = 0; j < 4; ++j) S[s][i + j] *= x[j] * of_scores;
                     }
             }
             if (key0 + kKeys > lim_min) {

@@ -130,11 +130,10 @@ __device__ inline f32x16 times(const f32x16& x, float f) {
     return y;
 }
 
-// A column's power of two, 2^kMost at first, for weights that become FP16 operands.
-template <int kMost>
+// A column's power of two, for weights that become FP16 operands.
 struct Fit {
-    static constexpr int kMostBits = 127 + kMost;
-    float f = __builtin_bit_cast(float, (unsigned)kMostBits << 23);
+    static constexpr int kMostBits = 127 + 126;  // so that its inverse is normal, too
+    float f = 0x1p126f;
 
     // So that |x| f stays below 2^15 for the column's x, of magnitudes up to `most`; what is
     // summed so far is rescaled where f changes.

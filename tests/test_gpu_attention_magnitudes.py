@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2308_15152_amd as emu
+from attention_plain import attention
 from test_gpu_attention_backward import check as check_gradient
 from test_gpu_attention_backward import gradient_of, gradients
 from test_gpu_attention_forward import DEV, check, dev, inputs
@@ -91,3 +92,34 @@ def test_rows_of_every_magnitude(first, seed):
     do = gradient_of(x, seed) * by(-20, 20)
     check(x, emu.attention_emu_forward(*dev(*x)))
     check_gradient(x, do, gradients(x, do))
+
+
+@pytest.mark.parametrize("size", [64, 128])
+@pytest.mark.parametrize("t", [200, 500])
+@pytest.mark.parametrize("q_by,k_by,v_by,do_by", [
+    (2.0 ** -110, 2.0 ** 110, 1.0, 1.0), (2.0 ** 110, 2.0 ** -110, 1.0, 1.0),
+    (1.0, 1.0, 2.0 ** 110, 2.0 ** -100), (1.0, 1.0, 2.0 ** -100, 2.0 ** 110),
+    (1.0, 1.0, 2.0 ** -100, 2.0 ** -10), (1.0, 1.0, 2.0 ** -10, 2.0 ** -100)])
+def test_magnitudes_near_the_ends(t, q_by, k_by, v_by, do_by, size):
+    """No product on the way to a result that has a value in FP32 passes its range."""
+    q, k, v = inputs(1, t, t, 4, 2, size, F32, seed=t)
+    x = q * q_by, k * k_by, v * v_by
+    do = gradient_of(x) * do_by
+    for value, _ in attention(*(y[0] for y in x), do=do[0]).values():
+        assert value.abs().max() < 2.0 ** 127
+    check(x, emu.attention_emu_forward(*dev(*x)))
+    check_gradient(x, do, gradients(x, do))
+
+
+@pytest.mark.parametrize("t", [200, 500])
+@pytest.mark.parametrize("by", [2.0 ** 30, 2.0 ** -30])
+def test_scales_beside_magnitudes(t, by):
+    """Small and large factors of the scores, with rows of zeros among those of q and k."""
+    q, k, v = inputs(1, t, t, 4, 2, 64, F32, seed=t)
+    x = q * by, k, v
+    for y in x[:2]:
+        y[:, 17::50] = 0.0
+    do = gradient_of(x)
+    scale = 0.125 / by
+    check(x, emu.attention_emu_forward(*dev(*x), scale=scale), scale=scale)
+    check_gradient(x, do, gradients(x, do, scale=scale), scale=scale)
