@@ -1,10 +1,15 @@
 // One pass of softmax attention over a range of keys, for a block's query rows.
 //
 // Per row, with scores s_j = q k_j (unscaled) and c = scale log2 e > 0, the pass keeps a
-// reference z (in units of c s), l = sum_j 2^(c s_j - z) and O = sum_j 2^(c s_j - z) v_j,
-// all in FP32.  z only moves, and O and l with it, where a row's largest score is more
-// than 2^kSlack above it: the weights then stay below 2^(kSlack + kBias) and the
-// result does not depend on z.
+// score m, its reference z = c m - kBias, l = sum_j 2^(c s_j - z) and O = sum_j 2^(c s_j - z) v_j,
+// all in FP32.  They only move where a row's largest score is more than 2^kSlack above m: the
+// weights then stay below 2^(kSlack + kBias) and the result does not depend on m.
+//
+// z is rounded, and all weights of a row are off by that: below |z| = kCoarse by 2^(1/8) at most.
+// From there on the last bit of z comes to be no longer small beside one, and weights would pass
+// FP16's range, or be zeros for all keys.  Such a row's weights are 2^(c (s_j - m) + kBias), with
+// a difference that is exact near the largest score.  That has to be where m moves: a branch of its
+// own between the scores and the products takes 4 x 4096 tokens from 573 to 620 us.
 //
 // The products are S^T = K Q^T and O^T = V^T P^T in 32 x 32 tiles: a lane holds
 // one query row, so that its reference, sum and rescaling are scalars of the lane, and
@@ -48,6 +53,7 @@ struct Attend {
     // FP16 weights keep 11 bits down to 2^-14: 2^-21 of a row's largest
     static constexpr float kBias = __is_same(E, f16_t) ? 7.0f : 0.0f;
     static constexpr float kSlack = 8.0f;
+    static constexpr float kCoarse = 0x1p22f;
 
     // rows: query rows there are; the block takes row0 to row0 + kRows - 1.
     // q_row(r): its elements; limit(r): how many keys it sees (not decreasing in r).
@@ -97,7 +103,13 @@ struct Attend {
         f32x16 O[D / 32];
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) O[dt] = f32x16{};
-        float l = 0.0f, z = kLeast;
+        float l = 0.0f, m = -__builtin_inff();
+        // z; -kBias of a coarse row, whose scores are taken less m
+        float less = kLeast;
+        bool coarse = false;
+        const auto reference = [&](float m) {
+            return m > -__builtin_inff() ? __builtin_fmaf(m, c, -kBias) : kLeast;
+        };
         // split values: a weight times its value's factor becomes an operand, for which each row
         // has a power of two by what it weighs itself: by the largest factor of a tile's values,
         // one that a row does not see, or hardly weighs, took the bits of all others
@@ -231,24 +243,33 @@ struct Attend {
             for (int s = 0; s < kKeys / 32; ++s)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, S[s][i]);
-            const float want = max_halves(top) * c - kBias;
-            if (__any(want > z + kSlack)) {
-                const float to = want > z + kSlack ? want : z;
-                const float f = __builtin_amdgcn_exp2f(z - to);
-                const float of_sum =
-                    kSplit ? __builtin_amdgcn_exp2f(z - to + fit.rise(to - z)) : f;
+            top = max_halves(top);
+            if (__any(__builtin_fmaf(top, c, -kBias) > less + kSlack || coarse)) {
+                const bool moves = (top - m) * c > kSlack;  // (z + kSlack may be z)
+                const float z = reference(m), to = moves ? reference(top) : z;
+                coarse = __builtin_fabsf(to) >= kCoarse && __builtin_fabsf(to) < -kLeast;
+                const float fall = moves ? (coarse ? (top - m) * c : to - z) : 0.0f;
+                m = moves ? top : m;
+                less = coarse ? -kBias : to;
+                const float f = __builtin_amdgcn_exp2f(-fall);
+                const float of_sum = kSplit ? __builtin_amdgcn_exp2f(fit.rise(fall) - fall) : f;
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) O[dt][i] *= of_sum;
                 l *= f;
-                z = to;
+                // (s_j - m: one more product, of ones and -m)
+                const float by = coarse ? -m : 0.0f;
+#pragma unroll
+                for (int s = 0; s < kKeys / 32; ++s)
+                    S[s] = __builtin_amdgcn_mfma_f32_32x32x2f32(half == 0 ? 1.0f : 0.0f, by, S[s], 0,
+                                                                0, 0);
             }
 #pragma unroll
             for (int s = 0; s < kKeys / 32; ++s) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    S[s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s][i], c, -z));
+                    S[s][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s][i], c, -less));
                     l += S[s][i];
                 }
             }
@@ -286,6 +307,7 @@ struct Attend {
             if (t + step < last) tile(t + step, Number<1>{});
         }
         l = sum_halves(l);
+        float z = reference(m);
         float unit = kSplit ? inverse_of_power(fit.f) : 1.0f;  // of O
         if (found) *bad = 1;
         __syncthreads();
