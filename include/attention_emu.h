@@ -70,7 +70,9 @@ int attention_emu_forward(const attention_emu_forward_t* a, hipStream_t stream);
  *   ds_ij = p_ij (do_i v_j - do_i o_i),  dq_i = scale sum_j ds_ij k_j,
  *   dk_j = scale sum_i ds_ij q_i,
  * sums over tokens and over a key head's query heads in FP32 in a fixed order; with 16-bit
- * types p and ds are rounded to the type before they multiply.  o and lse may be those of more
+ * types p and ds are rounded to the type before they multiply.  p is taken as one at most, for
+ * it is off by the last bit of lse, which is not small beside one where scores are of 2^20 and
+ * more.  o and lse may be those of more
  * keys than are given here (keys in parts: dq is the sum of the parts').  Gradients of
  * tokens that see no key and of keys that no token sees are zero.  Where q, k, v, o or d_o is
  * not finite, any gradient of its sequence's key head may not be; other sequences and

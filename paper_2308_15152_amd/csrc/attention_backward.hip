@@ -57,6 +57,10 @@ __device__ inline __attribute__((always_inline)) void schedule_steps(F f) {
     }
 }
 
+// From |z| = kCoarse on a weight p = 2^(c s - z) may be off by factors, for z's last bit comes to be
+// no longer small beside one: it is taken as one at most there, and NaN stays.
+constexpr float kCoarse = 0x1p16f;
+
 constexpr int kDqWaves = 4;
 constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
@@ -147,6 +151,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         const float lse = row_of<float>(a.lse, packed, n, sq, h)[token * a.lse.token];
         if (lse != -__builtin_inff()) z = lse * kLog2e;
     }
+    const bool coarse = __builtin_fabsf(z) >= kCoarse, any_coarse = __any(coarse && valid);
     // what the row's q and do have been divided by
     float q_factor = 1.0f, do_factor = 1.0f;
     if constexpr (kSplit) {
@@ -240,15 +245,18 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
             }
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            S[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i], c, -z));
-            dP[i] *= S[i];
-        }
-        if (key0 + kDqKeys > lim_min) {
+        for (int i = 0; i < 16; ++i) S[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i], c, -z));
+        // (for all weights, where they are formed, the one takes 1.5% of the time)
+        if (key0 + kDqKeys > lim_min || any_coarse) {
+            const float most = coarse ? 1.0f : __builtin_inff();
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 16; ++i) {
+                S[i] = __builtin_elementwise_minimum(S[i], most);
                 if (key0 + acc_row(i, half) >= lim) S[i] = dP[i] = 0.0f;
+            }
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dP[i] *= S[i];
         if constexpr (kSplit) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) dP[i] *= by[i];
@@ -616,9 +624,9 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kWaves / 4) void attention_
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float log = __builtin_fmaf(P[i + j], c, -x[j]);
-                // (scores of 2^24 and more have rounding errors that take p past one;
-                // NaN stays)
-                if constexpr (kNarrow<T> && !kSplit) log = __builtin_elementwise_minimum(log, kShift);
+                // (for all: FP16 has no room for more than one, and a branch in its own right takes
+                // 2 x 1024 tokens in FP32 from 304 to 384 us, by the registers it needs)
+                log = __builtin_elementwise_minimum(log, kShift);
                 P[i + j] = __builtin_amdgcn_exp2f(log);
             }
         }

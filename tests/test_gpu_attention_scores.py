@@ -7,6 +7,7 @@ import torch
 
 import paper_2308_15152_amd as emu
 from attention_plain import attention, near
+from test_gpu_attention_backward import gradient_of
 from test_gpu_attention_forward import DEV, TYPES, dev, inputs
 
 pytestmark = pytest.mark.gpu
@@ -78,3 +79,37 @@ def test_step(dtype, power, prefix, t):
                                scale=scale)
     for i, m in enumerate(lengths.tolist()):
         in_the_values_range(o[i], torch.cat([pv[0], v[i, :m]]), prefix + m, t, 2, True, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("power", [20, 24, 28, 30, 34])
+@pytest.mark.parametrize("t,n,hq,hk,size", [
+    (90, 90, 4, 2, 64), (400, 400, 4, 2, 64), (300, 900, 2, 1, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradient(dtype, power, t, n, hq, hk, size, causal):
+    """Weights of at most one: |dv| <= sum |do|, |ds| <= |do| |v| + |do| |o|, all over what may
+    see each other, and 1% for roundings."""
+    (q, k, v), scale = of_size(t, n, hq, hk, size, dtype, power, seed=power)
+    x = q, k, v * 2.0 ** -8
+    do = gradient_of(x, size=2.0 ** -8)
+    if dtype == torch.float16:  # (which has to hold the gradients, up to scale |do| |v| |k|)
+        do = do * 2.0 ** -max(power - 22, 0)
+    on = dev(*x)
+    o, lse = emu.attention_emu_forward(*on, causal=causal, scale=scale)
+    got = [y[0].cpu().double() for y in
+           emu.attention_emu_backward(*on, o, lse, do.to(DEV), causal=causal, scale=scale)]
+    q, k, v, o, do = (y[0].cpu().double().abs().movedim(1, 0) for y in (*x, o, do))
+    kk, vv = k.repeat_interleave(hq // hk, 0), v.repeat_interleave(hq // hk, 0)
+    seen = torch.ones(t, n, dtype=torch.float64)
+    if causal:
+        seen = seen.tril(n - t)
+    ds = seen * (do @ vv.mT + (do * o).sum(-1, keepdim=True))
+
+    def fold(y):
+        return y.unflatten(0, (hk, -1)).sum(1)
+
+    most = scale * ds @ kk, fold(scale * ds.mT @ q), fold(seen.mT @ do)
+    for name, y, z in zip(("dq", "dk", "dv"), got, most):
+        assert z.max() < torch.finfo(dtype).max, name
+        assert torch.isfinite(y).all(), name
+        assert (y.movedim(1, 0).abs() <= 1.01 * z + torch.finfo(dtype).tiny).all(), name
