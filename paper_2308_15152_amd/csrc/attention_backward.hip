@@ -65,8 +65,12 @@ constexpr int kDqWaves = 4;
 constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
 constexpr int kFewKeys = 128;
-// A row's weights are all there if they sum to one but for FP32's roundings.
+// A row's weights are taken to be all there if they sum to one up to this, and if the sum of ds is
+// no more than o's roundings explain (half a step by its own, about as much by the weights that
+// made it): keys that are elsewhere may weigh next to nothing and still make up all of delta.
 constexpr float kWhole = 0x1p-12f;
+template <class T>
+constexpr float kStep = __is_same(T, bf16_t) ? 0x1p-7f : 0x1p-10f;
 // Below so many blocks (two for each CU) two groups of waves share a block's keys: the gradient with
 // 384 blocks of 2048 keys takes 192 us for 203, that of 16 packed sequences, 2500 tokens in all, 112
 // for 127; with 512 blocks it would take 3 us more than without.
@@ -124,7 +128,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
     const bool valid = row < rows;
     const int64_t in_all = (packed ? sq.first : (int64_t)n * a.tokens) + token;
     Operand<T> Q[kBlocks], DO[kBlocks];
-    float delta = 0.0f;
+    float delta = 0.0f, of_delta = 0.0f;  // and the sum of its terms' magnitudes
     {
         const E* q = row_of<E>(args.q, packed, n, sq, h) + token * args.q.token;
         const E* x = row_of<E>(args.d_o, packed, n, sq, h) + token * args.d_o.token;
@@ -140,10 +144,14 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
             const Frag<Out<T>> x = load_chunk<Out<T>, kVec>(o, 2 * kb + half, a.size, valid);
             const Frag<Out<T>> y = load_chunk<Out<T>, kVec>(d, 2 * kb + half, a.size, valid);
 #pragma unroll
-            for (int j = 0; j < kPer<Out<T>>; ++j)
-                delta = __builtin_fmaf(to_f32(x[j]), to_f32(y[j]), delta);
+            for (int j = 0; j < kPer<Out<T>>; ++j) {
+                const float term = to_f32(x[j]) * to_f32(y[j]);
+                delta += term;
+                of_delta += __builtin_fabsf(term);
+            }
         }
         delta = sum_halves(delta);
+        of_delta = sum_halves(of_delta);
     }
     // (rows that see nothing have lse -infinity)
     float z = __builtin_inff();
@@ -295,7 +303,9 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
                 weight = sums[0][0][at] + sums[1][0][at];
                 rest = sums[0][1][at] + sums[1][1][at];
             }
-            if (__builtin_fabsf(weight - 1.0f) < kWhole) delta += rest;
+            if (__builtin_fabsf(weight - 1.0f) < kWhole &&
+                __builtin_fabsf(rest) <= kStep<E> * of_delta)
+                delta += rest;
             // (the places are free for the next pass)
             __syncthreads();
         }

@@ -1,11 +1,13 @@
-"""Attention in FP32 on values of very different magnitudes, against the formulas in 64 bits
-(attention_plain.py): what a row does not see, or weighs next to nothing, takes no bits from
-what it does."""
+"""Attention on values of very different magnitudes, in FP32 but for the last test, against the
+formulas in 64 bits (attention_plain.py): what a row does not see, or weighs next to nothing, takes
+no bits from what it does."""
+import math
+
 import pytest
 import torch
 
 import paper_2308_15152_amd as emu
-from attention_plain import attention
+from attention_plain import attention, least, near
 from test_gpu_attention_backward import check as check_gradient
 from test_gpu_attention_backward import gradient_of, gradients
 from test_gpu_attention_forward import DEV, check, dev, inputs
@@ -123,3 +125,49 @@ def test_scales_beside_magnitudes(t, by):
     scale = 0.125 / by
     check(x, emu.attention_emu_forward(*dev(*x), scale=scale), scale=scale)
     check_gradient(x, do, gradients(x, do, scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, F32])
+@pytest.mark.parametrize("n,cut", [(100, 80), (600, 500), (1500, 1400)])
+@pytest.mark.parametrize("score,by", [(-6.5, 2.0 ** 8), (-9.0, 2.0 ** 12), (-9.5, 2.0 ** 6),
+                                      (-9.5, 2.0 ** 13)])
+def test_keys_elsewhere_that_matter_little_but_for_their_values(dtype, n, cut, score, by):
+    """o and lse of all keys, the gradient over some: the others have a weight in all of about
+    e^score, and values so large that delta is theirs as well.  delta is off by the rounding
+    of o, half a step, and by what the kernel takes for that, two at most."""
+    t, size = 150, 64
+    q, k, v = inputs(1, t, n, 2, 1, size, F32, seed=n, spread=1.0)
+    q[..., 0], k[..., 0] = 8.0, 0.0  # the scale is 1 / 8
+    k[:, cut:, :, 1:] = 0.0
+    k[:, cut:, :, 0] = score + math.log(cut / (n - cut))
+    v[:, cut:] *= by
+    q, k, v = (y.to(dtype) for y in (q, k, v))
+    do = gradient_of((q, k, v)).to(dtype)
+    scale = size ** -0.5
+    Q, K, V, D = (y[0].double().movedim(1, 0) for y in (q, k, v, do))
+    s = scale * Q @ K.mT
+    lse = torch.logsumexp(s, -1)
+    p = (s - lse[..., None]).exp()
+    o = p @ V
+    on = dev(q, k[:, :cut], v[:, :cut], o.movedim(0, 1)[None].to(dtype),
+             lse.mT[None].float().contiguous(), do)
+    got = emu.attention_emu_backward(*on, causal=False)
+    g, mean = D @ V.mT, (D * o).sum(-1, keepdim=True)
+    e, r = 2.0 ** -24, torch.finfo(dtype).eps / 2
+    u = r if dtype != F32 else 0.0
+    of_mean = (D * o).abs().sum(-1, keepdim=True)
+    b = scale * Q.abs() @ K.abs().mT
+    w = ((size + 8) * e * b.amax(-1) + (n + 64) * e + e * lse.abs())[..., None]
+    ds = p * (g - mean)
+    off = p * (2 * w * (D.abs() @ V.abs().mT + of_mean) + (3 * r + (size + 4) * e) * of_mean)
+    off = off + u * ds.abs() + n * e * ds.abs() + e * ds.abs().amax(-1, keepdim=True)
+    off_k = off + e * ds.abs().amax(-2, keepdim=True)
+    ds, off, off_k, K = ds[..., :cut], off[..., :cut], off_k[..., :cut], K[:, :cut]
+    near(got[0][0].movedim(1, 0), bounded(scale * ds @ K, scale * off @ K.abs(), dtype), "dq")
+    near(got[1][0, :, 0], bounded((scale * ds.mT @ Q).sum(0), (scale * off_k.mT @ Q.abs()).sum(0),
+                                  dtype), "dk")
+
+
+def bounded(value, bound, dtype):
+    """With the result's own rounding."""
+    return value, bound + torch.finfo(dtype).eps / 2 * value.abs() + least(dtype)
