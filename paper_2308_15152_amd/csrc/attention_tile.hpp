@@ -396,7 +396,7 @@ struct Flow {
                     asm volatile(
                         "s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off[i]),
                         "s"(first), "s"(at + i * kThreads * 16)
-                        : "memory");
+                        : "m0", "memory");
             } else {
                 f[i] = load_chunk<T, false>(
                     reinterpret_cast<const T*>(reinterpret_cast<const char*>(first) + off[i]), c, size,
