@@ -66,8 +66,9 @@ constexpr int kDqRows = 32 * kDqWaves;
 constexpr int kDqKeys = 32;
 constexpr int kFewKeys = 128;
 // A row's weights are taken to be all there if they sum to one up to this, and if the sum of ds is
-// no more than o's roundings explain (half a step by its own, about as much by the weights that
-// made it): keys that are elsewhere may weigh next to nothing and still make up all of delta.
+// no more than a step of what o's roundings explain, of itself and of the weights that made it, by
+// half a step each: keys that are elsewhere may weigh next to nothing and still make up all
+// of delta.  (|ds| is summed by pairs of keys, which takes half as long: 0.4% of the time.)
 constexpr float kWhole = 0x1p-12f;
 template <class T>
 constexpr float kStep = __is_same(T, bf16_t) ? 0x1p-7f : 0x1p-10f;
@@ -211,7 +212,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         }
     };
     const typename KV::Read read(lds, lane);
-    float weight = 0.0f, rest = 0.0f;  // sums of the row's p and ds
+    float weight = 0.0f, rest = 0.0f, size_of_rest = 0.0f;  // sums of the row's p, ds and |ds|
     // one tile, in the first or the second place
     const auto step = [&](int t, auto odd, auto only_rest) __attribute__((always_inline)) {
         constexpr int k_at = decltype(odd)::value * 2 * kTileBytes, v_at = k_at + kTileBytes;
@@ -270,7 +271,12 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
             for (int i = 0; i < 16; ++i) dP[i] *= by[i];
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) weight += S[i], rest += dP[i];
+            for (int i = 0; i < 16; ++i) weight += S[i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float two = dP[i] + dP[i + 8];
+                rest += two, size_of_rest += __builtin_fabsf(two);
+            }
         }
         if constexpr (decltype(only_rest)::value != 0) return;
         if constexpr (kNarrow<T>) {
@@ -286,7 +292,7 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         }
     };
     const auto pass = [&](auto only_rest) __attribute__((always_inline)) {
-        weight = rest = 0.0f;
+        weight = rest = size_of_rest = 0.0f;
         if (group_of < count) load(group_of);
         for (int t = group_of; t < count + group_of; t += 2 * kGroups) {
             step(t, Number<0>{}, only_rest);
@@ -295,16 +301,23 @@ attention_dq_kernel(BackwardArgs args, int first_block) {
         if constexpr (!kSplit) {
             weight = sum_halves(weight);
             rest = sum_halves(rest);
+            size_of_rest = sum_halves(size_of_rest);
             if constexpr (kGroups == 2) {
-                __shared__ float sums[2][2][kDqRows];
+                __shared__ float sums[2][3][kDqRows];
                 const int at = 32 * wave + (lane & 31);
-                if (half == 0) sums[group_of][0][at] = weight, sums[group_of][1][at] = rest;
+                if (half == 0) {
+                    sums[group_of][0][at] = weight, sums[group_of][1][at] = rest;
+                    sums[group_of][2][at] = size_of_rest;
+                }
                 __syncthreads();
                 weight = sums[0][0][at] + sums[1][0][at];
                 rest = sums[0][1][at] + sums[1][1][at];
+                size_of_rest = sums[0][2][at] + sums[1][2][at];
             }
+            // (sum p |do v| <= sum |ds| + |delta|)
             if (__builtin_fabsf(weight - 1.0f) < kWhole &&
-                __builtin_fabsf(rest) <= kStep<E> * of_delta)
+                __builtin_fabsf(rest) <=
+                    kStep<E> * (of_delta + size_of_rest + __builtin_fabsf(delta)))
                 delta += rest;
             // (the places are free for the next pass)
             __syncthreads();

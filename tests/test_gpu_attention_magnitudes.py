@@ -1,4 +1,4 @@
-"""Attention on values of very different magnitudes, in FP32 but for the last test, against the
+"""Attention on values of very different magnitudes, in FP32 but for the last tests, against the
 formulas in 64 bits (attention_plain.py): what a row does not see, or weighs next to nothing, takes
 no bits from what it does."""
 import math
@@ -134,7 +134,8 @@ def test_scales_beside_magnitudes(t, by):
 def test_keys_elsewhere_that_matter_little_but_for_their_values(dtype, n, cut, score, by):
     """o and lse of all keys, the gradient over some: the others have a weight in all of about
     e^score, and values so large that delta is theirs as well.  delta is off by the rounding
-    of o, half a step, and by what the kernel takes for that, two at most."""
+    of o, half a step, and by what the kernel may take for that of o and of the weights that
+    made it: a step of sum |do o| + sum |ds| + |delta|, over the keys that are given."""
     t, size = 150, 64
     q, k, v = inputs(1, t, n, 2, 1, size, F32, seed=n, spread=1.0)
     q[..., 0], k[..., 0] = 8.0, 0.0  # the scale is 1 / 8
@@ -159,7 +160,9 @@ def test_keys_elsewhere_that_matter_little_but_for_their_values(dtype, n, cut, s
     b = scale * Q.abs() @ K.abs().mT
     w = ((size + 8) * e * b.amax(-1) + (n + 64) * e + e * lse.abs())[..., None]
     ds = p * (g - mean)
-    off = p * (2 * w * (D.abs() @ V.abs().mT + of_mean) + (3 * r + (size + 4) * e) * of_mean)
+    of_delta = (r + (size + 4) * e) * of_mean
+    of_delta = of_delta + 2 * r * (of_mean + ds[..., :cut].abs().sum(-1, keepdim=True) + mean.abs())
+    off = p * (2 * w * (D.abs() @ V.abs().mT + of_mean) + of_delta)
     off = off + u * ds.abs() + n * e * ds.abs() + e * ds.abs().amax(-1, keepdim=True)
     off_k = off + e * ds.abs().amax(-2, keepdim=True)
     ds, off, off_k, K = ds[..., :cut], off[..., :cut], off_k[..., :cut], K[:, :cut]
@@ -171,3 +174,15 @@ def test_keys_elsewhere_that_matter_little_but_for_their_values(dtype, n, cut, s
 def bounded(value, bound, dtype):
     """With the result's own rounding."""
     return value, bound + torch.finfo(dtype).eps / 2 * value.abs() + least(dtype)
+
+
+@pytest.mark.parametrize("size", [1, 2, 3])
+@pytest.mark.parametrize("seed", [26, 28, 43, 68])
+def test_heads_of_few_elements(seed, size):
+    """Where o is next to zero, delta's error is that of the weights that made it."""
+    lengths = [300, 38, 290, 444, 1]
+    bounds = [sum(lengths[:i]) for i in range(6)]
+    x = inputs(1, bounds[-1], bounds[-1], 2, 2, size, torch.bfloat16, seed=seed)
+    do = gradient_of(x, seed % 97)
+    cu = torch.tensor(bounds, dtype=torch.int32, device=DEV)
+    check_gradient(x, do, gradients(x, do, cu_seqlens=cu), True, None, bounds)
