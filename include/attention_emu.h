@@ -33,8 +33,9 @@ extern "C" {
  *     nothing outside the tensors is touched.  Rows of no sequence are not written.
  * A key or value that is not finite reaches only tokens that see it (as NaN, it may be, where the
  * formula says infinity).
- * Scores, statistics and sums are FP32.  With 16-bit types the weights e^{s_j - m} are
- * rounded to the type before they multiply v, the results once.  FP32 operands are taken as
+ * Scores, statistics and sums are FP32; weights below 2^-126 are zeros.  With 16-bit types the
+ * weights e^{s_j - m} are rounded to the type before they multiply v (FP16: to 2^-32 of the row's
+ * largest where they are small), the results once.  FP32 operands are taken as
  * two FP16 parts with a power of two for each row (22 bits of an element, down to 2^-39 of its
  * row's largest), and weights, times their value's power of two, in the same way with one for each
  * token (22 bits, down to 2^-34 of the largest such product that the token has), or both as they are

@@ -7,8 +7,8 @@
 // dp - delta in the accumulators of do v^T, which start at -delta.  Seven products of 2 D
 // operations a pair instead of the five that one pass with shared sums would take, for sums
 // whose order is fixed.  Bound by the matrix instructions and the reads of operands from LDS:
-// 2 x 4096 causal tokens, 16 heads of 128 in bfloat16, 520 us, of which dq 210 (980 TFLOP/s) and
-// dk and dv 314 (875).  With 16-byte chunks out of LDS permuted so that no two of a read meet on
+// 2 x 4096 causal tokens, 16 heads of 128 in bfloat16, 517 us (545 on another machine), of which dq
+// 205 (1005 TFLOP/s) and dk and dv 306 (898).  With 16-byte chunks out of LDS permuted so that no two of a read meet on
 // a bank, and addresses formed again for each tile instead of reloaded from scratch (a reload
 // waits for the tile's loads, too), dk and dv took 1340 -> 620; with keys and values, whose
 // registers did not suffice, partly in LDS, and two waves for each SIMD, 314.

@@ -1,9 +1,10 @@
 // Attention over whole sequences: one block per 32 kRowGroups query rows of a
 // key head (a token's query heads that share it are neighbouring rows, so that grouped heads read
 // a key once).  Bound by the matrix instructions and what keeps them from running at once: 4 x
-// 4096 causal tokens, 32 heads of 128 in bfloat16, 593 us (930 TFLOP/s of the 1270 of a large
-// product; 48% of the cycles have matrix instructions in flight, 45% vector ones), one prompt of
-// 32768 with 8 heads 2.12 ms (1040).  On that one, without the softmax's arithmetic 1880, without loads 1814.
+// 4096 causal tokens, 32 heads of 128 in bfloat16, 569 to 620 us on two machines (966 to 887 TFLOP/s
+// of the 1270 of a large product; 48% of the cycles have matrix instructions in flight, 46% vector
+// ones), one prompt of 32768 with 8 heads 2.08 to 2.22 ms (1056 to 990).  On that one, where it took
+// 2124, without the softmax's arithmetic 1880, without loads 1814.
 #include <algorithm>
 
 #include "attention_core.hpp"

@@ -1,7 +1,7 @@
 // FP32 rows as two FP16 planes and a power of two.  Bound by memory: 4 bytes an element are
 // read and 4 written (the row's padding, too): 9.4 us for the four inputs of a gradient of
 // 3 x 1001 tokens with 6 heads and 1234 keys with 2, of 80.  The products that they are for take a
-// third of FP16's rate instead of an eighth: that gradient 176 us for 910 with FP32 products.
+// third of FP16's rate instead of an eighth: that gradient 175 us for 910 with FP32 products.
 #include "attention_split.h"
 
 #include "attention_rows.hpp"
